@@ -26,7 +26,8 @@
  *     adloco_vector_param_sqnorm), adloco_outer_step and adloco_merge use none of it and may be issued on
  *     several streams at once -- the layers of one micro-batch only add into
  *     n and into their own S, and alternating them on two streams overlaps
- *     one kernel's tail with the next one's start.
+ *     one kernel's tail with the next one's start.  So may the operators between the
+ *     linear layers (adloco_add_rmsnorm to adloco_blockscale_matmul).
  *   - Sizes are int64_t element counts; all byte offsets are 64-bit inside.
  *   - There is no CPU fallback: without a usable CUDA device the calls fail
  *     with ADLOCO_ERR_CUDA.
@@ -335,6 +336,189 @@ int adloco_vector_param_sqnorm(adloco_ctx* ctx, const void* D, const void* X, in
 int adloco_embedding_sqnorm(adloco_ctx* ctx, const int32_t* token_ids, const void* D, int64_t B, int64_t T, int64_t d,
                             int64_t V, float* per_sample_sqnorm, int accumulate_norms, float* grad_sum,
                             int accumulate_sum, void* stream);
+
+/* ---- between the linear layers ------------------------------------------------ */
+
+/* The operators of a decoder block around its linear layers: norm, residual and dropout,
+ * rotary positions, and the linear layer in 8-bit floating point.  Their backward passes
+ * produce the X and Delta that the per-sample norms above read; the norm's own gain
+ * contributes its per-sample norms in the same pass.  None of them uses the ctx workspace, so
+ * all may be issued on several streams at once.  Rows are addressed by a pitch in elements;
+ * 16-byte aligned rows (base and pitch) take vector loads, others a slower element-wise path. */
+
+/* h = residual + drop(x);  y = gain * h / sqrt(mean(h^2) + eps) over each row of d elements.
+ *   x, y          dev [rows, d] in dtype
+ *   residual, h   dev [rows, d] in stream_dtype (BF16 or F32; F32 x with a BF16 stream is UNSUPPORTED).
+ *                 residual NULL: h = drop(x).  h may be NULL (not kept), or the same memory as residual.
+ *   gain          dev [d] in gain_dtype
+ *   rstd          dev [rows] float, receives 1 / sqrt(mean(h^2) + eps) for the backward pass; may be NULL
+ *   q, q_scale    y in 8 bits as adloco_blockscale_quantize writes it (from the unrounded y); both or
+ *                 neither.  q [rows, d] bytes with pitch q_stride (a multiple of 16, q 16-byte aligned),
+ *                 q_scale [rows, ceil(d / 128)] bytes with pitch q_scale_stride (a multiple of 4, q_scale 4-byte aligned)
+ *   y             may be NULL when q is given
+ *   dropout_p, seed, offset   as in adloco_dropout, element index row * d + column; 0 = none
+ * Sums, the root and the norm are formed in fp32 from the unrounded h; every output is rounded
+ * once.  1 <= d <= 16384. */
+typedef struct {
+    adloco_dtype dtype, stream_dtype, gain_dtype;
+    float eps;
+    int64_t rows, d;
+    const void* x;
+    int64_t x_stride;
+    const void* residual;
+    int64_t residual_stride;
+    const void* gain;
+    void* h;
+    int64_t h_stride;
+    void* y;
+    int64_t y_stride;
+    float* rstd;
+    void* q;
+    int64_t q_stride;
+    uint8_t* q_scale;
+    int64_t q_scale_stride;
+    double dropout_p;
+    uint64_t seed, offset;
+} adloco_rmsnorm_args;
+int adloco_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args* args, void* stream);
+
+/* Backward pass of adloco_add_rmsnorm over B samples of T rows (rows = B T, sample-major).
+ * With xhat = h rstd and m = mean(gain dy xhat) over the row:
+ *   dh = dh_residual + rstd (gain dy - xhat m)      gradient of h, hence of residual
+ *   dx = drop(dh)                                   gradient of x (the forward call's mask)
+ * and for the gain g_i = sum_t dy_{i,t} xhat_{i,t}:  n_i = ||g_i||^2,  S = sum_i g_i.
+ *   dy             dev [rows, d] in dtype;  h (the forward pass's), dh_residual, dh: in stream_dtype
+ *   dh_residual    the gradient that reaches h along the residual stream; NULL = 0; may be dh itself
+ *   dx             dev [rows, d] in dtype, may be NULL (without dropout dx equals dh)
+ *   per_sample_sqnorm, accumulate_norms, grad_sum, accumulate_sum   as in adloco_vector_param_sqnorm;
+ *                  both pointers may be NULL (a frozen gain)
+ *   workspace      dev, 16-byte aligned, at least adloco_add_rmsnorm_backward_workspace bytes; not
+ *                  needed (NULL) when neither norms nor sum are asked for.  One call at a time may use it.
+ * All sums are fp32 in a fixed order; only the addition of a sample's n_i to what other calls put
+ * there is an atomic. */
+typedef struct {
+    adloco_dtype dtype, stream_dtype, gain_dtype;
+    int32_t accumulate_norms, accumulate_sum, reserved;
+    int64_t B, T, d;
+    const void* dy;
+    int64_t dy_stride;
+    const void* h;
+    int64_t h_stride;
+    const float* rstd;
+    const void* gain;
+    const void* dh_residual;
+    int64_t dh_residual_stride;
+    void* dh;
+    int64_t dh_stride;
+    void* dx;
+    int64_t dx_stride;
+    double dropout_p;
+    uint64_t seed, offset;
+    float* per_sample_sqnorm;
+    float* grad_sum;
+    void* workspace;
+    int64_t workspace_bytes;
+} adloco_rmsnorm_backward_args;
+int64_t adloco_add_rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d);
+int adloco_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_args* args, void* stream);
+
+/* y = residual + drop(x) (residual NULL: y = drop(x)), the mask never stored: element e = row * cols + column
+ * stays when 16 bits drawn for it are at least r = round(p 65536), and is then multiplied by
+ * 65536 / (65536 - r).  The bits are those of the counter-based generator Philox-4x32-10 (Salmon,
+ * Moraes, Dror, Shaw 2011) with key = seed and counter = (e / 8, offset), word (e mod 8) / 2, low half
+ * first.  The same (p, seed, offset) gives the same mask in every call and in adloco_add_rmsnorm, so the
+ * backward pass of dropout is this call on the gradient.  A dropped element is exactly 0 whatever x holds
+ * there; p = 1 drops all.
+ *   x, residual, y   dev [rows, cols] in dtype, pitches in elements; y may be the same memory as x or residual
+ *   0 <= p <= 1 */
+int adloco_dropout(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride,
+                   const void* residual, int64_t residual_stride, void* y, int64_t y_stride, double p, uint64_t seed,
+                   uint64_t offset, void* stream);
+
+/* Frequencies of rotary positions for rot_dim (even) rotated elements a head: turns[j], j < rot_dim / 2, is
+ * w_j / (2 pi) in units of 2^-64, so that a position's phase is the low 64 bits of position * turns[j] --
+ * exact for any position, with no reduction of large angles.  HOST output.  w_j = base^(-2 j / rot_dim), then
+ *   NONE      as it is
+ *   LINEAR    w_j / factor                                       (positions squeezed)
+ *   NTK       base replaced by base factor^(rot_dim / (rot_dim - 2))   (the slowest pair slows by factor)
+ *   BY_PARTS  u w_j + (1 - u) w_j / factor with u = clamp((w_j context / (2 pi) - low) / (high - low), 0, 1):
+ *             pairs that turn more than `high` times within `context` positions keep their speed, pairs that
+ *             turn fewer than `low` times are squeezed
+ * base > 1 is not required, but base > 0, factor > 0, and for BY_PARTS high > low and context > 0. */
+enum { ADLOCO_ROPE_NONE = 0, ADLOCO_ROPE_LINEAR = 1, ADLOCO_ROPE_NTK = 2, ADLOCO_ROPE_BY_PARTS = 3 };
+int adloco_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double context, double low,
+                            double high, uint64_t* turns_host);
+
+/* One tensor of heads [B, T, heads, head_dim] with strides in elements (head_dim contiguous). */
+typedef struct {
+    const void* in;
+    void* out;         /* the same memory and strides as `in`, or no overlap */
+    int64_t heads;
+    int64_t in_batch, in_token, in_head;
+    int64_t out_batch, out_token, out_head;
+} adloco_rope_tensor;
+/* Rotates the first rot_dim elements of every head by the phase of its token's position and copies the rest:
+ *   (a, b) -> magnitude (a cos - b sin, a sin + b cos)
+ * over the pairs (x_j, x_{j + rot_dim / 2}) or, interleaved, (x_{2j}, x_{2j+1}).  inverse != 0 turns the other
+ * way, which is the backward pass (the rotation's transpose).
+ *   tensors     HOST array of 1..4 entries (queries and keys of different head counts go in one call)
+ *   turns_dev   dev copy of adloco_rope_frequencies' table
+ *   positions   dev int32 [B, T] with pitch positions_stride, or NULL: position first_position + t
+ * Phase arithmetic is exact, sine and cosine fp32, every output rounded once. */
+int adloco_rope(adloco_ctx* ctx, adloco_dtype dtype, const adloco_rope_tensor* tensors, int32_t n_tensors, int64_t B,
+                int64_t T, int64_t head_dim, int64_t rot_dim, const uint64_t* turns_dev, float magnitude,
+                const int32_t* positions, int64_t positions_stride, int64_t first_position, int interleaved, int inverse,
+                void* stream);
+
+/* ---- 8-bit floating point with a scale for each block of 128 --------------------- */
+
+/* Values are e4m3 (largest 448); a block's scale is the power of two 2^(s - 127), s its byte, the smallest for
+ * which the block's largest magnitude is at most 448 (a block of zeros has scale 1).  Multiplying by it is exact,
+ * so the only rounding is the one to e4m3 (to nearest, ties to even).  A block that holds an Inf or NaN gets
+ * s = 255, which stands for NaN: every product with it is NaN.
+ *
+ * Rows (activations and gradients): one scale for 128 consecutive elements of a row.
+ *   x      dev [rows, cols] in dtype, pitch x_stride
+ *   q      dev [rows, cols] bytes, pitch q_stride a multiple of 16, 16-byte aligned
+ *   scale  dev [rows, ceil(cols / 128)] bytes, pitch scale_stride a multiple of 4, 4-byte aligned */
+int adloco_blockscale_quantize(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t cols, const void* x,
+                               int64_t x_stride, void* q, int64_t q_stride, uint8_t* scale, int64_t scale_stride,
+                               void* stream);
+/* Weights: one scale for each 128 x 128 block of W [rows, cols]; optionally the transposed copy too, which the
+ * backward pass multiplies by (its scales are the same ones, transposed).
+ *   q      dev [rows, cols] bytes, pitch q_stride;  q_t  dev [cols, rows] bytes, pitch q_t_stride, may be NULL
+ *   scale  dev [ceil(rows / 128), ceil(cols / 128)] bytes, pitch scale_stride (any, >= its columns) */
+int adloco_blockscale_quantize_weight(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t cols, const void* W,
+                                      int64_t W_stride, void* q, int64_t q_stride, void* q_t, int64_t q_t_stride,
+                                      uint8_t* scale, int64_t scale_stride, void* stream);
+
+/* out [M, N] = A B^T (+ bias) with A [M, K] in rows' form and B [N, K] in weights' form:
+ *   out_mn = sum_k 2^(sa(m, k / 128) - 127) a_mk 2^(sb(n / 128, k / 128) - 127) b_nk (+ bias_n)
+ *   a, a_scale       as adloco_blockscale_quantize writes them (same pitch rules)
+ *   b                dev [N, K] bytes, pitch b_stride a multiple of 16, 16-byte aligned
+ *   b_scale          dev bytes; the block (n / 128, k / 128) is at n / 128 * b_scale_stride_n + k / 128 * b_scale_stride_k,
+ *                    so the transposed copy of a weight uses the weight's own scales with the strides exchanged
+ *   bias             dev [N] float, may be NULL
+ *   out              dev [M, N] in out_dtype, pitch out_stride; rows that are 16-byte aligned take the fast stores
+ * The layer y = x W^T is this call on (x, W); its input gradient dx = dy W on (dy, transposed copy of W).
+ * Tensor cores apply the scales; accumulation is fp32, the output is rounded once. */
+typedef struct {
+    int64_t M, N, K;
+    const void* a;
+    int64_t a_stride;
+    const uint8_t* a_scale;
+    int64_t a_scale_stride;
+    const void* b;
+    int64_t b_stride;
+    const uint8_t* b_scale;
+    int64_t b_scale_stride_n, b_scale_stride_k;
+    const float* bias;
+    void* out;
+    int64_t out_stride;
+    adloco_dtype out_dtype;
+    int32_t reserved;
+} adloco_blockscale_matmul_args;
+int adloco_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_args* args, void* stream);
 
 /* ---- switch-mode accumulation -------------------------------------------- */
 

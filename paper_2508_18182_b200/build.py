@@ -11,7 +11,8 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libadloco.so")
-SOURCES = ["api.cu", "stream_kernels.cu", "gram_kernels.cu"]
+SOURCES = ["api.cu", "stream_kernels.cu", "gram_kernels.cu", "block_api.cu", "block_kernels.cu",
+           "blockscale_gemm.cu"]
 HEADERS = ["common.cuh", os.path.join("..", "..", "include", "adloco.h")]
 
 
@@ -33,7 +34,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
            "-gencode", "arch=compute_100a,code=sm_100a",
            "-Xcompiler", "-fPIC,-O3,-Wall,-fvisibility=hidden",
            "-Xptxas", "-v" if verbose else "-warn-spills",
-           "-DADLOCO_BUILD"]
+           "-DADLOCO_BUILD", "--threads", "0"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or res.returncode != 0:

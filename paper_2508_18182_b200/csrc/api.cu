@@ -10,16 +10,6 @@ using namespace adloco;
 
 namespace {
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-    }
-    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
-};
-
 int ensure_staging(adloco_ctx* ctx, size_t bytes_each) {
     HostStaging& s = ctx->staging;
     if (!s.copy_stream) {

@@ -2,6 +2,7 @@
 // and the launch helpers that the entry points in api.cu use.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
 #include <atomic>
@@ -81,6 +82,17 @@ inline int set_cuda_error(adloco_ctx* ctx, cudaError_t e, const char* where) {
         cudaError_t e__ = (expr);                                         \
         if (e__ != cudaSuccess) return adloco::set_cuda_error((ctx), e__, #expr); \
     } while (0)
+
+// the ctx's device is current while an entry point runs
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = true;
+    explicit DeviceGuard(int dev) {
+        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
+        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+    }
+    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+};
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -180,5 +192,32 @@ int launch_direct_sqnorm(adloco_ctx* ctx, const void* X, const void* D, int64_t 
 int launch_direct_group(adloco_ctx* ctx, const adloco_linear_layer* layers, int n_layers, int64_t B, int64_t T,
                         float* n, int accumulate_norms, int accumulate_sum, int pair, cudaStream_t st);
 void free_tensor_map_cache(adloco_ctx* ctx);
+// the driver's encoder of TMA tensor maps, or null with the ctx's error text set
+typedef CUresult (*TensorMapEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                    const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                    CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+TensorMapEncode tensor_map_encode(adloco_ctx* ctx);
+
+// ---- between the linear layers, implemented in block_kernels.cu -------------------
+struct DropoutKey {
+    uint32_t drop = 0;        // an element stays when its 16 bits are >= drop (0: none dropped, 65536: all)
+    float scale = 1.f;        // of the elements that stay
+    uint32_t seed_lo = 0, seed_hi = 0, off_lo = 0, off_hi = 0;
+};
+int launch_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const DropoutKey& key, cudaStream_t st);
+int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d);
+int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_args& a, const DropoutKey& key, cudaStream_t st);
+int launch_dropout(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const void* x, int64_t x_stride, const void* r,
+                   int64_t r_stride, void* y, int64_t y_stride, const DropoutKey& key, cudaStream_t st);
+int launch_rope(adloco_ctx* ctx, int bf16, const adloco_rope_tensor* t, int n, int64_t B, int64_t T, int64_t D, int64_t R,
+                const uint64_t* turns, float magnitude, const int32_t* pos, int64_t pos_stride, int64_t first, int interleaved,
+                int inverse, cudaStream_t st);
+int launch_blockscale_quantize(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const void* x, int64_t x_stride, void* q,
+                               int64_t q_stride, uint8_t* scale, int64_t scale_stride, cudaStream_t st);
+int launch_blockscale_quantize_weight(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const void* W, int64_t W_stride,
+                                      void* q, int64_t q_stride, void* q_t, int64_t q_t_stride, uint8_t* scale,
+                                      int64_t scale_stride, cudaStream_t st);
+// implemented in blockscale_gemm.cu
+int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_args& a, cudaStream_t st);
 
 }  // namespace adloco

@@ -1630,18 +1630,14 @@ direct_group_kernel(const __grid_constant__ DirectGroupArgs<CAP> a) {
 // =====================================================================================
 // host side
 // =====================================================================================
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_fn(adloco_ctx* ctx) {
+TensorMapEncode tensor_map_encode(adloco_ctx* ctx) {
     // looked up once; the initialisation of a function-local static is thread-safe
-    static const EncodeTiledFn fn = []() -> EncodeTiledFn {
+    static const TensorMapEncode fn = []() -> TensorMapEncode {
         void* p = nullptr;
         cudaDriverEntryPointQueryResult q;
         const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q);
         if (e != cudaSuccess || q != cudaDriverEntryPointSuccess) return nullptr;
-        return reinterpret_cast<EncodeTiledFn>(p);
+        return reinterpret_cast<TensorMapEncode>(p);
     }();
     if (!fn) set_cuda_error(ctx, cudaErrorUnknown, "cuTensorMapEncodeTiled entry point");
     return fn;
@@ -1651,7 +1647,7 @@ static EncodeTiledFn encode_fn(adloco_ctx* ctx) {
 // box and 128-byte swizzle; out-of-range rows and columns read as zero.
 static int make_map(adloco_ctx* ctx, CUtensorMap* m, const void* base, int64_t B, int64_t T, int64_t d,
                     uint32_t box_tokens) {
-    EncodeTiledFn fn = encode_fn(ctx);
+    TensorMapEncode fn = tensor_map_encode(ctx);
     if (!fn) return ADLOCO_ERR_CUDA;
     const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)T, (cuuint64_t)B};
     const cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)T * (cuuint64_t)d * 2};
@@ -1670,7 +1666,7 @@ static int make_map(adloco_ctx* ctx, CUtensorMap* m, const void* base, int64_t B
 // fp32 matrix [rows, cols] (cols contiguous) as a 2-D map with a 32-row box of box_cols
 // columns: 32 columns with the 128-byte swizzle, 16 columns unswizzled
 static int make_map_f32(adloco_ctx* ctx, CUtensorMap* m, float* base, int64_t rows, int64_t cols, uint32_t box_cols) {
-    EncodeTiledFn fn = encode_fn(ctx);
+    TensorMapEncode fn = tensor_map_encode(ctx);
     if (!fn) return ADLOCO_ERR_CUDA;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)cols * 4};
