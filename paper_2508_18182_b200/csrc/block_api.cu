@@ -15,10 +15,20 @@ bool elem_aligned(const void* p, adloco_dtype t) { return (reinterpret_cast<uint
 
 int make_key(double p, uint64_t seed, uint64_t offset, DropoutKey* key) {
     if (!(p >= 0.0) || !(p <= 1.0)) return ADLOCO_ERR_INVALID_ARG;
-    key->drop = (uint32_t)std::nearbyint(p * 65536.0);
-    key->scale = key->drop < 65536u ? (float)(65536.0 / (65536.0 - (double)key->drop)) : 0.f;
-    key->seed_lo = (uint32_t)seed; key->seed_hi = (uint32_t)(seed >> 32);
+    const uint32_t drop = (uint32_t)std::nearbyint(p * 65536.0);
+    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+    for (int r = 0; r < 10; ++r, k0 += 0x9E3779B9u, k1 += 0xBB67AE85u) {      // Weyl sequence of the generator's key
+        key->round[2 * r] = k0;
+        key->round[2 * r + 1] = k1;
+    }
     key->off_lo = (uint32_t)offset; key->off_hi = (uint32_t)(offset >> 32);
+    key->on = drop != 0;
+    if (drop < 65536u) {
+        key->keep = (float)(65536u - drop) * (1.0f / 65536.0f);
+        key->scale = (float)(65536.0 / (65536.0 - (double)drop));
+    }
+    key->limit = (drop & 0xffffu) | (drop << 16);
+    if (drop == 65536u) key->pair = key->low = key->high = 0x4444u;
     return ADLOCO_OK;
 }
 

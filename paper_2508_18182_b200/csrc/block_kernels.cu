@@ -3,6 +3,7 @@
 // and quantisation to 8 bits with power-of-two scales.  All are bound by HBM: each input is read
 // once, each output written once, everything between stays in registers.
 #include <cuda_fp8.h>
+#include <atomic>
 
 #include "common.cuh"
 
@@ -10,111 +11,151 @@ namespace adloco {
 
 namespace {
 
+// ---- two fp32 operations an instruction ----------------------------------------------------
+struct F2 { float x, y; };
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 d;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
+        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 d;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ F2 both(float v) { return F2{v, v}; }
+
 // ---- eight adjacent elements of a row ---------------------------------------------------
-// The vector form is one 16-byte access (two for float); the guarded form takes rows that do not
-// start on 16-byte boundaries and a row's last, incomplete group.
+// As they lie in memory (four or eight words), so that what waits for use takes half the registers in bf16.  The
+// vector form is one 16-byte access (two for float); the guarded form takes rows that do not start on 16-byte
+// boundaries and a row's last, incomplete group, and reads what is missing as zero.
+template <typename T>
+struct Raw { uint32_t w[sizeof(T) * 2]; };
+
 template <bool VEC>
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, int n, float (&v)[8]) {
+__device__ __forceinline__ Raw<__nv_bfloat16> load_raw(const __nv_bfloat16* p, int n) {
+    Raw<__nv_bfloat16> r;
     if (VEC) {
-        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p));
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(u[i] << 16);
-            v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-        }
+        const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p));
+        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
     } else {
+        const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? __bfloat162float(p[i]) : 0.f;
+        for (int i = 0; i < 4; ++i)
+            r.w[i] = (2 * i < n ? (uint32_t)h[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)h[2 * i + 1] << 16 : 0u);
     }
+    return r;
 }
 template <bool VEC>
-__device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
+__device__ __forceinline__ Raw<float> load_raw(const float* p, int n) {
+    Raw<float> r;
     if (VEC) {
-        const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p)), b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+        r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
+        r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+        for (int i = 0; i < 8; ++i) r.w[i] = i < n ? __float_as_uint(p[i]) : 0u;
     }
+    return r;
 }
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+template <typename T>
+__device__ __forceinline__ Raw<T> zero_raw() {
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) * 2); ++i) r.w[i] = 0u;
+    return r;
+}
+// elements 2 i and 2 i + 1
+__device__ __forceinline__ F2 pair_of(const Raw<__nv_bfloat16>& r, int i) {
+    return F2{__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xffff0000u)};
+}
+__device__ __forceinline__ F2 pair_of(const Raw<float>& r, int i) {
+    return F2{__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1])};
+}
+__device__ __forceinline__ uint32_t pack2(F2 v) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ void set_pair(Raw<__nv_bfloat16>& r, int i, F2 v) { r.w[i] = pack2(v); }
+__device__ __forceinline__ void set_pair(Raw<float>& r, int i, F2 v) {
+    r.w[2 * i] = __float_as_uint(v.x);
+    r.w[2 * i + 1] = __float_as_uint(v.y);
+}
 template <bool VEC>
-__device__ __forceinline__ void store8(__nv_bfloat16* p, int n, const float (&v)[8]) {
+__device__ __forceinline__ void store_raw(__nv_bfloat16* p, int n, const Raw<__nv_bfloat16>& r) {
     if (VEC) {
-        __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])));
+        __stcs(reinterpret_cast<uint4*>(p), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
     } else {
+        unsigned short* h = reinterpret_cast<unsigned short*>(p);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = __float2bfloat16_rn(v[i]);
+            if (i < n) h[i] = (unsigned short)(r.w[i >> 1] >> (16 * (i & 1)));
     }
 }
 template <bool VEC>
-__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
+__device__ __forceinline__ void store_raw(float* p, int n, const Raw<float>& r) {
     if (VEC) {
-        __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-        __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+        __stcs(reinterpret_cast<uint4*>(p), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
+        __stcs(reinterpret_cast<uint4*>(p) + 1, make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = v[i];
+            if (i < n) p[i] = __uint_as_float(r.w[i]);
     }
 }
 // the gain is read by every row: it stays in L1
-__device__ __forceinline__ void load_gain8(const void* gain, int bf16, int col, int n, float (&g)[8]) {
+__device__ __forceinline__ void load_gain(const void* gain, int bf16, int col, int n, F2 (&g)[4]) {
     if (n == 8 && (reinterpret_cast<uintptr_t>(gain) & 15u) == 0) {
         if (bf16) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(gain) + col));
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(gain) + col));
+            const Raw<__nv_bfloat16> r = {{v.x, v.y, v.z, v.w}};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                g[2 * i] = __uint_as_float(u[i] << 16);
-                g[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-            }
+            for (int i = 0; i < 4; ++i) g[i] = pair_of(r, i);
         } else {
             const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(gain) + col);
             const float4 a = __ldg(p), b = __ldg(p + 1);
-            g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w;
-            g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
+            g[0] = F2{a.x, a.y}; g[1] = F2{a.z, a.w};
+            g[2] = F2{b.x, b.y}; g[3] = F2{b.z, b.w};
         }
         return;
     }
+    auto one = [&](int i) {
+        if (i >= n) return 0.f;
+        return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(gain)[col + i]) : __ldg(static_cast<const float*>(gain) + col + i);
+    };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i >= n) g[i] = 0.f;
-        else g[i] = bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(gain)[col + i]) : __ldg(static_cast<const float*>(gain) + col + i);
-    }
+    for (int i = 0; i < 4; ++i) g[i] = F2{one(2 * i), one(2 * i + 1)};
 }
 
-// ---- Philox-4x32-10 ---------------------------------------------------------------------
+// ---- Philox-4x32-10 and the mask -----------------------------------------------------------
 // Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3" (2011): ten rounds of two
 // 32 x 32 -> 64-bit products on a 128-bit counter.  One call serves eight elements, 16 bits each: with
 // 32 bits an element the integer work, not HBM, would set the time of dropout on bf16.
 __device__ __forceinline__ uint4 philox(uint64_t group, const DropoutKey& k) {
     uint32_t c0 = (uint32_t)group, c1 = (uint32_t)(group >> 32), c2 = k.off_lo, c3 = k.off_hi;
-    uint32_t k0 = k.seed_lo, k1 = k.seed_hi;
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)0xD2511F53u * c0, b = (uint64_t)0xCD9E8D57u * c2;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ k.round[2 * r];
         c1 = (uint32_t)b;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ k.round[2 * r + 1];
         c3 = (uint32_t)a;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
     }
     return make_uint4(c0, c1, c2, c3);
 }
-// drop() of the eight elements from flat index e on; a dropped element is 0 whatever it held.  Rows whose length
-// is not a multiple of eight start inside a group: such eight elements span two groups.
-__device__ __forceinline__ void drop8(float (&v)[8], uint64_t e, const DropoutKey& k) {
+// What stays of the eight elements from flat index e on: word i has the answer for elements 2 i and 2 i + 1 in bits
+// 15 and 31.  Rows whose length is not a multiple of eight start inside a group (ALIGNED false): their eight
+// elements span two groups.
+struct Kept { uint32_t w[4]; };
+template <bool ALIGNED>
+__device__ __forceinline__ Kept kept_of(uint64_t e, const DropoutKey& k) {
     const uint4 w = philox(e >> 3, k);
     uint32_t u[8] = {w.x, w.y, w.z, w.w, 0u, 0u, 0u, 0u};
-    const uint32_t sh = (uint32_t)e & 7u;
+    const uint32_t sh = ALIGNED ? 0u : (uint32_t)e & 7u;
     if (sh) {
         const uint4 w2 = philox((e >> 3) + 1, k);
         u[4] = w2.x; u[5] = w2.y; u[6] = w2.z; u[7] = w2.w;
@@ -126,12 +167,49 @@ __device__ __forceinline__ void drop8(float (&v)[8], uint64_t e, const DropoutKe
             for (int i = 0; i < 4; ++i) u[i] = __funnelshift_r(u[i], u[i + 1], 16);
         }
     }
+    Kept r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t h = (i & 1) ? u[i >> 1] >> 16 : u[i >> 1] & 0xffffu;
-        v[i] = h >= k.drop ? v[i] * k.scale : 0.f;
+    for (int i = 0; i < 4; ++i) {
+        // half >= limit in both halves at once: z's top bits compare the lower 15 bits, the top bits decide where they differ
+        const uint32_t z = (u[i] | 0x80008000u) - (k.limit & 0x7fff7fffu);
+        r.w[i] = (u[i] & ~k.limit) | ((u[i] | ~k.limit) & z);
+    }
+    return r;
+}
+// bytes of v by the selector's nibbles: with a nibble's top bit set, the byte's sign in all its bits; 4..7 give zero
+__device__ __forceinline__ uint32_t spread(uint32_t v, uint32_t selector) {
+    uint32_t r;
+    asm("prmt.b32 %0, %1, 0, %2;" : "=r"(r) : "r"(v), "r"(selector));
+    return r;
+}
+// a dropped element is 0 whatever it held
+__device__ __forceinline__ void drop_raw(Raw<__nv_bfloat16>& v, const Kept& m, const DropoutKey& k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v.w[i] &= spread(m.w[i], k.pair);
+}
+__device__ __forceinline__ void drop_raw(Raw<float>& v, const Kept& m, const DropoutKey& k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v.w[2 * i] &= spread(m.w[i], k.low);
+        v.w[2 * i + 1] &= spread(m.w[i], k.high);
     }
 }
+
+// x / keep + r as (x + r keep) / keep: keep has 16 bits and is exact, so where the residual cancels the branch the sum
+// still is as good as its inputs
+__device__ __forceinline__ F2 scaled(F2 x, const DropoutKey& k, F2 r) { return mul2(fma2(r, both(k.keep), x), both(k.scale)); }
+
+// n / d for n < 2^31 by a multiplication: with s = ceil(log2 d) and m = ceil(2^(31 + s) / d), the error of m d is
+// below d <= 2^s, and n times it below 2^(31 + s)
+struct FastDiv {
+    uint32_t d, m, s;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t div) : d(div), m(0), s(0) {
+        while ((uint64_t(1) << s) < div) ++s;
+        m = (uint32_t)(((uint64_t(1) << (31 + s)) + div - 1) / div);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> (31 + s)); }
+};
 
 // ---- 8-bit blocks -------------------------------------------------------------------------
 // The scale's byte from the bits of the block's largest magnitude: with that magnitude m 2^k, 1 <= m < 2, and
@@ -146,22 +224,24 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) {
 }
 // 1 / scale: a power of two, so multiplying by it is exact (byte 0..247 of a finite block)
 __device__ __forceinline__ float inv_scale(uint32_t byte) { return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23); }
-__device__ __forceinline__ uint32_t abs_max8(const float (&v)[8]) {
+__device__ __forceinline__ uint32_t abs_max8(const F2 (&v)[4]) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    for (int i = 0; i < 4; ++i) m = max(m, max(__float_as_uint(v[i].x) & 0x7fffffffu, __float_as_uint(v[i].y) & 0x7fffffffu));
     return m;
 }
-__device__ __forceinline__ uint2 to_e4m3x8(const float (&v)[8], float inv) {
+__device__ __forceinline__ uint2 to_e4m3x8(const F2 (&v)[4], float inv) {
     uint32_t h[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        h[i] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * i] * inv, v[2 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+    for (int i = 0; i < 4; ++i) {
+        const F2 u = mul2(v[i], both(inv));
+        h[i] = __nv_cvt_float2_to_fp8x2(make_float2(u.x, u.y), __NV_SATFINITE, __NV_E4M3);
+    }
     return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
 }
 // The 16 lanes that hold one block of a row (8 adjacent elements each) agree on its scale; the lane of the
 // block's first elements writes it.  Every lane of the warp takes part; n = 0 for lanes beyond the row.
-__device__ __forceinline__ void quantise_block(const float (&v)[8], int n, uint8_t* q_row, uint8_t* scale_row, int col) {
+__device__ __forceinline__ void quantise_block(const F2 (&v)[4], int n, uint8_t* q_row, uint8_t* scale_row, int col) {
     uint32_t m = n > 0 ? abs_max8(v) : 0u;          // elements beyond n are zero
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -200,7 +280,7 @@ __host__ __device__ constexpr int row_threads(int tpr) { return tpr > 256 ? tpr 
 
 // ---- norm, forward --------------------------------------------------------------------------
 // TPR threads hold a row of up to TPR * C * 8 elements in registers: one read of x and of the residual, the
-// sum of squares in fp32, then every output from the registers.
+// mean square in fp32, then every output from the registers.
 template <typename XT, typename ST, int TPR, int C, bool VEC>
 __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __grid_constant__ adloco_rmsnorm_args a,
                                                                         const __grid_constant__ DropoutKey key) {
@@ -213,56 +293,69 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
     const int64_t row = there ? row_asked : a.rows - 1;
     const int d = (int)a.d;
     const XT* x = static_cast<const XT*>(a.x) + row * a.x_stride;
-    const ST* r = a.residual ? static_cast<const ST*>(a.residual) + row * a.residual_stride : nullptr;
-    float h[C][8], e[C][8];
+    const ST* r = static_cast<const ST*>(a.residual) + row * a.residual_stride;
+    Raw<XT> xr[C];
+    Raw<ST> rr[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int col = (c * TPR + t) * 8, n = min(8, d - col);
-        if (n > 0) load8<VEC>(x + col, n, h[c]);
-        else for (int i = 0; i < 8; ++i) h[c][i] = 0.f;
+        xr[c] = zero_raw<XT>();
+        if (n > 0) xr[c] = load_raw<VEC>(x + col, n);
     }
-    if (r) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * TPR + t) * 8, n = min(8, d - col);
-            if (n > 0) load8<VEC>(r + col, n, e[c]);
-            else for (int i = 0; i < 8; ++i) e[c][i] = 0.f;
-        }
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * TPR + t) * 8, n = min(8, d - col);
+        rr[c] = zero_raw<ST>();
+        if (a.residual && n > 0) rr[c] = load_raw<VEC>(r + col, n);
     }
-    if (key.drop) {
+    if (key.on) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * 8;
-            if (col < d) drop8(h[c], (uint64_t)(row * d + col), key);
+            if (col < d) drop_raw(xr[c], kept_of<VEC>((uint64_t)(row * d + col), key), key);
         }
     }
     const float inv_d = 1.0f / (float)d;
-    float ss = 0.f;
+    F2 h[C][4], ss = both(0.f);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int col = (c * TPR + t) * 8, n = min(8, d - col);
+        Raw<ST> out;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (r) h[c][i] += e[c][i];
-            if (!VEC && i >= n) h[c][i] = 0.f;
-            ss = fmaf(h[c][i] * inv_d, h[c][i], ss);      // the mean: the sum of squares that fit fp32 may not fit
+        for (int i = 0; i < 4; ++i) {
+            h[c][i] = scaled(pair_of(xr[c], i), key, pair_of(rr[c], i));
+            ss = fma2(mul2(h[c][i], both(inv_d)), h[c][i], ss);      // the mean: a sum of squares that fit fp32 may not fit
+            set_pair(out, i, h[c][i]);
         }
-        if (a.h && there && n > 0) store8<VEC>(static_cast<ST*>(a.h) + row * a.h_stride + col, n, h[c]);
+        if (a.h && there && n > 0) store_raw<VEC>(static_cast<ST*>(a.h) + row * a.h_stride + col, n, out);
     }
-    ss = row_sum<TPR, THREADS>(ss, smem, 0);
-    const float rstd = rsqrtf(ss + a.eps);
+    const float mean = row_sum<TPR, THREADS>(ss.x + ss.y, smem, 0);
+    const float rstd = rsqrtf(mean + a.eps);
     if (a.rstd && there && t == 0) a.rstd[row] = rstd;
     uint8_t* q_row = static_cast<uint8_t*>(a.q) + row * a.q_stride;
     uint8_t* s_row = a.q_scale + row * a.q_scale_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int col = (c * TPR + t) * 8, n = there ? min(8, d - col) : 0;
-        float y[8], g[8];
-        if (n > 0) load_gain8(a.gain, a.gain_dtype == ADLOCO_BF16, col, n, g);
+        F2 g[4];
+        Raw<XT> out;
+        if (n > 0) {
+            load_gain(a.gain, a.gain_dtype == ADLOCO_BF16, col, n, g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = n > i ? h[c][i] * rstd * g[i] : 0.f;
-        if (a.y && n > 0) store8<VEC>(static_cast<XT*>(a.y) + row * a.y_stride + col, n, y);
-        if (a.q) quantise_block(y, n, q_row, s_row, col);
+            for (int i = 0; i < 4; ++i) {
+                g[i] = mul2(mul2(h[c][i], both(rstd)), g[i]);
+                set_pair(out, i, g[i]);
+            }
+            if (!VEC && n < 8) {                                     // elements beyond the row: 0, also where rstd is not finite
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (2 * i >= n) g[i].x = 0.f;
+                    if (2 * i + 1 >= n) g[i].y = 0.f;
+                }
+            }
+            if (a.y) store_raw<VEC>(static_cast<XT*>(a.y) + row * a.y_stride + col, n, out);
+        }
+        if (a.q) quantise_block(g, n, q_row, s_row, col);
     }
 }
 
@@ -271,102 +364,182 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
 // two row sums of the formula collapse into one (gain dy . xhat), and the gain's gradient dy xhat is added up in
 // registers over the block's rows; blocks leave it in the workspace [B, chunks, d] for rmsnorm_gain_kernel, so
 // h and dy are read once for both gradients and no sum depends on the order of atomics.
+// A thread's own elements of the next rows travel ahead through shared memory (cp.async, each thread reads only
+// what it copied, so no barrier): registers for three operands of one row leave 16 warps an SM, too few loads in
+// flight without it.
 struct RmsBackArgs {
     adloco_rmsnorm_backward_args a;
     int64_t chunks, rows_per_chunk;
 };
+__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void stage_async(uint32_t dst, uint32_t step, const T* src) {       // step: from one 16-byte piece to the next
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) copy16_async(dst + i * step, reinterpret_cast<const uint4*>(src) + i);
+}
+template <typename T>
+__device__ __forceinline__ Raw<T> staged(uint32_t at, uint32_t step) {
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const uint4 v = lds128(at + i * step);
+        r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
+    }
+    return r;
+}
+// 16-byte pieces a thread stages for one row: dy, h, and the stream's gradient
+template <typename XT, typename ST, int C>
+__host__ __device__ constexpr int stage_pieces() { return C * ((int)sizeof(XT) / 2 + 2 * ((int)sizeof(ST) / 2)); }
+// rows on their way or in use: three where they fit twice into an SM's shared memory, else two; one (no staging:
+// loads straight into registers) where not even two fit
+template <typename XT, typename ST, int C, int THREADS>
+__host__ __device__ constexpr int stage_depth() {
+    const int row = stage_pieces<XT, ST, C>() * 16 * THREADS;
+    return 3 * row <= 112 * 1024 ? 3 : 2 * row <= 224 * 1024 ? 2 : 1;
+}
+template <typename XT, typename ST, int C, int THREADS>
+__host__ __device__ constexpr int stage_smem() { return stage_depth<XT, ST, C, THREADS>() < 2 ? 0 : stage_depth<XT, ST, C, THREADS>() * stage_pieces<XT, ST, C>() * 16 * THREADS; }
+
 template <typename XT, typename ST, int TPR, int C, bool VEC, bool GAIN>
 __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(const __grid_constant__ RmsBackArgs p,
                                                                             const __grid_constant__ DropoutKey key) {
     constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
+    constexpr uint32_t STEP = THREADS * 16;                 // piece i of thread t at i * STEP + 16 t: free of bank conflicts
+    constexpr int XP = (int)sizeof(XT) / 2, SP = (int)sizeof(ST) / 2, PIECES = C * (XP + 2 * SP);
+    constexpr int DEPTH = stage_depth<XT, ST, C, THREADS>();
+    constexpr bool STAGED = VEC && DEPTH > 1;
     const adloco_rmsnorm_backward_args& a = p.a;
-    extern __shared__ float columns[];                     // [ROWS][d] when GAIN and ROWS > 1
+    extern __shared__ __align__(16) float columns[];        // the staged rows; at the end [ROWS][d] (GAIN and ROWS > 1)
     __shared__ float smem[2 * THREADS / 32];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = (int)a.d;
     const int64_t sample = (int64_t)blockIdx.x / p.chunks, chunk = (int64_t)blockIdx.x % p.chunks;
     const int64_t first = chunk * p.rows_per_chunk, last = min(a.T, first + p.rows_per_chunk);
     const float inv_d = 1.0f / (float)d;
-    float acc[GAIN ? C : 1][8];
+    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(columns)) + threadIdx.x * 16;
+    F2 acc[GAIN ? C : 1][4];
     if (GAIN) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[c][i] = 0.f;
+            for (int i = 0; i < 4; ++i) acc[c][i] = both(0.f);
     }
-    int turn = 0;
+    // copies of this thread's part of row at + sub into a stage; one group a call, empty beyond the last row
+    auto fetch = [&](int64_t at, int stage) {
+        if (at + sub < last) {
+            const int64_t row = sample * a.T + at + sub;
+            const uint32_t to = mine + (uint32_t)(stage * PIECES) * STEP;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * TPR + t) * 8;
+                if (col >= d) continue;
+                stage_async(to + (c * XP) * STEP, STEP, static_cast<const XT*>(a.dy) + row * a.dy_stride + col);
+                stage_async(to + (C * XP + c * SP) * STEP, STEP, static_cast<const ST*>(a.h) + row * a.h_stride + col);
+                if (a.dh_residual)
+                    stage_async(to + (C * XP + C * SP + c * SP) * STEP, STEP,
+                                static_cast<const ST*>(a.dh_residual) + row * a.dh_residual_stride + col);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (STAGED) {
+#pragma unroll
+        for (int k = 0; k < DEPTH - 1; ++k) fetch(first + k * ROWS, k);
+    }
+    int turn = 0, stage = 0;
     for (int64_t at = first; at < last; at += ROWS, ++turn) {
         const bool there = at + sub < last;
         if (TPR == 32 && !there) break;
         const int64_t row = sample * a.T + (there ? at + sub : last - 1);
-        const XT* dy = static_cast<const XT*>(a.dy) + row * a.dy_stride;
-        const ST* h = static_cast<const ST*>(a.h) + row * a.h_stride;
-        float u[C][8], v[C][8], r[C][8];
+        const float rstd = a.rstd[row];
+        if (STAGED) {
+            // the stage freed by the row before last (its values are in registers or done with) takes the next fetch
+            fetch(at + (DEPTH - 1) * ROWS, stage == 0 ? DEPTH - 1 : stage - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+        }
+        const uint32_t from = mine + (uint32_t)(stage * PIECES) * STEP;
+        F2 u[C][4], v[C][4], dot = both(0.f);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int col = (c * TPR + t) * 8, n = min(8, d - col);
-            if (n > 0) { load8<VEC>(dy + col, n, u[c]); load8<VEC>(h + col, n, v[c]); }
-            else for (int i = 0; i < 8; ++i) { u[c][i] = 0.f; v[c][i] = 0.f; }
+            const int col = (c * TPR + t) * 8, n = there ? min(8, d - col) : 0;
+            if (n <= 0) continue;
+            Raw<XT> ur;
+            Raw<ST> vr;
+            if (STAGED) {
+                ur = staged<XT>(from + (c * XP) * STEP, STEP);
+                vr = staged<ST>(from + (C * XP + c * SP) * STEP, STEP);
+            } else {
+                ur = load_raw<VEC>(static_cast<const XT*>(a.dy) + row * a.dy_stride + col, n);
+                vr = load_raw<VEC>(static_cast<const ST*>(a.h) + row * a.h_stride + col, n);
+            }
+            F2 g[4];
+            load_gain(a.gain, a.gain_dtype == ADLOCO_BF16, col, n, g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const F2 dy = pair_of(ur, i);
+                v[c][i] = mul2(pair_of(vr, i), both(rstd));                    // xhat
+                if (GAIN) acc[c][i] = fma2(dy, v[c][i], acc[c][i]);
+                u[c][i] = mul2(dy, g[i]);
+                dot = fma2(u[c][i], v[c][i], dot);
+            }
         }
-        if (a.dh_residual) {
+        const float m = row_sum<TPR, THREADS>(dot.x + dot.y, smem, turn) * inv_d;
+        if (there) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int col = (c * TPR + t) * 8, n = min(8, d - col);
-                if (n > 0) load8<VEC>(static_cast<const ST*>(a.dh_residual) + row * a.dh_residual_stride + col, n, r[c]);
+                if (n <= 0) continue;
+                Raw<ST> r = zero_raw<ST>(), out;
+                if (a.dh_residual) {
+                    if (STAGED) r = staged<ST>(from + (C * XP + C * SP + c * SP) * STEP, STEP);
+                    else r = load_raw<VEC>(static_cast<const ST*>(a.dh_residual) + row * a.dh_residual_stride + col, n);
+                }
+                F2 o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    o[i] = fma2(fma2(v[c][i], both(-m), u[c][i]), both(rstd), pair_of(r, i));
+                    set_pair(out, i, o[i]);
+                }
+                store_raw<VEC>(static_cast<ST*>(a.dh) + row * a.dh_stride + col, n, out);
+                if (a.dx) {
+                    Raw<XT> x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) set_pair(x, i, mul2(o[i], both(key.scale)));
+                    if (key.on) drop_raw(x, kept_of<VEC>((uint64_t)(row * d + col), key), key);
+                    store_raw<VEC>(static_cast<XT*>(a.dx) + row * a.dx_stride + col, n, x);
+                }
             }
         }
-        const float rstd = a.rstd[row];
-        float dot = 0.f;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * TPR + t) * 8, n = min(8, d - col);
-            if (n <= 0) continue;
-            float g[8];
-            load_gain8(a.gain, a.gain_dtype == ADLOCO_BF16, col, n, g);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[c][i] *= rstd;                                               // xhat
-                if (GAIN && there) acc[c][i] = fmaf(u[c][i], v[c][i], acc[c][i]);
-                u[c][i] *= g[i];
-                dot = fmaf(u[c][i], v[c][i], dot);
-            }
-        }
-        const float m = row_sum<TPR, THREADS>(dot, smem, turn) * inv_d;
-        if (!there) continue;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * TPR + t) * 8, n = min(8, d - col);
-            if (n <= 0) continue;
-            float o[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                o[i] = rstd * (u[c][i] - v[c][i] * m);
-                if (a.dh_residual) o[i] += r[c][i];
-            }
-            store8<VEC>(static_cast<ST*>(a.dh) + row * a.dh_stride + col, n, o);
-            if (a.dx) {
-                if (key.drop) drop8(o, (uint64_t)(row * d + col), key);
-                store8<VEC>(static_cast<XT*>(a.dx) + row * a.dx_stride + col, n, o);
-            }
-        }
+        stage = stage == DEPTH - 1 ? 0 : stage + 1;
     }
     if (!GAIN) return;
+    asm volatile("cp.async.wait_all;" ::: "memory");
     float* part = static_cast<float*>(a.workspace) + (int64_t)blockIdx.x * d;
     if (ROWS == 1) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int col = (c * TPR + t) * 8 + i;
-                if (col < d) part[col] = acc[c][i];
+            for (int i = 0; i < 4; ++i) {
+                const int col = (c * TPR + t) * 8 + 2 * i;
+                if (col < d) part[col] = acc[c][i].x;
+                if (col + 1 < d) part[col + 1] = acc[c][i].y;
             }
         return;
     }
+    __syncthreads();                                        // every thread is done with its stages
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int col = (c * TPR + t) * 8 + i;
-            if (col < d) columns[sub * d + col] = acc[c][i];
+        for (int i = 0; i < 4; ++i) {
+            const int col = (c * TPR + t) * 8 + 2 * i;
+            if (col < d) columns[sub * d + col] = acc[c][i].x;
+            if (col + 1 < d) columns[sub * d + col + 1] = acc[c][i].y;
         }
     __syncthreads();
     for (int col = threadIdx.x; col < d; col += THREADS) {
@@ -425,64 +598,75 @@ __global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float*
 }
 
 // ---- dropout ------------------------------------------------------------------------------------
-// A thread takes the eight elements of one call of the generator.  They are adjacent in memory unless a row ends
-// among them; the vector form needs rows of a multiple of eight elements, or no gaps between rows.
+// A thread takes the eight elements of one call of the generator, two such groups at a time so that enough loads
+// are in flight.  The eight are adjacent in memory unless a row ends among them; the vector form needs rows of a
+// multiple of eight elements, or no gaps between rows (FLAT).
 struct DropArgs {
     const void *x, *r;
     void* y;
     int64_t rows, cols, x_stride, r_stride, y_stride, groups;
+    int small;                       // group indices are below 2^31
+    FastDiv groups_per_row;          // VEC rows
 };
 template <typename T, bool VEC, bool FLAT>
 __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropArgs a, const __grid_constant__ DropoutKey key) {
+    constexpr int U = 2;
     const T* x = static_cast<const T*>(a.x);
     const T* r = static_cast<const T*>(a.r);
     T* y = static_cast<T*>(a.y);
     const int64_t total = a.rows * a.cols;
-    for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < a.groups; g += (int64_t)gridDim.x * 256) {
-        const int64_t e = g * 8;
-        const int n = (int)min((int64_t)8, total - e);
-        float v[8], s[8];
-        if (FLAT) {
-            if (VEC && n == 8) {
-                load8<true>(x + e, 8, v);
-                if (r) load8<true>(r + e, 8, s);
-            } else {
-                load8<false>(x + e, n, v);
-                if (r) load8<false>(r + e, n, s);
+    for (int64_t g0 = (int64_t)blockIdx.x * (256 * U) + threadIdx.x; g0 < a.groups; g0 += (int64_t)gridDim.x * (256 * U)) {
+        Raw<T> v[U], s[U];
+        int64_t row[U], col[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t g = g0 + k * 256, e = g * 8;
+            row[k] = 0; col[k] = e;
+            if (g >= a.groups) continue;
+            if (!FLAT) {
+                if (VEC) row[k] = a.small ? (int64_t)a.groups_per_row((uint32_t)g) : g / (int64_t)a.groups_per_row.d;
+                else row[k] = e / a.cols;
+                col[k] = e - row[k] * a.cols;
             }
-        } else {
-            const int64_t row = e / a.cols, col = e - row * a.cols;
-            if (VEC) {
-                load8<true>(x + row * a.x_stride + col, 8, v);
-                if (r) load8<true>(r + row * a.r_stride + col, 8, s);
+            const int n = (int)min((int64_t)8, total - e);
+            if (VEC && n == 8) {
+                v[k] = load_raw<true>(x + row[k] * a.x_stride + col[k], 8);
+                if (r) s[k] = load_raw<true>(r + row[k] * a.r_stride + col[k], 8);
+            } else if (FLAT) {
+                v[k] = load_raw<false>(x + e, n);
+                if (r) s[k] = load_raw<false>(r + e, n);
             } else {
-                int64_t i = row, j = col;
-                for (int k = 0; k < 8; ++k) {
-                    v[k] = s[k] = 0.f;
-                    if (k < n) {
-                        v[k] = (float)x[i * a.x_stride + j];
-                        if (r) s[k] = (float)r[i * a.r_stride + j];
-                        if (++j == a.cols) { j = 0; ++i; }
-                    }
+                v[k] = zero_raw<T>();
+                s[k] = zero_raw<T>();
+                T* vv = reinterpret_cast<T*>(v[k].w);
+                T* ss = reinterpret_cast<T*>(s[k].w);
+                int64_t i = row[k], j = col[k];
+                for (int q = 0; q < n; ++q) {
+                    vv[q] = x[i * a.x_stride + j];
+                    if (r) ss[q] = r[i * a.r_stride + j];
+                    if (++j == a.cols) { j = 0; ++i; }
                 }
             }
         }
-        drop8(v, (uint64_t)e, key);
-        if (r) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += s[k];
-        }
-        if (FLAT) {
-            if (VEC && n == 8) store8<true>(y + e, 8, v);
-            else store8<false>(y + e, n, v);
-        } else {
-            const int64_t row = e / a.cols, col = e - row * a.cols;
-            if (VEC) {
-                store8<true>(y + row * a.y_stride + col, 8, v);
+        for (int k = 0; k < U; ++k) {
+            const int64_t g = g0 + k * 256, e = g * 8;
+            if (g >= a.groups) continue;
+            if (key.on) drop_raw(v[k], kept_of<true>((uint64_t)e, key), key);
+            Raw<T> out;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                set_pair(out, i, scaled(pair_of(v[k], i), key, r ? pair_of(s[k], i) : both(0.f)));
+            const int n = (int)min((int64_t)8, total - e);
+            if (VEC && n == 8) {
+                store_raw<true>(y + row[k] * a.y_stride + col[k], 8, out);
+            } else if (FLAT) {
+                store_raw<false>(y + e, n, out);
             } else {
-                int64_t i = row, j = col;
-                for (int k = 0; k < n; ++k) {
-                    y[i * a.y_stride + j] = (T)v[k];
+                const T* oo = reinterpret_cast<const T*>(out.w);
+                int64_t i = row[k], j = col[k];
+                for (int q = 0; q < n; ++q) {
+                    y[i * a.y_stride + j] = oo[q];
                     if (++j == a.cols) { j = 0; ++i; }
                 }
             }
@@ -501,6 +685,7 @@ struct RopeArgs {
     int64_t B, T, tokens;
     int D, R, rot_units, units;        // units of P pairs a head: rotated, and with the copied rest
     int tokens_per_block;
+    FastDiv by_half, by_token, by_units, by_T;
     const uint64_t* turns;
     const int32_t* positions;
     int64_t positions_stride, first;
@@ -517,9 +702,9 @@ __global__ void __launch_bounds__(256) rope_kernel(const __grid_constant__ RopeA
     const int64_t token0 = (int64_t)blockIdx.x * a.tokens_per_block;
     const int here = (int)min((int64_t)a.tokens_per_block, a.tokens - token0);
     for (int i = threadIdx.x; i < here * half; i += 256) {
-        const int tok = i / half, j = i - tok * half;
-        const int64_t b = (token0 + tok) / a.T, s = (token0 + tok) - b * a.T;
-        const int64_t pos = a.positions ? (int64_t)a.positions[b * a.positions_stride + s] : a.first + s;
+        const int tok = (int)a.by_half(i), j = i - tok * half;
+        const uint32_t b = a.by_T((uint32_t)(token0 + tok)), s = (uint32_t)(token0 + tok) - b * (uint32_t)a.T;
+        const int64_t pos = a.positions ? (int64_t)a.positions[b * a.positions_stride + s] : a.first + (int64_t)s;
         // the phase in units of 2^-64 turns is exact; its top 32 bits, as a signed number, are half turns in [-1, 1)
         const int32_t top = (int32_t)(((uint64_t)pos * a.turns[j]) >> 32);
         float sn, cs;
@@ -528,16 +713,18 @@ __global__ void __launch_bounds__(256) rope_kernel(const __grid_constant__ RopeA
         turn_cs[i] = make_float2(a.magnitude * cs, a.magnitude * sn);
     }
     __syncthreads();
-    const int per_token = a.heads_before[a.n] * a.units;
-    for (int i = threadIdx.x; i < here * per_token; i += 256) {
-        const int tok = i / per_token, rem = i - tok * per_token;
-        int head = rem / a.units;
+    const int per_token = (int)a.by_token.d, work = here * per_token;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < work; i += 256) {
+        const int tok = (int)a.by_token(i), rem = i - tok * per_token;
+        int head = (int)a.by_units(rem);
         const int unit = rem - head * a.units;
         int k = 0;
-        while (k + 1 < a.n && head >= a.heads_before[k + 1]) ++k;
+#pragma unroll
+        for (int q = 1; q < 4; ++q) k += q < a.n && head >= a.heads_before[q];
         head -= a.heads_before[k];
         const adloco_rope_tensor& t = a.t[k];
-        const int64_t b = (token0 + tok) / a.T, s = (token0 + tok) - b * a.T;
+        const uint32_t b = a.by_T((uint32_t)(token0 + tok)), s = (uint32_t)(token0 + tok) - b * (uint32_t)a.T;
         const T* in = static_cast<const T*>(t.in) + b * t.in_batch + s * t.in_token + head * t.in_head;
         T* out = static_cast<T*>(t.out) + b * t.out_batch + s * t.out_token + head * t.out_head;
         using V = Pack<T, P>;
@@ -569,23 +756,39 @@ __global__ void __launch_bounds__(256) rope_kernel(const __grid_constant__ RopeA
 }
 
 // ---- quantisation -----------------------------------------------------------------------------------
-// Rows: 16 lanes hold a block of 128.
+// Rows: 16 lanes hold a block of 128, four blocks one after the other with their loads issued together.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) quantise_rows_kernel(const T* x, int64_t x_stride, uint8_t* q, int64_t q_stride,
-                                                            uint8_t* scale, int64_t scale_stride, int64_t rows, int64_t cols,
-                                                            int64_t blocks_per_row) {
-    const int64_t block = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const bool there = block < rows * blocks_per_row;
-    const int64_t row = there ? block / blocks_per_row : 0;
-    const int64_t col = (block - row * blocks_per_row) * 128 + (threadIdx.x & 15) * 8;
-    const int n = there ? (int)min((int64_t)8, cols - col) : 0;
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (n > 0) {
-        if (VEC && n == 8) load8<true>(x + row * x_stride + col, 8, v);
-        else load8<false>(x + row * x_stride + col, n, v);
+                                                            uint8_t* scale, int64_t scale_stride, uint32_t blocks, int64_t cols,
+                                                            const __grid_constant__ FastDiv blocks_per_row) {
+    constexpr int U = 4;
+    const uint32_t b0 = blockIdx.x * (16 * U) + (threadIdx.x >> 4);
+    const int lane_col = (threadIdx.x & 15) * 8;
+    Raw<T> v[U];
+    uint32_t row[U], kb[U];
+    int n[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const uint32_t b = b0 + 16 * k;
+        const bool there = b < blocks;
+        row[k] = there ? blocks_per_row(b) : 0u;
+        kb[k] = there ? b - row[k] * blocks_per_row.d : 0u;
+        const int64_t col = (int64_t)kb[k] * 128 + lane_col;
+        n[k] = there ? (int)min((int64_t)8, cols - col) : 0;
+        v[k] = zero_raw<T>();
+        if (n[k] <= 0) continue;
+        const T* at = x + row[k] * x_stride + col;
+        if (VEC && n[k] == 8) v[k] = load_raw<true>(at, 8);
+        else v[k] = load_raw<false>(at, n[k]);
     }
-    // columns relative to the block: its scale is element 0 of what is passed
-    quantise_block(v, n, q + row * q_stride + (col & ~(int64_t)127), scale + row * scale_stride + (col >> 7), (int)(col & 127));
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        F2 f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = pair_of(v[k], i);
+        // columns relative to the block: its scale is element 0 of what is passed
+        quantise_block(f, n[k], q + row[k] * q_stride + (int64_t)kb[k] * 128, scale + row[k] * scale_stride + kb[k], lane_col);
+    }
 }
 
 // Weights: a block of threads holds a 128 x 128 block (64 elements a thread), agrees on its scale, writes its
@@ -599,18 +802,23 @@ __global__ void __launch_bounds__(256) quantise_weight_kernel(const T* W, int64_
     const int64_t r0 = (int64_t)blockIdx.y * 128, c0 = (int64_t)blockIdx.x * 128;
     const int cl = (threadIdx.x & 15) * 8, rl = threadIdx.x >> 4;
     const int n = (int)max((int64_t)0, min((int64_t)8, cols - (c0 + cl)));
-    float v[8][8];
-    uint32_t m = 0;
+    Raw<T> raw[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int64_t r = r0 + rl + 16 * k;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
+        raw[k] = zero_raw<T>();
         if (r < rows && n > 0) {
-            if (vec && n == 8) load8<true>(W + r * W_stride + c0 + cl, 8, v[k]);
-            else load8<false>(W + r * W_stride + c0 + cl, n, v[k]);
+            if (vec && n == 8) raw[k] = load_raw<true>(W + r * W_stride + c0 + cl, 8);
+            else raw[k] = load_raw<false>(W + r * W_stride + c0 + cl, n);
         }
-        m = max(m, abs_max8(v[k]));
+    }
+    F2 v[4];
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pair_of(raw[k], i);
+        m = max(m, abs_max8(v));
     }
     m = __reduce_max_sync(0xffffffffu, m);
     if ((threadIdx.x & 31) == 0) amax[threadIdx.x >> 5] = m;
@@ -623,7 +831,9 @@ __global__ void __launch_bounds__(256) quantise_weight_kernel(const T* W, int64_
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int64_t r = r0 + rl + 16 * k;
-        const uint2 w = to_e4m3x8(v[k], inv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pair_of(raw[k], i);
+        const uint2 w = to_e4m3x8(v, inv);
         if (r < rows && n > 0) {
             uint8_t* to = q + r * q_stride + c0 + cl;
             if (n == 8) *reinterpret_cast<uint2*>(to) = w;
@@ -704,15 +914,32 @@ int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, 
     return B * rmsnorm_chunks(ctx, B, T, d) * d * (int64_t)sizeof(float);
 }
 
+template <typename XT, typename ST, int TPR, int C, bool VEC, bool GAIN>
+static int rmsnorm_backward_launch(adloco_ctx* ctx, const RmsBackArgs& p, const DropoutKey& key, unsigned grid, cudaStream_t st) {
+    constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
+    auto kernel = rmsnorm_backward_kernel<XT, ST, TPR, C, VEC, GAIN>;
+    size_t smem = VEC ? stage_smem<XT, ST, C, THREADS>() : 0;
+    if (GAIN && ROWS > 1 && smem < (size_t)ROWS * p.a.d * sizeof(float)) smem = (size_t)ROWS * p.a.d * sizeof(float);
+    if (smem > 48 * 1024) {
+        static std::atomic<bool> attr_set[64];   // the attribute is per device
+        if (!attr_set[ctx->device & 63].load()) {
+            ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+            attr_set[ctx->device & 63].store(true);
+        }
+    }
+    kernel<<<grid, THREADS, smem, st>>>(p, key);
+    return ADLOCO_OK;
+}
+
 template <typename XT, typename ST, bool VEC, bool GAIN>
-static void rmsnorm_backward_sized(const RmsBackArgs& p, const DropoutKey& key, cudaStream_t st) {
+static int rmsnorm_backward_sized(adloco_ctx* ctx, const RmsBackArgs& p, const DropoutKey& key, cudaStream_t st) {
     const int64_t d = p.a.d;
     const unsigned grid = (unsigned)(p.a.B * p.chunks);
-#define ADLOCO_LAUNCH(TPR, C)                                                                                                 \
-    rmsnorm_backward_kernel<XT, ST, TPR, C, VEC, GAIN>                                                                        \
-        <<<grid, row_threads(TPR), GAIN && row_threads(TPR) > TPR ? (size_t)(row_threads(TPR) / TPR) * d * sizeof(float) : 0, st>>>(p, key)
+#define ADLOCO_LAUNCH(TPR, C) rc = rmsnorm_backward_launch<XT, ST, TPR, C, VEC, GAIN>(ctx, p, key, grid, st)
+    int rc = ADLOCO_OK;
     ADLOCO_ROW_CASES(ADLOCO_LAUNCH)
 #undef ADLOCO_LAUNCH
+    return rc;
 }
 
 int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_args& a, const DropoutKey& key, cudaStream_t st) {
@@ -724,15 +951,17 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     p.a = a;
     p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d);
     p.rows_per_chunk = (a.T + p.chunks - 1) / p.chunks;
-#define ADLOCO_TYPES(XT, ST)                                                          \
-    if (vec && gain) rmsnorm_backward_sized<XT, ST, true, true>(p, key, st);          \
-    else if (vec) rmsnorm_backward_sized<XT, ST, true, false>(p, key, st);            \
-    else if (gain) rmsnorm_backward_sized<XT, ST, false, true>(p, key, st);           \
-    else rmsnorm_backward_sized<XT, ST, false, false>(p, key, st)
+    int rc = ADLOCO_OK;
+#define ADLOCO_TYPES(XT, ST)                                                               \
+    if (vec && gain) rc = rmsnorm_backward_sized<XT, ST, true, true>(ctx, p, key, st);     \
+    else if (vec) rc = rmsnorm_backward_sized<XT, ST, true, false>(ctx, p, key, st);       \
+    else if (gain) rc = rmsnorm_backward_sized<XT, ST, false, true>(ctx, p, key, st);      \
+    else rc = rmsnorm_backward_sized<XT, ST, false, false>(ctx, p, key, st)
     if (xb && sb) { ADLOCO_TYPES(__nv_bfloat16, __nv_bfloat16); }
     else if (xb) { ADLOCO_TYPES(__nv_bfloat16, float); }
     else { ADLOCO_TYPES(float, float); }
 #undef ADLOCO_TYPES
+    if (rc != ADLOCO_OK) return rc;
     ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
     ctx->launches++;
     if (gain) {
@@ -754,8 +983,10 @@ int launch_dropout(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const 
     a.groups = (rows * cols + 7) / 8;
     const bool flat = rows == 1 || (x_stride == cols && y_stride == cols && (!r || r_stride == cols));
     bool vec = aligned16(x) && aligned16(y) && aligned16(r);
-    if (!flat) vec = vec && (cols & 7) == 0 && vec_rows(x, x_stride, bf16) && vec_rows(y, y_stride, bf16) && vec_rows(r, r_stride, bf16);
-    const int64_t want = (a.groups + 255) / 256, most = (int64_t)ctx->sm_count * 64;
+    if (!flat) vec = vec && (cols & 7) == 0 && cols < 0x7fffffff && vec_rows(x, x_stride, bf16) && vec_rows(y, y_stride, bf16) && vec_rows(r, r_stride, bf16);
+    a.small = a.groups <= 0x7fffffff;
+    a.groups_per_row = FastDiv((uint32_t)(cols < 0x7fffffff ? (cols + 7) / 8 : 1));
+    const int64_t want = (a.groups + 511) / 512, most = (int64_t)ctx->sm_count * 64;
     const unsigned grid = (unsigned)(want < most ? want : most);
 #define ADLOCO_TYPES(T)                                                                          \
     if (flat && vec) dropout_kernel<T, true, true><<<grid, 256, 0, st>>>(a, key);                \
@@ -811,6 +1042,8 @@ int launch_rope(adloco_ctx* ctx, int bf16, const adloco_rope_tensor* t, int n, i
     if (tpb > 16) tpb = 16;
     if (tpb < 1) tpb = 1;
     a.tokens_per_block = (int)tpb;
+    a.by_half = FastDiv((uint32_t)(R / 2)); a.by_token = FastDiv((uint32_t)per_token);
+    a.by_units = FastDiv((uint32_t)a.units); a.by_T = FastDiv((uint32_t)T);
     const unsigned grid = (unsigned)((a.tokens + tpb - 1) / tpb);
     const size_t smem = (size_t)tpb * (size_t)(R / 2) * sizeof(float2);
     if (smem > 48 * 1024) return ADLOCO_ERR_UNSUPPORTED;
@@ -835,12 +1068,13 @@ int launch_rope(adloco_ctx* ctx, int bf16, const adloco_rope_tensor* t, int n, i
 
 int launch_blockscale_quantize(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const void* x, int64_t x_stride, void* q,
                                int64_t q_stride, uint8_t* scale, int64_t scale_stride, cudaStream_t st) {
-    const int64_t per_row = (cols + 127) / 128, grid = (rows * per_row + 15) / 16;
-    if (grid > 0x7fffffff) return ADLOCO_ERR_UNSUPPORTED;
+    const int64_t per_row = (cols + 127) / 128;
+    if (rows > 0x7fffffff / per_row) return ADLOCO_ERR_UNSUPPORTED;
+    const uint32_t blocks = (uint32_t)(rows * per_row), grid = (blocks + 63) / 64;
     const bool vec = vec_rows(x, x_stride, bf16);
-#define ADLOCO_LAUNCH(T, V)                                                                                                  \
-    quantise_rows_kernel<T, V><<<(unsigned)grid, 256, 0, st>>>(static_cast<const T*>(x), x_stride, static_cast<uint8_t*>(q), \
-                                                               q_stride, scale, scale_stride, rows, cols, per_row)
+#define ADLOCO_LAUNCH(T, V)                                                                                          \
+    quantise_rows_kernel<T, V><<<grid, 256, 0, st>>>(static_cast<const T*>(x), x_stride, static_cast<uint8_t*>(q),   \
+                                                     q_stride, scale, scale_stride, blocks, cols, FastDiv((uint32_t)per_row))
     if (bf16 && vec) ADLOCO_LAUNCH(__nv_bfloat16, true);
     else if (bf16) ADLOCO_LAUNCH(__nv_bfloat16, false);
     else if (vec) ADLOCO_LAUNCH(float, true);

@@ -199,10 +199,17 @@ typedef CUresult (*TensorMapEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_
 TensorMapEncode tensor_map_encode(adloco_ctx* ctx);
 
 // ---- between the linear layers, implemented in block_kernels.cu -------------------
+// A dropout mask as the kernels take it: the generator's key schedule is formed once on the host, so that a round's
+// key is an operand from the constant bank.
 struct DropoutKey {
-    uint32_t drop = 0;        // an element stays when its 16 bits are >= drop (0: none dropped, 65536: all)
-    float scale = 1.f;        // of the elements that stay
-    uint32_t seed_lo = 0, seed_hi = 0, off_lo = 0, off_hi = 0;
+    uint32_t round[20] = {0};           // of round r: [2 r], [2 r + 1]
+    uint32_t off_lo = 0, off_hi = 0;
+    uint32_t on = 0;                    // any element is dropped at all
+    float keep = 1.f, scale = 1.f;      // the share that stays (exact), and 1 / keep; both 1 where none is dropped, or all are
+    // two 16-bit numbers are compared with the drop threshold at a time: the threshold in both halves, and the byte
+    // selectors that spread a half's top bit over that half (pair), or over 32 bits (low, high); they select zero
+    // bytes when all are dropped
+    uint32_t limit = 0, pair = 0xBB99u, low = 0x9999u, high = 0xBBBBu;
 };
 int launch_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const DropoutKey& key, cudaStream_t st);
 int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d);
