@@ -47,15 +47,6 @@ static void* device_address_of_pinned(void* host) {
     return at.type == cudaMemoryTypeHost ? at.devicePointer : nullptr;
 }
 
-// thread-block clusters of two CTAs need compute capability 9.0 or later and the launch attribute
-bool pair_launch_ok(adloco_ctx* ctx) {
-    if (ctx->pair_ok < 0) {
-        int v = 0;
-        ctx->pair_ok = (cudaDeviceGetAttribute(&v, cudaDevAttrClusterLaunch, ctx->device) == cudaSuccess && v != 0) ? 1 : 0;
-    }
-    return ctx->pair_ok == 1;
-}
-
 }  // namespace
 
 extern "C" {
@@ -300,7 +291,7 @@ static int gram_route(adloco_ctx* ctx, const void* X, const void* D, int64_t B, 
     if (grad_sum && !aligned16(grad_sum)) return ADLOCO_ERR_ALIGNMENT;
     DeviceGuard g(ctx->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (variant == 1 && !pair_launch_ok(ctx)) return ADLOCO_ERR_UNSUPPORTED;
+    if (variant == 1 && !cta_pairs_possible(ctx)) return ADLOCO_ERR_UNSUPPORTED;
     if (variant < 0) variant = 0;
     int rc = variant == 1 ? launch_gram_pair(ctx, X, D, B, T, d_in, d_out, per_sample_sqnorm, accumulate_norms, st)
                           : launch_gram_sqnorm(ctx, X, D, B, T, d_in, d_out, per_sample_sqnorm, accumulate_norms, st);
@@ -379,8 +370,8 @@ int adloco_linear_sqnorm(adloco_ctx* ctx, const void* X, const void* D, int64_t 
     DeviceGuard g(ctx->device);
     // the automatic route takes the CTA-pair form of the direct kernel where clusters can be launched
     // and the tile is at least one pair's worth of rows
-    if (was_auto && method == ADLOCO_LINEAR_DIRECT && d_out > 128 && pair_launch_ok(ctx)) method = ADLOCO_LINEAR_DIRECT_PAIR;
-    if (method == ADLOCO_LINEAR_DIRECT_PAIR && !pair_launch_ok(ctx)) return ADLOCO_ERR_UNSUPPORTED;
+    if (was_auto && method == ADLOCO_LINEAR_DIRECT && d_out > 128 && cta_pairs_possible(ctx)) method = ADLOCO_LINEAR_DIRECT_PAIR;
+    if (method == ADLOCO_LINEAR_DIRECT_PAIR && !cta_pairs_possible(ctx)) return ADLOCO_ERR_UNSUPPORTED;
     return launch_direct_sqnorm(ctx, X, D, B, T, d_in, d_out, per_sample_sqnorm, accumulate_norms, grad_sum,
                                 accumulate_sum, method == ADLOCO_LINEAR_DIRECT_PAIR, static_cast<cudaStream_t>(stream));
 }
@@ -401,10 +392,10 @@ int adloco_linear_sqnorm_group(adloco_ctx* ctx, const adloco_linear_layer* layer
     DeviceGuard g(ctx->device);
     int pair = 0;
     if (method == ADLOCO_LINEAR_DIRECT_PAIR) {
-        if (!pair_launch_ok(ctx)) return ADLOCO_ERR_UNSUPPORTED;
+        if (!cta_pairs_possible(ctx)) return ADLOCO_ERR_UNSUPPORTED;
         pair = 1;
     } else if (method == ADLOCO_LINEAR_AUTO) {
-        pair = pair_launch_ok(ctx) ? 1 : 0;
+        pair = cta_pairs_possible(ctx) ? 1 : 0;
     }
     return launch_direct_group(ctx, layers, n_layers, B, T, per_sample_sqnorm, accumulate_norms, accumulate_sum, pair,
                                static_cast<cudaStream_t>(stream));

@@ -94,6 +94,15 @@ struct DeviceGuard {
     ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
 };
 
+// thread-block clusters of two CTAs need compute capability 9.0 or later and the launch attribute
+inline bool cta_pairs_possible(adloco_ctx* ctx) {
+    if (ctx->pair_ok < 0) {
+        int v = 0;
+        ctx->pair_ok = (cudaDeviceGetAttribute(&v, cudaDevAttrClusterLaunch, ctx->device) == cudaSuccess && v != 0) ? 1 : 0;
+    }
+    return ctx->pair_ok == 1;
+}
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 inline int check_params(const adloco_test_params* p) {

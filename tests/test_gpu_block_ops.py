@@ -338,7 +338,8 @@ def test_norm_to_8_bits(ctx, d):
 
 
 MATMULS = [(1, 1, 1), (1, 128, 128), (3, 5, 7), (2, 200, 33), (5, 2048, 640), (8, 300, 1100), (9, 256, 128), (17, 1000, 520), (64, 512, 2048),
-           (100, 96, 4096), (128, 128, 512), (129, 257, 130), (257, 384, 768), (300, 1001, 1000), (512, 768, 2304), (1000, 2304, 768), (4, 4096, 16)]
+           (100, 96, 4096), (128, 128, 512), (129, 257, 130), (257, 384, 768), (300, 1001, 1000), (512, 768, 2304), (1000, 2304, 768), (4, 4096, 16),
+           (2600, 2304, 768), (5003, 1000, 1100), (2305, 2050, 130), (20000, 129, 640)]
 
 
 @pytest.mark.parametrize("M,N,K", MATMULS)
@@ -390,6 +391,27 @@ def test_matmul_of_whole_numbers_is_exact(ctx, M, N, K):
     assert np.array_equal(np64(out), ref)
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 40, 1), (5, 130, 129), (200, 300, 1001), (2600, 2304, 135), (3, 64, 2060)])
+def test_what_lies_between_the_rows_is_not_looked_at(ctx, M, N, K):
+    """The bytes between a row's end and the next row, and the scale bytes there, may hold anything (NaN here)."""
+    g = torch.Generator().manual_seed(1)
+    x = torch.randint(-8, 9, (M, K), generator=g).float().to(DEV)
+    w = torch.randint(-8, 9, (N, K), generator=g).float().to(DEV)
+    kb = (K + 127) // 128
+    full = [torch.full((r, (c + 15) // 16 * 16 + 16), 0x7F, dtype=torch.uint8, device=DEV) for r, c in ((M, K), (N, K))]
+    a, b = full[0][:, :K], full[1][:, :K]
+    a.copy_(x.to(torch.float8_e4m3fn).view(torch.uint8))
+    b.copy_(w.to(torch.float8_e4m3fn).view(torch.uint8))
+    sa = torch.full((M, (kb + 3) // 4 * 4 + 4), 255, dtype=torch.uint8, device=DEV)[:, :kb]
+    sa.fill_(127)
+    sb = torch.full(((N + 127) // 128, kb + 3), 255, dtype=torch.uint8, device=DEV)[:, :kb]
+    sb.fill_(127)
+    out = torch.empty(M, N, device=DEV)
+    ctx.blockscale_matmul(a, sa, b, sb, out)
+    torch.cuda.synchronize()
+    assert np.array_equal(np64(out), np64(x) @ np64(w).T)
+
+
 @pytest.mark.parametrize("M", [2, 40, 300])
 def test_matmul_propagates_nan_blocks_only_where_they_are(ctx, M):
     N, K = 256, 384
@@ -405,11 +427,11 @@ def test_matmul_propagates_nan_blocks_only_where_they_are(ctx, M):
     assert torch.isnan(out[1]).all() and torch.isfinite(out[torch.arange(M, device=DEV) != 1]).all()
 
 
-def test_matmul_wait_that_runs_out_is_reported_and_the_context_stays_usable(ctx):
-    M, N, K = 300, 256, 512
+@pytest.mark.parametrize("M,N,K", [(300, 256, 512), (2600, 2304, 512)])
+def test_matmul_wait_that_runs_out_is_reported_and_the_context_stays_usable(ctx, M, N, K):
     x, W = rnd(1, M, K, dtype=BF), rnd(2, N, K)
     a, sa, b = pitched(M, K, 16), pitched(M, 4, 4), pitched(N, K, 16)
-    sb = torch.zeros(2, 4, dtype=torch.uint8, device=DEV)
+    sb = torch.zeros(N // 128, 4, dtype=torch.uint8, device=DEV)
     ctx.blockscale_quantize(x, a, sa)
     ctx.blockscale_quantize_weight(W, b, sb)
     out, again = torch.zeros(M, N, device=DEV), torch.zeros(M, N, device=DEV)
