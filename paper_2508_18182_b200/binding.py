@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -72,41 +73,12 @@ class LinearLayer(C.Structure):
                 ("grad_sum", C.c_void_p)]
 
 
-class RmsnormArgs(C.Structure):
-    _fields_ = [("dtype", C.c_int), ("stream_dtype", C.c_int), ("gain_dtype", C.c_int), ("eps", C.c_float),
-                ("rows", C.c_int64), ("d", C.c_int64), ("x", C.c_void_p), ("x_stride", C.c_int64),
-                ("residual", C.c_void_p), ("residual_stride", C.c_int64), ("gain", C.c_void_p),
-                ("h", C.c_void_p), ("h_stride", C.c_int64), ("y", C.c_void_p), ("y_stride", C.c_int64),
-                ("rstd", C.c_void_p), ("q", C.c_void_p), ("q_stride", C.c_int64),
-                ("q_scale", C.c_void_p), ("q_scale_stride", C.c_int64),
-                ("dropout_p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64)]
-
-
-class RmsnormBackwardArgs(C.Structure):
-    _fields_ = [("dtype", C.c_int), ("stream_dtype", C.c_int), ("gain_dtype", C.c_int),
-                ("accumulate_norms", C.c_int32), ("accumulate_sum", C.c_int32), ("reserved", C.c_int32),
-                ("B", C.c_int64), ("T", C.c_int64), ("d", C.c_int64), ("dy", C.c_void_p), ("dy_stride", C.c_int64),
-                ("h", C.c_void_p), ("h_stride", C.c_int64), ("rstd", C.c_void_p), ("gain", C.c_void_p),
-                ("dh_residual", C.c_void_p), ("dh_residual_stride", C.c_int64), ("dh", C.c_void_p), ("dh_stride", C.c_int64),
-                ("dx", C.c_void_p), ("dx_stride", C.c_int64),
-                ("dropout_p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64),
-                ("per_sample_sqnorm", C.c_void_p), ("grad_sum", C.c_void_p), ("workspace", C.c_void_p),
-                ("workspace_bytes", C.c_int64)]
-
-
-class RopeTensor(C.Structure):
-    _fields_ = [("inp", C.c_void_p), ("out", C.c_void_p), ("heads", C.c_int64),
-                ("in_batch", C.c_int64), ("in_token", C.c_int64), ("in_head", C.c_int64),
-                ("out_batch", C.c_int64), ("out_token", C.c_int64), ("out_head", C.c_int64)]
-
-
-class BlockscaleMatmulArgs(C.Structure):
-    _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("a", C.c_void_p), ("a_stride", C.c_int64),
-                ("a_scale", C.c_void_p), ("a_scale_stride", C.c_int64), ("b", C.c_void_p), ("b_stride", C.c_int64),
-                ("b_scale", C.c_void_p), ("b_scale_stride_n", C.c_int64), ("b_scale_stride_k", C.c_int64),
-                ("bias", C.c_void_p), ("out", C.c_void_p), ("out_stride", C.c_int64), ("out_dtype", C.c_int),
-                ("reserved", C.c_int32)]
-
+# Argument structs of the operators between the linear layers, packed in C layout (struct's native alignment): a
+# ctypes Structure costs more to fill than the call it is for.
+RMSNORM_ARGS = struct.Struct("@iiifqqPqPqPPqPqPPqPqdQQ")                    # adloco_rmsnorm_args
+RMSNORM_BACKWARD_ARGS = struct.Struct("@iiiiiiqqqPqPqPPPqPqPqdQQPPPq")      # adloco_rmsnorm_backward_args
+ROPE_TENSOR = struct.Struct("@PPqqqqqqq")                                   # adloco_rope_tensor
+BLOCKSCALE_MATMUL_ARGS = struct.Struct("@qqqPqPqPqPqqPPqii")                # adloco_blockscale_matmul_args
 
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
 LINEAR_METHODS = {"auto": 0, "gram": 1, "direct": 2, "pair": 3, "gram_one_cta": 4, "gram_pair": 5}
@@ -161,15 +133,15 @@ def load_library() -> C.CDLL:
         "adloco_refresh_instance": (C.c_int, [vp, vp, vp, C.c_int, i64, vp]),
         "adloco_check_merge": (C.c_int, [C.POINTER(i64), i32, i32, C.POINTER(i32)]),
         "adloco_merge": (C.c_int, [vp, C.POINTER(vp), C.POINTER(i64), C.c_int, i32, i64, vp, C.POINTER(i32), vp]),
-        "adloco_add_rmsnorm": (C.c_int, [vp, C.POINTER(RmsnormArgs), vp]),
-        "adloco_add_rmsnorm_backward": (C.c_int, [vp, C.POINTER(RmsnormBackwardArgs), vp]),
+        "adloco_add_rmsnorm": (C.c_int, [vp, C.c_char_p, vp]),
+        "adloco_add_rmsnorm_backward": (C.c_int, [vp, C.c_char_p, vp]),
         "adloco_add_rmsnorm_backward_workspace": (i64, [vp, i64, i64, i64]),
         "adloco_dropout": (C.c_int, [vp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, C.c_double, C.c_uint64, C.c_uint64, vp]),
         "adloco_rope_frequencies": (C.c_int, [i32, C.c_double, i32, C.c_double, C.c_double, C.c_double, C.c_double, vp]),
-        "adloco_rope": (C.c_int, [vp, C.c_int, C.POINTER(RopeTensor), i32, i64, i64, i64, i64, vp, f32, vp, i64, i64, C.c_int, C.c_int, vp]),
+        "adloco_rope": (C.c_int, [vp, C.c_int, C.c_char_p, i32, i64, i64, i64, i64, vp, f32, vp, i64, i64, C.c_int, C.c_int, vp]),
         "adloco_blockscale_quantize": (C.c_int, [vp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
         "adloco_blockscale_quantize_weight": (C.c_int, [vp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
-        "adloco_blockscale_matmul": (C.c_int, [vp, C.POINTER(BlockscaleMatmulArgs), vp]),
+        "adloco_blockscale_matmul": (C.c_int, [vp, C.c_char_p, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -198,12 +170,16 @@ def _dtype_code(dt):
 
 def _rows(t, what):
     """(rows, d, pitch) of a tensor [..., d] whose leading dimensions are one run of evenly spaced rows."""
-    shape, stride = t.shape, t.stride()
-    n = len(shape)
-    if n < 1 or (stride[-1] != 1 and shape[-1] > 1):
-        raise AdlocoError(ERR_INVALID_ARG, f"{what}: the last dimension must be contiguous")
+    shape = t.shape
+    if not shape:
+        raise AdlocoError(ERR_INVALID_ARG, f"{what}: a tensor of rows is needed")
     d = shape[-1]
-    rows, pitch, i = 1, d, n - 2
+    if t.is_contiguous():
+        return (t.numel() // d if d else 0), d, d
+    stride = t.stride()
+    if stride[-1] != 1 and d > 1:
+        raise AdlocoError(ERR_INVALID_ARG, f"{what}: the last dimension must be contiguous")
+    rows, pitch, i = 1, d, len(shape) - 2
     while i >= 0:                       # a dimension of extent one puts no demand on its stride
         if shape[i] != 1:
             if rows == 1:
@@ -215,21 +191,23 @@ def _rows(t, what):
     return rows, d, pitch
 
 
-def _rows_like(t, what, rows, d, dtype, device):
-    """Pointer and pitch of an optional tensor that must have the given rows, width, type and device."""
+def _rows_like(t, what, rows, d, dtype, dev):
+    """Pointer and pitch of an optional tensor that must have the given rows, width, type and device index."""
     if t is None:
-        return None, 0
+        return 0, 0
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.size(-1) == d and t.numel() == rows * d:
+        return t.data_ptr(), d
     r, w, pitch = _rows(t, what)
-    if r != rows or w != d or t.dtype != dtype or t.device != device:
-        raise AdlocoError(ERR_INVALID_ARG, f"{what}: expected {rows} rows of {d} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if r != rows or w != d or t.dtype is not dtype or t.get_device() != dev:
+        raise AdlocoError(ERR_INVALID_ARG, f"{what}: expected {rows} rows of {d} {dtype} on device {dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr(), pitch
 
 
-def _vector(t, what, n, dtype, device):
+def _vector(t, what, n, dtype, dev):
     if t is None:
-        return None
-    if t.numel() != n or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise AdlocoError(ERR_INVALID_ARG, f"{what}: expected {n} contiguous {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+        return 0
+    if t.numel() != n or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise AdlocoError(ERR_INVALID_ARG, f"{what}: expected {n} contiguous {dtype} on device {dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
@@ -427,9 +405,15 @@ class Context:
 
     # ------------------------------------------------------------------ between the linear layers
     def _on(self, t, what):
-        if t.device != self.device:
+        """The context's device index, which the tensor must be on."""
+        dev = self.device.index
+        if t.get_device() != dev:
             raise AdlocoError(ERR_INVALID_ARG, f"{what} is on {t.device}, the context on {self.device}")
-        return t.device
+        return dev
+
+    def _on_stream(self, stream):
+        """The given stream, or the current one of the context's device."""
+        return torch._C._cuda_getCurrentRawStream(self.device.index) if stream is None else stream.cuda_stream
 
     def add_rmsnorm(self, x, gain, *, residual=None, h=None, y=None, rstd=None, q=None, q_scale=None, eps=1e-5,
                     dropout=None, stream=None):
@@ -438,17 +422,20 @@ class Context:
         (p, seed, offset) or None.  q is float8_e4m3fn or uint8, q_scale uint8 [rows, ceil(d / 128)]."""
         dev = self._on(x, "x")
         rows, d, xs = _rows(x, "x")
-        like = residual if residual is not None else h
-        st = x.dtype if like is None else like.dtype
+        xt = x.dtype
+        st = residual.dtype if residual is not None else xt if h is None else h.dtype
         rp, rs = _rows_like(residual, "residual", rows, d, st, dev)
         hp, hs = _rows_like(h, "h", rows, d, st, dev)
-        yp, ys = _rows_like(y, "y", rows, d, x.dtype, dev)
-        qp, qs, sp, ss = self._bytes(q, q_scale, rows, d, "q", dev) if q is not None or q_scale is not None else (None, 0, None, 0)
-        p, seed, offset = _dropout_key(dropout)
-        a = RmsnormArgs(_dtype_code(x.dtype), _dtype_code(st), _dtype_code(gain.dtype), eps, rows, d, x.data_ptr(), xs, rp, rs,
-                        _vector(gain, "gain", d, gain.dtype, dev), hp, hs, yp, ys, _vector(rstd, "rstd", rows, torch.float32, dev),
-                        qp, qs, sp, ss, p, seed, offset)
-        self.check(self.lib.adloco_add_rmsnorm(self.h, C.byref(a), _stream(stream)), "adloco_add_rmsnorm")
+        yp, ys = _rows_like(y, "y", rows, d, xt, dev)
+        qp, qs, sp, ss = self._bytes(q, q_scale, rows, d, "q", dev) if q is not None or q_scale is not None else (0, 0, 0, 0)
+        p, seed, offset = (0.0, 0, 0) if dropout is None else _dropout_key(dropout)
+        code = _dtype_code(xt)
+        a = RMSNORM_ARGS.pack(code, code if st is xt else _dtype_code(st), _dtype_code(gain.dtype), eps, rows, d, x.data_ptr(), xs,
+                              rp, rs, _vector(gain, "gain", d, gain.dtype, dev), hp, hs, yp, ys,
+                              _vector(rstd, "rstd", rows, torch.float32, dev), qp, qs, sp, ss, p, seed, offset)
+        rc = self.lib.adloco_add_rmsnorm(self.h, a, self._on_stream(stream))
+        if rc != OK:
+            self.check(rc, "adloco_add_rmsnorm")
 
     def add_rmsnorm_backward(self, dy, h, rstd, gain, dh, *, dh_residual=None, dx=None, dropout=None, per_sample_sqnorm=None,
                              accumulate_norms=False, grad_sum=None, accumulate_sum=False, workspace=None, stream=None):
@@ -459,28 +446,33 @@ class Context:
         rows, d, dys = _rows(dy, "dy")
         B = dy.shape[0] if dy.dim() == 3 else 1
         T = rows // B if B else 0
-        hp, hs = _rows_like(h, "h", rows, d, h.dtype, dev)
-        rp, rs = _rows_like(dh_residual, "dh_residual", rows, d, h.dtype, dev)
-        op, os_ = _rows_like(dh, "dh", rows, d, h.dtype, dev)
-        xp, xs = _rows_like(dx, "dx", rows, d, dy.dtype, dev)
-        p, seed, offset = _dropout_key(dropout)
-        ws = None
+        dt, ht = dy.dtype, h.dtype
+        hp, hs = _rows_like(h, "h", rows, d, ht, dev)
+        rp, rs = _rows_like(dh_residual, "dh_residual", rows, d, ht, dev)
+        op, os_ = _rows_like(dh, "dh", rows, d, ht, dev)
+        xp, xs = _rows_like(dx, "dx", rows, d, dt, dev)
+        p, seed, offset = (0.0, 0, 0) if dropout is None else _dropout_key(dropout)
+        wp = wn = 0
         if per_sample_sqnorm is not None or grad_sum is not None:
             if workspace is None:
                 n = self.rmsnorm_backward_workspace(B, T, d)
                 if stream is None:
-                    workspace = torch.empty(n, dtype=torch.uint8, device=dev)
+                    workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
                 else:
                     with torch.cuda.stream(stream):
-                        workspace = torch.empty(n, dtype=torch.uint8, device=dev)
-            ws = _vector(workspace, "workspace", workspace.numel(), torch.uint8, dev)
-        a = RmsnormBackwardArgs(_dtype_code(dy.dtype), _dtype_code(h.dtype), _dtype_code(gain.dtype), bool(accumulate_norms),
-                                bool(accumulate_sum), 0, B, T, d, dy.data_ptr(), dys, hp, hs,
-                                _vector(rstd, "rstd", rows, torch.float32, dev), _vector(gain, "gain", d, gain.dtype, dev), rp, rs,
-                                op, os_, xp, xs, p, seed, offset,
-                                _vector(per_sample_sqnorm, "per_sample_sqnorm", B, torch.float32, dev),
-                                _vector(grad_sum, "grad_sum", d, torch.float32, dev), ws, 0 if ws is None else workspace.numel())
-        self.check(self.lib.adloco_add_rmsnorm_backward(self.h, C.byref(a), _stream(stream)), "adloco_add_rmsnorm_backward")
+                        workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+            wn = workspace.numel()
+            wp = _vector(workspace, "workspace", wn, torch.uint8, dev)
+        code = _dtype_code(dt)
+        a = RMSNORM_BACKWARD_ARGS.pack(code, code if ht is dt else _dtype_code(ht), _dtype_code(gain.dtype), accumulate_norms,
+                                       accumulate_sum, 0, B, T, d, dy.data_ptr(), dys, hp, hs,
+                                       _vector(rstd, "rstd", rows, torch.float32, dev), _vector(gain, "gain", d, gain.dtype, dev),
+                                       rp, rs, op, os_, xp, xs, p, seed, offset,
+                                       _vector(per_sample_sqnorm, "per_sample_sqnorm", B, torch.float32, dev),
+                                       _vector(grad_sum, "grad_sum", d, torch.float32, dev), wp, wn)
+        rc = self.lib.adloco_add_rmsnorm_backward(self.h, a, self._on_stream(stream))
+        if rc != OK:
+            self.check(rc, "adloco_add_rmsnorm_backward")
 
     def rmsnorm_backward_workspace(self, B, T, d) -> int:
         return self.lib.adloco_add_rmsnorm_backward_workspace(self.h, B, T, d)
@@ -492,45 +484,51 @@ class Context:
         rp, rs = _rows_like(residual, "residual", rows, d, x.dtype, dev)
         op, os_ = _rows_like(out, "out", rows, d, x.dtype, dev)
         p, seed, offset = _dropout_key((p, seed, offset))
-        self.check(self.lib.adloco_dropout(self.h, _dtype_code(x.dtype), rows, d, x.data_ptr(), xs, rp, rs, op, os_, p, seed,
-                                           offset, _stream(stream)), "adloco_dropout")
+        rc = self.lib.adloco_dropout(self.h, _dtype_code(x.dtype), rows, d, x.data_ptr(), xs, rp, rs, op, os_, p, seed,
+                                     offset, self._on_stream(stream))
+        if rc != OK:
+            self.check(rc, "adloco_dropout")
 
     def rope(self, tensors, table, *, outs=None, positions=None, first_position=0, interleaved=False, inverse=False,
              stream=None):
         """adloco_rope on tensors [B, T, heads, head_dim] of one B, T, head_dim and type (any strides but the last);
         outs default to in place.  positions: int32 [B, T], or first_position + t."""
         outs = tensors if outs is None else outs
-        x = tensors[0]
-        dev = self._on(x, "tensors[0]")
-        if x.dim() != 4 or len(outs) != len(tensors):
+        dev = self._on(tensors[0], "tensors[0]")
+        if tensors[0].dim() != 4 or len(outs) != len(tensors):
             raise AdlocoError(ERR_INVALID_ARG, "tensors are [B, T, heads, head_dim], with as many outs")
-        B, T, _, D = x.shape
-        dtype = x.dtype
-        arr = (RopeTensor * len(tensors))()
-        for i, (t, o) in enumerate(zip(tensors, outs)):
-            s, u = t.stride(), o.stride()
-            n = t.shape[2] if t.dim() == 4 else -1
-            if (t.shape != (B, T, n, D) or o.shape != t.shape or t.dtype != dtype or o.dtype != dtype or t.device != dev
-                    or o.device != dev or (D > 1 and (s[3] != 1 or u[3] != 1))):
-                raise AdlocoError(ERR_INVALID_ARG, "tensors and outs must share B, T, head_dim, type and device, with head_dim contiguous")
-            arr[i] = RopeTensor(t.data_ptr(), o.data_ptr(), n, s[0], s[1], s[2], u[0], u[1], u[2])
-        pp, ps = None, 0
+        B, T, _, D = tensors[0].shape
+        dtype = tensors[0].dtype
+        packed = b""
+        for t, o in zip(tensors, outs):
+            shape = t.shape
+            if (len(shape) != 4 or shape[0] != B or shape[1] != T or shape[3] != D or o.shape != shape or t.dtype is not dtype
+                    or o.dtype is not dtype or t.get_device() != dev or o.get_device() != dev):
+                raise AdlocoError(ERR_INVALID_ARG, "tensors and outs must share B, T, head_dim, type and device")
+            ib, it, ih, i1 = t.stride()
+            ob, ot, oh, o1 = o.stride()
+            if D > 1 and (i1 != 1 or o1 != 1):
+                raise AdlocoError(ERR_INVALID_ARG, "head_dim must be contiguous")
+            packed += ROPE_TENSOR.pack(t.data_ptr(), o.data_ptr(), shape[2], ib, it, ih, ob, ot, oh)
+        pp, ps = 0, 0
         if positions is not None:
-            if (positions.dtype != torch.int32 or positions.shape != (B, T) or positions.device != dev
+            if (positions.dtype is not torch.int32 or positions.shape != (B, T) or positions.get_device() != dev
                     or (T > 1 and positions.stride(1) != 1)):
                 raise AdlocoError(ERR_INVALID_ARG, "positions must be int32 [B, T] with contiguous rows")
             pp, ps = positions.data_ptr(), positions.stride(0) if B > 1 else T
-        if table.turns.device != dev:
+        if table.turns.get_device() != dev:
             raise AdlocoError(ERR_INVALID_ARG, f"the table is on {table.turns.device}")
-        self.check(self.lib.adloco_rope(self.h, _dtype_code(dtype), arr, len(tensors), B, T, D, table.rot_dim, table.turns.data_ptr(),
-                                        table.magnitude, pp, ps, first_position, interleaved, inverse, _stream(stream)), "adloco_rope")
+        rc = self.lib.adloco_rope(self.h, _dtype_code(dtype), packed, len(tensors), B, T, D, table.rot_dim, table.turns.data_ptr(),
+                                  table.magnitude, pp, ps, first_position, interleaved, inverse, self._on_stream(stream))
+        if rc != OK:
+            self.check(rc, "adloco_rope")
 
     @staticmethod
     def _bytes(q, scale, rows, cols, what, dev):
         """Pointers and pitches of an 8-bit matrix and its row scales."""
         if q is None or scale is None:
             raise AdlocoError(ERR_INVALID_ARG, f"{what} and its scales go together")
-        qp, qs = _rows_like(q, what, rows, cols, torch.uint8 if q.dtype == torch.uint8 else torch.float8_e4m3fn, dev)
+        qp, qs = _rows_like(q, what, rows, cols, torch.uint8 if q.dtype is torch.uint8 else torch.float8_e4m3fn, dev)
         sp, ss = _rows_like(scale, what + "_scale", rows, (cols + 127) // 128, torch.uint8, dev)
         if rows == 1:                    # a single row has no pitch: any that fits the rules will do
             qs, ss = (cols + 15) // 16 * 16, (ss + 3) // 4 * 4
@@ -542,22 +540,26 @@ class Context:
         dev = self._on(x, "x")
         rows, d, xs = _rows(x, "x")
         qp, qs, sp, ss = self._bytes(q, scale, rows, d, "q", dev)
-        self.check(self.lib.adloco_blockscale_quantize(self.h, _dtype_code(x.dtype), rows, d, x.data_ptr(), xs, qp, qs, sp, ss,
-                                                       _stream(stream)), "adloco_blockscale_quantize")
+        rc = self.lib.adloco_blockscale_quantize(self.h, _dtype_code(x.dtype), rows, d, x.data_ptr(), xs, qp, qs, sp, ss,
+                                                 self._on_stream(stream))
+        if rc != OK:
+            self.check(rc, "adloco_blockscale_quantize")
 
     def blockscale_quantize_weight(self, W, q, scale, *, q_t=None, stream=None):
         """adloco_blockscale_quantize_weight: W [rows, cols] to e4m3 with one scale for each 128 x 128 block (scale uint8
         [ceil(rows / 128), ceil(cols / 128)]), and its transposed copy into q_t [cols, rows]."""
         dev = self._on(W, "W")
         rows, cols, ws = _rows(W, "W")
-        f8 = torch.uint8 if q.dtype == torch.uint8 else torch.float8_e4m3fn
+        f8 = torch.uint8 if q.dtype is torch.uint8 else torch.float8_e4m3fn
         qp, qs = _rows_like(q, "q", rows, cols, f8, dev)
         tp, ts = _rows_like(q_t, "q_t", cols, rows, f8, dev)
         sp, ss = _rows_like(scale, "scale", (rows + 127) // 128, (cols + 127) // 128, torch.uint8, dev)
         qs = qs if rows > 1 else (cols + 15) // 16 * 16
         ts = ts if cols > 1 else (rows + 15) // 16 * 16
-        self.check(self.lib.adloco_blockscale_quantize_weight(self.h, _dtype_code(W.dtype), rows, cols, W.data_ptr(), ws, qp, qs, tp, ts,
-                                                              sp, ss, _stream(stream)), "adloco_blockscale_quantize_weight")
+        rc = self.lib.adloco_blockscale_quantize_weight(self.h, _dtype_code(W.dtype), rows, cols, W.data_ptr(), ws, qp, qs, tp, ts,
+                                                        sp, ss, self._on_stream(stream))
+        if rc != OK:
+            self.check(rc, "adloco_blockscale_quantize_weight")
 
     def blockscale_matmul(self, a, a_scale, b, b_scale, out, *, scale_transposed=False, bias=None, stream=None):
         """adloco_blockscale_matmul: out [M, N] = a [M, K] b [N, K]^T (+ bias) in 8 bits.  b_scale holds b's 128 x 128
@@ -566,15 +568,23 @@ class Context:
         M, K, _ = _rows(a, "a")
         N = b.shape[0]
         ap, as_, sp, ss = self._bytes(a, a_scale, M, K, "a", dev)
-        bp, bs = _rows_like(b, "b", N, K, torch.uint8 if b.dtype == torch.uint8 else torch.float8_e4m3fn, dev)
+        bp, bs = _rows_like(b, "b", N, K, torch.uint8 if b.dtype is torch.uint8 else torch.float8_e4m3fn, dev)
         if N == 1:
             bs = (K + 15) // 16 * 16
         nb, kb = (N + 127) // 128, (K + 127) // 128
-        bsp, pitch = _rows_like(b_scale, "b_scale", *((kb, nb) if scale_transposed else (nb, kb)), torch.uint8, dev)
-        op, os_ = _rows_like(out, "out", M, N, out.dtype, dev)
-        args = BlockscaleMatmulArgs(M, N, K, ap, as_, sp, ss, bp, bs, bsp, *((1, pitch) if scale_transposed else (pitch, 1)),
-                                    _vector(bias, "bias", N, torch.float32, dev), op, os_, _dtype_code(out.dtype), 0)
-        self.check(self.lib.adloco_blockscale_matmul(self.h, C.byref(args), _stream(stream)), "adloco_blockscale_matmul")
+        if scale_transposed:
+            bsp, sk = _rows_like(b_scale, "b_scale", kb, nb, torch.uint8, dev)
+            sn = 1
+        else:
+            bsp, sn = _rows_like(b_scale, "b_scale", nb, kb, torch.uint8, dev)
+            sk = 1
+        ot = out.dtype
+        op, os_ = _rows_like(out, "out", M, N, ot, dev)
+        args = BLOCKSCALE_MATMUL_ARGS.pack(M, N, K, ap, as_, sp, ss, bp, bs, bsp, sn, sk, _vector(bias, "bias", N, torch.float32, dev),
+                                           op, os_, _dtype_code(ot), 0)
+        rc = self.lib.adloco_blockscale_matmul(self.h, args, self._on_stream(stream))
+        if rc != OK:
+            self.check(rc, "adloco_blockscale_matmul")
 
     # ------------------------------------------------------------------ outer step
     def outer_step(self, instances, theta_in, mom_in, *, lr, momentum, nesterov=True, theta_out=None,

@@ -675,17 +675,19 @@ __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ Dr
 }
 
 // ---- rotary positions -----------------------------------------------------------------------------
-// A block takes a few tokens: it first forms the cosines and sines of their positions in shared memory (one
-// sincospi for each pair, shared by all heads of all tensors), then goes through the tokens' heads in units of P
-// pairs, neighbouring threads on neighbouring memory.
+// A thread takes one token and one unit of a head -- P pairs to rotate (two pieces of P elements: of either half, or
+// adjacent when interleaved), or two pieces of the part that is only copied -- in every heads_at_once-th head of all
+// tensors, so that its cosines and sines stay in registers over the heads.  Neighbouring threads take neighbouring
+// units, then heads, then tokens.  The block forms the cosines and sines of its tokens' positions once, in shared
+// memory, while the loads of the first heads are on their way.
 struct RopeArgs {
     adloco_rope_tensor t[4];
     int n;
     int heads_before[5];
     int64_t B, T, tokens;
-    int D, R, rot_units, units;        // units of P pairs a head: rotated, and with the copied rest
-    int tokens_per_block;
-    FastDiv by_half, by_token, by_units, by_T;
+    int D, R, rot_units, units;        // units a head: rotated, and with the copied rest
+    int lanes, tokens_per_block, heads_at_once;      // lanes: threads along a head's units
+    FastDiv by_half, by_lanes, by_heads, by_T;
     const uint64_t* turns;
     const int32_t* positions;
     int64_t positions_stride, first;
@@ -695,99 +697,160 @@ struct RopeArgs {
 template <typename T, int P>
 struct alignas(sizeof(T) * P) Pack { T v[P]; };
 
+constexpr int kRopeHeads = 4;          // heads of a thread whose loads are issued together
+
 template <typename T, int P, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) rope_kernel(const __grid_constant__ RopeArgs a) {
+    using V = Pack<T, P>;
     extern __shared__ float2 turn_cs[];                // [tokens_per_block][R / 2]
     const int half = a.R / 2;
-    const int64_t token0 = (int64_t)blockIdx.x * a.tokens_per_block;
+    const uint32_t token0 = blockIdx.x * (uint32_t)a.tokens_per_block;
     const int here = (int)min((int64_t)a.tokens_per_block, a.tokens - token0);
-    for (int i = threadIdx.x; i < here * half; i += 256) {
-        const int tok = (int)a.by_half(i), j = i - tok * half;
-        const uint32_t b = a.by_T((uint32_t)(token0 + tok)), s = (uint32_t)(token0 + tok) - b * (uint32_t)a.T;
-        const int64_t pos = a.positions ? (int64_t)a.positions[b * a.positions_stride + s] : a.first + (int64_t)s;
-        // the phase in units of 2^-64 turns is exact; its top 32 bits, as a signed number, are half turns in [-1, 1)
-        const int32_t top = (int32_t)(((uint64_t)pos * a.turns[j]) >> 32);
-        float sn, cs;
-        sincospif((float)top * 4.656612873077392578125e-10f, &sn, &cs);
-        if (a.inverse) sn = -sn;
-        turn_cs[i] = make_float2(a.magnitude * cs, a.magnitude * sn);
-    }
-    __syncthreads();
-    const int per_token = (int)a.by_token.d, work = here * per_token;
-#pragma unroll 2
-    for (int i = threadIdx.x; i < work; i += 256) {
-        const int tok = (int)a.by_token(i), rem = i - tok * per_token;
-        int head = (int)a.by_units(rem);
-        const int unit = rem - head * a.units;
-        int k = 0;
+    const uint32_t slot = a.by_lanes(threadIdx.x), lane = threadIdx.x - slot * a.lanes;
+    const uint32_t tok = a.by_heads(slot);
+    const int head0 = (int)(slot - tok * a.heads_at_once), heads = a.heads_before[a.n];
+    const bool mine = (int)tok < here;
+    const uint32_t b = a.by_T(token0 + (mine ? tok : 0u)), s = token0 + (mine ? tok : 0u) - b * (uint32_t)a.T;
+    bool formed = false;
+    for (int unit = (int)lane; unit < a.units || !formed; unit += a.lanes) {
+        const bool rotates = unit < a.rot_units;
+        // the two pieces; of the copied part the second may lie beyond the head
+        const int at0 = rotates ? (INTERLEAVED ? 2 * unit * P : unit * P) : a.R + (unit - a.rot_units) * 2 * P;
+        const int at1 = rotates && !INTERLEAVED ? at0 + half : at0 + P;
+        const bool second = at1 < a.D;
+        float2 cs[P];
+        for (int h0 = head0; h0 < heads || !formed; h0 += kRopeHeads * a.heads_at_once) {
+            V x0[kRopeHeads], x1[kRopeHeads];
+            T* out[kRopeHeads];
 #pragma unroll
-        for (int q = 1; q < 4; ++q) k += q < a.n && head >= a.heads_before[q];
-        head -= a.heads_before[k];
-        const adloco_rope_tensor& t = a.t[k];
-        const uint32_t b = a.by_T((uint32_t)(token0 + tok)), s = (uint32_t)(token0 + tok) - b * (uint32_t)a.T;
-        const T* in = static_cast<const T*>(t.in) + b * t.in_batch + s * t.in_token + head * t.in_head;
-        T* out = static_cast<T*>(t.out) + b * t.out_batch + s * t.out_token + head * t.out_head;
-        using V = Pack<T, P>;
-        if (unit >= a.rot_units) {                     // the part of the head that is not rotated
-            const int at = a.R + (unit - a.rot_units) * P;
-            *reinterpret_cast<V*>(out + at) = *reinterpret_cast<const V*>(in + at);
-            continue;
+            for (int i = 0; i < kRopeHeads; ++i) {
+                int head = h0 + i * a.heads_at_once;
+                out[i] = nullptr;
+                if (!mine || unit >= a.units || head >= heads) continue;
+                int k = 0;
+#pragma unroll
+                for (int q = 1; q < 4; ++q) k += q < a.n && head >= a.heads_before[q];
+                head -= a.heads_before[k];
+                const adloco_rope_tensor& t = a.t[k];
+                const T* in = static_cast<const T*>(t.in) + b * t.in_batch + s * t.in_token + head * t.in_head;
+                out[i] = static_cast<T*>(t.out) + b * t.out_batch + s * t.out_token + head * t.out_head;
+                x0[i] = *reinterpret_cast<const V*>(in + at0);
+                if (second) x1[i] = *reinterpret_cast<const V*>(in + at1);
+            }
+            if (!formed) {                             // every thread of the block comes here once
+                for (int i = threadIdx.x; i < here * half; i += 256) {
+                    const uint32_t w = a.by_half(i), j = i - w * half;
+                    const uint32_t wb = a.by_T(token0 + w), ws = token0 + w - wb * (uint32_t)a.T;
+                    const int64_t pos = a.positions ? (int64_t)a.positions[wb * a.positions_stride + ws] : a.first + (int64_t)ws;
+                    // the phase in units of 2^-64 turns is exact; its top 32 bits, as a signed number, are half turns in [-1, 1)
+                    const int32_t top = (int32_t)(((uint64_t)pos * a.turns[j]) >> 32);
+                    float sn, co;
+                    sincospif((float)top * 4.656612873077392578125e-10f, &sn, &co);
+                    if (a.inverse) sn = -sn;
+                    turn_cs[i] = make_float2(a.magnitude * co, a.magnitude * sn);
+                }
+                __syncthreads();
+                formed = true;
+            }
+            if (!mine || unit >= a.units) break;
+            if (rotates && h0 == head0) {
+#pragma unroll
+                for (int p = 0; p < P; ++p) cs[p] = turn_cs[tok * half + unit * P + p];
+            }
+#pragma unroll
+            for (int i = 0; i < kRopeHeads; ++i) {
+                if (out[i] == nullptr) continue;
+                if (rotates) {
+                    float f[2 * P];                    // pair p: f[2p], f[2p + 1] interleaved, else f[p], f[P + p]
+#pragma unroll
+                    for (int p = 0; p < P; ++p) { f[p] = (float)x0[i].v[p]; f[P + p] = (float)x1[i].v[p]; }
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        float& lo = f[INTERLEAVED ? 2 * p : p];
+                        float& hi = f[INTERLEAVED ? 2 * p + 1 : P + p];
+                        const float u = lo, w = hi;
+                        lo = u * cs[p].x - w * cs[p].y;
+                        hi = u * cs[p].y + w * cs[p].x;
+                    }
+#pragma unroll
+                    for (int p = 0; p < P; ++p) { x0[i].v[p] = (T)f[p]; x1[i].v[p] = (T)f[P + p]; }
+                }
+                *reinterpret_cast<V*>(out[i] + at0) = x0[i];
+                if (second) *reinterpret_cast<V*>(out[i] + at1) = x1[i];
+            }
         }
-        const int j0 = unit * P;                       // first pair
-        const int at0 = INTERLEAVED ? 2 * j0 : j0, at1 = INTERLEAVED ? 2 * j0 + P : j0 + half;
-        V x0 = *reinterpret_cast<const V*>(in + at0), x1 = *reinterpret_cast<const V*>(in + at1);
-        const float2* cs = turn_cs + tok * half + j0;
-        float f[2 * P];                                // pair p: f[2p], f[2p + 1] interleaved, else f[p], f[P + p]
-#pragma unroll
-        for (int p = 0; p < P; ++p) { f[p] = (float)x0.v[p]; f[P + p] = (float)x1.v[p]; }
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            float& lo = f[INTERLEAVED ? 2 * p : p];
-            float& hi = f[INTERLEAVED ? 2 * p + 1 : P + p];
-            const float u = lo, w = hi;
-            lo = u * cs[p].x - w * cs[p].y;
-            hi = u * cs[p].y + w * cs[p].x;
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p) { x0.v[p] = (T)f[p]; x1.v[p] = (T)f[P + p]; }
-        *reinterpret_cast<V*>(out + at0) = x0;
-        *reinterpret_cast<V*>(out + at1) = x1;
     }
 }
 
 // ---- quantisation -----------------------------------------------------------------------------------
-// Rows: 16 lanes hold a block of 128, four blocks one after the other with their loads issued together.
+// the largest magnitude's bits of eight elements; bf16 in pairs, as bits of the same number in fp32
+__device__ __forceinline__ uint32_t abs_max(const Raw<__nv_bfloat16>& r) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, r.w[i] & 0x7fff7fffu);
+    return max(m << 16, m & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t abs_max(const Raw<float>& r) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, r.w[i] & 0x7fffffffu);
+    return m;
+}
+template <typename T>
+__device__ __forceinline__ uint2 raw_to_e4m3(const Raw<T>& r, float inv) {
+    F2 f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = pair_of(r, i);
+    return to_e4m3x8(f, inv);
+}
+// Rows: 8 lanes hold a block of 128, 16 adjacent elements each; two blocks one after the other with their loads issued
+// together.  (With 8 elements a lane the exchange of the maximum and the scale's arithmetic, which every lane does,
+// took more issue slots than the elements: 19.7 us for 32768 x 768 bf16.)
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) quantise_rows_kernel(const T* x, int64_t x_stride, uint8_t* q, int64_t q_stride,
                                                             uint8_t* scale, int64_t scale_stride, uint32_t blocks, int64_t cols,
                                                             const __grid_constant__ FastDiv blocks_per_row) {
-    constexpr int U = 4;
-    const uint32_t b0 = blockIdx.x * (16 * U) + (threadIdx.x >> 4);
-    const int lane_col = (threadIdx.x & 15) * 8;
-    Raw<T> v[U];
+    constexpr int U = 2;
+    const uint32_t b0 = blockIdx.x * (32 * U) + (threadIdx.x >> 3);
+    const int lane_col = (threadIdx.x & 7) * 16;
+    Raw<T> v[U][2];
     uint32_t row[U], kb[U];
     int n[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-        const uint32_t b = b0 + 16 * k;
+        const uint32_t b = b0 + 32 * k;
         const bool there = b < blocks;
         row[k] = there ? blocks_per_row(b) : 0u;
         kb[k] = there ? b - row[k] * blocks_per_row.d : 0u;
         const int64_t col = (int64_t)kb[k] * 128 + lane_col;
-        n[k] = there ? (int)min((int64_t)8, cols - col) : 0;
-        v[k] = zero_raw<T>();
-        if (n[k] <= 0) continue;
+        n[k] = there ? (int)min((int64_t)16, cols - col) : 0;
         const T* at = x + row[k] * x_stride + col;
-        if (VEC && n[k] == 8) v[k] = load_raw<true>(at, 8);
-        else v[k] = load_raw<false>(at, n[k]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            v[k][j] = zero_raw<T>();
+            if (n[k] <= 8 * j) continue;
+            if (VEC && n[k] >= 8 * j + 8) v[k][j] = load_raw<true>(at + 8 * j, 8);
+            else v[k][j] = load_raw<false>(at + 8 * j, n[k] - 8 * j);
+        }
     }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-        F2 f[4];
+        uint32_t m = max(abs_max(v[k][0]), abs_max(v[k][1]));           // what is missing reads as zero
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = pair_of(v[k], i);
-        // columns relative to the block: its scale is element 0 of what is passed
-        quantise_block(f, n[k], q + row[k] * q_stride + (int64_t)kb[k] * 128, scale + row[k] * scale_stride + kb[k], lane_col);
+        for (int o = 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (n[k] <= 0) continue;
+        const uint32_t s = scale_byte(m);
+        const float inv = inv_scale(s);
+        const uint2 lo = raw_to_e4m3(v[k][0], inv), hi = raw_to_e4m3(v[k][1], inv);
+        uint8_t* to = q + row[k] * q_stride + (int64_t)kb[k] * 128 + lane_col;
+        const uint32_t w[4] = {lo.x, lo.y, hi.x, hi.y};
+        if (n[k] == 16) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);     // pitch and base are multiples of 16
+        else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i < n[k]) to[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+        }
+        if (lane_col == 0) scale[row[k] * scale_stride + kb[k]] = (uint8_t)s;
     }
 }
 
@@ -1031,22 +1094,27 @@ int launch_rope(adloco_ctx* ctx, int bf16, const adloco_rope_tensor* t, int n, i
     a.B = B; a.T = T; a.tokens = B * T;
     a.D = (int)D; a.R = (int)R;
     a.rot_units = (int)(R / 2 / P);
-    a.units = a.rot_units + (copies ? (int)((D - R) / P) : 0);
+    a.units = a.rot_units + (copies ? (int)((D - R + 2 * P - 1) / (2 * P)) : 0);
     a.turns = turns; a.positions = pos; a.positions_stride = pos_stride; a.first = first;
     a.magnitude = magnitude; a.inverse = inverse;
-    // about four units a thread, as long as every SM has several blocks
-    const int64_t per_token = (int64_t)a.heads_before[n] * a.units;
-    int64_t tpb = 1024 / per_token;
-    const int64_t spread = a.tokens / (4 * (int64_t)ctx->sm_count);
+    // a block's 256 threads: the units of a head, so many heads that a thread comes to about four of them, and with
+    // what is left tokens, as long as every SM has several blocks
+    const int heads = a.heads_before[n];
+    a.lanes = a.units < 256 ? a.units : 256;
+    const int slots = 256 / a.lanes;
+    a.heads_at_once = (heads + kRopeHeads - 1) / kRopeHeads;
+    if (a.heads_at_once > slots) a.heads_at_once = slots;
+    int64_t tpb = slots / a.heads_at_once;
+    const int64_t spread = a.tokens / (4 * (int64_t)ctx->sm_count), fit = 6144 / (R / 2);       // and 48 KB of sines
     if (tpb > spread) tpb = spread;
-    if (tpb > 16) tpb = 16;
+    if (tpb > fit) tpb = fit;
     if (tpb < 1) tpb = 1;
+    if (tpb == 1) a.heads_at_once = heads < slots ? heads : slots;      // one token: all threads along its heads
     a.tokens_per_block = (int)tpb;
-    a.by_half = FastDiv((uint32_t)(R / 2)); a.by_token = FastDiv((uint32_t)per_token);
-    a.by_units = FastDiv((uint32_t)a.units); a.by_T = FastDiv((uint32_t)T);
+    a.by_half = FastDiv((uint32_t)(R / 2)); a.by_lanes = FastDiv((uint32_t)a.lanes);
+    a.by_heads = FastDiv((uint32_t)a.heads_at_once); a.by_T = FastDiv((uint32_t)T);
     const unsigned grid = (unsigned)((a.tokens + tpb - 1) / tpb);
     const size_t smem = (size_t)tpb * (size_t)(R / 2) * sizeof(float2);
-    if (smem > 48 * 1024) return ADLOCO_ERR_UNSUPPORTED;
 #define ADLOCO_LAUNCH(TY, PP)                                                             \
     if (interleaved) rope_kernel<TY, PP, true><<<grid, 256, smem, st>>>(a);               \
     else rope_kernel<TY, PP, false><<<grid, 256, smem, st>>>(a)

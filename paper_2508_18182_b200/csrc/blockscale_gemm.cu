@@ -48,15 +48,66 @@ __device__ __forceinline__ uint32_t row_scale_word(const MatArgs& a, int m, int 
     if (m >= a.M) return w;
     const uint8_t* p = a.sa + (int64_t)m * a.sa_stride + g * 4;
     if (have == 4) return *reinterpret_cast<const uint32_t*>(p);
-    for (int j = 0; j < have; ++j) w = (w & ~(0xffu << (8 * j))) | ((uint32_t)p[j] << (8 * j));
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < have) w = (w & ~(0xffu << (8 * j))) | ((uint32_t)p[j] << (8 * j));
     return w;
 }
 __device__ __forceinline__ uint32_t block_scale_word(const MatArgs& a, int nb, int g, int have) {
     uint32_t w = 0x7f7f7f7fu;
     if (nb * 128 >= a.N) return w;
     const uint8_t* p = a.sb + nb * a.sb_n + (int64_t)(g * 4) * a.sb_k;
-    for (int j = 0; j < have; ++j) w = (w & ~(0xffu << (8 * j))) | ((uint32_t)p[j * a.sb_k] << (8 * j));
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < have) w = (w & ~(0xffu << (8 * j))) | ((uint32_t)p[j * a.sb_k] << (8 * j));
     return w;
+}
+// A scale warp's loop: the scale words of 512 of K at a time, for 128 rows of A and NB 128-row blocks of B, from global
+// memory into a ring of SLOTS slots of COLS columns of tensor memory.  Lane l of every lane quarter holds, in column c,
+// the word of row 32 c + l (the MMA reads each quarter's copy), so each of the four warps writes the same words.  The
+// words of the next 512 of K are loaded before the wait for a free slot: without that the loads' latency, once for
+// every four stages, held the MMAs up (85 us instead of 44 us at 32768 x 768 x 2304).
+template <int NB, int SLOTS, int COLS, bool PAIR>
+__device__ __forceinline__ void write_scales(const MatArgs& a, uint32_t tmem_sf, int worker, int workers, int tile_side, int row_offset,
+                                             uint32_t sf_full, uint32_t sf_empty, volatile int* abortp) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t at0 = tmem_sf + ((uint32_t)(warp & 3) << 21);      // lane 32 * (warp mod 4) of a tensor-memory address
+    const int groups = (a.kb + 3) / 4;
+    uint32_t w[4], b[NB];
+    auto load = [&](int tile, int g) {
+        const int have = min(4, a.kb - g * 4);
+        const int m0 = (tile / a.tiles_n) * tile_side + row_offset, nb = (tile % a.tiles_n) * NB;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[c] = row_scale_word(a, m0 + c * 32 + lane, g, have);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) b[i] = block_scale_word(a, nb + i, g, have);
+    };
+    Ring sf;
+    int tile = worker, g = 0;
+    if (tile < a.tiles) load(tile, 0);
+    while (tile < a.tiles) {
+        uint32_t w0[4], b0[NB];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w0[c] = w[c];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) b0[i] = b[i];
+        if (++g == groups) { g = 0; tile += workers; }
+        if (tile < a.tiles) load(tile, g);
+        if (!__all_sync(0xffffffffu, mbar_wait(sf_empty + 8u * sf.stage, sf.phase ^ 1u, abortp, a.wait_ns))) break;
+        tc_fence_after();
+        const uint32_t at = at0 + sf.stage * COLS;
+        tmem_st4(at, w0[0], w0[1], w0[2], w0[3]);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) tmem_st4(at + 4 + 4 * i, b0[i], b0[i], b0[i], b0[i]);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            if (PAIR) mbar_arrive_cluster(sf_full + 8u * sf.stage);
+            else mbar_arrive(sf_full + 8u * sf.stage);
+        }
+        sf.advance(SLOTS);
+    }
 }
 // 16 accumulator columns of row m to the output one by one, for outputs whose rows are not 16-byte aligned
 __device__ __forceinline__ void store_elements(const MatArgs& a, int m, int col, const uint32_t (&r)[16]) {
@@ -187,29 +238,7 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         }
     } else if (warp < 6) {
         // ---------------- scales into tensor memory ----------------
-        const uint32_t quarter = (uint32_t)(warp & 3) << 21;       // lane 32 * (warp mod 4) of a tensor-memory address
-        Ring sf;
-        bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
-            const int m0 = (tile / a.tiles_n) * MT, nb = tile % a.tiles_n;
-            for (int g = 0; g * 4 < a.kb; ++g) {
-                uint32_t w[4];
-                const int have = min(4, a.kb - g * 4);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) w[c] = row_scale_word(a, m0 + c * 32 + lane, g, have);
-                const uint32_t b = block_scale_word(a, nb, g, have);
-                if (!__all_sync(0xffffffffu, mbar_wait(sf_empty(sf.stage), sf.phase ^ 1u, abortp, a.wait_ns))) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t at = tmem + quarter + MT_SF_COL + sf.stage * 8u;
-                tmem_st4(at, w[0], w[1], w[2], w[3]);
-                tmem_st4(at + 4, b, b, b, b);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(sf_full(sf.stage));
-                sf.advance(MT_SLOTS);
-            }
-        }
+        write_scales<1, MT_SLOTS, 8, false>(a, tmem + MT_SF_COL, (int)blockIdx.x, (int)gridDim.x, MT, 0, sf_full(0), sf_empty(0), abortp);
     } else {
         // ---------------- epilogue ----------------
         const uint32_t q = warp & 3;
@@ -398,31 +427,8 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         }
     } else if (warp < 6) {
         // ---------------- scales into this CTA's tensor memory ----------------
-        const uint32_t quarter = (uint32_t)(warp & 3) << 21;
-        const uint32_t sf_full_0 = map_to_cta(sf_full(0), 0);
-        Ring sf;
-        bool ok = true;
-        for (int tile = worker; ok && tile < a.tiles; tile += workers) {
-            const int m0 = (tile / a.tiles_n) * 256 + (int)rank * MT, nb = (tile % a.tiles_n) * 2;
-            for (int g = 0; g * 4 < a.kb; ++g) {
-                uint32_t w[4];
-                const int have = min(4, a.kb - g * 4);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) w[c] = row_scale_word(a, m0 + c * 32 + lane, g, have);
-                const uint32_t b0 = block_scale_word(a, nb, g, have), b1 = block_scale_word(a, nb + 1, g, have);
-                if (!__all_sync(0xffffffffu, mbar_wait(sf_empty(sf.stage), sf.phase ^ 1u, abortp, a.wait_ns))) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t at = tmem + quarter + MP_SF_COL + sf.stage * 16u;
-                tmem_st4(at, w[0], w[1], w[2], w[3]);
-                tmem_st4(at + 4, b0, b0, b0, b0);
-                tmem_st4(at + 8, b1, b1, b1, b1);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(sf_full_0 + 8u * sf.stage);
-                sf.advance(MP_SLOTS);
-            }
-        }
+        write_scales<2, MP_SLOTS, 16, true>(a, tmem + MP_SF_COL, worker, workers, 256, (int)rank * MT, map_to_cta(sf_full(0), 0), sf_empty(0),
+                                            abortp);
     } else {
         // ---------------- epilogue ----------------
         const uint32_t q = warp & 3, slice = (uint32_t)(warp - 6) >> 2;      // 32 rows, 64 columns of this CTA's 128 x 256
@@ -478,10 +484,11 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
                     }
                 }
                 tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(acc_empty_0);             // the next tile's MMAs need not wait for the store
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive_cluster(acc_empty_0);
                     const int col = a.out_bf16 ? col0 : col0 + 32;
                     if (col < a.N) {
                         tma_store_2d(&tmO, box, col, row0);
