@@ -24,7 +24,7 @@ struct Ring {
 
 struct MatArgs {
     int M, N, K, kb;                 // kb: blocks of 128 along K
-    int tiles_n, tiles;              // tiles along N, and all
+    int tiles_m, tiles_n, tiles;     // tiles along M, along N, and all
     const uint8_t* sa;
     int64_t sa_stride;
     const uint8_t* sb;
@@ -41,74 +41,6 @@ __device__ __forceinline__ uint32_t pack_bf16(uint32_t a, uint32_t b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(a), __uint_as_float(b));
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-// The scale bytes of blocks 4 g .. 4 g + have - 1 of one row of A, or of one 128-row block of B; 127 (a scale of 1) where
-// there is none
-__device__ __forceinline__ uint32_t row_scale_word(const MatArgs& a, int m, int g, int have) {
-    uint32_t w = 0x7f7f7f7fu;
-    if (m >= a.M) return w;
-    const uint8_t* p = a.sa + (int64_t)m * a.sa_stride + g * 4;
-    if (have == 4) return *reinterpret_cast<const uint32_t*>(p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (j < have) w = (w & ~(0xffu << (8 * j))) | ((uint32_t)p[j] << (8 * j));
-    return w;
-}
-__device__ __forceinline__ uint32_t block_scale_word(const MatArgs& a, int nb, int g, int have) {
-    uint32_t w = 0x7f7f7f7fu;
-    if (nb * 128 >= a.N) return w;
-    const uint8_t* p = a.sb + nb * a.sb_n + (int64_t)(g * 4) * a.sb_k;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (j < have) w = (w & ~(0xffu << (8 * j))) | ((uint32_t)p[j * a.sb_k] << (8 * j));
-    return w;
-}
-// A scale warp's loop: the scale words of 512 of K at a time, for 128 rows of A and NB 128-row blocks of B, from global
-// memory into a ring of SLOTS slots of COLS columns of tensor memory.  Lane l of every lane quarter holds, in column c,
-// the word of row 32 c + l (the MMA reads each quarter's copy), so each of the four warps writes the same words.  The
-// words of the next 512 of K are loaded before the wait for a free slot: without that the loads' latency, once for
-// every four stages, held the MMAs up (85 us instead of 44 us at 32768 x 768 x 2304).
-template <int NB, int SLOTS, int COLS, bool PAIR>
-__device__ __forceinline__ void write_scales(const MatArgs& a, uint32_t tmem_sf, int worker, int workers, int tile_side, int row_offset,
-                                             uint32_t sf_full, uint32_t sf_empty, volatile int* abortp) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t at0 = tmem_sf + ((uint32_t)(warp & 3) << 21);      // lane 32 * (warp mod 4) of a tensor-memory address
-    const int groups = (a.kb + 3) / 4;
-    uint32_t w[4], b[NB];
-    auto load = [&](int tile, int g) {
-        const int have = min(4, a.kb - g * 4);
-        const int m0 = (tile / a.tiles_n) * tile_side + row_offset, nb = (tile % a.tiles_n) * NB;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) w[c] = row_scale_word(a, m0 + c * 32 + lane, g, have);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) b[i] = block_scale_word(a, nb + i, g, have);
-    };
-    Ring sf;
-    int tile = worker, g = 0;
-    if (tile < a.tiles) load(tile, 0);
-    while (tile < a.tiles) {
-        uint32_t w0[4], b0[NB];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) w0[c] = w[c];
-#pragma unroll
-        for (int i = 0; i < NB; ++i) b0[i] = b[i];
-        if (++g == groups) { g = 0; tile += workers; }
-        if (tile < a.tiles) load(tile, g);
-        if (!__all_sync(0xffffffffu, mbar_wait(sf_empty + 8u * sf.stage, sf.phase ^ 1u, abortp, a.wait_ns))) break;
-        tc_fence_after();
-        const uint32_t at = at0 + sf.stage * COLS;
-        tmem_st4(at, w0[0], w0[1], w0[2], w0[3]);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) tmem_st4(at + 4 + 4 * i, b0[i], b0[i], b0[i], b0[i]);
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-            if (PAIR) mbar_arrive_cluster(sf_full + 8u * sf.stage);
-            else mbar_arrive(sf_full + 8u * sf.stage);
-        }
-        sf.advance(SLOTS);
-    }
-}
 // 16 accumulator columns of row m to the output one by one, for outputs whose rows are not 16-byte aligned
 __device__ __forceinline__ void store_elements(const MatArgs& a, int m, int col, const uint32_t (&r)[16]) {
 #pragma unroll
@@ -121,40 +53,121 @@ __device__ __forceinline__ void store_elements(const MatArgs& a, int m, int col,
     }
 }
 
+// A wait of the whole warp, which goes on (or gives up) together.
+template <bool CLUSTER>
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abortp, uint64_t limit_ns) {
+    return __all_sync(0xffffffffu, mbar_wait<CLUSTER>(bar, parity, abortp, limit_ns)) != 0;
+}
+
+// The tiles of one worker.  Dealt round, the tiles along N fastest: the workers sit on the same few rows of A at a time.
+// In runs, the tiles along M fastest: a worker stays on one panel of B.
+struct TileWalk {
+    int at, end, step, per_line;
+    bool runs;
+    __device__ __forceinline__ TileWalk(const MatArgs& a, int worker, int workers, bool in_runs) : runs(in_runs) {
+        at = runs ? (int)((int64_t)a.tiles * worker / workers) : worker;
+        end = runs ? (int)((int64_t)a.tiles * (worker + 1) / workers) : a.tiles;
+        step = runs ? 1 : workers;
+        per_line = runs ? a.tiles_m : a.tiles_n;
+    }
+    __device__ __forceinline__ bool more() const { return at < end; }
+    __device__ __forceinline__ void next() { at += step; }
+    __device__ __forceinline__ int m() const { return runs ? at % per_line : at / per_line; }
+    __device__ __forceinline__ int n() const { return runs ? at / per_line : at % per_line; }
+};
+
+// The four scale warps' loop: the scale words (four blocks' bytes) of 512 of K at a time, for 128 rows of A and TILE_N
+// rows of B, from global memory into a ring of slots in shared memory: 512 bytes for A, then 512 for each 128 rows of B,
+// the word of row r at 16 (r mod 32) + 4 (r / 32), which is how tcgen05.cp spreads them over tensor memory.  A's words
+// come by cp.async, each warp's own 32 rows; B's bytes lie anywhere and come by one load of 8 lanes.  A turn issues its
+// loads, then finishes the turn before, so that loads have a turn's time and a slot is ready two turns before it is used.
+// The MMA thread copies a slot to tensor memory in front of the MMAs that read it.  (Written into tensor memory by these
+// warps instead, a turn took 2400 clocks: tcgen05.st queues behind the MMAs in flight.  32768 x 768 x 2304: 84 us.)
+// Rows of A's scales are whole aligned words; what a row's last word holds beyond its blocks is not used.
+constexpr int kScaleSlots = 4;
+template <int TILE_N>
+__host__ __device__ constexpr int scale_slot_bytes() { return 512 * (1 + (TILE_N + 127) / 128); }
+template <int TILE_M, int TILE_N>
+__device__ __forceinline__ void fetch_scales(const MatArgs& a, uint32_t ring, TileWalk walk, int row_offset, uint32_t sf_full,
+                                             uint32_t sf_empty, volatile int* abortp) {
+    constexpr int BLOCKS = (TILE_N + 127) / 128, SLOT = scale_slot_bytes<TILE_N>();
+    const int quarter = __shfl_sync(0xffffffffu, (threadIdx.x >> 5) & 3, 0), lane = threadIdx.x & 31;
+    const int groups = (a.kb + 3) / 4;
+    uint32_t byte[2], shift[2];                           // lanes 0-3, 4-7: B's bytes of the two 128-row blocks
+    int g = 0, m0 = 0, n0 = 0;                            // of the next fetch
+    Ring fill, done;
+    auto fetch = [&](int i) -> bool {                     // turn's loads into slot fill.stage
+        if (!wait_warp<false>(sf_empty + 8u * fill.stage, fill.phase ^ 1u, abortp, a.wait_ns)) return false;
+        if (g == 0) { m0 = walk.m() * TILE_M + row_offset; n0 = walk.n() * TILE_N; }
+        const int m = m0 + quarter * 32 + lane, nb = (n0 >> 7) + ((lane >> 2) & 1), k = g * 4 + (lane & 3);
+        const uint32_t to = ring + fill.stage * SLOT + (uint32_t)(lane * 16 + quarter * 4);
+        if (m < a.M)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(a.sa + (int64_t)m * a.sa_stride + g * 4) : "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        byte[i] = 127u;
+        if (lane < 8 && nb * 128 < a.N && k < a.kb) byte[i] = __ldg(a.sb + nb * a.sb_n + k * a.sb_k);
+        shift[i] = (uint32_t)(n0 & 127);                  // rows of the tile's first 128-row block before the tile
+        if (++g == groups) { g = 0; walk.next(); }
+        fill.advance(kScaleSlots);
+        return true;
+    };
+    if (!walk.more() || !fetch(0)) return;
+    for (;;) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const bool last = !walk.more();
+            if (!last && !fetch(i ^ 1)) return;
+            if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
+            else asm volatile("cp.async.wait_group 1;" ::: "memory");
+            const uint32_t part = byte[i] << (8 * (lane & 3));
+            if (quarter < BLOCKS) {                       // warp q: the q-th 128 rows of B's part
+                const uint32_t b0 = __reduce_or_sync(0xffffffffu, lane < 4 ? part : 0u);
+                const uint32_t b1 = BLOCKS > 1 ? __reduce_or_sync(0xffffffffu, lane >= 4 && lane < 8 ? part : 0u) : b0;
+                uint32_t v[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] = shift[i] + 128u * quarter + 32u * c < 128u ? b0 : b1;
+                st_shared_v4(ring + done.stage * SLOT + (uint32_t)(512 + quarter * 512 + lane * 16), v[0], v[1], v[2], v[3]);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sf_full + 8u * done.stage);
+            done.advance(kScaleSlots);
+            if (last) return;
+        }
+    }
+}
 // ---- 128 x 128 tiles, one CTA each --------------------------------------------------------------
 // Persistent, 320 threads: warp 0 TMA, warp 1 MMA, warps 2-5 scales, warps 6-9 epilogue.  A stage is 128 of K (a
 // 128-byte swizzle row of either operand): four MMAs of K = 32 that use the same byte of the scale words.  A scale
-// word holds the bytes of four stages; the scale warps write the words of 512 of K at a time into a ring of slots
-// in tensor memory (lane = row mod 32, column = row / 32, the same in all four lane quarters, which is how the
-// MMA reads them).
+// word holds the bytes of four stages: the scale warps bring the words of 512 of K at a time.
 constexpr int MT = 128;
 constexpr int MT_STAGES = 6;
 constexpr int MT_STAGE_BYTES = 2 * MT * 128;
-constexpr int MT_SLOTS = 4;                                   // scale slots of 8 columns: 4 for A, 4 for B
 constexpr int MT_SF_COL = 2 * MT;                             // tensor memory: two accumulators, then the slots
-constexpr int MT_SMEM = MT_STAGES * MT_STAGE_BYTES + 1024 + 256;
+constexpr int MT_SMEM = MT_STAGES * MT_STAGE_BYTES + 1024 + 256 + kScaleSlots * scale_slot_bytes<MT>();
 constexpr int MT_THREADS = 320;
 
 __global__ void __launch_bounds__(MT_THREADS, 1)
 blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const MatArgs a) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t bars = smem_base + MT_STAGES * MT_STAGE_BYTES;
+    const uint32_t bars = smem_base + MT_STAGES * MT_STAGE_BYTES, sf_ring = bars + 256;
     auto full_bar = [&](uint32_t s) { return bars + 8u * s; };
     auto empty_bar = [&](uint32_t s) { return bars + 8u * (MT_STAGES + s); };
     auto sf_full = [&](uint32_t s) { return bars + 8u * (2 * MT_STAGES + s); };
-    auto sf_empty = [&](uint32_t s) { return bars + 8u * (2 * MT_STAGES + MT_SLOTS + s); };
-    auto acc_full = [&](uint32_t s) { return bars + 8u * (2 * MT_STAGES + 2 * MT_SLOTS + s); };
-    auto acc_empty = [&](uint32_t s) { return bars + 8u * (2 * MT_STAGES + 2 * MT_SLOTS + 2 + s); };
-    const uint32_t drain_bar = bars + 8u * (2 * MT_STAGES + 2 * MT_SLOTS + 4);
+    auto sf_empty = [&](uint32_t s) { return bars + 8u * (2 * MT_STAGES + kScaleSlots + s); };
+    auto acc_full = [&](uint32_t s) { return bars + 8u * (2 * MT_STAGES + 2 * kScaleSlots + s); };
+    auto acc_empty = [&](uint32_t s) { return bars + 8u * (2 * MT_STAGES + 2 * kScaleSlots + 2 + s); };
+    const uint32_t drain_bar = bars + 8u * (2 * MT_STAGES + 2 * kScaleSlots + 4);
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // warp: known to be uniform
+    TileWalk walk(a, (int)blockIdx.x, (int)gridDim.x, false);
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (uint32_t s = 0; s < MT_STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (uint32_t s = 0; s < MT_SLOTS; ++s) { mbar_init(sf_full(s), 4); mbar_init(sf_empty(s), 1); }
+        for (uint32_t s = 0; s < kScaleSlots; ++s) { mbar_init(sf_full(s), 4); mbar_init(sf_empty(s), 1); }
         for (uint32_t s = 0; s < 2; ++s) { mbar_init(acc_full(s), 1); mbar_init(acc_empty(s), 4); }
         mbar_init(drain_bar, 1);
         fence_barrier_init();
@@ -177,8 +190,8 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             Ring ps;
             uint32_t issued = 0;
             bool ok = true;
-            for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
-                const int m0 = (tile / a.tiles_n) * MT, n0 = (tile % a.tiles_n) * MT;
+            for (; ok && walk.more(); walk.next()) {
+                const int m0 = walk.m() * MT, n0 = walk.n() * MT;
                 for (int k = 0; k < a.kb; ++k) {
                     if (!mbar_wait(empty_bar(ps.stage), ps.phase ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
                     const uint32_t sA = smem_base + ps.stage * MT_STAGE_BYTES;
@@ -201,50 +214,56 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             }
         }
     } else if (warp == 1) {
-        // ---------------- MMA issuer ----------------
-        if (lane == 0) {
-            Ring ps, sf;
-            uint32_t n = 0;
-            bool ok = true;
-            for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x, ++n) {
-                const uint32_t buf = n & 1u;
-                if (!mbar_wait(acc_empty(buf), ((n >> 1) & 1u) ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
+        // ---------------- MMA issuer (the whole warp keeps step, one lane issues) ----------------
+        const bool leader = elect_one();
+        const uint64_t desc0 = smem_desc_sw128(0, 16, 1024);
+        Ring ps, sf;
+        uint32_t n = 0;
+        bool ok = true;
+        for (; ok && walk.more(); walk.next(), ++n) {
+            const uint32_t buf = n & 1u;
+            if (!wait_warp<false>(acc_empty(buf), ((n >> 1) & 1u) ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
+            for (int k = 0; k < a.kb; ++k) {
+                if ((k & 3) == 0 && !wait_warp<false>(sf_full(sf.stage), sf.phase, abortp, a.wait_ns)) { ok = false; break; }
+                if (!wait_warp<false>(full_bar(ps.stage), ps.phase, abortp, a.wait_ns)) { ok = false; break; }
                 tc_fence_after();
-                for (int k = 0; k < a.kb; ++k) {
-                    if ((k & 3) == 0 && !mbar_wait(sf_full(sf.stage), sf.phase, abortp, a.wait_ns)) { ok = false; break; }
-                    if (!mbar_wait(full_bar(ps.stage), ps.phase, abortp, a.wait_ns)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t sA = smem_base + ps.stage * MT_STAGE_BYTES, sB = sA + MT * 128;
-                    const uint32_t sf_col = tmem + MT_SF_COL + sf.stage * 8u;
+                if (leader) {
+                    const uint32_t sf_col = tmem + MT_SF_COL + sf.stage * 16u, slot = sf_ring + sf.stage * scale_slot_bytes<MT>();
+                    if ((k & 3) == 0) {
+                        tmem_copy_scales(sf_col, smem_desc_rows16(slot));
+                        tmem_copy_scales(sf_col + 4, smem_desc_rows16(slot + 512));
+                    }
+                    // K-major, 128-byte swizzle: 32 elements further along K = 32 bytes = 2 units of the descriptor's address
+                    const uint64_t dA = desc0 + ((smem_base + ps.stage * MT_STAGE_BYTES) >> 4), dB = dA + ((MT * 128) >> 4);
                     const uint32_t idesc = idesc_mxf8(MT, MT, (uint32_t)k & 3u);
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)       // K-major, 128-byte swizzle: 32 elements further along K = 32 bytes
-                        mma_mxf8(tmem + buf * MT, smem_desc_sw128(sA + kk * 32, 16, 1024), smem_desc_sw128(sB + kk * 32, 16, 1024),
-                                 idesc, sf_col, sf_col + 4, (k == 0 && kk == 0) ? 0u : 1u);
+                    for (int kk = 0; kk < 4; ++kk)
+                        mma_mxf8(tmem + buf * MT, dA + 2 * kk, dB + 2 * kk, idesc, sf_col, sf_col + 4, (k == 0 && kk == 0) ? 0u : 1u);
                     mma_commit(empty_bar(ps.stage));
-                    ps.advance(MT_STAGES);
-                    if ((k & 3) == 3 || k == a.kb - 1) {
-                        mma_commit(sf_empty(sf.stage));
-                        sf.advance(MT_SLOTS);
-                    }
+                    if ((k & 3) == 3 || k == a.kb - 1) mma_commit(sf_empty(sf.stage));
                 }
-                if (ok) mma_commit(acc_full(buf));
+                __syncwarp();
+                ps.advance(MT_STAGES);
+                if ((k & 3) == 3 || k == a.kb - 1) sf.advance(kScaleSlots);
             }
-            if (!ok) {
-                mma_commit(drain_bar);
-                int never = 0;
-                mbar_wait(drain_bar, 0, &never, kLeaveLimitNs);
-            }
+            if (ok && leader) mma_commit(acc_full(buf));
+            __syncwarp();
         }
+        if (!ok && leader) {
+            mma_commit(drain_bar);
+            int never = 0;
+            mbar_wait(drain_bar, 0, &never, kLeaveLimitNs);
+        }
+        __syncwarp();
     } else if (warp < 6) {
-        // ---------------- scales into tensor memory ----------------
-        write_scales<1, MT_SLOTS, 8, false>(a, tmem + MT_SF_COL, (int)blockIdx.x, (int)gridDim.x, MT, 0, sf_full(0), sf_empty(0), abortp);
+        // ---------------- scales ----------------
+        fetch_scales<MT, MT>(a, sf_ring, walk, 0, sf_full(0), sf_empty(0), abortp);
     } else {
         // ---------------- epilogue ----------------
         const uint32_t q = warp & 3;
         uint32_t n = 0;
-        for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x, ++n) {
-            const int m0 = (tile / a.tiles_n) * MT, n0 = (tile % a.tiles_n) * MT;
+        for (; walk.more(); walk.next(), ++n) {
+            const int m0 = walk.m() * MT, n0 = walk.n() * MT;
             const uint32_t buf = n & 1u;
             if (!__all_sync(0xffffffffu, mbar_wait(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns))) break;
             tc_fence_after();
@@ -309,47 +328,58 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     if (threadIdx.x == 0 && abort_flag) atomicExch(a.status, (int)ADLOCO_ERR_TIMEOUT);
 }
 
-// ---- 256 x 256 tiles shared by a CTA pair ---------------------------------------------------------
+// ---- 256 x 192 tiles shared by a CTA pair ---------------------------------------------------------
 // One MMA over the two CTAs of a cluster (cta_group::2): CTA r holds rows 128 r .. + 127 of the tile in its tensor
-// memory and loads those rows of A and one half of the rows of B, 32 KB a stage for 512 clocks of tensor work --
-// 64 bytes a clock, what L2 delivers to an SM; a 128 x 128 tile of its own asks for 128, a 128 x 256 one for 96.
-// The accumulator takes 256 of the 512 columns of tensor memory and the scale slots need some of the rest, so there
-// is no room for a second one: 16 epilogue warps empty it in one go, each 32 rows x 64 columns, into shared memory
-// (rounded to the output type), hand it back, and TMA stores write the boxes while the next tile's MMAs run.
-constexpr int MP_STAGES = 5;
-constexpr int MP_STAGE_BYTES = 2 * MT * 128;                  // 128 rows of A and 128 of B
-constexpr int MP_EPI_WARPS = 16;
+// memory and loads those rows of A and one half of the rows of B.  192 columns leave room in tensor memory for two
+// accumulators and the scale slots, so the tensor pipe never waits for the epilogue: with one accumulator of 256
+// columns a tile's hand-over (last MMA, signal, read-out, signal, first MMA) cost about 1.3 us beside the 1.8 us of
+// a tile's MMAs at K = 768.
+// What bounds the rest is the feed from L2, about 9.4 TB/s over all SMs.  RESIDENT: where a panel of B (96 rows a CTA,
+// up to 768 of K) fits shared memory it is loaded once for a run of tiles along M and only A is streamed, 16 KB a
+// stage instead of 28.
+constexpr int MP_N = 192;
+constexpr int MP_STAGES = 6;
+constexpr int MP_A_BYTES = MT * 128, MP_B_BYTES = (MP_N / 2) * 128;
+constexpr int MP_RESIDENT_KB = 6;                             // largest K of a resident panel, in blocks of 128
+constexpr int MP_EPI_WARPS = 4 * MP_N / 64;                   // each 32 rows x 64 columns of a CTA's 128 x 192
 constexpr int MP_BOX_BYTES = 32 * 128;                        // 32 rows of 128 bytes: one epilogue warp's store
-constexpr int MP_SLOTS = 8;                                   // scale slots of 16 columns: 4 for A, 8 for B
-constexpr int MP_SF_COL = 256;
-constexpr int MP_SMEM = MP_STAGES * MP_STAGE_BYTES + MP_EPI_WARPS * MP_BOX_BYTES + 1024 + 256;
+constexpr int MP_SF_COL = 2 * MP_N;
+constexpr int MP_SMEM = MP_STAGES * (MP_A_BYTES + MP_B_BYTES) + MP_EPI_WARPS * MP_BOX_BYTES + 1024 + 512 + kScaleSlots * scale_slot_bytes<MP_N>();
 constexpr int MP_THREADS = 32 * (6 + MP_EPI_WARPS);           // warp 0 TMA, warp 1 MMA, warps 2-5 scales, the rest epilogue
+static_assert(MP_RESIDENT_KB <= MP_STAGES, "a resident panel takes the B parts of the ring");
 
+template <bool RESIDENT>
 __global__ void __launch_bounds__(MP_THREADS, 1)
 blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                        const __grid_constant__ CUtensorMap tmO, const MatArgs a) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t boxes = smem_base + MP_STAGES * MP_STAGE_BYTES;
-    const uint32_t bars = boxes + MP_EPI_WARPS * MP_BOX_BYTES;
+    const uint32_t panel = smem_base + MP_STAGES * MP_A_BYTES;         // the B part of stage s, or block k of a resident panel
+    const uint32_t boxes = panel + MP_STAGES * MP_B_BYTES;
+    const uint32_t bars = boxes + MP_EPI_WARPS * MP_BOX_BYTES, sf_ring = bars + 512;
     auto full_bar = [&](uint32_t s) { return bars + 8u * s; };
     auto empty_bar = [&](uint32_t s) { return bars + 8u * (MP_STAGES + s); };
     auto sf_full = [&](uint32_t s) { return bars + 8u * (2 * MP_STAGES + s); };
-    auto sf_empty = [&](uint32_t s) { return bars + 8u * (2 * MP_STAGES + MP_SLOTS + s); };
-    const uint32_t acc_full = bars + 8u * (2 * MP_STAGES + 2 * MP_SLOTS);
-    const uint32_t acc_empty = acc_full + 8u, drain_bar = acc_full + 16u;
+    auto sf_empty = [&](uint32_t s) { return bars + 8u * (2 * MP_STAGES + kScaleSlots + s); };
+    auto acc_full = [&](uint32_t s) { return bars + 8u * (2 * MP_STAGES + 2 * kScaleSlots + s); };
+    auto acc_empty = [&](uint32_t s) { return bars + 8u * (2 * MP_STAGES + 2 * kScaleSlots + 2 + s); };
+    auto panel_full = [&](uint32_t k) { return bars + 8u * (2 * MP_STAGES + 2 * kScaleSlots + 4 + k); };
+    const uint32_t panel_empty = bars + 8u * (2 * MP_STAGES + 2 * kScaleSlots + 4 + MP_RESIDENT_KB);
+    const uint32_t drain_bar = panel_empty + 8u;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // warp: known to be uniform
     const uint32_t rank = cluster_cta_rank();                  // 0: the CTA that issues the MMAs
-    const int worker = (int)(blockIdx.x >> 1), workers = (int)(gridDim.x >> 1);
+    TileWalk walk(a, (int)(blockIdx.x >> 1), (int)(gridDim.x >> 1), RESIDENT);
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (uint32_t s = 0; s < MP_STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (uint32_t s = 0; s < MP_SLOTS; ++s) { mbar_init(sf_full(s), 8); mbar_init(sf_empty(s), 1); }
-        mbar_init(acc_full, 1);
-        mbar_init(acc_empty, 2 * MP_EPI_WARPS);                // the epilogue warps of both CTAs
+        // the even CTA's four scale warps and word from the odd CTA that its four are done
+        for (uint32_t s = 0; s < kScaleSlots; ++s) { mbar_init(sf_full(s), rank == 0 ? 5 : 4); mbar_init(sf_empty(s), 1); }
+        for (uint32_t s = 0; s < 2; ++s) { mbar_init(acc_full(s), 1); mbar_init(acc_empty(s), 2 * MP_EPI_WARPS); }
+        for (uint32_t k = 0; k < MP_RESIDENT_KB; ++k) mbar_init(panel_full(k), 1);
+        mbar_init(panel_empty, 1);
         mbar_init(drain_bar, 1);
         fence_barrier_init();
         prefetch_tmap(&tmA);
@@ -369,15 +399,27 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         if (lane == 0) {
             Ring ps;
             bool ok = true;
-            for (int tile = worker; ok && tile < a.tiles; tile += workers) {
-                const int m0 = (tile / a.tiles_n) * 256 + (int)rank * MT, n0 = (tile % a.tiles_n) * 256 + (int)rank * MT;
+            int panels = 0, panel_n = -1;                      // panels loaded so far, and which is there
+            for (; ok && walk.more(); walk.next()) {
+                const int m0 = walk.m() * 256 + (int)rank * MT, n0 = walk.n() * MP_N + (int)rank * (MP_N / 2);
+                const bool fresh = RESIDENT && walk.n() != panel_n;
+                if (fresh) {
+                    // the MMAs that read the last panel are done
+                    if (panels > 0 && !mbar_wait(panel_empty, (uint32_t)(panels - 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
+                    panel_n = walk.n();
+                    ++panels;
+                }
                 for (int k = 0; k < a.kb; ++k) {
                     if (!mbar_wait(empty_bar(ps.stage), ps.phase ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
-                    const uint32_t sA = smem_base + ps.stage * MP_STAGE_BYTES;
                     const uint32_t bar = map_to_cta(full_bar(ps.stage), 0);
-                    if (rank == 0) mbar_arrive_expect_tx(full_bar(ps.stage), 2 * MP_STAGE_BYTES);
-                    tma_load_2d_pair(sA, &tmA, bar, k * 128, m0);
-                    tma_load_2d_pair(sA + MT * 128, &tmB, bar, k * 128, n0);
+                    if (rank == 0) mbar_arrive_expect_tx(full_bar(ps.stage), 2 * (MP_A_BYTES + (RESIDENT ? 0 : MP_B_BYTES)));
+                    tma_load_2d_pair(smem_base + ps.stage * MP_A_BYTES, &tmA, bar, k * 128, m0);
+                    if (!RESIDENT) {
+                        tma_load_2d_pair(panel + ps.stage * MP_B_BYTES, &tmB, bar, k * 128, n0);
+                    } else if (fresh) {
+                        if (rank == 0) mbar_arrive_expect_tx(panel_full(k), 2 * MP_B_BYTES);
+                        tma_load_2d_pair(panel + k * MP_B_BYTES, &tmB, map_to_cta(panel_full(k), 0), k * 128, n0);
+                    }
                     ps.advance(MP_STAGES);
                 }
             }
@@ -390,57 +432,91 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             }
         }
     } else if (warp == 1) {
-        // ---------------- MMA issuer (even CTA only) ----------------
-        if (lane == 0 && rank == 0) {
+        // ---------------- MMA issuer (even CTA only; the whole warp keeps step, one lane issues) ----------------
+        if (rank == 0) {
+            const bool leader = elect_one();
+            const uint64_t desc0 = smem_desc_sw128(0, 16, 1024);
             Ring ps, sf;
             uint32_t n = 0;
             bool ok = true;
-            for (int tile = worker; ok && tile < a.tiles; tile += workers, ++n) {
-                if (!mbar_wait<true>(acc_empty, (n & 1u) ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
-                tc_fence_after();
+            int panels = 0, panel_n = -1;
+            for (; ok && walk.more(); ++n) {
+                const uint32_t buf = n & 1u;
+                const bool fresh = RESIDENT && walk.n() != panel_n;
+                if (fresh) { panel_n = walk.n(); ++panels; }
+                if (!wait_warp<true>(acc_empty(buf), ((n >> 1) & 1u) ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
                 for (int k = 0; k < a.kb; ++k) {
-                    if ((k & 3) == 0 && !mbar_wait<true>(sf_full(sf.stage), sf.phase, abortp, a.wait_ns)) { ok = false; break; }
-                    if (!mbar_wait(full_bar(ps.stage), ps.phase, abortp, a.wait_ns)) { ok = false; break; }
+                    if ((k & 3) == 0 && !wait_warp<true>(sf_full(sf.stage), sf.phase, abortp, a.wait_ns)) { ok = false; break; }
+                    if (fresh && !wait_warp<false>(panel_full(k), (uint32_t)(panels - 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
+                    if (!wait_warp<false>(full_bar(ps.stage), ps.phase, abortp, a.wait_ns)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t sA = smem_base + ps.stage * MP_STAGE_BYTES, sB = sA + MT * 128;
-                    const uint32_t sf_col = tmem + MP_SF_COL + sf.stage * 16u;
-                    const uint32_t idesc = idesc_mxf8(256, 256, (uint32_t)k & 3u);
+                    if (leader) {
+                        // 32 elements further along K = 32 bytes = 2 units of the descriptor's address
+                        const uint64_t dA = desc0 + ((smem_base + ps.stage * MP_A_BYTES) >> 4);
+                        const uint64_t dB = desc0 + ((panel + (RESIDENT ? (uint32_t)k : ps.stage) * MP_B_BYTES) >> 4);
+                        const uint32_t sf_col = tmem + MP_SF_COL + sf.stage * 16u, slot = sf_ring + sf.stage * scale_slot_bytes<MP_N>();
+                        if ((k & 3) == 0) {
+                            tmem_copy_scales_pair(sf_col, smem_desc_rows16(slot));
+                            tmem_copy_scales_pair(sf_col + 4, smem_desc_rows16(slot + 512));
+                            tmem_copy_scales_pair(sf_col + 8, smem_desc_rows16(slot + 1024));
+                        }
+                        const uint32_t idesc = idesc_mxf8(256, MP_N, (uint32_t)k & 3u);
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-                        mma_mxf8_pair(tmem, smem_desc_sw128(sA + kk * 32, 16, 1024), smem_desc_sw128(sB + kk * 32, 16, 1024),
-                                      idesc, sf_col, sf_col + 4, (k == 0 && kk == 0) ? 0u : 1u);
-                    mma_commit_pair(empty_bar(ps.stage), 3);
-                    ps.advance(MP_STAGES);
-                    if ((k & 3) == 3 || k == a.kb - 1) {
-                        mma_commit_pair(sf_empty(sf.stage), 3);
-                        sf.advance(MP_SLOTS);
+                        for (int kk = 0; kk < 4; ++kk)
+                            mma_mxf8_pair(tmem + buf * MP_N, dA + 2 * kk, dB + 2 * kk, idesc, sf_col, sf_col + 4, (k == 0 && kk == 0) ? 0u : 1u);
+                        mma_commit_pair(empty_bar(ps.stage), 3);
+                        if ((k & 3) == 3 || k == a.kb - 1) mma_commit_pair(sf_empty(sf.stage), 3);
                     }
+                    __syncwarp();
+                    ps.advance(MP_STAGES);
+                    if ((k & 3) == 3 || k == a.kb - 1) sf.advance(kScaleSlots);
                 }
-                if (ok) mma_commit_pair(acc_full, 3);
+                walk.next();
+                if (ok && leader) {
+                    mma_commit_pair(acc_full(buf), 3);
+                    if (RESIDENT && walk.more() && walk.n() != panel_n) mma_commit_pair(panel_empty, 3);
+                }
+                __syncwarp();
             }
-            if (!ok) {
+            if (!ok && leader) {
                 st_cluster_u32(map_to_cta(smem_u32(&abort_flag), 1u), 1u);
                 mma_commit_pair(drain_bar, 1);
                 int never = 0;
                 mbar_wait(drain_bar, 0, &never, kLeaveLimitNs);
             }
+            __syncwarp();
+        } else {
+            // the odd CTA's: passes its scale warps' signals on to the even CTA.  A release at cluster scope waits for every
+            // load that its thread has in flight, and the scale warps always have some: signalled by them directly, a turn
+            // took 2700 clocks.
+            const uint32_t there = map_to_cta(sf_full(0), 0);
+            Ring sf;
+            bool ok = true;
+            for (; ok && walk.more(); walk.next()) {
+                for (int k = 0; k < a.kb; k += 4) {
+                    if (!wait_warp<false>(sf_full(sf.stage), sf.phase, abortp, a.wait_ns)) { ok = false; break; }
+                    if (lane == 0) mbar_arrive_cluster(there + 8u * sf.stage);
+                    sf.advance(kScaleSlots);
+                }
+            }
         }
     } else if (warp < 6) {
-        // ---------------- scales into this CTA's tensor memory ----------------
-        write_scales<2, MP_SLOTS, 16, true>(a, tmem + MP_SF_COL, worker, workers, 256, (int)rank * MT, map_to_cta(sf_full(0), 0), sf_empty(0),
-                                            abortp);
+        // ---------------- this CTA's scales ----------------
+        fetch_scales<256, MP_N>(a, sf_ring, walk, (int)rank * MT, sf_full(0), sf_empty(0), abortp);
     } else {
         // ---------------- epilogue ----------------
-        const uint32_t q = warp & 3, slice = (uint32_t)(warp - 6) >> 2;      // 32 rows, 64 columns of this CTA's 128 x 256
-        const uint32_t acc_empty_0 = map_to_cta(acc_empty, 0);
+        const uint32_t q = warp & 3, slice = (uint32_t)(warp - 6) >> 2;
+        const uint32_t acc_empty_0 = map_to_cta(acc_empty(0), 0);
         const uint32_t box = boxes + (uint32_t)(warp - 6) * MP_BOX_BYTES;
-        const uint32_t row_addr = box + lane * 128u, taddr = tmem + ((q * 32u) << 16) + slice * 64u;
+        const uint32_t row_addr = box + lane * 128u;
         uint32_t n = 0;
-        for (int tile = worker; tile < a.tiles; tile += workers, ++n) {
-            const int row0 = (tile / a.tiles_n) * 256 + (int)rank * MT + (int)q * 32;
-            const int col0 = (tile % a.tiles_n) * 256 + (int)slice * 64;
+        for (; walk.more(); walk.next(), ++n) {
+            const uint32_t buf = n & 1u;
+            const uint32_t taddr = tmem + ((q * 32u) << 16) + buf * MP_N + slice * 64u;
+            const int row0 = walk.m() * 256 + (int)rank * MT + (int)q * 32;
+            const int col0 = walk.n() * MP_N + (int)slice * 64;
             const bool some = row0 < a.M && col0 < a.N;                      // uniform across the warp
-            if (!__all_sync(0xffffffffu, mbar_wait(acc_full, n & 1u, abortp, a.wait_ns))) break;
+            if (!__all_sync(0xffffffffu, mbar_wait(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns))) break;
             tc_fence_after();
             if (some && a.out_vec) {
                 if (lane == 0) bulk_wait_read_all();                         // the last store has read the box
@@ -485,7 +561,7 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(acc_empty_0);             // the next tile's MMAs need not wait for the store
+                if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty_0 + 8u * buf);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
@@ -509,7 +585,7 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(acc_empty_0);
+            if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty_0 + 8u * buf);
         }
         if (lane == 0) bulk_wait_all();                                      // this warp's stores are complete
         __syncwarp();
@@ -558,20 +634,20 @@ int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
     const int64_t piece = a.out_bf16 ? 8 : 4;
     a.out_vec = aligned16(p.out) && p.out_stride % piece == 0 && p.N % piece == 0;
     a.status = ctx->gemm_status; a.wait_ns = ctx->wait_limit_ns;
-    const int64_t pair_tiles = ((p.M + 255) / 256) * ((p.N + 255) / 256);
+    const int64_t pair_tiles = ((p.M + 255) / 256) * ((p.N + MP_N - 1) / MP_N);
     const bool pair = pair_tiles >= ctx->sm_count / 2 && cta_pairs_possible(ctx);
-    const int64_t side = pair ? 256 : MT;
-    const int64_t tm = (p.M + side - 1) / side, tn = (p.N + side - 1) / side;
+    const int64_t tm = (p.M + (pair ? 255 : MT - 1)) / (pair ? 256 : MT), tn = (p.N + (pair ? MP_N : MT) - 1) / (pair ? MP_N : MT);
     if (tm * tn > 0x7fffffff) return ADLOCO_ERR_UNSUPPORTED;
-    a.tiles_n = (int)tn; a.tiles = (int)(tm * tn);
+    a.tiles_m = (int)tm; a.tiles_n = (int)tn; a.tiles = (int)(tm * tn);
     CUtensorMap tmA, tmB, tmO;
     int rc = make_map(ctx, &tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.a, p.M, p.K, p.a_stride, 128, MT);
-    if (rc == ADLOCO_OK) rc = make_map(ctx, &tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.b, p.N, p.K, p.b_stride, 128, MT);
+    if (rc == ADLOCO_OK) rc = make_map(ctx, &tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.b, p.N, p.K, p.b_stride, 128, pair ? MP_N / 2 : MT);
     if (rc != ADLOCO_OK) return rc;
     static std::atomic<bool> attr_set[64];   // the attributes are per device
     if (!attr_set[ctx->device & 63].load()) {
         ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(blockscale_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MT_SMEM));
-        ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(blockscale_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MP_SMEM));
+        ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(blockscale_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, MP_SMEM));
+        ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(blockscale_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, MP_SMEM));
         attr_set[ctx->device & 63].store(true);
     }
     if (pair) {
@@ -592,7 +668,8 @@ int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
         attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        ADLOCO_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, blockscale_pair_kernel, tmA, tmB, tmO, a));
+        if (a.kb <= MP_RESIDENT_KB) ADLOCO_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, blockscale_pair_kernel<true>, tmA, tmB, tmO, a));
+        else ADLOCO_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, blockscale_pair_kernel<false>, tmA, tmB, tmO, a));
     } else {
         blockscale_tile_kernel<<<a.tiles < ctx->sm_count ? a.tiles : ctx->sm_count, MT_THREADS, MT_SMEM, st>>>(tmA, tmB, a);
         ADLOCO_CUDA_TRY(ctx, cudaGetLastError());

@@ -427,11 +427,11 @@ def test_matmul_propagates_nan_blocks_only_where_they_are(ctx, M):
     assert torch.isnan(out[1]).all() and torch.isfinite(out[torch.arange(M, device=DEV) != 1]).all()
 
 
-@pytest.mark.parametrize("M,N,K", [(300, 256, 512), (2600, 2304, 512)])
+@pytest.mark.parametrize("M,N,K", [(300, 256, 16384), (2600, 2304, 16384)])      # waits enough that the clock moves in one of them
 def test_matmul_wait_that_runs_out_is_reported_and_the_context_stays_usable(ctx, M, N, K):
     x, W = rnd(1, M, K, dtype=BF), rnd(2, N, K)
-    a, sa, b = pitched(M, K, 16), pitched(M, 4, 4), pitched(N, K, 16)
-    sb = torch.zeros(N // 128, 4, dtype=torch.uint8, device=DEV)
+    a, sa, b = pitched(M, K, 16), pitched(M, K // 128, 4), pitched(N, K, 16)
+    sb = torch.zeros(N // 128, K // 128, dtype=torch.uint8, device=DEV)
     ctx.blockscale_quantize(x, a, sa)
     ctx.blockscale_quantize_weight(W, b, sb)
     out, again = torch.zeros(M, N, device=DEV), torch.zeros(M, N, device=DEV)
