@@ -676,108 +676,141 @@ __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ Dr
 
 // ---- rotary positions -----------------------------------------------------------------------------
 // A thread takes one token and one unit of a head -- P pairs to rotate (two pieces of P elements: of either half, or
-// adjacent when interleaved), or two pieces of the part that is only copied -- in every heads_at_once-th head of all
-// tensors, so that its cosines and sines stay in registers over the heads.  Neighbouring threads take neighbouring
-// units, then heads, then tokens.  The block forms the cosines and sines of its tokens' positions once, in shared
-// memory, while the loads of the first heads are on their way.
+// adjacent when interleaved), or two pieces of the part that is only copied -- in kRopeHeads heads of one tensor, whose
+// loads it issues together before it forms its P sines and cosines, once for all of them.  Neighbouring threads take
+// neighbouring units, then heads, then tokens; a grid row takes a tensor, so that its pointers and strides are uniform.
+// What costs here is instructions: a thread that looked its heads' tensors up and converted element by element needed
+// 790 of them for 48 elements and took 69 us for the queries and keys of 32768 tokens of 12 heads of 64 in bf16.
 struct RopeArgs {
     adloco_rope_tensor t[4];
-    int n;
-    int heads_before[5];
+    int at_once[4], tokens_per_block[4];       // of a tensor: threads along its heads, tokens of a block
+    FastDiv by_heads[4];
     int64_t B, T, tokens;
-    int D, R, rot_units, units;        // units a head: rotated, and with the copied rest
-    int lanes, tokens_per_block, heads_at_once;      // lanes: threads along a head's units
-    FastDiv by_half, by_lanes, by_heads, by_T;
+    int D, R, rot_units, units;                // units a head: rotated, and with the copied rest
+    int lanes;                                 // threads along a head's units
+    FastDiv by_lanes, by_T;
     const uint64_t* turns;
     const int32_t* positions;
     int64_t positions_stride, first;
     float magnitude;
     int inverse;
 };
+// P adjacent elements as they lie in memory
 template <typename T, int P>
-struct alignas(sizeof(T) * P) Pack { T v[P]; };
-
-constexpr int kRopeHeads = 4;          // heads of a thread whose loads are issued together
+struct alignas(sizeof(T) * P) Piece;
+template <int P>
+struct alignas(4 * P) Piece<float, P> {
+    float v[P];
+    __device__ __forceinline__ void get(float* y) const {
+#pragma unroll
+        for (int p = 0; p < P; ++p) y[p] = v[p];
+    }
+    __device__ __forceinline__ void set(const float* y) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) v[p] = y[p];
+    }
+};
+template <int P>
+struct alignas(2 * P) Piece<__nv_bfloat16, P> {
+    uint32_t w[P / 2];
+    __device__ __forceinline__ void get(float* y) const {
+#pragma unroll
+        for (int i = 0; i < P / 2; ++i) { y[2 * i] = __uint_as_float(w[i] << 16); y[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+    __device__ __forceinline__ void set(const float* y) {
+#pragma unroll
+        for (int i = 0; i < P / 2; ++i) w[i] = pack2(F2{y[2 * i], y[2 * i + 1]});
+    }
+};
+template <>
+struct alignas(2) Piece<__nv_bfloat16, 1> {
+    __nv_bfloat16 v;
+    __device__ __forceinline__ void get(float* y) const { y[0] = __bfloat162float(v); }
+    __device__ __forceinline__ void set(const float* y) { v = __float2bfloat16_rn(y[0]); }
+};
 
 template <typename T, int P, bool INTERLEAVED>
-__global__ void __launch_bounds__(256) rope_kernel(const __grid_constant__ RopeArgs a) {
-    using V = Pack<T, P>;
-    extern __shared__ float2 turn_cs[];                // [tokens_per_block][R / 2]
-    const int half = a.R / 2;
-    const uint32_t token0 = blockIdx.x * (uint32_t)a.tokens_per_block;
-    const int here = (int)min((int64_t)a.tokens_per_block, a.tokens - token0);
+__device__ __forceinline__ void rotate(Piece<T, P>& x0, Piece<T, P>& x1, const float (&cs)[P], const float (&sn)[P]) {
+    float y[2 * P];                                    // pair p: y[2p], y[2p + 1] interleaved, else y[p], y[P + p]
+    x0.get(y);
+    x1.get(y + P);
+    if (P == 1) {
+        const float lo = y[0], hi = y[P];
+        y[0] = lo * cs[0] - hi * sn[0];
+        y[P] = lo * sn[0] + hi * cs[0];
+    }
+#pragma unroll
+    for (int p = 0; p + 1 < P; p += 2) {               // two pairs an instruction
+        float &l0 = y[INTERLEAVED ? 2 * p : p], &l1 = y[INTERLEAVED ? 2 * p + 2 : p + 1];
+        float &h0 = y[INTERLEAVED ? 2 * p + 1 : P + p], &h1 = y[INTERLEAVED ? 2 * p + 3 : P + p + 1];
+        const F2 lo = {l0, l1}, hi = {h0, h1}, c = {cs[p], cs[p + 1]}, s = {sn[p], sn[p + 1]};
+        const F2 a = mul2(hi, s), b = fma2(lo, s, mul2(hi, c));
+        const F2 d = fma2(lo, c, F2{-a.x, -a.y});
+        l0 = d.x; l1 = d.y;
+        h0 = b.x; h1 = b.y;
+    }
+    x0.set(y);
+    x1.set(y + P);
+}
+// Sine and cosine of top 2^-31 half turns.  For fp32 outputs to fp32; for bf16 ones by the fast instructions, whose error of
+// 2^-21 is far below the outputs' rounding.
+__device__ __forceinline__ void sine_cosine(int32_t top, float& sn, float& cs, float) { sincospif((float)top * 0x1p-31f, &sn, &cs); }
+__device__ __forceinline__ void sine_cosine(int32_t top, float& sn, float& cs, __nv_bfloat16) {
+    const float angle = (float)top * (3.14159265358979f * 0x1p-31f);      // in [-pi, pi]
+    sn = __sinf(angle);
+    cs = __cosf(angle);
+}
+
+constexpr int kRopeHeads = 6;
+
+template <typename T, int P, bool INTERLEAVED>
+__global__ void __launch_bounds__(256, 2) rope_kernel(const __grid_constant__ RopeArgs a) {
+    using V = Piece<T, P>;
+    const adloco_rope_tensor& t = a.t[blockIdx.y];
+    const int heads = (int)t.heads, at_once = a.at_once[blockIdx.y], tokens_per_block = a.tokens_per_block[blockIdx.y];
     const uint32_t slot = a.by_lanes(threadIdx.x), lane = threadIdx.x - slot * a.lanes;
-    const uint32_t tok = a.by_heads(slot);
-    const int head0 = (int)(slot - tok * a.heads_at_once), heads = a.heads_before[a.n];
-    const bool mine = (int)tok < here;
-    const uint32_t b = a.by_T(token0 + (mine ? tok : 0u)), s = token0 + (mine ? tok : 0u) - b * (uint32_t)a.T;
-    bool formed = false;
-    for (int unit = (int)lane; unit < a.units || !formed; unit += a.lanes) {
+    const uint32_t tok = a.by_heads[blockIdx.y](slot);
+    const int head0 = (int)slot - (int)tok * at_once;
+    const int64_t token = (int64_t)blockIdx.x * tokens_per_block + tok;
+    if ((int)tok >= tokens_per_block || token >= a.tokens) return;
+    const uint32_t b = a.by_T((uint32_t)token), s = (uint32_t)token - b * (uint32_t)a.T;
+    const int64_t in_step = at_once * t.in_head, out_step = at_once * t.out_head;
+    for (int unit = (int)lane; unit < a.units; unit += a.lanes) {
         const bool rotates = unit < a.rot_units;
         // the two pieces; of the copied part the second may lie beyond the head
-        const int at0 = rotates ? (INTERLEAVED ? 2 * unit * P : unit * P) : a.R + (unit - a.rot_units) * 2 * P;
-        const int at1 = rotates && !INTERLEAVED ? at0 + half : at0 + P;
-        const bool second = at1 < a.D;
-        float2 cs[P];
-        for (int h0 = head0; h0 < heads || !formed; h0 += kRopeHeads * a.heads_at_once) {
+        const int at = rotates ? (INTERLEAVED ? 2 * unit * P : unit * P) : a.R + (unit - a.rot_units) * 2 * P;
+        const int apart = rotates && !INTERLEAVED ? a.R / 2 : P;
+        const bool second = at + apart < a.D;
+        const T* in = static_cast<const T*>(t.in) + b * t.in_batch + s * t.in_token + head0 * t.in_head + at;
+        T* out = static_cast<T*>(t.out) + b * t.out_batch + s * t.out_token + head0 * t.out_head + at;
+        float cs[P], sn[P];
+        for (int h0 = head0; h0 < heads; h0 += kRopeHeads * at_once) {
             V x0[kRopeHeads], x1[kRopeHeads];
-            T* out[kRopeHeads];
 #pragma unroll
             for (int i = 0; i < kRopeHeads; ++i) {
-                int head = h0 + i * a.heads_at_once;
-                out[i] = nullptr;
-                if (!mine || unit >= a.units || head >= heads) continue;
-                int k = 0;
-#pragma unroll
-                for (int q = 1; q < 4; ++q) k += q < a.n && head >= a.heads_before[q];
-                head -= a.heads_before[k];
-                const adloco_rope_tensor& t = a.t[k];
-                const T* in = static_cast<const T*>(t.in) + b * t.in_batch + s * t.in_token + head * t.in_head;
-                out[i] = static_cast<T*>(t.out) + b * t.out_batch + s * t.out_token + head * t.out_head;
-                x0[i] = *reinterpret_cast<const V*>(in + at0);
-                if (second) x1[i] = *reinterpret_cast<const V*>(in + at1);
+                if (h0 + i * at_once >= heads) continue;
+                x0[i] = *reinterpret_cast<const V*>(in + i * in_step);
+                if (second) x1[i] = *reinterpret_cast<const V*>(in + i * in_step + apart);
             }
-            if (!formed) {                             // every thread of the block comes here once
-                for (int i = threadIdx.x; i < here * half; i += 256) {
-                    const uint32_t w = a.by_half(i), j = i - w * half;
-                    const uint32_t wb = a.by_T(token0 + w), ws = token0 + w - wb * (uint32_t)a.T;
-                    const int64_t pos = a.positions ? (int64_t)a.positions[wb * a.positions_stride + ws] : a.first + (int64_t)ws;
-                    // the phase in units of 2^-64 turns is exact; its top 32 bits, as a signed number, are half turns in [-1, 1)
-                    const int32_t top = (int32_t)(((uint64_t)pos * a.turns[j]) >> 32);
-                    float sn, co;
-                    sincospif((float)top * 4.656612873077392578125e-10f, &sn, &co);
-                    if (a.inverse) sn = -sn;
-                    turn_cs[i] = make_float2(a.magnitude * co, a.magnitude * sn);
-                }
-                __syncthreads();
-                formed = true;
-            }
-            if (!mine || unit >= a.units) break;
             if (rotates && h0 == head0) {
+                const int64_t pos = a.positions ? (int64_t)a.positions[b * a.positions_stride + s] : a.first + (int64_t)s;
 #pragma unroll
-                for (int p = 0; p < P; ++p) cs[p] = turn_cs[tok * half + unit * P + p];
+                for (int p = 0; p < P; ++p) {
+                    // the phase in units of 2^-64 turns is exact; its top 32 bits, as a signed number, are half turns in [-1, 1)
+                    sine_cosine((int32_t)(((uint64_t)pos * __ldg(a.turns + unit * P + p)) >> 32), sn[p], cs[p], T());
+                    cs[p] *= a.magnitude;
+                    sn[p] *= a.inverse ? -a.magnitude : a.magnitude;
+                }
             }
 #pragma unroll
             for (int i = 0; i < kRopeHeads; ++i) {
-                if (out[i] == nullptr) continue;
-                if (rotates) {
-                    float f[2 * P];                    // pair p: f[2p], f[2p + 1] interleaved, else f[p], f[P + p]
-#pragma unroll
-                    for (int p = 0; p < P; ++p) { f[p] = (float)x0[i].v[p]; f[P + p] = (float)x1[i].v[p]; }
-#pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        float& lo = f[INTERLEAVED ? 2 * p : p];
-                        float& hi = f[INTERLEAVED ? 2 * p + 1 : P + p];
-                        const float u = lo, w = hi;
-                        lo = u * cs[p].x - w * cs[p].y;
-                        hi = u * cs[p].y + w * cs[p].x;
-                    }
-#pragma unroll
-                    for (int p = 0; p < P; ++p) { x0[i].v[p] = (T)f[p]; x1[i].v[p] = (T)f[P + p]; }
-                }
-                *reinterpret_cast<V*>(out[i] + at0) = x0[i];
-                if (second) *reinterpret_cast<V*>(out[i] + at1) = x1[i];
+                if (h0 + i * at_once >= heads) continue;
+                if (rotates) rotate<T, P, INTERLEAVED>(x0[i], x1[i], cs, sn);
+                *reinterpret_cast<V*>(out + i * out_step) = x0[i];
+                if (second) *reinterpret_cast<V*>(out + i * out_step + apart) = x1[i];
             }
+            in += kRopeHeads * in_step;
+            out += kRopeHeads * out_step;
         }
     }
 }
@@ -1069,7 +1102,6 @@ int launch_rope(adloco_ctx* ctx, int bf16, const adloco_rope_tensor* t, int n, i
                 int inverse, cudaStream_t st) {
     RopeArgs a;
     memset(&a, 0, sizeof(a));
-    a.n = n;
     const int64_t es = bf16 ? 2 : 4;
     bool copies = false;                                 // in place the part that is not rotated is there already
     int64_t P = 16 / es;                                 // pairs a unit: up to 16 bytes on either side of the pairs
@@ -1078,7 +1110,6 @@ int launch_rope(adloco_ctx* ctx, int bf16, const adloco_rope_tensor* t, int n, i
         if (B == 1) a.t[i].in_batch = a.t[i].out_batch = 0;      // strides of extents of one are not looked at
         if (T == 1) a.t[i].in_token = a.t[i].out_token = 0;
         if (t[i].heads == 1) a.t[i].in_head = a.t[i].out_head = 0;
-        a.heads_before[i + 1] = a.heads_before[i] + (int)t[i].heads;
         copies = copies || t[i].in != t[i].out;
     }
     auto fits = [&](int64_t p) {
@@ -1097,27 +1128,27 @@ int launch_rope(adloco_ctx* ctx, int bf16, const adloco_rope_tensor* t, int n, i
     a.units = a.rot_units + (copies ? (int)((D - R + 2 * P - 1) / (2 * P)) : 0);
     a.turns = turns; a.positions = pos; a.positions_stride = pos_stride; a.first = first;
     a.magnitude = magnitude; a.inverse = inverse;
-    // a block's 256 threads: the units of a head, so many heads that a thread comes to about four of them, and with
-    // what is left tokens, as long as every SM has several blocks
-    const int heads = a.heads_before[n];
+    // a block's 256 threads: the units of a head, so many heads of the tensor that a thread comes to kRopeHeads of them, and
+    // tokens with what is left; where that gives an SM fewer than four blocks, more threads along the heads
     a.lanes = a.units < 256 ? a.units : 256;
-    const int slots = 256 / a.lanes;
-    a.heads_at_once = (heads + kRopeHeads - 1) / kRopeHeads;
-    if (a.heads_at_once > slots) a.heads_at_once = slots;
-    int64_t tpb = slots / a.heads_at_once;
-    const int64_t spread = a.tokens / (4 * (int64_t)ctx->sm_count), fit = 6144 / (R / 2);       // and 48 KB of sines
-    if (tpb > spread) tpb = spread;
-    if (tpb > fit) tpb = fit;
-    if (tpb < 1) tpb = 1;
-    if (tpb == 1) a.heads_at_once = heads < slots ? heads : slots;      // one token: all threads along its heads
-    a.tokens_per_block = (int)tpb;
-    a.by_half = FastDiv((uint32_t)(R / 2)); a.by_lanes = FastDiv((uint32_t)a.lanes);
-    a.by_heads = FastDiv((uint32_t)a.heads_at_once); a.by_T = FastDiv((uint32_t)T);
-    const unsigned grid = (unsigned)((a.tokens + tpb - 1) / tpb);
-    const size_t smem = (size_t)tpb * (size_t)(R / 2) * sizeof(float2);
+    a.by_lanes = FastDiv((uint32_t)a.lanes);
+    a.by_T = FastDiv((uint32_t)T);
+    const int64_t slots = 256 / a.lanes;
+    int64_t blocks = 0;
+    for (int i = 0; i < n; ++i) {
+        int64_t at_once = (t[i].heads + kRopeHeads - 1) / kRopeHeads;
+        while (at_once < t[i].heads && a.tokens * at_once < slots * 4 * ctx->sm_count) ++at_once;
+        if (at_once > slots) at_once = slots;
+        a.at_once[i] = (int)at_once;
+        a.tokens_per_block[i] = (int)(slots / at_once);
+        a.by_heads[i] = FastDiv((uint32_t)at_once);
+        const int64_t need = (a.tokens + a.tokens_per_block[i] - 1) / a.tokens_per_block[i];
+        if (need > blocks) blocks = need;
+    }
+    const dim3 grid((unsigned)blocks, (unsigned)n);
 #define ADLOCO_LAUNCH(TY, PP)                                                             \
-    if (interleaved) rope_kernel<TY, PP, true><<<grid, 256, smem, st>>>(a);               \
-    else rope_kernel<TY, PP, false><<<grid, 256, smem, st>>>(a)
+    if (interleaved) rope_kernel<TY, PP, true><<<grid, 256, 0, st>>>(a);               \
+    else rope_kernel<TY, PP, false><<<grid, 256, 0, st>>>(a)
     if (bf16) {
         if (P == 8) { ADLOCO_LAUNCH(__nv_bfloat16, 8); }
         else if (P == 4) { ADLOCO_LAUNCH(__nv_bfloat16, 4); }
