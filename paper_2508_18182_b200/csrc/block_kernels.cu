@@ -276,6 +276,51 @@ __device__ __forceinline__ float row_sum(float v, float* smem, int turn) {
     return s;
 }
 
+// ---- rows that do not start on 16-byte boundaries ------------------------------------------------
+// They pass through shared memory, coalesced on the global side element by element and in groups of eight on the other:
+// eight guarded scalar accesses a thread touch eight times the cache lines (norm backward of 1665 rows of 1001 fp32: 31 us).
+__host__ __device__ constexpr int pad8(int d) { return (d + 7) / 8 * 8; }
+template <int TPR>
+__device__ __forceinline__ void copy_in(float* buf, const float* row, int d, int t) {          // complete after copies_done()
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(buf));
+#pragma unroll 8
+    for (int j = t; j < d; j += TPR) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4u * j), "l"(row + j) : "memory");
+    if (t < pad8(d) - d) buf[d + t] = 0.f;
+}
+template <int TPR>
+__device__ __forceinline__ void copy_in(__nv_bfloat16* buf, const __nv_bfloat16* row, int d, int t) {
+#pragma unroll 16
+    for (int j = t; j < pad8(d); j += TPR) buf[j] = j < d ? row[j] : __nv_bfloat16(0.f);
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+template <int TPR, typename T>
+__device__ __forceinline__ void copy_out(T* row, const T* buf, int d, int t) {
+#pragma unroll 8
+    for (int j = t; j < d; j += TPR) row[j] = buf[j];
+}
+// the threads of a row (and, where a row is wider than a warp, of all rows of the block)
+template <int TPR>
+__device__ __forceinline__ void row_barrier() {
+    if (TPR == 32) __syncwarp();
+    else __syncthreads();
+}
+template <typename T>
+__device__ __forceinline__ Raw<T> from_buffer(const T* p) {
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+        r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void to_buffer(T* p, const Raw<T>& r) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+        reinterpret_cast<uint4*>(p)[i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+}
+
 __host__ __device__ constexpr int row_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 
 // ---- norm, forward --------------------------------------------------------------------------
@@ -284,29 +329,39 @@ __host__ __device__ constexpr int row_threads(int tpr) { return tpr > 256 ? tpr 
 template <typename XT, typename ST, int TPR, int C, bool VEC>
 __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __grid_constant__ adloco_rmsnorm_args a,
                                                                         const __grid_constant__ DropoutKey key) {
+    after_predecessor();
     constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
+    extern __shared__ __align__(16) uint8_t row_buffers[];                  // !VEC: x, then the residual, of ROWS rows
     __shared__ float smem[2 * THREADS / 32];
-    const int t = threadIdx.x % TPR;
-    const int64_t row_asked = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const int64_t row_asked = (int64_t)blockIdx.x * ROWS + sub;
     const bool there = row_asked < a.rows;
     if (TPR == 32 && !there) return;                       // whole warps leave; wider rows meet at a barrier
     const int64_t row = there ? row_asked : a.rows - 1;
     const int d = (int)a.d;
     const XT* x = static_cast<const XT*>(a.x) + row * a.x_stride;
     const ST* r = static_cast<const ST*>(a.residual) + row * a.residual_stride;
+    XT* x_buf = reinterpret_cast<XT*>(row_buffers) + sub * pad8(d);
+    ST* r_buf = reinterpret_cast<ST*>(reinterpret_cast<XT*>(row_buffers) + ROWS * pad8(d)) + sub * pad8(d);
+    if (!VEC) {
+        copy_in<TPR>(x_buf, x, d, t);
+        if (a.residual) copy_in<TPR>(r_buf, r, d, t);
+        copies_done();
+        row_barrier<TPR>();
+    }
     Raw<XT> xr[C];
     Raw<ST> rr[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int col = (c * TPR + t) * 8, n = min(8, d - col);
+        const int col = (c * TPR + t) * 8;
         xr[c] = zero_raw<XT>();
-        if (n > 0) xr[c] = load_raw<VEC>(x + col, n);
+        if (col < d) xr[c] = VEC ? load_raw<true>(x + col, 8) : from_buffer(x_buf + col);
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int col = (c * TPR + t) * 8, n = min(8, d - col);
+        const int col = (c * TPR + t) * 8;
         rr[c] = zero_raw<ST>();
-        if (a.residual && n > 0) rr[c] = load_raw<VEC>(r + col, n);
+        if (a.residual && col < d) rr[c] = VEC ? load_raw<true>(r + col, 8) : from_buffer(r_buf + col);
     }
     if (key.on) {
 #pragma unroll
@@ -319,7 +374,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
     F2 h[C][4], ss = both(0.f);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int col = (c * TPR + t) * 8, n = min(8, d - col);
+        const int col = (c * TPR + t) * 8;
         Raw<ST> out;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -327,7 +382,10 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
             ss = fma2(mul2(h[c][i], both(inv_d)), h[c][i], ss);      // the mean: a sum of squares that fit fp32 may not fit
             set_pair(out, i, h[c][i]);
         }
-        if (a.h && there && n > 0) store_raw<VEC>(static_cast<ST*>(a.h) + row * a.h_stride + col, n, out);
+        if (a.h && there && col < d) {
+            if (VEC) store_raw<true>(static_cast<ST*>(a.h) + row * a.h_stride + col, 8, out);
+            else to_buffer(r_buf + col, out);
+        }
     }
     const float mean = row_sum<TPR, THREADS>(ss.x + ss.y, smem, 0);
     const float rstd = rsqrtf(mean + a.eps);
@@ -353,9 +411,17 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
                     if (2 * i + 1 >= n) g[i].y = 0.f;
                 }
             }
-            if (a.y) store_raw<VEC>(static_cast<XT*>(a.y) + row * a.y_stride + col, n, out);
+            if (a.y) {
+                if (VEC) store_raw<true>(static_cast<XT*>(a.y) + row * a.y_stride + col, 8, out);
+                else to_buffer(x_buf + col, out);
+            }
         }
         if (a.q) quantise_block(g, n, q_row, s_row, col);
+    }
+    if (!VEC) {
+        row_barrier<TPR>();
+        if (a.h && there) copy_out<TPR>(static_cast<ST*>(a.h) + row * a.h_stride, r_buf, d, t);
+        if (a.y && there) copy_out<TPR>(static_cast<XT*>(a.y) + row * a.y_stride, x_buf, d, t);
     }
 }
 
@@ -397,12 +463,12 @@ __device__ __forceinline__ Raw<T> staged(uint32_t at, uint32_t step) {
 // 16-byte pieces a thread stages for one row: dy, h, and the stream's gradient
 template <typename XT, typename ST, int C>
 __host__ __device__ constexpr int stage_pieces() { return C * ((int)sizeof(XT) / 2 + 2 * ((int)sizeof(ST) / 2)); }
-// rows on their way or in use: three where they fit twice into an SM's shared memory, else two; one (no staging:
-// loads straight into registers) where not even two fit
+// rows on their way or in use: two (with three blocks an SM at widths up to 768 in bf16; three rows deep and two blocks
+// measured slower), or one -- no staging, loads straight into registers -- where two do not fit
 template <typename XT, typename ST, int C, int THREADS>
 __host__ __device__ constexpr int stage_depth() {
     const int row = stage_pieces<XT, ST, C>() * 16 * THREADS;
-    return 3 * row <= 112 * 1024 ? 3 : 2 * row <= 224 * 1024 ? 2 : 1;
+    return 2 * row <= 224 * 1024 ? 2 : 1;
 }
 template <typename XT, typename ST, int C, int THREADS>
 __host__ __device__ constexpr int stage_smem() { return stage_depth<XT, ST, C, THREADS>() < 2 ? 0 : stage_depth<XT, ST, C, THREADS>() * stage_pieces<XT, ST, C>() * 16 * THREADS; }
@@ -410,19 +476,25 @@ __host__ __device__ constexpr int stage_smem() { return stage_depth<XT, ST, C, T
 template <typename XT, typename ST, int TPR, int C, bool VEC, bool GAIN>
 __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(const __grid_constant__ RmsBackArgs p,
                                                                             const __grid_constant__ DropoutKey key) {
+    after_predecessor();
     constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
     constexpr uint32_t STEP = THREADS * 16;                 // piece i of thread t at i * STEP + 16 t: free of bank conflicts
     constexpr int XP = (int)sizeof(XT) / 2, SP = (int)sizeof(ST) / 2, PIECES = C * (XP + 2 * SP);
     constexpr int DEPTH = stage_depth<XT, ST, C, THREADS>();
     constexpr bool STAGED = VEC && DEPTH > 1;
     const adloco_rmsnorm_backward_args& a = p.a;
-    extern __shared__ __align__(16) float columns[];        // the staged rows; at the end [ROWS][d] (GAIN and ROWS > 1)
+    extern __shared__ __align__(16) float columns[];        // staged rows, or (!VEC) dy, h and the stream's gradient of ROWS rows;
+                                                            // at the end [ROWS][d] (GAIN and ROWS > 1)
     __shared__ float smem[2 * THREADS / 32];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = (int)a.d;
     const int64_t sample = (int64_t)blockIdx.x / p.chunks, chunk = (int64_t)blockIdx.x % p.chunks;
     const int64_t first = chunk * p.rows_per_chunk, last = min(a.T, first + p.rows_per_chunk);
     const float inv_d = 1.0f / (float)d;
     const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(columns)) + threadIdx.x * 16;
+    const int wide = pad8(d);
+    XT* u_buf = reinterpret_cast<XT*>(columns) + sub * wide;
+    ST* v_buf = reinterpret_cast<ST*>(reinterpret_cast<XT*>(columns) + ROWS * wide) + sub * wide;
+    ST* r_buf = v_buf + ROWS * wide;
     F2 acc[GAIN ? C : 1][4];
     if (GAIN) {
 #pragma unroll
@@ -453,68 +525,89 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
         for (int k = 0; k < DEPTH - 1; ++k) fetch(first + k * ROWS, k);
     }
     int turn = 0, stage = 0;
+    const float* rstds = a.rstd + sample * a.T;
+    float rstd_next = rstds[min(first + sub, last - 1)];     // a row ahead of its use
     for (int64_t at = first; at < last; at += ROWS, ++turn) {
         const bool there = at + sub < last;
         if (TPR == 32 && !there) break;
         const int64_t row = sample * a.T + (there ? at + sub : last - 1);
-        const float rstd = a.rstd[row];
+        const float rstd = rstd_next;
+        rstd_next = rstds[min(at + ROWS + sub, last - 1)];
+        const XT* dy = static_cast<const XT*>(a.dy) + row * a.dy_stride;
+        const ST* h = static_cast<const ST*>(a.h) + row * a.h_stride;
+        const ST* res = static_cast<const ST*>(a.dh_residual) + row * a.dh_residual_stride;
+        const uint32_t from = mine + (uint32_t)(stage * PIECES) * STEP;
         if (STAGED) {
-            // the stage freed by the row before last (its values are in registers or done with) takes the next fetch
+            // the stage freed by the row before (its values are in registers or stored) takes the next fetch
             fetch(at + (DEPTH - 1) * ROWS, stage == 0 ? DEPTH - 1 : stage - 1);
             asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+        } else if (!VEC) {
+            row_barrier<TPR>();                              // the buffers' last rows are stored
+            copy_in<TPR>(u_buf, dy, d, t);
+            copy_in<TPR>(v_buf, h, d, t);
+            if (a.dh_residual) copy_in<TPR>(r_buf, res, d, t);
+            copies_done();
+            row_barrier<TPR>();
         }
-        const uint32_t from = mine + (uint32_t)(stage * PIECES) * STEP;
-        F2 u[C][4], v[C][4], dot = both(0.f);
+        auto dy_of = [&](int c, int col) {
+            return STAGED ? staged<XT>(from + (c * XP) * STEP, STEP) : VEC ? load_raw<true>(dy + col, 8) : from_buffer(u_buf + col);
+        };
+        auto h_of = [&](int c, int col) {
+            return STAGED ? staged<ST>(from + (C * XP + c * SP) * STEP, STEP) : VEC ? load_raw<true>(h + col, 8) : from_buffer(v_buf + col);
+        };
+        // The row is gone through twice, before and after its sum, from shared memory: holding gain dy and xhat in registers in
+        // between left two blocks an SM instead of three.  (Rows too wide for two stages are read from global memory twice.)
+        F2 dot = both(0.f);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int col = (c * TPR + t) * 8, n = there ? min(8, d - col) : 0;
-            if (n <= 0) continue;
-            Raw<XT> ur;
-            Raw<ST> vr;
-            if (STAGED) {
-                ur = staged<XT>(from + (c * XP) * STEP, STEP);
-                vr = staged<ST>(from + (C * XP + c * SP) * STEP, STEP);
-            } else {
-                ur = load_raw<VEC>(static_cast<const XT*>(a.dy) + row * a.dy_stride + col, n);
-                vr = load_raw<VEC>(static_cast<const ST*>(a.h) + row * a.h_stride + col, n);
-            }
+            const int col = (c * TPR + t) * 8;
+            if (!there || col >= d) continue;
+            const Raw<XT> ur = dy_of(c, col);
+            const Raw<ST> vr = h_of(c, col);
             F2 g[4];
-            load_gain(a.gain, a.gain_dtype == ADLOCO_BF16, col, n, g);
+            load_gain(a.gain, a.gain_dtype == ADLOCO_BF16, col, min(8, d - col), g);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const F2 dy = pair_of(ur, i);
-                v[c][i] = mul2(pair_of(vr, i), both(rstd));                    // xhat
-                if (GAIN) acc[c][i] = fma2(dy, v[c][i], acc[c][i]);
-                u[c][i] = mul2(dy, g[i]);
-                dot = fma2(u[c][i], v[c][i], dot);
+                const F2 u = pair_of(ur, i), v = mul2(pair_of(vr, i), both(rstd));      // dy, xhat
+                if (GAIN) acc[c][i] = fma2(u, v, acc[c][i]);
+                dot = fma2(mul2(u, g[i]), v, dot);
             }
         }
         const float m = row_sum<TPR, THREADS>(dot.x + dot.y, smem, turn) * inv_d;
+        const float m_rstd = -m * rstd;
         if (there) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const int col = (c * TPR + t) * 8, n = min(8, d - col);
-                if (n <= 0) continue;
+                const int col = (c * TPR + t) * 8;
+                if (col >= d) continue;
+                const Raw<XT> ur = dy_of(c, col);
+                const Raw<ST> vr = h_of(c, col);
                 Raw<ST> r = zero_raw<ST>(), out;
-                if (a.dh_residual) {
-                    if (STAGED) r = staged<ST>(from + (C * XP + C * SP + c * SP) * STEP, STEP);
-                    else r = load_raw<VEC>(static_cast<const ST*>(a.dh_residual) + row * a.dh_residual_stride + col, n);
-                }
-                F2 o[4];
+                if (a.dh_residual)
+                    r = STAGED ? staged<ST>(from + (C * XP + C * SP + c * SP) * STEP, STEP) : VEC ? load_raw<true>(res + col, 8) : from_buffer(r_buf + col);
+                F2 g[4], o[4];
+                load_gain(a.gain, a.gain_dtype == ADLOCO_BF16, col, min(8, d - col), g);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    o[i] = fma2(fma2(v[c][i], both(-m), u[c][i]), both(rstd), pair_of(r, i));
+                    o[i] = fma2(fma2(pair_of(vr, i), both(m_rstd), mul2(pair_of(ur, i), g[i])), both(rstd), pair_of(r, i));
                     set_pair(out, i, o[i]);
                 }
-                store_raw<VEC>(static_cast<ST*>(a.dh) + row * a.dh_stride + col, n, out);
+                if (VEC) store_raw<true>(static_cast<ST*>(a.dh) + row * a.dh_stride + col, 8, out);
+                else to_buffer(v_buf + col, out);
                 if (a.dx) {
                     Raw<XT> x;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) set_pair(x, i, mul2(o[i], both(key.scale)));
                     if (key.on) drop_raw(x, kept_of<VEC>((uint64_t)(row * d + col), key), key);
-                    store_raw<VEC>(static_cast<XT*>(a.dx) + row * a.dx_stride + col, n, x);
+                    if (VEC) store_raw<true>(static_cast<XT*>(a.dx) + row * a.dx_stride + col, 8, x);
+                    else to_buffer(u_buf + col, x);
                 }
             }
+        }
+        if (!VEC) {
+            row_barrier<TPR>();
+            if (there) copy_out<TPR>(static_cast<ST*>(a.dh) + row * a.dh_stride, v_buf, d, t);
+            if (there && a.dx) copy_out<TPR>(static_cast<XT*>(a.dx) + row * a.dx_stride, u_buf, d, t);
         }
         stage = stage == DEPTH - 1 ? 0 : stage + 1;
     }
@@ -532,7 +625,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
             }
         return;
     }
-    __syncthreads();                                        // every thread is done with its stages
+    __syncthreads();                                        // every thread is done with its rows
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -550,50 +643,64 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
     }
 }
 
-// Adds up the workspace in a fixed order.  Blocks [0, B) (when norms are asked for): one sample's gradient over
-// all columns, squared and summed.  The rest: 32 columns each of the sum over all samples.
-constexpr int kGainThreads = 512;
-__global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float* part, int64_t B, int64_t chunks, int d,
-                                                                    float* norms, int accumulate_norms, float* sum,
-                                                                    int accumulate_sum) {
-    constexpr int G = kGainThreads / 32;
-    __shared__ float smem[G][33];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t norm_blocks = norms ? B : 0;
-    if ((int64_t)blockIdx.x < norm_blocks) {
-        const float* mine = part + (int64_t)blockIdx.x * chunks * d;
-        float ss = 0.f;
-        for (int col = threadIdx.x; col < d; col += kGainThreads) {
-            float g = 0.f;
-#pragma unroll 8
-            for (int64_t k = 0; k < chunks; ++k) g += mine[k * d + col];
-            ss = fmaf(g, g, ss);
-        }
-        ss = warp_sum(ss);
-        if (lane == 0) smem[0][warp] = ss;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            float n = 0.f;
-            for (int w = 0; w < G; ++w) n += smem[0][w];
-            if (accumulate_norms) atomicAdd(norms + blockIdx.x, n);      // layers on other streams add here too
-            else norms[blockIdx.x] = n;
-        }
-        return;
-    }
-    const int col = (int)(blockIdx.x - norm_blocks) * 32 + lane;
+// Adds up the workspace in a fixed order: a block takes 8 columns, a warp every 16th sample, and a lane one column in a
+// quarter of the sample's chunks.  Leaves the sum over all samples, and each sample's sum of squares over the 8 columns,
+// squares[block][sample], for rmsnorm_norms_kernel.
+constexpr int kGainThreads = 512, kGainCols = 8;
+__global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float* part, int64_t B, int64_t chunks, int d, float* squares,
+                                                                    float* sum, int accumulate_sum) {
+    constexpr int WARPS = kGainThreads / 32;
+    __shared__ float smem[WARPS][kGainCols];
+    after_predecessor();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = lane >> 3;
+    const int col = (int)blockIdx.x * kGainCols + (lane & 7);
     float s = 0.f;
-    if (col < d) {
-        const int64_t rows = B * chunks;
+    for (int64_t b = warp; b < B; b += WARPS) {
+        const float* mine = part + b * chunks * d + col;
+        float g = 0.f;
+        if (col < d) {
 #pragma unroll 8
-        for (int64_t k = warp; k < rows; k += G) s += part[k * d + col];
+            for (int64_t k = quarter; k < chunks; k += 4) g += mine[k * d];
+        }
+        g += __shfl_xor_sync(0xffffffffu, g, 8);
+        g += __shfl_xor_sync(0xffffffffu, g, 16);
+        s += g;
+        if (squares) {
+            float q = g * g;
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+            if (lane == 0) squares[(int64_t)blockIdx.x * B + b] = q;
+        }
     }
-    smem[warp][lane] = s;
+    if (!sum) return;
+    if (lane < kGainCols) smem[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && col < d) {
+    if (warp == 0 && lane < kGainCols && col < d) {
         float t = 0.f;
 #pragma unroll
-        for (int w = 0; w < G; ++w) t += smem[w][lane];
+        for (int w = 0; w < WARPS; ++w) t += smem[w][lane];
         sum[col] = accumulate_sum ? sum[col] + t : t;
+    }
+}
+// n_i from squares[blocks][B]: a block takes 32 samples, its warps share the rows
+__global__ void __launch_bounds__(256) rmsnorm_norms_kernel(const float* squares, int64_t B, int blocks, float* norms, int accumulate) {
+    __shared__ float smem[8][32];
+    after_predecessor();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t b = (int64_t)blockIdx.x * 32 + lane;
+    float n = 0.f;
+    if (b < B) {
+#pragma unroll 16
+        for (int k = warp; k < blocks; k += 8) n += squares[(int64_t)k * B + b];
+    }
+    smem[warp][lane] = n;
+    __syncthreads();
+    if (warp == 0 && b < B) {
+        n = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) n += smem[w][lane];
+        if (accumulate) atomicAdd(norms + b, n);      // layers on other streams add here too
+        else norms[b] = n;
     }
 }
 
@@ -610,6 +717,7 @@ struct DropArgs {
 };
 template <typename T, bool VEC, bool FLAT>
 __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropArgs a, const __grid_constant__ DropoutKey key) {
+    after_predecessor();
     constexpr int U = 2;
     const T* x = static_cast<const T*>(a.x);
     const T* r = static_cast<const T*>(a.r);
@@ -679,7 +787,7 @@ __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ Dr
 // adjacent when interleaved), or two pieces of the part that is only copied -- in kRopeHeads heads of one tensor, whose
 // loads it issues together before it forms its P sines and cosines, once for all of them.  Neighbouring threads take
 // neighbouring units, then heads, then tokens; a grid row takes a tensor, so that its pointers and strides are uniform.
-// What costs here is instructions: a thread that looked its heads' tensors up and converted element by element needed
+// What costs here is instructions and loads in flight (three heads a thread: 36 us, two at twice the warps: 39 us, six: 34 us): a thread that looked its heads' tensors up and converted element by element needed
 // 790 of them for 48 elements and took 69 us for the queries and keys of 32768 tokens of 12 heads of 64 in bf16.
 struct RopeArgs {
     adloco_rope_tensor t[4];
@@ -765,6 +873,7 @@ constexpr int kRopeHeads = 6;
 
 template <typename T, int P, bool INTERLEAVED>
 __global__ void __launch_bounds__(256, 2) rope_kernel(const __grid_constant__ RopeArgs a) {
+    after_predecessor();
     using V = Piece<T, P>;
     const adloco_rope_tensor& t = a.t[blockIdx.y];
     const int heads = (int)t.heads, at_once = a.at_once[blockIdx.y], tokens_per_block = a.tokens_per_block[blockIdx.y];
@@ -843,6 +952,7 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) quantise_rows_kernel(const T* x, int64_t x_stride, uint8_t* q, int64_t q_stride,
                                                             uint8_t* scale, int64_t scale_stride, uint32_t blocks, int64_t cols,
                                                             const __grid_constant__ FastDiv blocks_per_row) {
+    after_predecessor();
     constexpr int U = 2;
     const uint32_t b0 = blockIdx.x * (32 * U) + (threadIdx.x >> 3);
     const int lane_col = (threadIdx.x & 7) * 16;
@@ -893,6 +1003,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) quantise_weight_kernel(const T* W, int64_t W_stride, uint8_t* q, int64_t q_stride, uint8_t* q_t,
                                                               int64_t q_t_stride, uint8_t* scale, int64_t scale_stride, int64_t rows,
                                                               int64_t cols, int vec) {
+    after_predecessor();
     __shared__ uint32_t amax[8];
     alignas(16) __shared__ uint8_t tile[128][132];                   // [column][row]; rows of 33 words: threads of a warp fall on different banks
     const int64_t r0 = (int64_t)blockIdx.y * 128, c0 = (int64_t)blockIdx.x * 128;
@@ -972,58 +1083,81 @@ bool vec_rows(const void* p, int64_t stride, bool bf16) {
     else if (groups <= 1024) { LAUNCH(512, 2); }                                      \
     else { LAUNCH(512, 4); }
 
+// more than 48 KB of shared memory a block, static arrays included, has to be asked for, once for each kernel and device
+template <typename Kernel>
+static int allow_smem(adloco_ctx* ctx, Kernel kernel, size_t most, std::atomic<bool> (&done)[64]) {
+    if (done[ctx->device & 63].load()) return ADLOCO_OK;
+    ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most));
+    done[ctx->device & 63].store(true);
+    return ADLOCO_OK;
+}
+
+template <typename XT, typename ST, int TPR, int C, bool VEC>
+static int add_rmsnorm_launch(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const DropoutKey& key, cudaStream_t st) {
+    constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
+    auto kernel = add_rmsnorm_kernel<XT, ST, TPR, C, VEC>;
+    const size_t smem = VEC ? 0 : (size_t)ROWS * pad8((int)a.d) * (sizeof(XT) + sizeof(ST));
+    if (smem > 40 * 1024) {
+        static std::atomic<bool> done[64];
+        const int rc = allow_smem(ctx, kernel, (size_t)ROWS * TPR * C * 8 * (sizeof(XT) + sizeof(ST)), done);
+        if (rc != ADLOCO_OK) return rc;
+    }
+    ADLOCO_CUDA_TRY(ctx, launch_early(kernel, dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), THREADS, smem, st, 1, a, key));
+    return ADLOCO_OK;
+}
 template <typename XT, typename ST, bool VEC>
-static void add_rmsnorm_sized(const adloco_rmsnorm_args& a, const DropoutKey& key, cudaStream_t st) {
+static int add_rmsnorm_sized(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const DropoutKey& key, cudaStream_t st) {
     const int64_t d = a.d;
-#define ADLOCO_LAUNCH(TPR, C)                                                                                      \
-    add_rmsnorm_kernel<XT, ST, TPR, C, VEC>                                                                        \
-        <<<(unsigned)((a.rows + row_threads(TPR) / TPR - 1) / (row_threads(TPR) / TPR)), row_threads(TPR), 0, st>>>(a, key)
+    int rc = ADLOCO_OK;
+#define ADLOCO_LAUNCH(TPR, C) rc = add_rmsnorm_launch<XT, ST, TPR, C, VEC>(ctx, a, key, st)
     ADLOCO_ROW_CASES(ADLOCO_LAUNCH)
 #undef ADLOCO_LAUNCH
+    return rc;
 }
 
 int launch_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const DropoutKey& key, cudaStream_t st) {
     const bool xb = a.dtype == ADLOCO_BF16, sb = a.stream_dtype == ADLOCO_BF16;
     const bool vec = (a.d & 7) == 0 && vec_rows(a.x, a.x_stride, xb) && vec_rows(a.residual, a.residual_stride, sb) &&
                      vec_rows(a.h, a.h_stride, sb) && vec_rows(a.y, a.y_stride, xb);
+    int rc = ADLOCO_OK;
 #define ADLOCO_TYPES(XT, ST)                                              \
-    if (vec) add_rmsnorm_sized<XT, ST, true>(a, key, st);                 \
-    else add_rmsnorm_sized<XT, ST, false>(a, key, st)
+    if (vec) rc = add_rmsnorm_sized<XT, ST, true>(ctx, a, key, st);       \
+    else rc = add_rmsnorm_sized<XT, ST, false>(ctx, a, key, st)
     if (xb && sb) { ADLOCO_TYPES(__nv_bfloat16, __nv_bfloat16); }
     else if (xb) { ADLOCO_TYPES(__nv_bfloat16, float); }
     else { ADLOCO_TYPES(float, float); }
 #undef ADLOCO_TYPES
+    if (rc != ADLOCO_OK) return rc;
     ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
     ctx->launches++;
     return ADLOCO_OK;
 }
 
-// Blocks a sample's rows are cut into: about two blocks an SM over all samples, at least a row for every group of
+// Blocks a sample's rows are cut into: about as many over all samples as are resident at once (three an SM, two for wider rows), at least a row for every group of
 // threads in a block.
 static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d) {
     const int64_t rows_at_once = d <= 1024 ? 8 : d <= 4096 ? 2 : 1;
     const int64_t most = (T + rows_at_once - 1) / rows_at_once;
-    const int64_t want = 2 * (int64_t)ctx->sm_count / B;
+    const int64_t want = (d <= 768 ? 3 : 2) * (int64_t)ctx->sm_count / B;
     return want < 1 ? 1 : want > most ? most : want;
 }
 int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d) {
-    return B * rmsnorm_chunks(ctx, B, T, d) * d * (int64_t)sizeof(float);
+    return (B * rmsnorm_chunks(ctx, B, T, d) * d + B * ((d + kGainCols - 1) / kGainCols)) * (int64_t)sizeof(float);
 }
 
 template <typename XT, typename ST, int TPR, int C, bool VEC, bool GAIN>
 static int rmsnorm_backward_launch(adloco_ctx* ctx, const RmsBackArgs& p, const DropoutKey& key, unsigned grid, cudaStream_t st) {
     constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
     auto kernel = rmsnorm_backward_kernel<XT, ST, TPR, C, VEC, GAIN>;
-    size_t smem = VEC ? stage_smem<XT, ST, C, THREADS>() : 0;
+    constexpr size_t row_bytes = sizeof(XT) + 2 * sizeof(ST);
+    size_t smem = VEC ? stage_smem<XT, ST, C, THREADS>() : (size_t)ROWS * pad8((int)p.a.d) * row_bytes;
     if (GAIN && ROWS > 1 && smem < (size_t)ROWS * p.a.d * sizeof(float)) smem = (size_t)ROWS * p.a.d * sizeof(float);
-    if (smem > 48 * 1024) {
-        static std::atomic<bool> attr_set[64];   // the attribute is per device
-        if (!attr_set[ctx->device & 63].load()) {
-            ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-            attr_set[ctx->device & 63].store(true);
-        }
+    if (smem > 40 * 1024) {
+        static std::atomic<bool> done[64];
+        const int rc = allow_smem(ctx, kernel, VEC ? stage_smem<XT, ST, C, THREADS>() : (size_t)ROWS * TPR * C * 8 * row_bytes, done);
+        if (rc != ADLOCO_OK) return rc;
     }
-    kernel<<<grid, THREADS, smem, st>>>(p, key);
+    ADLOCO_CUDA_TRY(ctx, launch_early(kernel, dim3(grid), THREADS, smem, st, 1, p, key));
     return ADLOCO_OK;
 }
 
@@ -1061,12 +1195,17 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
     ctx->launches++;
     if (gain) {
-        const int64_t grid = (a.per_sample_sqnorm ? a.B : 0) + (a.grad_sum ? (a.d + 31) / 32 : 0);
-        rmsnorm_gain_kernel<<<(unsigned)grid, kGainThreads, 0, st>>>(static_cast<const float*>(a.workspace), a.B, p.chunks, (int)a.d,
-                                                                     a.per_sample_sqnorm, a.accumulate_norms, a.grad_sum,
-                                                                     a.accumulate_sum);
-        ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
+        const int blocks = (int)((a.d + kGainCols - 1) / kGainCols);
+        float* part = static_cast<float*>(a.workspace);
+        float* squares = a.per_sample_sqnorm ? part + a.B * p.chunks * a.d : nullptr;
+        ADLOCO_CUDA_TRY(ctx, launch_early(rmsnorm_gain_kernel, dim3((unsigned)blocks), kGainThreads, 0, st, 1, (const float*)part, a.B,
+                                          p.chunks, (int)a.d, squares, a.grad_sum, (int)a.accumulate_sum));
         ctx->launches++;
+        if (squares) {
+            ADLOCO_CUDA_TRY(ctx, launch_early(rmsnorm_norms_kernel, dim3((unsigned)((a.B + 31) / 32)), 256, 0, st, 1, (const float*)squares,
+                                              a.B, blocks, a.per_sample_sqnorm, (int)a.accumulate_norms));
+            ctx->launches++;
+        }
     }
     return ADLOCO_OK;
 }
@@ -1084,15 +1223,16 @@ int launch_dropout(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const 
     a.groups_per_row = FastDiv((uint32_t)(cols < 0x7fffffff ? (cols + 7) / 8 : 1));
     const int64_t want = (a.groups + 511) / 512, most = (int64_t)ctx->sm_count * 64;
     const unsigned grid = (unsigned)(want < most ? want : most);
+    cudaError_t e = cudaSuccess;
 #define ADLOCO_TYPES(T)                                                                          \
-    if (flat && vec) dropout_kernel<T, true, true><<<grid, 256, 0, st>>>(a, key);                \
-    else if (flat) dropout_kernel<T, false, true><<<grid, 256, 0, st>>>(a, key);                 \
-    else if (vec) dropout_kernel<T, true, false><<<grid, 256, 0, st>>>(a, key);                  \
-    else dropout_kernel<T, false, false><<<grid, 256, 0, st>>>(a, key)
+    if (flat && vec) e = launch_early(dropout_kernel<T, true, true>, dim3(grid), 256, 0, st, 1, a, key);                \
+    else if (flat) e = launch_early(dropout_kernel<T, false, true>, dim3(grid), 256, 0, st, 1, a, key);                 \
+    else if (vec) e = launch_early(dropout_kernel<T, true, false>, dim3(grid), 256, 0, st, 1, a, key);                  \
+    else e = launch_early(dropout_kernel<T, false, false>, dim3(grid), 256, 0, st, 1, a, key)
     if (bf16) { ADLOCO_TYPES(__nv_bfloat16); }
     else { ADLOCO_TYPES(float); }
 #undef ADLOCO_TYPES
-    ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
+    ADLOCO_CUDA_TRY(ctx, e);
     ctx->launches++;
     return ADLOCO_OK;
 }
@@ -1146,9 +1286,10 @@ int launch_rope(adloco_ctx* ctx, int bf16, const adloco_rope_tensor* t, int n, i
         if (need > blocks) blocks = need;
     }
     const dim3 grid((unsigned)blocks, (unsigned)n);
+    cudaError_t e = cudaSuccess;
 #define ADLOCO_LAUNCH(TY, PP)                                                             \
-    if (interleaved) rope_kernel<TY, PP, true><<<grid, 256, 0, st>>>(a);               \
-    else rope_kernel<TY, PP, false><<<grid, 256, 0, st>>>(a)
+    if (interleaved) e = launch_early(rope_kernel<TY, PP, true>, grid, 256, 0, st, 1, a);               \
+    else e = launch_early(rope_kernel<TY, PP, false>, grid, 256, 0, st, 1, a)
     if (bf16) {
         if (P == 8) { ADLOCO_LAUNCH(__nv_bfloat16, 8); }
         else if (P == 4) { ADLOCO_LAUNCH(__nv_bfloat16, 4); }
@@ -1160,7 +1301,7 @@ int launch_rope(adloco_ctx* ctx, int bf16, const adloco_rope_tensor* t, int n, i
         else { ADLOCO_LAUNCH(float, 1); }
     }
 #undef ADLOCO_LAUNCH
-    ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
+    ADLOCO_CUDA_TRY(ctx, e);
     ctx->launches++;
     return ADLOCO_OK;
 }
@@ -1171,15 +1312,16 @@ int launch_blockscale_quantize(adloco_ctx* ctx, int bf16, int64_t rows, int64_t 
     if (rows > 0x7fffffff / per_row) return ADLOCO_ERR_UNSUPPORTED;
     const uint32_t blocks = (uint32_t)(rows * per_row), grid = (blocks + 63) / 64;
     const bool vec = vec_rows(x, x_stride, bf16);
-#define ADLOCO_LAUNCH(T, V)                                                                                          \
-    quantise_rows_kernel<T, V><<<grid, 256, 0, st>>>(static_cast<const T*>(x), x_stride, static_cast<uint8_t*>(q),   \
-                                                     q_stride, scale, scale_stride, blocks, cols, FastDiv((uint32_t)per_row))
+    cudaError_t e = cudaSuccess;
+#define ADLOCO_LAUNCH(T, V)                                                                                                      \
+    e = launch_early(quantise_rows_kernel<T, V>, dim3(grid), 256, 0, st, 1, static_cast<const T*>(x), x_stride, static_cast<uint8_t*>(q), \
+                     q_stride, scale, scale_stride, blocks, cols, FastDiv((uint32_t)per_row))
     if (bf16 && vec) ADLOCO_LAUNCH(__nv_bfloat16, true);
     else if (bf16) ADLOCO_LAUNCH(__nv_bfloat16, false);
     else if (vec) ADLOCO_LAUNCH(float, true);
     else ADLOCO_LAUNCH(float, false);
 #undef ADLOCO_LAUNCH
-    ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
+    ADLOCO_CUDA_TRY(ctx, e);
     ctx->launches++;
     return ADLOCO_OK;
 }
@@ -1192,13 +1334,14 @@ int launch_blockscale_quantize_weight(adloco_ctx* ctx, int bf16, int64_t rows, i
     const int vec = vec_rows(W, W_stride, bf16);
     const dim3 grid((unsigned)gx, (unsigned)gy);
     uint8_t *qb = static_cast<uint8_t*>(q), *qtb = static_cast<uint8_t*>(q_t);
+    cudaError_t e;
     if (bf16)
-        quantise_weight_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(W), W_stride, qb, q_stride, qtb,
-                                                                    q_t_stride, scale, scale_stride, rows, cols, vec);
+        e = launch_early(quantise_weight_kernel<__nv_bfloat16>, grid, 256, 0, st, 1, static_cast<const __nv_bfloat16*>(W), W_stride, qb,
+                         q_stride, qtb, q_t_stride, scale, scale_stride, rows, cols, vec);
     else
-        quantise_weight_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float*>(W), W_stride, qb, q_stride, qtb, q_t_stride,
-                                                            scale, scale_stride, rows, cols, vec);
-    ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
+        e = launch_early(quantise_weight_kernel<float>, grid, 256, 0, st, 1, static_cast<const float*>(W), W_stride, qb, q_stride, qtb,
+                         q_t_stride, scale, scale_stride, rows, cols, vec);
+    ADLOCO_CUDA_TRY(ctx, e);
     ctx->launches++;
     return ADLOCO_OK;
 }

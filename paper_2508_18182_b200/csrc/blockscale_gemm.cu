@@ -181,6 +181,7 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    after_predecessor();
     const uint32_t tmem = tmem_slot;
     volatile int* abortp = &abort_flag;
 
@@ -391,6 +392,7 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     __syncthreads();
     cluster_sync_all();                                        // the peer's barriers exist before anything is signalled on them
     tc_fence_after();
+    after_predecessor();
     const uint32_t tmem = tmem_slot;
     volatile int* abortp = &abort_flag;
 
@@ -658,21 +660,11 @@ int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
             if (rc != ADLOCO_OK) return rc;
         }
         const int workers = a.tiles < ctx->sm_count / 2 ? a.tiles : ctx->sm_count / 2;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(2 * workers));
-        cfg.blockDim = dim3(MP_THREADS);
-        cfg.dynamicSmemBytes = MP_SMEM;
-        cfg.stream = st;
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
-        if (a.kb <= MP_RESIDENT_KB) ADLOCO_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, blockscale_pair_kernel<true>, tmA, tmB, tmO, a));
-        else ADLOCO_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, blockscale_pair_kernel<false>, tmA, tmB, tmO, a));
+        if (a.kb <= MP_RESIDENT_KB) ADLOCO_CUDA_TRY(ctx, launch_early(blockscale_pair_kernel<true>, dim3(2 * workers), MP_THREADS, MP_SMEM, st, 2, tmA, tmB, tmO, a));
+        else ADLOCO_CUDA_TRY(ctx, launch_early(blockscale_pair_kernel<false>, dim3(2 * workers), MP_THREADS, MP_SMEM, st, 2, tmA, tmB, tmO, a));
     } else {
-        blockscale_tile_kernel<<<a.tiles < ctx->sm_count ? a.tiles : ctx->sm_count, MT_THREADS, MT_SMEM, st>>>(tmA, tmB, a);
-        ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
+        ADLOCO_CUDA_TRY(ctx, launch_early(blockscale_tile_kernel, dim3(a.tiles < ctx->sm_count ? a.tiles : ctx->sm_count), MT_THREADS, MT_SMEM,
+                                          st, 1, tmA, tmB, a));
     }
     ctx->launches++;
     return ADLOCO_OK;

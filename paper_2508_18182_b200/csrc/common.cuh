@@ -112,6 +112,36 @@ inline int check_params(const adloco_test_params* p) {
     return ADLOCO_OK;
 }
 
+// A launch that may begin while the kernel before it on the stream drains (programmatic dependent launch): the kernel
+// calls after_predecessor() before it touches memory, which waits for that kernel's completion and its writes.  Only for
+// kernels that do.
+#ifdef __CUDACC__
+__device__ __forceinline__ void after_predecessor() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+template <typename... Params, typename... Args>
+inline cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, unsigned cluster,
+                                const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cluster > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+#endif
+
 // ---- launchers implemented in stream_kernels.cu --------------------------------
 enum NtMode { NT_ONESHOT = 0, NT_PANEL = 1, NT_MICRO = 2 };
 
