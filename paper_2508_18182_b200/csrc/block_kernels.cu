@@ -436,6 +436,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
 struct RmsBackArgs {
     adloco_rmsnorm_backward_args a;
     int64_t chunks, rows_per_chunk;
+    unsigned* ticket;          // of rmsnorm_gain_kernel; set to zero here
 };
 __device__ __forceinline__ void copy16_async(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -489,6 +490,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = (int)a.d;
     const int64_t sample = (int64_t)blockIdx.x / p.chunks, chunk = (int64_t)blockIdx.x % p.chunks;
     const int64_t first = chunk * p.rows_per_chunk, last = min(a.T, first + p.rows_per_chunk);
+    if (GAIN && blockIdx.x == 0 && threadIdx.x == 0) *p.ticket = 0u;
     const float inv_d = 1.0f / (float)d;
     const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(columns)) + threadIdx.x * 16;
     const int wide = pad8(d);
@@ -643,43 +645,80 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
     }
 }
 
-// Adds up the workspace in a fixed order: a block takes 8 columns, a warp every 16th sample, and a lane one column in a
-// quarter of the sample's chunks.  Leaves the sum over all samples, and each sample's sum of squares over the 8 columns,
-// squares[block][sample], for rmsnorm_norms_kernel.
+// Adds up the workspace in a fixed order: a block takes 8 columns, a warp every 16th sample (two at a time), and a lane one
+// column in a quarter of the sample's chunks.  Leaves the sum over all samples, and each sample's sum of squares over the 8
+// columns, squares[block][sample].  The last block to finish adds those up to the norms; for many samples, where one block
+// would be long at it, rmsnorm_norms_kernel does (ticket null).
 constexpr int kGainThreads = 512, kGainCols = 8;
+constexpr int64_t kGainLastBlock = 128;          // samples up to which the last block forms the norms
+__device__ __forceinline__ void put_norm(float* norms, int64_t b, float n, int accumulate) {
+    if (accumulate) atomicAdd(norms + b, n);      // layers on other streams add here too
+    else norms[b] = n;
+}
 __global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float* part, int64_t B, int64_t chunks, int d, float* squares,
-                                                                    float* sum, int accumulate_sum) {
+                                                                    float* sum, int accumulate_sum, unsigned* ticket, float* norms,
+                                                                    int accumulate_norms) {
     constexpr int WARPS = kGainThreads / 32;
-    __shared__ float smem[WARPS][kGainCols];
+    __shared__ float smem[WARPS][33];
+    __shared__ bool last;
     after_predecessor();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = lane >> 3;
     const int col = (int)blockIdx.x * kGainCols + (lane & 7);
     float s = 0.f;
-    for (int64_t b = warp; b < B; b += WARPS) {
-        const float* mine = part + b * chunks * d + col;
-        float g = 0.f;
+    for (int64_t b0 = warp; b0 < B; b0 += 2 * WARPS) {
+        float g[2] = {0.f, 0.f};
         if (col < d) {
-#pragma unroll 8
-            for (int64_t k = quarter; k < chunks; k += 4) g += mine[k * d];
+#pragma unroll 4
+            for (int64_t k = quarter; k < chunks; k += 4) {
+                g[0] += part[(b0 * chunks + k) * d + col];
+                if (b0 + WARPS < B) g[1] += part[((b0 + WARPS) * chunks + k) * d + col];
+            }
         }
-        g += __shfl_xor_sync(0xffffffffu, g, 8);
-        g += __shfl_xor_sync(0xffffffffu, g, 16);
-        s += g;
-        if (squares) {
-            float q = g * g;
 #pragma unroll
-            for (int o = 4; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
-            if (lane == 0) squares[(int64_t)blockIdx.x * B + b] = q;
+        for (int j = 0; j < 2; ++j) {
+            g[j] += __shfl_xor_sync(0xffffffffu, g[j], 8);
+            g[j] += __shfl_xor_sync(0xffffffffu, g[j], 16);
+            s += g[j];
+            if (squares) {
+                float q = g[j] * g[j];
+#pragma unroll
+                for (int o = 4; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+                if (lane == 0 && b0 + j * WARPS < B) squares[(int64_t)blockIdx.x * B + b0 + j * WARPS] = q;
+            }
         }
     }
-    if (!sum) return;
-    if (lane < kGainCols) smem[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0 && lane < kGainCols && col < d) {
-        float t = 0.f;
+    if (sum) {
+        if (lane < kGainCols) smem[warp][lane] = s;
+        __syncthreads();
+        if (warp == 0 && lane < kGainCols && col < d) {
+            float t = 0.f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) t += smem[w][lane];
-        sum[col] = accumulate_sum ? sum[col] + t : t;
+            for (int w = 0; w < WARPS; ++w) t += smem[w][lane];
+            sum[col] = accumulate_sum ? sum[col] + t : t;
+        }
+    }
+    if (!ticket) return;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    for (int64_t b0 = 0; b0 < B; b0 += 32) {
+        float n = 0.f;
+        if (b0 + lane < B) {
+#pragma unroll 8
+            for (int k = warp; k < (int)gridDim.x; k += WARPS) n += __ldcg(squares + (int64_t)k * B + b0 + lane);
+        }
+        smem[warp][lane] = n;
+        __syncthreads();
+        if (warp == 0 && b0 + lane < B) {
+            n = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) n += smem[w][lane];
+            put_norm(norms, b0 + lane, n, accumulate_norms);
+        }
+        __syncthreads();
     }
 }
 // n_i from squares[blocks][B]: a block takes 32 samples, its warps share the rows
@@ -699,87 +738,98 @@ __global__ void __launch_bounds__(256) rmsnorm_norms_kernel(const float* squares
         n = 0.f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) n += smem[w][lane];
-        if (accumulate) atomicAdd(norms + b, n);      // layers on other streams add here too
-        else norms[b] = n;
+        put_norm(norms, b, n, accumulate);
     }
 }
 
 // ---- dropout ------------------------------------------------------------------------------------
 // A thread takes the eight elements of one call of the generator, two such groups at a time so that enough loads
 // are in flight.  The eight are adjacent in memory unless a row ends among them; the vector form needs rows of a
-// multiple of eight elements, or no gaps between rows (FLAT).
+// multiple of eight elements, or no gaps between rows (FLAT), and takes whole groups only.
 struct DropArgs {
     const void *x, *r;
     void* y;
-    int64_t rows, cols, x_stride, r_stride, y_stride, groups;
+    int64_t rows, cols, x_stride, r_stride, y_stride;
+    int64_t groups, whole;           // groups, and those of eight elements
     int small;                       // group indices are below 2^31
     FastDiv groups_per_row;          // VEC rows
 };
-template <typename T, bool VEC, bool FLAT>
-__global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropArgs a, const __grid_constant__ DropoutKey key) {
-    after_predecessor();
-    constexpr int U = 2;
+// the elements of a group that has fewer than eight, or that a row's end or the alignment cuts
+template <typename T>
+__device__ __noinline__ void drop_elements(const DropArgs& a, const DropoutKey& key, int64_t g) {
     const T* x = static_cast<const T*>(a.x);
     const T* r = static_cast<const T*>(a.r);
     T* y = static_cast<T*>(a.y);
-    const int64_t total = a.rows * a.cols;
-    for (int64_t g0 = (int64_t)blockIdx.x * (256 * U) + threadIdx.x; g0 < a.groups; g0 += (int64_t)gridDim.x * (256 * U)) {
-        Raw<T> v[U], s[U];
-        int64_t row[U], col[U];
+    const int64_t e = g * 8;
+    const int n = (int)min((int64_t)8, a.rows * a.cols - e);
+    int64_t row = e / a.cols, col = e - row * a.cols;
+    Raw<float> v = zero_raw<float>(), s = zero_raw<float>();
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int64_t g = g0 + k * 256, e = g * 8;
-            row[k] = 0; col[k] = e;
-            if (g >= a.groups) continue;
-            if (!FLAT) {
-                if (VEC) row[k] = a.small ? (int64_t)a.groups_per_row((uint32_t)g) : g / (int64_t)a.groups_per_row.d;
-                else row[k] = e / a.cols;
-                col[k] = e - row[k] * a.cols;
-            }
-            const int n = (int)min((int64_t)8, total - e);
-            if (VEC && n == 8) {
-                v[k] = load_raw<true>(x + row[k] * a.x_stride + col[k], 8);
-                if (r) s[k] = load_raw<true>(r + row[k] * a.r_stride + col[k], 8);
-            } else if (FLAT) {
-                v[k] = load_raw<false>(x + e, n);
-                if (r) s[k] = load_raw<false>(r + e, n);
-            } else {
-                v[k] = zero_raw<T>();
-                s[k] = zero_raw<T>();
-                T* vv = reinterpret_cast<T*>(v[k].w);
-                T* ss = reinterpret_cast<T*>(s[k].w);
-                int64_t i = row[k], j = col[k];
-                for (int q = 0; q < n; ++q) {
-                    vv[q] = x[i * a.x_stride + j];
-                    if (r) ss[q] = r[i * a.r_stride + j];
-                    if (++j == a.cols) { j = 0; ++i; }
-                }
-            }
-        }
+    for (int q = 0; q < 8; ++q) {
+        if (q >= n) continue;
+        v.w[q] = __float_as_uint((float)x[row * a.x_stride + col]);
+        if (r) s.w[q] = __float_as_uint((float)r[row * a.r_stride + col]);
+        if (++col == a.cols) { col = 0; ++row; }
+    }
+    if (key.on) drop_raw(v, kept_of<true>((uint64_t)e, key), key);
+    row = e / a.cols;
+    col = e - row * a.cols;
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int64_t g = g0 + k * 256, e = g * 8;
-            if (g >= a.groups) continue;
-            if (key.on) drop_raw(v[k], kept_of<true>((uint64_t)e, key), key);
-            Raw<T> out;
+    for (int i = 0; i < 4; ++i) {
+        const F2 o = scaled(pair_of(v, i), key, pair_of(s, i));
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                set_pair(out, i, scaled(pair_of(v[k], i), key, r ? pair_of(s[k], i) : both(0.f)));
-            const int n = (int)min((int64_t)8, total - e);
-            if (VEC && n == 8) {
-                store_raw<true>(y + row[k] * a.y_stride + col[k], 8, out);
-            } else if (FLAT) {
-                store_raw<false>(y + e, n, out);
-            } else {
-                const T* oo = reinterpret_cast<const T*>(out.w);
-                int64_t i = row[k], j = col[k];
-                for (int q = 0; q < n; ++q) {
-                    y[i * a.y_stride + j] = oo[q];
-                    if (++j == a.cols) { j = 0; ++i; }
-                }
-            }
+        for (int q = 2 * i; q < 2 * i + 2; ++q) {
+            if (q >= n) continue;
+            y[row * a.y_stride + col] = (T)(q & 1 ? o.y : o.x);
+            if (++col == a.cols) { col = 0; ++row; }
         }
     }
+}
+template <typename T, bool VEC, bool FLAT, bool RES>
+__global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropArgs a, const __grid_constant__ DropoutKey key) {
+    constexpr int U = 2;
+    after_predecessor();
+    const T* x = static_cast<const T*>(a.x);
+    const T* r = static_cast<const T*>(a.r);
+    T* y = static_cast<T*>(a.y);
+    for (int64_t g0 = (int64_t)blockIdx.x * (256 * U) + threadIdx.x; g0 < a.groups; g0 += (int64_t)gridDim.x * (256 * U)) {
+        if constexpr (!VEC) {
+            drop_elements<T>(a, key, g0);
+            if (g0 + 256 < a.groups) drop_elements<T>(a, key, g0 + 256);
+            continue;
+        } else {
+        Raw<T> v[U], s[U];
+        int64_t out[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t g = g0 + k * 256;
+            if (g >= a.whole) continue;
+            int64_t at = g * 8, at_r = at;
+            out[k] = at;
+            if (!FLAT) {
+                const int64_t row = a.small ? (int64_t)a.groups_per_row((uint32_t)g) : g / (int64_t)a.groups_per_row.d;
+                const int64_t col = at - row * a.cols;
+                at = row * a.x_stride + col;
+                at_r = row * a.r_stride + col;
+                out[k] = row * a.y_stride + col;
+            }
+            v[k] = load_raw<true>(x + at, 8);
+            if (RES) s[k] = load_raw<true>(r + at_r, 8);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t g = g0 + k * 256;
+            if (g >= a.whole) continue;
+            if (key.on) drop_raw(v[k], kept_of<true>((uint64_t)g * 8, key), key);
+            Raw<T> o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                set_pair(o, i, RES ? scaled(pair_of(v[k], i), key, pair_of(s[k], i)) : mul2(pair_of(v[k], i), both(key.scale)));
+            store_raw<true>(y + out[k], 8, o);
+        }
+        }
+    }
+    if (VEC && blockIdx.x == 0 && threadIdx.x == 0 && a.whole < a.groups) drop_elements<T>(a, key, a.whole);
 }
 
 // ---- rotary positions -----------------------------------------------------------------------------
@@ -1142,7 +1192,8 @@ static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64
     return want < 1 ? 1 : want > most ? most : want;
 }
 int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d) {
-    return (B * rmsnorm_chunks(ctx, B, T, d) * d + B * ((d + kGainCols - 1) / kGainCols)) * (int64_t)sizeof(float);
+    // partial gradients, partial squares, and a counter
+    return (B * rmsnorm_chunks(ctx, B, T, d) * d + B * ((d + kGainCols - 1) / kGainCols) + 1) * (int64_t)sizeof(float);
 }
 
 template <typename XT, typename ST, int TPR, int C, bool VEC, bool GAIN>
@@ -1181,6 +1232,7 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     p.a = a;
     p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d);
     p.rows_per_chunk = (a.T + p.chunks - 1) / p.chunks;
+    p.ticket = gain ? reinterpret_cast<unsigned*>(static_cast<char*>(a.workspace) + rmsnorm_backward_workspace(ctx, a.B, a.T, a.d)) - 1 : nullptr;
     int rc = ADLOCO_OK;
 #define ADLOCO_TYPES(XT, ST)                                                               \
     if (vec && gain) rc = rmsnorm_backward_sized<XT, ST, true, true>(ctx, p, key, st);     \
@@ -1198,10 +1250,12 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
         const int blocks = (int)((a.d + kGainCols - 1) / kGainCols);
         float* part = static_cast<float*>(a.workspace);
         float* squares = a.per_sample_sqnorm ? part + a.B * p.chunks * a.d : nullptr;
+        const bool by_last = squares && a.B <= kGainLastBlock;
         ADLOCO_CUDA_TRY(ctx, launch_early(rmsnorm_gain_kernel, dim3((unsigned)blocks), kGainThreads, 0, st, 1, (const float*)part, a.B,
-                                          p.chunks, (int)a.d, squares, a.grad_sum, (int)a.accumulate_sum));
+                                          p.chunks, (int)a.d, squares, a.grad_sum, (int)a.accumulate_sum,
+                                          by_last ? p.ticket : (unsigned*)nullptr, a.per_sample_sqnorm, (int)a.accumulate_norms));
         ctx->launches++;
-        if (squares) {
+        if (squares && !by_last) {
             ADLOCO_CUDA_TRY(ctx, launch_early(rmsnorm_norms_kernel, dim3((unsigned)((a.B + 31) / 32)), 256, 0, st, 1, (const float*)squares,
                                               a.B, blocks, a.per_sample_sqnorm, (int)a.accumulate_norms));
             ctx->launches++;
@@ -1216,6 +1270,7 @@ int launch_dropout(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const 
     a.x = x; a.r = r; a.y = y;
     a.rows = rows; a.cols = cols; a.x_stride = x_stride; a.r_stride = r_stride; a.y_stride = y_stride;
     a.groups = (rows * cols + 7) / 8;
+    a.whole = rows * cols / 8;
     const bool flat = rows == 1 || (x_stride == cols && y_stride == cols && (!r || r_stride == cols));
     bool vec = aligned16(x) && aligned16(y) && aligned16(r);
     if (!flat) vec = vec && (cols & 7) == 0 && cols < 0x7fffffff && vec_rows(x, x_stride, bf16) && vec_rows(y, y_stride, bf16) && vec_rows(r, r_stride, bf16);
@@ -1224,13 +1279,16 @@ int launch_dropout(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const 
     const int64_t want = (a.groups + 511) / 512, most = (int64_t)ctx->sm_count * 64;
     const unsigned grid = (unsigned)(want < most ? want : most);
     cudaError_t e = cudaSuccess;
-#define ADLOCO_TYPES(T)                                                                          \
-    if (flat && vec) e = launch_early(dropout_kernel<T, true, true>, dim3(grid), 256, 0, st, 1, a, key);                \
-    else if (flat) e = launch_early(dropout_kernel<T, false, true>, dim3(grid), 256, 0, st, 1, a, key);                 \
-    else if (vec) e = launch_early(dropout_kernel<T, true, false>, dim3(grid), 256, 0, st, 1, a, key);                  \
-    else e = launch_early(dropout_kernel<T, false, false>, dim3(grid), 256, 0, st, 1, a, key)
+#define ADLOCO_LAUNCH(T, V, F, R) e = launch_early(dropout_kernel<T, V, F, R>, dim3(grid), 256, 0, st, 1, a, key)
+#define ADLOCO_TYPES(T)                                                       \
+    if (!vec) ADLOCO_LAUNCH(T, false, false, false);                          \
+    else if (flat && r) ADLOCO_LAUNCH(T, true, true, true);                   \
+    else if (flat) ADLOCO_LAUNCH(T, true, true, false);                       \
+    else if (r) ADLOCO_LAUNCH(T, true, false, true);                          \
+    else ADLOCO_LAUNCH(T, true, false, false)
     if (bf16) { ADLOCO_TYPES(__nv_bfloat16); }
     else { ADLOCO_TYPES(float); }
+#undef ADLOCO_LAUNCH
 #undef ADLOCO_TYPES
     ADLOCO_CUDA_TRY(ctx, e);
     ctx->launches++;

@@ -37,7 +37,7 @@ struct adloco_ctx {
     int device = 0;
     int sm_count = 0;
     int64_t launches = 0;
-    char cuda_err[256] = {0};
+    char cuda_err[384] = {0};
 
     // workspace of the streaming reductions
     float* n_partials = nullptr;   // [grid][B] per-block partial row sums of squares
