@@ -7,7 +7,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
 from dataclasses import dataclass
 
 import torch
@@ -73,13 +72,6 @@ class LinearLayer(C.Structure):
                 ("grad_sum", C.c_void_p)]
 
 
-# Argument structs of the operators between the linear layers, packed in C layout (struct's native alignment): a
-# ctypes Structure costs more to fill than the call it is for.
-RMSNORM_ARGS = struct.Struct("@iiifqqPqPqPPqPqPPqPqdQQ")                    # adloco_rmsnorm_args
-RMSNORM_BACKWARD_ARGS = struct.Struct("@iiiiiiqqqPqPqPPPqPqPqdQQPPPq")      # adloco_rmsnorm_backward_args
-ROPE_TENSOR = struct.Struct("@PPqqqqqqq")                                   # adloco_rope_tensor
-BLOCKSCALE_MATMUL_ARGS = struct.Struct("@qqqPqPqPqPqqPPqii")                # adloco_blockscale_matmul_args
-
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
 LINEAR_METHODS = {"auto": 0, "gram": 1, "direct": 2, "pair": 3, "gram_one_cta": 4, "gram_pair": 5}
 
@@ -133,15 +125,15 @@ def load_library() -> C.CDLL:
         "adloco_refresh_instance": (C.c_int, [vp, vp, vp, C.c_int, i64, vp]),
         "adloco_check_merge": (C.c_int, [C.POINTER(i64), i32, i32, C.POINTER(i32)]),
         "adloco_merge": (C.c_int, [vp, C.POINTER(vp), C.POINTER(i64), C.c_int, i32, i64, vp, C.POINTER(i32), vp]),
-        "adloco_add_rmsnorm": (C.c_int, [vp, C.c_char_p, vp]),
-        "adloco_add_rmsnorm_backward": (C.c_int, [vp, C.c_char_p, vp]),
+        "adloco_add_rmsnorm": (C.c_int, [vp, vp, vp]),
+        "adloco_add_rmsnorm_backward": (C.c_int, [vp, vp, vp]),
         "adloco_add_rmsnorm_backward_workspace": (i64, [vp, i64, i64, i64]),
         "adloco_dropout": (C.c_int, [vp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, C.c_double, C.c_uint64, C.c_uint64, vp]),
         "adloco_rope_frequencies": (C.c_int, [i32, C.c_double, i32, C.c_double, C.c_double, C.c_double, C.c_double, vp]),
-        "adloco_rope": (C.c_int, [vp, C.c_int, C.c_char_p, i32, i64, i64, i64, i64, vp, f32, vp, i64, i64, C.c_int, C.c_int, vp]),
+        "adloco_rope": (C.c_int, [vp, C.c_int, vp, i32, i64, i64, i64, i64, vp, f32, vp, i64, i64, C.c_int, C.c_int, vp]),
         "adloco_blockscale_quantize": (C.c_int, [vp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
         "adloco_blockscale_quantize_weight": (C.c_int, [vp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
-        "adloco_blockscale_matmul": (C.c_int, [vp, C.c_char_p, vp]),
+        "adloco_blockscale_matmul": (C.c_int, [vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -168,59 +160,6 @@ def _dtype_code(dt):
     raise AdlocoError(ERR_UNSUPPORTED, f"unsupported dtype {dt}")
 
 
-def _rows(t, what):
-    """(rows, d, pitch) of a tensor [..., d] whose leading dimensions are one run of evenly spaced rows."""
-    shape = t.shape
-    if not shape:
-        raise AdlocoError(ERR_INVALID_ARG, f"{what}: a tensor of rows is needed")
-    d = shape[-1]
-    if t.is_contiguous():
-        return (t.numel() // d if d else 0), d, d
-    stride = t.stride()
-    if stride[-1] != 1 and d > 1:
-        raise AdlocoError(ERR_INVALID_ARG, f"{what}: the last dimension must be contiguous")
-    rows, pitch, i = 1, d, len(shape) - 2
-    while i >= 0:                       # a dimension of extent one puts no demand on its stride
-        if shape[i] != 1:
-            if rows == 1:
-                pitch = stride[i]
-            elif stride[i] != rows * pitch:
-                raise AdlocoError(ERR_INVALID_ARG, f"{what}: rows must be evenly spaced")
-            rows *= shape[i]
-        i -= 1
-    return rows, d, pitch
-
-
-def _rows_like(t, what, rows, d, dtype, dev):
-    """Pointer and pitch of an optional tensor that must have the given rows, width, type and device index."""
-    if t is None:
-        return 0, 0
-    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.size(-1) == d and t.numel() == rows * d:
-        return t.data_ptr(), d
-    r, w, pitch = _rows(t, what)
-    if r != rows or w != d or t.dtype is not dtype or t.get_device() != dev:
-        raise AdlocoError(ERR_INVALID_ARG, f"{what}: expected {rows} rows of {d} {dtype} on device {dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    return t.data_ptr(), pitch
-
-
-def _vector(t, what, n, dtype, dev):
-    if t is None:
-        return 0
-    if t.numel() != n or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
-        raise AdlocoError(ERR_INVALID_ARG, f"{what}: expected {n} contiguous {dtype} on device {dev}, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    return t.data_ptr()
-
-
-def _dropout_key(dropout):
-    """(p, seed, offset) of an optional mask."""
-    if dropout is None:
-        return 0.0, 0, 0
-    p, seed, offset = dropout
-    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
-        raise AdlocoError(ERR_INVALID_ARG, "seed and offset are unsigned 64-bit numbers")
-    return p, seed, offset
-
-
 def make_params(eta, ddof=1, b_cur=1, b_max=1, b_cap=0, switch_n=2) -> TestParams:
     return TestParams(float(eta), int(ddof), int(switch_n), int(b_cur), int(b_max), int(b_cap))
 
@@ -230,6 +169,8 @@ class Context:
 
     def __init__(self, device: int = 0):
         self.lib = load_library()
+        from . import _tensor_calls as calls        # marshalling of the operators between the linear layers
+        self.calls = calls
         h = C.c_void_p()
         rc = self.lib.adloco_create(C.byref(h), int(device))
         if rc != OK:
@@ -404,187 +345,74 @@ class Context:
         self.check(rc, "adloco_embedding_sqnorm")
 
     # ------------------------------------------------------------------ between the linear layers
-    def _on(self, t, what):
-        """The context's device index, which the tensor must be on."""
-        dev = self.device.index
-        if t.get_device() != dev:
-            raise AdlocoError(ERR_INVALID_ARG, f"{what} is on {t.device}, the context on {self.device}")
-        return dev
-
-    def _on_stream(self, stream):
-        """The given stream, or the current one of the context's device."""
-        return torch._C._cuda_getCurrentRawStream(self.device.index) if stream is None else stream.cuda_stream
+    def _passed(self, rc, what: str):
+        """The status of a call of tensor_calls.cpp: 0, an adloco_status, or (status, why it was not made)."""
+        if rc != OK:
+            if isinstance(rc, tuple):
+                raise AdlocoError(rc[0], f"{what}: {rc[1]}")
+            self.check(rc, what)
 
     def add_rmsnorm(self, x, gain, *, residual=None, h=None, y=None, rstd=None, q=None, q_scale=None, eps=1e-5,
                     dropout=None, stream=None):
         """adloco_add_rmsnorm: h = residual + drop(x), y = gain * h / rms(h), rows along the last dimension.
         Outputs are written into h, y, rstd and (8 bits) q, q_scale, those that are given; dropout is
         (p, seed, offset) or None.  q is float8_e4m3fn or uint8, q_scale uint8 [rows, ceil(d / 128)]."""
-        dev = self._on(x, "x")
-        rows, d, xs = _rows(x, "x")
-        xt = x.dtype
-        st = residual.dtype if residual is not None else xt if h is None else h.dtype
-        rp, rs = _rows_like(residual, "residual", rows, d, st, dev)
-        hp, hs = _rows_like(h, "h", rows, d, st, dev)
-        yp, ys = _rows_like(y, "y", rows, d, xt, dev)
-        qp, qs, sp, ss = self._bytes(q, q_scale, rows, d, "q", dev) if q is not None or q_scale is not None else (0, 0, 0, 0)
-        p, seed, offset = (0.0, 0, 0) if dropout is None else _dropout_key(dropout)
-        code = _dtype_code(xt)
-        a = RMSNORM_ARGS.pack(code, code if st is xt else _dtype_code(st), _dtype_code(gain.dtype), eps, rows, d, x.data_ptr(), xs,
-                              rp, rs, _vector(gain, "gain", d, gain.dtype, dev), hp, hs, yp, ys,
-                              _vector(rstd, "rstd", rows, torch.float32, dev), qp, qs, sp, ss, p, seed, offset)
-        rc = self.lib.adloco_add_rmsnorm(self.h, a, self._on_stream(stream))
+        rc = self.calls.add_rmsnorm(self.h.value, self.device.index, x, gain, residual, h, y, rstd, q, q_scale, eps, dropout, stream)
         if rc != OK:
-            self.check(rc, "adloco_add_rmsnorm")
+            self._passed(rc, "adloco_add_rmsnorm")
 
     def add_rmsnorm_backward(self, dy, h, rstd, gain, dh, *, dh_residual=None, dx=None, dropout=None, per_sample_sqnorm=None,
                              accumulate_norms=False, grad_sum=None, accumulate_sum=False, workspace=None, stream=None):
         """adloco_add_rmsnorm_backward on dy [B, T, d] (or [rows, d]: one sample): dh, and dx where given, are the
         gradients of the residual and of x; per_sample_sqnorm and grad_sum are the gain's.  workspace: a uint8
         tensor of rmsnorm_backward_workspace(B, T, d) bytes; without one it comes from torch's allocator."""
-        dev = self._on(dy, "dy")
-        rows, d, dys = _rows(dy, "dy")
-        B = dy.shape[0] if dy.dim() == 3 else 1
-        T = rows // B if B else 0
-        dt, ht = dy.dtype, h.dtype
-        hp, hs = _rows_like(h, "h", rows, d, ht, dev)
-        rp, rs = _rows_like(dh_residual, "dh_residual", rows, d, ht, dev)
-        op, os_ = _rows_like(dh, "dh", rows, d, ht, dev)
-        xp, xs = _rows_like(dx, "dx", rows, d, dt, dev)
-        p, seed, offset = (0.0, 0, 0) if dropout is None else _dropout_key(dropout)
-        wp = wn = 0
-        if per_sample_sqnorm is not None or grad_sum is not None:
-            if workspace is None:
-                n = self.rmsnorm_backward_workspace(B, T, d)
-                if stream is None:
-                    workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
-                else:
-                    with torch.cuda.stream(stream):
-                        workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
-            wn = workspace.numel()
-            wp = _vector(workspace, "workspace", wn, torch.uint8, dev)
-        code = _dtype_code(dt)
-        a = RMSNORM_BACKWARD_ARGS.pack(code, code if ht is dt else _dtype_code(ht), _dtype_code(gain.dtype), accumulate_norms,
-                                       accumulate_sum, 0, B, T, d, dy.data_ptr(), dys, hp, hs,
-                                       _vector(rstd, "rstd", rows, torch.float32, dev), _vector(gain, "gain", d, gain.dtype, dev),
-                                       rp, rs, op, os_, xp, xs, p, seed, offset,
-                                       _vector(per_sample_sqnorm, "per_sample_sqnorm", B, torch.float32, dev),
-                                       _vector(grad_sum, "grad_sum", d, torch.float32, dev), wp, wn)
-        rc = self.lib.adloco_add_rmsnorm_backward(self.h, a, self._on_stream(stream))
+        if workspace is None and stream is not None and not (per_sample_sqnorm is None and grad_sum is None):
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(self.rmsnorm_backward_workspace(*(dy.shape if dy.dim() == 3 else (1, *dy.shape))),
+                                        dtype=torch.uint8, device=self.device)
+        rc = self.calls.add_rmsnorm_backward(self.h.value, self.device.index, dy, h, rstd, gain, dh, dh_residual, dx, dropout,
+                                             per_sample_sqnorm, accumulate_norms, grad_sum, accumulate_sum, workspace, stream)
         if rc != OK:
-            self.check(rc, "adloco_add_rmsnorm_backward")
+            self._passed(rc, "adloco_add_rmsnorm_backward")
 
     def rmsnorm_backward_workspace(self, B, T, d) -> int:
         return self.lib.adloco_add_rmsnorm_backward_workspace(self.h, B, T, d)
 
     def dropout(self, x, out, *, p, seed, offset=0, residual=None, stream=None):
         """adloco_dropout: out = residual + drop(x); the backward pass is the same call on the gradient."""
-        dev = self._on(x, "x")
-        rows, d, xs = _rows(x, "x")
-        rp, rs = _rows_like(residual, "residual", rows, d, x.dtype, dev)
-        op, os_ = _rows_like(out, "out", rows, d, x.dtype, dev)
-        p, seed, offset = _dropout_key((p, seed, offset))
-        rc = self.lib.adloco_dropout(self.h, _dtype_code(x.dtype), rows, d, x.data_ptr(), xs, rp, rs, op, os_, p, seed,
-                                     offset, self._on_stream(stream))
+        rc = self.calls.dropout(self.h.value, self.device.index, x, out, residual, p, seed, offset, stream)
         if rc != OK:
-            self.check(rc, "adloco_dropout")
+            self._passed(rc, "adloco_dropout")
 
     def rope(self, tensors, table, *, outs=None, positions=None, first_position=0, interleaved=False, inverse=False,
              stream=None):
         """adloco_rope on tensors [B, T, heads, head_dim] of one B, T, head_dim and type (any strides but the last);
         outs default to in place.  positions: int32 [B, T], or first_position + t."""
-        outs = tensors if outs is None else outs
-        dev = self._on(tensors[0], "tensors[0]")
-        if tensors[0].dim() != 4 or len(outs) != len(tensors):
-            raise AdlocoError(ERR_INVALID_ARG, "tensors are [B, T, heads, head_dim], with as many outs")
-        B, T, _, D = tensors[0].shape
-        dtype = tensors[0].dtype
-        packed = b""
-        for t, o in zip(tensors, outs):
-            shape = t.shape
-            if (len(shape) != 4 or shape[0] != B or shape[1] != T or shape[3] != D or o.shape != shape or t.dtype is not dtype
-                    or o.dtype is not dtype or t.get_device() != dev or o.get_device() != dev):
-                raise AdlocoError(ERR_INVALID_ARG, "tensors and outs must share B, T, head_dim, type and device")
-            ib, it, ih, i1 = t.stride()
-            ob, ot, oh, o1 = o.stride()
-            if D > 1 and (i1 != 1 or o1 != 1):
-                raise AdlocoError(ERR_INVALID_ARG, "head_dim must be contiguous")
-            packed += ROPE_TENSOR.pack(t.data_ptr(), o.data_ptr(), shape[2], ib, it, ih, ob, ot, oh)
-        pp, ps = 0, 0
-        if positions is not None:
-            if (positions.dtype is not torch.int32 or positions.shape != (B, T) or positions.get_device() != dev
-                    or (T > 1 and positions.stride(1) != 1)):
-                raise AdlocoError(ERR_INVALID_ARG, "positions must be int32 [B, T] with contiguous rows")
-            pp, ps = positions.data_ptr(), positions.stride(0) if B > 1 else T
-        if table.turns.get_device() != dev:
-            raise AdlocoError(ERR_INVALID_ARG, f"the table is on {table.turns.device}")
-        rc = self.lib.adloco_rope(self.h, _dtype_code(dtype), packed, len(tensors), B, T, D, table.rot_dim, table.turns.data_ptr(),
-                                  table.magnitude, pp, ps, first_position, interleaved, inverse, self._on_stream(stream))
+        rc = self.calls.rope(self.h.value, self.device.index, tensors, tensors if outs is None else outs, table.turns, table.rot_dim,
+                             table.magnitude, positions, first_position, interleaved, inverse, stream)
         if rc != OK:
-            self.check(rc, "adloco_rope")
-
-    @staticmethod
-    def _bytes(q, scale, rows, cols, what, dev):
-        """Pointers and pitches of an 8-bit matrix and its row scales."""
-        if q is None or scale is None:
-            raise AdlocoError(ERR_INVALID_ARG, f"{what} and its scales go together")
-        qp, qs = _rows_like(q, what, rows, cols, torch.uint8 if q.dtype is torch.uint8 else torch.float8_e4m3fn, dev)
-        sp, ss = _rows_like(scale, what + "_scale", rows, (cols + 127) // 128, torch.uint8, dev)
-        if rows == 1:                    # a single row has no pitch: any that fits the rules will do
-            qs, ss = (cols + 15) // 16 * 16, (ss + 3) // 4 * 4
-        return qp, qs, sp, ss
+            self._passed(rc, "adloco_rope")
 
     def blockscale_quantize(self, x, q, scale, *, stream=None):
         """adloco_blockscale_quantize: rows of x to e4m3 (q: float8_e4m3fn or uint8, pitch a multiple of 16) with one
         power-of-two scale for each 128 elements (uint8 exponents, pitch a multiple of 4)."""
-        dev = self._on(x, "x")
-        rows, d, xs = _rows(x, "x")
-        qp, qs, sp, ss = self._bytes(q, scale, rows, d, "q", dev)
-        rc = self.lib.adloco_blockscale_quantize(self.h, _dtype_code(x.dtype), rows, d, x.data_ptr(), xs, qp, qs, sp, ss,
-                                                 self._on_stream(stream))
+        rc = self.calls.blockscale_quantize(self.h.value, self.device.index, x, q, scale, stream)
         if rc != OK:
-            self.check(rc, "adloco_blockscale_quantize")
+            self._passed(rc, "adloco_blockscale_quantize")
 
     def blockscale_quantize_weight(self, W, q, scale, *, q_t=None, stream=None):
         """adloco_blockscale_quantize_weight: W [rows, cols] to e4m3 with one scale for each 128 x 128 block (scale uint8
         [ceil(rows / 128), ceil(cols / 128)]), and its transposed copy into q_t [cols, rows]."""
-        dev = self._on(W, "W")
-        rows, cols, ws = _rows(W, "W")
-        f8 = torch.uint8 if q.dtype is torch.uint8 else torch.float8_e4m3fn
-        qp, qs = _rows_like(q, "q", rows, cols, f8, dev)
-        tp, ts = _rows_like(q_t, "q_t", cols, rows, f8, dev)
-        sp, ss = _rows_like(scale, "scale", (rows + 127) // 128, (cols + 127) // 128, torch.uint8, dev)
-        qs = qs if rows > 1 else (cols + 15) // 16 * 16
-        ts = ts if cols > 1 else (rows + 15) // 16 * 16
-        rc = self.lib.adloco_blockscale_quantize_weight(self.h, _dtype_code(W.dtype), rows, cols, W.data_ptr(), ws, qp, qs, tp, ts,
-                                                        sp, ss, self._on_stream(stream))
+        rc = self.calls.blockscale_quantize_weight(self.h.value, self.device.index, W, q, scale, q_t, stream)
         if rc != OK:
-            self.check(rc, "adloco_blockscale_quantize_weight")
+            self._passed(rc, "adloco_blockscale_quantize_weight")
 
     def blockscale_matmul(self, a, a_scale, b, b_scale, out, *, scale_transposed=False, bias=None, stream=None):
         """adloco_blockscale_matmul: out [M, N] = a [M, K] b [N, K]^T (+ bias) in 8 bits.  b_scale holds b's 128 x 128
         block scales, or, with scale_transposed, those of the weight whose transposed copy b is."""
-        dev = self._on(a, "a")
-        M, K, _ = _rows(a, "a")
-        N = b.shape[0]
-        ap, as_, sp, ss = self._bytes(a, a_scale, M, K, "a", dev)
-        bp, bs = _rows_like(b, "b", N, K, torch.uint8 if b.dtype is torch.uint8 else torch.float8_e4m3fn, dev)
-        if N == 1:
-            bs = (K + 15) // 16 * 16
-        nb, kb = (N + 127) // 128, (K + 127) // 128
-        if scale_transposed:
-            bsp, sk = _rows_like(b_scale, "b_scale", kb, nb, torch.uint8, dev)
-            sn = 1
-        else:
-            bsp, sn = _rows_like(b_scale, "b_scale", nb, kb, torch.uint8, dev)
-            sk = 1
-        ot = out.dtype
-        op, os_ = _rows_like(out, "out", M, N, ot, dev)
-        args = BLOCKSCALE_MATMUL_ARGS.pack(M, N, K, ap, as_, sp, ss, bp, bs, bsp, sn, sk, _vector(bias, "bias", N, torch.float32, dev),
-                                           op, os_, _dtype_code(ot), 0)
-        rc = self.lib.adloco_blockscale_matmul(self.h, args, self._on_stream(stream))
+        rc = self.calls.blockscale_matmul(self.h.value, self.device.index, a, a_scale, b, b_scale, out, scale_transposed, bias, stream)
         if rc != OK:
-            self.check(rc, "adloco_blockscale_matmul")
+            self._passed(rc, "adloco_blockscale_matmul")
 
     # ------------------------------------------------------------------ outer step
     def outer_step(self, instances, theta_in, mom_in, *, lr, momentum, nesterov=True, theta_out=None,

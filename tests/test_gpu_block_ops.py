@@ -506,10 +506,10 @@ def test_null_pointers_and_empty_sizes_are_argument_errors(ctx):
     lib, h = ctx.lib, ctx.h
     before = ctx.launch_count
     buf = C.c_void_p(torch.zeros(1024, device=DEV).data_ptr())
-    a, b, m = (bytes(s.size) for s in (A.RMSNORM_ARGS, A.RMSNORM_BACKWARD_ARGS, A.BLOCKSCALE_MATMUL_ARGS))
-    assert lib.adloco_add_rmsnorm(h, None, None) == A.ERR_INVALID_ARG and lib.adloco_add_rmsnorm(h, a, None) == A.ERR_INVALID_ARG
-    assert lib.adloco_add_rmsnorm_backward(h, b, None) == A.ERR_INVALID_ARG
-    assert lib.adloco_blockscale_matmul(h, m, None) == A.ERR_INVALID_ARG
+    zeros = C.create_string_buffer(256)          # an argument struct of nothing
+    assert lib.adloco_add_rmsnorm(h, None, None) == A.ERR_INVALID_ARG and lib.adloco_add_rmsnorm(h, zeros, None) == A.ERR_INVALID_ARG
+    assert lib.adloco_add_rmsnorm_backward(h, zeros, None) == A.ERR_INVALID_ARG
+    assert lib.adloco_blockscale_matmul(h, zeros, None) == A.ERR_INVALID_ARG
     assert lib.adloco_dropout(None, 0, 1, 1, buf, 1, None, 0, buf, 1, 0.5, 0, 0, None) == A.ERR_INVALID_ARG
     assert lib.adloco_dropout(h, 0, 0, 1, buf, 1, None, 0, buf, 1, 0.5, 0, 0, None) == A.ERR_INVALID_ARG
     assert lib.adloco_rope(h, 0, None, 1, 1, 1, 8, 8, buf, 1.0, None, 0, 0, 0, 0, None) == A.ERR_INVALID_ARG
