@@ -604,6 +604,105 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     if (threadIdx.x == 0 && abort_flag) atomicExch(a.status, (int)ADLOCO_ERR_TIMEOUT);
 }
 
+// ---- few rows of A -----------------------------------------------------------------------------------
+// Up to 16 tokens (8 tokens of 4096 x 4096: 5.4 us against 10.7 us in 128 x 128 tiles; with 17 to 32 the tiles win, 10.7 us
+// against 14): the time is B's bytes from memory.  A block takes 16 rows of B, its warps the blocks of 128 of K in
+// turn; a lane loads 16 bytes of two rows of B and of a row of each eight of A straight into the fragments of the warp's
+// own matrix instruction (m16n8k32, B's rows as its M): the order of K within 64 is the same for both and does not
+// matter.  A block of 128's sum is scaled in fp32 and added up; the warps' sums meet in shared memory in a fixed order.
+constexpr int FR_ROWS = 16, FR_MAX_WARPS = 16, FR_MAX_M = 16;
+__device__ __forceinline__ uint4 bytes16(const uint8_t* row, int k, int K) {      // zeros beyond K
+    if (k + 16 <= K) return __ldg(reinterpret_cast<const uint4*>(row + k));
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (k + i < K) w[i >> 2] |= (uint32_t)row[k + i] << (8 * (i & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) {                          // 2^(byte - 127); 255: NaN
+    return byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? 0x1p-127f : __uint_as_float(byte << 23);
+}
+__device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+struct FewArgs {
+    MatArgs a;
+    const uint8_t *A, *B;
+    int64_t a_stride, b_stride;
+};
+template <int TILES>                                                                // of eight rows of A
+__global__ void __launch_bounds__(32 * FR_MAX_WARPS) blockscale_few_kernel(const __grid_constant__ FewArgs p) {
+    extern __shared__ float sums[];                                                 // [warps][TILES * 8][FR_ROWS + 1]
+    after_predecessor();
+    const MatArgs& a = p.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, g = lane >> 2, t = lane & 3;
+    const int n0 = (int)blockIdx.x * FR_ROWS;
+    const bool r0 = n0 + g < a.N, r1 = n0 + g + 8 < a.N;
+    const uint8_t* b0 = p.B + (int64_t)(n0 + g) * p.b_stride;
+    const uint8_t* b1 = b0 + 8 * p.b_stride;
+    const uint8_t* sb = a.sb + (n0 >> 7) * a.sb_n;
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    float acc[TILES][4];
+#pragma unroll
+    for (int j = 0; j < TILES; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+#pragma unroll 2
+    for (int kb = warp; kb < a.kb; kb += warps) {
+        uint4 w0[2], w1[2], x[TILES][2];
+        uint32_t sa[TILES][2];
+        const uint32_t sbyte = __ldg(sb + kb * a.sb_k);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = kb * 128 + h * 64 + t * 16;
+            w0[h] = r0 && k < a.K ? bytes16(b0, k, a.K) : none;
+            w1[h] = r1 && k < a.K ? bytes16(b1, k, a.K) : none;
+#pragma unroll
+            for (int j = 0; j < TILES; ++j) {
+                const int m = j * 8 + g;
+                x[j][h] = m < a.M && k < a.K ? bytes16(p.A + (int64_t)m * p.a_stride, k, a.K) : none;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < TILES; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int m = j * 8 + 2 * t + i;
+                sa[j][i] = m < a.M ? (uint32_t)__ldg(a.sa + (int64_t)m * a.sa_stride + kb) : 127u;
+            }
+        const float fb = scale_of(sbyte);
+#pragma unroll
+        for (int j = 0; j < TILES; ++j) {
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                mma_e4m3(d, w0[h].x, w1[h].x, w0[h].y, w1[h].y, x[j][h].x, x[j][h].y);
+                mma_e4m3(d, w0[h].z, w1[h].z, w0[h].w, w1[h].w, x[j][h].z, x[j][h].w);
+            }
+            // the two scales one after the other: their product may leave the range of fp32 where the result does not
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[j][i] = fmaf(d[i] * scale_of(sa[j][i & 1]), fb, acc[j][i]);
+        }
+    }
+    float* mine = sums + warp * (TILES * 8) * (FR_ROWS + 1);
+#pragma unroll
+    for (int j = 0; j < TILES; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine[(j * 8 + 2 * t + (i & 1)) * (FR_ROWS + 1) + g + 8 * (i >> 1)] = acc[j][i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < TILES * 8 * FR_ROWS; i += blockDim.x) {
+        const int m = i / FR_ROWS, r = i % FR_ROWS, n = n0 + r;
+        if (m >= a.M || n >= a.N) continue;
+        float v = 0.f;
+        for (int w = 0; w < warps; ++w) v += sums[(w * TILES * 8 + m) * (FR_ROWS + 1) + r];
+        if (a.bias) v += a.bias[n];
+        const int64_t at = (int64_t)m * a.out_stride + n;
+        if (a.out_bf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+        else static_cast<float*>(a.out)[at] = v;
+    }
+}
+
 // matrix [rows, cols] of `es`-byte elements with a pitch in elements, as a 2-D map with a box of box_rows rows of
 // box_cols elements (128 bytes), 128-byte swizzle; elements outside the matrix read as zero and are not written
 int make_map(adloco_ctx* ctx, CUtensorMap* m, CUtensorMapDataType type, int64_t es, const void* base, int64_t rows, int64_t cols,
@@ -636,6 +735,22 @@ int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
     const int64_t piece = a.out_bf16 ? 8 : 4;
     a.out_vec = aligned16(p.out) && p.out_stride % piece == 0 && p.N % piece == 0;
     a.status = ctx->gemm_status; a.wait_ns = ctx->wait_limit_ns;
+    a.tiles_m = a.tiles_n = a.tiles = 0;
+    if (p.M <= FR_MAX_M) {
+        FewArgs f;
+        f.a = a;
+        f.A = static_cast<const uint8_t*>(p.a); f.a_stride = p.a_stride;
+        f.B = static_cast<const uint8_t*>(p.b); f.b_stride = p.b_stride;
+        const int warps = a.kb < FR_MAX_WARPS ? a.kb : FR_MAX_WARPS;
+        const dim3 grid((unsigned)((p.N + FR_ROWS - 1) / FR_ROWS));
+        const int tiles = p.M <= 8 ? 1 : 2;
+        const size_t smem = (size_t)warps * tiles * 8 * (FR_ROWS + 1) * sizeof(float);
+        const cudaError_t e = tiles == 1 ? launch_early(blockscale_few_kernel<1>, grid, 32 * warps, smem, st, 1, f)
+                                         : launch_early(blockscale_few_kernel<2>, grid, 32 * warps, smem, st, 1, f);
+        ADLOCO_CUDA_TRY(ctx, e);
+        ctx->launches++;
+        return ADLOCO_OK;
+    }
     const int64_t pair_tiles = ((p.M + 255) / 256) * ((p.N + MP_N - 1) / MP_N);
     const bool pair = pair_tiles >= ctx->sm_count / 2 && cta_pairs_possible(ctx);
     const int64_t tm = (p.M + (pair ? 255 : MT - 1)) / (pair ? 256 : MT), tn = (p.N + (pair ? MP_N : MT) - 1) / (pair ? MP_N : MT);
