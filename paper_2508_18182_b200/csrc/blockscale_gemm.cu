@@ -24,7 +24,7 @@ struct Ring {
 
 struct MatArgs {
     int M, N, K, kb;                 // kb: blocks of 128 along K
-    int tiles_m, tiles_n, tiles;     // tiles along M, along N, and all
+    int tiles_n, tiles;              // tiles along N, and all
     const uint8_t* sa;
     int64_t sa_stride;
     const uint8_t* sb;
@@ -59,21 +59,25 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, mbar_wait<CLUSTER>(bar, parity, abortp, limit_ns)) != 0;
 }
 
-// The tiles of one worker.  Dealt round, the tiles along N fastest: the workers sit on the same few rows of A at a time.
-// In runs, the tiles along M fastest: a worker stays on one panel of B.
+// The tiles of one worker: dealt round, the tiles along N fastest, so that all workers sit on the same few rows of A at a
+// time -- a tile of A is then read from HBM once and from L2 by the rest.  (Runs of tiles along M instead let a tile's uses
+// drift apart, past what L2 keeps beside the output's stream: 37888 x 768 x 2304 took 76 us, 55 without the stores.)
 struct TileWalk {
-    int at, end, step, per_line;
-    bool runs;
-    __device__ __forceinline__ TileWalk(const MatArgs& a, int worker, int workers, bool in_runs) : runs(in_runs) {
-        at = runs ? (int)((int64_t)a.tiles * worker / workers) : worker;
-        end = runs ? (int)((int64_t)a.tiles * (worker + 1) / workers) : a.tiles;
-        step = runs ? 1 : workers;
-        per_line = runs ? a.tiles_m : a.tiles_n;
+    int left, m, n, step_m, step_n, line;                  // no division on the way
+    __device__ __forceinline__ TileWalk(const MatArgs& a, int worker, int workers) : line(a.tiles_n) {
+        left = worker < a.tiles ? (a.tiles - worker - 1) / workers + 1 : 0;
+        m = worker / line;
+        n = worker % line;
+        step_m = workers / line;
+        step_n = workers % line;
     }
-    __device__ __forceinline__ bool more() const { return at < end; }
-    __device__ __forceinline__ void next() { at += step; }
-    __device__ __forceinline__ int m() const { return runs ? at % per_line : at / per_line; }
-    __device__ __forceinline__ int n() const { return runs ? at / per_line : at % per_line; }
+    __device__ __forceinline__ bool more() const { return left > 0; }
+    __device__ __forceinline__ void next() {
+        --left;
+        m += step_m;
+        n += step_n;
+        if (n >= line) { n -= line; ++m; }
+    }
 };
 
 // The four scale warps' loop: the scale words (four blocks' bytes) of 512 of K at a time, for 128 rows of A and TILE_N
@@ -98,7 +102,7 @@ __device__ __forceinline__ void fetch_scales(const MatArgs& a, uint32_t ring, Ti
     Ring fill, done;
     auto fetch = [&](int i) -> bool {                     // turn's loads into slot fill.stage
         if (!wait_warp<false>(sf_empty + 8u * fill.stage, fill.phase ^ 1u, abortp, a.wait_ns)) return false;
-        if (g == 0) { m0 = walk.m() * TILE_M + row_offset; n0 = walk.n() * TILE_N; }
+        if (g == 0) { m0 = walk.m * TILE_M + row_offset; n0 = walk.n * TILE_N; }
         const int m = m0 + quarter * 32 + lane, nb = (n0 >> 7) + ((lane >> 2) & 1), k = g * 4 + (lane & 3);
         const uint32_t to = ring + fill.stage * SLOT + (uint32_t)(lane * 16 + quarter * 4);
         if (m < a.M)
@@ -163,7 +167,7 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     __shared__ int abort_flag;
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // warp: known to be uniform
-    TileWalk walk(a, (int)blockIdx.x, (int)gridDim.x, false);
+    TileWalk walk(a, (int)blockIdx.x, (int)gridDim.x);
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (uint32_t s = 0; s < MT_STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -192,7 +196,7 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             uint32_t issued = 0;
             bool ok = true;
             for (; ok && walk.more(); walk.next()) {
-                const int m0 = walk.m() * MT, n0 = walk.n() * MT;
+                const int m0 = walk.m * MT, n0 = walk.n * MT;
                 for (int k = 0; k < a.kb; ++k) {
                     if (!mbar_wait(empty_bar(ps.stage), ps.phase ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
                     const uint32_t sA = smem_base + ps.stage * MT_STAGE_BYTES;
@@ -264,7 +268,7 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         const uint32_t q = warp & 3;
         uint32_t n = 0;
         for (; walk.more(); walk.next(), ++n) {
-            const int m0 = walk.m() * MT, n0 = walk.n() * MT;
+            const int m0 = walk.m * MT, n0 = walk.n * MT;
             const uint32_t buf = n & 1u;
             if (!__all_sync(0xffffffffu, mbar_wait(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns))) break;
             tc_fence_after();
@@ -335,9 +339,9 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
 // accumulators and the scale slots, so the tensor pipe never waits for the epilogue: with one accumulator of 256
 // columns a tile's hand-over (last MMA, signal, read-out, signal, first MMA) cost about 1.3 us beside the 1.8 us of
 // a tile's MMAs at K = 768.
-// What bounds the rest is the feed from L2, about 9.4 TB/s over all SMs.  RESIDENT: where a panel of B (96 rows a CTA,
-// up to 768 of K) fits shared memory it is loaded once for a run of tiles along M and only A is streamed, 16 KB a
-// stage instead of 28.
+// What bounds the rest is shared memory: a stage's MMAs read 28 KB of it and the copies write as much, 448 of its clocks
+// against 384 of the tensor pipe (measured at long K: 447).  RESIDENT: where a panel of B (96 rows a CTA, up to 768 of K)
+// fits, a worker keeps one panel, loaded once, and only A is streamed, 16 KB a stage instead of 28.
 constexpr int MP_N = 192;
 constexpr int MP_STAGES = 6;
 constexpr int MP_A_BYTES = MT * 128, MP_B_BYTES = (MP_N / 2) * 128;
@@ -365,14 +369,13 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     auto acc_full = [&](uint32_t s) { return bars + 8u * (2 * MP_STAGES + 2 * kScaleSlots + s); };
     auto acc_empty = [&](uint32_t s) { return bars + 8u * (2 * MP_STAGES + 2 * kScaleSlots + 2 + s); };
     auto panel_full = [&](uint32_t k) { return bars + 8u * (2 * MP_STAGES + 2 * kScaleSlots + 4 + k); };
-    const uint32_t panel_empty = bars + 8u * (2 * MP_STAGES + 2 * kScaleSlots + 4 + MP_RESIDENT_KB);
-    const uint32_t drain_bar = panel_empty + 8u;
+    const uint32_t drain_bar = bars + 8u * (2 * MP_STAGES + 2 * kScaleSlots + 4 + MP_RESIDENT_KB);
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // warp: known to be uniform
     const uint32_t rank = cluster_cta_rank();                  // 0: the CTA that issues the MMAs
-    TileWalk walk(a, (int)(blockIdx.x >> 1), (int)(gridDim.x >> 1), RESIDENT);
+    TileWalk walk(a, (int)(blockIdx.x >> 1), (int)(gridDim.x >> 1));
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (uint32_t s = 0; s < MP_STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -380,7 +383,6 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         for (uint32_t s = 0; s < kScaleSlots; ++s) { mbar_init(sf_full(s), rank == 0 ? 5 : 4); mbar_init(sf_empty(s), 1); }
         for (uint32_t s = 0; s < 2; ++s) { mbar_init(acc_full(s), 1); mbar_init(acc_empty(s), 2 * MP_EPI_WARPS); }
         for (uint32_t k = 0; k < MP_RESIDENT_KB; ++k) mbar_init(panel_full(k), 1);
-        mbar_init(panel_empty, 1);
         mbar_init(drain_bar, 1);
         fence_barrier_init();
         prefetch_tmap(&tmA);
@@ -401,16 +403,9 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         if (lane == 0) {
             Ring ps;
             bool ok = true;
-            int panels = 0, panel_n = -1;                      // panels loaded so far, and which is there
+            bool fresh = RESIDENT;                             // the panel comes along with the first tile
             for (; ok && walk.more(); walk.next()) {
-                const int m0 = walk.m() * 256 + (int)rank * MT, n0 = walk.n() * MP_N + (int)rank * (MP_N / 2);
-                const bool fresh = RESIDENT && walk.n() != panel_n;
-                if (fresh) {
-                    // the MMAs that read the last panel are done
-                    if (panels > 0 && !mbar_wait(panel_empty, (uint32_t)(panels - 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
-                    panel_n = walk.n();
-                    ++panels;
-                }
+                const int m0 = walk.m * 256 + (int)rank * MT, n0 = walk.n * MP_N + (int)rank * (MP_N / 2);
                 for (int k = 0; k < a.kb; ++k) {
                     if (!mbar_wait(empty_bar(ps.stage), ps.phase ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
                     const uint32_t bar = map_to_cta(full_bar(ps.stage), 0);
@@ -424,6 +419,7 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
                     }
                     ps.advance(MP_STAGES);
                 }
+                fresh = false;
             }
             if (!ok) {
                 // leaving after a time-out: the byte counts of copies in flight complete on the even CTA's barriers, which the
@@ -441,15 +437,12 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             Ring ps, sf;
             uint32_t n = 0;
             bool ok = true;
-            int panels = 0, panel_n = -1;
-            for (; ok && walk.more(); ++n) {
+            for (; ok && walk.more(); walk.next(), ++n) {
                 const uint32_t buf = n & 1u;
-                const bool fresh = RESIDENT && walk.n() != panel_n;
-                if (fresh) { panel_n = walk.n(); ++panels; }
                 if (!wait_warp<true>(acc_empty(buf), ((n >> 1) & 1u) ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
                 for (int k = 0; k < a.kb; ++k) {
                     if ((k & 3) == 0 && !wait_warp<true>(sf_full(sf.stage), sf.phase, abortp, a.wait_ns)) { ok = false; break; }
-                    if (fresh && !wait_warp<false>(panel_full(k), (uint32_t)(panels - 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
+                    if (RESIDENT && n == 0 && !wait_warp<false>(panel_full(k), 0, abortp, a.wait_ns)) { ok = false; break; }
                     if (!wait_warp<false>(full_bar(ps.stage), ps.phase, abortp, a.wait_ns)) { ok = false; break; }
                     tc_fence_after();
                     if (leader) {
@@ -473,11 +466,7 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
                     ps.advance(MP_STAGES);
                     if ((k & 3) == 3 || k == a.kb - 1) sf.advance(kScaleSlots);
                 }
-                walk.next();
-                if (ok && leader) {
-                    mma_commit_pair(acc_full(buf), 3);
-                    if (RESIDENT && walk.more() && walk.n() != panel_n) mma_commit_pair(panel_empty, 3);
-                }
+                if (ok && leader) mma_commit_pair(acc_full(buf), 3);
                 __syncwarp();
             }
             if (!ok && leader) {
@@ -515,8 +504,8 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         for (; walk.more(); walk.next(), ++n) {
             const uint32_t buf = n & 1u;
             const uint32_t taddr = tmem + ((q * 32u) << 16) + buf * MP_N + slice * 64u;
-            const int row0 = walk.m() * 256 + (int)rank * MT + (int)q * 32;
-            const int col0 = walk.n() * MP_N + (int)slice * 64;
+            const int row0 = walk.m * 256 + (int)rank * MT + (int)q * 32;
+            const int col0 = walk.n * MP_N + (int)slice * 64;
             const bool some = row0 < a.M && col0 < a.N;                      // uniform across the warp
             if (!__all_sync(0xffffffffu, mbar_wait(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns))) break;
             tc_fence_after();
@@ -735,7 +724,7 @@ int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
     const int64_t piece = a.out_bf16 ? 8 : 4;
     a.out_vec = aligned16(p.out) && p.out_stride % piece == 0 && p.N % piece == 0;
     a.status = ctx->gemm_status; a.wait_ns = ctx->wait_limit_ns;
-    a.tiles_m = a.tiles_n = a.tiles = 0;
+    a.tiles_n = a.tiles = 0;
     if (p.M <= FR_MAX_M) {
         FewArgs f;
         f.a = a;
@@ -755,7 +744,7 @@ int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
     const bool pair = pair_tiles >= ctx->sm_count / 2 && cta_pairs_possible(ctx);
     const int64_t tm = (p.M + (pair ? 255 : MT - 1)) / (pair ? 256 : MT), tn = (p.N + (pair ? MP_N : MT) - 1) / (pair ? MP_N : MT);
     if (tm * tn > 0x7fffffff) return ADLOCO_ERR_UNSUPPORTED;
-    a.tiles_m = (int)tm; a.tiles_n = (int)tn; a.tiles = (int)(tm * tn);
+    a.tiles_n = (int)tn; a.tiles = (int)(tm * tn);
     CUtensorMap tmA, tmB, tmO;
     int rc = make_map(ctx, &tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.a, p.M, p.K, p.a_stride, 128, MT);
     if (rc == ADLOCO_OK) rc = make_map(ctx, &tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.b, p.N, p.K, p.b_stride, 128, pair ? MP_N / 2 : MT);
@@ -774,8 +763,15 @@ int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
                             : make_map(ctx, &tmO, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, p.out, p.M, p.N, p.out_stride, 32, 32);
             if (rc != ADLOCO_OK) return rc;
         }
-        const int workers = a.tiles < ctx->sm_count / 2 ? a.tiles : ctx->sm_count / 2;
-        if (a.kb <= MP_RESIDENT_KB) ADLOCO_CUDA_TRY(ctx, launch_early(blockscale_pair_kernel<true>, dim3(2 * workers), MP_THREADS, MP_SMEM, st, 2, tmA, tmB, tmO, a));
+        const int most = ctx->sm_count / 2;
+        // a worker keeps its panel when the workers in use are a multiple of the panels; that may leave some idle and take more
+        // rounds, against stages of 475 clocks of shared memory instead of 571 (K = 768, with the epilogue): 54.8 us against 56.1 at
+        // 32768 x 2304 x 768 with 22 rounds against 21, 24.8 against 23.3 at 32768 x 768 x 768 with 8 against 7
+        const int groups = most / a.tiles_n, kept = groups * a.tiles_n;
+        const int64_t rounds = (a.tiles + most - 1) / most, rounds_kept = groups ? (tm + groups - 1) / groups : 0;
+        const bool resident = a.kb <= MP_RESIDENT_KB && groups > 0 && rounds_kept * 10 <= rounds * 11;
+        const int workers = resident ? kept : a.tiles < most ? a.tiles : most;
+        if (resident) ADLOCO_CUDA_TRY(ctx, launch_early(blockscale_pair_kernel<true>, dim3(2 * workers), MP_THREADS, MP_SMEM, st, 2, tmA, tmB, tmO, a));
         else ADLOCO_CUDA_TRY(ctx, launch_early(blockscale_pair_kernel<false>, dim3(2 * workers), MP_THREADS, MP_SMEM, st, 2, tmA, tmB, tmO, a));
     } else {
         ADLOCO_CUDA_TRY(ctx, launch_early(blockscale_tile_kernel, dim3(a.tiles < ctx->sm_count ? a.tiles : ctx->sm_count), MT_THREADS, MT_SMEM,
