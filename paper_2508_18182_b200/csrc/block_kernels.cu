@@ -1017,14 +1017,38 @@ __global__ void __launch_bounds__(256) quantise_rows_kernel(const T* x, int64_t 
         kb[k] = there ? b - row[k] * blocks_per_row.d : 0u;
         const int64_t col = (int64_t)kb[k] * 128 + lane_col;
         n[k] = there ? (int)min((int64_t)16, cols - col) : 0;
+        if (!VEC) continue;
         const T* at = x + row[k] * x_stride + col;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             v[k][j] = zero_raw<T>();
             if (n[k] <= 8 * j) continue;
-            if (VEC && n[k] >= 8 * j + 8) v[k][j] = load_raw<true>(at + 8 * j, 8);
+            if (n[k] >= 8 * j + 8) v[k][j] = load_raw<true>(at + 8 * j, 8);
             else v[k][j] = load_raw<false>(at + 8 * j, n[k] - 8 * j);
         }
+    }
+    if constexpr (!VEC) {
+        // rows off the 16-byte grid: the warp loads its blocks one after the other, 32 adjacent elements an instruction, and hands
+        // them out through shared memory
+        __shared__ alignas(16) T stage[8][U][4][128];
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t b = blockIdx.x * (32 * U) + 32 * k + warp * 4 + g;
+                const bool there = b < blocks;
+                const uint32_t br = there ? blocks_per_row(b) : 0u;
+                const int64_t c0 = there ? (int64_t)(b - br * blocks_per_row.d) * 128 : cols;
+                const T* from = x + br * x_stride + c0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) stage[warp][k][g][32 * i + lane] = c0 + 32 * i + lane < cols ? from[32 * i + lane] : T(0.f);
+            }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) v[k][j] = from_buffer(&stage[warp][k][(lane >> 3)][lane_col + 8 * j]);
     }
 #pragma unroll
     for (int k = 0; k < U; ++k) {

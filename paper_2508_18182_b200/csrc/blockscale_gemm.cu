@@ -41,16 +41,70 @@ __device__ __forceinline__ uint32_t pack_bf16(uint32_t a, uint32_t b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(a), __uint_as_float(b));
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-// 16 accumulator columns of row m to the output one by one, for outputs whose rows are not 16-byte aligned
-__device__ __forceinline__ void store_elements(const MatArgs& a, int m, int col, const uint32_t (&r)[16]) {
+// An epilogue warp's box of shared memory: 32 rows of 128 bytes (64 bf16 or 32 fp32 columns), piece j of row i at piece
+// j ^ (i mod 8), so that a thread's row written and a row's pieces read by neighbouring lanes fall on all banks.
+constexpr int kBoxBytes = 32 * 128;
+__device__ __forceinline__ uint32_t box_piece(uint32_t box, int row, int piece) { return box + row * 128u + ((uint32_t)(piece ^ (row & 7)) << 4); }
+
+// 16 accumulator columns, col .. col + 15 of the output, of this lane's row into the box from column `at` of it on
+__device__ __forceinline__ void fill_box(const MatArgs& a, uint32_t box, int lane, int at, int col, uint32_t (&r)[16]) {
+    if (a.bias) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        if (col + e >= a.N) continue;
-        const float v = __uint_as_float(r[e]) + (a.bias ? __ldg(a.bias + col + e) : 0.f);
-        const int64_t at = (int64_t)m * a.out_stride + col + e;
-        if (a.out_bf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
-        else static_cast<float*>(a.out)[at] = v;
+        for (int e = 0; e < 16; ++e)
+            if (col + e < a.N) r[e] = __float_as_uint(__uint_as_float(r[e]) + __ldg(a.bias + col + e));
     }
+    if (a.out_bf16) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint32_t p[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = pack_bf16(r[8 * j + 2 * e], r[8 * j + 2 * e + 1]);
+            st_shared_v4(box_piece(box, lane, at / 8 + j), p[0], p[1], p[2], p[3]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st_shared_v4(box_piece(box, lane, at / 4 + j), r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+    }
+}
+// The box to the output at (row0, col): whole pieces where rows are 16-byte aligned, else element by element, both along rows.
+__device__ __forceinline__ void flush_box(const MatArgs& a, uint32_t box, int lane, int row0, int col) {
+    __syncwarp();
+    const int es = a.out_bf16 ? 2 : 4;
+    char* out = static_cast<char*>(a.out) + ((int64_t)row0 * a.out_stride + col) * es;
+    const int64_t pitch = a.out_stride * es;
+    if (a.out_vec) {
+        const int piece = lane & 7;
+        if (col + piece * (16 / es) < a.N) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int row = i * 4 + (lane >> 3);
+                uint4 v;
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(box_piece(box, row, piece)) : "memory");
+                if (row0 + row < a.M) __stcs(reinterpret_cast<uint4*>(out + row * pitch + piece * 16), v);
+            }
+        }
+    } else {
+        const int rows = min(32, a.M - row0);
+#pragma unroll 4
+        for (int row = 0; row < rows; ++row) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int c = h * 32 + lane;                                    // bf16: two sweeps of 32 columns; fp32: one
+                if (h * 32 * es >= 128 || col + c >= a.N) continue;
+                const uint32_t from = box_piece(box, row, c * es / 16) + (uint32_t)(c * es & 15);
+                if (es == 2) {
+                    unsigned short v;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(from) : "memory");
+                    reinterpret_cast<unsigned short*>(out + row * pitch)[c] = v;
+                } else {
+                    uint32_t v;
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(from) : "memory");
+                    reinterpret_cast<uint32_t*>(out + row * pitch)[c] = v;
+                }
+            }
+        }
+    }
+    __syncwarp();
 }
 
 // A wait of the whole warp, which goes on (or gives up) together.
@@ -148,14 +202,14 @@ constexpr int MT = 128;
 constexpr int MT_STAGES = 6;
 constexpr int MT_STAGE_BYTES = 2 * MT * 128;
 constexpr int MT_SF_COL = 2 * MT;                             // tensor memory: two accumulators, then the slots
-constexpr int MT_SMEM = MT_STAGES * MT_STAGE_BYTES + 1024 + 256 + kScaleSlots * scale_slot_bytes<MT>();
+constexpr int MT_SMEM = MT_STAGES * MT_STAGE_BYTES + 4 * kBoxBytes + 1024 + 256 + kScaleSlots * scale_slot_bytes<MT>();
 constexpr int MT_THREADS = 320;
 
 __global__ void __launch_bounds__(MT_THREADS, 1)
 blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const MatArgs a) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t bars = smem_base + MT_STAGES * MT_STAGE_BYTES, sf_ring = bars + 256;
+    const uint32_t boxes = smem_base + MT_STAGES * MT_STAGE_BYTES, bars = boxes + 4 * kBoxBytes, sf_ring = bars + 256;
     auto full_bar = [&](uint32_t s) { return bars + 8u * s; };
     auto empty_bar = [&](uint32_t s) { return bars + 8u * (MT_STAGES + s); };
     auto sf_full = [&](uint32_t s) { return bars + 8u * (2 * MT_STAGES + s); };
@@ -272,50 +326,16 @@ blockscale_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             const uint32_t buf = n & 1u;
             if (!__all_sync(0xffffffffu, mbar_wait(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns))) break;
             tc_fence_after();
-            const int m = m0 + (int)q * 32 + lane;
+            const uint32_t box = boxes + q * kBoxBytes;
+            const int row0 = m0 + (int)q * 32, wide = a.out_bf16 ? 64 : 32;      // columns of a box
 #pragma unroll 1
-            for (int c = 0; c < MT; c += 32) {
-                uint32_t r[32];
-                tmem_ld32(tmem + ((q * 32u) << 16) + buf * MT + c, r);
+            for (int c = 0; c < MT; c += 16) {
+                uint32_t r[16];
+                tmem_ld16(tmem + ((q * 32u) << 16) + buf * MT + c, r);
                 tmem_ld_wait();
-                if (m >= a.M) continue;
-                const int col = n0 + c;
-                if (a.bias) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (col + e < a.N) r[e] = __float_as_uint(__uint_as_float(r[e]) + __ldg(a.bias + col + e));
-                }
-                if (a.out_bf16) {
-                    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.out) + (int64_t)m * a.out_stride + col;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        if (a.out_vec && col + e + 8 <= a.N) {
-                            uint32_t p[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(r[e + 2 * j]), __uint_as_float(r[e + 2 * j + 1]));
-                                p[j] = *reinterpret_cast<const uint32_t*>(&h);
-                            }
-                            *reinterpret_cast<uint4*>(o + e) = make_uint4(p[0], p[1], p[2], p[3]);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (col + e + j < a.N) o[e + j] = __float2bfloat16_rn(__uint_as_float(r[e + j]));
-                        }
-                    }
-                } else {
-                    float* o = static_cast<float*>(a.out) + (int64_t)m * a.out_stride + col;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        if (a.out_vec && col + e + 4 <= a.N) {
-                            *reinterpret_cast<uint4*>(o + e) = make_uint4(r[e], r[e + 1], r[e + 2], r[e + 3]);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                if (col + e + j < a.N) o[e + j] = __uint_as_float(r[e + j]);
-                        }
-                    }
-                }
+                if (row0 >= a.M || n0 + (c & -wide) >= a.N) continue;            // uniform across the warp
+                fill_box(a, box, lane, c & (wide - 1), n0 + c, r);
+                if (((c + 16) & (wide - 1)) == 0) flush_box(a, box, lane, row0, n0 + (c & -wide));
             }
             tc_fence_before();
             __syncwarp();
@@ -347,9 +367,8 @@ constexpr int MP_STAGES = 6;
 constexpr int MP_A_BYTES = MT * 128, MP_B_BYTES = (MP_N / 2) * 128;
 constexpr int MP_RESIDENT_KB = 6;                             // largest K of a resident panel, in blocks of 128
 constexpr int MP_EPI_WARPS = 4 * MP_N / 64;                   // each 32 rows x 64 columns of a CTA's 128 x 192
-constexpr int MP_BOX_BYTES = 32 * 128;                        // 32 rows of 128 bytes: one epilogue warp's store
 constexpr int MP_SF_COL = 2 * MP_N;
-constexpr int MP_SMEM = MP_STAGES * (MP_A_BYTES + MP_B_BYTES) + MP_EPI_WARPS * MP_BOX_BYTES + 1024 + 512 + kScaleSlots * scale_slot_bytes<MP_N>();
+constexpr int MP_SMEM = MP_STAGES * (MP_A_BYTES + MP_B_BYTES) + MP_EPI_WARPS * kBoxBytes + 1024 + 512 + kScaleSlots * scale_slot_bytes<MP_N>();
 constexpr int MP_THREADS = 32 * (6 + MP_EPI_WARPS);           // warp 0 TMA, warp 1 MMA, warps 2-5 scales, the rest epilogue
 static_assert(MP_RESIDENT_KB <= MP_STAGES, "a resident panel takes the B parts of the ring");
 
@@ -361,7 +380,7 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t panel = smem_base + MP_STAGES * MP_A_BYTES;         // the B part of stage s, or block k of a resident panel
     const uint32_t boxes = panel + MP_STAGES * MP_B_BYTES;
-    const uint32_t bars = boxes + MP_EPI_WARPS * MP_BOX_BYTES, sf_ring = bars + 512;
+    const uint32_t bars = boxes + MP_EPI_WARPS * kBoxBytes, sf_ring = bars + 512;
     auto full_bar = [&](uint32_t s) { return bars + 8u * s; };
     auto empty_bar = [&](uint32_t s) { return bars + 8u * (MP_STAGES + s); };
     auto sf_full = [&](uint32_t s) { return bars + 8u * (2 * MP_STAGES + s); };
@@ -498,8 +517,7 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         // ---------------- epilogue ----------------
         const uint32_t q = warp & 3, slice = (uint32_t)(warp - 6) >> 2;
         const uint32_t acc_empty_0 = map_to_cta(acc_empty(0), 0);
-        const uint32_t box = boxes + (uint32_t)(warp - 6) * MP_BOX_BYTES;
-        const uint32_t row_addr = box + lane * 128u;
+        const uint32_t box = boxes + (uint32_t)(warp - 6) * kBoxBytes;
         uint32_t n = 0;
         for (; walk.more(); walk.next(), ++n) {
             const uint32_t buf = n & 1u;
@@ -512,71 +530,35 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             if (some && a.out_vec) {
                 if (lane == 0) bulk_wait_read_all();                         // the last store has read the box
                 __syncwarp();
+            }
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t r[16];
-                    tmem_ld16(taddr + c * 16, r);
-                    tmem_ld_wait();
-                    if (a.bias) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int col = col0 + c * 16 + e;
-                            if (col < a.N) r[e] = __float_as_uint(__uint_as_float(r[e]) + __ldg(a.bias + col));
-                        }
-                    }
-                    // 128-byte swizzle of the store's box: piece j of row i at piece j ^ (i mod 8)
-                    if (a.out_bf16) {
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            uint32_t p[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) p[e] = pack_bf16(r[8 * j + 2 * e], r[8 * j + 2 * e + 1]);
-                            st_shared_v4(row_addr + ((((uint32_t)(2 * c + j)) ^ (lane & 7u)) << 4), p[0], p[1], p[2], p[3]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            st_shared_v4(row_addr + ((((uint32_t)(4 * (c & 1) + j)) ^ (lane & 7u)) << 4), r[4 * j], r[4 * j + 1], r[4 * j + 2],
-                                         r[4 * j + 3]);
-                        if (c == 1) {                                        // fp32: a box holds 32 columns, the slice is two
-                            fence_proxy_async_smem();
-                            __syncwarp();
-                            if (lane == 0) {
-                                tma_store_2d(&tmO, box, col0, row0);
-                                bulk_commit_group();
-                                bulk_wait_read_all();
-                            }
-                            __syncwarp();
-                        }
-                    }
+            for (int c = 0; c < 64; c += 16) {
+                uint32_t r[16];
+                tmem_ld16(taddr + c, r);
+                tmem_ld_wait();
+                if (c == 48) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty_0 + 8u * buf);
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty_0 + 8u * buf);
+                if (!some) continue;
+                fill_box(a, box, lane, a.out_bf16 ? c : c & 31, col0 + c, r);
+                const bool full = a.out_bf16 ? c == 48 : (c & 16) != 0;      // 64 columns of bf16, 32 of fp32
+                const int col = a.out_bf16 ? col0 : col0 + (c & 32);
+                if (!full || col >= a.N) continue;
+                if (!a.out_vec) {
+                    flush_box(a, box, lane, row0, col);
+                    continue;
+                }
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    const int col = a.out_bf16 ? col0 : col0 + 32;
-                    if (col < a.N) {
-                        tma_store_2d(&tmO, box, col, row0);
-                        bulk_commit_group();
-                    }
+                    tma_store_2d(&tmO, box, col, row0);
+                    bulk_commit_group();
+                    if (c < 48) bulk_wait_read_all();
                 }
-                continue;
+                __syncwarp();
             }
-            if (some) {
-                const int m = row0 + lane;
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t r[16];
-                    tmem_ld16(taddr + c * 16, r);
-                    tmem_ld_wait();
-                    if (m < a.M) store_elements(a, m, col0 + c * 16, r);
-                }
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty_0 + 8u * buf);
         }
         if (lane == 0) bulk_wait_all();                                      // this warp's stores are complete
         __syncwarp();
@@ -720,7 +702,7 @@ int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
     a.sb = p.b_scale; a.sb_n = p.b_scale_stride_n; a.sb_k = p.b_scale_stride_k;
     a.bias = p.bias; a.out = p.out; a.out_stride = p.out_stride;
     a.out_bf16 = p.out_dtype == ADLOCO_BF16;
-    // whole 16-byte pieces of every row: a TMA store writes a row's last piece in full, beyond the matrix too
+    // whole 16-byte pieces of every row (a TMA store writes a row's last piece in full, beyond the matrix too)
     const int64_t piece = a.out_bf16 ? 8 : 4;
     a.out_vec = aligned16(p.out) && p.out_stride % piece == 0 && p.N % piece == 0;
     a.status = ctx->gemm_status; a.wait_ns = ctx->wait_limit_ns;
