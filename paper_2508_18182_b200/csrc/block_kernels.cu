@@ -436,7 +436,6 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
 struct RmsBackArgs {
     adloco_rmsnorm_backward_args a;
     int64_t chunks, rows_per_chunk;
-    unsigned* ticket;          // of rmsnorm_gain_kernel; set to zero here
 };
 __device__ __forceinline__ void copy16_async(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -490,7 +489,6 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = (int)a.d;
     const int64_t sample = (int64_t)blockIdx.x / p.chunks, chunk = (int64_t)blockIdx.x % p.chunks;
     const int64_t first = chunk * p.rows_per_chunk, last = min(a.T, first + p.rows_per_chunk);
-    if (GAIN && blockIdx.x == 0 && threadIdx.x == 0) *p.ticket = 0u;
     const float inv_d = 1.0f / (float)d;
     const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(columns)) + threadIdx.x * 16;
     const int wide = pad8(d);
@@ -645,100 +643,77 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
     }
 }
 
-// Adds up the workspace in a fixed order: a block takes 8 columns, a warp every 16th sample (two at a time), and a lane one
-// column in a quarter of the sample's chunks.  Leaves the sum over all samples, and each sample's sum of squares over the 8
-// columns, squares[block][sample].  The last block to finish adds those up to the norms; for many samples, where one block
-// would be long at it, rmsnorm_norms_kernel does (ticket null).
+// Adds up the workspace [B][chunks][d] in a fixed order, two kinds of blocks side by side.  Blocks [0, sums): eight columns
+// of the sum over all samples; a warp reads eight columns of four rows at a time.  The others: one sample's norm; a lane has
+// one column in a quarter of the sample's chunks, a warp every 16th eight columns.  Both read the workspace once each from
+// L2, with nothing to wait for in between: a chain from columns to squares to norms, by a counter, took 3 us more.
 constexpr int kGainThreads = 512, kGainCols = 8;
-constexpr int64_t kGainLastBlock = 128;          // samples up to which the last block forms the norms
-__device__ __forceinline__ void put_norm(float* norms, int64_t b, float n, int accumulate) {
-    if (accumulate) atomicAdd(norms + b, n);      // layers on other streams add here too
-    else norms[b] = n;
-}
-__global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float* part, int64_t B, int64_t chunks, int d, float* squares,
-                                                                    float* sum, int accumulate_sum, unsigned* ticket, float* norms,
-                                                                    int accumulate_norms) {
+__global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float* part, int64_t B, int64_t chunks, int d, int sums, float* sum,
+                                                                    int accumulate_sum, float* norms, int accumulate_norms) {
     constexpr int WARPS = kGainThreads / 32;
-    __shared__ float smem[WARPS][33];
-    __shared__ bool last;
+    __shared__ float smem[WARPS][kGainCols];
     after_predecessor();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = lane >> 3;
-    const int col = (int)blockIdx.x * kGainCols + (lane & 7);
-    float s = 0.f;
-    for (int64_t b0 = warp; b0 < B; b0 += 2 * WARPS) {
-        float g[2] = {0.f, 0.f};
-        if (col < d) {
-#pragma unroll 4
-            for (int64_t k = quarter; k < chunks; k += 4) {
-                g[0] += part[(b0 * chunks + k) * d + col];
-                if (b0 + WARPS < B) g[1] += part[((b0 + WARPS) * chunks + k) * d + col];
-            }
-        }
+    if ((int)blockIdx.x < sums) {
+        const int col = (int)blockIdx.x * kGainCols + (lane & 7);
+        const int64_t rows = B * chunks;
+        float s = 0.f;
+        // loads in groups that leave together, short last groups included (an unrolled loop's remainder goes one by one)
+        for (int64_t k0 = warp * 4 + quarter; k0 < rows; k0 += WARPS * 4 * 8) {
+            float v[8];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            g[j] += __shfl_xor_sync(0xffffffffu, g[j], 8);
-            g[j] += __shfl_xor_sync(0xffffffffu, g[j], 16);
-            s += g[j];
-            if (squares) {
-                float q = g[j] * g[j];
+            for (int u = 0; u < 8; ++u) v[u] = k0 + u * WARPS * 4 < rows && col < d ? part[(k0 + u * WARPS * 4) * d + col] : 0.f;
 #pragma unroll
-                for (int o = 4; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
-                if (lane == 0 && b0 + j * WARPS < B) squares[(int64_t)blockIdx.x * B + b0 + j * WARPS] = q;
-            }
+            for (int u = 0; u < 8; ++u) s += v[u];
         }
-    }
-    if (sum) {
+        s += __shfl_xor_sync(0xffffffffu, s, 8);
+        s += __shfl_xor_sync(0xffffffffu, s, 16);
         if (lane < kGainCols) smem[warp][lane] = s;
         __syncthreads();
         if (warp == 0 && lane < kGainCols && col < d) {
-            float t = 0.f;
+            s = 0.f;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) t += smem[w][lane];
-            sum[col] = accumulate_sum ? sum[col] + t : t;
+            for (int w = 0; w < WARPS; ++w) s += smem[w][lane];
+            sum[col] = accumulate_sum ? sum[col] + s : s;
+        }
+        return;
+    }
+    const int64_t b = (int64_t)blockIdx.x - sums;
+    const float* mine = part + b * chunks * d;
+    float q = 0.f;
+    for (int c0 = warp * kGainCols; c0 < d; c0 += 3 * WARPS * kGainCols) {          // three groups of columns at a time
+        float g[3] = {0.f, 0.f, 0.f};
+        for (int64_t k0 = quarter; k0 < chunks; k0 += 4 * 6) {
+            float v[6][3];
+#pragma unroll
+            for (int u = 0; u < 6; ++u)
+#pragma unroll
+                for (int j = 0; j < 3; ++j) {
+                    const int col = c0 + j * WARPS * kGainCols + (lane & 7);
+                    v[u][j] = k0 + 4 * u < chunks && col < d ? mine[(k0 + 4 * u) * d + col] : 0.f;
+                }
+#pragma unroll
+            for (int u = 0; u < 6; ++u)
+#pragma unroll
+                for (int j = 0; j < 3; ++j) g[j] += v[u][j];
+        }
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            g[j] += __shfl_xor_sync(0xffffffffu, g[j], 8);
+            g[j] += __shfl_xor_sync(0xffffffffu, g[j], 16);
+            q = fmaf(g[j], g[j], q);
         }
     }
-    if (!ticket) return;
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(ticket, 1u) == gridDim.x - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    for (int64_t b0 = 0; b0 < B; b0 += 32) {
-        float n = 0.f;
-        if (b0 + lane < B) {
-#pragma unroll 8
-            for (int k = warp; k < (int)gridDim.x; k += WARPS) n += __ldcg(squares + (int64_t)k * B + b0 + lane);
-        }
-        smem[warp][lane] = n;
-        __syncthreads();
-        if (warp == 0 && b0 + lane < B) {
-            n = 0.f;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) n += smem[w][lane];
-            put_norm(norms, b0 + lane, n, accumulate_norms);
-        }
-        __syncthreads();
-    }
-}
-// n_i from squares[blocks][B]: a block takes 32 samples, its warps share the rows
-__global__ void __launch_bounds__(256) rmsnorm_norms_kernel(const float* squares, int64_t B, int blocks, float* norms, int accumulate) {
-    __shared__ float smem[8][32];
-    after_predecessor();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t b = (int64_t)blockIdx.x * 32 + lane;
-    float n = 0.f;
-    if (b < B) {
-#pragma unroll 16
-        for (int k = warp; k < blocks; k += 8) n += squares[(int64_t)k * B + b];
-    }
-    smem[warp][lane] = n;
+    for (int o = 4; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);       // the four quarters hold the same
+    if (lane == 0) smem[warp][0] = q;
     __syncthreads();
-    if (warp == 0 && b < B) {
-        n = 0.f;
+    if (threadIdx.x == 0) {
+        q = 0.f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) n += smem[w][lane];
-        put_norm(norms, b, n, accumulate);
+        for (int w = 0; w < WARPS; ++w) q += smem[w][0];
+        if (accumulate_norms) atomicAdd(norms + b, q);      // layers on other streams add here too
+        else norms[b] = q;
     }
 }
 
@@ -1216,8 +1191,7 @@ static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64
     return want < 1 ? 1 : want > most ? most : want;
 }
 int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d) {
-    // partial gradients, partial squares, and a counter
-    return (B * rmsnorm_chunks(ctx, B, T, d) * d + B * ((d + kGainCols - 1) / kGainCols) + 1) * (int64_t)sizeof(float);
+    return B * rmsnorm_chunks(ctx, B, T, d) * d * (int64_t)sizeof(float);
 }
 
 template <typename XT, typename ST, int TPR, int C, bool VEC, bool GAIN>
@@ -1256,7 +1230,6 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     p.a = a;
     p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d);
     p.rows_per_chunk = (a.T + p.chunks - 1) / p.chunks;
-    p.ticket = gain ? reinterpret_cast<unsigned*>(static_cast<char*>(a.workspace) + rmsnorm_backward_workspace(ctx, a.B, a.T, a.d)) - 1 : nullptr;
     int rc = ADLOCO_OK;
 #define ADLOCO_TYPES(XT, ST)                                                               \
     if (vec && gain) rc = rmsnorm_backward_sized<XT, ST, true, true>(ctx, p, key, st);     \
@@ -1271,19 +1244,12 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
     ctx->launches++;
     if (gain) {
-        const int blocks = (int)((a.d + kGainCols - 1) / kGainCols);
-        float* part = static_cast<float*>(a.workspace);
-        float* squares = a.per_sample_sqnorm ? part + a.B * p.chunks * a.d : nullptr;
-        const bool by_last = squares && a.B <= kGainLastBlock;
-        ADLOCO_CUDA_TRY(ctx, launch_early(rmsnorm_gain_kernel, dim3((unsigned)blocks), kGainThreads, 0, st, 1, (const float*)part, a.B,
-                                          p.chunks, (int)a.d, squares, a.grad_sum, (int)a.accumulate_sum,
-                                          by_last ? p.ticket : (unsigned*)nullptr, a.per_sample_sqnorm, (int)a.accumulate_norms));
+        const int sums = a.grad_sum ? (int)((a.d + kGainCols - 1) / kGainCols) : 0;
+        const unsigned blocks = (unsigned)(sums + (a.per_sample_sqnorm ? a.B : 0));
+        ADLOCO_CUDA_TRY(ctx, launch_early(rmsnorm_gain_kernel, dim3(blocks), kGainThreads, 0, st, 1, static_cast<const float*>(a.workspace), a.B,
+                                          p.chunks, (int)a.d, sums, a.grad_sum, (int)a.accumulate_sum, a.per_sample_sqnorm,
+                                          (int)a.accumulate_norms));
         ctx->launches++;
-        if (squares && !by_last) {
-            ADLOCO_CUDA_TRY(ctx, launch_early(rmsnorm_norms_kernel, dim3((unsigned)((a.B + 31) / 32)), 256, 0, st, 1, (const float*)squares,
-                                              a.B, blocks, a.per_sample_sqnorm, (int)a.accumulate_norms));
-            ctx->launches++;
-        }
     }
     return ADLOCO_OK;
 }
