@@ -394,7 +394,7 @@ int adloco_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args* args, void* s
  *                  both pointers may be NULL (a frozen gain)
  *   workspace      dev, 16-byte aligned, at least adloco_add_rmsnorm_backward_workspace bytes; not
  *                  needed (NULL) when neither norms nor sum are asked for.  One call at a time may use it.
- * All sums are fp32 in a fixed order; only the addition of a sample's n_i to what other calls put
+ * B <= 2^27, B T <= 2^30.  All sums are fp32 in a fixed order; only the addition of a sample's n_i to what other calls put
  * there is an atomic. */
 typedef struct {
     adloco_dtype dtype, stream_dtype, gain_dtype;
@@ -480,7 +480,8 @@ int adloco_rope(adloco_ctx* ctx, adloco_dtype dtype, const adloco_rope_tensor* t
  * Rows (activations and gradients): one scale for 128 consecutive elements of a row.
  *   x      dev [rows, cols] in dtype, pitch x_stride
  *   q      dev [rows, cols] bytes, pitch q_stride a multiple of 16, 16-byte aligned
- *   scale  dev [rows, ceil(cols / 128)] bytes, pitch scale_stride a multiple of 4, 4-byte aligned */
+ *   scale  dev [rows, ceil(cols / 128)] bytes, pitch scale_stride a multiple of 4, 4-byte aligned (the product
+ *          reads whole aligned words; what a row's last word holds beyond its blocks does not matter) */
 int adloco_blockscale_quantize(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t cols, const void* x,
                                int64_t x_stride, void* q, int64_t q_stride, uint8_t* scale, int64_t scale_stride,
                                void* stream);

@@ -80,7 +80,7 @@ int adloco_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args* a, void* stre
 }
 
 int64_t adloco_add_rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d) {
-    if (!ctx || B < 1 || T < 1 || d < 1 || B > kMaxExtent || T > kMaxExtent || d > 16384) return 0;
+    if (!ctx || B < 1 || T < 1 || d < 1 || B > (kMaxExtent >> 3) || T > kMaxExtent || d > 16384) return 0;
     return rmsnorm_backward_workspace(ctx, B, T, d);
 }
 
@@ -89,7 +89,8 @@ int adloco_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     int rc = check_types(a->dtype, a->stream_dtype, a->gain_dtype);
     if (rc != ADLOCO_OK) return rc;
     if (a->B < 1 || a->T < 1 || a->d < 1) return ADLOCO_ERR_INVALID_ARG;
-    if (a->B > kMaxExtent || a->T > kMaxExtent || a->B * a->T > kMaxExtent || a->d > 16384) return ADLOCO_ERR_UNSUPPORTED;
+    // samples: a cluster of eight blocks each forms their norms
+    if (a->B > (kMaxExtent >> 3) || a->T > kMaxExtent || a->B * a->T > kMaxExtent || a->d > 16384) return ADLOCO_ERR_UNSUPPORTED;
     if (a->dy_stride < a->d || a->h_stride < a->d || a->dh_stride < a->d ||
         (a->dh_residual && a->dh_residual_stride < a->d) || (a->dx && a->dx_stride < a->d))
         return ADLOCO_ERR_INVALID_ARG;

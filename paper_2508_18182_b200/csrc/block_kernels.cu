@@ -6,6 +6,7 @@
 #include <atomic>
 
 #include "common.cuh"
+#include "ptx.cuh"
 
 namespace adloco {
 
@@ -239,12 +240,13 @@ __device__ __forceinline__ uint2 to_e4m3x8(const F2 (&v)[4], float inv) {
     }
     return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
 }
-// The 16 lanes that hold one block of a row (8 adjacent elements each) agree on its scale; the lane of the
+// The LANES lanes that hold one block of a row (8 adjacent elements each; fewer than 16 where the row ends) agree on its scale; the lane of the
 // block's first elements writes it.  Every lane of the warp takes part; n = 0 for lanes beyond the row.
+template <int LANES>
 __device__ __forceinline__ void quantise_block(const F2 (&v)[4], int n, uint8_t* q_row, uint8_t* scale_row, int col) {
     uint32_t m = n > 0 ? abs_max8(v) : 0u;          // elements beyond n are zero
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
     if (n <= 0) return;
     const uint32_t s = scale_byte(m);
     const uint2 w = to_e4m3x8(v, inv_scale(s));
@@ -263,9 +265,13 @@ __device__ __forceinline__ float warp_sum(float v) {
 // halves of smem, so one barrier a call is enough
 template <int TPR, int THREADS>
 __device__ __forceinline__ float row_sum(float v, float* smem, int turn) {
+    if (TPR <= 32) {
+#pragma unroll
+        for (int o = TPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
     v = warp_sum(v);
-    if (TPR == 32) return v;
-    constexpr int W = TPR / 32;
+    constexpr int W = TPR > 32 ? TPR / 32 : 1;
     float* half = smem + (turn & 1) * (THREADS / 32);
     if ((threadIdx.x & 31) == 0) half[threadIdx.x >> 5] = v;
     __syncthreads();
@@ -301,7 +307,7 @@ __device__ __forceinline__ void copy_out(T* row, const T* buf, int d, int t) {
 // the threads of a row (and, where a row is wider than a warp, of all rows of the block)
 template <int TPR>
 __device__ __forceinline__ void row_barrier() {
-    if (TPR == 32) __syncwarp();
+    if (TPR <= 32) __syncwarp();
     else __syncthreads();
 }
 template <typename T>
@@ -336,7 +342,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     const int64_t row_asked = (int64_t)blockIdx.x * ROWS + sub;
     const bool there = row_asked < a.rows;
-    if (TPR == 32 && !there) return;                       // whole warps leave; wider rows meet at a barrier
+    if (TPR <= 32 && __all_sync(0xffffffffu, !there)) return;            // whole warps leave; wider rows meet at a barrier
     const int64_t row = there ? row_asked : a.rows - 1;
     const int d = (int)a.d;
     const XT* x = static_cast<const XT*>(a.x) + row * a.x_stride;
@@ -416,7 +422,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
                 else to_buffer(x_buf + col, out);
             }
         }
-        if (a.q) quantise_block(g, n, q_row, s_row, col);
+        if (a.q) quantise_block<(TPR < 16 ? TPR : 16)>(g, n, q_row, s_row, col);
     }
     if (!VEC) {
         row_barrier<TPR>();
@@ -529,7 +535,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
     float rstd_next = rstds[min(first + sub, last - 1)];     // a row ahead of its use
     for (int64_t at = first; at < last; at += ROWS, ++turn) {
         const bool there = at + sub < last;
-        if (TPR == 32 && !there) break;
+        if (TPR <= 32 && __all_sync(0xffffffffu, !there)) break;
         const int64_t row = sample * a.T + (there ? at + sub : last - 1);
         const float rstd = rstd_next;
         rstd_next = rstds[min(at + ROWS + sub, last - 1)];
@@ -644,21 +650,26 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
 }
 
 // Adds up the workspace [B][chunks][d] in a fixed order, two kinds of blocks side by side.  Blocks [0, sums): eight columns
-// of the sum over all samples; a warp reads eight columns of four rows at a time.  The others: one sample's norm; a lane has
-// one column in a quarter of the sample's chunks, a warp every 16th eight columns.  Both read the workspace once each from
-// L2, with nothing to wait for in between: a chain from columns to squares to norms, by a counter, took 3 us more.
-constexpr int kGainThreads = 512, kGainCols = 8;
+// of the sum over all samples; a warp reads eight columns of four rows at a time.  The others, SPAN for each sample's norm:
+// a lane has one column in a quarter of the sample's chunks, a warp every 16 SPANth eight columns.  With few samples, whose
+// chunks are many, SPAN is a cluster of eight whose sums of squares meet in the first one's shared memory (one sample of
+// 8192 x 768: 47 us with one block, 30 with eight; 64 samples of 256 x 768: 29.7 against 34.2).  Both kinds read the workspace
+// once each from L2, with nothing to wait for in between: a chain from columns to squares to norms, by a counter, took 3 us
+// more.  Loads leave in groups, short last groups included (an unrolled loop's remainder would go one by one).
+constexpr int kGainThreads = 512, kGainCols = 8, kGainCluster = 8;
+constexpr int64_t kGainSpread = 131072;          // elements of a sample's chunks from which on its norm takes a cluster
+template <int SPAN>
 __global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float* part, int64_t B, int64_t chunks, int d, int sums, float* sum,
                                                                     int accumulate_sum, float* norms, int accumulate_norms) {
     constexpr int WARPS = kGainThreads / 32;
     __shared__ float smem[WARPS][kGainCols];
+    __shared__ float squares[kGainCluster];
     after_predecessor();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = lane >> 3;
-    if ((int)blockIdx.x < sums) {
+    if ((int)blockIdx.x < sums) {                       // whole clusters
         const int col = (int)blockIdx.x * kGainCols + (lane & 7);
         const int64_t rows = B * chunks;
         float s = 0.f;
-        // loads in groups that leave together, short last groups included (an unrolled loop's remainder goes one by one)
         for (int64_t k0 = warp * 4 + quarter; k0 < rows; k0 += WARPS * 4 * 8) {
             float v[8];
 #pragma unroll
@@ -678,27 +689,32 @@ __global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float*
         }
         return;
     }
-    const int64_t b = (int64_t)blockIdx.x - sums;
+    constexpr int COLS = SPAN > 1 ? 1 : 3, ROWS = SPAN > 1 ? 16 : 6;      // loads of a group: of so many eights of columns, and chunks
+    constexpr int STEP = SPAN * WARPS * kGainCols;
+    const int64_t b = ((int64_t)blockIdx.x - sums) / SPAN;
+    const int rank = SPAN > 1 ? (int)ptx::cluster_cta_rank() : 0;
     const float* mine = part + b * chunks * d;
     float q = 0.f;
-    for (int c0 = warp * kGainCols; c0 < d; c0 += 3 * WARPS * kGainCols) {          // three groups of columns at a time
-        float g[3] = {0.f, 0.f, 0.f};
-        for (int64_t k0 = quarter; k0 < chunks; k0 += 4 * 6) {
-            float v[6][3];
+    for (int c0 = (rank * WARPS + warp) * kGainCols; c0 < d; c0 += COLS * STEP) {
+        float g[COLS];
 #pragma unroll
-            for (int u = 0; u < 6; ++u)
+        for (int j = 0; j < COLS; ++j) g[j] = 0.f;
+        for (int64_t k0 = quarter; k0 < chunks; k0 += 4 * ROWS) {
+            float v[ROWS][COLS];
 #pragma unroll
-                for (int j = 0; j < 3; ++j) {
-                    const int col = c0 + j * WARPS * kGainCols + (lane & 7);
+            for (int u = 0; u < ROWS; ++u)
+#pragma unroll
+                for (int j = 0; j < COLS; ++j) {
+                    const int col = c0 + j * STEP + (lane & 7);
                     v[u][j] = k0 + 4 * u < chunks && col < d ? mine[(k0 + 4 * u) * d + col] : 0.f;
                 }
 #pragma unroll
-            for (int u = 0; u < 6; ++u)
+            for (int u = 0; u < ROWS; ++u)
 #pragma unroll
-                for (int j = 0; j < 3; ++j) g[j] += v[u][j];
+                for (int j = 0; j < COLS; ++j) g[j] += v[u][j];
         }
 #pragma unroll
-        for (int j = 0; j < 3; ++j) {
+        for (int j = 0; j < COLS; ++j) {
             g[j] += __shfl_xor_sync(0xffffffffu, g[j], 8);
             g[j] += __shfl_xor_sync(0xffffffffu, g[j], 16);
             q = fmaf(g[j], g[j], q);
@@ -712,6 +728,15 @@ __global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float*
         q = 0.f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) q += smem[w][0];
+        if (SPAN > 1) ptx::st_cluster_u32(ptx::map_to_cta(ptx::smem_u32(&squares[rank]), 0), __float_as_uint(q));
+    }
+    if (SPAN > 1) ptx::cluster_sync_all();
+    if (rank == 0 && threadIdx.x == 0) {
+        if (SPAN > 1) {
+            q = 0.f;
+#pragma unroll
+            for (int r = 0; r < kGainCluster; ++r) q += squares[r];
+        }
         if (accumulate_norms) atomicAdd(norms + b, q);      // layers on other streams add here too
         else norms[b] = q;
     }
@@ -1119,10 +1144,13 @@ bool vec_rows(const void* p, int64_t stride, bool bf16) {
 
 }  // namespace
 
-// Threads a row and groups of eight a thread: a warp up to 1024 elements, four warps up to 4096, sixteen beyond.
+// Threads a row and groups of eight a thread: a quarter of a warp up to 64 elements, a half up to 128, a warp up to 1024, four
+// warps up to 4096, sixteen beyond.
 #define ADLOCO_ROW_CASES(LAUNCH)                                                      \
     const int64_t groups = (d + 7) / 8;                                               \
-    if (groups <= 32) { LAUNCH(32, 1); }                                              \
+    if (groups <= 8) { LAUNCH(8, 1); }                                                \
+    else if (groups <= 16) { LAUNCH(16, 1); }                                         \
+    else if (groups <= 32) { LAUNCH(32, 1); }                                         \
     else if (groups <= 64) { LAUNCH(32, 2); }                                         \
     else if (groups <= 96) { LAUNCH(32, 3); }                                         \
     else if (groups <= 128) { LAUNCH(32, 4); }                                        \
@@ -1182,16 +1210,19 @@ int launch_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const Drop
     return ADLOCO_OK;
 }
 
-// Blocks a sample's rows are cut into: about as many over all samples as are resident at once (three an SM, two for wider rows), at least a row for every group of
-// threads in a block.
-static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d) {
-    const int64_t rows_at_once = d <= 1024 ? 8 : d <= 4096 ? 2 : 1;
+// Blocks a sample's rows are cut into: about as many over all samples as are resident at once, at least a row for every
+// group of threads in a block.  Blocks an SM by width (registers set them in bf16; of 2, 3, 4 and 6 these measured best at
+// 256, 768, 1024, 2048, 3000 and 4096); `fit` is what shared memory allows beside that.
+static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d, int64_t fit) {
+    const int64_t rows_at_once = d <= 64 ? 32 : d <= 128 ? 16 : d <= 1024 ? 8 : d <= 4096 ? 2 : 1;
     const int64_t most = (T + rows_at_once - 1) / rows_at_once;
-    const int64_t want = (d <= 768 ? 3 : 2) * (int64_t)ctx->sm_count / B;
+    int64_t blocks = d <= 256 ? 4 : d <= 768 ? 3 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 3072 ? 3 : 2;
+    if (blocks > fit) blocks = fit < 1 ? 1 : fit;
+    const int64_t want = blocks * (int64_t)ctx->sm_count / B;
     return want < 1 ? 1 : want > most ? most : want;
 }
 int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d) {
-    return B * rmsnorm_chunks(ctx, B, T, d) * d * (int64_t)sizeof(float);
+    return B * rmsnorm_chunks(ctx, B, T, d, 8) * d * (int64_t)sizeof(float);
 }
 
 template <typename XT, typename ST, int TPR, int C, bool VEC, bool GAIN>
@@ -1228,7 +1259,9 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     const bool gain = a.per_sample_sqnorm || a.grad_sum;
     RmsBackArgs p;
     p.a = a;
-    p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d);
+    const int64_t row_bytes = (xb ? 2 : 4) + 2 * (sb ? 2 : 4), threads = a.d > 4096 ? 512 : 256;
+    const int64_t groups = a.d <= 1024 ? (a.d + 255) / 256 : a.d <= 4096 ? (a.d + 1023) / 1024 : (a.d + 4095) / 4096;     // of eight a thread
+    p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d, 227 * 1024 / (2 * threads * groups * 8 * row_bytes + 1024));
     p.rows_per_chunk = (a.T + p.chunks - 1) / p.chunks;
     int rc = ADLOCO_OK;
 #define ADLOCO_TYPES(XT, ST)                                                               \
@@ -1244,11 +1277,13 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     ADLOCO_CUDA_TRY(ctx, cudaGetLastError());
     ctx->launches++;
     if (gain) {
-        const int sums = a.grad_sum ? (int)((a.d + kGainCols - 1) / kGainCols) : 0;
-        const unsigned blocks = (unsigned)(sums + (a.per_sample_sqnorm ? a.B : 0));
-        ADLOCO_CUDA_TRY(ctx, launch_early(rmsnorm_gain_kernel, dim3(blocks), kGainThreads, 0, st, 1, static_cast<const float*>(a.workspace), a.B,
-                                          p.chunks, (int)a.d, sums, a.grad_sum, (int)a.accumulate_sum, a.per_sample_sqnorm,
-                                          (int)a.accumulate_norms));
+        const bool spread = a.per_sample_sqnorm && p.chunks * a.d > kGainSpread;
+        const int64_t span = spread ? kGainCluster : 1, cols = kGainCols * span;     // the sum's blocks in whole clusters
+        const int sums = a.grad_sum ? (int)((a.d + cols - 1) / cols * span) : 0;
+        const dim3 blocks((unsigned)(sums + (a.per_sample_sqnorm ? a.B * span : 0)));
+        ADLOCO_CUDA_TRY(ctx, launch_early(spread ? rmsnorm_gain_kernel<kGainCluster> : rmsnorm_gain_kernel<1>, blocks, kGainThreads, 0, st,
+                                          (unsigned)span, static_cast<const float*>(a.workspace), a.B, p.chunks, (int)a.d, sums, a.grad_sum,
+                                          (int)a.accumulate_sum, a.per_sample_sqnorm, (int)a.accumulate_norms));
         ctx->launches++;
     }
     return ADLOCO_OK;

@@ -69,7 +69,8 @@ def test_add_rmsnorm(ctx, d, xt, st):
 
 
 @pytest.mark.parametrize("B,T,d", [(1, 1, 8), (3, 5, 8), (1, 1, 1024), (2, 19, 100), (5, 33, 768), (4, 9, 1001), (2, 70, 1032), (3, 17, 2050),
-                                   (2, 11, 4096), (1, 9, 8192), (2, 3, 16384), (700, 1, 64), (2, 3000, 72)])
+                                   (2, 11, 4096), (1, 9, 8192), (2, 3, 16384), (700, 1, 64), (2, 3000, 72),
+                                   (1, 5000, 776), (2, 2100, 1024), (5, 40, 128), (3, 70, 60), (9, 33, 130)])
 @pytest.mark.parametrize("xt,st", TYPES)
 def test_add_rmsnorm_backward(ctx, B, T, d, xt, st):
     h = rnd(1, B, T, d, dtype=st, std=2.0)
