@@ -283,26 +283,85 @@ __device__ __forceinline__ float row_sum(float v, float* smem, int turn) {
 }
 
 // ---- rows that do not start on 16-byte boundaries ------------------------------------------------
-// They pass through shared memory, coalesced on the global side element by element and in groups of eight on the other:
-// eight guarded scalar accesses a thread touch eight times the cache lines (norm backward of 1665 rows of 1001 fp32: 31 us).
+// They pass through shared memory at the alignment they have in global memory (a row's element j at byte skew + j es of its
+// buffer, skew = the row's address modulo 16): whole 16-byte pieces go by cp.async, the ends one by one, and a group of eight
+// elements is put together from the aligned pieces around it.  (Element-wise copies: norm of 12544 x 1001 bf16 61 us, its
+// backward pass 155 us; eight guarded scalar accesses a thread were slower still.)  Rows of fp32 go element by element into
+// an aligned buffer instead (skew 0): four bytes a lane are whole cache lines already, and a group written back to a skewed
+// buffer would be eight stores that meet in four banks (norm backward of 1665 x 1001 fp32: 22.2 us so, 18.3 us this way).
 __host__ __device__ constexpr int pad8(int d) { return (d + 7) / 8 * 8; }
+// bytes of a row's buffer: the skew before it, and the piece read beyond its last group
+__host__ __device__ constexpr int buffer_bytes(int d, int es) { return (pad8(d) * es + 15) / 16 * 16 + 32; }
+
+// 16 bytes from byte `off` (a multiple of the element size) of a 16-byte aligned buffer; the shift is the same for all of a row
+__device__ __forceinline__ uint4 unaligned16(const uint8_t* buf, int off) {
+    const uint4* p = reinterpret_cast<const uint4*>(buf + (off & ~15));
+    uint4 a = p[0];
+    const int sh = off & 15;
+    if (sh == 0) return a;
+    const uint4 b = p[1];
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (sh & 8) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (sh & 4) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    if (sh & 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// A row into its buffer, zeros up to a multiple of eight elements; returns the skew.  Complete after copies_done().
 template <int TPR>
-__device__ __forceinline__ void copy_in(float* buf, const float* row, int d, int t) {          // complete after copies_done()
+__device__ __forceinline__ int copy_in(uint8_t* buf, const float* row, int d, int t) {
     const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(buf));
 #pragma unroll 8
     for (int j = t; j < d; j += TPR) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4u * j), "l"(row + j) : "memory");
-    if (t < pad8(d) - d) buf[d + t] = 0.f;
+    if (t < pad8(d) - d) reinterpret_cast<float*>(buf)[d + t] = 0.f;
+    return 0;
 }
 template <int TPR>
-__device__ __forceinline__ void copy_in(__nv_bfloat16* buf, const __nv_bfloat16* row, int d, int t) {
-#pragma unroll 16
-    for (int j = t; j < pad8(d); j += TPR) buf[j] = j < d ? row[j] : __nv_bfloat16(0.f);
+__device__ __forceinline__ int copy_in(uint8_t* buf, const __nv_bfloat16* row, int d, int t) {
+    using T = __nv_bfloat16;
+    constexpr int ES = (int)sizeof(T), PER = 16 / ES;
+    const int skew = (int)(reinterpret_cast<uintptr_t>(row) & 15);
+    const int head = min(d, ((16 - skew) & 15) / ES), pieces = (d - head) / PER, rest = head + pieces * PER;
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(buf)) + skew + head * ES;
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(row + head);
+#pragma unroll 4
+    for (int c = t; c < pieces; c += TPR) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16u * c), "l"(from + 16 * (int64_t)c) : "memory");
+    T* at = reinterpret_cast<T*>(buf + skew);
+    for (int i = t; i < head + pad8(d) - rest; i += TPR) {
+        const int j = i < head ? i : rest + i - head;
+        at[j] = j < d ? row[j] : T(0.f);
+    }
+    return skew;
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-template <int TPR, typename T>
-__device__ __forceinline__ void copy_out(T* row, const T* buf, int d, int t) {
+// A buffer's row (at its skew) to global memory
+template <int TPR>
+__device__ __forceinline__ void copy_out(float* row, const uint8_t* buf, int, int d, int t) {
+    const float* at = reinterpret_cast<const float*>(buf);
 #pragma unroll 8
-    for (int j = t; j < d; j += TPR) row[j] = buf[j];
+    for (int j = t; j < d; j += TPR) row[j] = at[j];
+}
+template <int TPR>
+__device__ __forceinline__ void copy_out(__nv_bfloat16* row, const uint8_t* buf, int skew, int d, int t) {
+    using T = __nv_bfloat16;
+    constexpr int ES = (int)sizeof(T), PER = 16 / ES;
+    const int head = min(d, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / ES), pieces = (d - head) / PER, rest = head + pieces * PER;
+    uint4* to = reinterpret_cast<uint4*>(row + head);
+#pragma unroll 4
+    for (int c = t; c < pieces; c += TPR) __stcs(to + c, unaligned16(buf, skew + head * ES + 16 * c));
+    const T* at = reinterpret_cast<const T*>(buf + skew);
+    for (int i = t; i < head + d - rest; i += TPR) {
+        const int j = i < head ? i : rest + i - head;
+        row[j] = at[j];
+    }
 }
 // the threads of a row (and, where a row is wider than a warp, of all rows of the block)
 template <int TPR>
@@ -310,8 +369,9 @@ __device__ __forceinline__ void row_barrier() {
     if (TPR <= 32) __syncwarp();
     else __syncthreads();
 }
+// eight elements from 16-byte aligned shared memory
 template <typename T>
-__device__ __forceinline__ Raw<T> from_buffer(const T* p) {
+__device__ __forceinline__ Raw<T> from_aligned(const T* p) {
     Raw<T> r;
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
@@ -320,13 +380,36 @@ __device__ __forceinline__ Raw<T> from_buffer(const T* p) {
     }
     return r;
 }
+// eight elements of a row's buffer from column col on
 template <typename T>
-__device__ __forceinline__ void to_buffer(T* p, const Raw<T>& r) {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-        reinterpret_cast<uint4*>(p)[i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+__device__ __forceinline__ Raw<T> from_buffer(const uint8_t* buf, int skew, int col) {
+    if constexpr (sizeof(T) == 4) {
+        return from_aligned(reinterpret_cast<const T*>(buf) + col);
+    } else {
+        const uint4 v = unaligned16(buf, skew + col * (int)sizeof(T));
+        Raw<T> r;
+        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+        return r;
+    }
 }
-
+// ... and back to where they were, which no other thread reads
+__device__ __forceinline__ void to_buffer(uint8_t* buf, int, int col, const Raw<float>& r) {
+    uint4* p = reinterpret_cast<uint4*>(buf + col * 4);
+    p[0] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+    p[1] = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
+}
+__device__ __forceinline__ void to_buffer(uint8_t* buf, int skew, int col, const Raw<__nv_bfloat16>& r) {
+    uint8_t* p = buf + skew + col * 2;
+    if (skew & 2) {
+        *reinterpret_cast<unsigned short*>(p) = (unsigned short)r.w[0];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint32_t*>(p + 2 + 4 * i) = __funnelshift_r(r.w[i], r.w[i + 1], 16);
+        *reinterpret_cast<unsigned short*>(p + 14) = (unsigned short)(r.w[3] >> 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(p + 4 * i) = r.w[i];
+    }
+}
 __host__ __device__ constexpr int row_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 
 // ---- norm, forward --------------------------------------------------------------------------
@@ -347,11 +430,12 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
     const int d = (int)a.d;
     const XT* x = static_cast<const XT*>(a.x) + row * a.x_stride;
     const ST* r = static_cast<const ST*>(a.residual) + row * a.residual_stride;
-    XT* x_buf = reinterpret_cast<XT*>(row_buffers) + sub * pad8(d);
-    ST* r_buf = reinterpret_cast<ST*>(reinterpret_cast<XT*>(row_buffers) + ROWS * pad8(d)) + sub * pad8(d);
+    uint8_t* x_buf = row_buffers + sub * buffer_bytes(d, sizeof(XT));
+    uint8_t* r_buf = row_buffers + ROWS * buffer_bytes(d, sizeof(XT)) + sub * buffer_bytes(d, sizeof(ST));
+    int x_skew = 0, r_skew = 0;
     if (!VEC) {
-        copy_in<TPR>(x_buf, x, d, t);
-        if (a.residual) copy_in<TPR>(r_buf, r, d, t);
+        x_skew = copy_in<TPR>(x_buf, x, d, t);
+        if (a.residual) r_skew = copy_in<TPR>(r_buf, r, d, t);
         copies_done();
         row_barrier<TPR>();
     }
@@ -361,13 +445,13 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
     for (int c = 0; c < C; ++c) {
         const int col = (c * TPR + t) * 8;
         xr[c] = zero_raw<XT>();
-        if (col < d) xr[c] = VEC ? load_raw<true>(x + col, 8) : from_buffer(x_buf + col);
+        if (col < d) xr[c] = VEC ? load_raw<true>(x + col, 8) : from_buffer<XT>(x_buf, x_skew, col);
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int col = (c * TPR + t) * 8;
         rr[c] = zero_raw<ST>();
-        if (a.residual && col < d) rr[c] = VEC ? load_raw<true>(r + col, 8) : from_buffer(r_buf + col);
+        if (a.residual && col < d) rr[c] = VEC ? load_raw<true>(r + col, 8) : from_buffer<ST>(r_buf, r_skew, col);
     }
     if (key.on) {
 #pragma unroll
@@ -390,7 +474,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
         }
         if (a.h && there && col < d) {
             if (VEC) store_raw<true>(static_cast<ST*>(a.h) + row * a.h_stride + col, 8, out);
-            else to_buffer(r_buf + col, out);
+            else to_buffer(r_buf, r_skew, col, out);
         }
     }
     const float mean = row_sum<TPR, THREADS>(ss.x + ss.y, smem, 0);
@@ -419,15 +503,15 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
             }
             if (a.y) {
                 if (VEC) store_raw<true>(static_cast<XT*>(a.y) + row * a.y_stride + col, 8, out);
-                else to_buffer(x_buf + col, out);
+                else to_buffer(x_buf, x_skew, col, out);
             }
         }
         if (a.q) quantise_block<(TPR < 16 ? TPR : 16)>(g, n, q_row, s_row, col);
     }
     if (!VEC) {
         row_barrier<TPR>();
-        if (a.h && there) copy_out<TPR>(static_cast<ST*>(a.h) + row * a.h_stride, r_buf, d, t);
-        if (a.y && there) copy_out<TPR>(static_cast<XT*>(a.y) + row * a.y_stride, x_buf, d, t);
+        if (a.h && there) copy_out<TPR>(static_cast<ST*>(a.h) + row * a.h_stride, r_buf, r_skew, d, t);
+        if (a.y && there) copy_out<TPR>(static_cast<XT*>(a.y) + row * a.y_stride, x_buf, x_skew, d, t);
     }
 }
 
@@ -497,10 +581,11 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
     const int64_t first = chunk * p.rows_per_chunk, last = min(a.T, first + p.rows_per_chunk);
     const float inv_d = 1.0f / (float)d;
     const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(columns)) + threadIdx.x * 16;
-    const int wide = pad8(d);
-    XT* u_buf = reinterpret_cast<XT*>(columns) + sub * wide;
-    ST* v_buf = reinterpret_cast<ST*>(reinterpret_cast<XT*>(columns) + ROWS * wide) + sub * wide;
-    ST* r_buf = v_buf + ROWS * wide;
+    const int wide_x = buffer_bytes(d, sizeof(XT)), wide_s = buffer_bytes(d, sizeof(ST));
+    uint8_t* u_buf = reinterpret_cast<uint8_t*>(columns) + sub * wide_x;
+    uint8_t* v_buf = reinterpret_cast<uint8_t*>(columns) + ROWS * wide_x + sub * wide_s;
+    uint8_t* r_buf = v_buf + ROWS * wide_s;
+    int u_skew = 0, v_skew = 0, r_skew = 0;
     F2 acc[GAIN ? C : 1][4];
     if (GAIN) {
 #pragma unroll
@@ -549,17 +634,17 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
             asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
         } else if (!VEC) {
             row_barrier<TPR>();                              // the buffers' last rows are stored
-            copy_in<TPR>(u_buf, dy, d, t);
-            copy_in<TPR>(v_buf, h, d, t);
-            if (a.dh_residual) copy_in<TPR>(r_buf, res, d, t);
+            u_skew = copy_in<TPR>(u_buf, dy, d, t);
+            v_skew = copy_in<TPR>(v_buf, h, d, t);
+            if (a.dh_residual) r_skew = copy_in<TPR>(r_buf, res, d, t);
             copies_done();
             row_barrier<TPR>();
         }
         auto dy_of = [&](int c, int col) {
-            return STAGED ? staged<XT>(from + (c * XP) * STEP, STEP) : VEC ? load_raw<true>(dy + col, 8) : from_buffer(u_buf + col);
+            return STAGED ? staged<XT>(from + (c * XP) * STEP, STEP) : VEC ? load_raw<true>(dy + col, 8) : from_buffer<XT>(u_buf, u_skew, col);
         };
         auto h_of = [&](int c, int col) {
-            return STAGED ? staged<ST>(from + (C * XP + c * SP) * STEP, STEP) : VEC ? load_raw<true>(h + col, 8) : from_buffer(v_buf + col);
+            return STAGED ? staged<ST>(from + (C * XP + c * SP) * STEP, STEP) : VEC ? load_raw<true>(h + col, 8) : from_buffer<ST>(v_buf, v_skew, col);
         };
         // The row is gone through twice, before and after its sum, from shared memory: holding gain dy and xhat in registers in
         // between left two blocks an SM instead of three.  (Rows too wide for two stages are read from global memory twice.)
@@ -590,7 +675,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
                 const Raw<ST> vr = h_of(c, col);
                 Raw<ST> r = zero_raw<ST>(), out;
                 if (a.dh_residual)
-                    r = STAGED ? staged<ST>(from + (C * XP + C * SP + c * SP) * STEP, STEP) : VEC ? load_raw<true>(res + col, 8) : from_buffer(r_buf + col);
+                    r = STAGED ? staged<ST>(from + (C * XP + C * SP + c * SP) * STEP, STEP) : VEC ? load_raw<true>(res + col, 8) : from_buffer<ST>(r_buf, r_skew, col);
                 F2 g[4], o[4];
                 load_gain(a.gain, a.gain_dtype == ADLOCO_BF16, col, min(8, d - col), g);
 #pragma unroll
@@ -599,21 +684,21 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
                     set_pair(out, i, o[i]);
                 }
                 if (VEC) store_raw<true>(static_cast<ST*>(a.dh) + row * a.dh_stride + col, 8, out);
-                else to_buffer(v_buf + col, out);
+                else to_buffer(v_buf, v_skew, col, out);
                 if (a.dx) {
                     Raw<XT> x;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) set_pair(x, i, mul2(o[i], both(key.scale)));
                     if (key.on) drop_raw(x, kept_of<VEC>((uint64_t)(row * d + col), key), key);
                     if (VEC) store_raw<true>(static_cast<XT*>(a.dx) + row * a.dx_stride + col, 8, x);
-                    else to_buffer(u_buf + col, x);
+                    else to_buffer(u_buf, u_skew, col, x);
                 }
             }
         }
         if (!VEC) {
             row_barrier<TPR>();
-            if (there) copy_out<TPR>(static_cast<ST*>(a.dh) + row * a.dh_stride, v_buf, d, t);
-            if (there && a.dx) copy_out<TPR>(static_cast<XT*>(a.dx) + row * a.dx_stride, u_buf, d, t);
+            if (there) copy_out<TPR>(static_cast<ST*>(a.dh) + row * a.dh_stride, v_buf, v_skew, d, t);
+            if (there && a.dx) copy_out<TPR>(static_cast<XT*>(a.dx) + row * a.dx_stride, u_buf, u_skew, d, t);
         }
         stage = stage == DEPTH - 1 ? 0 : stage + 1;
     }
@@ -1048,7 +1133,7 @@ __global__ void __launch_bounds__(256) quantise_rows_kernel(const T* x, int64_t 
 #pragma unroll
         for (int k = 0; k < U; ++k)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) v[k][j] = from_buffer(&stage[warp][k][(lane >> 3)][lane_col + 8 * j]);
+            for (int j = 0; j < 2; ++j) v[k][j] = from_aligned(&stage[warp][k][(lane >> 3)][lane_col + 8 * j]);
     }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
@@ -1173,10 +1258,10 @@ template <typename XT, typename ST, int TPR, int C, bool VEC>
 static int add_rmsnorm_launch(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const DropoutKey& key, cudaStream_t st) {
     constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
     auto kernel = add_rmsnorm_kernel<XT, ST, TPR, C, VEC>;
-    const size_t smem = VEC ? 0 : (size_t)ROWS * pad8((int)a.d) * (sizeof(XT) + sizeof(ST));
+    const size_t smem = VEC ? 0 : (size_t)ROWS * (buffer_bytes((int)a.d, sizeof(XT)) + buffer_bytes((int)a.d, sizeof(ST)));
     if (smem > 40 * 1024) {
         static std::atomic<bool> done[64];
-        const int rc = allow_smem(ctx, kernel, (size_t)ROWS * TPR * C * 8 * (sizeof(XT) + sizeof(ST)), done);
+        const int rc = allow_smem(ctx, kernel, (size_t)ROWS * (buffer_bytes(TPR * C * 8, sizeof(XT)) + buffer_bytes(TPR * C * 8, sizeof(ST))), done);
         if (rc != ADLOCO_OK) return rc;
     }
     ADLOCO_CUDA_TRY(ctx, launch_early(kernel, dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), THREADS, smem, st, 1, a, key));
@@ -1229,12 +1314,12 @@ template <typename XT, typename ST, int TPR, int C, bool VEC, bool GAIN>
 static int rmsnorm_backward_launch(adloco_ctx* ctx, const RmsBackArgs& p, const DropoutKey& key, unsigned grid, cudaStream_t st) {
     constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
     auto kernel = rmsnorm_backward_kernel<XT, ST, TPR, C, VEC, GAIN>;
-    constexpr size_t row_bytes = sizeof(XT) + 2 * sizeof(ST);
-    size_t smem = VEC ? stage_smem<XT, ST, C, THREADS>() : (size_t)ROWS * pad8((int)p.a.d) * row_bytes;
+    auto buffers = [](int d) { return (size_t)ROWS * (buffer_bytes(d, sizeof(XT)) + 2 * buffer_bytes(d, sizeof(ST))); };
+    size_t smem = VEC ? stage_smem<XT, ST, C, THREADS>() : buffers((int)p.a.d);
     if (GAIN && ROWS > 1 && smem < (size_t)ROWS * p.a.d * sizeof(float)) smem = (size_t)ROWS * p.a.d * sizeof(float);
     if (smem > 40 * 1024) {
         static std::atomic<bool> done[64];
-        const int rc = allow_smem(ctx, kernel, VEC ? stage_smem<XT, ST, C, THREADS>() : (size_t)ROWS * TPR * C * 8 * row_bytes, done);
+        const int rc = allow_smem(ctx, kernel, VEC ? stage_smem<XT, ST, C, THREADS>() : buffers(TPR * C * 8), done);
         if (rc != ADLOCO_OK) return rc;
     }
     ADLOCO_CUDA_TRY(ctx, launch_early(kernel, dim3(grid), THREADS, smem, st, 1, p, key));
