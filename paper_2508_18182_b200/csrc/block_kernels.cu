@@ -1297,17 +1297,18 @@ int launch_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const Drop
 
 // Blocks a sample's rows are cut into: about as many over all samples as are resident at once, at least a row for every
 // group of threads in a block.  Blocks an SM by width (registers set them in bf16; of 2, 3, 4 and 6 these measured best at
-// 256, 768, 1024, 2048, 3000 and 4096); `fit` is what shared memory allows beside that.
-static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d, int64_t fit) {
+// 256, 768, 1024, 2048, 3000 and 4096; five for narrow rows off the 16-byte grid); `fit` is what shared memory allows beside that.
+static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d, bool vec, int64_t fit) {
     const int64_t rows_at_once = d <= 64 ? 32 : d <= 128 ? 16 : d <= 1024 ? 8 : d <= 4096 ? 2 : 1;
     const int64_t most = (T + rows_at_once - 1) / rows_at_once;
-    int64_t blocks = d <= 256 ? 4 : d <= 768 ? 3 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 3072 ? 3 : 2;
+    int64_t blocks = d <= 256 ? (vec ? 4 : 5) : d <= 768 ? 3 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 3072 ? 3 : 2;
     if (blocks > fit) blocks = fit < 1 ? 1 : fit;
     const int64_t want = blocks * (int64_t)ctx->sm_count / B;
     return want < 1 ? 1 : want > most ? most : want;
 }
 int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d) {
-    return B * rmsnorm_chunks(ctx, B, T, d, 8) * d * (int64_t)sizeof(float);
+    const int64_t one = rmsnorm_chunks(ctx, B, T, d, true, 8), other = rmsnorm_chunks(ctx, B, T, d, false, 8);
+    return B * (one > other ? one : other) * d * (int64_t)sizeof(float);
 }
 
 template <typename XT, typename ST, int TPR, int C, bool VEC, bool GAIN>
@@ -1346,7 +1347,8 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     p.a = a;
     const int64_t row_bytes = (xb ? 2 : 4) + 2 * (sb ? 2 : 4), threads = a.d > 4096 ? 512 : 256;
     const int64_t groups = a.d <= 1024 ? (a.d + 255) / 256 : a.d <= 4096 ? (a.d + 1023) / 1024 : (a.d + 4095) / 4096;     // of eight a thread
-    p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d, 227 * 1024 / (2 * threads * groups * 8 * row_bytes + 1024));
+    const int64_t smem = (vec ? 2 : 1) * threads * groups * 8 * row_bytes;            // two rows on their way, or one in its buffers
+    p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d, vec, 227 * 1024 / (smem + 1024));
     p.rows_per_chunk = (a.T + p.chunks - 1) / p.chunks;
     int rc = ADLOCO_OK;
 #define ADLOCO_TYPES(XT, ST)                                                               \
