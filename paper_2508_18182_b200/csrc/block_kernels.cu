@@ -2,6 +2,7 @@
 // dropout, its backward pass with the gain's per-sample norms, dropout alone, rotary positions,
 // and quantisation to 8 bits with power-of-two scales.  All are bound by HBM: each input is read
 // once, each output written once, everything between stays in registers.
+#include <algorithm>
 #include <cuda_fp8.h>
 #include <atomic>
 
@@ -315,9 +316,13 @@ __device__ __forceinline__ uint4 unaligned16(const uint8_t* buf, int off) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// A row into its buffer, zeros up to a multiple of eight elements; returns the skew.  Complete after copies_done().
+// A row into its buffer, zeros up to a multiple of eight elements; returns the skew.  The ends that are not copied
+// asynchronously wait in registers (`ends`) for finish_in, so that a row can be on its way during the one before it.
+// Complete after start_in, copies_done (or a wait for its group) and finish_in.
 template <int TPR>
-__device__ __forceinline__ int copy_in(uint8_t* buf, const float* row, int d, int t) {
+__host__ __device__ constexpr int row_ends() { return TPR >= 32 ? 1 : 32 / TPR; }      // up to 7 before, 7 after, 7 zeros
+template <int TPR>
+__device__ __forceinline__ int start_in(uint8_t* buf, const float* row, int d, int t, float (&)[row_ends<TPR>()]) {
     const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(buf));
 #pragma unroll 8
     for (int j = t; j < d; j += TPR) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4u * j), "l"(row + j) : "memory");
@@ -325,23 +330,39 @@ __device__ __forceinline__ int copy_in(uint8_t* buf, const float* row, int d, in
     return 0;
 }
 template <int TPR>
-__device__ __forceinline__ int copy_in(uint8_t* buf, const __nv_bfloat16* row, int d, int t) {
-    using T = __nv_bfloat16;
-    constexpr int ES = (int)sizeof(T), PER = 16 / ES;
+__device__ __forceinline__ void finish_in(uint8_t*, int, int, int, const float (&)[row_ends<TPR>()]) {}
+template <int TPR>
+__device__ __forceinline__ int start_in(uint8_t* buf, const __nv_bfloat16* row, int d, int t, __nv_bfloat16 (&ends)[row_ends<TPR>()]) {
     const int skew = (int)(reinterpret_cast<uintptr_t>(row) & 15);
-    const int head = min(d, ((16 - skew) & 15) / ES), pieces = (d - head) / PER, rest = head + pieces * PER;
-    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(buf)) + skew + head * ES;
+    const int head = min(d, ((16 - skew) & 15) / 2), pieces = (d - head) / 8, rest = head + pieces * 8;
+    const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(buf)) + skew + head * 2;
     const uint8_t* from = reinterpret_cast<const uint8_t*>(row + head);
 #pragma unroll 4
     for (int c = t; c < pieces; c += TPR) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16u * c), "l"(from + 16 * (int64_t)c) : "memory");
-    T* at = reinterpret_cast<T*>(buf + skew);
-    for (int i = t; i < head + pad8(d) - rest; i += TPR) {
-        const int j = i < head ? i : rest + i - head;
-        at[j] = j < d ? row[j] : T(0.f);
+#pragma unroll
+    for (int k = 0; k < row_ends<TPR>(); ++k) {
+        const int i = t + k * TPR, j = i < head ? i : rest + i - head;
+        ends[k] = j < d ? row[j] : __nv_bfloat16(0.f);
     }
     return skew;
 }
+template <int TPR>
+__device__ __forceinline__ void finish_in(uint8_t* buf, int skew, int d, int t, const __nv_bfloat16 (&ends)[row_ends<TPR>()]) {
+    const int head = min(d, ((16 - skew) & 15) / 2), rest = head + (d - head) / 8 * 8;
+#pragma unroll
+    for (int k = 0; k < row_ends<TPR>(); ++k) {
+        const int i = t + k * TPR, j = i < head ? i : rest + i - head;
+        if (j < pad8(d)) reinterpret_cast<__nv_bfloat16*>(buf + skew)[j] = ends[k];
+    }
+}
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+template <int TPR, typename T>
+__device__ __forceinline__ int copy_in(uint8_t* buf, const T* row, int d, int t) {
+    T ends[row_ends<TPR>()];
+    const int skew = start_in<TPR>(buf, row, d, t, ends);
+    finish_in<TPR>(buf, skew, d, t, ends);
+    return skew;
+}
 // A buffer's row (at its skew) to global memory
 template <int TPR>
 __device__ __forceinline__ void copy_out(float* row, const uint8_t* buf, int, int d, int t) {
@@ -523,9 +544,11 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
 // A thread's own elements of the next rows travel ahead through shared memory (cp.async, each thread reads only
 // what it copied, so no barrier): registers for three operands of one row leave 16 warps an SM, too few loads in
 // flight without it.
+constexpr size_t kTwoRows = 120 * 1024;          // above what two rows' buffers of a block take off the 16-byte grid
 struct RmsBackArgs {
     adloco_rmsnorm_backward_args a;
     int64_t chunks, rows_per_chunk;
+    int buffers;                                            // rows in shared memory off the 16-byte grid: one, or one ahead
 };
 __device__ __forceinline__ void copy16_async(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -585,7 +608,21 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
     uint8_t* u_buf = reinterpret_cast<uint8_t*>(columns) + sub * wide_x;
     uint8_t* v_buf = reinterpret_cast<uint8_t*>(columns) + ROWS * wide_x + sub * wide_s;
     uint8_t* r_buf = v_buf + ROWS * wide_s;
-    int u_skew = 0, v_skew = 0, r_skew = 0;
+    const int other = p.buffers > 1 ? ROWS * (wide_x + 2 * wide_s) : 0;     // from a row's buffers to the next row's
+    int u_skew = 0, v_skew = 0, r_skew = 0, u_next = 0, v_next = 0, r_next = 0;
+    XT u_ends[row_ends<TPR>()] = {};
+    ST v_ends[row_ends<TPR>()] = {}, r_ends[row_ends<TPR>()] = {};
+    // !VEC: starts the copies of row at + sub into its buffers, one group a call, empty beyond the last row
+    auto start = [&](int64_t at, int offset) {
+        if (at + sub < last) {
+            const int64_t row = sample * a.T + at + sub;
+            u_next = start_in<TPR>(u_buf + offset, static_cast<const XT*>(a.dy) + row * a.dy_stride, d, t, u_ends);
+            v_next = start_in<TPR>(v_buf + offset, static_cast<const ST*>(a.h) + row * a.h_stride, d, t, v_ends);
+            if (a.dh_residual) r_next = start_in<TPR>(r_buf + offset, static_cast<const ST*>(a.dh_residual) + row * a.dh_residual_stride, d, t, r_ends);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (!VEC && other) start(first, 0);
     F2 acc[GAIN ? C : 1][4];
     if (GAIN) {
 #pragma unroll
@@ -633,12 +670,19 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
             fetch(at + (DEPTH - 1) * ROWS, stage == 0 ? DEPTH - 1 : stage - 1);
             asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
         } else if (!VEC) {
-            row_barrier<TPR>();                              // the buffers' last rows are stored
-            u_skew = copy_in<TPR>(u_buf, dy, d, t);
-            v_skew = copy_in<TPR>(v_buf, h, d, t);
-            if (a.dh_residual) r_skew = copy_in<TPR>(r_buf, res, d, t);
+            if (!other) {
+                row_barrier<TPR>();                          // the buffers' last rows are stored
+                start(at, 0);
+            }
+            u_skew = u_next; v_skew = v_next; r_skew = r_next;
+            if (there) {
+                finish_in<TPR>(u_buf, u_skew, d, t, u_ends);
+                finish_in<TPR>(v_buf, v_skew, d, t, v_ends);
+                if (a.dh_residual) finish_in<TPR>(r_buf, r_skew, d, t, r_ends);
+            }
             copies_done();
-            row_barrier<TPR>();
+            row_barrier<TPR>();                              // this row is there, and the row before it stored
+            if (other) start(at + ROWS, turn & 1 ? -other : other);
         }
         auto dy_of = [&](int c, int col) {
             return STAGED ? staged<XT>(from + (c * XP) * STEP, STEP) : VEC ? load_raw<true>(dy + col, 8) : from_buffer<XT>(u_buf, u_skew, col);
@@ -699,6 +743,8 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
             row_barrier<TPR>();
             if (there) copy_out<TPR>(static_cast<ST*>(a.dh) + row * a.dh_stride, v_buf, v_skew, d, t);
             if (there && a.dx) copy_out<TPR>(static_cast<XT*>(a.dx) + row * a.dx_stride, u_buf, u_skew, d, t);
+            const int step = turn & 1 ? -other : other;
+            u_buf += step; v_buf += step; r_buf += step;
         }
         stage = stage == DEPTH - 1 ? 0 : stage + 1;
     }
@@ -1298,10 +1344,13 @@ int launch_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const Drop
 // Blocks a sample's rows are cut into: about as many over all samples as are resident at once, at least a row for every
 // group of threads in a block.  Blocks an SM by width (registers set them in bf16; of 2, 3, 4 and 6 these measured best at
 // 256, 768, 1024, 2048, 3000 and 4096; five for narrow rows off the 16-byte grid); `fit` is what shared memory allows beside that.
+static int64_t rmsnorm_blocks(int64_t d, bool vec) {
+    return d <= 256 ? (vec ? 4 : 5) : d <= 768 ? 3 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 3072 ? 3 : 2;
+}
 static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d, bool vec, int64_t fit) {
     const int64_t rows_at_once = d <= 64 ? 32 : d <= 128 ? 16 : d <= 1024 ? 8 : d <= 4096 ? 2 : 1;
     const int64_t most = (T + rows_at_once - 1) / rows_at_once;
-    int64_t blocks = d <= 256 ? (vec ? 4 : 5) : d <= 768 ? 3 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 3072 ? 3 : 2;
+    int64_t blocks = rmsnorm_blocks(d, vec);
     if (blocks > fit) blocks = fit < 1 ? 1 : fit;
     const int64_t want = blocks * (int64_t)ctx->sm_count / B;
     return want < 1 ? 1 : want > most ? most : want;
@@ -1316,11 +1365,11 @@ static int rmsnorm_backward_launch(adloco_ctx* ctx, const RmsBackArgs& p, const 
     constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
     auto kernel = rmsnorm_backward_kernel<XT, ST, TPR, C, VEC, GAIN>;
     auto buffers = [](int d) { return (size_t)ROWS * (buffer_bytes(d, sizeof(XT)) + 2 * buffer_bytes(d, sizeof(ST))); };
-    size_t smem = VEC ? stage_smem<XT, ST, C, THREADS>() : buffers((int)p.a.d);
+    size_t smem = VEC ? stage_smem<XT, ST, C, THREADS>() : p.buffers * buffers((int)p.a.d);
     if (GAIN && ROWS > 1 && smem < (size_t)ROWS * p.a.d * sizeof(float)) smem = (size_t)ROWS * p.a.d * sizeof(float);
     if (smem > 40 * 1024) {
         static std::atomic<bool> done[64];
-        const int rc = allow_smem(ctx, kernel, VEC ? stage_smem<XT, ST, C, THREADS>() : buffers(TPR * C * 8), done);
+        const int rc = allow_smem(ctx, kernel, VEC ? stage_smem<XT, ST, C, THREADS>() : std::max(buffers(TPR * C * 8), std::min(2 * buffers(TPR * C * 8), kTwoRows)), done);
         if (rc != ADLOCO_OK) return rc;
     }
     ADLOCO_CUDA_TRY(ctx, launch_early(kernel, dim3(grid), THREADS, smem, st, 1, p, key));
@@ -1347,7 +1396,10 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     p.a = a;
     const int64_t row_bytes = (xb ? 2 : 4) + 2 * (sb ? 2 : 4), threads = a.d > 4096 ? 512 : 256;
     const int64_t groups = a.d <= 1024 ? (a.d + 255) / 256 : a.d <= 4096 ? (a.d + 1023) / 1024 : (a.d + 4095) / 4096;     // of eight a thread
-    const int64_t smem = (vec ? 2 : 1) * threads * groups * 8 * row_bytes;            // two rows on their way, or one in its buffers
+    const int64_t one = threads * groups * 8 * row_bytes;
+    // a row ahead where it takes no block from an SM
+    p.buffers = !vec && (2 * one + 1024) * rmsnorm_blocks(a.d, vec) <= 227 * 1024 ? 2 : 1;
+    const int64_t smem = (vec ? 2 : p.buffers) * one;
     p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d, vec, 227 * 1024 / (smem + 1024));
     p.rows_per_chunk = (a.T + p.chunks - 1) / p.chunks;
     int rc = ADLOCO_OK;
