@@ -70,7 +70,9 @@ def test_add_rmsnorm(ctx, d, xt, st):
 
 @pytest.mark.parametrize("B,T,d", [(1, 1, 8), (3, 5, 8), (1, 1, 1024), (2, 19, 100), (5, 33, 768), (4, 9, 1001), (2, 70, 1032), (3, 17, 2050),
                                    (2, 11, 4096), (1, 9, 8192), (2, 3, 16384), (700, 1, 64), (2, 3000, 72),
-                                   (1, 5000, 776), (2, 2100, 1024), (5, 40, 128), (3, 70, 60), (9, 33, 130)])
+                                   (1, 5000, 776), (2, 2100, 1024), (5, 40, 128), (3, 70, 60), (9, 33, 130),
+                                   # several rows of a block off the 16-byte grid, one ahead of the other where two fit
+                                   (1, 7003, 1001), (2, 12011, 101), (1, 48007, 63), (2, 9001, 255), (1, 2503, 4095), (1, 4001, 2049)])
 @pytest.mark.parametrize("xt,st", TYPES)
 def test_add_rmsnorm_backward(ctx, B, T, d, xt, st):
     h = rnd(1, B, T, d, dtype=st, std=2.0)
@@ -135,6 +137,32 @@ def test_norm_gradient_is_that_of_the_forward_call_by_differences(ctx):
         fine, coarse = central(2.0 ** -5), central(2.0 ** -4)
         scale = sum((g.double().abs() * w.abs()).sum().item() for g, w in zip((dx, dh, S), v))
         assert abs((4 * fine - coarse) / 3 - slope) < 2e-3 * scale / np.sqrt(3 * B * T * d) * 10
+
+
+@pytest.mark.parametrize("xt,st", TYPES)
+def test_norm_backward_on_pitched_and_shifted_rows_in_place(ctx, xt, st):
+    """Rows that start at every offset from the 16-byte grid, each operand at its own pitch and shift; the stream's
+    gradient is written over the one that comes in, dx over dy, and what lies between the rows stays as it was."""
+    B, T = 3, 900
+    for d, pitch, shift in ((768, 777, 3), (101, 107, 1), (510, 515, 5), (1000, 1001, 0)):
+        wide = {k: rnd(i, B * T, pitch + i, dtype=t) for i, (k, t) in enumerate((("dy", xt), ("h", st), ("res", st)))}
+        dy, h, res = (wide[k][:, shift:shift + d].unflatten(0, (B, T)) for k in ("dy", "h", "res"))
+        gain = rnd(9, d)
+        rstd = torch.rsqrt(h.float().square().mean(-1) + 1e-6)
+        args = [np64(v) for v in (dy, h, rstd, gain)]
+        dh_ref, dx_ref, n_ref, S_ref = O.add_rmsnorm_backward(*args, np64(res), MASK)
+        u, hat = np.abs(args[0] * args[3]), args[1] * args[2][..., None]
+        size = np.abs(np64(res)) + args[2][..., None] * (u + np.abs(hat) * np.mean(u * np.abs(hat), -1, keepdims=True))
+        before = {k: v.clone() for k, v in wide.items()}
+        S = torch.empty(d, device=DEV)
+        ctx.add_rmsnorm_backward(dy, h, rstd, gain, res, dh_residual=res, dx=dy, dropout=MASK, grad_sum=S)
+        torch.cuda.synchronize()
+        close(res, dh_ref, rounding(st) * np.abs(dh_ref) + 2.0 ** -19 * size, "dh")
+        close(dy, dx_ref, rounding(xt) * np.abs(dx_ref) + 2.0 ** -18 * size, "dx")
+        close(S, S_ref, (T + B + 80) * 2.0 ** -23 * np.abs(args[0] * hat).sum((0, 1)) + 2.0 ** -22 * np.abs(S_ref), "S")
+        assert torch.equal(wide["h"], before["h"])
+        for k in ("dy", "res"):
+            assert torch.equal(wide[k][:, :shift], before[k][:, :shift]) and torch.equal(wide[k][:, shift + d:], before[k][:, shift + d:])
 
 
 def test_norm_on_pitched_and_shifted_rows_in_place_and_on_another_stream(ctx):
