@@ -350,7 +350,7 @@ def test_quantise_weights_exactly(ctx, rows, cols, dtype):
     assert np.array_equal(s.cpu().numpy(), e + 127) and np.array_equal(values(q), v) and np.array_equal(values(qt), v.T)
 
 
-@pytest.mark.parametrize("d", [128, 100, 768, 1000, 2048, 4104])
+@pytest.mark.parametrize("d", [1, 60, 64, 128, 100, 136, 768, 1000, 1001, 2048, 4104])
 def test_norm_to_8_bits(ctx, d):
     x, res, gain = rnd(1, 9, d, dtype=BF), rnd(2, 9, d, dtype=BF, std=2.0), torch.exp(rnd(3, d))
     q, s = pitched(9, d, 16), pitched(9, (d + 127) // 128, 4)
