@@ -344,7 +344,7 @@ int adloco_embedding_sqnorm(adloco_ctx* ctx, const int32_t* token_ids, const voi
  * produce the X and Delta that the per-sample norms above read; the norm's own gain
  * contributes its per-sample norms in the same pass.  None of them uses the ctx workspace, so
  * all may be issued on several streams at once.  Rows are addressed by a pitch in elements;
- * 16-byte aligned rows (base and pitch) take vector loads, others a slower element-wise path. */
+ * 16-byte aligned rows (base and pitch) take vector loads; others are slower, the norm's through shared memory. */
 
 /* h = residual + drop(x);  y = gain * h / sqrt(mean(h^2) + eps) over each row of d elements.
  *   x, y          dev [rows, d] in dtype
@@ -389,7 +389,7 @@ int adloco_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args* args, void* s
  * and for the gain g_i = sum_t dy_{i,t} xhat_{i,t}:  n_i = ||g_i||^2,  S = sum_i g_i.
  *   dy             dev [rows, d] in dtype;  h (the forward pass's), dh_residual, dh: in stream_dtype
  *   dh_residual    the gradient that reaches h along the residual stream; NULL = 0; may be dh itself
- *   dx             dev [rows, d] in dtype, may be NULL (without dropout dx equals dh)
+ *   dx             dev [rows, d] in dtype, may be NULL (without dropout dx equals dh) or dy itself
  *   per_sample_sqnorm, accumulate_norms, grad_sum, accumulate_sum   as in adloco_vector_param_sqnorm;
  *                  both pointers may be NULL (a frozen gain)
  *   workspace      dev, 16-byte aligned, at least adloco_add_rmsnorm_backward_workspace bytes; not

@@ -286,10 +286,11 @@ __device__ __forceinline__ float row_sum(float v, float* smem, int turn) {
 // ---- rows that do not start on 16-byte boundaries ------------------------------------------------
 // They pass through shared memory at the alignment they have in global memory (a row's element j at byte skew + j es of its
 // buffer, skew = the row's address modulo 16): whole 16-byte pieces go by cp.async, the ends one by one, and a group of eight
-// elements is put together from the aligned pieces around it.  (Element-wise copies: norm of 12544 x 1001 bf16 61 us, its
-// backward pass 155 us; eight guarded scalar accesses a thread were slower still.)  Rows of fp32 go element by element into
-// an aligned buffer instead (skew 0): four bytes a lane are whole cache lines already, and a group written back to a skewed
-// buffer would be eight stores that meet in four banks (norm backward of 1665 x 1001 fp32: 22.2 us so, 18.3 us this way).
+// elements is put together from the aligned pieces around it.  (Norm of 6272 x 1001 bf16: 18.7 us, its backward pass 45.9;
+// with element-wise copies 31 and 78; eight guarded scalar accesses a thread were slower still.)  Rows of fp32 go element by
+// element into an aligned buffer instead (skew 0): four bytes a lane are whole cache lines already, and a group written back
+// to a skewed buffer would be eight stores that meet in four banks (norm backward of 1665 x 1001 fp32 by 145 blocks: 22.2 us
+// so, 18.3 us this way).
 __host__ __device__ constexpr int pad8(int d) { return (d + 7) / 8 * 8; }
 // bytes of a row's buffer: the skew before it, and the piece read beyond its last group
 __host__ __device__ constexpr int buffer_bytes(int d, int es) { return (pad8(d) * es + 15) / 16 * 16 + 32; }
