@@ -286,7 +286,7 @@ __device__ __forceinline__ float row_sum(float v, float* smem, int turn) {
 // ---- rows that do not start on 16-byte boundaries ------------------------------------------------
 // They pass through shared memory at the alignment they have in global memory (a row's element j at byte skew + j es of its
 // buffer, skew = the row's address modulo 16): whole 16-byte pieces go by cp.async, the ends one by one, and a group of eight
-// elements is put together from the aligned pieces around it.  (Norm of 6272 x 1001 bf16: 18.7 us, its backward pass 45.9;
+// elements is put together from the aligned pieces around it.  (Norm of 6272 x 1001 bf16: 18.7 us, its backward pass 46.3;
 // with element-wise copies 31 and 78; eight guarded scalar accesses a thread were slower still.)  Rows of fp32 go element by
 // element into an aligned buffer instead (skew 0): four bytes a lane are whole cache lines already, and a group written back
 // to a skewed buffer would be eight stores that meet in four banks (norm backward of 1665 x 1001 fp32 by 145 blocks: 22.2 us
@@ -1342,19 +1342,20 @@ int launch_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const Drop
     return ADLOCO_OK;
 }
 
-// Blocks a sample's rows are cut into: about as many over all samples as are resident at once, at least a row for every
-// group of threads in a block.  Blocks an SM by width (registers set them in bf16; of 2, 3, 4 and 6 these measured best at
+// Blocks a sample's rows are cut into: about as many over all samples as are resident at once, each with whole turns of a row
+// for every group of its threads (4 samples of 1024 x 300 bf16 by ten rows a block, eight and two: 24.4 us; by sixteen: 15.7).  Blocks an SM by width (registers set them in bf16; of 2, 3, 4 and 6 these measured best at
 // 256, 768, 1024, 2048, 3000 and 4096; five for narrow rows off the 16-byte grid); `fit` is what shared memory allows beside that.
 static int64_t rmsnorm_blocks(int64_t d, bool vec) {
     return d <= 256 ? (vec ? 4 : 5) : d <= 768 ? 3 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 3072 ? 3 : 2;
 }
 static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d, bool vec, int64_t fit) {
     const int64_t rows_at_once = d <= 64 ? 32 : d <= 128 ? 16 : d <= 1024 ? 8 : d <= 4096 ? 2 : 1;
-    const int64_t most = (T + rows_at_once - 1) / rows_at_once;
     int64_t blocks = rmsnorm_blocks(d, vec);
     if (blocks > fit) blocks = fit < 1 ? 1 : fit;
     const int64_t want = blocks * (int64_t)ctx->sm_count / B;
-    return want < 1 ? 1 : want > most ? most : want;
+    if (want <= 1 || T <= rows_at_once) return 1;
+    const int64_t rows = ((T + want - 1) / want + rows_at_once - 1) / rows_at_once * rows_at_once;
+    return (T + rows - 1) / rows;
 }
 int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d) {
     const int64_t one = rmsnorm_chunks(ctx, B, T, d, true, 8), other = rmsnorm_chunks(ctx, B, T, d, false, 8);
