@@ -821,6 +821,7 @@ __global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float*
         }
         return;
     }
+    if (SPAN > 1) ptx::cluster_started();
     constexpr int COLS = SPAN > 1 ? 1 : 3, ROWS = SPAN > 1 ? 16 : 6;      // loads of a group: of so many eights of columns, and chunks
     constexpr int STEP = SPAN * WARPS * kGainCols;
     const int64_t b = ((int64_t)blockIdx.x - sums) / SPAN;
@@ -856,6 +857,7 @@ __global__ void __launch_bounds__(kGainThreads) rmsnorm_gain_kernel(const float*
     for (int o = 4; o > 0; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);       // the four quarters hold the same
     if (lane == 0) smem[warp][0] = q;
     __syncthreads();
+    if (SPAN > 1) ptx::cluster_all_started();            // a block without columns comes here before the first one may have started
     if (threadIdx.x == 0) {
         q = 0.f;
 #pragma unroll
