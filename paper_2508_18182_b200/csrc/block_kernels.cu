@@ -113,13 +113,13 @@ __device__ __forceinline__ void store_raw(float* p, int n, const Raw<float>& r) 
 __device__ __forceinline__ void load_gain(const void* gain, int bf16, int col, int n, F2 (&g)[4]) {
     if (n == 8 && (reinterpret_cast<uintptr_t>(gain) & 15u) == 0) {
         if (bf16) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(gain) + col));
+            const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(gain) + col);
             const Raw<__nv_bfloat16> r = {{v.x, v.y, v.z, v.w}};
 #pragma unroll
             for (int i = 0; i < 4; ++i) g[i] = pair_of(r, i);
         } else {
             const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(gain) + col);
-            const float4 a = __ldg(p), b = __ldg(p + 1);
+            const float4 a = p[0], b = p[1];
             g[0] = F2{a.x, a.y}; g[1] = F2{a.z, a.w};
             g[2] = F2{b.x, b.y}; g[3] = F2{b.z, b.w};
         }
@@ -127,7 +127,7 @@ __device__ __forceinline__ void load_gain(const void* gain, int bf16, int col, i
     }
     auto one = [&](int i) {
         if (i >= n) return 0.f;
-        return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(gain)[col + i]) : __ldg(static_cast<const float*>(gain) + col + i);
+        return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(gain)[col + i]) : static_cast<const float*>(gain)[col + i];
     };
 #pragma unroll
     for (int i = 0; i < 4; ++i) g[i] = F2{one(2 * i), one(2 * i + 1)};
@@ -1090,7 +1090,7 @@ __global__ void __launch_bounds__(256, 2) rope_kernel(const __grid_constant__ Ro
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
                     // the phase in units of 2^-64 turns is exact; its top 32 bits, as a signed number, are half turns in [-1, 1)
-                    sine_cosine((int32_t)(((uint64_t)pos * __ldg(a.turns + unit * P + p)) >> 32), sn[p], cs[p], T());
+                    sine_cosine((int32_t)(((uint64_t)pos * a.turns[unit * P + p]) >> 32), sn[p], cs[p], T());
                     cs[p] *= a.magnitude;
                     sn[p] *= a.inverse ? -a.magnitude : a.magnitude;
                 }

@@ -51,7 +51,7 @@ __device__ __forceinline__ void fill_box(const MatArgs& a, uint32_t box, int lan
     if (a.bias) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-            if (col + e < a.N) r[e] = __float_as_uint(__uint_as_float(r[e]) + __ldg(a.bias + col + e));
+            if (col + e < a.N) r[e] = __float_as_uint(__uint_as_float(r[e]) + a.bias[col + e]);
     }
     if (a.out_bf16) {
 #pragma unroll
@@ -163,7 +163,7 @@ __device__ __forceinline__ void fetch_scales(const MatArgs& a, uint32_t ring, Ti
             asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(a.sa + (int64_t)m * a.sa_stride + g * 4) : "memory");
         asm volatile("cp.async.commit_group;" ::: "memory");
         byte[i] = 127u;
-        if (lane < 8 && nb * 128 < a.N && k < a.kb) byte[i] = __ldg(a.sb + nb * a.sb_n + k * a.sb_k);
+        if (lane < 8 && nb * 128 < a.N && k < a.kb) byte[i] = a.sb[nb * a.sb_n + k * a.sb_k];
         shift[i] = (uint32_t)(n0 & 127);                  // rows of the tile's first 128-row block before the tile
         if (++g == groups) { g = 0; walk.next(); }
         fill.advance(kScaleSlots);
@@ -583,7 +583,7 @@ blockscale_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
 // matter.  A block of 128's sum is scaled in fp32 and added up; the warps' sums meet in shared memory in a fixed order.
 constexpr int FR_ROWS = 16, FR_MAX_WARPS = 16, FR_MAX_M = 16;
 __device__ __forceinline__ uint4 bytes16(const uint8_t* row, int k, int K) {      // zeros beyond K
-    if (k + 16 <= K) return __ldg(reinterpret_cast<const uint4*>(row + k));
+    if (k + 16 <= K) return *reinterpret_cast<const uint4*>(row + k);
     uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -623,7 +623,7 @@ __global__ void __launch_bounds__(32 * FR_MAX_WARPS) blockscale_few_kernel(const
     for (int kb = warp; kb < a.kb; kb += warps) {
         uint4 w0[2], w1[2], x[TILES][2];
         uint32_t sa[TILES][2];
-        const uint32_t sbyte = __ldg(sb + kb * a.sb_k);
+        const uint32_t sbyte = sb[kb * a.sb_k];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int k = kb * 128 + h * 64 + t * 16;
@@ -640,7 +640,7 @@ __global__ void __launch_bounds__(32 * FR_MAX_WARPS) blockscale_few_kernel(const
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int m = j * 8 + 2 * t + i;
-                sa[j][i] = m < a.M ? (uint32_t)__ldg(a.sa + (int64_t)m * a.sa_stride + kb) : 127u;
+                sa[j][i] = m < a.M ? (uint32_t)a.sa[(int64_t)m * a.sa_stride + kb] : 127u;
             }
         const float fb = scale_of(sbyte);
 #pragma unroll

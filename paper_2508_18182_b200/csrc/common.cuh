@@ -114,7 +114,8 @@ inline int check_params(const adloco_test_params* p) {
 
 // A launch that may begin while the kernel before it on the stream drains (programmatic dependent launch): the kernel
 // calls after_predecessor() before it touches memory, which waits for that kernel's completion and its writes.  Only for
-// kernels that do.
+// kernels that do, and that take nothing through the non-coherent path (__ldg, __restrict__ on const): it is for data that
+// does not change while the kernel runs, and this one runs while the kernel before it may still write any operand.
 #ifdef __CUDACC__
 __device__ __forceinline__ void after_predecessor() {
     asm volatile("griddepcontrol.wait;" ::: "memory");

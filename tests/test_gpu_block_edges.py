@@ -42,3 +42,50 @@ def test_norms_of_one_long_sample_with_more_blocks_than_columns(ctx, d):
         ctx.add_rmsnorm_backward(dy, h, rstd, gain, dh, per_sample_sqnorm=n[i], grad_sum=S[i] if i % 2 else None)
     torch.cuda.synchronize()
     assert (np64(n) == n_ref).all() and (np64(S[1::2]) == g).all()
+
+
+# ------------------------------------------------------------------------------------ launches that overlap
+@pytest.mark.parametrize("M,N,K", [(1, 2048, 1024), (12, 512, 2048), (40, 300, 512), (2600, 2304, 256)])
+def test_every_operand_may_be_written_by_the_call_before(ctx, M, N, K):
+    """Operands are overwritten in place between products, nothing waits: each product has the values of its turn."""
+    x, w = [whole(i, M, K, top=8) for i in range(4)], [whole(9 + i, N, K, top=8) for i in range(4)]
+    a, sa, b, sb = pitched(M, K, 16), pitched(M, K // 128, 4), pitched(N, K, 16), torch.zeros(-(-N // 128), K // 128, dtype=torch.uint8, device=DEV)
+    bias, zero, out = torch.zeros(1, N, device=DEV), [whole(20 + i, 1, N, top=8) for i in range(4)], torch.zeros(24, M, N, device=DEV)
+    torch.cuda.synchronize()
+    for i in range(24):
+        ctx.blockscale_quantize_weight(w[i % 3], b, sb)
+        ctx.blockscale_quantize(x[i % 4], a, sa)
+        ctx.dropout(zero[i // 6], bias, p=0.0, seed=0)
+        ctx.blockscale_matmul(a, sa, b, sb, out[i], bias=bias[0])
+    torch.cuda.synchronize()
+    for i in range(24):
+        ref = x[i % 4].double() @ w[i % 3].double().t() + zero[i // 6].double()
+        assert torch.equal(out[i].double(), ref), i
+
+
+def test_gain_and_turns_may_be_written_by_the_call_before(ctx):
+    x, gains = whole(1, 64, 256, top=3), [whole(2 + i, 1, 256, top=5) for i in range(3)]
+    gain, out, ones = torch.zeros(1, 256, device=DEV), torch.zeros(30, 64, 256, device=DEV), torch.ones(64, device=DEV)
+    dh = torch.zeros(30, 64, 256, device=DEV)
+    tables, table = [A.RopeTable(64, base=10.0 ** (2 + i)) for i in range(3)], A.RopeTable(64)
+    heads, turned, ref = rnd(5, 1, 8, 2, 64), torch.zeros(30, 1, 8, 2, 64, device=DEV), torch.zeros(3, 1, 8, 2, 64, device=DEV)
+    for i in range(3):
+        ctx.rope([heads], tables[i], outs=[ref[i]])
+    torch.cuda.synchronize()
+    for i in range(30):
+        ctx.dropout(gains[i % 3], gain, p=0.0, seed=0)
+        ctx.add_rmsnorm(x, gain[0], y=out[i], eps=0.5)
+        ctx.dropout(gains[(i + 1) % 3], gain, p=0.0, seed=0)
+        ctx.add_rmsnorm_backward(x, x, ones, gain[0], dh[i])
+    for i in range(30):
+        table.turns.copy_(tables[i % 3].turns)
+        ctx.rope([heads], table, outs=[turned[i]])
+    torch.cuda.synchronize()
+    for i in range(30):
+        r = torch.rsqrt(x.double().square().mean(-1, keepdim=True) + 0.5)
+        assert torch.allclose(out[i].double(), x.double() * r * gains[i % 3].double(), rtol=2.0 ** -19, atol=0)
+        g = gains[(i + 1) % 3].double()
+        u = x.double() * g
+        exact = u - x.double() * (u * x.double()).mean(-1, keepdim=True)
+        assert torch.allclose(dh[i].double(), exact, rtol=2.0 ** -19, atol=2.0 ** -19 * 200)
+        assert torch.equal(turned[i], ref[i % 3])

@@ -43,3 +43,14 @@ def test_no_block_reaches_into_another_one_that_may_not_have_started():
             if "cluster_all_started" in body:
                 assert body.index("cluster_started") < body.index("cluster_all_started"), (f, name)
     assert reaching >= 3
+
+
+def test_kernels_launched_early_read_nothing_through_the_non_coherent_path():
+    """A kernel that starts while the one before it drains may not use loads for data that is constant while it runs."""
+    early = [f for f in CUDA_SOURCES if re.search(r"\blaunch_early\s*\(", _source(f))]
+    assert {"block_kernels.cu", "blockscale_gemm.cu"} <= set(early)
+    for f in early + ["ptx.cuh", "common.cuh"]:
+        assert not re.search(r"__ldg\b|ld\.global(\.\w+)*\.nc|__restrict__", _source(f)), f
+    for f in early:
+        for name, body in _kernels(_source(f)):
+            assert re.search(r"\bafter_predecessor\s*\(\s*\)", body), (f, name)
