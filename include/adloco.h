@@ -357,8 +357,9 @@ int adloco_embedding_sqnorm(adloco_ctx* ctx, const int32_t* token_ids, const voi
  *                 q_scale [rows, ceil(d / 128)] bytes with pitch q_scale_stride (a multiple of 4, q_scale 4-byte aligned)
  *   y             may be NULL when q is given
  *   dropout_p, seed, offset   as in adloco_dropout, element index row * d + column; 0 = none
- * Sums, the root and the norm are formed in fp32 from the unrounded h; every output is rounded
- * once.  1 <= d <= 16384. */
+ * Sums, the root and the norm are formed in fp32 from the unrounded h; every output is rounded to its type
+ * once.  Where x is dropped h is exactly the residual; elsewhere residual + x s takes two fused fp32 operations
+ * with s as the sum of two numbers.  1 <= d <= 16384. */
 typedef struct {
     adloco_dtype dtype, stream_dtype, gain_dtype;
     float eps;
@@ -428,7 +429,7 @@ int adloco_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
  * Moraes, Dror, Shaw 2011) with key = seed and counter = (e / 8, offset), word (e mod 8) / 2, low half
  * first.  The same (p, seed, offset) gives the same mask in every call and in adloco_add_rmsnorm, so the
  * backward pass of dropout is this call on the gradient.  A dropped element is exactly 0 whatever x holds
- * there; p = 1 drops all.
+ * there, and y exactly the residual; p = 1 drops all.  The sum is formed in fp32 as adloco_add_rmsnorm's h.
  *   x, residual, y   dev [rows, cols] in dtype, pitches in elements; y may be the same memory as x or residual
  *   0 <= p <= 1 */
 int adloco_dropout(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride,

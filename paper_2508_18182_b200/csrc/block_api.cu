@@ -13,7 +13,7 @@ bool known(adloco_dtype t) { return t == ADLOCO_F32 || t == ADLOCO_BF16; }
 uintptr_t elem_bytes(adloco_dtype t) { return t == ADLOCO_BF16 ? 2 : 4; }
 bool elem_aligned(const void* p, adloco_dtype t) { return (reinterpret_cast<uintptr_t>(p) & (elem_bytes(t) - 1)) == 0; }
 
-int make_key(double p, uint64_t seed, uint64_t offset, DropoutKey* key) {
+int make_key(double p, uint64_t seed, uint64_t offset, bool residual, DropoutKey* key) {
     if (!(p >= 0.0) || !(p <= 1.0)) return ADLOCO_ERR_INVALID_ARG;
     const uint32_t drop = (uint32_t)std::nearbyint(p * 65536.0);
     uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
@@ -24,11 +24,15 @@ int make_key(double p, uint64_t seed, uint64_t offset, DropoutKey* key) {
     key->off_lo = (uint32_t)offset; key->off_hi = (uint32_t)(offset >> 32);
     key->on = drop != 0;
     if (drop < 65536u) {
-        key->keep = (float)(65536u - drop) * (1.0f / 65536.0f);
-        key->scale = (float)(65536.0 / (65536.0 - (double)drop));
+        const double scale = 65536.0 / (65536.0 - (double)drop);
+        key->scale = key->high = (float)scale;
+        if (residual) {
+            if ((double)key->high > scale) key->high = std::nextafterf(key->high, 0.f);
+            key->low = (float)(scale - (double)key->high);
+        }
     }
     key->limit = (drop & 0xffffu) | (drop << 16);
-    if (drop == 65536u) key->pair = key->low = key->high = 0x4444u;
+    if (drop == 65536u) key->of_pair = key->of_low = key->of_high = 0x4444u;
     return ADLOCO_OK;
 }
 
@@ -73,7 +77,7 @@ int adloco_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args* a, void* stre
         if (rc != ADLOCO_OK) return rc;
     }
     DropoutKey key;
-    rc = make_key(a->dropout_p, a->seed, a->offset, &key);
+    rc = make_key(a->dropout_p, a->seed, a->offset, a->residual != nullptr, &key);
     if (rc != ADLOCO_OK) return rc;
     DeviceGuard g(ctx->device);
     return launch_add_rmsnorm(ctx, *a, key, static_cast<cudaStream_t>(stream));
@@ -105,7 +109,7 @@ int adloco_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
         if (a->workspace_bytes < rmsnorm_backward_workspace(ctx, a->B, a->T, a->d)) return ADLOCO_ERR_WORKSPACE;
     }
     DropoutKey key;
-    rc = make_key(a->dropout_p, a->seed, a->offset, &key);
+    rc = make_key(a->dropout_p, a->seed, a->offset, false, &key);
     if (rc != ADLOCO_OK) return rc;
     DeviceGuard g(ctx->device);
     return launch_add_rmsnorm_backward(ctx, *a, key, static_cast<cudaStream_t>(stream));
@@ -120,7 +124,7 @@ int adloco_dropout(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t co
     if (x_stride < cols || y_stride < cols || (residual && residual_stride < cols)) return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(x, dtype) || !elem_aligned(y, dtype) || !elem_aligned(residual, dtype)) return ADLOCO_ERR_ALIGNMENT;
     DropoutKey key;
-    const int rc = make_key(p, seed, offset, &key);
+    const int rc = make_key(p, seed, offset, residual != nullptr, &key);
     if (rc != ADLOCO_OK) return rc;
     DeviceGuard g(ctx->device);
     return launch_dropout(ctx, dtype == ADLOCO_BF16, rows, cols, x, x_stride, residual, residual_stride, y, y_stride, key,

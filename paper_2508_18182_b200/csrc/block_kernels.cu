@@ -187,19 +187,24 @@ __device__ __forceinline__ uint32_t spread(uint32_t v, uint32_t selector) {
 // a dropped element is 0 whatever it held
 __device__ __forceinline__ void drop_raw(Raw<__nv_bfloat16>& v, const Kept& m, const DropoutKey& k) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v.w[i] &= spread(m.w[i], k.pair);
+    for (int i = 0; i < 4; ++i) v.w[i] &= spread(m.w[i], k.of_pair);
 }
 __device__ __forceinline__ void drop_raw(Raw<float>& v, const Kept& m, const DropoutKey& k) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        v.w[2 * i] &= spread(m.w[i], k.low);
-        v.w[2 * i + 1] &= spread(m.w[i], k.high);
+        v.w[2 * i] &= spread(m.w[i], k.of_low);
+        v.w[2 * i + 1] &= spread(m.w[i], k.of_high);
     }
 }
 
-// x / keep + r as (x + r keep) / keep: keep has 16 bits and is exact, so where the residual cancels the branch the sum
-// still is as good as its inputs
-__device__ __forceinline__ F2 scaled(F2 x, const DropoutKey& k, F2 r) { return mul2(fma2(r, both(k.keep), x), both(k.scale)); }
+// r + x scale by two fused operations, the scale's high part first: exactly r where x was dropped, and as good as its inputs
+// where the residual cancels the branch, since what is rounded is then small already.  (The low part first would be lost in
+// r; r + x scale with a rounded scale loses as much.)  low = 0 is left out: times an Inf it would give NaN.
+__device__ __forceinline__ F2 scaled(F2 x, const DropoutKey& k, F2 r) {
+    F2 v = fma2(x, both(k.high), r);
+    if (k.low != 0.f) v = fma2(x, both(k.low), v);
+    return v;
+}
 
 // n / d for n < 2^31 by a multiplication: with s = ceil(log2 d) and m = ceil(2^(31 + s) / d), the error of m d is
 // below d <= 2^s, and n times it below 2^(31 + s)

@@ -245,11 +245,12 @@ struct DropoutKey {
     uint32_t round[20] = {0};           // of round r: [2 r], [2 r + 1]
     uint32_t off_lo = 0, off_hi = 0;
     uint32_t on = 0;                    // any element is dropped at all
-    float keep = 1.f, scale = 1.f;      // the share that stays (exact), and 1 / keep; both 1 where none is dropped, or all are
+    float scale = 1.f;                  // 1 over the share that stays; 1 where none is dropped, or all are
+    float high = 1.f, low = 0.f;        // the same beside a residual: the sum of two numbers, the first rounded down (low >= 0)
     // two 16-bit numbers are compared with the drop threshold at a time: the threshold in both halves, and the byte
-    // selectors that spread a half's top bit over that half (pair), or over 32 bits (low, high); they select zero
-    // bytes when all are dropped
-    uint32_t limit = 0, pair = 0xBB99u, low = 0x9999u, high = 0xBBBBu;
+    // selectors that spread a half's top bit over that half (of_pair), or over 32 bits (of_low, of_high); they select
+    // zero bytes when all are dropped
+    uint32_t limit = 0, of_pair = 0xBB99u, of_low = 0x9999u, of_high = 0xBBBBu;
 };
 int launch_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const DropoutKey& key, cudaStream_t st);
 int64_t rmsnorm_backward_workspace(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d);

@@ -89,3 +89,44 @@ def test_gain_and_turns_may_be_written_by_the_call_before(ctx):
         exact = u - x.double() * (u * x.double()).mean(-1, keepdim=True)
         assert torch.allclose(dh[i].double(), exact, rtol=2.0 ** -19, atol=2.0 ** -19 * 200)
         assert torch.equal(turned[i], ref[i % 3])
+
+# --------------------------------------------------------------------------------- residual beside dropout
+@pytest.mark.parametrize("p", [0.0, 0.05, 0.1, 0.25, 0.3, 0.5, 0.999, 1.0])
+@pytest.mark.parametrize("xt", [F32, BF])
+def test_residual_is_returned_as_it_is_where_the_branch_is_dropped(ctx, p, xt):
+    """An fp32 residual: bit for bit where the mask drops; elsewhere r + x s is formed by two fused operations with s held as
+    a sum of two fp32 numbers, so it is off by the rounding of either (2^-24 of the result, nearly) and by 2^-45 of x s.
+    Inf and NaN count where they are kept and nowhere else."""
+    rows, d = 50, 1000
+    mask = (p, 77, 5)
+    x, r = rnd(1, rows, d, dtype=xt, std=2.0), rnd(2, rows, d, std=0.7)
+    kept = O.keep_mask(rows * d, *mask).reshape(rows, d)
+    s = 65536 / max(65536 - round(p * 65536), 1)
+    near = torch.tensor(kept, device=DEV) & (rnd(3, rows, d) > 0)           # the residual cancels the branch, nearly
+    r[near] = (x.double() * -s * (1 + 2.0 ** -18 * rnd(4, rows, d).double())).float()[near]
+    x[0, ::3], x[1, ::3], x[2, ::3] = float("inf"), float("-inf"), float("nan")
+    r[3, ::5], r[4, ::5] = float("inf"), float("-inf")
+    x[5], r[5] = 1e38, -3e38                                                # x s may lie outside fp32, the sum does not
+    gain, out, h, y = torch.ones(d, device=DEV), torch.empty(rows, d, device=DEV), torch.empty(rows, d, device=DEV), torch.empty_like(x)
+    ctx.add_rmsnorm(x, gain, residual=r, h=h, y=y, dropout=mask)
+    results = [h]
+    if xt == F32:
+        ctx.dropout(x, out, p=p, seed=77, offset=5, residual=r)
+        wide = torch.zeros(rows, d + 3, device=DEV)[:, :d]                 # rows off the 16-byte grid: element by element
+        ctx.dropout(x, wide, p=p, seed=77, offset=5, residual=r)
+        off = torch.zeros(rows, d + 3, device=DEV)[:, 1:d + 1]
+        ctx.add_rmsnorm(x, gain, residual=r, h=off, y=y, dropout=mask)
+        results += [out, wide, off]
+    torch.cuda.synchronize()
+    dropped = torch.tensor(~kept, device=DEV)
+    x64, r64 = np64(x), np64(r)
+    with np.errstate(all="ignore"):
+        ref = r64 + np.where(kept, x64 * s, 0.0)
+        ref = np.where(np.abs(ref) > 3.4028235677973366e38, np.sign(ref) * np.inf, ref)
+    finite = np.isfinite(ref)
+    tol = (2.0 ** -23 * np.abs(ref) + 2.0 ** -45 * s * np.where(kept, np.abs(x64), 0.0)) * (1 + 2.0 ** -20) + 2.0 ** -149
+    for got in results:
+        assert torch.equal(got[dropped], r[dropped])
+        g = np64(got)
+        assert np.array_equal(g[~finite], ref[~finite], equal_nan=True)
+        assert (np.abs(g - ref)[finite] <= tol[finite]).all()
