@@ -453,7 +453,7 @@ int adloco_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, doubl
 /* One tensor of heads [B, T, heads, head_dim] with strides in elements (head_dim contiguous). */
 typedef struct {
     const void* in;
-    void* out;         /* the same memory and strides as `in`, or no overlap */
+    void* out;         /* the same memory and strides as `in`, or no overlap; its heads must not fall on one another */
     int64_t heads;
     int64_t in_batch, in_token, in_head;
     int64_t out_batch, out_token, out_head;

@@ -1,4 +1,5 @@
 // C ABI of the operators between the linear layers: argument checks and dispatch.
+#include <algorithm>
 #include <cmath>
 
 #include "common.cuh"
@@ -53,6 +54,53 @@ int check_row_scales(const void* s, int64_t stride, int64_t cols) {
     if (stride < (cols + 127) / 128) return ADLOCO_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(s) & 3u) != 0 || (stride & 3) != 0) return ADLOCO_ERR_ALIGNMENT;
     return ADLOCO_OK;
+}
+
+// Do runs of `width` elements at i s[0] + j s[1] + k s[2], i < n[0], j < n[1], k < n[2], fall on one another?  Strides that
+// nest (each one spans what the smaller ones reach) do not.  Otherwise two runs meet exactly when a difference
+// i s[0] + j s[1] + k s[2], not all of i, j, k zero, is less than the width; the smallest stride's k follows from i and j.  A
+// layout that takes more than kSteps of them to decide counts as falling on itself.
+bool fall_on_one_another(const int64_t (&extents)[3], const int64_t (&strides)[3], int64_t width) {
+    constexpr int64_t kSteps = 1 << 20;
+    typedef __int128 wide;
+    struct Dim { int64_t n; wide s; } d[3];
+    for (int i = 0; i < 3; ++i) d[i] = Dim{extents[i], extents[i] > 1 ? (wide)strides[i] : 0};
+    std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.s > b.s; });
+    bool nested = true;
+    wide reach = width;
+    for (int i = 2; i >= 0; --i) {
+        if (d[i].n > 1 && d[i].s < reach) nested = false;
+        reach += d[i].s * (d[i].n - 1);
+    }
+    if (nested) return false;
+    const wide most_k = d[2].s * (d[2].n - 1), most_j = d[1].s * (d[1].n - 1);
+    int64_t steps = 0;
+    for (int64_t i = 0; i < d[0].n && i * d[0].s < most_j + most_k + width; ++i) {
+        if (++steps > kSteps) return true;
+        const wide at = i * d[0].s;
+        // j with |at + j s| < most_k + width, both signs of j where i is zero being the same
+        int64_t j = 0, last = d[1].n - 1;
+        if (d[1].s > 0) {
+            const wide low = -((at + most_k + width) / d[1].s), high = (most_k + width - at) / d[1].s;
+            j = (int64_t)std::max<wide>(i ? low : 0, -(wide)(d[1].n - 1));
+            last = (int64_t)std::min<wide>(high, d[1].n - 1);
+        } else if (d[1].n > 1) {
+            return true;                                     // a stride of zero
+        }
+        for (; j <= last; ++j) {
+            if (++steps > kSteps) return true;
+            const wide off = at + j * d[1].s, far = off < 0 ? -off : off;
+            int64_t k = 0;
+            if (d[2].n > 1) {
+                if (d[2].s == 0) return true;
+                k = (int64_t)std::min<wide>(far / d[2].s, d[2].n - 1);
+            }
+            const wide here = far - k * d[2].s, next = k + 1 < d[2].n ? (k + 1) * d[2].s - far : (wide)width;
+            const bool same = i == 0 && j == 0;              // k = 0 is the run itself
+            if ((!(same && k == 0) && here < width) || (next >= 0 && next < width)) return true;
+        }
+    }
+    return false;
 }
 
 }  // namespace
@@ -173,10 +221,8 @@ int adloco_rope(adloco_ctx* ctx, adloco_dtype dtype, const adloco_rope_tensor* t
         if (!t.in || !t.out || t.heads < 1) return ADLOCO_ERR_INVALID_ARG;
         if (t.in_batch < 0 || t.in_token < 0 || t.in_head < 0 || t.out_batch < 0 || t.out_token < 0 || t.out_head < 0)
             return ADLOCO_ERR_INVALID_ARG;
-        // the outputs of one tensor must not fall on one another
-        if ((B > 1 && t.out_batch < head_dim) || (T > 1 && t.out_token < head_dim) || (t.heads > 1 && t.out_head < head_dim))
-            return ADLOCO_ERR_INVALID_ARG;
         if (t.heads > 65536) return ADLOCO_ERR_UNSUPPORTED;
+        if (fall_on_one_another({B, T, t.heads}, {t.out_batch, t.out_token, t.out_head}, head_dim)) return ADLOCO_ERR_INVALID_ARG;
         if (!elem_aligned(t.in, dtype) || !elem_aligned(t.out, dtype)) return ADLOCO_ERR_ALIGNMENT;
         heads += t.heads;
     }

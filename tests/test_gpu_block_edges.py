@@ -130,3 +130,38 @@ def test_residual_is_returned_as_it_is_where_the_branch_is_dropped(ctx, p, xt):
         g = np64(got)
         assert np.array_equal(g[~finite], ref[~finite], equal_nan=True)
         assert (np.abs(g - ref)[finite] <= tol[finite]).all()
+
+# ------------------------------------------------------------------------------------------------- rotary
+def test_rope_refuses_outputs_that_fall_on_one_another(ctx):
+    t = A.RopeTable(64)
+    x = rnd(1, 3, 4, 5, 64)
+    flat = torch.empty(1 << 16, device=DEV)
+    before = ctx.launch_count
+    # strides of sample, token and head in heads of 64
+    for b, n, h in ((100, 1, 1), (100, 4, 1), (100, 1, 3), (8, 5, 1), (12, 3, 10), (61, 6, 2), (0, 5, 1)):
+        with pytest.raises(A.AdlocoError) as e:
+            ctx.rope([x], t, outs=[flat.as_strided(x.shape, (b * 64, n * 64, h * 64, 1))])
+        assert e.value.status == A.ERR_INVALID_ARG, (b, n, h)
+    with pytest.raises(A.AdlocoError) as e:                     # heads of which two share their last and first element
+        ctx.rope([x], t, outs=[flat.as_strided(x.shape, (2000, 320, 63, 1))])
+    assert e.value.status == A.ERR_INVALID_ARG and ctx.launch_count == before
+
+
+@pytest.mark.parametrize("b,n,h", [(20, 5, 1), (5, 15, 1), (4, 1, 12), (1, 3, 12), (1, 15, 3), (60, 3, 13), (7, 21, 4), (24, 6, 25), (1, 6, 15), (1, 9, 12)])
+def test_rope_writes_wherever_the_outputs_lie_apart(ctx, b, n, h):
+    """Any order of the dimensions, also strides that do not nest."""
+    shape = (3, 4, 5, 64)
+    places = {b * i + n * j + h * k for i in range(3) for j in range(4) for k in range(5)}
+    assert len(places) == 60
+    t = A.RopeTable(64)
+    x = rnd(1, *shape)
+    dense = torch.empty_like(x)
+    ctx.rope([x], t, outs=[dense])
+    flat = torch.full((1 << 14,), 7.0, device=DEV)
+    out = flat.as_strided(shape, (b * 64, n * 64, h * 64, 1))
+    ctx.rope([x], t, outs=[out])
+    torch.cuda.synchronize()
+    assert torch.equal(out, dense)
+    rest = torch.ones(256, dtype=torch.bool, device=DEV)
+    rest[torch.tensor(sorted(places), device=DEV)] = False
+    assert (flat.view(256, 64)[rest] == 7).all()
