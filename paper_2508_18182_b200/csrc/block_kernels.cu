@@ -109,26 +109,37 @@ __device__ __forceinline__ void store_raw(float* p, int n, const Raw<float>& r) 
             if (i < n) p[i] = __uint_as_float(r.w[i]);
     }
 }
-// the gain is read by every row: it stays in L1
+// The gain is read by every row: it stays in L1.  FREE loads may move across the memory clobbers of the copies and stores
+// around them, down to the next settled(); others stay in their place.  Kernels on an fp32 stream take the first, whose one or
+// two blocks an SM hide little (norm backward of 32768 x 768, bf16 on fp32: 107 us, 126 in their place), those on a bf16
+// stream the second, which leave the registers for one block more (98304 x 64: 17.7 us, 20.2 with free ones; 1216 x 5120:
+// 32 and 35).
+template <bool FREE>
+__device__ __forceinline__ uint4 gain16(const void* p) {
+    if (!FREE) return *static_cast<const uint4*>(p);
+    uint4 v;
+    asm("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(__cvta_generic_to_global(p)));
+    return v;
+}
+template <bool FREE>
 __device__ __forceinline__ void load_gain(const void* gain, int bf16, int col, int n, F2 (&g)[4]) {
+    const __nv_bfloat16* half = static_cast<const __nv_bfloat16*>(gain) + col;
+    const float* full = static_cast<const float*>(gain) + col;
     if (n == 8 && (reinterpret_cast<uintptr_t>(gain) & 15u) == 0) {
         if (bf16) {
-            const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(gain) + col);
+            const uint4 v = gain16<FREE>(half);
             const Raw<__nv_bfloat16> r = {{v.x, v.y, v.z, v.w}};
 #pragma unroll
             for (int i = 0; i < 4; ++i) g[i] = pair_of(r, i);
         } else {
-            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(gain) + col);
-            const float4 a = p[0], b = p[1];
-            g[0] = F2{a.x, a.y}; g[1] = F2{a.z, a.w};
-            g[2] = F2{b.x, b.y}; g[3] = F2{b.z, b.w};
+            const uint4 a = gain16<FREE>(full), b = gain16<FREE>(full + 4);
+            const Raw<float> r = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[i] = pair_of(r, i);
         }
         return;
     }
-    auto one = [&](int i) {
-        if (i >= n) return 0.f;
-        return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(gain)[col + i]) : static_cast<const float*>(gain)[col + i];
-    };
+    auto one = [&](int i) { return i >= n ? 0.f : bf16 ? __bfloat162float(half[i]) : full[i]; };
 #pragma unroll
     for (int i = 0; i < 4; ++i) g[i] = F2{one(2 * i), one(2 * i + 1)};
 }
@@ -446,6 +457,8 @@ template <typename XT, typename ST, int TPR, int C, bool VEC>
 __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __grid_constant__ adloco_rmsnorm_args a,
                                                                         const __grid_constant__ DropoutKey key) {
     after_predecessor();
+    constexpr bool FREE = sizeof(ST) == 4;
+    const void* gain = FREE ? settled(a.gain) : a.gain;
     constexpr int THREADS = row_threads(TPR), ROWS = THREADS / TPR;
     extern __shared__ __align__(16) uint8_t row_buffers[];                  // !VEC: x, then the residual, of ROWS rows
     __shared__ float smem[2 * THREADS / 32];
@@ -515,7 +528,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) add_rmsnorm_kernel(const __g
         F2 g[4];
         Raw<XT> out;
         if (n > 0) {
-            load_gain(a.gain, a.gain_dtype == ADLOCO_BF16, col, n, g);
+            load_gain<FREE>(gain, a.gain_dtype == ADLOCO_BF16, col, n, g);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 g[i] = mul2(mul2(h[c][i], both(rstd)), g[i]);
@@ -600,7 +613,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
     constexpr uint32_t STEP = THREADS * 16;                 // piece i of thread t at i * STEP + 16 t: free of bank conflicts
     constexpr int XP = (int)sizeof(XT) / 2, SP = (int)sizeof(ST) / 2, PIECES = C * (XP + 2 * SP);
     constexpr int DEPTH = stage_depth<XT, ST, C, THREADS>();
-    constexpr bool STAGED = VEC && DEPTH > 1;
+    constexpr bool STAGED = VEC && DEPTH > 1, FREE = sizeof(ST) == 4;
     const adloco_rmsnorm_backward_args& a = p.a;
     extern __shared__ __align__(16) float columns[];        // staged rows, or (!VEC) dy, h and the stream's gradient of ROWS rows;
                                                             // at the end [ROWS][d] (GAIN and ROWS > 1)
@@ -698,6 +711,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
         };
         // The row is gone through twice, before and after its sum, from shared memory: holding gain dy and xhat in registers in
         // between left two blocks an SM instead of three.  (Rows too wide for two stages are read from global memory twice.)
+        const void* gain = FREE ? settled(a.gain) : a.gain;
         F2 dot = both(0.f);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -706,7 +720,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
             const Raw<XT> ur = dy_of(c, col);
             const Raw<ST> vr = h_of(c, col);
             F2 g[4];
-            load_gain(a.gain, a.gain_dtype == ADLOCO_BF16, col, min(8, d - col), g);
+            load_gain<FREE>(gain, a.gain_dtype == ADLOCO_BF16, col, min(8, d - col), g);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const F2 u = pair_of(ur, i), v = mul2(pair_of(vr, i), both(rstd));      // dy, xhat
@@ -716,6 +730,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
         }
         const float m = row_sum<TPR, THREADS>(dot.x + dot.y, smem, turn) * inv_d;
         const float m_rstd = -m * rstd;
+        if (FREE) gain = settled(a.gain);
         if (there) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
@@ -727,7 +742,7 @@ __global__ void __launch_bounds__(row_threads(TPR)) rmsnorm_backward_kernel(cons
                 if (a.dh_residual)
                     r = STAGED ? staged<ST>(from + (C * XP + C * SP + c * SP) * STEP, STEP) : VEC ? load_raw<true>(res + col, 8) : from_buffer<ST>(r_buf, r_skew, col);
                 F2 g[4], o[4];
-                load_gain(a.gain, a.gain_dtype == ADLOCO_BF16, col, min(8, d - col), g);
+                load_gain<FREE>(gain, a.gain_dtype == ADLOCO_BF16, col, min(8, d - col), g);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     o[i] = fma2(fma2(pair_of(vr, i), both(m_rstd), mul2(pair_of(ur, i), g[i])), both(rstd), pair_of(r, i));

@@ -121,6 +121,13 @@ __device__ __forceinline__ void after_predecessor() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
+// An operand's address, not known to the compiler before after_predecessor() is through: loads that it may move as it likes
+// (asm without volatile) stay behind the wait when they go by this address.
+template <typename T>
+__device__ __forceinline__ T* settled(T* p) {
+    asm volatile("" : "+l"(p));
+    return p;
+}
 template <typename... Params, typename... Args>
 inline cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, unsigned cluster,
                                 const Args&... args) {
