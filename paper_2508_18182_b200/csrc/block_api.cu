@@ -222,6 +222,10 @@ int adloco_rope(adloco_ctx* ctx, adloco_dtype dtype, const adloco_rope_tensor* t
         if (t.in_batch < 0 || t.in_token < 0 || t.in_head < 0 || t.out_batch < 0 || t.out_token < 0 || t.out_head < 0)
             return ADLOCO_ERR_INVALID_ARG;
         if (t.heads > 65536) return ADLOCO_ERR_UNSUPPORTED;
+        // in place: the same strides, those of extents of one aside
+        if (t.in == t.out && ((B > 1 && t.in_batch != t.out_batch) || (T > 1 && t.in_token != t.out_token) ||
+                              (t.heads > 1 && t.in_head != t.out_head)))
+            return ADLOCO_ERR_INVALID_ARG;
         if (fall_on_one_another({B, T, t.heads}, {t.out_batch, t.out_token, t.out_head}, head_dim)) return ADLOCO_ERR_INVALID_ARG;
         if (!elem_aligned(t.in, dtype) || !elem_aligned(t.out, dtype)) return ADLOCO_ERR_ALIGNMENT;
         heads += t.heads;

@@ -165,3 +165,21 @@ def test_rope_writes_wherever_the_outputs_lie_apart(ctx, b, n, h):
     rest = torch.ones(256, dtype=torch.bool, device=DEV)
     rest[torch.tensor(sorted(places), device=DEV)] = False
     assert (flat.view(256, 64)[rest] == 7).all()
+
+
+def test_rope_in_place_needs_the_strides_of_the_input(ctx):
+    """The same memory in another order is neither in place nor apart."""
+    t = A.RopeTable(32)
+    buf = rnd(1, 2, 6, 4, 64)
+    kept, before = buf.clone(), ctx.launch_count
+    for out in (buf.view(2, 4, 6, 64).transpose(1, 2), buf.view(-1).as_strided(buf.shape, (64, 512, 128, 1))):
+        with pytest.raises(A.AdlocoError) as e:
+            ctx.rope([buf], t, outs=[out])
+        assert e.value.status == A.ERR_INVALID_ARG
+    assert ctx.launch_count == before and torch.equal(buf, kept)
+    # strides of extents of one are not looked at
+    one, ref = rnd(2, 1, 1, 4, 64), torch.empty(1, 1, 4, 64, device=DEV)
+    ctx.rope([one], t, outs=[ref], first_position=9)
+    ctx.rope([one], t, outs=[one.as_strided((1, 1, 4, 64), (7, 9, 64, 1))], first_position=9)
+    torch.cuda.synchronize()
+    assert torch.equal(one, ref)
