@@ -198,6 +198,7 @@ int adloco_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, doubl
         }
         double t = w / two_pi;                                  // whole turns a position do not matter
         t -= std::floor(t);
+        if (!std::isfinite(t)) return ADLOCO_ERR_INVALID_ARG;   // a base or a factor that takes the frequency out of range
         const double units = std::nearbyint(t * 18446744073709551616.0);
         turns_host[j] = units >= 18446744073709551616.0 ? 0u : (uint64_t)units;
     }

@@ -108,3 +108,12 @@ def test_eight_bit_numbers():
     q, e = O.quantise(x, 1)
     assert e.shape == (5, 3) and np.abs(O.widen(q, e, 1) - x).max() <= 2.0 ** -4 * np.abs(x).max()
     assert np.all(np.abs(O.widen(q, e, 1) - x) <= 2.0 ** -4 * np.abs(x) + 2.0 ** -10 * np.repeat(2.0 ** e, 128, 1)[:, :300])
+
+
+@pytest.mark.parametrize("rot_dim,kw", [(4, dict(base=1.0, scaling="ntk", factor=1e-200)), (8, dict(scaling="linear", factor=1e-320)),
+                                        (8, dict(scaling="by_parts", factor=1e-320, context=1.0, low=10.0, high=20.0))])
+def test_frequencies_that_leave_the_range_of_numbers_are_refused(rot_dim, kw):
+    with pytest.raises(A.AdlocoError) as e:
+        A.RopeTable(rot_dim, device="cpu", **kw)
+    assert e.value.status == A.ERR_INVALID_ARG
+    A.RopeTable(rot_dim, device="cpu", **{**kw, "factor": 4.0})
