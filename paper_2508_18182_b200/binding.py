@@ -6,6 +6,7 @@ not built or no CUDA device is present, loading or the first call fails.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 
@@ -169,8 +170,6 @@ class Context:
 
     def __init__(self, device: int = 0):
         self.lib = load_library()
-        from . import _tensor_calls as calls        # marshalling of the operators between the linear layers
-        self.calls = calls
         h = C.c_void_p()
         rc = self.lib.adloco_create(C.byref(h), int(device))
         if rc != OK:
@@ -181,6 +180,17 @@ class Context:
         self._res_dev = torch.zeros(TestResult_size(), dtype=torch.uint8, device=self.device)
         self._res_host = torch.zeros(TestResult_size(), dtype=torch.uint8).pin_memory()
         self._sums_dev = torch.zeros(C.sizeof(TestSums), dtype=torch.uint8, device=self.device)
+
+    @functools.cached_property
+    def calls(self):
+        """The marshalling of the operators between the linear layers (tensor_calls.cpp): loaded by the first of them, nothing
+        else needs it.  There is no fallback either."""
+        try:
+            from . import _tensor_calls
+        except ImportError as e:
+            raise ImportError("the operators between the linear layers need _tensor_calls.so, built against this torch: run "
+                              f"`python -m paper_2508_18182_b200.build` ({e})") from e
+        return _tensor_calls
 
     def close(self):
         if getattr(self, "h", None):

@@ -36,7 +36,14 @@ def _build_calls(force: bool, verbose: bool) -> None:
     if not force and not _older(CALLS, [source, os.path.join(CSRC, HEADERS[-1]), os.path.abspath(__file__)]):
         return
     import sysconfig
-    import torch
+    try:
+        import torch
+    except ImportError:
+        torch = None
+    if torch is None or torch.version.cuda is None:
+        # the library needs nvcc alone, and all but the operators between the linear layers is reached without the module
+        sys.stderr.write("_tensor_calls.so is not built: it needs torch with CUDA\n")
+        return
     root = os.path.dirname(torch.__file__)
     includes = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                 sysconfig.get_paths()["include"], os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")]
@@ -52,7 +59,8 @@ def _build_calls(force: bool, verbose: bool) -> None:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles every .cu of the library into paper_2508_18182_b200/libadloco.so, and the marshalling module."""
+    """Compiles every .cu of the library into paper_2508_18182_b200/libadloco.so, and the marshalling module where torch
+    has CUDA."""
     if not force and not _stale():
         _build_calls(force, verbose)
         return LIB
