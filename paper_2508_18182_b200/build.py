@@ -32,9 +32,6 @@ def _stale() -> bool:
 
 
 def _build_calls(force: bool, verbose: bool) -> None:
-    source = os.path.join(CSRC, "tensor_calls.cpp")
-    if not force and not _older(CALLS, [source, os.path.join(CSRC, HEADERS[-1]), os.path.abspath(__file__)]):
-        return
     import sysconfig
     try:
         import torch
@@ -44,6 +41,13 @@ def _build_calls(force: bool, verbose: bool) -> None:
         # the library needs nvcc alone, and all but the operators between the linear layers is reached without the module
         sys.stderr.write("_tensor_calls.so is not built: it needs torch with CUDA\n")
         return
+    source = os.path.join(CSRC, "tensor_calls.cpp")
+    # it is good for one torch and one Python: which ones it was compiled against stands beside it
+    stamp = os.path.splitext(CALLS)[0] + ".stamp"
+    against = f"torch {torch.__version__}, Python {sys.version_info.major}.{sys.version_info.minor}\n"
+    if not force and not _older(CALLS, [source, os.path.join(CSRC, HEADERS[-1]), os.path.abspath(__file__)]):
+        if os.path.exists(stamp) and open(stamp).read() == against:
+            return
     root = os.path.dirname(torch.__file__)
     includes = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                 sysconfig.get_paths()["include"], os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")]
@@ -56,6 +60,8 @@ def _build_calls(force: bool, verbose: bool) -> None:
         sys.stderr.write(res.stdout + res.stderr)
     if res.returncode != 0:
         raise RuntimeError("building _tensor_calls.so failed")
+    with open(stamp, "w") as f:
+        f.write(against)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -47,3 +47,23 @@ def test_torch_without_cuda_does_not_fail_the_build(monkeypatch, tmp_path, capsy
     monkeypatch.setattr(subprocess, "run", lambda *a, **k: pytest.fail("nothing to compile"))
     assert B.build() == B.LIB
     assert "torch with CUDA" in capsys.readouterr().err
+
+
+def test_the_module_is_rebuilt_for_another_torch(monkeypatch, tmp_path):
+    """Its age says nothing about the torch it was compiled against; a stamp beside it does."""
+    built = []
+
+    def compiler(cmd, **kw):
+        built.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+        return subprocess.CompletedProcess(cmd, 0, "", "")
+    monkeypatch.setattr(B, "CALLS", str(tmp_path / "_tensor_calls.so"))
+    monkeypatch.setattr(B, "_stale", lambda: False)
+    monkeypatch.setattr(subprocess, "run", compiler)
+    B.build()
+    B.build()
+    assert len(built) == 1
+    monkeypatch.setattr(torch, "__version__", "0.0.1+other")
+    B.build()
+    B.build()
+    assert len(built) == 2
