@@ -373,13 +373,14 @@ class Context:
 
     def add_rmsnorm_backward(self, dy, h, rstd, gain, dh, *, dh_residual=None, dx=None, dropout=None, per_sample_sqnorm=None,
                              accumulate_norms=False, grad_sum=None, accumulate_sum=False, workspace=None, stream=None):
-        """adloco_add_rmsnorm_backward on dy [B, T, d] (or [rows, d]: one sample): dh, and dx where given, are the
+        """adloco_add_rmsnorm_backward on dy [B, T, d] (any other shape [..., d] is one sample): dh, and dx where given, are the
         gradients of the residual and of x; per_sample_sqnorm and grad_sum are the gain's.  workspace: a uint8
         tensor of rmsnorm_backward_workspace(B, T, d) bytes; without one it comes from torch's allocator."""
-        if workspace is None and stream is not None and not (per_sample_sqnorm is None and grad_sum is None):
+        if (workspace is None and stream is not None and not (per_sample_sqnorm is None and grad_sum is None)
+                and isinstance(dy, torch.Tensor) and dy.numel() > 0 and dy.dim() > 0):      # others are refused by the call
+            B, d = dy.shape[0] if dy.dim() == 3 else 1, dy.shape[-1]
             with torch.cuda.stream(stream):
-                workspace = torch.empty(self.rmsnorm_backward_workspace(*(dy.shape if dy.dim() == 3 else (1, *dy.shape))),
-                                        dtype=torch.uint8, device=self.device)
+                workspace = torch.empty(self.rmsnorm_backward_workspace(B, dy.numel() // (B * d), d), dtype=torch.uint8, device=self.device)
         rc = self.calls.add_rmsnorm_backward(self.h.value, self.device.index, dy, h, rstd, gain, dh, dh_residual, dx, dropout,
                                              per_sample_sqnorm, accumulate_norms, grad_sum, accumulate_sum, workspace, stream)
         if rc != OK:

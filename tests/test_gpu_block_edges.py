@@ -183,3 +183,26 @@ def test_rope_in_place_needs_the_strides_of_the_input(ctx):
     ctx.rope([one], t, outs=[one.as_strided((1, 1, 4, 64), (7, 9, 64, 1))], first_position=9)
     torch.cuda.synchronize()
     assert torch.equal(one, ref)
+
+# --------------------------------------------------------------------------------------------- the binding
+@pytest.mark.parametrize("shape", [(96,), (7, 96), (3, 7, 96), (2, 5, 3, 96)])
+def test_norm_backward_takes_its_workspace_for_any_shape_and_stream(ctx, shape):
+    """A tensor of three dimensions is samples of rows; any other one is one sample.  With a stream and without."""
+    dy, h, gain = rnd(1, *shape), rnd(2, *shape), rnd(3, 96)
+    rstd = torch.rsqrt(h.square().mean(-1) + 1e-6)
+    B = shape[0] if len(shape) == 3 else 1
+    args = [np64(v).reshape(B, -1, 96) for v in (dy, h)] + [np64(rstd).reshape(B, -1), np64(gain)]
+    dh_ref, _, n_ref, S_ref = O.add_rmsnorm_backward(*args)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (None, side):
+        dh, n, S = torch.zeros_like(h), torch.zeros(B, device=DEV), torch.zeros(96, device=DEV)
+        torch.cuda.synchronize()
+        ctx.add_rmsnorm_backward(dy, h, rstd, gain, dh, per_sample_sqnorm=n, grad_sum=S, stream=stream)
+        torch.cuda.synchronize()
+        assert np.allclose(np64(dh), dh_ref.reshape(shape), rtol=1e-4, atol=1e-5) and np.allclose(np64(n), n_ref, rtol=1e-4)
+        assert np.allclose(np64(S), S_ref, rtol=1e-4, atol=1e-4)
+    for bad in (dy.reshape(-1)[0], None, dy.cpu(), dy[..., :0]):
+        with pytest.raises(A.AdlocoError) as e:
+            ctx.add_rmsnorm_backward(bad, h, rstd, gain, dh, grad_sum=S, stream=side)
+        assert e.value.status == A.ERR_INVALID_ARG
