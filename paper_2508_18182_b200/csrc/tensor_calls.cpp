@@ -112,6 +112,11 @@ double real(PyObject* o) {
     if (v == -1.0 && PyErr_Occurred()) { PyErr_Clear(); refuse(ADLOCO_ERR_INVALID_ARG, "expected a number"); }
     return v;
 }
+bool truth(PyObject* o, const char* what) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) { PyErr_Clear(); refuse(ADLOCO_ERR_INVALID_ARG, std::string(what) + ": expected True or False"); }
+    return v != 0;
+}
 struct Mask {
     double p = 0.0;
     uint64_t seed = 0, offset = 0;
@@ -204,9 +209,9 @@ int add_rmsnorm_backward(PyObject* const* v) {
     const Mask m = mask_of(v[9]);
     a.dropout_p = m.p; a.seed = m.seed; a.offset = m.offset;
     a.per_sample_sqnorm = static_cast<float*>(vector(tensor(v[10], "per_sample_sqnorm", true), "per_sample_sqnorm", a.B, at::kFloat, dev));
-    a.accumulate_norms = PyObject_IsTrue(v[11]);
+    a.accumulate_norms = truth(v[11], "accumulate_norms");
     a.grad_sum = static_cast<float*>(vector(tensor(v[12], "grad_sum", true), "grad_sum", a.d, at::kFloat, dev));
-    a.accumulate_sum = PyObject_IsTrue(v[13]);
+    a.accumulate_sum = truth(v[13], "accumulate_sum");
     at::Tensor own;                                    // from torch's allocator, on the current stream
     if (a.per_sample_sqnorm || a.grad_sum) {
         const at::Tensor* ws = tensor(v[14], "workspace", true);
@@ -269,7 +274,7 @@ int rope(PyObject* const* v) {
     on(turns, "the table", dev);
     return adloco_rope(handle(v[0]), code(x, "tensors"), t, (int32_t)n, B, T, D, whole(v[5]), static_cast<const uint64_t*>(turns.data_ptr()),
                        (float)real(v[6]), pos ? static_cast<const int32_t*>(pos->data_ptr()) : nullptr, pitch, whole(v[8]),
-                       PyObject_IsTrue(v[9]), PyObject_IsTrue(v[10]), stream_of(v[11], dev));
+                       truth(v[9], "interleaved"), truth(v[10], "inverse"), stream_of(v[11], dev));
 }
 
 // handle, device, x, q, scale, stream
@@ -307,7 +312,7 @@ int blockscale_matmul(PyObject* const* v) {
     const Rows ar = bytes_like(&at_, "a", a.M, a.K, dev), sr = row_scales_like(&need(v[3], "a_scale"), "a_scale", a.M, a.K, dev);
     const Rows br = bytes_like(&bt, "b", a.N, a.K, dev);
     const int64_t nb = (a.N + 127) / 128, kb = (a.K + 127) / 128;
-    const bool transposed = PyObject_IsTrue(v[7]);
+    const bool transposed = truth(v[7], "scale_transposed");
     const Rows bs = rows_like(&need(v[5], "b_scale"), "b_scale", transposed ? kb : nb, transposed ? nb : kb, at::kByte, dev);
     const Rows orow = rows_like(&ot, "out", a.M, a.N, ot.scalar_type(), dev);
     a.a = ar.p; a.a_stride = ar.pitch;

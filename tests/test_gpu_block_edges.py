@@ -206,3 +206,21 @@ def test_norm_backward_takes_its_workspace_for_any_shape_and_stream(ctx, shape):
         with pytest.raises(A.AdlocoError) as e:
             ctx.add_rmsnorm_backward(bad, h, rstd, gain, dh, grad_sum=S, stream=side)
         assert e.value.status == A.ERR_INVALID_ARG
+
+
+def test_flags_without_a_truth_value_are_argument_errors(ctx):
+    x, gain, r = rnd(1, 2, 4, 64), rnd(2, 64), torch.ones(2, 4, device=DEV)
+    n, S = torch.zeros(2, device=DEV), torch.zeros(64, device=DEV)
+    q, s, b, sb = pitched(32, 64, 16), pitched(32, 1, 4), pitched(64, 64, 16), torch.full((1, 1), 127, dtype=torch.uint8, device=DEV)
+    heads, table, out = rnd(3, 1, 4, 2, 64), A.RopeTable(64), torch.zeros(32, 64, device=DEV)
+    neither = torch.tensor([1, 2])
+    before = ctx.launch_count
+    for call in (lambda: ctx.add_rmsnorm_backward(x, x, r, gain, torch.empty_like(x), per_sample_sqnorm=n, accumulate_norms=neither),
+                 lambda: ctx.add_rmsnorm_backward(x, x, r, gain, torch.empty_like(x), grad_sum=S, accumulate_sum=neither),
+                 lambda: ctx.rope([heads], table, interleaved=neither),
+                 lambda: ctx.rope([heads], table, inverse=neither),
+                 lambda: ctx.blockscale_matmul(q, s, b, sb, out, scale_transposed=neither)):
+        with pytest.raises(A.AdlocoError) as e:
+            call()
+        assert e.value.status == A.ERR_INVALID_ARG
+    assert ctx.launch_count == before
