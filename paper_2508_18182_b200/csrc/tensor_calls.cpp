@@ -151,6 +151,17 @@ void* stream_of(PyObject* o, int64_t dev) {
     return reinterpret_cast<void*>(static_cast<uintptr_t>(s));
 }
 
+// A call of the library with the interpreter's lock released, as the rest of the binding makes them: a launch waits where the
+// queue to the device is full.  The arguments are formed before.
+template <typename F, typename... Args>
+int unlocked(F f, Args... args) {
+    struct Released {
+        PyThreadState* state = PyEval_SaveThread();
+        ~Released() { PyEval_RestoreThread(state); }
+    } released;
+    return f(args...);
+}
+
 // handle, device, x, gain, residual, h, y, rstd, q, q_scale, eps, dropout, stream
 int add_rmsnorm(PyObject* const* v) {
     const int64_t dev = whole(v[1]);
@@ -180,7 +191,7 @@ int add_rmsnorm(PyObject* const* v) {
     a.q_scale = static_cast<uint8_t*>(sr.p); a.q_scale_stride = sr.pitch;
     const Mask m = mask_of(v[11]);
     a.dropout_p = m.p; a.seed = m.seed; a.offset = m.offset;
-    return adloco_add_rmsnorm(handle(v[0]), &a, stream_of(v[12], dev));
+    return unlocked(adloco_add_rmsnorm, handle(v[0]), &a, stream_of(v[12], dev));
 }
 
 // handle, device, dy, h, rstd, gain, dh, dh_residual, dx, dropout, norms, accumulate_norms, sum, accumulate_sum, workspace, stream
@@ -223,7 +234,7 @@ int add_rmsnorm_backward(PyObject* const* v) {
         a.workspace = vector(ws, "workspace", ws->numel(), at::kByte, dev);
         a.workspace_bytes = ws->numel();
     }
-    return adloco_add_rmsnorm_backward(handle(v[0]), &a, stream_of(v[15], dev));
+    return unlocked(adloco_add_rmsnorm_backward, handle(v[0]), &a, stream_of(v[15], dev));
 }
 
 // handle, device, x, out, residual, p, seed, offset, stream
@@ -234,7 +245,7 @@ int dropout(PyObject* const* v) {
     const Rows xr = rows_of(x, "x");
     const Rows yr = rows_like(&need(v[3], "out"), "out", xr.rows, xr.d, x.scalar_type(), dev);
     const Rows rr = rows_like(tensor(v[4], "residual", true), "residual", xr.rows, xr.d, x.scalar_type(), dev);
-    return adloco_dropout(handle(v[0]), code(x, "x"), xr.rows, xr.d, xr.p, xr.pitch, rr.p, rr.pitch, yr.p, yr.pitch, real(v[5]),
+    return unlocked(adloco_dropout, handle(v[0]), code(x, "x"), xr.rows, xr.d, xr.p, xr.pitch, rr.p, rr.pitch, yr.p, yr.pitch, real(v[5]),
                           unsigned_whole(v[6], "seed"), unsigned_whole(v[7], "offset"), stream_of(v[8], dev));
 }
 
@@ -272,7 +283,7 @@ int rope(PyObject* const* v) {
     }
     const at::Tensor& turns = need(v[4], "table");
     on(turns, "the table", dev);
-    return adloco_rope(handle(v[0]), code(x, "tensors"), t, (int32_t)n, B, T, D, whole(v[5]), static_cast<const uint64_t*>(turns.data_ptr()),
+    return unlocked(adloco_rope, handle(v[0]), code(x, "tensors"), t, (int32_t)n, B, T, D, whole(v[5]), static_cast<const uint64_t*>(turns.data_ptr()),
                        (float)real(v[6]), pos ? static_cast<const int32_t*>(pos->data_ptr()) : nullptr, pitch, whole(v[8]),
                        truth(v[9], "interleaved"), truth(v[10], "inverse"), stream_of(v[11], dev));
 }
@@ -284,7 +295,7 @@ int blockscale_quantize(PyObject* const* v) {
     on(x, "x", dev);
     const Rows xr = rows_of(x, "x"), qr = bytes_like(&need(v[3], "q"), "q", xr.rows, xr.d, dev);
     const Rows sr = row_scales_like(&need(v[4], "scale"), "scale", xr.rows, xr.d, dev);
-    return adloco_blockscale_quantize(handle(v[0]), code(x, "x"), xr.rows, xr.d, xr.p, xr.pitch, qr.p, qr.pitch, static_cast<uint8_t*>(sr.p),
+    return unlocked(adloco_blockscale_quantize, handle(v[0]), code(x, "x"), xr.rows, xr.d, xr.p, xr.pitch, qr.p, qr.pitch, static_cast<uint8_t*>(sr.p),
                                       sr.pitch, stream_of(v[5], dev));
 }
 
@@ -296,7 +307,7 @@ int blockscale_quantize_weight(PyObject* const* v) {
     const Rows wr = rows_of(W, "W"), qr = bytes_like(&need(v[3], "q"), "q", wr.rows, wr.d, dev);
     const Rows tr = bytes_like(tensor(v[5], "q_t", true), "q_t", wr.d, wr.rows, dev);
     const Rows sr = rows_like(&need(v[4], "scale"), "scale", (wr.rows + 127) / 128, (wr.d + 127) / 128, at::kByte, dev);
-    return adloco_blockscale_quantize_weight(handle(v[0]), code(W, "W"), wr.rows, wr.d, wr.p, wr.pitch, qr.p, qr.pitch, tr.p, tr.pitch,
+    return unlocked(adloco_blockscale_quantize_weight, handle(v[0]), code(W, "W"), wr.rows, wr.d, wr.p, wr.pitch, qr.p, qr.pitch, tr.p, tr.pitch,
                                              static_cast<uint8_t*>(sr.p), sr.pitch, stream_of(v[6], dev));
 }
 
@@ -323,7 +334,7 @@ int blockscale_matmul(PyObject* const* v) {
     a.b_scale_stride_k = transposed ? bs.pitch : 1;
     a.bias = static_cast<const float*>(vector(tensor(v[8], "bias", true), "bias", a.N, at::kFloat, dev));
     a.out = orow.p; a.out_stride = orow.pitch; a.out_dtype = code(ot, "out");
-    return adloco_blockscale_matmul(handle(v[0]), &a, stream_of(v[9], dev));
+    return unlocked(adloco_blockscale_matmul, handle(v[0]), &a, stream_of(v[9], dev));
 }
 
 template <int (*F)(PyObject* const*), int N>

@@ -1,6 +1,9 @@
 """GPU tests of the operators between the linear layers at the places where they could go wrong: what only few shapes,
 types or callers reach.  Oracle and tolerances as in test_gpu_block_ops.py; whole numbers small enough that every sum
 fits fp32 are compared for equality."""
+import threading
+import time
+
 import numpy as np
 import pytest
 import torch
@@ -224,3 +227,35 @@ def test_flags_without_a_truth_value_are_argument_errors(ctx):
             call()
         assert e.value.status == A.ERR_INVALID_ARG
     assert ctx.launch_count == before
+
+
+def test_other_threads_run_while_a_call_waits_for_room_in_the_launch_queue(ctx):
+    """Behind a kernel of about half a second the queue fills up and a call waits; a thread that wakes every few
+    milliseconds goes on meanwhile."""
+    x = torch.zeros(1, 64, device=DEV)
+    ctx.dropout(x, x, p=0.5, seed=1)
+    torch.cuda.synchronize()
+    stop, wakes = threading.Event(), [time.perf_counter()]
+
+    def tick():
+        while not stop.wait(0.002):
+            wakes.append(time.perf_counter())
+    thread = threading.Thread(target=tick)
+    thread.start()
+    torch.cuda._sleep(1_000_000_000)
+    longest = 0.0
+    for _ in range(6000):
+        t0 = time.perf_counter()
+        ctx.dropout(x, x, p=0.5, seed=1)
+        longest = max(longest, time.perf_counter() - t0)
+        if longest > 0.1:
+            break
+    t_end = time.perf_counter()
+    time.sleep(0.01)
+    stop.set()
+    thread.join()
+    torch.cuda.synchronize()
+    if longest <= 0.1:
+        pytest.skip("the launch queue took every call")
+    gaps = np.diff([w for w in wakes if w <= t_end] + [t_end])
+    assert gaps.max() < 0.5 * longest, (gaps.max(), longest)
