@@ -85,11 +85,14 @@ inline int set_cuda_error(adloco_ctx* ctx, cudaError_t e, const char* where) {
 
 // the ctx's device is current while an entry point runs
 struct DeviceGuard {
-    int prev = -1;
+    int prev = -1;                      // what to go back to, -1: nothing was changed
     bool ok = true;
     explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+        int now;
+        if (cudaGetDevice(&now) != cudaSuccess) { ok = false; return; }
+        if (now == dev) return;
+        prev = now;
+        if (cudaSetDevice(dev) != cudaSuccess) ok = false;
     }
     ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
 };
