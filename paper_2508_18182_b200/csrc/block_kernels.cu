@@ -1364,14 +1364,19 @@ int launch_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args& a, const Drop
     return ADLOCO_OK;
 }
 
-// Blocks a sample's rows are cut into: about as many over all samples as are resident at once, each with whole turns of a row
-// for every group of its threads (4 samples of 1024 x 300 bf16 by ten rows a block, eight and two: 24.4 us; by sixteen: 15.7).  Blocks an SM by width (registers set them in bf16; of 2, 3, 4 and 6 these measured best at
-// 256, 768, 1024, 2048, 3000 and 4096; five for narrow rows off the 16-byte grid); `fit` is what shared memory allows beside that.
+// Blocks a sample's rows are cut into: about as many over all samples as are resident at once, counted in whole turns of a row
+// for every group of a block's threads (4 samples of 1024 x 300 bf16 by ten rows a block, eight and two: 24.4 us; by
+// sixteen: 15.7).  The rows are then spread evenly over the blocks, which gives none of them more turns.  Blocks an SM by
+// width: of 2, 3, 4 and 6 these measured best at 256, 768, 1024, 2048, 3000 and 4096 in bf16, where registers set them; five
+// for narrow rows off the 16-byte grid.  `fit` is what shared memory allows beside that, and what decides on the grid from 257
+// on where the stream is fp32; off the grid the registers of 512 threads leave one block, however little memory it takes
+// (counted as two, 64 samples of 12 x 8191 bf16 took 100 us instead of 72).
 static int64_t rmsnorm_blocks(int64_t d, bool vec) {
     return d <= 256 ? (vec ? 4 : 5) : d <= 768 ? 3 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 3072 ? 3 : 2;
 }
+static int64_t rows_of_block(int64_t d) { return d <= 64 ? 32 : d <= 128 ? 16 : d <= 1024 ? 8 : d <= 4096 ? 2 : 1; }
 static int64_t rmsnorm_chunks(const adloco_ctx* ctx, int64_t B, int64_t T, int64_t d, bool vec, int64_t fit) {
-    const int64_t rows_at_once = d <= 64 ? 32 : d <= 128 ? 16 : d <= 1024 ? 8 : d <= 4096 ? 2 : 1;
+    const int64_t rows_at_once = rows_of_block(d);
     int64_t blocks = rmsnorm_blocks(d, vec);
     if (blocks > fit) blocks = fit < 1 ? 1 : fit;
     const int64_t want = blocks * (int64_t)ctx->sm_count / B;
@@ -1420,11 +1425,13 @@ int launch_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     p.a = a;
     const int64_t row_bytes = (xb ? 2 : 4) + 2 * (sb ? 2 : 4), threads = a.d > 4096 ? 512 : 256;
     const int64_t groups = a.d <= 1024 ? (a.d + 255) / 256 : a.d <= 4096 ? (a.d + 1023) / 1024 : (a.d + 4095) / 4096;     // of eight a thread
-    const int64_t one = threads * groups * 8 * row_bytes;
+    const int64_t one = vec ? threads * groups * 8 * row_bytes
+                            : rows_of_block(a.d) * (buffer_bytes((int)a.d, xb ? 2 : 4) + 2 * buffer_bytes((int)a.d, sb ? 2 : 4));
+    constexpr int64_t most = 227 * 1024, beside = 1024 + 128;      // of an SM; what a block takes beside its rows
     // a row ahead where it takes no block from an SM
-    p.buffers = !vec && (2 * one + 1024) * rmsnorm_blocks(a.d, vec) <= 227 * 1024 ? 2 : 1;
+    p.buffers = !vec && (2 * one + beside) * rmsnorm_blocks(a.d, vec) <= most ? 2 : 1;
     const int64_t smem = (vec ? 2 : p.buffers) * one;
-    p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d, vec, 227 * 1024 / (smem + 1024));
+    p.chunks = rmsnorm_chunks(ctx, a.B, a.T, a.d, vec, !vec && threads > 256 ? 1 : most / (smem + beside));
     p.rows_per_chunk = (a.T + p.chunks - 1) / p.chunks;
     int rc = ADLOCO_OK;
 #define ADLOCO_TYPES(XT, ST)                                                               \

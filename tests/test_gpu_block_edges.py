@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import oracle.block_oracle as O
+import test_gpu_block_ops as parity
 from paper_2508_18182_b200 import binding as A
 from test_gpu_block_ops import BF, DEV, F32, MASK, TYPES, close, np64, pitched, rnd, rounding
 
@@ -259,3 +260,26 @@ def test_other_threads_run_while_a_call_waits_for_room_in_the_launch_queue(ctx):
         pytest.skip("the launch queue took every call")
     gaps = np.diff([w for w in wakes if w <= t_end] + [t_end])
     assert gaps.max() < 0.5 * longest, (gaps.max(), longest)
+
+
+# ------------------------------------------------------------------------------------------- widths of a row
+# one at least of every instantiation that the other file's widths leave out: on the 16-byte grid 512 (two groups a lane, going
+# back), 2560 and 2824 (three groups of 128 threads) and what lies between its widths above 4096; off the grid two, three and
+# four groups of 128 threads and both forms of 512
+@pytest.mark.parametrize("d", [512, 520, 1100, 1500, 2560, 2824, 3001, 3500, 4097, 5001, 5120, 8191, 8200, 9001, 12288, 12001, 16383])
+@pytest.mark.parametrize("xt,st", TYPES)
+def test_norm_of_every_width_forward(ctx, d, xt, st):
+    parity.test_add_rmsnorm(ctx, d, xt, st)
+
+
+@pytest.mark.parametrize("B,T,d", [(3, 41, 512), (2, 300, 520), (2, 33, 1100), (1, 2500, 1300), (2, 35, 1500), (2, 29, 2560), (1, 1300, 2824), (2, 27, 3001),
+                                   (2, 25, 3500), (3, 1, 4097), (2, 700, 4097), (1, 900, 5001), (2, 17, 5120), (2, 13, 8191), (2, 11, 8200),
+                                   (1, 700, 9001), (3, 10, 9001), (2, 9, 12288), (1, 500, 12001), (2, 7, 16383), (1, 1, 16383), (300, 1, 5001)])
+@pytest.mark.parametrize("xt,st", TYPES)
+def test_norm_of_every_width_backward(ctx, B, T, d, xt, st):
+    parity.test_add_rmsnorm_backward(ctx, B, T, d, xt, st)
+
+
+@pytest.mark.parametrize("d", [512, 1100, 2560, 3500, 5001, 8192, 12001])
+def test_norm_of_every_width_to_8_bits(ctx, d):
+    parity.test_norm_to_8_bits(ctx, d)
