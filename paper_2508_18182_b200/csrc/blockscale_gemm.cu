@@ -174,7 +174,10 @@ __device__ __forceinline__ void fetch_scales(const MatArgs& a, uint32_t ring, Ti
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const bool last = !walk.more();
-            if (!last && !fetch(i ^ 1)) return;
+            if (!last && !fetch(i ^ 1)) {                 // leaving after a time-out: the turn before has copies in flight
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                return;
+            }
             if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
             else asm volatile("cp.async.wait_group 1;" ::: "memory");
             const uint32_t part = byte[i] << (8 * (lane & 3));

@@ -54,3 +54,12 @@ def test_kernels_launched_early_read_nothing_through_the_non_coherent_path():
     for f in early:
         for name, body in _kernels(_source(f)):
             assert re.search(r"\bafter_predecessor\s*\(\s*\)", body), (f, name)
+
+
+def test_scale_warps_that_give_up_wait_for_their_copies():
+    """A warp that leaves after a wait ran out may not leave asynchronous copies into shared memory behind."""
+    text = _source("blockscale_gemm.cu")
+    body = text[text.index("if (!walk.more() || !fetch(0)) return;"):]
+    body = body[:body.index("__global__")]
+    leave = body[body.index("!fetch(i ^ 1)"):]
+    assert re.match(r"!fetch\(i \^ 1\)\)\s*\{\s*asm volatile\(\"cp\.async\.wait_all;\"[^;]*\);\s*return;", leave), leave[:200]
