@@ -283,3 +283,66 @@ def test_norm_of_every_width_backward(ctx, B, T, d, xt, st):
 @pytest.mark.parametrize("d", [512, 1100, 2560, 3500, 5001, 8192, 12001])
 def test_norm_of_every_width_to_8_bits(ctx, d):
     parity.test_norm_to_8_bits(ctx, d)
+
+
+# ------------------------------------------------------------------------------------- offsets beyond 32 bits
+def far_rows(buffer, at, rows, cols, pitch):
+    return buffer[at:].as_strided((rows, cols), (pitch, 1))
+
+
+def test_rows_that_lie_more_than_32_bits_apart(ctx):
+    """Three rows, 2^31 elements from one to the next: every operator finds them, on and off the 16-byte grid."""
+    pitch, d = (1 << 31) + 8, 776
+    big = torch.empty(2 * pitch + (1 << 16), dtype=BF, device=DEV)
+    near = [rnd(i, 3, d, dtype=BF) for i in range(4)]
+    gain, mask = rnd(9, d), (0.25, 3, 4)
+    for shift in (0, 1):
+        x, r, y, h, u, dh = (far_rows(big, 1024 * i + shift, 3, d, pitch) for i in range(6))
+        x.copy_(near[0]), r.copy_(near[1]), u.copy_(near[2])
+        rstd, ref = torch.empty(3, device=DEV), [torch.empty(3, d, dtype=BF, device=DEV) for _ in range(3)]
+        ctx.add_rmsnorm(x, gain, residual=r, h=h, y=y, rstd=rstd, dropout=mask)
+        ctx.add_rmsnorm(near[0], gain, residual=near[1], h=ref[0], y=ref[1], dropout=mask)
+        torch.cuda.synchronize()
+        assert torch.equal(h, ref[0]) and torch.equal(y, ref[1])
+        S, S_ref = torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+        ctx.add_rmsnorm_backward(u, h, rstd, gain, dh, grad_sum=S)
+        ctx.add_rmsnorm_backward(near[2], ref[0], rstd, gain, ref[2], grad_sum=S_ref)
+        torch.cuda.synchronize()
+        assert torch.equal(dh, ref[2]) and torch.allclose(S, S_ref, rtol=2.0 ** -20, atol=2.0 ** -18)
+        ctx.dropout(x, y, p=0.25, seed=3, offset=4, residual=r)
+        ctx.dropout(near[0], ref[0], p=0.25, seed=3, offset=4, residual=near[1])
+        torch.cuda.synchronize()
+        assert torch.equal(y, ref[0])
+        q, s, q_ref, s_ref = pitched(3, d, 16), pitched(3, 7, 4), pitched(3, d, 16), pitched(3, 7, 4)
+        ctx.blockscale_quantize(x, q, s)
+        ctx.blockscale_quantize(near[0], q_ref, s_ref)
+        torch.cuda.synchronize()
+        assert torch.equal(q, q_ref) and torch.equal(s, s_ref)
+    # heads: samples and tokens 2^31 elements apart
+    table, heads = A.RopeTable(64), rnd(5, 3, 1, 2, 64, dtype=BF)
+    ref = torch.empty_like(heads)
+    ctx.rope([heads], table, outs=[ref], first_position=7)
+    for strides in ((pitch, 128, 64, 1), (1 << 33, pitch, 64, 1)):
+        shape = (3, 1, 2, 64) if strides[0] == pitch else (1, 3, 2, 64)
+        a, o = big.as_strided(shape, strides), big[4096:].as_strided(shape, strides)
+        a.copy_(heads.view(shape))
+        pos = torch.full(shape[:2], 7, dtype=torch.int32, device=DEV)
+        ctx.rope([a], table, outs=[o], positions=pos)
+        torch.cuda.synchronize()
+        assert torch.equal(o, ref.view(shape))
+
+
+@pytest.mark.parametrize("M", [3, 40])
+def test_products_whose_operands_pass_32_bits(ctx, M):
+    """A's and the output's rows 2^27 (40 rows) or 2^31 (3 rows) apart, B's 2^25."""
+    N, K, far = 130, 300, (1 << 31 if M == 3 else 1 << 27) + 16
+    a_flat, o_flat = torch.empty((M - 1) * far + 512, dtype=torch.uint8, device=DEV), torch.empty((M - 1) * far + 512, dtype=BF, device=DEV)
+    b_flat = torch.empty((N - 1) * ((1 << 25) + 16) + 512, dtype=torch.uint8, device=DEV)
+    a, b, out = a_flat.as_strided((M, K), (far, 1)), b_flat.as_strided((N, K), ((1 << 25) + 16, 1)), o_flat.as_strided((M, N), (far, 1))
+    x, w = whole(1, M, K, top=8), whole(2, N, K, top=8)
+    sa, sb = pitched(M, 3, 4), torch.zeros(2, 3, dtype=torch.uint8, device=DEV)
+    ctx.blockscale_quantize(x, a, sa)
+    ctx.blockscale_quantize_weight(w, b, sb)
+    ctx.blockscale_matmul(a, sa, b, sb, out)
+    torch.cuda.synchronize()
+    assert ctx.device_status() == 0 and torch.equal(out, (x @ w.t()).to(BF))
