@@ -343,7 +343,8 @@ int adloco_embedding_sqnorm(adloco_ctx* ctx, const int32_t* token_ids, const voi
  * rotary positions, and the linear layer in 8-bit floating point.  Their backward passes
  * produce the X and Delta that the per-sample norms above read; the norm's own gain
  * contributes its per-sample norms in the same pass.  None of them uses the ctx workspace, so
- * all may be issued on several streams at once.  Rows are addressed by a pitch in elements;
+ * all may be issued on several streams at once.  Rows are addressed by a pitch in elements, the
+ * same one where an output may be the same memory as an input and is;
  * 16-byte aligned rows (base and pitch) take vector loads; others are slower, the norm's through shared memory. */
 
 /* h = residual + drop(x);  y = gain * h / sqrt(mean(h^2) + eps) over each row of d elements.

@@ -37,6 +37,11 @@ int make_key(double p, uint64_t seed, uint64_t offset, bool residual, DropoutKey
     return ADLOCO_OK;
 }
 
+// An output at the address of an input is that input, row for row: with another pitch its rows are other rows' inputs.
+bool in_step(const void* out, int64_t out_stride, const void* in, int64_t in_stride, int64_t rows) {
+    return out == nullptr || out != in || rows == 1 || out_stride == in_stride;
+}
+
 // the pair of types an operator with a residual stream takes
 int check_types(adloco_dtype t, adloco_dtype stream, adloco_dtype gain) {
     if (!known(t) || !known(stream) || !known(gain)) return ADLOCO_ERR_UNSUPPORTED;
@@ -114,7 +119,7 @@ int adloco_add_rmsnorm(adloco_ctx* ctx, const adloco_rmsnorm_args* a, void* stre
     if (a->rows < 1 || a->d < 1 || !(a->eps >= 0.f) || !std::isfinite(a->eps)) return ADLOCO_ERR_INVALID_ARG;
     if (a->rows > kMaxExtent || a->d > 16384) return ADLOCO_ERR_UNSUPPORTED;
     if (a->x_stride < a->d || (a->residual && a->residual_stride < a->d) || (a->h && a->h_stride < a->d) ||
-        (a->y && a->y_stride < a->d))
+        (a->y && a->y_stride < a->d) || !in_step(a->h, a->h_stride, a->residual, a->residual_stride, a->rows))
         return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(a->x, a->dtype) || !elem_aligned(a->y, a->dtype) || !elem_aligned(a->residual, a->stream_dtype) ||
         !elem_aligned(a->h, a->stream_dtype) || !elem_aligned(a->gain, a->gain_dtype) || !elem_aligned(a->rstd, ADLOCO_F32))
@@ -144,7 +149,9 @@ int adloco_add_rmsnorm_backward(adloco_ctx* ctx, const adloco_rmsnorm_backward_a
     // samples: a cluster of eight blocks each forms their norms
     if (a->B > (kMaxExtent >> 3) || a->T > kMaxExtent || a->B * a->T > kMaxExtent || a->d > 16384) return ADLOCO_ERR_UNSUPPORTED;
     if (a->dy_stride < a->d || a->h_stride < a->d || a->dh_stride < a->d ||
-        (a->dh_residual && a->dh_residual_stride < a->d) || (a->dx && a->dx_stride < a->d))
+        (a->dh_residual && a->dh_residual_stride < a->d) || (a->dx && a->dx_stride < a->d) ||
+        !in_step(a->dh, a->dh_stride, a->dh_residual, a->dh_residual_stride, a->B * a->T) ||
+        !in_step(a->dx, a->dx_stride, a->dy, a->dy_stride, a->B * a->T))
         return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(a->dy, a->dtype) || !elem_aligned(a->dx, a->dtype) || !elem_aligned(a->h, a->stream_dtype) ||
         !elem_aligned(a->dh, a->stream_dtype) || !elem_aligned(a->dh_residual, a->stream_dtype) ||
@@ -169,7 +176,9 @@ int adloco_dropout(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t co
     if (!ctx || !x || !y || rows < 1 || cols < 1) return ADLOCO_ERR_INVALID_ARG;
     if (!known(dtype)) return ADLOCO_ERR_UNSUPPORTED;
     if (rows > kMaxExtent || cols > (int64_t(1) << 40) || rows > (int64_t(1) << 50) / cols) return ADLOCO_ERR_UNSUPPORTED;
-    if (x_stride < cols || y_stride < cols || (residual && residual_stride < cols)) return ADLOCO_ERR_INVALID_ARG;
+    if (x_stride < cols || y_stride < cols || (residual && residual_stride < cols) || !in_step(y, y_stride, x, x_stride, rows) ||
+        !in_step(y, y_stride, residual, residual_stride, rows))
+        return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(x, dtype) || !elem_aligned(y, dtype) || !elem_aligned(residual, dtype)) return ADLOCO_ERR_ALIGNMENT;
     DropoutKey key;
     const int rc = make_key(p, seed, offset, residual != nullptr, &key);

@@ -346,3 +346,19 @@ def test_products_whose_operands_pass_32_bits(ctx, M):
     ctx.blockscale_matmul(a, sa, b, sb, out)
     torch.cuda.synchronize()
     assert ctx.device_status() == 0 and torch.equal(out, (x @ w.t()).to(BF))
+
+
+def test_the_same_memory_with_another_pitch_is_refused(ctx):
+    """An output over its input is in place only where their rows are the same ones."""
+    flat = rnd(1, 4, 256)
+    tight, spaced = flat.view(-1).as_strided((4, 64), (64, 1)), flat[:, :64]
+    x, gain, rstd, kept, before = rnd(2, 4, 64), rnd(3, 64), torch.ones(4, device=DEV), flat.clone(), ctx.launch_count
+    for call in (lambda: ctx.add_rmsnorm(x, gain, residual=tight, h=spaced, y=torch.empty_like(x)),
+                 lambda: ctx.add_rmsnorm_backward(x, x, rstd, gain, spaced, dh_residual=tight),
+                 lambda: ctx.add_rmsnorm_backward(tight, x, rstd, gain, torch.empty_like(x), dx=spaced),
+                 lambda: ctx.dropout(tight, spaced, p=0.5, seed=1),
+                 lambda: ctx.dropout(x, spaced, p=0.5, seed=1, residual=tight)):
+        with pytest.raises(A.AdlocoError) as e:
+            call()
+        assert e.value.status == A.ERR_INVALID_ARG
+    assert ctx.launch_count == before and torch.equal(flat, kept)
