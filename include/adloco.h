@@ -466,7 +466,8 @@ typedef struct {
  *   tensors     HOST array of 1..4 entries (queries and keys of different head counts go in one call)
  *   turns_dev   dev copy of adloco_rope_frequencies' table
  *   positions   dev int32 [B, T] with pitch positions_stride, or NULL: position first_position + t
- * Phase arithmetic is exact, sine and cosine fp32, every output rounded once. */
+ * Phase arithmetic is exact, every output rounded once; sine and cosine are fp32's for F32 and those of the fast
+ * instructions for BF16 (off by 2^-21, against the output's rounding of 2^-9). */
 int adloco_rope(adloco_ctx* ctx, adloco_dtype dtype, const adloco_rope_tensor* tensors, int32_t n_tensors, int64_t B,
                 int64_t T, int64_t head_dim, int64_t rot_dim, const uint64_t* turns_dev, float magnitude,
                 const int32_t* positions, int64_t positions_stride, int64_t first_position, int interleaved, int inverse,

@@ -302,11 +302,11 @@ __device__ __forceinline__ float row_sum(float v, float* smem, int turn) {
 // ---- rows that do not start on 16-byte boundaries ------------------------------------------------
 // They pass through shared memory at the alignment they have in global memory (a row's element j at byte skew + j es of its
 // buffer, skew = the row's address modulo 16): whole 16-byte pieces go by cp.async, the ends one by one, and a group of eight
-// elements is put together from the aligned pieces around it.  (Norm of 6272 x 1001 bf16: 18.7 us, its backward pass 46.3;
+// elements is put together from the aligned pieces around it.  (Norm of 6272 x 1001 bf16 out of L2: 18.7 us, its backward pass 45.9;
 // with element-wise copies 31 and 78; eight guarded scalar accesses a thread were slower still.)  Rows of fp32 go element by
 // element into an aligned buffer instead (skew 0): four bytes a lane are whole cache lines already, and a group written back
-// to a skewed buffer would be eight stores that meet in four banks (norm backward of 1665 x 1001 fp32 by 145 blocks: 22.2 us
-// so, 18.3 us this way).
+// to a skewed buffer would be eight stores that meet in four banks (norm backward of 1665 x 1001 fp32, when it was cut into
+// 145 blocks: 22.2 us so, 18.3 us this way; 19.9 with the 210 blocks of today).
 __host__ __device__ constexpr int pad8(int d) { return (d + 7) / 8 * 8; }
 // bytes of a row's buffer: the skew before it, and the piece read beyond its last group
 __host__ __device__ constexpr int buffer_bytes(int d, int es) { return (pad8(d) * es + 15) / 16 * 16 + 32; }
@@ -595,7 +595,8 @@ __device__ __forceinline__ Raw<T> staged(uint32_t at, uint32_t step) {
 // 16-byte pieces a thread stages for one row: dy, h, and the stream's gradient
 template <typename XT, typename ST, int C>
 __host__ __device__ constexpr int stage_pieces() { return C * ((int)sizeof(XT) / 2 + 2 * ((int)sizeof(ST) / 2)); }
-// rows on their way or in use: two (with three blocks an SM at widths up to 768 in bf16; three rows deep and two blocks
+// rows on their way or in use: two (with three blocks an SM at widths up to 768 in bf16; on an fp32 stream one block is left at
+// 768, and 32768 x 768 takes 108 us with a bf16 branch, 143 in fp32, against floors of 62 and 77; three rows deep and two blocks
 // measured slower), or one -- no staging, loads straight into registers -- where two do not fit
 template <typename XT, typename ST, int C, int THREADS>
 __host__ __device__ constexpr int stage_depth() {
@@ -1233,7 +1234,7 @@ __global__ void __launch_bounds__(256) quantise_weight_kernel(const T* W, int64_
                                                               int64_t cols, int vec) {
     after_predecessor();
     __shared__ uint32_t amax[8];
-    alignas(16) __shared__ uint8_t tile[128][132];                   // [column][row]; rows of 33 words: threads of a warp fall on different banks
+    alignas(16) __shared__ uint8_t tile[128][132];                   // [column][row]; 33 words a row: the 16 columns a warp writes, eight apart, meet four on a bank (128 words: all on one)
     const int64_t r0 = (int64_t)blockIdx.y * 128, c0 = (int64_t)blockIdx.x * 128;
     const int cl = (threadIdx.x & 15) * 8, rl = threadIdx.x >> 4;
     const int n = (int)max((int64_t)0, min((int64_t)8, cols - (c0 + cl)));
