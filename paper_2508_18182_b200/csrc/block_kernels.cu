@@ -306,7 +306,7 @@ __device__ __forceinline__ float row_sum(float v, float* smem, int turn) {
 // with element-wise copies 31 and 78; eight guarded scalar accesses a thread were slower still.)  Rows of fp32 go element by
 // element into an aligned buffer instead (skew 0): four bytes a lane are whole cache lines already, and a group written back
 // to a skewed buffer would be eight stores that meet in four banks (norm backward of 1665 x 1001 fp32, when it was cut into
-// 145 blocks: 22.2 us so, 18.3 us this way; 19.9 with the 210 blocks of today).
+// 145 blocks: 22.2 us so, 18.3 us this way).
 __host__ __device__ constexpr int pad8(int d) { return (d + 7) / 8 * 8; }
 // bytes of a row's buffer: the skew before it, and the piece read beyond its last group
 __host__ __device__ constexpr int buffer_bytes(int d, int es) { return (pad8(d) * es + 15) / 16 * 16 + 32; }
