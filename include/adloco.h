@@ -524,6 +524,172 @@ typedef struct {
 } adloco_blockscale_matmul_args;
 int adloco_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_args* args, void* stream);
 
+/* The values that rows in 8 bits stand for (adloco_blockscale_quantize's, or what the linear layers below keep), rounded to
+ * dtype: exact but where a value leaves its range (a block with the byte 255 is all NaN).  This is how an activation kept
+ * in 8 bits comes back as the X of adloco_linear_sqnorm.
+ *   q, scale  as adloco_blockscale_quantize writes them (same rules);  x  dev [rows, cols] in dtype, pitch x_stride */
+int adloco_blockscale_dequantize(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t cols, const void* q,
+                                 int64_t q_stride, const uint8_t* scale, int64_t scale_stride, void* x, int64_t x_stride,
+                                 void* stream);
+
+/* ---- linear layers in bf16, alone and as the gated feed-forward -------------------- */
+
+/* The products of a decoder's layers with what follows them in the same pass, forward and backward.  The gradients of the
+ * weights, with their per-sample norms, are adloco_linear_sqnorm's, on the x and the gradients that these calls take and
+ * return.  Operands of a product (x, w, dy) are bf16 with 16-byte aligned rows (base, and a pitch that is a multiple of 8);
+ * other tensors may have any pitch, 16-byte aligned rows being the fast ones.  Products are exact, sums fp32: the tensor
+ * cores' own in bf16 outputs (they cut off low bits: a relative error of 1e-6 after 1000 terms), with every 512 terms added
+ * up to nearest where an output is F32; every output is rounded once.  An output may be the same memory as an elementwise operand
+ * (residual, z, gate, up) of the same type and pitch; no other overlap is allowed.
+ * None of them uses the ctx workspace. */
+typedef enum {
+    ADLOCO_ACT_NONE = 0,
+    ADLOCO_ACT_RELU = 1,
+    ADLOCO_ACT_GELU = 2,        /* z (1 + erf(z / sqrt 2)) / 2 */
+    ADLOCO_ACT_GELU_TANH = 3,   /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+    ADLOCO_ACT_SILU = 4         /* z / (1 + exp(-z)) */
+} adloco_activation;
+
+/* A matrix that the forward pass keeps for the backward one: bf16 (scale NULL), or 8 bits with a power-of-two scale for each
+ * 128 elements of a row, as adloco_blockscale_quantize writes them from the unrounded values (its rules for pitches and
+ * alignment; bf16: 16-byte aligned rows).  p NULL: not kept. */
+typedef struct {
+    void* p;
+    int64_t stride;
+    uint8_t* scale;
+    int64_t scale_stride;
+} adloco_kept;
+
+/* z = x w^T + bias;  y = residual + act(z)
+ *   x [M, K], w [N, K] dev bf16;  bias dev [N] float, may be NULL
+ *   residual, y  dev [M, N] in out_dtype;  residual may be NULL
+ *   z            kept for adloco_linear_backward of the next layer, [M, N]; optional */
+typedef struct {
+    int64_t M, N, K;
+    const void* x;
+    int64_t x_stride;
+    const void* w;
+    int64_t w_stride;
+    const float* bias;
+    const void* residual;
+    int64_t residual_stride;
+    void* y;
+    int64_t y_stride;
+    adloco_kept z;
+    int32_t activation;
+    adloco_dtype out_dtype;
+} adloco_linear_args;
+int adloco_linear(adloco_ctx* ctx, const adloco_linear_args* args, void* stream);
+
+/* The way back through a layer y = a w^T and through the activation a = act(z) that made its input:
+ *   dx = residual + (dy w) act'(z)          a = act(z), recomputed for the weight's gradient
+ *   dy [M, N], w [N, K] dev bf16 (the forward call's w, as it lies)
+ *   z         what the forward pass kept, [M, K]; may be NULL where activation is NONE
+ *   residual, dx  dev [M, K] in out_dtype; residual may be NULL
+ *   a         dev [M, K] bf16, may be NULL; needs z */
+typedef struct {
+    int64_t M, N, K;
+    const void* dy;
+    int64_t dy_stride;
+    const void* w;
+    int64_t w_stride;
+    adloco_kept z;
+    const void* residual;
+    int64_t residual_stride;
+    void* dx;
+    int64_t dx_stride;
+    void* a;
+    int64_t a_stride;
+    int32_t activation;
+    adloco_dtype out_dtype;
+} adloco_linear_backward_args;
+int adloco_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args* args, void* stream);
+
+/* The gated feed-forward's first half in one pass:  gate = x w_gate^T,  up = x w_up^T,  a = act(gate) up
+ *   x [M, d], w_gate, w_up [f, d] dev bf16;  a dev [M, f] bf16
+ *   gate, up  kept for the backward pass, [M, f], both or neither, in one form */
+typedef struct {
+    int64_t M, d, f;
+    const void* x;
+    int64_t x_stride;
+    const void* w_gate;
+    int64_t w_gate_stride;
+    const void* w_up;
+    int64_t w_up_stride;
+    void* a;
+    int64_t a_stride;
+    adloco_kept gate, up;
+    int32_t activation;
+    int32_t reserved;
+} adloco_gated_linear_args;
+int adloco_gated_linear(adloco_ctx* ctx, const adloco_gated_linear_args* args, void* stream);
+
+/* The way back through the layer y = a w_down^T after it and through the gate:  with da = dy w_down,
+ *   d_gate = da up act'(gate)     d_up = da act(gate)     a = act(gate) up, recomputed
+ *   dy [M, d], w_down [d, f] dev bf16;  gate, up as kept;  d_gate, d_up, a dev [M, f] bf16; a may be NULL
+ * With [w_gate; w_up] as one matrix [2 f, d] and [d_gate | d_up] as one [M, 2 f], the input's gradient is
+ * adloco_linear_backward of the two, and both weights' gradients and norms adloco_linear_sqnorm's. */
+typedef struct {
+    int64_t M, d, f;
+    const void* dy;
+    int64_t dy_stride;
+    const void* w_down;
+    int64_t w_down_stride;
+    adloco_kept gate, up;
+    void* d_gate;
+    int64_t d_gate_stride;
+    void* d_up;
+    int64_t d_up_stride;
+    void* a;
+    int64_t a_stride;
+    int32_t activation;
+    int32_t reserved;
+} adloco_gated_linear_backward_args;
+int adloco_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_backward_args* args, void* stream);
+
+/* ---- the loss ----------------------------------------------------------------------- */
+
+/* Of each row of logits l: lse = log sum_j exp(l_j), the log-probability logp = l_t - lse of its given token t, the entropy
+ * -sum_j p_j log p_j with p_j = exp(l_j - lse), and the log-probabilities and ids of its `top` most probable tokens, the
+ * largest first, equal ones by the lower id.
+ *   logits   dev [rows, V] in dtype, pitch logits_stride;  targets dev int32 [rows], may be NULL when logp is
+ *   logp, entropy, lse   dev [rows] float, each may be NULL;  top_values float, top_ids int32 dev [rows, top]
+ *            contiguous, both or neither, 0 <= top <= 64, top <= V
+ * A row whose target is outside [0, V) has logp 0.  Logits of -Inf (tokens ruled out) have probability 0 and log-probability
+ * -Inf; a row of nothing else has lse, logp and top_values -Inf and entropy 0.  A row with a NaN or +Inf has NaN in all of them,
+ * and ids of some tokens of the vocabulary.  fp32 throughout, one pass over the logits (the choice of the top tokens reads them again, from L2). */
+typedef struct {
+    int64_t rows, V;
+    const void* logits;
+    int64_t logits_stride;
+    const int32_t* targets;
+    float *logp, *entropy, *lse;
+    float* top_values;
+    int32_t* top_ids;
+    int32_t top;
+    adloco_dtype dtype;
+} adloco_token_logprobs_args;
+int adloco_token_logprobs(adloco_ctx* ctx, const adloco_token_logprobs_args* args, void* stream);
+
+/* The logits' gradient of sum_r d_logp_r logp_r + d_entropy_r entropy_r:
+ *   d_logits_j = d_logp (delta_jt - p_j) - d_entropy p_j (log p_j + entropy),    p_j = exp(l_j - lse)
+ *   logits, targets, lse, entropy  as given to and by the call above (entropy and d_entropy: both or neither)
+ *   d_logits  dev [rows, V] in dtype, pitch d_logits_stride; may be logits itself, with the same pitch
+ * A row whose target is outside [0, V) takes no part in logp.  A row that takes part in nothing (and whose d_entropy is 0 or
+ * not given), or with lse -Inf, gets zeros whatever its logits hold. */
+typedef struct {
+    int64_t rows, V;
+    const void* logits;
+    int64_t logits_stride;
+    const int32_t* targets;
+    const float *lse, *d_logp, *entropy, *d_entropy;
+    void* d_logits;
+    int64_t d_logits_stride;
+    int32_t reserved;
+    adloco_dtype dtype;
+} adloco_token_logprobs_backward_args;
+int adloco_token_logprobs_backward(adloco_ctx* ctx, const adloco_token_logprobs_backward_args* args, void* stream);
+
 /* ---- switch-mode accumulation -------------------------------------------- */
 
 /* Accumulator of the test sums over the micro-batches of one large batch:

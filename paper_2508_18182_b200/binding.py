@@ -31,6 +31,8 @@ EXPORTS = (
     "adloco_add_rmsnorm", "adloco_add_rmsnorm_backward", "adloco_add_rmsnorm_backward_workspace", "adloco_dropout",
     "adloco_rope", "adloco_rope_frequencies",
     "adloco_blockscale_quantize", "adloco_blockscale_quantize_weight", "adloco_blockscale_matmul",
+    "adloco_blockscale_dequantize", "adloco_linear", "adloco_linear_backward", "adloco_gated_linear", "adloco_gated_linear_backward",
+    "adloco_token_logprobs", "adloco_token_logprobs_backward",
 )
 
 
@@ -135,6 +137,13 @@ def load_library() -> C.CDLL:
         "adloco_blockscale_quantize": (C.c_int, [vp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
         "adloco_blockscale_quantize_weight": (C.c_int, [vp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
         "adloco_blockscale_matmul": (C.c_int, [vp, vp, vp]),
+        "adloco_blockscale_dequantize": (C.c_int, [vp, C.c_int, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
+        "adloco_linear": (C.c_int, [vp, vp, vp]),
+        "adloco_linear_backward": (C.c_int, [vp, vp, vp]),
+        "adloco_gated_linear": (C.c_int, [vp, vp, vp]),
+        "adloco_gated_linear_backward": (C.c_int, [vp, vp, vp]),
+        "adloco_token_logprobs": (C.c_int, [vp, vp, vp]),
+        "adloco_token_logprobs_backward": (C.c_int, [vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -424,6 +433,59 @@ class Context:
         rc = self.calls.blockscale_matmul(self.h.value, self.device.index, a, a_scale, b, b_scale, out, scale_transposed, bias, stream)
         if rc != OK:
             self._passed(rc, "adloco_blockscale_matmul")
+
+    def blockscale_dequantize(self, q, scale, x, *, stream=None):
+        """adloco_blockscale_dequantize: the values that rows in 8 bits stand for, into x (bf16 or float32)."""
+        rc = self.calls.blockscale_dequantize(self.h.value, self.device.index, q, scale, x, stream)
+        if rc != OK:
+            self._passed(rc, "adloco_blockscale_dequantize")
+
+    # ------------------------------------------------------------------ linear layers in bf16
+    def linear(self, x, w, y, *, bias=None, activation="none", residual=None, z=None, z_scale=None, stream=None):
+        """adloco_linear: z = x w^T + bias, y = residual + act(z).  x [..., K], w [N, K] bf16, bias float32 [N]; y and residual
+        bf16 or float32.  z keeps the activation's input for linear_backward: bf16, or 8 bits beside z_scale.
+        activation: "none", "relu", "gelu", "gelu_tanh" or "silu"."""
+        rc = self.calls.linear(self.h.value, self.device.index, x, w, y, bias, activation, residual, z, z_scale, stream)
+        if rc != OK:
+            self._passed(rc, "adloco_linear")
+
+    def linear_backward(self, dy, w, dx, *, activation="none", z=None, z_scale=None, a=None, residual=None, stream=None):
+        """adloco_linear_backward: dx = residual + (dy w) act'(z), the way back through the layer w [N, K] and the activation
+        that made its input from z; a receives that input again, act(z), for linear_sqnorm."""
+        rc = self.calls.linear_backward(self.h.value, self.device.index, dy, w, dx, activation, z, z_scale, a, residual, stream)
+        if rc != OK:
+            self._passed(rc, "adloco_linear_backward")
+
+    def gated_linear(self, x, w_gate, w_up, a, *, activation="silu", gate=None, up=None, gate_scale=None, up_scale=None, stream=None):
+        """adloco_gated_linear: a = act(x w_gate^T) * (x w_up^T).  gate and up keep the two projections for the backward pass:
+        bf16, or 8 bits beside their scales."""
+        rc = self.calls.gated_linear(self.h.value, self.device.index, x, w_gate, w_up, a, activation, gate, up, gate_scale, up_scale, stream)
+        if rc != OK:
+            self._passed(rc, "adloco_gated_linear")
+
+    def gated_linear_backward(self, dy, w_down, gate, up, d_gate, d_up, *, activation="silu", gate_scale=None, up_scale=None, a=None,
+                              stream=None):
+        """adloco_gated_linear_backward: the way back through the layer w_down [d, f] after gated_linear and through the gate,
+        into d_gate and d_up; a receives w_down's input again, for linear_sqnorm."""
+        rc = self.calls.gated_linear_backward(self.h.value, self.device.index, dy, w_down, gate, up, d_gate, d_up, activation, gate_scale, up_scale, a,
+                                              stream)
+        if rc != OK:
+            self._passed(rc, "adloco_gated_linear_backward")
+
+    # ------------------------------------------------------------------ the loss
+    def token_logprobs(self, logits, targets, logp, *, entropy=None, lse=None, top_values=None, top_ids=None, stream=None):
+        """adloco_token_logprobs: for each row of logits the log-probability of its target (int32; outside the vocabulary: 0) into
+        logp, and where given its entropy, log of the sum of exponentials (for the backward pass), and the log-probabilities
+        and ids (int32) of its most probable tokens, as many as top_values has in a row."""
+        rc = self.calls.token_logprobs(self.h.value, self.device.index, logits, targets, logp, entropy, lse, top_values, top_ids, stream)
+        if rc != OK:
+            self._passed(rc, "adloco_token_logprobs")
+
+    def token_logprobs_backward(self, logits, targets, lse, d_logp, d_logits, *, entropy=None, d_entropy=None, stream=None):
+        """adloco_token_logprobs_backward: the logits' gradient of sum d_logp logp + d_entropy entropy; d_logits may be logits."""
+        rc = self.calls.token_logprobs_backward(self.h.value, self.device.index, logits, targets, lse, d_logp, d_logits, entropy, d_entropy, stream)
+        if rc != OK:
+            self._passed(rc, "adloco_token_logprobs_backward")
 
     # ------------------------------------------------------------------ outer step
     def outer_step(self, instances, theta_in, mom_in, *, lr, momentum, nesterov=True, theta_out=None,

@@ -14,7 +14,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libadloco.so")
 CALLS = os.path.join(PKG, "_tensor_calls.so")
 SOURCES = ["api.cu", "stream_kernels.cu", "gram_kernels.cu", "block_api.cu", "block_kernels.cu",
-           "blockscale_gemm.cu"]
+           "blockscale_gemm.cu", "dense_gemm.cu", "token_kernels.cu"]
 HEADERS = ["common.cuh", os.path.join("..", "..", "include", "adloco.h")]
 
 

@@ -1,6 +1,7 @@
 // C ABI of the operators between the linear layers: argument checks and dispatch.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "common.cuh"
 
@@ -105,6 +106,44 @@ bool fall_on_one_another(const int64_t (&extents)[3], const int64_t (&strides)[3
             if ((!(same && k == 0) && here < width) || (next >= 0 && next < width)) return true;
         }
     }
+    return false;
+}
+
+// an operand of a bf16 product: rows that the tensor cores' copies can take
+int check_operand(const void* p, int64_t stride, int64_t cols) {
+    if (!p || stride < cols) return ADLOCO_ERR_INVALID_ARG;
+    if (!aligned16(p) || (stride & 7) != 0) return ADLOCO_ERR_ALIGNMENT;
+    return ADLOCO_OK;
+}
+int check_kept(const adloco_kept& k, int64_t cols) {
+    if (!k.p) return k.scale ? ADLOCO_ERR_INVALID_ARG : ADLOCO_OK;
+    if (!k.scale) return check_operand(k.p, k.stride, cols);
+    const int rc = check_bytes(k.p, k.stride, cols);
+    return rc != ADLOCO_OK ? rc : check_row_scales(k.scale, k.scale_stride, cols);
+}
+// What a product's epilogue reads and writes element by element: an output may be one of those operands, in its type and
+// pitch, but no other output and no operand of the product.
+struct Matrix {
+    const void* p;
+    int64_t stride, bytes;              // an element's
+};
+bool apart(std::initializer_list<Matrix> outs, std::initializer_list<Matrix> elementwise, std::initializer_list<const void*> operands, int64_t rows) {
+    for (const Matrix* o = outs.begin(); o != outs.end(); ++o) {
+        if (!o->p) continue;
+        for (const Matrix* other = outs.begin(); other != o; ++other)
+            if (other->p == o->p) return false;
+        for (const Matrix& e : elementwise)
+            if (e.p == o->p && (e.bytes != o->bytes || !in_step(o->p, o->stride, e.p, e.stride, rows))) return false;
+        for (const void* x : operands)
+            if (x == o->p) return false;
+    }
+    return true;
+}
+Matrix matrix_of(const adloco_kept& k) { return Matrix{k.p, k.stride, k.scale ? 1 : 2}; }
+bool known_act(int32_t a) { return a >= ADLOCO_ACT_NONE && a <= ADLOCO_ACT_SILU; }
+bool too_large(std::initializer_list<int64_t> extents) {
+    for (int64_t e : extents)
+        if (e > kMaxExtent) return true;
     return false;
 }
 
@@ -290,6 +329,114 @@ int adloco_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
     if (!elem_aligned(a->out, a->out_dtype) || !elem_aligned(a->bias, ADLOCO_F32)) return ADLOCO_ERR_ALIGNMENT;
     DeviceGuard g(ctx->device);
     return launch_blockscale_matmul(ctx, *a, static_cast<cudaStream_t>(stream));
+}
+
+int adloco_blockscale_dequantize(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t cols, const void* q,
+                                 int64_t q_stride, const uint8_t* scale, int64_t scale_stride, void* x, int64_t x_stride,
+                                 void* stream) {
+    if (!ctx || !q || !scale || !x || rows < 1 || cols < 1 || x_stride < cols || x == q) return ADLOCO_ERR_INVALID_ARG;
+    if (!known(dtype) || too_large({rows, cols})) return ADLOCO_ERR_UNSUPPORTED;
+    if (!elem_aligned(x, dtype)) return ADLOCO_ERR_ALIGNMENT;
+    int rc = check_bytes(q, q_stride, cols);
+    if (rc == ADLOCO_OK) rc = check_row_scales(scale, scale_stride, cols);
+    if (rc != ADLOCO_OK) return rc;
+    DeviceGuard g(ctx->device);
+    return launch_blockscale_dequantize(ctx, dtype == ADLOCO_BF16, rows, cols, q, q_stride, scale, scale_stride, x, x_stride,
+                                        static_cast<cudaStream_t>(stream));
+}
+
+int adloco_linear(adloco_ctx* ctx, const adloco_linear_args* a, void* stream) {
+    if (!ctx || !a || !a->y || a->M < 1 || a->N < 1 || a->K < 1 || !known_act(a->activation)) return ADLOCO_ERR_INVALID_ARG;
+    if (!known(a->out_dtype) || too_large({a->M, a->N, a->K})) return ADLOCO_ERR_UNSUPPORTED;
+    if (a->y_stride < a->N || (a->residual && a->residual_stride < a->N)) return ADLOCO_ERR_INVALID_ARG;
+    int rc = check_operand(a->x, a->x_stride, a->K);
+    if (rc == ADLOCO_OK) rc = check_operand(a->w, a->w_stride, a->K);
+    if (rc == ADLOCO_OK) rc = check_kept(a->z, a->N);
+    if (rc != ADLOCO_OK) return rc;
+    const int64_t es = (int64_t)elem_bytes(a->out_dtype);
+    if (!apart({{a->y, a->y_stride, es}, matrix_of(a->z)}, {{a->residual, a->residual_stride, es}}, {a->x, a->w, a->bias}, a->M)) return ADLOCO_ERR_INVALID_ARG;
+    if (!elem_aligned(a->y, a->out_dtype) || !elem_aligned(a->residual, a->out_dtype) || !elem_aligned(a->bias, ADLOCO_F32)) return ADLOCO_ERR_ALIGNMENT;
+    DeviceGuard g(ctx->device);
+    return launch_linear(ctx, *a, static_cast<cudaStream_t>(stream));
+}
+
+int adloco_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args* a, void* stream) {
+    if (!ctx || !a || !a->dx || a->M < 1 || a->N < 1 || a->K < 1 || !known_act(a->activation)) return ADLOCO_ERR_INVALID_ARG;
+    if (!known(a->out_dtype) || too_large({a->M, a->N, a->K})) return ADLOCO_ERR_UNSUPPORTED;
+    if (a->dx_stride < a->K || (a->residual && a->residual_stride < a->K) || (a->a && a->a_stride < a->K)) return ADLOCO_ERR_INVALID_ARG;
+    if (!a->z.p && (a->activation != ADLOCO_ACT_NONE || a->a)) return ADLOCO_ERR_INVALID_ARG;
+    int rc = check_operand(a->dy, a->dy_stride, a->N);
+    if (rc == ADLOCO_OK) rc = check_operand(a->w, a->w_stride, a->K);
+    if (rc == ADLOCO_OK) rc = check_kept(a->z, a->K);
+    if (rc != ADLOCO_OK) return rc;
+    const int64_t es = (int64_t)elem_bytes(a->out_dtype);
+    if (!apart({{a->dx, a->dx_stride, es}, {a->a, a->a_stride, 2}}, {{a->residual, a->residual_stride, es}, matrix_of(a->z)}, {a->dy, a->w}, a->M))
+        return ADLOCO_ERR_INVALID_ARG;
+    if (!elem_aligned(a->dx, a->out_dtype) || !elem_aligned(a->residual, a->out_dtype) || !elem_aligned(a->a, ADLOCO_BF16)) return ADLOCO_ERR_ALIGNMENT;
+    DeviceGuard g(ctx->device);
+    return launch_linear_backward(ctx, *a, static_cast<cudaStream_t>(stream));
+}
+
+int adloco_gated_linear(adloco_ctx* ctx, const adloco_gated_linear_args* a, void* stream) {
+    if (!ctx || !a || !a->a || a->M < 1 || a->d < 1 || a->f < 1 || !known_act(a->activation) || a->a_stride < a->f) return ADLOCO_ERR_INVALID_ARG;
+    if (too_large({a->M, a->d, a->f})) return ADLOCO_ERR_UNSUPPORTED;
+    if (!a->gate.p != !a->up.p || !a->gate.scale != !a->up.scale) return ADLOCO_ERR_INVALID_ARG;
+    int rc = check_operand(a->x, a->x_stride, a->d);
+    if (rc == ADLOCO_OK) rc = check_operand(a->w_gate, a->w_gate_stride, a->d);
+    if (rc == ADLOCO_OK) rc = check_operand(a->w_up, a->w_up_stride, a->d);
+    if (rc == ADLOCO_OK) rc = check_kept(a->gate, a->f);
+    if (rc == ADLOCO_OK) rc = check_kept(a->up, a->f);
+    if (rc != ADLOCO_OK) return rc;
+    if (!apart({{a->a, a->a_stride, 2}, matrix_of(a->gate), matrix_of(a->up)}, {}, {a->x, a->w_gate, a->w_up}, a->M)) return ADLOCO_ERR_INVALID_ARG;
+    if (!elem_aligned(a->a, ADLOCO_BF16)) return ADLOCO_ERR_ALIGNMENT;
+    DeviceGuard g(ctx->device);
+    return launch_gated_linear(ctx, *a, static_cast<cudaStream_t>(stream));
+}
+
+int adloco_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_backward_args* a, void* stream) {
+    if (!ctx || !a || !a->gate.p || !a->up.p || !a->d_gate || !a->d_up || a->M < 1 || a->d < 1 || a->f < 1 || !known_act(a->activation))
+        return ADLOCO_ERR_INVALID_ARG;
+    if (too_large({a->M, a->d, a->f})) return ADLOCO_ERR_UNSUPPORTED;
+    if (!a->gate.scale != !a->up.scale || a->d_gate_stride < a->f || a->d_up_stride < a->f || (a->a && a->a_stride < a->f)) return ADLOCO_ERR_INVALID_ARG;
+    int rc = check_operand(a->dy, a->dy_stride, a->d);
+    if (rc == ADLOCO_OK) rc = check_operand(a->w_down, a->w_down_stride, a->f);
+    if (rc == ADLOCO_OK) rc = check_kept(a->gate, a->f);
+    if (rc == ADLOCO_OK) rc = check_kept(a->up, a->f);
+    if (rc != ADLOCO_OK) return rc;
+    if (!apart({{a->d_gate, a->d_gate_stride, 2}, {a->d_up, a->d_up_stride, 2}, {a->a, a->a_stride, 2}}, {matrix_of(a->gate), matrix_of(a->up)},
+               {a->dy, a->w_down}, a->M))
+        return ADLOCO_ERR_INVALID_ARG;
+    if (!elem_aligned(a->d_gate, ADLOCO_BF16) || !elem_aligned(a->d_up, ADLOCO_BF16) || !elem_aligned(a->a, ADLOCO_BF16)) return ADLOCO_ERR_ALIGNMENT;
+    DeviceGuard g(ctx->device);
+    return launch_gated_linear_backward(ctx, *a, static_cast<cudaStream_t>(stream));
+}
+
+int adloco_token_logprobs(adloco_ctx* ctx, const adloco_token_logprobs_args* a, void* stream) {
+    if (!ctx || !a || !a->logits || a->rows < 1 || a->V < 1 || a->logits_stride < a->V) return ADLOCO_ERR_INVALID_ARG;
+    if (!known(a->dtype) || too_large({a->rows, a->V}) || a->top > 64) return ADLOCO_ERR_UNSUPPORTED;
+    if (a->top < 0 || a->top > a->V || (a->top > 0) != (a->top_values != nullptr) || (a->top > 0) != (a->top_ids != nullptr)) return ADLOCO_ERR_INVALID_ARG;
+    if (a->logp && !a->targets) return ADLOCO_ERR_INVALID_ARG;
+    if (!a->logp && !a->entropy && !a->lse && a->top == 0) return ADLOCO_ERR_INVALID_ARG;
+    if (!elem_aligned(a->logits, a->dtype) || !elem_aligned(a->targets, ADLOCO_F32) || !elem_aligned(a->logp, ADLOCO_F32) ||
+        !elem_aligned(a->entropy, ADLOCO_F32) || !elem_aligned(a->lse, ADLOCO_F32) || !elem_aligned(a->top_values, ADLOCO_F32) ||
+        !elem_aligned(a->top_ids, ADLOCO_F32))
+        return ADLOCO_ERR_ALIGNMENT;
+    DeviceGuard g(ctx->device);
+    return launch_token_logprobs(ctx, *a, static_cast<cudaStream_t>(stream));
+}
+
+int adloco_token_logprobs_backward(adloco_ctx* ctx, const adloco_token_logprobs_backward_args* a, void* stream) {
+    if (!ctx || !a || !a->logits || !a->targets || !a->lse || !a->d_logp || !a->d_logits || a->rows < 1 || a->V < 1) return ADLOCO_ERR_INVALID_ARG;
+    if (!known(a->dtype) || too_large({a->rows, a->V})) return ADLOCO_ERR_UNSUPPORTED;
+    if (a->logits_stride < a->V || a->d_logits_stride < a->V || !a->entropy != !a->d_entropy ||
+        !in_step(a->d_logits, a->d_logits_stride, a->logits, a->logits_stride, a->rows))
+        return ADLOCO_ERR_INVALID_ARG;
+    if (!elem_aligned(a->logits, a->dtype) || !elem_aligned(a->d_logits, a->dtype) || !elem_aligned(a->targets, ADLOCO_F32) ||
+        !elem_aligned(a->lse, ADLOCO_F32) || !elem_aligned(a->d_logp, ADLOCO_F32) || !elem_aligned(a->entropy, ADLOCO_F32) ||
+        !elem_aligned(a->d_entropy, ADLOCO_F32))
+        return ADLOCO_ERR_ALIGNMENT;
+    DeviceGuard g(ctx->device);
+    return launch_token_logprobs_backward(ctx, *a, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

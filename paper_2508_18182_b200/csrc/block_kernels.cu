@@ -7,6 +7,7 @@
 #include <atomic>
 
 #include "common.cuh"
+#include "e4m3.cuh"
 #include "ptx.cuh"
 
 namespace adloco {
@@ -230,18 +231,6 @@ struct FastDiv {
 };
 
 // ---- 8-bit blocks -------------------------------------------------------------------------
-// The scale's byte from the bits of the block's largest magnitude: with that magnitude m 2^k, 1 <= m < 2, and
-// 448 = 1.75 2^8, the smallest whole e with m 2^k <= 448 2^e is k - 8, or k - 7 where m > 1.75; adding
-// 0x1fffff to the fraction carries into the exponent exactly when m > 1.75.  An Inf or NaN (compared as whole
-// numbers, so that a NaN is not lost in a maximum) gives 255.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) {
-    if (amax_bits >= 0x7f800000u) return 255u;
-    if (amax_bits == 0u) return 127u;
-    const int b = (int)((amax_bits + 0x1fffffu) >> 23) - 8;
-    return b < 0 ? 0u : (uint32_t)b;
-}
-// 1 / scale: a power of two, so multiplying by it is exact (byte 0..247 of a finite block)
-__device__ __forceinline__ float inv_scale(uint32_t byte) { return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23); }
 __device__ __forceinline__ uint32_t abs_max8(const F2 (&v)[4]) {
     uint32_t m = 0;
 #pragma unroll

@@ -4,6 +4,8 @@
 #include <atomic>
 
 #include "common.cuh"
+#include "e4m3.cuh"
+#include "gemm_parts.cuh"
 #include "ptx.cuh"
 
 namespace adloco {
@@ -11,16 +13,6 @@ namespace adloco {
 using namespace ptx;
 
 namespace {
-
-constexpr uint64_t kPairLeaveNs = 1000000ull;      // 1 ms: a CTA pair leaving after a time-out; copies in flight land long before
-constexpr uint64_t kLeaveLimitNs = 50000000ull;    // 50 ms per barrier while leaving after a time-out
-
-struct Ring {
-    uint32_t stage = 0, phase = 0;
-    __device__ __forceinline__ void advance(uint32_t n) {
-        if (++stage == n) { stage = 0; phase ^= 1u; }
-    }
-};
 
 struct MatArgs {
     int M, N, K, kb;                 // kb: blocks of 128 along K
@@ -37,10 +29,6 @@ struct MatArgs {
     uint64_t wait_ns;
 };
 
-__device__ __forceinline__ uint32_t pack_bf16(uint32_t a, uint32_t b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(a), __uint_as_float(b));
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
 // An epilogue warp's box of shared memory: 32 rows of 128 bytes (64 bf16 or 32 fp32 columns), piece j of row i at piece
 // j ^ (i mod 8), so that a thread's row written and a row's pieces read by neighbouring lanes fall on all banks.
 constexpr int kBoxBytes = 32 * 128;
@@ -105,12 +93,6 @@ __device__ __forceinline__ void flush_box(const MatArgs& a, uint32_t box, int la
         }
     }
     __syncwarp();
-}
-
-// A wait of the whole warp, which goes on (or gives up) together.
-template <bool CLUSTER>
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abortp, uint64_t limit_ns) {
-    return __all_sync(0xffffffffu, mbar_wait<CLUSTER>(bar, parity, abortp, limit_ns)) != 0;
 }
 
 // The tiles of one worker: dealt round, the tiles along N fastest, so that all workers sit on the same few rows of A at a
@@ -593,9 +575,6 @@ __device__ __forceinline__ uint4 bytes16(const uint8_t* row, int k, int K) {    
         if (k + i < K) w[i >> 2] |= (uint32_t)row[k + i] << (8 * (i & 3));
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ float scale_of(uint32_t byte) {                          // 2^(byte - 127); 255: NaN
-    return byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? 0x1p-127f : __uint_as_float(byte << 23);
-}
 __device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -675,25 +654,6 @@ __global__ void __launch_bounds__(32 * FR_MAX_WARPS) blockscale_few_kernel(const
         if (a.out_bf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
         else static_cast<float*>(a.out)[at] = v;
     }
-}
-
-// matrix [rows, cols] of `es`-byte elements with a pitch in elements, as a 2-D map with a box of box_rows rows of
-// box_cols elements (128 bytes), 128-byte swizzle; elements outside the matrix read as zero and are not written
-int make_map(adloco_ctx* ctx, CUtensorMap* m, CUtensorMapDataType type, int64_t es, const void* base, int64_t rows, int64_t cols,
-             int64_t pitch, uint32_t box_cols, uint32_t box_rows) {
-    TensorMapEncode fn = tensor_map_encode(ctx);
-    if (!fn) return ADLOCO_ERR_CUDA;
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)(pitch * es)};
-    const cuuint32_t box[2] = {box_cols, box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = fn(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        snprintf(ctx->cuda_err, sizeof(ctx->cuda_err), "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
-        return ADLOCO_ERR_CUDA;
-    }
-    return ADLOCO_OK;
 }
 
 }  // namespace

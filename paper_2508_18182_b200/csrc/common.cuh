@@ -277,5 +277,15 @@ int launch_blockscale_quantize_weight(adloco_ctx* ctx, int bf16, int64_t rows, i
                                       int64_t scale_stride, cudaStream_t st);
 // implemented in blockscale_gemm.cu
 int launch_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_args& a, cudaStream_t st);
+// implemented in dense_gemm.cu
+int launch_linear(adloco_ctx* ctx, const adloco_linear_args& a, cudaStream_t st);
+int launch_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args& a, cudaStream_t st);
+int launch_gated_linear(adloco_ctx* ctx, const adloco_gated_linear_args& a, cudaStream_t st);
+int launch_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_backward_args& a, cudaStream_t st);
+// implemented in token_kernels.cu
+int launch_blockscale_dequantize(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const void* q, int64_t q_stride,
+                                 const uint8_t* scale, int64_t scale_stride, void* x, int64_t x_stride, cudaStream_t st);
+int launch_token_logprobs(adloco_ctx* ctx, const adloco_token_logprobs_args& a, cudaStream_t st);
+int launch_token_logprobs_backward(adloco_ctx* ctx, const adloco_token_logprobs_backward_args& a, cudaStream_t st);
 
 }  // namespace adloco

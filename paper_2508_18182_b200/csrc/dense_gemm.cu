@@ -1,0 +1,948 @@
+// Linear layers in bf16 with what follows them in the product's epilogue: bias, activation and residual; the gated pair
+// of projections act(x Wg^T) * (x Wu^T); and the way back through either,
+//   dx = (dy W) act'(z)      d_gate = (dy Wd) up act'(gate),  d_up = (dy Wd) act(gate).
+// What the backward pass needs (z, or gate and up) is kept in bf16 or in 8 bits with a power-of-two scale for each block
+// of 128 of a row, written by the forward epilogue and read by the backward one; the layer's input is recomputed there.
+#include <atomic>
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "e4m3.cuh"
+#include "gemm_parts.cuh"
+#include "ptx.cuh"
+
+namespace adloco {
+
+using namespace ptx;
+
+namespace {
+
+enum Kind { LINEAR, LINEAR_BACK, GATED, GATED_BACK };
+enum Form { kNone, kBf16, kF32, kBytes };
+enum { IN0, IN1, OUT0, OUT1, OUT2, SIDES };
+
+// An elementwise operand or output of the epilogue.  Its box: 32 rows x 32 columns in shared memory, one for the even
+// chunks of 32 columns and one for the odd ones (the same one where the epilogue does not fetch ahead).
+struct Side {
+    void* p = nullptr;
+    int64_t pitch = 0;                // elements
+    uint8_t* scale = nullptr;
+    int64_t scale_pitch = 0;
+    int form = kNone;
+    int tma = 0;                      // 1: boxes go by TMA; 0: by the warp's own accesses, whole 16-byte pieces where `pieces`
+    int pieces = 0;
+    uint32_t box[2] = {0, 0};
+};
+
+struct GemmArgs {
+    int M, N, K;                      // output rows, output columns (of each projection), contraction
+    int kb;                           // blocks of 64 along K
+    int tiles_n, tiles;
+    int act;
+    int stages;
+    uint32_t warp_bytes;              // boxes of one epilogue warp
+    uint32_t in_bytes;                // that arrive by TMA for one chunk
+    const float* bias;
+    Side side[SIDES];
+    int* status;
+    uint64_t wait_ns;
+};
+struct Maps { CUtensorMap a, b[2], side[SIDES]; };
+
+// ---- activations ------------------------------------------------------------------------------
+// Value and derivative in fp32.  The logistic function takes the fast exponential and division (relative error 2^-21,
+// against the 2^-9 of a result in bf16); the error function is CUDA's.
+template <int ACT> struct Act {};
+__device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float value(Act<ADLOCO_ACT_NONE>, float z) { return z; }
+__device__ __forceinline__ float value(Act<ADLOCO_ACT_RELU>, float z) { return z < 0.f ? 0.f : z; }
+__device__ __forceinline__ float value(Act<ADLOCO_ACT_GELU>, float z) { return z * fmaf(0.5f, erff(z * 0.70710678f), 0.5f); }
+// (1 + tanh(v)) / 2 is the logistic function of 2 v, v = sqrt(2 / pi) (z + 0.044715 z^3)
+constexpr float kTanhSlope = 1.5957691216f;
+__device__ __forceinline__ float value(Act<ADLOCO_ACT_GELU_TANH>, float z) { return z * logistic(kTanhSlope * z * fmaf(0.044715f * z, z, 1.f)); }
+__device__ __forceinline__ float value(Act<ADLOCO_ACT_SILU>, float z) { return z * logistic(z); }
+
+__device__ __forceinline__ float slope(Act<ADLOCO_ACT_NONE>, float z, float& a) { a = z; return 1.f; }
+__device__ __forceinline__ float slope(Act<ADLOCO_ACT_RELU>, float z, float& a) { a = z < 0.f ? 0.f : z; return z > 0.f ? 1.f : z == z ? 0.f : z; }
+__device__ __forceinline__ float slope(Act<ADLOCO_ACT_GELU>, float z, float& a) {
+    const float h = fmaf(0.5f, erff(z * 0.70710678f), 0.5f);
+    a = z * h;
+    return fmaf(z * 0.39894228f, __expf(-0.5f * z * z), h);
+}
+__device__ __forceinline__ float slope(Act<ADLOCO_ACT_GELU_TANH>, float z, float& a) {
+    const float h = logistic(kTanhSlope * z * fmaf(0.044715f * z, z, 1.f));
+    a = z * h;
+    return fmaf(a * (1.f - h), kTanhSlope * fmaf(0.134145f * z, z, 1.f), h);
+}
+__device__ __forceinline__ float slope(Act<ADLOCO_ACT_SILU>, float z, float& a) {
+    const float h = logistic(z);
+    a = z * h;
+    return fmaf(a, 1.f - h, h);
+}
+// f with the activation as a type: one branch for a group of elements
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    switch (act) {
+        case ADLOCO_ACT_RELU: f(Act<ADLOCO_ACT_RELU>{}); break;
+        case ADLOCO_ACT_GELU: f(Act<ADLOCO_ACT_GELU>{}); break;
+        case ADLOCO_ACT_GELU_TANH: f(Act<ADLOCO_ACT_GELU_TANH>{}); break;
+        case ADLOCO_ACT_SILU: f(Act<ADLOCO_ACT_SILU>{}); break;
+        default: f(Act<ADLOCO_ACT_NONE>{});
+    }
+}
+
+// ---- boxes --------------------------------------------------------------------------------------
+// A row of a box is P pieces of 16 bytes (2 of bytes, 4 of bf16, 8 of fp32), swizzled as the tensor map of that width does
+// it, so that neighbouring rows' equal pieces fall on different banks.
+__device__ __forceinline__ int pieces_of(int form) { return form == kF32 ? 8 : form == kBf16 ? 4 : 2; }
+template <int P>
+__device__ __forceinline__ uint32_t piece_at(uint32_t box, int row, int piece) {
+    return box + (uint32_t)row * (16u * P) + ((uint32_t)(piece ^ ((row * P >> 3) & (P - 1))) << 4);
+}
+__device__ __forceinline__ uint32_t piece_at(int form, uint32_t box, int row, int piece) {
+    return form == kF32 ? piece_at<8>(box, row, piece) : form == kBf16 ? piece_at<4>(box, row, piece) : piece_at<2>(box, row, piece);
+}
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void pair_to_floats(uint32_t w, float& a, float& b) {
+    a = __uint_as_float(w << 16);
+    b = __uint_as_float(w & 0xffff0000u);
+}
+__device__ __forceinline__ void bytes_to_floats(uint32_t w, float s, float* v) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> (16 * h)), __NV_E4M3);
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r));
+        v[2 * h] = f.x * s;
+        v[2 * h + 1] = f.y * s;
+    }
+}
+// columns 8 g .. 8 g + 7 of this lane's row; s: the scale of bytes
+__device__ __forceinline__ void read8(int form, uint32_t box, int row, int g, float s, float (&v)[8]) {
+    if (form == kBf16) {
+        const uint4 w = lds16(piece_at<4>(box, row, g));
+        pair_to_floats(w.x, v[0], v[1]); pair_to_floats(w.y, v[2], v[3]);
+        pair_to_floats(w.z, v[4], v[5]); pair_to_floats(w.w, v[6], v[7]);
+    } else if (form == kF32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint4 w = lds16(piece_at<8>(box, row, 2 * g + h));
+            v[4 * h] = __uint_as_float(w.x); v[4 * h + 1] = __uint_as_float(w.y);
+            v[4 * h + 2] = __uint_as_float(w.z); v[4 * h + 3] = __uint_as_float(w.w);
+        }
+    } else {
+        uint32_t a, b;
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(piece_at<2>(box, row, g >> 1) + 8u * (g & 1)) : "memory");
+        bytes_to_floats(a, s, v);
+        bytes_to_floats(b, s, v + 4);
+    }
+}
+__device__ __forceinline__ uint32_t pack(float a, float b) { return pack_bf16(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ void write8(int form, uint32_t box, int row, int g, float inv, const float (&v)[8]) {
+    if (form == kBf16) {
+        st_shared_v4(piece_at<4>(box, row, g), pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]), pack(v[6], v[7]));
+    } else if (form == kF32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            st_shared_v4(piece_at<8>(box, row, 2 * g + h), __float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]),
+                         __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3]));
+    } else {
+        uint32_t h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            h[i] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * i] * inv, v[2 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+        asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(piece_at<2>(box, row, g >> 1) + 8u * (g & 1)), "r"(h[0] | (h[1] << 16)),
+                     "r"(h[2] | (h[3] << 16)) : "memory");
+    }
+}
+// A box by the warp's own accesses: where rows do not start on 16-byte boundaries (element by element along rows), or
+// where a row's last 16-byte piece is not whole, which a TMA store would write in full.
+__device__ __forceinline__ void box_in(const Side& s, uint32_t box, int lane, int row0, int col, int M, int N) {
+    const int rows = min(32, M - row0);
+    for (int row = 0; row < rows; ++row) {
+        const int64_t at = (int64_t)(row0 + row) * s.pitch + col + lane;
+        if (s.form == kF32) {
+            const uint32_t v = col + lane < N ? static_cast<const uint32_t*>(s.p)[at] : 0u;
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(piece_at<8>(box, row, lane >> 2) + 4u * (lane & 3)), "r"(v) : "memory");
+        } else {
+            const unsigned short v = col + lane < N ? static_cast<const unsigned short*>(s.p)[at] : (unsigned short)0;
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(piece_at<4>(box, row, lane >> 3) + 2u * (lane & 7)), "h"(v) : "memory");
+        }
+    }
+    __syncwarp();
+}
+__device__ __forceinline__ void box_out(const Side& s, uint32_t box, int lane, int row0, int col, int M, int N) {
+    __syncwarp();
+    const int es = s.form == kF32 ? 4 : s.form == kBf16 ? 2 : 1, P = pieces_of(s.form), each = 16 / es;
+    char* out = static_cast<char*>(s.p) + ((int64_t)row0 * s.pitch + col) * es;
+    const int64_t pitch = s.pitch * es;
+    if (s.pieces) {
+        const int piece = lane & (P - 1), c = piece * each;
+        for (int row = lane / P; row < 32; row += 32 / P) {
+            if (row0 + row >= M || col + c >= N) continue;
+            const uint4 v = lds16(piece_at(s.form, box, row, piece));
+            char* to = out + row * pitch + piece * 16;
+            if (col + c + each <= N) {
+                *reinterpret_cast<uint4*>(to) = v;
+            } else {
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                for (int b = 0; b < (N - col - c) * es; ++b) to[b] = (char)(w[b >> 2] >> (8 * (b & 3)));
+            }
+        }
+    } else {
+        const int rows = min(32, M - row0);
+        for (int row = 0; row < rows && col + lane < N; ++row) {
+            const uint32_t from = piece_at(s.form, box, row, lane / each) + (uint32_t)((lane & (each - 1)) * es);
+            if (es == 4) {
+                uint32_t v;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(from) : "memory");
+                reinterpret_cast<uint32_t*>(out + row * pitch)[lane] = v;
+            } else {
+                unsigned short v;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(from) : "memory");
+                reinterpret_cast<unsigned short*>(out + row * pitch)[lane] = v;
+            }
+        }
+    }
+    fence_proxy_async_smem();                          // a fetch may write the box next
+    __syncwarp();
+}
+
+// the largest magnitude, a NaN included
+__device__ __forceinline__ float larger(float m, float v) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(fabsf(v)));
+    return r;
+}
+
+// ---- the tile kernel ------------------------------------------------------------------------------
+// Persistent, 320 threads: warp 0 brings tiles by TMA, warp 1 issues the MMAs, warps 2-9 are the epilogue.  PAIR: 256 x BN
+// tiles shared by the two CTAs of a cluster (cta_group::2): CTA r holds rows 128 r .. + 127 of the tile in its tensor memory
+// and loads those rows of A and half of B's; otherwise 128 x BN tiles of one CTA.  A stage is 64 of K.  Two accumulators
+// take turns, so that a tile's epilogue runs beside the next tile's MMAs.  B is a weight [N, K] forward, its rows along the
+// tensor cores' K; backward the same weight is read as it lies, its rows along the contraction (MN-major).
+// GATED: the tile's columns are BN / 2 of each projection (in a pair, CTA r brings projection r), so a thread of the epilogue
+// has both numbers of an output.
+// LONG: the tensor cores cut off each sum's low bits (relative error 1e-6 after 1000 terms, growing with their number); with
+// fp32 outputs the sum of every 512 of K is added up in registers instead, rounded to nearest.
+// The epilogue's eight warps each own 32 rows and half the columns, in chunks of 32: the operands of the next chunk arrive by
+// TMA while this one is computed, the results leave by TMA.
+constexpr int DG_THREADS = 320, DG_EPI = 8;
+constexpr int DG_A_BYTES = 128 * 128;
+constexpr int DG_MAX_STAGES = 8;
+constexpr int DG_SEGMENT = 8;                              // blocks of K in one sum of a LONG tile
+constexpr int DG_BAR_BYTES = 512;
+constexpr int DG_SMEM = 232448 - 256;                      // what a block can have, less the kernel's own few words
+template <bool PAIR, int BN>
+__host__ __device__ constexpr int dg_stage_bytes() { return DG_A_BYTES + (PAIR ? BN / 2 : BN) * 128; }
+
+// The tiles of one worker: dealt round, the tiles along N fastest, so that all workers sit on the same rows of A at a time.
+struct Walk {
+    int left, m, n, step_m, step_n, line;
+    __device__ __forceinline__ Walk(const GemmArgs& a, int worker, int workers) : line(a.tiles_n) {
+        left = worker < a.tiles ? (a.tiles - worker - 1) / workers + 1 : 0;
+        m = worker / line;
+        n = worker % line;
+        step_m = workers / line;
+        step_n = workers % line;
+    }
+    __device__ __forceinline__ bool more() const { return left > 0; }
+    __device__ __forceinline__ void next() {
+        --left;
+        m += step_m;
+        n += step_n;
+        if (n >= line) { n -= line; ++m; }
+    }
+};
+
+template <int KIND, bool PAIR, int BN, bool LONG>
+__global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmArgs a) {
+    constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK;
+    constexpr int COLS = TWO ? BN / 2 : BN;                // output columns of a tile
+    constexpr int TM = PAIR ? 256 : 128;
+    constexpr int CHUNKS = COLS / 64;                      // of an epilogue warp
+    constexpr int STAGE = dg_stage_bytes<PAIR, BN>();
+    constexpr int B_ROWS = PAIR ? BN / 2 : BN;             // of the weight (or of its columns, backward) in a CTA's stage
+    static_assert(CHUNKS >= 1 && (!BACK || B_ROWS % 64 == 0), "a chunk is 32 columns, a box of the weight's columns 64");
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t boxes = smem_base + (uint32_t)a.stages * STAGE;
+    const uint32_t bars = boxes + DG_EPI * a.warp_bytes;
+    auto full_bar = [&](uint32_t s) { return bars + 8u * s; };
+    auto empty_bar = [&](uint32_t s) { return bars + 8u * (DG_MAX_STAGES + s); };
+    auto acc_full = [&](uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + s); };
+    auto acc_empty = [&](uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 2 + s); };
+    auto in_bar = [&](uint32_t w, uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * w + s); };
+    const uint32_t drain_bar = bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * DG_EPI);
+    static_assert(8 * (2 * DG_MAX_STAGES + 5 + 2 * DG_EPI) <= DG_BAR_BYTES, "barriers");
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // warp: known to be uniform
+    const uint32_t rank = PAIR ? cluster_cta_rank() : 0;       // 0: the CTA that issues the MMAs
+    Walk walk(a, PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x);
+    const uint32_t stages = (uint32_t)a.stages;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (uint32_t s = 0; s < stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+        for (uint32_t s = 0; s < 2; ++s) { mbar_init(acc_full(s), 1); mbar_init(acc_empty(s), (PAIR ? 2 : 1) * DG_EPI); }
+        for (uint32_t w = 0; w < DG_EPI; ++w)
+            for (uint32_t s = 0; s < 2; ++s) mbar_init(in_bar(w, s), 1);
+        mbar_init(drain_bar, 1);
+        fence_barrier_init();
+        prefetch_tmap(&maps.a);
+        prefetch_tmap(&maps.b[0]);
+        if (TWO) prefetch_tmap(&maps.b[1]);
+        for (int i = 0; i < SIDES; ++i)
+            if (a.side[i].tma) prefetch_tmap(&maps.side[i]);
+    }
+    if (warp == 1) {
+        if (PAIR) { tmem_alloc_pair(smem_u32(&tmem_slot), 512); tmem_relinquish_pair(); }
+        else { tmem_alloc(smem_u32(&tmem_slot), 512); tmem_relinquish(); }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();                              // the peer's barriers exist before anything is signalled on them
+    tc_fence_after();
+    after_predecessor();
+    const uint32_t tmem = tmem_slot;
+    volatile int* abortp = &abort_flag;
+    const int segments = LONG ? (a.kb + DG_SEGMENT - 1) / DG_SEGMENT : 1;
+
+    if (warp == 0) {
+        // ---------------- TMA producer, one per CTA ----------------
+        if (lane == 0) {
+            Ring ps;
+            uint32_t issued = 0;
+            bool ok = true;
+            for (; ok && walk.more(); walk.next()) {
+                const int m0 = walk.m * TM + (int)rank * 128, n0 = walk.n * COLS;
+                for (int k = 0; k < a.kb; ++k) {
+                    if (!mbar_wait(empty_bar(ps.stage), ps.phase ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
+                    const uint32_t sA = smem_base + ps.stage * STAGE, sB = sA + DG_A_BYTES;
+                    const uint32_t bar = PAIR ? map_to_cta(full_bar(ps.stage), 0) : full_bar(ps.stage);
+                    if (rank == 0) mbar_arrive_expect_tx(full_bar(ps.stage), (PAIR ? 2 : 1) * STAGE);
+                    auto load = [&](uint32_t dst, const CUtensorMap* m, int c0, int c1) {
+                        if (PAIR) tma_load_2d_pair(dst, m, bar, c0, c1);
+                        else tma_load_2d(dst, m, bar, c0, c1);
+                    };
+                    load(sA, &maps.a, k * 64, m0);
+                    if (TWO) {
+                        if (PAIR) {
+                            load(sB, &maps.b[rank], k * 64, n0);
+                        } else {
+                            load(sB, &maps.b[0], k * 64, n0);
+                            load(sB + COLS * 128, &maps.b[1], k * 64, n0);
+                        }
+                    } else if (!BACK) {
+                        load(sB, &maps.b[0], k * 64, n0 + (int)rank * B_ROWS);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < B_ROWS; c += 64) load(sB + c * 128, &maps.b[0], n0 + (int)rank * B_ROWS + c, k * 64);
+                    }
+                    ++issued;
+                    ps.advance(stages);
+                }
+            }
+            if (!ok) {
+                if (PAIR) {
+                    // leaving after a time-out: the byte counts of copies in flight complete on the even CTA's barriers, which
+                    // the odd CTA cannot wait on: both sit out a grace period far beyond the flight time of a copy
+                    st_cluster_u32(map_to_cta(smem_u32(&abort_flag), rank ^ 1u), 1u);
+                    const uint64_t t0 = globaltimer_ns();
+                    while (globaltimer_ns() - t0 < kPairLeaveNs) { }
+                } else {
+                    Ring q = ps;                               // the copies still in flight land first
+                    const uint32_t back = issued < stages ? issued : stages;
+                    for (uint32_t r = 0; r < back; ++r) {
+                        if (q.stage == 0) { q.stage = stages - 1; q.phase ^= 1u; } else { --q.stage; }
+                        int never = 0;
+                        mbar_wait(full_bar(q.stage), q.phase, &never, kLeaveLimitNs);
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer (of a pair the even CTA's; the whole warp keeps step, one lane issues) ----------------
+        if (rank == 0) {
+            const bool leader = elect_one();
+            constexpr uint32_t idesc = idesc_bf16_f32(TM, BN, 0, BACK ? 1 : 0);
+            const uint64_t descA = smem_desc_sw128(0, 16, 1024);
+            const uint64_t descB = BACK ? smem_desc_sw128(0, 64 * 128, 1024) : descA;
+            Ring ps;
+            uint32_t n = 0;
+            bool ok = true;
+            for (; ok && walk.more(); walk.next()) {
+                for (int k0 = 0; ok && k0 < a.kb; ++n) {
+                    const uint32_t buf = n & 1u;
+                    const int k1 = LONG ? min(a.kb, k0 + DG_SEGMENT) : a.kb;
+                    if (!wait_warp<PAIR>(acc_empty(buf), ((n >> 1) & 1u) ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
+                    for (int k = k0; k < k1; ++k) {
+                        if (!wait_warp<false>(full_bar(ps.stage), ps.phase, abortp, a.wait_ns)) { ok = false; break; }
+                        tc_fence_after();
+                        if (leader) {
+                            const uint32_t at = smem_base + ps.stage * STAGE;
+                            const uint64_t dA = descA + (at >> 4), dB = descB + ((at + DG_A_BYTES) >> 4);
+#pragma unroll
+                            for (int kk = 0; kk < 4; ++kk) {
+                                // 16 of K further: 32 bytes along a row, or 16 rows of 128 bytes
+                                const uint64_t db = dB + (BACK ? 128 : 2) * kk;
+                                if (PAIR) mma_bf16_pair(tmem + buf * BN, dA + 2 * kk, db, idesc, (k == k0 && kk == 0) ? 0u : 1u);
+                                else mma_bf16(tmem + buf * BN, dA + 2 * kk, db, idesc, (k == k0 && kk == 0) ? 0u : 1u);
+                            }
+                            if (PAIR) mma_commit_pair(empty_bar(ps.stage), 3);
+                            else mma_commit(empty_bar(ps.stage));
+                        }
+                        __syncwarp();
+                        ps.advance(stages);
+                    }
+                    if (ok && leader) {
+                        if (PAIR) mma_commit_pair(acc_full(buf), 3);
+                        else mma_commit(acc_full(buf));
+                    }
+                    __syncwarp();
+                    k0 = k1;
+                }
+            }
+            if (!ok && leader) {
+                if (PAIR) {
+                    st_cluster_u32(map_to_cta(smem_u32(&abort_flag), 1u), 1u);
+                    mma_commit_pair(drain_bar, 1);
+                } else {
+                    mma_commit(drain_bar);
+                }
+                int never = 0;
+                mbar_wait(drain_bar, 0, &never, kLeaveLimitNs);
+            }
+            __syncwarp();
+        }
+    } else {
+        // ---------------- epilogue ----------------
+        const uint32_t q = warp & 3, half = (uint32_t)(warp - 2) >> 2, w = (uint32_t)(warp - 2);
+        const uint32_t acc_empty_0 = PAIR ? map_to_cta(acc_empty(0), 0) : acc_empty(0);
+        const uint32_t mine = boxes + w * a.warp_bytes;
+        const uint32_t lane_tmem = tmem + ((q * 32u) << 16);
+        const int first = (int)half * (COLS / 2);              // of the tile's columns
+        const bool fetches = a.in_bytes != 0;
+        uint32_t n = 0, chunk = 0;                             // accumulators and chunks so far
+        uint32_t fetched = 0;                                  // chunks whose operands have been asked for
+        auto row_of = [&](const Walk& t) { return t.m * TM + (int)rank * 128 + (int)q * 32; };
+        auto col_of = [&](const Walk& t, int i) { return t.n * COLS + first + 32 * i; };
+        auto stored = [&]() {                                  // this warp's stores so far have read their boxes
+            if (lane == 0) bulk_wait_read_all();
+            __syncwarp();
+        };
+        auto fetch = [&](uint32_t c, int row, int col) {       // chunk c's operands; all lanes, boxes free
+            if (lane == 0) {
+                mbar_arrive_expect_tx(in_bar(w, c & 1u), a.in_bytes);
+                for (int i = IN0; i <= IN1; ++i)
+                    if (a.side[i].tma) tma_load_2d(mine + a.side[i].box[c & 1u], &maps.side[i], in_bar(w, c & 1u), col, row);
+            }
+            fetched = c + 1;
+        };
+        auto release = [&](uint32_t buf) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_cluster_relaxed(acc_empty_0 + 8u * buf);
+                else mbar_arrive(acc_empty_0 + 8u * buf);
+            }
+        };
+        const int form0 = a.side[OUT0].form, form1 = a.side[OUT1].form, form2 = a.side[OUT2].form;
+        const int in0 = a.side[IN0].form, in1 = a.side[IN1].form;
+        bool ok = true;
+        for (; ok && walk.more(); walk.next()) {
+            const int row0 = row_of(walk), row = row0 + lane;
+            const int valid = row0 < a.M ? min(CHUNKS, max(0, (a.N - col_of(walk, 0) + 31) / 32)) : 0;
+            if (fetches && fetched == chunk && valid > 0) {
+                stored();
+                fetch(chunk, row0, col_of(walk, 0));
+            }
+            float sum[LONG ? CHUNKS : 1][32];
+            uint32_t buf = n & 1u;
+            if (LONG) {
+#pragma unroll
+                for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sum[i][e] = 0.f;
+                for (int s = 0; s < segments; ++s, ++n) {
+                    buf = n & 1u;
+                    if (!wait_warp<false>(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < CHUNKS; ++i) {
+                        uint32_t r[32];
+                        tmem_ld32(lane_tmem + buf * BN + first + 32 * i, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) sum[i][e] += __uint_as_float(r[e]);
+                    }
+                    release(buf);
+                }
+                if (!ok) break;
+            } else {
+                if (!wait_warp<false>(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
+                tc_fence_after();
+                ++n;
+            }
+            const uint32_t acc = lane_tmem + buf * BN;
+            // the scales of what is kept in 8 bits: both warps of these rows look at all 128 columns of the block
+            float inv1 = 0.f, inv2 = 0.f;
+            if ((KIND == LINEAR || KIND == GATED) && form1 == kBytes && valid > 0) {
+                const int block = first & ~127, col0 = walk.n * COLS + block;
+                float m1 = 0.f, m2 = 0.f;
+#pragma unroll 1
+                for (int c = 0; c < (COLS < 128 ? COLS : 128); c += 32) {
+                    uint32_t r[32];
+                    tmem_ld32(acc + block + c, r);
+                    tmem_ld_wait();
+                    if (KIND == LINEAR && a.bias) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (col0 + c + e < a.N) r[e] = __float_as_uint(__uint_as_float(r[e]) + a.bias[col0 + c + e]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) m1 = larger(m1, __uint_as_float(r[e]));
+                    if (TWO) {
+                        tmem_ld32(acc + COLS + block + c, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) m2 = larger(m2, __uint_as_float(r[e]));
+                    }
+                }
+                const uint32_t s1 = scale_byte(__float_as_uint(m1)), s2 = scale_byte(__float_as_uint(m2));
+                inv1 = inv_scale(s1);
+                inv2 = inv_scale(s2);
+                if (first == block && row < a.M) {
+                    a.side[OUT1].scale[(int64_t)row * a.side[OUT1].scale_pitch + (col0 >> 7)] = (uint8_t)s1;
+                    if (TWO) a.side[OUT2].scale[(int64_t)row * a.side[OUT2].scale_pitch + (col0 >> 7)] = (uint8_t)s2;
+                }
+            }
+            // the scales of what was kept
+            float scale0 = 1.f, scale1 = 1.f;
+            if (BACK && valid > 0 && row < a.M) {
+                const int block = col_of(walk, 0) >> 7;
+                if (in0 == kBytes) scale0 = scale_of(a.side[IN0].scale[(int64_t)row * a.side[IN0].scale_pitch + block]);
+                if (in1 == kBytes) scale1 = scale_of(a.side[IN1].scale[(int64_t)row * a.side[IN1].scale_pitch + block]);
+            }
+
+            auto one_chunk = [&](int i, const float* held) -> bool {
+                const int col = col_of(walk, i);
+                const uint32_t b = chunk & 1u;
+                uint32_t r[32], u[TWO ? 32 : 1];
+                if (!LONG) {
+                    tmem_ld32(acc + first + 32 * i, r);
+                    if constexpr (TWO) tmem_ld32(acc + COLS + first + 32 * i, u);
+                }
+                stored();                                      // boxes of the chunk before this one
+                if (fetches) {
+                    const uint32_t now = chunk;
+                    if (i + 1 < valid) {
+                        fetch(now + 1, row0, col + 32);
+                    } else if (walk.left > 1) {
+                        Walk t = walk;
+                        t.next();
+                        if (row_of(t) < a.M && col_of(t, 0) < a.N) fetch(now + 1, row_of(t), col_of(t, 0));
+                    }
+                    if (!wait_warp<false>(in_bar(w, b), (now >> 1) & 1u, abortp, a.wait_ns)) return false;
+                }
+                for (int k = IN0; k <= IN1; ++k)
+                    if (a.side[k].form != kNone && !a.side[k].tma) box_in(a.side[k], mine + a.side[k].box[b], lane, row0, col, a.M, a.N);
+                if (!LONG) {
+                    tmem_ld_wait();
+                    if (i == CHUNKS - 1) release(buf);
+                }
+                const uint32_t box_in0 = mine + a.side[IN0].box[b], box_in1 = mine + a.side[IN1].box[b];
+                const uint32_t box0 = mine + a.side[OUT0].box[b], box1 = mine + a.side[OUT1].box[b], box2 = mine + a.side[OUT2].box[b];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    float v[8], x[8], y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = LONG ? held[8 * g + e] : __uint_as_float(r[8 * g + e]);
+                    if (KIND == LINEAR) {
+                        if (a.bias) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (col + 8 * g + e < a.N) v[e] += a.bias[col + 8 * g + e];
+                        }
+                        if (form1 != kNone) write8(form1, box1, lane, g, inv1, v);
+                        with_act(a.act, [&](auto t) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = value(t, v[e]);
+                        });
+                        if (in0 != kNone) {
+                            read8(in0, box_in0, lane, g, 1.f, x);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] += x[e];
+                        }
+                        write8(form0, box0, lane, g, 1.f, v);
+                    } else if (KIND == LINEAR_BACK) {
+                        if (in1 != kNone) {
+                            read8(in1, box_in1, lane, g, scale1, x);
+                            with_act(a.act, [&](auto t) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[e] *= slope(t, x[e], y[e]);
+                            });
+                            if (form1 != kNone) write8(form1, box1, lane, g, 1.f, y);
+                        }
+                        if (in0 != kNone) {
+                            read8(in0, box_in0, lane, g, 1.f, x);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] += x[e];
+                        }
+                        write8(form0, box0, lane, g, 1.f, v);
+                    } else if (KIND == GATED) {
+                        if constexpr (TWO) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(u[8 * g + e]);
+                        }
+                        if (form1 != kNone) {
+                            write8(form1, box1, lane, g, inv1, v);
+                            write8(form2, box2, lane, g, inv2, x);
+                        }
+                        with_act(a.act, [&](auto t) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = value(t, v[e]) * x[e];
+                        });
+                        write8(kBf16, box0, lane, g, 1.f, v);
+                    } else {
+                        read8(in0, box_in0, lane, g, scale0, x);
+                        read8(in1, box_in1, lane, g, scale1, y);
+                        float up[8];
+                        with_act(a.act, [&](auto t) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                float h;
+                                const float s = slope(t, x[e], h);
+                                x[e] = v[e] * y[e] * s;
+                                up[e] = v[e] * h;
+                                y[e] *= h;
+                            }
+                        });
+                        if (form0 != kNone) write8(kBf16, box0, lane, g, 1.f, y);
+                        write8(kBf16, box1, lane, g, 1.f, x);
+                        write8(kBf16, box2, lane, g, 1.f, up);
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    for (int k = OUT0; k <= OUT2; ++k)
+                        if (a.side[k].tma) tma_store_2d(&maps.side[k], mine + a.side[k].box[b], col, row0);
+                    bulk_commit_group();
+                }
+                for (int k = OUT0; k <= OUT2; ++k)
+                    if (a.side[k].form != kNone && !a.side[k].tma) box_out(a.side[k], mine + a.side[k].box[b], lane, row0, col, a.M, a.N);
+                ++chunk;
+                return true;
+            };
+            if constexpr (LONG) {
+#pragma unroll
+                for (int i = 0; i < CHUNKS; ++i)
+                    if (ok && i < valid) ok = one_chunk(i, sum[i]);
+            } else {
+#pragma unroll 1
+                for (int i = 0; ok && i < valid; ++i) ok = one_chunk(i, sum[0]);
+                if (ok && valid < CHUNKS) release(buf);
+            }
+        }
+        if (!ok && fetches && lane == 0) {                     // leaving after a time-out: operands on their way land first
+            int never = 0;
+            for (uint32_t c = chunk; c < fetched; ++c) mbar_wait(in_bar(w, c & 1u), (c >> 1) & 1u, &never, kLeaveLimitNs);
+        }
+        if (lane == 0) bulk_wait_all();                        // this warp's stores are complete
+        __syncwarp();
+    }
+
+    // ---------------- teardown ----------------
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();                              // neither CTA frees tensor memory or leaves while its peer still works
+    if (warp == 1) {
+        tc_fence_after();
+        if (PAIR) tmem_dealloc_pair(tmem, 512);
+        else tmem_dealloc(tmem, 512);
+    }
+    if (threadIdx.x == 0 && abort_flag) atomicExch(a.status, (int)ADLOCO_ERR_TIMEOUT);
+}
+
+// ---- few rows ---------------------------------------------------------------------------------------
+// Up to 16 tokens forward: the time is the weight's bytes from memory.  A block takes 16 rows of the weight (or eight of
+// either projection), its warps the blocks of 128 of K in turn; a lane loads 16 bytes of two of those rows and of a row of
+// each eight of x straight into the fragments of the warp's own matrix instruction (m16n8k16, the weight's rows as its M):
+// the order of K within 32 is the same for both and does not matter.  The warps' sums meet in shared memory, in a fixed order.
+constexpr int FEW_ROWS = 16, FEW_MAX_WARPS = 16, FEW_MAX_M = 16;
+struct FewArgs {
+    int M, N, K, act;
+    const __nv_bfloat16 *x, *w[2];
+    int64_t x_stride, w_stride[2];
+    const float* bias;
+    Side residual, out0, out1, out2;
+};
+__device__ __forceinline__ uint4 eight_of(const __nv_bfloat16* row, int k, int K) {      // zeros beyond K
+    if (k + 8 <= K) return *reinterpret_cast<const uint4*>(row + k);
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    const unsigned short* h = reinterpret_cast<const unsigned short*>(row);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (k + i < K) w[i >> 1] |= (uint32_t)h[k + i] << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float load_one(const Side& s, int64_t at) {
+    return s.form == kF32 ? static_cast<const float*>(s.p)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(s.p)[at]);
+}
+__device__ __forceinline__ void store_one(const Side& s, int64_t at, float v) {
+    if (s.form == kF32) static_cast<float*>(s.p)[at] = v;
+    else static_cast<__nv_bfloat16*>(s.p)[at] = __float2bfloat16_rn(v);
+}
+template <int TILES, bool TWO>                                                      // TILES: of eight rows of x
+__global__ void __launch_bounds__(32 * FEW_MAX_WARPS) dense_few_kernel(const __grid_constant__ FewArgs a) {
+    extern __shared__ float sums[];                                                 // [warps][TILES * 8][FEW_ROWS + 1]
+    after_predecessor();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, g = lane >> 2, t = lane & 3;
+    const int n0 = (int)blockIdx.x * (TWO ? FEW_ROWS / 2 : FEW_ROWS);
+    const bool r0 = n0 + g < a.N, r1 = TWO ? r0 : n0 + g + 8 < a.N;
+    const __nv_bfloat16* w0 = a.w[0] + (int64_t)(n0 + g) * a.w_stride[0];
+    const __nv_bfloat16* w1 = TWO ? a.w[1] + (int64_t)(n0 + g) * a.w_stride[1] : w0 + 8 * a.w_stride[0];
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    float acc[TILES][4];
+#pragma unroll
+    for (int j = 0; j < TILES; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+    const int blocks = (a.K + 127) / 128;
+    for (int kb = warp; kb < blocks; kb += warps) {
+        uint4 p[4], q[4], x[TILES][4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const int k = kb * 128 + h * 32 + t * 8;
+            p[h] = r0 && k < a.K ? eight_of(w0, k, a.K) : none;
+            q[h] = r1 && k < a.K ? eight_of(w1, k, a.K) : none;
+        }
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const int k = kb * 128 + h * 32 + t * 8;
+#pragma unroll
+            for (int j = 0; j < TILES; ++j) {
+                const int m = j * 8 + g;
+                x[j][h] = m < a.M && k < a.K ? eight_of(a.x + (int64_t)m * a.x_stride, k, a.K) : none;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+#pragma unroll
+            for (int j = 0; j < TILES; ++j) {
+                mma_16816(acc[j], p[h].x, q[h].x, p[h].y, q[h].y, x[j][h].x, x[j][h].y);
+                mma_16816(acc[j], p[h].z, q[h].z, p[h].w, q[h].w, x[j][h].z, x[j][h].w);
+            }
+    }
+    float* mine = sums + warp * (TILES * 8) * (FEW_ROWS + 1);
+#pragma unroll
+    for (int j = 0; j < TILES; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine[(j * 8 + 2 * t + (i & 1)) * (FEW_ROWS + 1) + g + 8 * (i >> 1)] = acc[j][i];
+    __syncthreads();
+    constexpr int OUT = TWO ? FEW_ROWS / 2 : FEW_ROWS;
+    for (int i = threadIdx.x; i < TILES * 8 * OUT; i += blockDim.x) {
+        const int m = i / OUT, r = i % OUT, n = n0 + r;
+        if (m >= a.M || n >= a.N) continue;
+        float v = 0.f, u = 0.f;
+        for (int w = 0; w < warps; ++w) {
+            const float* at = sums + (w * TILES * 8 + m) * (FEW_ROWS + 1);
+            v += at[r];
+            if (TWO) u += at[r + 8];
+        }
+        if (!TWO && a.bias) v += a.bias[n];
+        const float res = !TWO && a.residual.form != kNone ? load_one(a.residual, (int64_t)m * a.residual.pitch + n) : 0.f;      // before any output
+        if (a.out1.form != kNone) store_one(a.out1, (int64_t)m * a.out1.pitch + n, v);
+        if (TWO && a.out2.form != kNone) store_one(a.out2, (int64_t)m * a.out2.pitch + n, u);
+        with_act(a.act, [&](auto t) { v = value(t, v); });
+        if (TWO) v *= u;
+        else if (a.residual.form != kNone) v += res;
+        store_one(a.out0, (int64_t)m * a.out0.pitch + n, v);
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------
+int64_t elem(int form) { return form == kF32 ? 4 : form == kBf16 ? 2 : 1; }
+Side side_of(const void* p, int64_t pitch, int form) {
+    Side s;
+    if (!p) return s;
+    s.p = const_cast<void*>(p);
+    s.pitch = pitch;
+    s.form = form;
+    return s;
+}
+Side kept_side(const adloco_kept& k) {
+    Side s = side_of(k.p, k.stride, k.scale ? kBytes : kBf16);
+    s.scale = k.scale;
+    s.scale_pitch = k.scale_stride;
+    return s;
+}
+
+// What a call is, before tiles are chosen.
+struct Product {
+    int64_t M, N, K;
+    int act;
+    const void* a;
+    int64_t a_stride;
+    const void* b[2];
+    int64_t b_stride[2];
+    const float* bias;
+    Side side[SIDES];
+};
+
+template <int KIND, bool PAIR, int BN, bool LONG>
+int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
+    constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK;
+    constexpr int COLS = TWO ? BN / 2 : BN, TM = PAIR ? 256 : 128, STAGE = dg_stage_bytes<PAIR, BN>();
+    GemmArgs a;
+    a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K; a.kb = (int)((p.K + 63) / 64);
+    const int64_t tm = (p.M + TM - 1) / TM, tn = (p.N + COLS - 1) / COLS;
+    if (tm * tn > 0x7fffffff) return ADLOCO_ERR_UNSUPPORTED;
+    a.tiles_n = (int)tn; a.tiles = (int)(tm * tn);
+    a.act = p.act; a.bias = p.bias;
+    a.status = ctx->gemm_status; a.wait_ns = ctx->wait_limit_ns;
+    a.in_bytes = 0;
+    Maps maps;
+    int rc = make_map(ctx, &maps.a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.a, p.M, p.K, p.a_stride, 64, 128);
+    for (int i = 0; i < (TWO ? 2 : 1) && rc == ADLOCO_OK; ++i)
+        rc = BACK ? make_map(ctx, &maps.b[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.b[i], p.K, p.N, p.b_stride[i], 64, 64)
+                  : make_map(ctx, &maps.b[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.b[i], p.N, p.K, p.b_stride[i], 64, TWO ? COLS : PAIR ? BN / 2 : BN);
+    if (!TWO) maps.b[1] = maps.b[0];
+    for (int i = 0; i < SIDES && rc == ADLOCO_OK; ++i) {
+        Side& s = a.side[i] = p.side[i];
+        maps.side[i] = maps.a;                        // not looked at where no box goes by TMA
+        if (s.form == kNone) continue;
+        const int64_t es = elem(s.form);
+        s.pieces = aligned16(s.p) && s.pitch * es % 16 == 0;
+        // a store writes a row's last 16 bytes in full, beyond the matrix too
+        s.tma = s.pieces && (i <= IN1 || p.N * es % 16 == 0);
+        if (!s.tma) continue;
+        rc = s.form == kBf16 ? make_map(ctx, &maps.side[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, s.p, p.M, p.N, s.pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)
+           : s.form == kF32 ? make_map(ctx, &maps.side[i], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, s.p, p.M, p.N, s.pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B)
+                            : make_map(ctx, &maps.side[i], CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, s.p, p.M, p.N, s.pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_32B);
+        if (i <= IN1) a.in_bytes += (uint32_t)(1024 * es);
+    }
+    if (rc != ADLOCO_OK) return rc;
+    // the boxes of an epilogue warp, largest first so that each starts on a multiple of its swizzle's span: operands twice
+    // (they are fetched a chunk ahead), outputs once, an output over the operand of its form that is read at the same place
+    constexpr int over[SIDES] = {-1, -1, KIND == GATED_BACK ? -1 : IN0, KIND == GATED_BACK ? IN0 : KIND == LINEAR_BACK ? IN1 : -1,
+                                 KIND == GATED_BACK ? IN1 : -1};
+    uint32_t used = 0;
+    for (int form : {kF32, kBf16, kBytes})
+        for (int i = 0; i < SIDES; ++i) {
+            Side& s = a.side[i];
+            if (s.form != form || (over[i] >= 0 && a.side[over[i]].form == form)) continue;
+            const uint32_t bytes = (uint32_t)(1024 * elem(form));
+            s.box[0] = used;
+            s.box[1] = i <= IN1 ? used + bytes : used;
+            used = s.box[1] + bytes;
+        }
+    for (int i = OUT0; i < SIDES; ++i)
+        if (over[i] >= 0 && a.side[i].form != kNone && a.side[over[i]].form == a.side[i].form)
+            for (int b = 0; b < 2; ++b) a.side[i].box[b] = a.side[over[i]].box[b];
+    a.warp_bytes = (used + 1023u) & ~1023u;
+    const int64_t left = DG_SMEM - 1024 - DG_BAR_BYTES - (int64_t)DG_EPI * a.warp_bytes;
+    a.stages = (int)(left / STAGE < DG_MAX_STAGES ? left / STAGE : DG_MAX_STAGES);
+    if (a.stages < 2) return ADLOCO_ERR_UNSUPPORTED;
+    auto* kernel = dense_tile_kernel<KIND, PAIR, BN, LONG>;
+    static std::atomic<bool> attr_set[64];            // the attribute is per device
+    if (!attr_set[ctx->device & 63].load()) {
+        ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DG_SMEM));
+        attr_set[ctx->device & 63].store(true);
+    }
+    const size_t smem = (size_t)a.stages * STAGE + DG_EPI * (size_t)a.warp_bytes + DG_BAR_BYTES + 1024;
+    const int most = PAIR ? ctx->sm_count / 2 : ctx->sm_count, workers = a.tiles < most ? a.tiles : most;
+    ADLOCO_CUDA_TRY(ctx, launch_early(kernel, dim3((PAIR ? 2 : 1) * workers), DG_THREADS, smem, st, PAIR ? 2 : 1, maps, a));
+    ctx->launches++;
+    return ADLOCO_OK;
+}
+
+template <int KIND, bool LONG>
+int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
+    constexpr int COLS = KIND == GATED ? 128 : 256;
+    const int64_t pairs = ((p.M + 255) / 256) * ((p.N + COLS - 1) / COLS);
+    if (pairs >= ctx->sm_count / 2 && cta_pairs_possible(ctx)) return launch_tiles<KIND, true, 256, LONG>(ctx, p, st);
+    bool bytes = false;                               // 8-bit outputs: a block of 128 columns in one tile
+    for (int i = OUT0; i < SIDES; ++i) bytes = bytes || p.side[i].form == kBytes;
+    const int64_t rows = (p.M + 127) / 128;
+    if constexpr (KIND == GATED) {
+        if (bytes || rows * ((p.N + 127) / 128) >= ctx->sm_count) return launch_tiles<KIND, false, 256, LONG>(ctx, p, st);
+        return launch_tiles<KIND, false, 128, LONG>(ctx, p, st);
+    } else {
+        if (bytes || rows * ((p.N + 127) / 128) >= ctx->sm_count) return launch_tiles<KIND, false, 128, LONG>(ctx, p, st);
+        return launch_tiles<KIND, false, 64, LONG>(ctx, p, st);
+    }
+}
+
+template <bool TWO>
+int launch_few(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
+    FewArgs a;
+    a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K; a.act = p.act;
+    a.x = static_cast<const __nv_bfloat16*>(p.a); a.x_stride = p.a_stride;
+    for (int i = 0; i < 2; ++i) { a.w[i] = static_cast<const __nv_bfloat16*>(p.b[i]); a.w_stride[i] = p.b_stride[i]; }
+    a.bias = p.bias;
+    a.residual = p.side[IN0]; a.out0 = p.side[OUT0]; a.out1 = p.side[OUT1]; a.out2 = p.side[OUT2];
+    const int each = TWO ? FEW_ROWS / 2 : FEW_ROWS, blocks = (int)((p.K + 127) / 128);
+    const int warps = blocks < FEW_MAX_WARPS ? blocks : FEW_MAX_WARPS, tiles = p.M <= 8 ? 1 : 2;
+    const dim3 grid((unsigned)((p.N + each - 1) / each));
+    const size_t smem = (size_t)warps * tiles * 8 * (FEW_ROWS + 1) * sizeof(float);
+    const cudaError_t e = tiles == 1 ? launch_early(dense_few_kernel<1, TWO>, grid, 32 * warps, smem, st, 1, a)
+                                     : launch_early(dense_few_kernel<2, TWO>, grid, 32 * warps, smem, st, 1, a);
+    ADLOCO_CUDA_TRY(ctx, e);
+    ctx->launches++;
+    return ADLOCO_OK;
+}
+
+}  // namespace
+
+int launch_linear(adloco_ctx* ctx, const adloco_linear_args& c, cudaStream_t st) {
+    Product p = {c.M, c.N, c.K, c.activation, c.x, c.x_stride, {c.w, c.w}, {c.w_stride, c.w_stride}, c.bias, {}};
+    const int form = c.out_dtype == ADLOCO_BF16 ? kBf16 : kF32;
+    p.side[IN0] = side_of(c.residual, c.residual_stride, form);
+    p.side[OUT0] = side_of(c.y, c.y_stride, form);
+    p.side[OUT1] = kept_side(c.z);
+    if (c.M <= FEW_MAX_M && p.side[OUT1].form != kBytes) return launch_few<false>(ctx, p, st);
+    return form == kF32 && c.K > 64 * DG_SEGMENT && p.side[OUT1].form != kBytes ? choose_tiles<LINEAR, true>(ctx, p, st)
+                                                                               : choose_tiles<LINEAR, false>(ctx, p, st);
+}
+
+int launch_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args& c, cudaStream_t st) {
+    Product p = {c.M, c.K, c.N, c.activation, c.dy, c.dy_stride, {c.w, c.w}, {c.w_stride, c.w_stride}, nullptr, {}};
+    const int form = c.out_dtype == ADLOCO_BF16 ? kBf16 : kF32;
+    p.side[IN0] = side_of(c.residual, c.residual_stride, form);
+    p.side[IN1] = kept_side(c.z);
+    p.side[OUT0] = side_of(c.dx, c.dx_stride, form);
+    p.side[OUT1] = side_of(c.a, c.a_stride, kBf16);
+    return form == kF32 && c.N > 64 * DG_SEGMENT ? choose_tiles<LINEAR_BACK, true>(ctx, p, st) : choose_tiles<LINEAR_BACK, false>(ctx, p, st);
+}
+
+int launch_gated_linear(adloco_ctx* ctx, const adloco_gated_linear_args& c, cudaStream_t st) {
+    Product p = {c.M, c.f, c.d, c.activation, c.x, c.x_stride, {c.w_gate, c.w_up}, {c.w_gate_stride, c.w_up_stride}, nullptr, {}};
+    p.side[OUT0] = side_of(c.a, c.a_stride, kBf16);
+    p.side[OUT1] = kept_side(c.gate);
+    p.side[OUT2] = kept_side(c.up);
+    if (c.M <= FEW_MAX_M && p.side[OUT1].form != kBytes) return launch_few<true>(ctx, p, st);
+    return choose_tiles<GATED, false>(ctx, p, st);
+}
+
+int launch_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_backward_args& c, cudaStream_t st) {
+    Product p = {c.M, c.f, c.d, c.activation, c.dy, c.dy_stride, {c.w_down, c.w_down}, {c.w_down_stride, c.w_down_stride}, nullptr, {}};
+    p.side[IN0] = kept_side(c.gate);
+    p.side[IN1] = kept_side(c.up);
+    p.side[OUT0] = side_of(c.a, c.a_stride, kBf16);
+    p.side[OUT1] = side_of(c.d_gate, c.d_gate_stride, kBf16);
+    p.side[OUT2] = side_of(c.d_up, c.d_up_stride, kBf16);
+    return choose_tiles<GATED_BACK, false>(ctx, p, st);
+}
+
+}  // namespace adloco

@@ -337,6 +337,179 @@ int blockscale_matmul(PyObject* const* v) {
     return unlocked(adloco_blockscale_matmul, handle(v[0]), &a, stream_of(v[9], dev));
 }
 
+// handle, device, q, scale, x, stream
+int blockscale_dequantize(PyObject* const* v) {
+    const int64_t dev = whole(v[1]);
+    const at::Tensor& x = need(v[4], "x");
+    on(x, "x", dev);
+    const Rows xr = rows_of(x, "x"), qr = bytes_like(&need(v[2], "q"), "q", xr.rows, xr.d, dev);
+    const Rows sr = row_scales_like(&need(v[3], "scale"), "scale", xr.rows, xr.d, dev);
+    return unlocked(adloco_blockscale_dequantize, handle(v[0]), code(x, "x"), xr.rows, xr.d, qr.p, qr.pitch, static_cast<uint8_t*>(sr.p), sr.pitch,
+                    xr.p, xr.pitch, stream_of(v[5], dev));
+}
+
+// bf16 rows that a product takes
+Rows operand(const at::Tensor& t, const char* what, int64_t rows, int64_t d, int64_t dev) {
+    Rows r = rows_like(&t, what, rows, d, at::kBFloat16, dev);
+    if (rows == 1) r.pitch = (d + 7) / 8 * 8;         // a single row has no pitch
+    return r;
+}
+Rows weight(const at::Tensor& t, const char* what, int64_t rows, int64_t d, int64_t dev) {
+    if (t.dim() != 2) refuse(ADLOCO_ERR_INVALID_ARG, std::string(what) + ": expected a matrix, got " + described(t));
+    return operand(t, what, rows < 0 ? t.size(0) : rows, d < 0 ? t.size(1) : d, dev);
+}
+// what is kept for the backward pass, in bf16 or in bytes with their scales
+adloco_kept kept(PyObject* t, PyObject* s, const char* what, int64_t rows, int64_t d, int64_t dev) {
+    const at::Tensor *x = tensor(t, what, true), *scale = tensor(s, what, true);
+    adloco_kept k = {};
+    if (!x) {
+        if (scale) refuse(ADLOCO_ERR_INVALID_ARG, std::string(what) + ": scales without values");
+        return k;
+    }
+    if (!scale) {
+        const Rows r = operand(*x, what, rows, d, dev);
+        k.p = r.p; k.stride = r.pitch;
+        return k;
+    }
+    const Rows r = bytes_like(x, what, rows, d, dev), sr = row_scales_like(scale, what, rows, d, dev);
+    k.p = r.p; k.stride = r.pitch;
+    k.scale = static_cast<uint8_t*>(sr.p); k.scale_stride = sr.pitch;
+    return k;
+}
+int32_t activation(PyObject* o) {
+    static const char* const names[] = {"none", "relu", "gelu", "gelu_tanh", "silu"};
+    if (o == Py_None) return ADLOCO_ACT_NONE;
+    if (PyUnicode_Check(o))
+        for (int32_t i = 0; i < 5; ++i)
+            if (PyUnicode_CompareWithASCIIString(o, names[i]) == 0) return i;
+    refuse(ADLOCO_ERR_INVALID_ARG, "activation: expected none, relu, gelu, gelu_tanh or silu");
+}
+
+// handle, device, x, w, y, bias, activation, residual, z, z_scale, stream
+int linear(PyObject* const* v) {
+    const int64_t dev = whole(v[1]);
+    const at::Tensor &x = need(v[2], "x"), &w = need(v[3], "w"), &y = need(v[4], "y");
+    on(x, "x", dev);
+    adloco_linear_args a = {};
+    const Rows shape = rows_of(x, "x"), wr = weight(w, "w", -1, shape.d, dev);
+    a.M = shape.rows; a.K = shape.d; a.N = w.size(0);
+    const Rows xr = operand(x, "x", a.M, a.K, dev), yr = rows_like(&y, "y", a.M, a.N, y.scalar_type(), dev);
+    const Rows rr = rows_like(tensor(v[7], "residual", true), "residual", a.M, a.N, y.scalar_type(), dev);
+    a.x = xr.p; a.x_stride = xr.pitch;
+    a.w = wr.p; a.w_stride = wr.pitch;
+    a.bias = static_cast<const float*>(vector(tensor(v[5], "bias", true), "bias", a.N, at::kFloat, dev));
+    a.residual = rr.p; a.residual_stride = rr.pitch;
+    a.y = yr.p; a.y_stride = yr.pitch; a.out_dtype = code(y, "y");
+    a.z = kept(v[8], v[9], "z", a.M, a.N, dev);
+    a.activation = activation(v[6]);
+    return unlocked(adloco_linear, handle(v[0]), &a, stream_of(v[10], dev));
+}
+
+// handle, device, dy, w, dx, activation, z, z_scale, a, residual, stream
+int linear_backward(PyObject* const* v) {
+    const int64_t dev = whole(v[1]);
+    const at::Tensor &dy = need(v[2], "dy"), &w = need(v[3], "w"), &dx = need(v[4], "dx");
+    on(dy, "dy", dev);
+    adloco_linear_backward_args a = {};
+    const Rows shape = rows_of(dy, "dy"), wr = weight(w, "w", shape.d, -1, dev);
+    a.M = shape.rows; a.N = shape.d; a.K = w.size(1);
+    const Rows dr = operand(dy, "dy", a.M, a.N, dev), xr = rows_like(&dx, "dx", a.M, a.K, dx.scalar_type(), dev);
+    const Rows rr = rows_like(tensor(v[9], "residual", true), "residual", a.M, a.K, dx.scalar_type(), dev);
+    const Rows ar = rows_like(tensor(v[8], "a", true), "a", a.M, a.K, at::kBFloat16, dev);
+    a.dy = dr.p; a.dy_stride = dr.pitch;
+    a.w = wr.p; a.w_stride = wr.pitch;
+    a.z = kept(v[6], v[7], "z", a.M, a.K, dev);
+    a.residual = rr.p; a.residual_stride = rr.pitch;
+    a.dx = xr.p; a.dx_stride = xr.pitch; a.out_dtype = code(dx, "dx");
+    a.a = ar.p; a.a_stride = ar.pitch;
+    a.activation = activation(v[5]);
+    return unlocked(adloco_linear_backward, handle(v[0]), &a, stream_of(v[10], dev));
+}
+
+// handle, device, x, w_gate, w_up, a, activation, gate, up, gate_scale, up_scale, stream
+int gated_linear(PyObject* const* v) {
+    const int64_t dev = whole(v[1]);
+    const at::Tensor &x = need(v[2], "x"), &wg = need(v[3], "w_gate");
+    on(x, "x", dev);
+    adloco_gated_linear_args a = {};
+    const Rows shape = rows_of(x, "x"), gr = weight(wg, "w_gate", -1, shape.d, dev);
+    a.M = shape.rows; a.d = shape.d; a.f = wg.size(0);
+    const Rows ur = weight(need(v[4], "w_up"), "w_up", a.f, a.d, dev), xr = operand(x, "x", a.M, a.d, dev);
+    const Rows ar = rows_like(&need(v[5], "a"), "a", a.M, a.f, at::kBFloat16, dev);
+    a.x = xr.p; a.x_stride = xr.pitch;
+    a.w_gate = gr.p; a.w_gate_stride = gr.pitch;
+    a.w_up = ur.p; a.w_up_stride = ur.pitch;
+    a.a = ar.p; a.a_stride = ar.pitch;
+    a.activation = activation(v[6]);
+    a.gate = kept(v[7], v[9], "gate", a.M, a.f, dev);
+    a.up = kept(v[8], v[10], "up", a.M, a.f, dev);
+    return unlocked(adloco_gated_linear, handle(v[0]), &a, stream_of(v[11], dev));
+}
+
+// handle, device, dy, w_down, gate, up, d_gate, d_up, activation, gate_scale, up_scale, a, stream
+int gated_linear_backward(PyObject* const* v) {
+    const int64_t dev = whole(v[1]);
+    const at::Tensor &dy = need(v[2], "dy"), &w = need(v[3], "w_down");
+    on(dy, "dy", dev);
+    adloco_gated_linear_backward_args a = {};
+    const Rows shape = rows_of(dy, "dy"), wr = weight(w, "w_down", shape.d, -1, dev);
+    a.M = shape.rows; a.d = shape.d; a.f = w.size(1);
+    const Rows dr = operand(dy, "dy", a.M, a.d, dev);
+    a.dy = dr.p; a.dy_stride = dr.pitch;
+    a.w_down = wr.p; a.w_down_stride = wr.pitch;
+    need(v[4], "gate"); need(v[5], "up");
+    a.gate = kept(v[4], v[9], "gate", a.M, a.f, dev);
+    a.up = kept(v[5], v[10], "up", a.M, a.f, dev);
+    const Rows gr = rows_like(&need(v[6], "d_gate"), "d_gate", a.M, a.f, at::kBFloat16, dev), ur = rows_like(&need(v[7], "d_up"), "d_up", a.M, a.f, at::kBFloat16, dev);
+    const Rows ar = rows_like(tensor(v[11], "a", true), "a", a.M, a.f, at::kBFloat16, dev);
+    a.d_gate = gr.p; a.d_gate_stride = gr.pitch;
+    a.d_up = ur.p; a.d_up_stride = ur.pitch;
+    a.a = ar.p; a.a_stride = ar.pitch;
+    a.activation = activation(v[8]);
+    return unlocked(adloco_gated_linear_backward, handle(v[0]), &a, stream_of(v[12], dev));
+}
+
+// handle, device, logits, targets, logp, entropy, lse, top_values, top_ids, stream
+int token_logprobs(PyObject* const* v) {
+    const int64_t dev = whole(v[1]);
+    const at::Tensor& l = need(v[2], "logits");
+    on(l, "logits", dev);
+    const Rows lr = rows_of(l, "logits");
+    adloco_token_logprobs_args a = {};
+    a.rows = lr.rows; a.V = lr.d; a.logits = lr.p; a.logits_stride = lr.pitch; a.dtype = code(l, "logits");
+    a.targets = static_cast<const int32_t*>(vector(tensor(v[3], "targets", true), "targets", a.rows, at::kInt, dev));
+    a.logp = static_cast<float*>(vector(tensor(v[4], "logp", true), "logp", a.rows, at::kFloat, dev));
+    a.entropy = static_cast<float*>(vector(tensor(v[5], "entropy", true), "entropy", a.rows, at::kFloat, dev));
+    a.lse = static_cast<float*>(vector(tensor(v[6], "lse", true), "lse", a.rows, at::kFloat, dev));
+    const at::Tensor *tv = tensor(v[7], "top_values", true), *ti = tensor(v[8], "top_ids", true);
+    if (!tv != !ti) refuse(ADLOCO_ERR_INVALID_ARG, "top_values and top_ids go together");
+    if (tv) {
+        const int64_t top = tv->dim() ? tv->size(tv->dim() - 1) : 0;
+        if (top < 1 || top > 64) refuse(ADLOCO_ERR_UNSUPPORTED, "top_values: 1 to 64 tokens a row, got " + described(*tv));
+        a.top = (int32_t)top;
+        a.top_values = static_cast<float*>(vector(tv, "top_values", a.rows * top, at::kFloat, dev));
+        a.top_ids = static_cast<int32_t*>(vector(ti, "top_ids", a.rows * top, at::kInt, dev));
+    }
+    return unlocked(adloco_token_logprobs, handle(v[0]), &a, stream_of(v[9], dev));
+}
+
+// handle, device, logits, targets, lse, d_logp, d_logits, entropy, d_entropy, stream
+int token_logprobs_backward(PyObject* const* v) {
+    const int64_t dev = whole(v[1]);
+    const at::Tensor& l = need(v[2], "logits");
+    on(l, "logits", dev);
+    const Rows lr = rows_of(l, "logits"), dr = rows_like(&need(v[6], "d_logits"), "d_logits", lr.rows, lr.d, l.scalar_type(), dev);
+    adloco_token_logprobs_backward_args a = {};
+    a.rows = lr.rows; a.V = lr.d; a.logits = lr.p; a.logits_stride = lr.pitch; a.dtype = code(l, "logits");
+    a.d_logits = dr.p; a.d_logits_stride = dr.pitch;
+    a.targets = static_cast<const int32_t*>(vector(&need(v[3], "targets"), "targets", a.rows, at::kInt, dev));
+    a.lse = static_cast<const float*>(vector(&need(v[4], "lse"), "lse", a.rows, at::kFloat, dev));
+    a.d_logp = static_cast<const float*>(vector(&need(v[5], "d_logp"), "d_logp", a.rows, at::kFloat, dev));
+    a.entropy = static_cast<const float*>(vector(tensor(v[7], "entropy", true), "entropy", a.rows, at::kFloat, dev));
+    a.d_entropy = static_cast<const float*>(vector(tensor(v[8], "d_entropy", true), "d_entropy", a.rows, at::kFloat, dev));
+    return unlocked(adloco_token_logprobs_backward, handle(v[0]), &a, stream_of(v[9], dev));
+}
+
 template <int (*F)(PyObject* const*), int N>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != N) {
@@ -355,7 +528,9 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define ADLOCO_METHOD(f, n) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<f, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ADLOCO_METHOD(add_rmsnorm, 13), ADLOCO_METHOD(add_rmsnorm_backward, 16), ADLOCO_METHOD(dropout, 9),
                          ADLOCO_METHOD(rope, 12), ADLOCO_METHOD(blockscale_quantize, 6), ADLOCO_METHOD(blockscale_quantize_weight, 7),
-                         ADLOCO_METHOD(blockscale_matmul, 10), {nullptr, nullptr, 0, nullptr}};
+                         ADLOCO_METHOD(blockscale_matmul, 10), ADLOCO_METHOD(blockscale_dequantize, 6), ADLOCO_METHOD(linear, 11),
+                         ADLOCO_METHOD(linear_backward, 11), ADLOCO_METHOD(gated_linear, 12), ADLOCO_METHOD(gated_linear_backward, 13),
+                         ADLOCO_METHOD(token_logprobs, 10), ADLOCO_METHOD(token_logprobs_backward, 10), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensor_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,582 @@
+// The loss of a decoder and the way back from 8 bits: log-probabilities of given tokens with entropy and the best
+// alternatives, their gradient, and the values that rows in 8 bits stand for.  All are bound by HBM.
+#include <atomic>
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "e4m3.cuh"
+#include "ptx.cuh"
+
+namespace adloco {
+
+using namespace ptx;
+
+namespace {
+
+constexpr float kLog2e = 1.44269504f;
+__device__ __forceinline__ float exp2_fast(float x) {          // relative error 2^-22; 0 below 2^-126
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// ---- 16 bytes of a row as numbers -----------------------------------------------------------
+template <typename T> struct Piece { static constexpr int N = 16 / sizeof(T); };
+__device__ __forceinline__ float number(const float* p) { return *p; }
+__device__ __forceinline__ float number(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void unpack(const uint4& w, float (&v)[4]) {
+    v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+}
+__device__ __forceinline__ void unpack(const uint4& w, float (&v)[8]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint4 repack(const float (&v)[4]) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ uint4 repack(const float (&v)[8]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        u[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// A run of n numbers that starts anywhere: `head` of them before the first 16-byte boundary, `body` whole pieces of 16
+// bytes, `tail` behind.
+template <typename T>
+struct Run {
+    const T* p;
+    int head, body, tail;
+    __device__ __forceinline__ Run(const T* at, int n) : p(at) {
+        const int skew = (int)((reinterpret_cast<uintptr_t>(at) & 15u) / sizeof(T));
+        head = skew ? min(n, Piece<T>::N - skew) : 0;
+        body = (n - head) / Piece<T>::N;
+        tail = n - head - body * Piece<T>::N;
+    }
+    __device__ __forceinline__ const uint4* pieces() const { return reinterpret_cast<const uint4*>(p + head); }
+    __device__ __forceinline__ int index(int piece) const { return head + piece * Piece<T>::N; }
+};
+
+// ---- log-probabilities -----------------------------------------------------------------------
+// One pass with the running maximum m and the sums S = sum e^(l - m), E = sum (l - m) e^(l - m) of each thread's share:
+//   lse = m + log S,   entropy = log S - E / S.
+// A row is shared by TPR threads (a warp, or a block), a long row of few by the blocks of a cluster.  m starts at the
+// lowest finite number, so that l - m is a number for every finite l, and -Inf gives the 0 that it should.
+//
+// The best tokens: the top-th largest of the maxima of 128 groups of threads (32 in a warp) is a lower bound of the
+// top-th largest logit.  Only the few threads whose own maximum reaches it have anything that counts: the row's threads
+// look at those threads' shares once more together, collect what reaches the bound, and sort that by counting.  Where
+// too much reaches it (long runs of equal logits), they take the best one by one instead, a pass over the row for each.
+constexpr int kMaxTop = 64;
+constexpr int kTopThreads = 512;
+constexpr int kCluster = 8;
+template <int TPR> __host__ __device__ constexpr int groups_of() { return TPR < 128 ? TPR : 128; }
+template <int TPR> __host__ __device__ constexpr int candidates_of() { return TPR == 32 ? 512 : 1024; }
+
+// a number's place among numbers as an unsigned one, NaN lowest, -0 as 0; then the lower index first
+__device__ __forceinline__ uint64_t key_of(float v, int index) {
+    const uint32_t b = __float_as_uint(v + 0.f);
+    const uint32_t o = v != v ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+    return ((uint64_t)o << 32) | (uint32_t)~index;
+}
+__device__ __forceinline__ float value_of(uint64_t key) {
+    const uint32_t o = (uint32_t)(key >> 32);
+    return o == 0u ? __uint_as_float(0x7fffffffu) : __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
+}
+
+struct Sums { float m, s, e; };
+__device__ __forceinline__ Sums joined(const Sums& a, const Sums& b) {
+    const float m = fmaxf(a.m, b.m), da = a.m - m, db = b.m - m;
+    const float fa = exp2_fast(da * kLog2e), fb = exp2_fast(db * kLog2e);
+    // (l - m) e^(l - m) over a's share, with l - m = (l - a.m) + da; a share without numbers has s = 0, and da may be huge
+    const float ea = a.s == 0.f ? 0.f : fmaf(da, a.s, a.e) * fa, eb = b.s == 0.f ? 0.f : fmaf(db, b.s, b.e) * fb;
+    return Sums{m, fmaf(a.s, fa, b.s * fb), (fa == 0.f && a.s == a.s ? 0.f : ea) + (fb == 0.f && b.s == b.s ? 0.f : eb)};
+}
+
+template <int TPR>
+struct RowShared {
+    Sums sums[TPR / 32];
+    float group_max[groups_of<TPR>()];
+    float bound;
+    int hot, found;
+    unsigned short hot_thread[TPR];
+    uint64_t best[kMaxTop];
+    uint64_t wave[TPR / 32];
+    uint64_t candidate[candidates_of<TPR>()];
+};
+
+struct LogprobArgs {
+    int64_t rows, stride;
+    int V, top;
+    const void* logits;
+    const int32_t* targets;
+    float *logp, *entropy, *lse, *top_values;
+    int32_t* top_ids;
+};
+
+template <int TPR>
+__device__ __forceinline__ void row_sync() {
+    if (TPR == 32) __syncwarp();
+    else __syncthreads();
+}
+
+template <typename T, bool ENTROPY, int U>
+__device__ __forceinline__ void add_piece(const uint4 (&w)[U], Sums& a, float& top) {
+    constexpr int N = Piece<T>::N;
+    float v[U][N];
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        unpack(w[u], v[u]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = fmaxf(m, v[u][i]);
+    }
+    top = fmaxf(top, m);
+    if (m > a.m) {
+        const float d = a.m - m, f = exp2_fast(d * kLog2e);
+        if (ENTROPY) a.e = f == 0.f && a.s == a.s ? 0.f : fmaf(d, a.s, a.e) * f;
+        a.s *= f;
+        a.m = m;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float s0 = 0.f, s1 = 0.f, e0 = 0.f, e1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float d0 = v[u][i] - a.m, d1 = v[u][i + 1] - a.m;
+            const float x0 = exp2_fast(d0 * kLog2e), x1 = exp2_fast(d1 * kLog2e);
+            s0 += x0; s1 += x1;
+            if (ENTROPY) { e0 = fmaf(x0, max_or_nan(d0, -1e4f), e0); e1 = fmaf(x1, max_or_nan(d1, -1e4f), e1); }
+        }
+        a.s += s0 + s1;
+        if (ENTROPY) a.e += e0 + e1;
+    }
+}
+__device__ __forceinline__ void add_one(float v, Sums& a, float& top) {
+    top = fmaxf(top, v);
+    const float m = fmaxf(a.m, v);
+    const float d = a.m - m, f = exp2_fast(d * kLog2e);
+    const float dv = v - m, x = exp2_fast(dv * kLog2e);
+    a.e = (f == 0.f && a.s == a.s ? 0.f : fmaf(d, a.s, a.e) * f) + x * max_or_nan(dv, -1e4f);
+    a.s = fmaf(a.s, f, x);
+    a.m = m;
+}
+
+// The largest `top` keys of a run of n numbers whose first has index `base`, in order, into sh.best; all threads of the row.
+template <typename T, int TPR>
+__device__ __noinline__ void best_one_by_one(RowShared<TPR>& sh, const T* p, int n, int base, int top) {
+    const int t = threadIdx.x & (TPR - 1), lane = t & 31;
+    uint64_t last = ~0ull;
+    for (int k = 0; k < top; ++k) {
+        uint64_t most = 0;
+        for (int i = t; i < n; i += TPR) {
+            const uint64_t key = key_of(number(p + i), base + i);
+            if (key < last && key > most) most = key;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) { const uint64_t other = __shfl_xor_sync(0xffffffffu, most, o); most = other > most ? other : most; }
+        if (lane == 0) sh.wave[t >> 5] = most;
+        row_sync<TPR>();
+        most = 0;
+        for (int i = 0; i < TPR / 32; ++i) most = sh.wave[i] > most ? sh.wave[i] : most;
+        row_sync<TPR>();
+        if (t == 0) sh.best[k] = most;
+        last = most;
+        if (most == 0) {                                        // fewer numbers than asked for
+            for (int i = k + t; i < top; i += TPR) sh.best[i] = 0;
+            break;
+        }
+    }
+    row_sync<TPR>();
+}
+
+template <typename T, int TPR>
+__device__ __forceinline__ void best_of_run(RowShared<TPR>& sh, const Run<T>& run, int n, int base, int top, float own_max) {
+    constexpr int G = groups_of<TPR>(), CAP = candidates_of<TPR>(), N = Piece<T>::N;
+    const int t = threadIdx.x & (TPR - 1);
+    float g = own_max;
+#pragma unroll
+    for (int o = TPR / G / 2; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
+    if (t % (TPR / G) == 0) sh.group_max[t / (TPR / G)] = g;
+    if (t == 0) { sh.hot = 0; sh.found = 0; sh.bound = -INFINITY; }
+    row_sync<TPR>();
+    if (t < G && top <= G) {
+        const float mine = sh.group_max[t];
+        int above = 0;
+#pragma unroll 8
+        for (int i = 0; i < G; ++i) {
+            const float other = sh.group_max[i];
+            above += other > mine || (other == mine && i < t);
+        }
+        if (above == top - 1) sh.bound = mine;
+    }
+    row_sync<TPR>();
+    const float bound = sh.bound;
+    if (own_max >= bound) sh.hot_thread[atomicAdd(&sh.hot, 1)] = (unsigned short)t;
+    row_sync<TPR>();
+    const int hot = sh.hot;
+    auto offer = [&](float v, int i) {
+        if (v >= bound) {
+            const int at = atomicAdd(&sh.found, 1);
+            if (at < CAP) sh.candidate[at] = key_of(v, base + i);
+        }
+    };
+    const int shares = (run.body + TPR - 1) / TPR + 1;          // pieces of a thread, and its one of the head and of the tail
+    for (int i = t; i < hot * shares; i += TPR) {
+        const int who = sh.hot_thread[i % hot], k = i / hot - 1;
+        if (k < 0) {
+            if (who < run.head) offer(number(run.p + who), who);
+            if (who < run.tail) offer(number(run.p + n - run.tail + who), n - run.tail + who);
+        } else if (who + k * TPR < run.body) {
+            const int piece = who + k * TPR;
+            float v[N];
+            unpack(run.pieces()[piece], v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) offer(v[e], run.index(piece) + e);
+        }
+    }
+    row_sync<TPR>();
+    const int found = sh.found;
+    if (found > CAP || found < min(top, n)) {                   // too much reaches the bound, or NaN in the way
+        best_one_by_one<T, TPR>(sh, run.p, n, base, top);
+        return;
+    }
+    for (int i = t; i < found; i += TPR) {
+        const uint64_t key = sh.candidate[i];
+        int above = 0;
+        for (int j = 0; j < found; ++j) above += sh.candidate[j] > key;
+        if (above < top) sh.best[above] = key;
+    }
+    for (int i = found + t; i < top; i += TPR) sh.best[i] = 0;
+    row_sync<TPR>();
+}
+
+template <typename T, int TPR, bool CLUSTER, bool ENTROPY>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) logprob_kernel(const __grid_constant__ LogprobArgs a) {
+    constexpr int ROWS = TPR < 128 ? 128 / TPR : 1;             // of a block
+    constexpr int U = 4;
+    __shared__ RowShared<TPR> shared_rows[ROWS];
+    RowShared<TPR>& sh = shared_rows[threadIdx.x / TPR];
+    const int t = threadIdx.x & (TPR - 1), lane = t & 31;
+    const uint32_t rank = CLUSTER ? cluster_cta_rank() : 0;
+    if (CLUSTER) cluster_started();
+    after_predecessor();
+    const int64_t row = CLUSTER ? blockIdx.x / kCluster : (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+    if (!CLUSTER && row >= a.rows) return;                      // whole warps
+    // this block's part of the row
+    const int part = CLUSTER ? ((a.V + kCluster - 1) / kCluster + 7) / 8 * 8 : a.V;
+    const int from = min(a.V, (int)rank * part), n = min(a.V - from, part);
+    const T* p = static_cast<const T*>(a.logits) + row * a.stride;
+    const Run<T> run(p + from, n);
+    Sums sums = {-3.402823466e38f, 0.f, 0.f};
+    float own_max = -INFINITY;
+    {
+        const uint4* pieces = run.pieces();
+        int i = t;
+        for (; i + (U - 1) * TPR < run.body; i += U * TPR) {
+            uint4 w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) w[u] = pieces[i + u * TPR];
+            add_piece<T, ENTROPY, U>(w, sums, own_max);
+        }
+        for (; i < run.body; i += TPR) {
+            const uint4 w[1] = {pieces[i]};
+            add_piece<T, ENTROPY, 1>(w, sums, own_max);
+        }
+        if (t < run.head) add_one(number(run.p + t), sums, own_max);
+        if (t < run.tail) add_one(number(run.p + n - run.tail + t), sums, own_max);
+    }
+    Sums all = sums;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const Sums other = {__shfl_xor_sync(0xffffffffu, all.m, o), __shfl_xor_sync(0xffffffffu, all.s, o), __shfl_xor_sync(0xffffffffu, all.e, o)};
+        all = joined(all, other);
+    }
+    if (TPR > 32) {
+        if (lane == 0) sh.sums[t >> 5] = all;
+        row_sync<TPR>();
+        all = sh.sums[0];
+        for (int i = 1; i < TPR / 32; ++i) all = joined(all, sh.sums[i]);
+        row_sync<TPR>();
+    }
+    if (a.top) best_of_run<T, TPR>(sh, run, n, from, a.top, own_max);
+    int own_top = a.top;
+    if (CLUSTER) {                                              // the first block takes all blocks' sums and best
+        if (t == 0) sh.sums[0] = all;
+        __syncthreads();
+        cluster_all_started();
+        cluster_sync_all();
+        if (rank == 0) {
+            const uint32_t at = smem_u32(&sh.sums[0]), list = smem_u32(&sh.best[0]);
+            auto far = [](uint32_t addr, uint32_t r) {
+                uint32_t v;
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_to_cta(addr, r)) : "memory");
+                return v;
+            };
+            for (uint32_t r = 1; r < (uint32_t)kCluster; ++r)
+                all = joined(all, Sums{__uint_as_float(far(at, r)), __uint_as_float(far(at + 4, r)), __uint_as_float(far(at + 8, r))});
+            for (int i = t; i < kCluster * a.top; i += TPR) {
+                const uint32_t r = (uint32_t)(i / a.top), k = (uint32_t)(i % a.top);
+                sh.candidate[i] = (uint64_t)far(list + 8 * k, r) | ((uint64_t)far(list + 8 * k + 4, r) << 32);
+            }
+        }
+        cluster_sync_all();                                     // nobody leaves while its memory is read
+        if (rank != 0) return;
+        if (a.top) {
+            const int found = kCluster * a.top;                 // keys are of different tokens, or 0
+            for (int i = t; i < found; i += TPR) {
+                const uint64_t key = sh.candidate[i];
+                int above = 0;
+                for (int j = 0; j < found; ++j) above += sh.candidate[j] > key;
+                if (key != 0 && above < a.top) sh.best[above] = key;
+            }
+            __syncthreads();
+        }
+    }
+    const bool none = all.s == 0.f;                             // every logit is -Inf
+    const float log_s = logf(all.s);
+    const float lse = none ? -INFINITY : all.m + log_s;
+    if (t == 0) {
+        if (a.logp) {
+            const int32_t target = a.targets[row];
+            float v = 0.f;
+            if (target >= 0 && target < a.V) v = none ? -INFINITY : number(p + target) - lse;
+            a.logp[row] = v;
+        }
+        if (ENTROPY) a.entropy[row] = none ? 0.f : log_s - __fdiv_rn(all.e, all.s);
+        if (a.lse) a.lse[row] = lse;
+    }
+    for (int i = t; i < own_top; i += TPR) {
+        const uint64_t key = sh.best[i];
+        a.top_values[row * a.top + i] = none ? -INFINITY : value_of(key) - lse;
+        a.top_ids[row * a.top + i] = (int32_t)~(uint32_t)key;
+    }
+}
+
+// ---- their gradient ----------------------------------------------------------------------------
+// d_j = s (delta_jt - p_j) - c p_j (log p_j + H): every logit read once, every gradient written once.  A warp or a block a
+// row, long rows in parts.
+struct LogprobBackArgs {
+    int64_t rows, stride, out_stride, items;
+    int V, parts, span;                                         // parts of a row, logits in one
+    const void* logits;
+    const int32_t* targets;
+    const float *lse, *d_logp, *entropy, *d_entropy;
+    void* d_logits;
+};
+template <typename T, int TPR>
+__global__ void __launch_bounds__(256) logprob_back_kernel(const __grid_constant__ LogprobBackArgs a) {
+    constexpr int N = Piece<T>::N, U = 4, ROWS = 256 / TPR;
+    after_predecessor();
+    const int t = threadIdx.x & (TPR - 1);
+    for (int64_t item = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; item < a.items; item += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = item / a.parts;
+        const int from = (int)(item % a.parts) * a.span, n = min(a.V - from, a.span);
+        const T* p = static_cast<const T*>(a.logits) + row * a.stride + from;
+        T* out = static_cast<T*>(a.d_logits) + row * a.out_stride + from;
+        const int target = a.targets[row];
+        const float lse = a.lse[row], s = target >= 0 && target < a.V ? a.d_logp[row] : 0.f;
+        const float c = a.d_entropy ? a.d_entropy[row] : 0.f, H = a.d_entropy ? a.entropy[row] : 0.f;
+        const bool zero = (s == 0.f && c == 0.f) || lse == -INFINITY;
+        const int at = target - from;
+        auto one = [&](float l, int i) {
+            if (zero) return 0.f;
+            const float x = max_or_nan(l - lse, -1e4f), prob = exp2_fast(x * kLog2e);
+            const float d = -prob * fmaf(c, x + H, s);
+            return i == at ? d + s : d;
+        };
+        Run<T> run(p, n);
+        if ((reinterpret_cast<uintptr_t>(p) & 15u) != (reinterpret_cast<uintptr_t>(out) & 15u)) {
+            for (int i = t; i < n; i += TPR) put(out + i, one(number(p + i), i));
+            continue;
+        }
+        const uint4* pieces = run.pieces();
+        uint4* to = reinterpret_cast<uint4*>(out + run.head);
+        for (int i0 = t; i0 < run.body; i0 += U * TPR) {
+            uint4 w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * TPR < run.body) w[u] = __ldcs(pieces + i0 + u * TPR);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u * TPR >= run.body) continue;
+                float v[N];
+                unpack(w[u], v);
+                const int first = run.index(i0 + u * TPR);
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = one(v[e], first + e);
+                __stcs(to + i0 + u * TPR, repack(v));
+            }
+        }
+        if (t < run.head) put(out + t, one(number(p + t), t));
+        if (t < run.tail) put(out + n - run.tail + t, one(number(p + n - run.tail + t), n - run.tail + t));
+    }
+}
+
+// ---- values of 8 bits ----------------------------------------------------------------------------
+__device__ __forceinline__ float2 two_of(uint32_t w) {
+    const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
+    return __half22float2(*reinterpret_cast<const __half2*>(&r));
+}
+struct DequantArgs {
+    int64_t rows, q_stride, scale_stride, x_stride;
+    int cols;
+    const uint8_t *q, *scale;
+    void* x;
+};
+// VEC: 16 numbers a thread, rows of x on the 16-byte grid.  Otherwise a warp takes a block of 128, lanes side by side.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) dequantise_kernel(const __grid_constant__ DequantArgs a) {
+    constexpr int EACH = 4;                                     // pieces, or blocks of a warp, a thread
+    after_predecessor();
+    const uint32_t per_row = VEC ? (uint32_t)(a.cols + 15) / 16 : (uint32_t)(a.cols + 127) / 128;
+    const int64_t base = (int64_t)blockIdx.x * (VEC ? 256 * EACH : 8 * EACH);
+    const int64_t row0 = base / per_row;
+    const uint32_t skip = (uint32_t)(base - row0 * per_row);
+    if (VEC) {
+        uint4 w[EACH];
+        uint32_t byte[EACH], col[EACH];
+        int64_t row[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const uint32_t at = skip + threadIdx.x + 256 * i, r = at / per_row;
+            row[i] = row0 + r;
+            col[i] = (at - r * per_row) * 16;
+            if (row[i] >= a.rows) continue;
+            const uint8_t* q = a.q + row[i] * a.q_stride + col[i];
+            if ((int)col[i] + 16 <= a.cols) {
+                w[i] = __ldcs(reinterpret_cast<const uint4*>(q));
+            } else {                                            // a row's last, incomplete piece
+                uint32_t u[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int b = 0; b < 16; ++b)
+                    if ((int)col[i] + b < a.cols) u[b >> 2] |= (uint32_t)q[b] << (8 * (b & 3));
+                w[i] = make_uint4(u[0], u[1], u[2], u[3]);
+            }
+            byte[i] = a.scale[row[i] * a.scale_stride + (col[i] >> 7)];
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (row[i] >= a.rows) continue;
+            const float s = scale_of(byte[i]);
+            const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+            T* to = static_cast<T*>(a.x) + row[i] * a.x_stride + col[i];
+            float v[16];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float2 f = two_of(u[e >> 1] >> (16 * (e & 1)));
+                v[2 * e] = f.x * s;
+                v[2 * e + 1] = f.y * s;
+            }
+            constexpr int N = Piece<T>::N;
+#pragma unroll
+            for (int e = 0; e < 16; e += N) {
+                if ((int)col[i] + e + N <= a.cols) {
+                    float part[N];
+#pragma unroll
+                    for (int j = 0; j < N; ++j) part[j] = v[e + j];
+                    __stcs(reinterpret_cast<uint4*>(to + e), repack(part));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if ((int)col[i] + e + j < a.cols) put(to + e + j, v[e + j]);
+                }
+            }
+        }
+    } else {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const uint32_t at = skip + (threadIdx.x >> 5) + 8 * i, r = at / per_row;
+            const int64_t row = row0 + r;
+            const int block = (int)(at - r * per_row);
+            if (row >= a.rows) continue;
+            const float s = scale_of(a.scale[row * a.scale_stride + block]);
+            const uint8_t* q = a.q + row * a.q_stride + block * 128;
+            T* to = static_cast<T*>(a.x) + row * a.x_stride + block * 128;
+            uint32_t v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = block * 128 + e * 32 + lane < a.cols ? q[e * 32 + lane] : 0u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (block * 128 + e * 32 + lane < a.cols) put(to + e * 32 + lane, two_of(v[e]).x * s);
+        }
+    }
+}
+
+template <typename T, int TPR, bool CLUSTER>
+int launch_logprob_rows(adloco_ctx* ctx, const LogprobArgs& a, cudaStream_t st) {
+    constexpr int ROWS = TPR < 128 ? 128 / TPR : 1, THREADS = TPR < 128 ? 128 : TPR;
+    const int64_t blocks = CLUSTER ? a.rows * kCluster : (a.rows + ROWS - 1) / ROWS;
+    if (blocks > 0x7fffffff) return ADLOCO_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks);
+    const cudaError_t e = a.entropy ? launch_early(logprob_kernel<T, TPR, CLUSTER, true>, grid, THREADS, 0, st, CLUSTER ? kCluster : 1, a)
+                                    : launch_early(logprob_kernel<T, TPR, CLUSTER, false>, grid, THREADS, 0, st, CLUSTER ? kCluster : 1, a);
+    ADLOCO_CUDA_TRY(ctx, e);
+    ctx->launches++;
+    return ADLOCO_OK;
+}
+template <typename T>
+int launch_logprob(adloco_ctx* ctx, const LogprobArgs& a, cudaStream_t st) {
+    if (a.V <= 512) return launch_logprob_rows<T, 32, false>(ctx, a, st);
+    if (a.V <= 4096) return launch_logprob_rows<T, 128, false>(ctx, a, st);
+    // a cluster a row where there are fewer rows than would fill the machine and each is long
+    if (a.rows * 4 <= ctx->sm_count && a.V >= 16384 && cta_pairs_possible(ctx)) return launch_logprob_rows<T, kTopThreads, true>(ctx, a, st);
+    return launch_logprob_rows<T, kTopThreads, false>(ctx, a, st);
+}
+template <typename T>
+int launch_logprob_back(adloco_ctx* ctx, LogprobBackArgs a, cudaStream_t st) {
+    const bool narrow = a.V <= 2048;
+    a.span = narrow ? a.V : 256 * 4 * Piece<T>::N;
+    a.parts = (a.V + a.span - 1) / a.span;
+    a.items = a.rows * a.parts;
+    const int64_t blocks = narrow ? (a.items + 7) / 8 : a.items, most = int64_t(1) << 30;
+    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    ADLOCO_CUDA_TRY(ctx, narrow ? launch_early(logprob_back_kernel<T, 32>, grid, 256, 0, st, 1, a) : launch_early(logprob_back_kernel<T, 256>, grid, 256, 0, st, 1, a));
+    ctx->launches++;
+    return ADLOCO_OK;
+}
+template <typename T>
+int launch_dequantise(adloco_ctx* ctx, const DequantArgs& a, cudaStream_t st) {
+    const bool vec = aligned16(a.x) && a.x_stride % Piece<T>::N == 0;
+    const int64_t units = a.rows * (vec ? (a.cols + 15) / 16 : (a.cols + 127) / 128), each = vec ? 1024 : 32;
+    if ((units + each - 1) / each > 0x7fffffff) return ADLOCO_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)((units + each - 1) / each));
+    ADLOCO_CUDA_TRY(ctx, vec ? launch_early(dequantise_kernel<T, true>, grid, 256, 0, st, 1, a) : launch_early(dequantise_kernel<T, false>, grid, 256, 0, st, 1, a));
+    ctx->launches++;
+    return ADLOCO_OK;
+}
+
+}  // namespace
+
+int launch_blockscale_dequantize(adloco_ctx* ctx, int bf16, int64_t rows, int64_t cols, const void* q, int64_t q_stride,
+                                 const uint8_t* scale, int64_t scale_stride, void* x, int64_t x_stride, cudaStream_t st) {
+    const DequantArgs a = {rows, q_stride, scale_stride, x_stride, (int)cols, static_cast<const uint8_t*>(q), scale, x};
+    return bf16 ? launch_dequantise<__nv_bfloat16>(ctx, a, st) : launch_dequantise<float>(ctx, a, st);
+}
+
+int launch_token_logprobs(adloco_ctx* ctx, const adloco_token_logprobs_args& c, cudaStream_t st) {
+    const LogprobArgs a = {c.rows, c.logits_stride, (int)c.V, c.top, c.logits, c.targets, c.logp, c.entropy, c.lse, c.top_values, c.top_ids};
+    return c.dtype == ADLOCO_BF16 ? launch_logprob<__nv_bfloat16>(ctx, a, st) : launch_logprob<float>(ctx, a, st);
+}
+
+int launch_token_logprobs_backward(adloco_ctx* ctx, const adloco_token_logprobs_backward_args& c, cudaStream_t st) {
+    LogprobBackArgs a = {c.rows, c.logits_stride, c.d_logits_stride, 0, (int)c.V, 0, 0, c.logits, c.targets, c.lse, c.d_logp, c.entropy, c.d_entropy, c.d_logits};
+    return c.dtype == ADLOCO_BF16 ? launch_logprob_back<__nv_bfloat16>(ctx, a, st) : launch_logprob_back<float>(ctx, a, st);
+}
+
+}  // namespace adloco
