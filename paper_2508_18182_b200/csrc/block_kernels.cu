@@ -8,28 +8,12 @@
 
 #include "common.cuh"
 #include "e4m3.cuh"
+#include "f32x2.cuh"
 #include "ptx.cuh"
 
 namespace adloco {
 
 namespace {
-
-// ---- two fp32 operations an instruction ----------------------------------------------------
-struct F2 { float x, y; };
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-    F2 d;
-    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
-        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-    F2 d;
-    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-__device__ __forceinline__ F2 both(float v) { return F2{v, v}; }
 
 // ---- eight adjacent elements of a row ---------------------------------------------------
 // As they lie in memory (four or eight words), so that what waits for use takes half the registers in bf16.  The

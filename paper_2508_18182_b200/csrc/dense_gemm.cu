@@ -8,6 +8,7 @@
 
 #include "common.cuh"
 #include "e4m3.cuh"
+#include "f32x2.cuh"
 #include "gemm_parts.cuh"
 #include "ptx.cuh"
 
@@ -42,6 +43,7 @@ struct GemmArgs {
     int stages;
     uint32_t warp_bytes;              // boxes of one epilogue warp
     uint32_t in_bytes;                // that arrive by TMA for one chunk
+    int twice;                        // outputs have two boxes each, for even and odd chunks
     const float* bias;
     Side side[SIDES];
     int* status;
@@ -50,36 +52,66 @@ struct GemmArgs {
 struct Maps { CUtensorMap a, b[2], side[SIDES]; };
 
 // ---- activations ------------------------------------------------------------------------------
-// Value and derivative in fp32.  The logistic function takes the fast exponential and division (relative error 2^-21,
-// against the 2^-9 of a result in bf16); the error function is CUDA's.
+// Value and derivative of two numbers in fp32, from the fast exponential and reciprocal.  The error function is formula
+// 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions (1964): with t = 1 / (1 + 0.3275911 x), x >= 0,
+//   1 - erf(x) = (a1 t + a2 t^2 + ... + a5 t^5) exp(-x^2), off by less than 1.5e-7,
+// whose exponential is the one that the derivative needs too.  (With CUDA's erff, a branch for each group of eight and the
+// bias loaded number by number, 32768 x 768 -> 2048 took 208 us; 109 so.)
 template <int ACT> struct Act {};
-__device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
-__device__ __forceinline__ float value(Act<ADLOCO_ACT_NONE>, float z) { return z; }
-__device__ __forceinline__ float value(Act<ADLOCO_ACT_RELU>, float z) { return z < 0.f ? 0.f : z; }
-__device__ __forceinline__ float value(Act<ADLOCO_ACT_GELU>, float z) { return z * fmaf(0.5f, erff(z * 0.70710678f), 0.5f); }
+__device__ __forceinline__ F2 logistic(F2 z) {
+    const F2 e = exp2_fast(mul2(z, both(-1.44269504f)));
+    return rcp_fast(add2(e, both(1.f)));
+}
+// the normal distribution's tail beyond |z|, and exp(-z^2 / 2)
+__device__ __forceinline__ F2 tail_of(F2 z, F2& e) {
+    e = exp2_fast(mul2(mul2(z, z), both(-0.72134752f)));
+    const F2 t = rcp_fast(F2{fmaf(fabsf(z.x), 0.23164189f, 1.f), fmaf(fabsf(z.y), 0.23164189f, 1.f)});
+    F2 q = fma2(t, both(0.5307027145f), both(-0.7265760135f));       // half of 7.1.26's coefficients
+    q = fma2(q, t, both(0.7107068705f));
+    q = fma2(q, t, both(-0.142248368f));
+    q = fma2(q, t, both(0.127414796f));
+    return mul2(mul2(q, t), e);
+}
+__device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }                 // a NaN stays one
 // (1 + tanh(v)) / 2 is the logistic function of 2 v, v = sqrt(2 / pi) (z + 0.044715 z^3)
 constexpr float kTanhSlope = 1.5957691216f;
-__device__ __forceinline__ float value(Act<ADLOCO_ACT_GELU_TANH>, float z) { return z * logistic(kTanhSlope * z * fmaf(0.044715f * z, z, 1.f)); }
-__device__ __forceinline__ float value(Act<ADLOCO_ACT_SILU>, float z) { return z * logistic(z); }
+__device__ __forceinline__ F2 tanh_gate(F2 z) {
+    return logistic(mul2(z, fma2(mul2(z, z), both(kTanhSlope * 0.044715f), both(kTanhSlope))));
+}
 
-__device__ __forceinline__ float slope(Act<ADLOCO_ACT_NONE>, float z, float& a) { a = z; return 1.f; }
-__device__ __forceinline__ float slope(Act<ADLOCO_ACT_RELU>, float z, float& a) { a = z < 0.f ? 0.f : z; return z > 0.f ? 1.f : z == z ? 0.f : z; }
-__device__ __forceinline__ float slope(Act<ADLOCO_ACT_GELU>, float z, float& a) {
-    const float h = fmaf(0.5f, erff(z * 0.70710678f), 0.5f);
-    a = z * h;
-    return fmaf(z * 0.39894228f, __expf(-0.5f * z * z), h);
+__device__ __forceinline__ F2 value(Act<ADLOCO_ACT_NONE>, F2 z) { return z; }
+__device__ __forceinline__ F2 value(Act<ADLOCO_ACT_RELU>, F2 z) { return F2{relu(z.x), relu(z.y)}; }
+__device__ __forceinline__ F2 value(Act<ADLOCO_ACT_GELU>, F2 z) {
+    F2 e;
+    const F2 q = tail_of(z, e);
+    return F2{fmaf(-fabsf(z.x), q.x, fmaxf(z.x, 0.f)), fmaf(-fabsf(z.y), q.y, fmaxf(z.y, 0.f))};
 }
-__device__ __forceinline__ float slope(Act<ADLOCO_ACT_GELU_TANH>, float z, float& a) {
-    const float h = logistic(kTanhSlope * z * fmaf(0.044715f * z, z, 1.f));
-    a = z * h;
-    return fmaf(a * (1.f - h), kTanhSlope * fmaf(0.134145f * z, z, 1.f), h);
+__device__ __forceinline__ F2 value(Act<ADLOCO_ACT_GELU_TANH>, F2 z) { return mul2(z, tanh_gate(z)); }
+__device__ __forceinline__ F2 value(Act<ADLOCO_ACT_SILU>, F2 z) { return mul2(z, logistic(z)); }
+
+__device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_NONE>, F2 z, F2& a) { a = z; return both(1.f); }
+__device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_RELU>, F2 z, F2& a) {
+    a = F2{relu(z.x), relu(z.y)};
+    return F2{z.x > 0.f ? 1.f : a.x, z.y > 0.f ? 1.f : a.y};                                // 0, or the NaN
 }
-__device__ __forceinline__ float slope(Act<ADLOCO_ACT_SILU>, float z, float& a) {
-    const float h = logistic(z);
-    a = z * h;
-    return fmaf(a, 1.f - h, h);
+__device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_GELU>, F2 z, F2& a) {
+    F2 e;
+    const F2 q = tail_of(z, e), p = fma2(q, both(-1.f), both(1.f));
+    const F2 h = {z.x < 0.f ? q.x : p.x, z.y < 0.f ? q.y : p.y};
+    a = mul2(z, h);
+    return fma2(mul2(z, e), both(0.39894228f), h);
 }
-// f with the activation as a type: one branch for a group of elements
+__device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_GELU_TANH>, F2 z, F2& a) {
+    const F2 h = tanh_gate(z);
+    a = mul2(z, h);
+    return fma2(mul2(a, fma2(h, both(-1.f), both(1.f))), fma2(mul2(z, z), both(kTanhSlope * 0.134145f), both(kTanhSlope)), h);
+}
+__device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_SILU>, F2 z, F2& a) {
+    const F2 h = logistic(z);
+    a = mul2(z, h);
+    return fma2(a, fma2(h, both(-1.f), both(1.f)), h);
+}
+// f with the activation as a type: one branch for all that it does
 template <typename F>
 __device__ __forceinline__ void with_act(int act, F f) {
     switch (act) {
@@ -107,74 +139,90 @@ __device__ __forceinline__ uint4 lds16(uint32_t at) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
-__device__ __forceinline__ void pair_to_floats(uint32_t w, float& a, float& b) {
-    a = __uint_as_float(w << 16);
-    b = __uint_as_float(w & 0xffff0000u);
-}
-__device__ __forceinline__ void bytes_to_floats(uint32_t w, float s, float* v) {
+__device__ __forceinline__ F2 pair_of(uint32_t w) { return F2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; }
+__device__ __forceinline__ void bytes_to_pairs(uint32_t w, float s, F2* v) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> (16 * h)), __NV_E4M3);
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r));
-        v[2 * h] = f.x * s;
-        v[2 * h + 1] = f.y * s;
+        v[h] = mul2(F2{f.x, f.y}, both(s));
     }
 }
 // columns 8 g .. 8 g + 7 of this lane's row; s: the scale of bytes
-__device__ __forceinline__ void read8(int form, uint32_t box, int row, int g, float s, float (&v)[8]) {
+__device__ __forceinline__ void read8(int form, uint32_t box, int row, int g, float s, F2 (&v)[4]) {
     if (form == kBf16) {
         const uint4 w = lds16(piece_at<4>(box, row, g));
-        pair_to_floats(w.x, v[0], v[1]); pair_to_floats(w.y, v[2], v[3]);
-        pair_to_floats(w.z, v[4], v[5]); pair_to_floats(w.w, v[6], v[7]);
+        v[0] = pair_of(w.x); v[1] = pair_of(w.y); v[2] = pair_of(w.z); v[3] = pair_of(w.w);
     } else if (form == kF32) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint4 w = lds16(piece_at<8>(box, row, 2 * g + h));
-            v[4 * h] = __uint_as_float(w.x); v[4 * h + 1] = __uint_as_float(w.y);
-            v[4 * h + 2] = __uint_as_float(w.z); v[4 * h + 3] = __uint_as_float(w.w);
+            v[2 * h] = F2{__uint_as_float(w.x), __uint_as_float(w.y)};
+            v[2 * h + 1] = F2{__uint_as_float(w.z), __uint_as_float(w.w)};
         }
     } else {
         uint32_t a, b;
         asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(piece_at<2>(box, row, g >> 1) + 8u * (g & 1)) : "memory");
-        bytes_to_floats(a, s, v);
-        bytes_to_floats(b, s, v + 4);
+        bytes_to_pairs(a, s, v);
+        bytes_to_pairs(b, s, v + 2);
     }
 }
-__device__ __forceinline__ uint32_t pack(float a, float b) { return pack_bf16(__float_as_uint(a), __float_as_uint(b)); }
-__device__ __forceinline__ void write8(int form, uint32_t box, int row, int g, float inv, const float (&v)[8]) {
+__device__ __forceinline__ uint32_t pack(F2 v) { return pack_bf16(__float_as_uint(v.x), __float_as_uint(v.y)); }
+__device__ __forceinline__ void write8(int form, uint32_t box, int row, int g, float inv, const F2 (&v)[4]) {
     if (form == kBf16) {
-        st_shared_v4(piece_at<4>(box, row, g), pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]), pack(v[6], v[7]));
+        st_shared_v4(piece_at<4>(box, row, g), pack(v[0]), pack(v[1]), pack(v[2]), pack(v[3]));
     } else if (form == kF32) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            st_shared_v4(piece_at<8>(box, row, 2 * g + h), __float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]),
-                         __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3]));
+            st_shared_v4(piece_at<8>(box, row, 2 * g + h), __float_as_uint(v[2 * h].x), __float_as_uint(v[2 * h].y),
+                         __float_as_uint(v[2 * h + 1].x), __float_as_uint(v[2 * h + 1].y));
     } else {
         uint32_t h[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            h[i] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * i] * inv, v[2 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+        for (int i = 0; i < 4; ++i) {
+            const F2 u = mul2(v[i], both(inv));
+            h[i] = __nv_cvt_float2_to_fp8x2(make_float2(u.x, u.y), __NV_SATFINITE, __NV_E4M3);
+        }
         asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(piece_at<2>(box, row, g >> 1) + 8u * (g & 1)), "r"(h[0] | (h[1] << 16)),
                      "r"(h[2] | (h[3] << 16)) : "memory");
     }
 }
+// all 32 columns of a chunk, the branch on the form taken once
+__device__ __forceinline__ void write32(int form, uint32_t box, int row, float inv, const F2 (&v)[4][4]) {
+    if (form == kBf16) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) write8(kBf16, box, row, g, inv, v[g]);
+    } else if (form == kBytes) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) write8(kBytes, box, row, g, inv, v[g]);
+    }
+}
 // A box by the warp's own accesses: where rows do not start on 16-byte boundaries (element by element along rows), or
 // where a row's last 16-byte piece is not whole, which a TMA store would write in full.
-__device__ __forceinline__ void box_in(const Side& s, uint32_t box, int lane, int row0, int col, int M, int N) {
-    const int rows = min(32, M - row0);
-    for (int row = 0; row < rows; ++row) {
-        const int64_t at = (int64_t)(row0 + row) * s.pitch + col + lane;
-        if (s.form == kF32) {
-            const uint32_t v = col + lane < N ? static_cast<const uint32_t*>(s.p)[at] : 0u;
-            asm volatile("st.shared.u32 [%0], %1;" ::"r"(piece_at<8>(box, row, lane >> 2) + 4u * (lane & 3)), "r"(v) : "memory");
-        } else {
-            const unsigned short v = col + lane < N ? static_cast<const unsigned short*>(s.p)[at] : (unsigned short)0;
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(piece_at<4>(box, row, lane >> 3) + 2u * (lane & 7)), "h"(v) : "memory");
+template <typename W>
+__device__ __forceinline__ void box_in_of(const Side& s, uint32_t box, int lane, int row0, int col, int M, int N) {
+    constexpr int P = sizeof(W) == 4 ? 8 : 4, EACH = 16 / sizeof(W);
+    const W* from = static_cast<const W*>(s.p) + (int64_t)row0 * s.pitch + col + lane;
+    const int rows = col + lane < N ? M - row0 : 0;
+#pragma unroll 1
+    for (int row = 0; row < 32; row += 16) {           // sixteen rows' loads in flight
+        W v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = row + i < rows ? from[(row + i) * s.pitch] : W(0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t to = piece_at<P>(box, row + i, lane / EACH) + (uint32_t)(lane % EACH * sizeof(W));
+            if (sizeof(W) == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"((uint32_t)v[i]) : "memory");
+            else asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"((unsigned short)v[i]) : "memory");
         }
     }
+}
+__device__ __noinline__ void box_in(const Side& s, uint32_t box, int lane, int row0, int col, int M, int N) {
+    if (s.form == kF32) box_in_of<uint32_t>(s, box, lane, row0, col, M, N);
+    else box_in_of<unsigned short>(s, box, lane, row0, col, M, N);
     __syncwarp();
 }
-__device__ __forceinline__ void box_out(const Side& s, uint32_t box, int lane, int row0, int col, int M, int N) {
+__device__ __noinline__ void box_out(const Side& s, uint32_t box, int lane, int row0, int col, int M, int N) {
     __syncwarp();
     const int es = s.form == kF32 ? 4 : s.form == kBf16 ? 2 : 1, P = pieces_of(s.form), each = 16 / es;
     char* out = static_cast<char*>(s.p) + ((int64_t)row0 * s.pitch + col) * es;
@@ -226,15 +274,15 @@ __device__ __forceinline__ float larger(float m, float v) {
 // tensor cores' K; backward the same weight is read as it lies, its rows along the contraction (MN-major).
 // GATED: the tile's columns are BN / 2 of each projection (in a pair, CTA r brings projection r), so a thread of the epilogue
 // has both numbers of an output.
-// LONG: the tensor cores cut off each sum's low bits (relative error 1e-6 after 1000 terms, growing with their number); with
-// fp32 outputs the sum of every 512 of K is added up in registers instead, rounded to nearest.
+// F32 (outputs): the tensor cores cut off each sum's low bits (relative error 1e-6 after 1000 terms, growing with their number); the
+// sum of every 512 of K is added up in registers instead, rounded to nearest.
 // The epilogue's eight warps each own 32 rows and half the columns, in chunks of 32: the operands of the next chunk arrive by
 // TMA while this one is computed, the results leave by TMA.
 constexpr int DG_THREADS = 320, DG_EPI = 8;
 constexpr int DG_A_BYTES = 128 * 128;
 constexpr int DG_MAX_STAGES = 8;
-constexpr int DG_SEGMENT = 8;                              // blocks of K in one sum of a LONG tile
-constexpr int DG_BAR_BYTES = 512;
+constexpr int DG_SEGMENT = 8;                              // blocks of K in one sum of an F32 tile
+constexpr int DG_BAR_BYTES = 512 + DG_EPI * 512;            // and 128 columns of the bias for each warp of the epilogue
 constexpr int DG_SMEM = 232448 - 256;                      // what a block can have, less the kernel's own few words
 template <bool PAIR, int BN>
 __host__ __device__ constexpr int dg_stage_bytes() { return DG_A_BYTES + (PAIR ? BN / 2 : BN) * 128; }
@@ -258,9 +306,9 @@ struct Walk {
     }
 };
 
-template <int KIND, bool PAIR, int BN, bool LONG>
+template <int KIND, bool PAIR, int BN, bool F32>
 __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmArgs a) {
-    constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK;
+    constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK, FORWARD = !BACK;
     constexpr int COLS = TWO ? BN / 2 : BN;                // output columns of a tile
     constexpr int TM = PAIR ? 256 : 128;
     constexpr int CHUNKS = COLS / 64;                      // of an epilogue warp
@@ -278,7 +326,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     auto acc_empty = [&](uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 2 + s); };
     auto in_bar = [&](uint32_t w, uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * w + s); };
     const uint32_t drain_bar = bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * DG_EPI);
-    static_assert(8 * (2 * DG_MAX_STAGES + 5 + 2 * DG_EPI) <= DG_BAR_BYTES, "barriers");
+    static_assert(8 * (2 * DG_MAX_STAGES + 5 + 2 * DG_EPI) <= 512, "barriers");
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
@@ -311,7 +359,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     after_predecessor();
     const uint32_t tmem = tmem_slot;
     volatile int* abortp = &abort_flag;
-    const int segments = LONG ? (a.kb + DG_SEGMENT - 1) / DG_SEGMENT : 1;
+    const int segments = F32 ? (a.kb + DG_SEGMENT - 1) / DG_SEGMENT : 1;
 
     if (warp == 0) {
         // ---------------- TMA producer, one per CTA ----------------
@@ -379,7 +427,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
             for (; ok && walk.more(); walk.next()) {
                 for (int k0 = 0; ok && k0 < a.kb; ++n) {
                     const uint32_t buf = n & 1u;
-                    const int k1 = LONG ? min(a.kb, k0 + DG_SEGMENT) : a.kb;
+                    const int k1 = F32 ? min(a.kb, k0 + DG_SEGMENT) : a.kb;
                     if (!wait_warp<PAIR>(acc_empty(buf), ((n >> 1) & 1u) ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
                     for (int k = k0; k < k1; ++k) {
                         if (!wait_warp<false>(full_bar(ps.stage), ps.phase, abortp, a.wait_ns)) { ok = false; break; }
@@ -452,7 +500,9 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 else mbar_arrive(acc_empty_0 + 8u * buf);
             }
         };
-        const int form0 = a.side[OUT0].form, form1 = a.side[OUT1].form, form2 = a.side[OUT2].form;
+        const uint32_t bias_at = bars + 512 + w * 512;
+        const bool twice = a.twice != 0;
+        const int form0 = a.side[OUT0].form, form1 = a.side[OUT1].form;
         const int in0 = a.side[IN0].form, in1 = a.side[IN1].form;
         bool ok = true;
         for (; ok && walk.more(); walk.next()) {
@@ -462,13 +512,33 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 stored();
                 fetch(chunk, row0, col_of(walk, 0));
             }
-            float sum[LONG ? CHUNKS : 1][32];
+            // the bias of the tile's 128 columns around this warp's, one copy a warp
+            const int block = first & ~127, col0 = walk.n * COLS + block;
+            if (KIND == LINEAR && a.bias && valid > 0) {
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < (COLS < 128 ? COLS : 128); c += 32) {
+                    const float v = col0 + c + lane < a.N ? a.bias[col0 + c + lane] : 0.f;
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(bias_at + 4u * (c + lane)), "f"(v) : "memory");
+                }
+                __syncwarp();
+            }
+            auto add_bias = [&](int c, F2 (&v)[4]) {           // to the eight columns from c of that block on
+                if (KIND != LINEAR || !a.bias) return;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 w = lds16(bias_at + 4u * c + 16u * h);
+                    v[2 * h] = add2(v[2 * h], F2{__uint_as_float(w.x), __uint_as_float(w.y)});
+                    v[2 * h + 1] = add2(v[2 * h + 1], F2{__uint_as_float(w.z), __uint_as_float(w.w)});
+                }
+            };
+            F2 sum[F32 ? CHUNKS : 1][4][4];
             uint32_t buf = n & 1u;
-            if (LONG) {
+            if (F32) {
 #pragma unroll
                 for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) sum[i][e] = 0.f;
+                    for (int e = 0; e < 16; ++e) sum[i][e >> 2][e & 3] = both(0.f);
                 for (int s = 0; s < segments; ++s, ++n) {
                     buf = n & 1u;
                     if (!wait_warp<false>(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
@@ -479,39 +549,53 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                         tmem_ld32(lane_tmem + buf * BN + first + 32 * i, r);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) sum[i][e] += __uint_as_float(r[e]);
+                        for (int e = 0; e < 16; ++e)
+                            sum[i][e >> 2][e & 3] = add2(sum[i][e >> 2][e & 3], F2{__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])});
                     }
                     release(buf);
                 }
                 if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) add_bias(first - block + 32 * i + 8 * g, sum[i][g]);
             } else {
                 if (!wait_warp<false>(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
                 tc_fence_after();
                 ++n;
             }
             const uint32_t acc = lane_tmem + buf * BN;
-            // the scales of what is kept in 8 bits: both warps of these rows look at all 128 columns of the block
+            // the scales of what is kept in 8 bits: both warps of these rows look at all 128 columns of the block (F32: one
+            // has them all, in its sums)
             float inv1 = 0.f, inv2 = 0.f;
-            if ((KIND == LINEAR || KIND == GATED) && form1 == kBytes && valid > 0) {
-                const int block = first & ~127, col0 = walk.n * COLS + block;
+            if (FORWARD && form1 == kBytes && valid > 0) {
                 float m1 = 0.f, m2 = 0.f;
+                if (F32) {
+#pragma unroll
+                    for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) m1 = larger(larger(m1, sum[i][e >> 2][e & 3].x), sum[i][e >> 2][e & 3].y);
+                } else {
 #pragma unroll 1
-                for (int c = 0; c < (COLS < 128 ? COLS : 128); c += 32) {
-                    uint32_t r[32];
-                    tmem_ld32(acc + block + c, r);
-                    tmem_ld_wait();
-                    if (KIND == LINEAR && a.bias) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (col0 + c + e < a.N) r[e] = __float_as_uint(__uint_as_float(r[e]) + a.bias[col0 + c + e]);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) m1 = larger(m1, __uint_as_float(r[e]));
-                    if (TWO) {
-                        tmem_ld32(acc + COLS + block + c, r);
+                    for (int c = 0; c < (COLS < 128 ? COLS : 128); c += 32) {
+                        uint32_t r[32];
+                        tmem_ld32(acc + block + c, r);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) m2 = larger(m2, __uint_as_float(r[e]));
+                        for (int g = 0; g < 4; ++g) {
+                            F2 v[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] = F2{__uint_as_float(r[8 * g + 2 * e]), __uint_as_float(r[8 * g + 2 * e + 1])};
+                            add_bias(c + 8 * g, v);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) m1 = larger(larger(m1, v[e].x), v[e].y);
+                        }
+                        if (TWO) {
+                            tmem_ld32(acc + COLS + block + c, r);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) m2 = larger(m2, __uint_as_float(r[e]));
+                        }
                     }
                 }
                 const uint32_t s1 = scale_byte(__float_as_uint(m1)), s2 = scale_byte(__float_as_uint(m2));
@@ -525,21 +609,20 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
             // the scales of what was kept
             float scale0 = 1.f, scale1 = 1.f;
             if (BACK && valid > 0 && row < a.M) {
-                const int block = col_of(walk, 0) >> 7;
-                if (in0 == kBytes) scale0 = scale_of(a.side[IN0].scale[(int64_t)row * a.side[IN0].scale_pitch + block]);
-                if (in1 == kBytes) scale1 = scale_of(a.side[IN1].scale[(int64_t)row * a.side[IN1].scale_pitch + block]);
+                const int at = col_of(walk, 0) >> 7;
+                if (KIND == GATED_BACK && in0 == kBytes) scale0 = scale_of(a.side[IN0].scale[(int64_t)row * a.side[IN0].scale_pitch + at]);
+                if (in1 == kBytes) scale1 = scale_of(a.side[IN1].scale[(int64_t)row * a.side[IN1].scale_pitch + at]);
             }
 
-            auto one_chunk = [&](int i, const float* held) -> bool {
+            auto one_chunk = [&](int i, F2 (&v)[4][4]) -> bool {
                 const int col = col_of(walk, i);
                 const uint32_t b = chunk & 1u;
-                uint32_t r[32], u[TWO ? 32 : 1];
-                if (!LONG) {
-                    tmem_ld32(acc + first + 32 * i, r);
-                    if constexpr (TWO) tmem_ld32(acc + COLS + first + 32 * i, u);
-                }
-                stored();                                      // boxes of the chunk before this one
+                F2 x[TWO ? 4 : 1][4];
+                uint32_t r[F32 ? 1 : 32], u[TWO ? 32 : 1];
+                if constexpr (!F32) tmem_ld32(acc + first + 32 * i, r);
+                if constexpr (TWO) tmem_ld32(acc + COLS + first + 32 * i, u);
                 if (fetches) {
+                    stored();                                  // the next chunk's boxes are free
                     const uint32_t now = chunk;
                     if (i + 1 < valid) {
                         fetch(now + 1, row0, col + 32);
@@ -549,85 +632,77 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                         if (row_of(t) < a.M && col_of(t, 0) < a.N) fetch(now + 1, row_of(t), col_of(t, 0));
                     }
                     if (!wait_warp<false>(in_bar(w, b), (now >> 1) & 1u, abortp, a.wait_ns)) return false;
+                } else {
+                    if (lane == 0) {
+                        if (twice) bulk_wait_read_but_one();
+                        else bulk_wait_read_all();
+                    }
+                    __syncwarp();
                 }
-                for (int k = IN0; k <= IN1; ++k)
-                    if (a.side[k].form != kNone && !a.side[k].tma) box_in(a.side[k], mine + a.side[k].box[b], lane, row0, col, a.M, a.N);
-                if (!LONG) {
+                if constexpr (KIND != GATED)
+                    for (int k = IN0; k <= IN1; ++k)
+                        if (a.side[k].form != kNone && !a.side[k].tma) box_in(a.side[k], mine + a.side[k].box[b], lane, row0, col, a.M, a.N);
+                if constexpr (!F32) {
                     tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e >> 2][e & 3] = F2{__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])};
+                    if constexpr (TWO) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e >> 2][e & 3] = F2{__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1])};
+                    }
                     if (i == CHUNKS - 1) release(buf);
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) add_bias(first - block + 32 * i + 8 * g, v[g]);
                 }
                 const uint32_t box_in0 = mine + a.side[IN0].box[b], box_in1 = mine + a.side[IN1].box[b];
                 const uint32_t box0 = mine + a.side[OUT0].box[b], box1 = mine + a.side[OUT1].box[b], box2 = mine + a.side[OUT2].box[b];
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    float v[8], x[8], y[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = LONG ? held[8 * g + e] : __uint_as_float(r[8 * g + e]);
-                    if (KIND == LINEAR) {
-                        if (a.bias) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (col + 8 * g + e < a.N) v[e] += a.bias[col + 8 * g + e];
-                        }
-                        if (form1 != kNone) write8(form1, box1, lane, g, inv1, v);
-                        with_act(a.act, [&](auto t) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] = value(t, v[e]);
-                        });
-                        if (in0 != kNone) {
-                            read8(in0, box_in0, lane, g, 1.f, x);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] += x[e];
-                        }
-                        write8(form0, box0, lane, g, 1.f, v);
-                    } else if (KIND == LINEAR_BACK) {
-                        if (in1 != kNone) {
-                            read8(in1, box_in1, lane, g, scale1, x);
-                            with_act(a.act, [&](auto t) {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) v[e] *= slope(t, x[e], y[e]);
-                            });
-                            if (form1 != kNone) write8(form1, box1, lane, g, 1.f, y);
-                        }
-                        if (in0 != kNone) {
-                            read8(in0, box_in0, lane, g, 1.f, x);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] += x[e];
-                        }
-                        write8(form0, box0, lane, g, 1.f, v);
-                    } else if (KIND == GATED) {
-                        if constexpr (TWO) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(u[8 * g + e]);
-                        }
-                        if (form1 != kNone) {
-                            write8(form1, box1, lane, g, inv1, v);
-                            write8(form2, box2, lane, g, inv2, x);
-                        }
-                        with_act(a.act, [&](auto t) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] = value(t, v[e]) * x[e];
-                        });
-                        write8(kBf16, box0, lane, g, 1.f, v);
-                    } else {
-                        read8(in0, box_in0, lane, g, scale0, x);
-                        read8(in1, box_in1, lane, g, scale1, y);
-                        float up[8];
-                        with_act(a.act, [&](auto t) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                float h;
-                                const float s = slope(t, x[e], h);
-                                x[e] = v[e] * y[e] * s;
-                                up[e] = v[e] * h;
-                                y[e] *= h;
-                            }
-                        });
-                        if (form0 != kNone) write8(kBf16, box0, lane, g, 1.f, y);
-                        write8(kBf16, box1, lane, g, 1.f, x);
-                        write8(kBf16, box2, lane, g, 1.f, up);
-                    }
+                if constexpr (FORWARD) {
+                    write32(form1, box1, lane, inv1, v);
+                    if constexpr (TWO) write32(form1, box2, lane, inv2, x);
                 }
+                with_act(a.act, [&](auto t) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        F2 p[4], q[4];
+                        if constexpr (KIND == LINEAR) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[g][e] = value(t, v[g][e]);
+                        } else if constexpr (KIND == GATED) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[g][e] = mul2(value(t, v[g][e]), x[g][e]);
+                        } else if constexpr (KIND == LINEAR_BACK) {
+                            if (in1 != kNone) {
+                                read8(in1, box_in1, lane, g, scale1, p);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) v[g][e] = mul2(v[g][e], slope(t, p[e], q[e]));
+                                if (form1 != kNone) write8(kBf16, box1, lane, g, 1.f, q);
+                            }
+                        } else {
+                            read8(in0, box_in0, lane, g, scale0, p);
+                            read8(in1, box_in1, lane, g, scale1, q);
+                            F2 up[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                F2 h;
+                                const F2 s = slope(t, p[e], h);
+                                p[e] = mul2(mul2(v[g][e], q[e]), s);
+                                up[e] = mul2(v[g][e], h);
+                                q[e] = mul2(q[e], h);
+                            }
+                            if (form0 != kNone) write8(kBf16, box0, lane, g, 1.f, q);
+                            write8(kBf16, box1, lane, g, 1.f, p);
+                            write8(kBf16, box2, lane, g, 1.f, up);
+                        }
+                        if constexpr (KIND == LINEAR || KIND == LINEAR_BACK) {
+                            if (in0 != kNone) {
+                                read8(F32 ? kF32 : kBf16, box_in0, lane, g, 1.f, p);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) v[g][e] = add2(v[g][e], p[e]);
+                            }
+                        }
+                        if constexpr (KIND != GATED_BACK) write8(F32 ? kF32 : kBf16, box0, lane, g, 1.f, v[g]);
+                    }
+                });
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
@@ -640,7 +715,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 ++chunk;
                 return true;
             };
-            if constexpr (LONG) {
+            if constexpr (F32) {
 #pragma unroll
                 for (int i = 0; i < CHUNKS; ++i)
                     if (ok && i < valid) ok = one_chunk(i, sum[i]);
@@ -764,7 +839,7 @@ __global__ void __launch_bounds__(32 * FEW_MAX_WARPS) dense_few_kernel(const __g
         const float res = !TWO && a.residual.form != kNone ? load_one(a.residual, (int64_t)m * a.residual.pitch + n) : 0.f;      // before any output
         if (a.out1.form != kNone) store_one(a.out1, (int64_t)m * a.out1.pitch + n, v);
         if (TWO && a.out2.form != kNone) store_one(a.out2, (int64_t)m * a.out2.pitch + n, u);
-        with_act(a.act, [&](auto t) { v = value(t, v); });
+        with_act(a.act, [&](auto t) { v = value(t, both(v)).x; });
         if (TWO) v *= u;
         else if (a.residual.form != kNone) v += res;
         store_one(a.out0, (int64_t)m * a.out0.pitch + n, v);
@@ -800,7 +875,7 @@ struct Product {
     Side side[SIDES];
 };
 
-template <int KIND, bool PAIR, int BN, bool LONG>
+template <int KIND, bool PAIR, int BN, bool F32>
 int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK;
     constexpr int COLS = TWO ? BN / 2 : BN, TM = PAIR ? 256 : 128, STAGE = dg_stage_bytes<PAIR, BN>();
@@ -834,17 +909,21 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     }
     if (rc != ADLOCO_OK) return rc;
     // the boxes of an epilogue warp, largest first so that each starts on a multiple of its swizzle's span: operands twice
-    // (they are fetched a chunk ahead), outputs once, an output over the operand of its form that is read at the same place
+    // (they are fetched a chunk ahead), outputs twice where nothing is fetched and that takes no more than 8 KB, an output over
+    // the operand of its form that is read at the same place
     constexpr int over[SIDES] = {-1, -1, KIND == GATED_BACK ? -1 : IN0, KIND == GATED_BACK ? IN0 : KIND == LINEAR_BACK ? IN1 : -1,
                                  KIND == GATED_BACK ? IN1 : -1};
+    int64_t outputs = 0;
+    for (int i = OUT0; i < SIDES; ++i) outputs += a.side[i].form == kNone ? 0 : 1024 * elem(a.side[i].form);
+    a.twice = a.in_bytes == 0 && 2 * outputs <= 8192;
     uint32_t used = 0;
-    for (int form : {kF32, kBf16, kBytes})
+    for (int form : {(int)kF32, (int)kBf16, (int)kBytes})
         for (int i = 0; i < SIDES; ++i) {
             Side& s = a.side[i];
             if (s.form != form || (over[i] >= 0 && a.side[over[i]].form == form)) continue;
             const uint32_t bytes = (uint32_t)(1024 * elem(form));
             s.box[0] = used;
-            s.box[1] = i <= IN1 ? used + bytes : used;
+            s.box[1] = i <= IN1 || a.twice ? used + bytes : used;
             used = s.box[1] + bytes;
         }
     for (int i = OUT0; i < SIDES; ++i)
@@ -854,7 +933,7 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     const int64_t left = DG_SMEM - 1024 - DG_BAR_BYTES - (int64_t)DG_EPI * a.warp_bytes;
     a.stages = (int)(left / STAGE < DG_MAX_STAGES ? left / STAGE : DG_MAX_STAGES);
     if (a.stages < 2) return ADLOCO_ERR_UNSUPPORTED;
-    auto* kernel = dense_tile_kernel<KIND, PAIR, BN, LONG>;
+    auto* kernel = dense_tile_kernel<KIND, PAIR, BN, F32>;
     static std::atomic<bool> attr_set[64];            // the attribute is per device
     if (!attr_set[ctx->device & 63].load()) {
         ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DG_SMEM));
@@ -867,20 +946,24 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     return ADLOCO_OK;
 }
 
-template <int KIND, bool LONG>
+template <int KIND, bool F32>
 int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     constexpr int COLS = KIND == GATED ? 128 : 256;
     const int64_t pairs = ((p.M + 255) / 256) * ((p.N + COLS - 1) / COLS);
-    if (pairs >= ctx->sm_count / 2 && cta_pairs_possible(ctx)) return launch_tiles<KIND, true, 256, LONG>(ctx, p, st);
-    bool bytes = false;                               // 8-bit outputs: a block of 128 columns in one tile
+    if (pairs >= ctx->sm_count / 2 && cta_pairs_possible(ctx)) return launch_tiles<KIND, true, 256, F32>(ctx, p, st);
+    bool bytes = false;                               // 8-bit outputs: a block of 128 columns in one tile (F32: in one warp)
     for (int i = OUT0; i < SIDES; ++i) bytes = bytes || p.side[i].form == kBytes;
     const int64_t rows = (p.M + 127) / 128;
+    [[maybe_unused]] const bool wide = bytes || rows * ((p.N + 127) / 128) >= ctx->sm_count;
     if constexpr (KIND == GATED) {
-        if (bytes || rows * ((p.N + 127) / 128) >= ctx->sm_count) return launch_tiles<KIND, false, 256, LONG>(ctx, p, st);
-        return launch_tiles<KIND, false, 128, LONG>(ctx, p, st);
+        if (wide) return launch_tiles<KIND, false, 256, F32>(ctx, p, st);
+        return launch_tiles<KIND, false, 128, F32>(ctx, p, st);
     } else {
-        if (bytes || rows * ((p.N + 127) / 128) >= ctx->sm_count) return launch_tiles<KIND, false, 128, LONG>(ctx, p, st);
-        return launch_tiles<KIND, false, 64, LONG>(ctx, p, st);
+        if constexpr (KIND == LINEAR && F32) {
+            if (bytes) return launch_tiles<KIND, false, 256, F32>(ctx, p, st);
+        }
+        if (wide) return launch_tiles<KIND, false, 128, F32>(ctx, p, st);
+        return launch_tiles<KIND, false, 64, F32>(ctx, p, st);
     }
 }
 
@@ -912,8 +995,7 @@ int launch_linear(adloco_ctx* ctx, const adloco_linear_args& c, cudaStream_t st)
     p.side[OUT0] = side_of(c.y, c.y_stride, form);
     p.side[OUT1] = kept_side(c.z);
     if (c.M <= FEW_MAX_M && p.side[OUT1].form != kBytes) return launch_few<false>(ctx, p, st);
-    return form == kF32 && c.K > 64 * DG_SEGMENT && p.side[OUT1].form != kBytes ? choose_tiles<LINEAR, true>(ctx, p, st)
-                                                                               : choose_tiles<LINEAR, false>(ctx, p, st);
+    return form == kF32 ? choose_tiles<LINEAR, true>(ctx, p, st) : choose_tiles<LINEAR, false>(ctx, p, st);
 }
 
 int launch_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args& c, cudaStream_t st) {
@@ -923,7 +1005,7 @@ int launch_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args& c
     p.side[IN1] = kept_side(c.z);
     p.side[OUT0] = side_of(c.dx, c.dx_stride, form);
     p.side[OUT1] = side_of(c.a, c.a_stride, kBf16);
-    return form == kF32 && c.N > 64 * DG_SEGMENT ? choose_tiles<LINEAR_BACK, true>(ctx, p, st) : choose_tiles<LINEAR_BACK, false>(ctx, p, st);
+    return form == kF32 ? choose_tiles<LINEAR_BACK, true>(ctx, p, st) : choose_tiles<LINEAR_BACK, false>(ctx, p, st);
 }
 
 int launch_gated_linear(adloco_ctx* ctx, const adloco_gated_linear_args& c, cudaStream_t st) {

@@ -5,6 +5,7 @@
 
 #include "common.cuh"
 #include "e4m3.cuh"
+#include "f32x2.cuh"
 #include "ptx.cuh"
 
 namespace adloco {
@@ -14,11 +15,6 @@ using namespace ptx;
 namespace {
 
 constexpr float kLog2e = 1.44269504f;
-__device__ __forceinline__ float exp2_fast(float x) {          // relative error 2^-22; 0 below 2^-126
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ float max_or_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -75,48 +71,50 @@ struct Run {
 // One pass with the running maximum m and the sums S = sum e^(l - m), E = sum (l - m) e^(l - m) of each thread's share:
 //   lse = m + log S,   entropy = log S - E / S.
 // A row is shared by TPR threads (a warp, or a block), a long row of few by the blocks of a cluster.  m starts at the
-// lowest finite number, so that l - m is a number for every finite l, and -Inf gives the 0 that it should.
+// lowest finite number, so that l - m is a number for every finite l, and -Inf gives the 0 that it should.  Shares are
+// brought to the row's maximum once and then only added (joined two by two, each pair with its own maximum, they cost
+// half as much as the pass itself).
 //
-// The best tokens: the top-th largest of the maxima of 128 groups of threads (32 in a warp) is a lower bound of the
-// top-th largest logit.  Only the few threads whose own maximum reaches it have anything that counts: the row's threads
-// look at those threads' shares once more together, collect what reaches the bound, and sort that by counting.  Where
-// too much reaches it (long runs of equal logits), they take the best one by one instead, a pass over the row for each.
+// The best tokens: the top-th largest of the maxima of G groups of threads is a lower bound of the top-th largest
+// logit.  Only the few threads whose own maximum reaches it have anything that counts: the row's threads look at those
+// threads' shares once more together, collect what reaches the bound, and sort that by counting.  Where too much
+// reaches it (long runs of equal logits), they take the best one by one instead, a pass over the row for each.
 constexpr int kMaxTop = 64;
-constexpr int kTopThreads = 512;
+constexpr int kTopThreads = 256;
 constexpr int kCluster = 8;
 template <int TPR> __host__ __device__ constexpr int groups_of() { return TPR < 128 ? TPR : 128; }
-template <int TPR> __host__ __device__ constexpr int candidates_of() { return TPR == 32 ? 512 : 1024; }
+constexpr int kCandidates = 512;                                // of a row
+static_assert(kCluster * kMaxTop <= kCandidates, "what a cluster's blocks bring");
 
 // a number's place among numbers as an unsigned one, NaN lowest, -0 as 0; then the lower index first
-__device__ __forceinline__ uint64_t key_of(float v, int index) {
+__device__ __forceinline__ uint32_t place_of(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);
-    const uint32_t o = v != v ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
-    return ((uint64_t)o << 32) | (uint32_t)~index;
+    return v != v ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float value_of(uint64_t key) {
-    const uint32_t o = (uint32_t)(key >> 32);
-    return o == 0u ? __uint_as_float(0x7fffffffu) : __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
+__device__ __forceinline__ float number_at(uint32_t place) {
+    return place == 0u ? __uint_as_float(0x7fffffffu) : __uint_as_float((place & 0x80000000u) ? place & 0x7fffffffu : ~place);
 }
+__device__ __forceinline__ uint64_t key_of(float v, int index) { return ((uint64_t)place_of(v) << 32) | (uint32_t)~index; }
+__device__ __forceinline__ float value_of(uint64_t key) { return number_at((uint32_t)(key >> 32)); }
 
 struct Sums { float m, s, e; };
-__device__ __forceinline__ Sums joined(const Sums& a, const Sums& b) {
-    const float m = fmaxf(a.m, b.m), da = a.m - m, db = b.m - m;
-    const float fa = exp2_fast(da * kLog2e), fb = exp2_fast(db * kLog2e);
-    // (l - m) e^(l - m) over a's share, with l - m = (l - a.m) + da; a share without numbers has s = 0, and da may be huge
-    const float ea = a.s == 0.f ? 0.f : fmaf(da, a.s, a.e) * fa, eb = b.s == 0.f ? 0.f : fmaf(db, b.s, b.e) * fb;
-    return Sums{m, fmaf(a.s, fa, b.s * fb), (fa == 0.f && a.s == a.s ? 0.f : ea) + (fb == 0.f && b.s == b.s ? 0.f : eb)};
+// sums to a maximum m that is no smaller.  A share without numbers has s = 0; the distance may be beyond all bounds.
+__device__ __forceinline__ Sums brought_to(const Sums& a, float m) {
+    const float d = a.m - m, f = exp2_fast(d * kLog2e);
+    return Sums{m, a.s * f, f == 0.f && a.s == a.s ? 0.f : fmaf(d, a.s, a.e) * f};
 }
 
 template <int TPR>
 struct RowShared {
-    Sums sums[TPR / 32];
-    float group_max[groups_of<TPR>()];
-    float bound;
+    float m[TPR / 32], s[TPR / 32], e[TPR / 32];
+    Sums sums;
+    uint32_t group_max[groups_of<TPR>()];
+    uint32_t bound;
     int hot, found;
     unsigned short hot_thread[TPR];
     uint64_t best[kMaxTop];
     uint64_t wave[TPR / 32];
-    uint64_t candidate[candidates_of<TPR>()];
+    uint64_t candidate[kCandidates];
 };
 
 struct LogprobArgs {
@@ -135,7 +133,7 @@ __device__ __forceinline__ void row_sync() {
 }
 
 template <typename T, bool ENTROPY, int U>
-__device__ __forceinline__ void add_piece(const uint4 (&w)[U], Sums& a, float& top) {
+__device__ __forceinline__ void add_pieces(const uint4 (&w)[U], Sums& a, float& top) {
     constexpr int N = Piece<T>::N;
     float v[U][N];
     float m = -INFINITY;
@@ -143,37 +141,29 @@ __device__ __forceinline__ void add_piece(const uint4 (&w)[U], Sums& a, float& t
     for (int u = 0; u < U; ++u) {
         unpack(w[u], v[u]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) m = fmaxf(m, v[u][i]);
+        for (int i = 0; i < N; i += 2) m = fmaxf(m, fmaxf(v[u][i], v[u][i + 1]));
     }
     top = fmaxf(top, m);
-    if (m > a.m) {
-        const float d = a.m - m, f = exp2_fast(d * kLog2e);
-        if (ENTROPY) a.e = f == 0.f && a.s == a.s ? 0.f : fmaf(d, a.s, a.e) * f;
-        a.s *= f;
-        a.m = m;
-    }
+    if (m > a.m) a = brought_to(a, m);
+    const F2 minus = both(-a.m);
+    F2 s = both(0.f), e = both(0.f);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        float s0 = 0.f, s1 = 0.f, e0 = 0.f, e1 = 0.f;
+    for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
-            const float d0 = v[u][i] - a.m, d1 = v[u][i + 1] - a.m;
-            const float x0 = exp2_fast(d0 * kLog2e), x1 = exp2_fast(d1 * kLog2e);
-            s0 += x0; s1 += x1;
-            if (ENTROPY) { e0 = fmaf(x0, max_or_nan(d0, -1e4f), e0); e1 = fmaf(x1, max_or_nan(d1, -1e4f), e1); }
+            const F2 d = add2(F2{v[u][i], v[u][i + 1]}, minus), x = exp2_fast(mul2(d, both(kLog2e)));
+            s = add2(s, x);
+            if (ENTROPY) e = fma2(x, F2{max_or_nan(d.x, -1e4f), max_or_nan(d.y, -1e4f)}, e);
         }
-        a.s += s0 + s1;
-        if (ENTROPY) a.e += e0 + e1;
-    }
+    a.s += s.x + s.y;
+    if (ENTROPY) a.e += e.x + e.y;
 }
 __device__ __forceinline__ void add_one(float v, Sums& a, float& top) {
     top = fmaxf(top, v);
-    const float m = fmaxf(a.m, v);
-    const float d = a.m - m, f = exp2_fast(d * kLog2e);
-    const float dv = v - m, x = exp2_fast(dv * kLog2e);
-    a.e = (f == 0.f && a.s == a.s ? 0.f : fmaf(d, a.s, a.e) * f) + x * max_or_nan(dv, -1e4f);
-    a.s = fmaf(a.s, f, x);
-    a.m = m;
+    a = brought_to(a, fmaxf(a.m, v));
+    const float d = v - a.m, x = exp2_fast(d * kLog2e);
+    a.s += x;
+    a.e = fmaf(x, max_or_nan(d, -1e4f), a.e);
 }
 
 // The largest `top` keys of a run of n numbers whose first has index `base`, in order, into sh.best; all threads of the row.
@@ -204,71 +194,10 @@ __device__ __noinline__ void best_one_by_one(RowShared<TPR>& sh, const T* p, int
     row_sync<TPR>();
 }
 
-template <typename T, int TPR>
-__device__ __forceinline__ void best_of_run(RowShared<TPR>& sh, const Run<T>& run, int n, int base, int top, float own_max) {
-    constexpr int G = groups_of<TPR>(), CAP = candidates_of<TPR>(), N = Piece<T>::N;
-    const int t = threadIdx.x & (TPR - 1);
-    float g = own_max;
-#pragma unroll
-    for (int o = TPR / G / 2; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
-    if (t % (TPR / G) == 0) sh.group_max[t / (TPR / G)] = g;
-    if (t == 0) { sh.hot = 0; sh.found = 0; sh.bound = -INFINITY; }
-    row_sync<TPR>();
-    if (t < G && top <= G) {
-        const float mine = sh.group_max[t];
-        int above = 0;
-#pragma unroll 8
-        for (int i = 0; i < G; ++i) {
-            const float other = sh.group_max[i];
-            above += other > mine || (other == mine && i < t);
-        }
-        if (above == top - 1) sh.bound = mine;
-    }
-    row_sync<TPR>();
-    const float bound = sh.bound;
-    if (own_max >= bound) sh.hot_thread[atomicAdd(&sh.hot, 1)] = (unsigned short)t;
-    row_sync<TPR>();
-    const int hot = sh.hot;
-    auto offer = [&](float v, int i) {
-        if (v >= bound) {
-            const int at = atomicAdd(&sh.found, 1);
-            if (at < CAP) sh.candidate[at] = key_of(v, base + i);
-        }
-    };
-    const int shares = (run.body + TPR - 1) / TPR + 1;          // pieces of a thread, and its one of the head and of the tail
-    for (int i = t; i < hot * shares; i += TPR) {
-        const int who = sh.hot_thread[i % hot], k = i / hot - 1;
-        if (k < 0) {
-            if (who < run.head) offer(number(run.p + who), who);
-            if (who < run.tail) offer(number(run.p + n - run.tail + who), n - run.tail + who);
-        } else if (who + k * TPR < run.body) {
-            const int piece = who + k * TPR;
-            float v[N];
-            unpack(run.pieces()[piece], v);
-#pragma unroll
-            for (int e = 0; e < N; ++e) offer(v[e], run.index(piece) + e);
-        }
-    }
-    row_sync<TPR>();
-    const int found = sh.found;
-    if (found > CAP || found < min(top, n)) {                   // too much reaches the bound, or NaN in the way
-        best_one_by_one<T, TPR>(sh, run.p, n, base, top);
-        return;
-    }
-    for (int i = t; i < found; i += TPR) {
-        const uint64_t key = sh.candidate[i];
-        int above = 0;
-        for (int j = 0; j < found; ++j) above += sh.candidate[j] > key;
-        if (above < top) sh.best[above] = key;
-    }
-    for (int i = found + t; i < top; i += TPR) sh.best[i] = 0;
-    row_sync<TPR>();
-}
-
 template <typename T, int TPR, bool CLUSTER, bool ENTROPY>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) logprob_kernel(const __grid_constant__ LogprobArgs a) {
     constexpr int ROWS = TPR < 128 ? 128 / TPR : 1;             // of a block
-    constexpr int U = 4;
+    constexpr int U = 4, N = Piece<T>::N;
     __shared__ RowShared<TPR> shared_rows[ROWS];
     RowShared<TPR>& sh = shared_rows[threadIdx.x / TPR];
     const int t = threadIdx.x & (TPR - 1), lane = t & 31;
@@ -282,53 +211,135 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) logprob_kernel(const __
     const int from = min(a.V, (int)rank * part), n = min(a.V - from, part);
     const T* p = static_cast<const T*>(a.logits) + row * a.stride;
     const Run<T> run(p + from, n);
+    const int32_t target = a.logp && t == 0 && rank == 0 ? a.targets[row] : -1;
+    const bool given = target >= 0 && target < a.V;
+    const float at_target = given ? number(p + target) : 0.f;
     Sums sums = {-3.402823466e38f, 0.f, 0.f};
     float own_max = -INFINITY;
     {
         const uint4* pieces = run.pieces();
+        if (t < run.head) add_one(number(run.p + t), sums, own_max);
+        if (t < run.tail) add_one(number(run.p + n - run.tail + t), sums, own_max);
         int i = t;
         for (; i + (U - 1) * TPR < run.body; i += U * TPR) {
             uint4 w[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) w[u] = pieces[i + u * TPR];
-            add_piece<T, ENTROPY, U>(w, sums, own_max);
+            add_pieces<T, ENTROPY, U>(w, sums, own_max);
         }
         for (; i < run.body; i += TPR) {
             const uint4 w[1] = {pieces[i]};
-            add_piece<T, ENTROPY, 1>(w, sums, own_max);
+            add_pieces<T, ENTROPY, 1>(w, sums, own_max);
         }
-        if (t < run.head) add_one(number(run.p + t), sums, own_max);
-        if (t < run.tail) add_one(number(run.p + n - run.tail + t), sums, own_max);
     }
-    Sums all = sums;
+    // the row's maximum, and the maxima of groups of threads, each with its number in the low bits so that no two are alike
+    // (which lowers a bound made of them, if anything)
+    const int G = TPR < 128 ? TPR : a.top <= 16 ? 64 : 128;
+    float m = sums.m, g = own_max;
+    for (int o = 1; o < TPR / G; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
+    if (a.top && t % (TPR / G) == 0) sh.group_max[t / (TPR / G)] = (place_of(g) & ~127u) | (uint32_t)(t / (TPR / G));
+    if (t == 0) { sh.hot = 0; sh.found = 0; sh.bound = 0; }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (TPR > 32) {
+        if (lane == 0) sh.m[t >> 5] = m;
+        row_sync<TPR>();
+#pragma unroll
+        for (int i = 0; i < TPR / 32; ++i) m = fmaxf(m, sh.m[i]);
+    } else {
+        row_sync<TPR>();
+    }
+    Sums all = brought_to(sums, m);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        const Sums other = {__shfl_xor_sync(0xffffffffu, all.m, o), __shfl_xor_sync(0xffffffffu, all.s, o), __shfl_xor_sync(0xffffffffu, all.e, o)};
-        all = joined(all, other);
+        all.s += __shfl_xor_sync(0xffffffffu, all.s, o);
+        if (ENTROPY) all.e += __shfl_xor_sync(0xffffffffu, all.e, o);
     }
+    if (TPR > 32 && lane == 0) { sh.s[t >> 5] = all.s; sh.e[t >> 5] = all.e; }
+    if (a.top && a.top <= G && t < G) {
+        const uint32_t mine = sh.group_max[t];
+        const uint4* others = reinterpret_cast<const uint4*>(sh.group_max);
+        int above = 0;
+#pragma unroll 4
+        for (int i = 0; i < G / 4; ++i) {
+            const uint4 o = others[i];
+            above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+        }
+        if (above == a.top - 1) sh.bound = mine & ~127u;
+    }
+    row_sync<TPR>();
     if (TPR > 32) {
-        if (lane == 0) sh.sums[t >> 5] = all;
-        row_sync<TPR>();
-        all = sh.sums[0];
-        for (int i = 1; i < TPR / 32; ++i) all = joined(all, sh.sums[i]);
-        row_sync<TPR>();
+        all.s = all.e = 0.f;
+#pragma unroll
+        for (int i = 0; i < TPR / 32; ++i) { all.s += sh.s[i]; all.e += sh.e[i]; }
     }
-    if (a.top) best_of_run<T, TPR>(sh, run, n, from, a.top, own_max);
-    int own_top = a.top;
+    if (a.top) {
+        const uint32_t bound = sh.bound;
+        if (place_of(own_max) >= bound) sh.hot_thread[atomicAdd(&sh.hot, 1)] = (unsigned short)t;
+        row_sync<TPR>();
+        const int hot = sh.hot;
+        auto offer = [&](float v, int i) {
+            const uint32_t place = place_of(v);
+            if (place >= bound && place != 0u) {
+                const int at = atomicAdd(&sh.found, 1);
+                if (at < kCandidates) sh.candidate[at] = ((uint64_t)place << 32) | (uint32_t)~(from + i);
+            }
+        };
+        const int shares = (run.body + TPR - 1) / TPR + 1;      // pieces of a thread, and its one of the head and of the tail
+        for (int i = t; i < hot * shares; i += TPR) {
+            const int who = sh.hot_thread[i % hot], k = i / hot - 1;
+            if (k < 0) {
+                if (who < run.head) offer(number(run.p + who), who);
+                if (who < run.tail) offer(number(run.p + n - run.tail + who), n - run.tail + who);
+            } else if (who + k * TPR < run.body) {
+                const int piece = who + k * TPR;
+                float v[N];
+                unpack(run.pieces()[piece], v);
+#pragma unroll
+                for (int e = 0; e < N; ++e) offer(v[e], run.index(piece) + e);
+            }
+        }
+        row_sync<TPR>();
+        const int found = sh.found;
+        if (found > kCandidates || found < min(a.top, n)) {     // too much reaches the bound, or NaN in the way
+            best_one_by_one<T, TPR>(sh, run.p, n, from, a.top);
+        } else {
+            for (int i = t; i < found; i += TPR) {
+                const uint64_t key = sh.candidate[i];
+                int above = 0;
+                for (int j = 0; j < found; ++j) above += sh.candidate[j] > key;
+                if (above < a.top) sh.best[above] = key;
+            }
+            for (int i = found + t; i < a.top; i += TPR) sh.best[i] = 0;
+            row_sync<TPR>();
+        }
+    }
+    all.m = m;
     if (CLUSTER) {                                              // the first block takes all blocks' sums and best
-        if (t == 0) sh.sums[0] = all;
+        if (t == 0) sh.sums = all;
         __syncthreads();
         cluster_all_started();
         cluster_sync_all();
         if (rank == 0) {
-            const uint32_t at = smem_u32(&sh.sums[0]), list = smem_u32(&sh.best[0]);
+            const uint32_t at = smem_u32(&sh.sums), list = smem_u32(&sh.best[0]);
             auto far = [](uint32_t addr, uint32_t r) {
                 uint32_t v;
                 asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_to_cta(addr, r)) : "memory");
                 return v;
             };
-            for (uint32_t r = 1; r < (uint32_t)kCluster; ++r)
-                all = joined(all, Sums{__uint_as_float(far(at, r)), __uint_as_float(far(at + 4, r)), __uint_as_float(far(at + 8, r))});
+            Sums each[kCluster];
+#pragma unroll
+            for (int r = 0; r < kCluster; ++r) {
+                each[r] = Sums{__uint_as_float(far(at, r)), __uint_as_float(far(at + 4, r)), __uint_as_float(far(at + 8, r))};
+                all.m = fmaxf(all.m, each[r].m);
+            }
+            all.s = all.e = 0.f;
+#pragma unroll
+            for (int r = 0; r < kCluster; ++r) {
+                const Sums s = brought_to(each[r], all.m);
+                all.s += s.s;
+                all.e += s.e;
+            }
             for (int i = t; i < kCluster * a.top; i += TPR) {
                 const uint32_t r = (uint32_t)(i / a.top), k = (uint32_t)(i % a.top);
                 sh.candidate[i] = (uint64_t)far(list + 8 * k, r) | ((uint64_t)far(list + 8 * k + 4, r) << 32);
@@ -351,16 +362,11 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) logprob_kernel(const __
     const float log_s = logf(all.s);
     const float lse = none ? -INFINITY : all.m + log_s;
     if (t == 0) {
-        if (a.logp) {
-            const int32_t target = a.targets[row];
-            float v = 0.f;
-            if (target >= 0 && target < a.V) v = none ? -INFINITY : number(p + target) - lse;
-            a.logp[row] = v;
-        }
+        if (a.logp) a.logp[row] = !given ? 0.f : none ? -INFINITY : at_target - lse;
         if (ENTROPY) a.entropy[row] = none ? 0.f : log_s - __fdiv_rn(all.e, all.s);
         if (a.lse) a.lse[row] = lse;
     }
-    for (int i = t; i < own_top; i += TPR) {
+    for (int i = t; i < a.top; i += TPR) {
         const uint64_t key = sh.best[i];
         a.top_values[row * a.top + i] = none ? -INFINITY : value_of(key) - lse;
         a.top_ids[row * a.top + i] = (int32_t)~(uint32_t)key;
@@ -389,14 +395,19 @@ __global__ void __launch_bounds__(256) logprob_back_kernel(const __grid_constant
         const T* p = static_cast<const T*>(a.logits) + row * a.stride + from;
         T* out = static_cast<T*>(a.d_logits) + row * a.out_stride + from;
         const int target = a.targets[row];
-        const float lse = a.lse[row], s = target >= 0 && target < a.V ? a.d_logp[row] : 0.f;
+        const float lse = a.lse[row], weight = a.d_logp[row], s = target >= 0 && target < a.V ? weight : 0.f;
         const float c = a.d_entropy ? a.d_entropy[row] : 0.f, H = a.d_entropy ? a.entropy[row] : 0.f;
         const bool zero = (s == 0.f && c == 0.f) || lse == -INFINITY;
         const int at = target - from;
+        // -p (c (log p + H) + s); where p is 0 the logarithm is kept finite
+        const F2 minus = both(-lse), slope = both(-c), offset = both(-fmaf(c, H, s));
+        auto two = [&](F2 l) {
+            const F2 d = add2(l, minus), x = {max_or_nan(d.x, -1e4f), max_or_nan(d.y, -1e4f)};
+            return mul2(exp2_fast(mul2(x, both(kLog2e))), fma2(x, slope, offset));
+        };
         auto one = [&](float l, int i) {
             if (zero) return 0.f;
-            const float x = max_or_nan(l - lse, -1e4f), prob = exp2_fast(x * kLog2e);
-            const float d = -prob * fmaf(c, x + H, s);
+            const float d = two(both(l)).x;
             return i == at ? d + s : d;
         };
         Run<T> run(p, n);
@@ -416,10 +427,18 @@ __global__ void __launch_bounds__(256) logprob_back_kernel(const __grid_constant
                 if (i0 + u * TPR >= run.body) continue;
                 float v[N];
                 unpack(w[u], v);
-                const int first = run.index(i0 + u * TPR);
+                const int mine = at - run.index(i0 + u * TPR);  // the target's place among these
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[e] = one(v[e], first + e);
-                __stcs(to + i0 + u * TPR, repack(v));
+                for (int e = 0; e < N; e += 2) {
+                    const F2 d = two(F2{v[e], v[e + 1]});
+                    v[e] = d.x;
+                    v[e + 1] = d.y;
+                }
+                if (mine >= 0 && mine < N) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[e] += e == mine ? s : 0.f;
+                }
+                __stcs(to + i0 + u * TPR, zero ? make_uint4(0u, 0u, 0u, 0u) : repack(v));
             }
         }
         if (t < run.head) put(out + t, one(number(p + t), t));
@@ -532,8 +551,8 @@ int launch_logprob_rows(adloco_ctx* ctx, const LogprobArgs& a, cudaStream_t st) 
 }
 template <typename T>
 int launch_logprob(adloco_ctx* ctx, const LogprobArgs& a, cudaStream_t st) {
-    if (a.V <= 512) return launch_logprob_rows<T, 32, false>(ctx, a, st);
-    if (a.V <= 4096) return launch_logprob_rows<T, 128, false>(ctx, a, st);
+    // a warp a row while its 32 maxima bound the best tokens, or all of the row are candidates
+    if (a.V <= kCandidates || (a.V <= 4096 && a.top <= 24)) return launch_logprob_rows<T, 32, false>(ctx, a, st);
     // a cluster a row where there are fewer rows than would fill the machine and each is long
     if (a.rows * 4 <= ctx->sm_count && a.V >= 16384 && cta_pairs_possible(ctx)) return launch_logprob_rows<T, kTopThreads, true>(ctx, a, st);
     return launch_logprob_rows<T, kTopThreads, false>(ctx, a, st);
