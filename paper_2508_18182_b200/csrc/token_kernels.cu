@@ -108,7 +108,7 @@ template <int TPR>
 struct RowShared {
     float m[TPR / 32], s[TPR / 32], e[TPR / 32];
     Sums sums;
-    uint32_t group_max[groups_of<TPR>()];
+    alignas(16) uint32_t group_max[groups_of<TPR>()];
     uint32_t bound;
     int hot, found;
     unsigned short hot_thread[TPR];
