@@ -80,8 +80,10 @@ struct Run {
 // threads' shares once more together, collect what reaches the bound, and sort that by counting.  Where too much
 // reaches it (long runs of equal logits), they take the best one by one instead, a pass over the row for each.
 constexpr int kMaxTop = 64;
-constexpr int kTopThreads = 256;
+constexpr int kTopThreads = 256, kClusterThreads = 512;
 constexpr int kCluster = 8;
+// 64 registers a thread: more blocks with fewer spill (8192 x 50257 bf16: 170 us; with 5 and 6 blocks an SM 235 and 312)
+template <int TPR, bool CLUSTER> constexpr int kBlocks = TPR == 32 ? 8 : CLUSTER ? 2 : 4;
 template <int TPR> __host__ __device__ constexpr int groups_of() { return TPR < 128 ? TPR : 128; }
 constexpr int kCandidates = 512;                                // of a row
 static_assert(kCluster * kMaxTop <= kCandidates, "what a cluster's blocks bring");
@@ -158,12 +160,12 @@ __device__ __forceinline__ void add_pieces(const uint4 (&w)[U], Sums& a, float& 
     a.s += s.x + s.y;
     if (ENTROPY) a.e += e.x + e.y;
 }
-__device__ __forceinline__ void add_one(float v, Sums& a, float& top) {
-    top = fmaxf(top, v);
-    a = brought_to(a, fmaxf(a.m, v));
-    const float d = v - a.m, x = exp2_fast(d * kLog2e);
-    a.s += x;
-    a.e = fmaf(x, max_or_nan(d, -1e4f), a.e);
+__device__ __forceinline__ void add_two(float u, float v, Sums& a, float& top) {      // -Inf adds nothing
+    top = fmaxf(top, fmaxf(u, v));
+    a = brought_to(a, fmaxf(a.m, fmaxf(u, v)));
+    const F2 d = {u - a.m, v - a.m}, x = exp2_fast(mul2(d, both(kLog2e)));
+    a.s += x.x + x.y;
+    a.e += fmaf(x.x, max_or_nan(d.x, -1e4f), x.y * max_or_nan(d.y, -1e4f));
 }
 
 // The largest `top` keys of a run of n numbers whose first has index `base`, in order, into sh.best; all threads of the row.
@@ -195,9 +197,10 @@ __device__ __noinline__ void best_one_by_one(RowShared<TPR>& sh, const T* p, int
 }
 
 template <typename T, int TPR, bool CLUSTER, bool ENTROPY>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) logprob_kernel(const __grid_constant__ LogprobArgs a) {
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, kBlocks<TPR, CLUSTER>) logprob_kernel(const __grid_constant__ LogprobArgs a) {
     constexpr int ROWS = TPR < 128 ? 128 / TPR : 1;             // of a block
-    constexpr int U = 4, N = Piece<T>::N;
+    constexpr int U = TPR > 32 && sizeof(T) == 4 ? 8 : 4, N = Piece<T>::N;      // pieces a thread has on their way
+    constexpr bool PRE = TPR > 32 && sizeof(T) == 2;            // the next U while U are added up: where these take the longer time
     __shared__ RowShared<TPR> shared_rows[ROWS];
     RowShared<TPR>& sh = shared_rows[threadIdx.x / TPR];
     const int t = threadIdx.x & (TPR - 1), lane = t & 31;
@@ -217,20 +220,33 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) logprob_kernel(const __
     Sums sums = {-3.402823466e38f, 0.f, 0.f};
     float own_max = -INFINITY;
     {
+        // the ends of the row come first and are added last
+        const float first = t < run.head ? number(run.p + t) : -INFINITY, last = t < run.tail ? number(run.p + n - run.tail + t) : -INFINITY;
         const uint4* pieces = run.pieces();
-        if (t < run.head) add_one(number(run.p + t), sums, own_max);
-        if (t < run.tail) add_one(number(run.p + n - run.tail + t), sums, own_max);
-        int i = t;
-        for (; i + (U - 1) * TPR < run.body; i += U * TPR) {
+        uint4 next[U];
+        auto load = [&](int i) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * TPR < run.body) next[u] = pieces[i + u * TPR];
+        };
+        load(t);
+        for (int i = t; i < run.body; i += U * TPR) {
             uint4 w[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) w[u] = pieces[i + u * TPR];
-            add_pieces<T, ENTROPY, U>(w, sums, own_max);
+            for (int u = 0; u < U; ++u) w[u] = next[u];
+            if (PRE) load(i + U * TPR);
+            if (i + (U - 1) * TPR < run.body) {
+                add_pieces<T, ENTROPY, U>(w, sums, own_max);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U - 1; ++u) {
+                    const uint4 one[1] = {w[u]};
+                    if (i + u * TPR < run.body) add_pieces<T, ENTROPY, 1>(one, sums, own_max);
+                }
+            }
+            if (!PRE) load(i + U * TPR);
         }
-        for (; i < run.body; i += TPR) {
-            const uint4 w[1] = {pieces[i]};
-            add_pieces<T, ENTROPY, 1>(w, sums, own_max);
-        }
+        add_two(first, last, sums, own_max);
     }
     // the row's maximum, and the maxima of groups of threads, each with its number in the low bits so that no two are alike
     // (which lowers a bound made of them, if anything)
@@ -274,29 +290,34 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) logprob_kernel(const __
         for (int i = 0; i < TPR / 32; ++i) { all.s += sh.s[i]; all.e += sh.e[i]; }
     }
     if (a.top) {
-        const uint32_t bound = sh.bound;
-        if (place_of(own_max) >= bound) sh.hot_thread[atomicAdd(&sh.hot, 1)] = (unsigned short)t;
+        const uint32_t bound = sh.bound;                        // below -Inf's place (too few groups): everything counts
+        const float least = bound < 0x007fffffu ? -INFINITY : number_at(bound);
+        if (own_max >= least) sh.hot_thread[atomicAdd(&sh.hot, 1)] = (unsigned short)t;
         row_sync<TPR>();
         const int hot = sh.hot;
         auto offer = [&](float v, int i) {
-            const uint32_t place = place_of(v);
-            if (place >= bound && place != 0u) {
-                const int at = atomicAdd(&sh.found, 1);
-                if (at < kCandidates) sh.candidate[at] = ((uint64_t)place << 32) | (uint32_t)~(from + i);
-            }
+            const int at = atomicAdd(&sh.found, 1);
+            if (at < kCandidates) sh.candidate[at] = key_of(v, from + i);
         };
-        const int shares = (run.body + TPR - 1) / TPR + 1;      // pieces of a thread, and its one of the head and of the tail
-        for (int i = t; i < hot * shares; i += TPR) {
-            const int who = sh.hot_thread[i % hot], k = i / hot - 1;
+        // pieces of a thread, and its one of the head and of the tail: a power of two or less
+        const int bits = 32 - __clz((run.body + TPR - 1) / TPR);
+        for (int i = t; i < hot << bits; i += TPR) {
+            const int who = sh.hot_thread[i >> bits], k = (i & ((1 << bits) - 1)) - 1;
             if (k < 0) {
-                if (who < run.head) offer(number(run.p + who), who);
-                if (who < run.tail) offer(number(run.p + n - run.tail + who), n - run.tail + who);
+                const int last = n - run.tail + who;
+                if (who < run.head && number(run.p + who) >= least) offer(number(run.p + who), who);
+                if (who < run.tail && number(run.p + last) >= least) offer(number(run.p + last), last);
             } else if (who + k * TPR < run.body) {
                 const int piece = who + k * TPR;
                 float v[N];
                 unpack(run.pieces()[piece], v);
+                uint32_t hits = 0;                              // few: one after the other, lanes together
 #pragma unroll
-                for (int e = 0; e < N; ++e) offer(v[e], run.index(piece) + e);
+                for (int e = 0; e < N; ++e) hits |= v[e] >= least ? 1u << e : 0u;
+                for (; hits; hits &= hits - 1) {
+                    const int at = run.index(piece) + __ffs(hits) - 1;
+                    offer(number(run.p + at), at);
+                }
             }
         }
         row_sync<TPR>();
@@ -307,6 +328,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) logprob_kernel(const __
             for (int i = t; i < found; i += TPR) {
                 const uint64_t key = sh.candidate[i];
                 int above = 0;
+#pragma unroll 4
                 for (int j = 0; j < found; ++j) above += sh.candidate[j] > key;
                 if (above < a.top) sh.best[above] = key;
             }
@@ -352,6 +374,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) logprob_kernel(const __
             for (int i = t; i < found; i += TPR) {
                 const uint64_t key = sh.candidate[i];
                 int above = 0;
+#pragma unroll 4
                 for (int j = 0; j < found; ++j) above += sh.candidate[j] > key;
                 if (key != 0 && above < a.top) sh.best[above] = key;
             }
@@ -549,12 +572,13 @@ int launch_logprob_rows(adloco_ctx* ctx, const LogprobArgs& a, cudaStream_t st) 
     ctx->launches++;
     return ADLOCO_OK;
 }
+constexpr int kWarpV = 12288;
 template <typename T>
 int launch_logprob(adloco_ctx* ctx, const LogprobArgs& a, cudaStream_t st) {
-    // a warp a row while its 32 maxima bound the best tokens, or all of the row are candidates
-    if (a.V <= kCandidates || (a.V <= 4096 && a.top <= 24)) return launch_logprob_rows<T, 32, false>(ctx, a, st);
     // a cluster a row where there are fewer rows than would fill the machine and each is long
-    if (a.rows * 4 <= ctx->sm_count && a.V >= 16384 && cta_pairs_possible(ctx)) return launch_logprob_rows<T, kTopThreads, true>(ctx, a, st);
+    if (a.rows * 4 <= ctx->sm_count && a.V >= 16384 && cta_pairs_possible(ctx)) return launch_logprob_rows<T, kClusterThreads, true>(ctx, a, st);
+    // a warp a row while its 32 maxima bound the best tokens and there are rows for many warps, or where all of the row are candidates
+    if (a.V <= kCandidates || (a.V <= kWarpV && a.top <= 24 && a.rows >= 8 * ctx->sm_count)) return launch_logprob_rows<T, 32, false>(ctx, a, st);
     return launch_logprob_rows<T, kTopThreads, false>(ctx, a, st);
 }
 template <typename T>
