@@ -3,6 +3,7 @@
 //   dx = (dy W) act'(z)      d_gate = (dy Wd) up act'(gate),  d_up = (dy Wd) act(gate).
 // What the backward pass needs (z, or gate and up) is kept in bf16 or in 8 bits with a power-of-two scale for each block
 // of 128 of a row, written by the forward epilogue and read by the backward one; the layer's input is recomputed there.
+#include <algorithm>
 #include <atomic>
 #include <cuda_fp8.h>
 
@@ -41,6 +42,7 @@ struct GemmArgs {
     int tiles_n, tiles;
     int act;
     int stages;
+    int a_bytes;                      // of A in a stage: of all its 128 rows, or of those that exist
     uint32_t warp_bytes;              // boxes of one epilogue warp
     uint32_t in_bytes;                // that arrive by TMA for one chunk
     int twice;                        // outputs have two boxes each, for even and odd chunks
@@ -148,23 +150,32 @@ __device__ __forceinline__ void bytes_to_pairs(uint32_t w, float s, F2* v) {
         v[h] = mul2(F2{f.x, f.y}, both(s));
     }
 }
-// columns 8 g .. 8 g + 7 of this lane's row; s: the scale of bytes
-__device__ __forceinline__ void read8(int form, uint32_t box, int row, int g, float s, F2 (&v)[4]) {
-    if (form == kBf16) {
-        const uint4 w = lds16(piece_at<4>(box, row, g));
-        v[0] = pair_of(w.x); v[1] = pair_of(w.y); v[2] = pair_of(w.z); v[3] = pair_of(w.w);
-    } else if (form == kF32) {
+// A chunk's operand of this lane's row as it lies in its box: read in one go, ahead of all that is computed from it (reads
+// and writes of shared memory keep their order, so that reads between writes would each wait for what is computed before).
+template <int FORM> struct Raw32 { uint4 w[FORM == kF32 ? 8 : FORM == kBf16 ? 4 : 2]; };
+template <int FORM>
+__device__ __forceinline__ void read32(uint32_t box, int row, Raw32<FORM>& r) {
+    constexpr int P = FORM == kF32 ? 8 : FORM == kBf16 ? 4 : 2;
+#pragma unroll
+    for (int i = 0; i < P; ++i) r.w[i] = lds16(piece_at<P>(box, row, i));
+}
+// its columns 8 g .. 8 g + 7; s: the scale of bytes
+template <int FORM>
+__device__ __forceinline__ void numbers8(const Raw32<FORM>& r, int g, float s, F2 (&v)[4]) {
+    if constexpr (FORM == kF32) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint4 w = lds16(piece_at<8>(box, row, 2 * g + h));
+            const uint4 w = r.w[2 * g + h];
             v[2 * h] = F2{__uint_as_float(w.x), __uint_as_float(w.y)};
             v[2 * h + 1] = F2{__uint_as_float(w.z), __uint_as_float(w.w)};
         }
+    } else if constexpr (FORM == kBf16) {
+        const uint4 w = r.w[g];
+        v[0] = pair_of(w.x); v[1] = pair_of(w.y); v[2] = pair_of(w.z); v[3] = pair_of(w.w);
     } else {
-        uint32_t a, b;
-        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(piece_at<2>(box, row, g >> 1) + 8u * (g & 1)) : "memory");
-        bytes_to_pairs(a, s, v);
-        bytes_to_pairs(b, s, v + 2);
+        const uint4 w = r.w[g >> 1];
+        bytes_to_pairs((g & 1) ? w.z : w.x, s, v);
+        bytes_to_pairs((g & 1) ? w.w : w.y, s, v + 2);
     }
 }
 __device__ __forceinline__ uint32_t pack(F2 v) { return pack_bf16(__float_as_uint(v.x), __float_as_uint(v.y)); }
@@ -204,17 +215,14 @@ __device__ __forceinline__ void box_in_of(const Side& s, uint32_t box, int lane,
     constexpr int P = sizeof(W) == 4 ? 8 : 4, EACH = 16 / sizeof(W);
     const W* from = static_cast<const W*>(s.p) + (int64_t)row0 * s.pitch + col + lane;
     const int rows = col + lane < N ? M - row0 : 0;
-#pragma unroll 1
-    for (int row = 0; row < 32; row += 16) {           // sixteen rows' loads in flight
-        W v[16];
+    W v[32];                                           // all rows' loads in flight
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = row + i < rows ? from[(row + i) * s.pitch] : W(0);
+    for (int i = 0; i < 32; ++i) v[i] = i < rows ? from[i * s.pitch] : W(0);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t to = piece_at<P>(box, row + i, lane / EACH) + (uint32_t)(lane % EACH * sizeof(W));
-            if (sizeof(W) == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"((uint32_t)v[i]) : "memory");
-            else asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"((unsigned short)v[i]) : "memory");
-        }
+    for (int i = 0; i < 32; ++i) {
+        const uint32_t to = piece_at<P>(box, i, lane / EACH) + (uint32_t)(lane % EACH * sizeof(W));
+        if (sizeof(W) == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"((uint32_t)v[i]) : "memory");
+        else asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"((unsigned short)v[i]) : "memory");
     }
 }
 __device__ __noinline__ void box_in(const Side& s, uint32_t box, int lane, int row0, int col, int M, int N) {
@@ -306,7 +314,7 @@ struct Walk {
     }
 };
 
-template <int KIND, bool PAIR, int BN, bool F32>
+template <int KIND, bool PAIR, int BN, bool F32, bool IN8>
 __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmArgs a) {
     constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK, FORWARD = !BACK;
     constexpr int COLS = TWO ? BN / 2 : BN;                // output columns of a tile
@@ -373,7 +381,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     if (!mbar_wait(empty_bar(ps.stage), ps.phase ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
                     const uint32_t sA = smem_base + ps.stage * STAGE, sB = sA + DG_A_BYTES;
                     const uint32_t bar = PAIR ? map_to_cta(full_bar(ps.stage), 0) : full_bar(ps.stage);
-                    if (rank == 0) mbar_arrive_expect_tx(full_bar(ps.stage), (PAIR ? 2 : 1) * STAGE);
+                    if (rank == 0) mbar_arrive_expect_tx(full_bar(ps.stage), (PAIR ? 2 : 1) * (STAGE - DG_A_BYTES + a.a_bytes));
                     auto load = [&](uint32_t dst, const CUtensorMap* m, int c0, int c1) {
                         if (PAIR) tma_load_2d_pair(dst, m, bar, c0, c1);
                         else tma_load_2d(dst, m, bar, c0, c1);
@@ -502,8 +510,20 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
         };
         const uint32_t bias_at = bars + 512 + w * 512;
         const bool twice = a.twice != 0;
+        const bool by_hand = KIND != GATED && KIND != GATED_BACK && a.side[IN0].form != kNone && !a.side[IN0].tma;
+        constexpr int OUT = F32 ? kF32 : kBf16, KEPT = IN8 ? kBytes : kBf16, FORM0 = KIND == GATED_BACK ? KEPT : OUT;
         const int form0 = a.side[OUT0].form, form1 = a.side[OUT1].form;
         const int in0 = a.side[IN0].form, in1 = a.side[IN1].form;
+        constexpr int AROUND = COLS < 128 ? COLS : 128;
+        float bias_next[AROUND / 32];
+        auto load_bias = [&](const Walk& t) {
+#pragma unroll
+            for (int c = 0; c < AROUND / 32; ++c) {
+                const int at = t.n * COLS + (first & ~127) + 32 * c + lane;
+                bias_next[c] = at < a.N ? a.bias[at] : 0.f;
+            }
+        };
+        if (KIND == LINEAR && a.bias && walk.more()) load_bias(walk);
         bool ok = true;
         for (; ok && walk.more(); walk.next()) {
             const int row0 = row_of(walk), row = row0 + lane;
@@ -512,16 +532,24 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 stored();
                 fetch(chunk, row0, col_of(walk, 0));
             }
-            // the bias of the tile's 128 columns around this warp's, one copy a warp
+            if (by_hand && valid > 0) {                        // a residual whose rows lie anywhere: two chunks before the accumulator
+                stored();
+                for (int i = 0; i < min(2, valid); ++i)
+                    box_in(a.side[IN0], mine + a.side[IN0].box[(chunk + i) & 1u], lane, row0, col_of(walk, i), a.M, a.N);
+            }
+            // the bias of the tile's 128 columns around this warp's, one copy a warp; the next tile's is on its way meanwhile
             const int block = first & ~127, col0 = walk.n * COLS + block;
-            if (KIND == LINEAR && a.bias && valid > 0) {
+            if (KIND == LINEAR && a.bias) {
                 __syncwarp();
 #pragma unroll
-                for (int c = 0; c < (COLS < 128 ? COLS : 128); c += 32) {
-                    const float v = col0 + c + lane < a.N ? a.bias[col0 + c + lane] : 0.f;
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(bias_at + 4u * (c + lane)), "f"(v) : "memory");
-                }
+                for (int c = 0; c < AROUND / 32; ++c)
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(bias_at + 4u * (32 * c + lane)), "f"(bias_next[c]) : "memory");
                 __syncwarp();
+                if (walk.left > 1) {
+                    Walk t = walk;
+                    t.next();
+                    load_bias(t);
+                }
             }
             auto add_bias = [&](int c, F2 (&v)[4]) {           // to the eight columns from c of that block on
                 if (KIND != LINEAR || !a.bias) return;
@@ -577,7 +605,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                         for (int e = 0; e < 16; ++e) m1 = larger(larger(m1, sum[i][e >> 2][e & 3].x), sum[i][e >> 2][e & 3].y);
                 } else {
 #pragma unroll 1
-                    for (int c = 0; c < (COLS < 128 ? COLS : 128); c += 32) {
+                    for (int c = 0; c < AROUND; c += 32) {
                         uint32_t r[32];
                         tmem_ld32(acc + block + c, r);
                         tmem_ld_wait();
@@ -608,10 +636,10 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
             }
             // the scales of what was kept
             float scale0 = 1.f, scale1 = 1.f;
-            if (BACK && valid > 0 && row < a.M) {
+            if (IN8 && valid > 0 && row < a.M) {
                 const int at = col_of(walk, 0) >> 7;
-                if (KIND == GATED_BACK && in0 == kBytes) scale0 = scale_of(a.side[IN0].scale[(int64_t)row * a.side[IN0].scale_pitch + at]);
-                if (in1 == kBytes) scale1 = scale_of(a.side[IN1].scale[(int64_t)row * a.side[IN1].scale_pitch + at]);
+                if (KIND == GATED_BACK) scale0 = scale_of(a.side[IN0].scale[(int64_t)row * a.side[IN0].scale_pitch + at]);
+                scale1 = scale_of(a.side[IN1].scale[(int64_t)row * a.side[IN1].scale_pitch + at]);
             }
 
             auto one_chunk = [&](int i, F2 (&v)[4][4]) -> bool {
@@ -639,9 +667,6 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     }
                     __syncwarp();
                 }
-                if constexpr (KIND != GATED)
-                    for (int k = IN0; k <= IN1; ++k)
-                        if (a.side[k].form != kNone && !a.side[k].tma) box_in(a.side[k], mine + a.side[k].box[b], lane, row0, col, a.M, a.N);
                 if constexpr (!F32) {
                     tmem_ld_wait();
 #pragma unroll
@@ -660,6 +685,12 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     write32(form1, box1, lane, inv1, v);
                     if constexpr (TWO) write32(form1, box2, lane, inv2, x);
                 }
+                Raw32<FORM0> raw0;                             // the residual, or gate
+                Raw32<KEPT> raw1;                              // z, or up
+                if constexpr (KIND != GATED && FORM0 != kF32)  // (an fp32 one would take the registers of the sums)
+                    if (in0 != kNone) read32<FORM0>(box_in0, lane, raw0);
+                if constexpr (BACK)
+                    if (in1 != kNone) read32<KEPT>(box_in1, lane, raw1);
                 with_act(a.act, [&](auto t) {
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
@@ -672,14 +703,14 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                             for (int e = 0; e < 4; ++e) v[g][e] = mul2(value(t, v[g][e]), x[g][e]);
                         } else if constexpr (KIND == LINEAR_BACK) {
                             if (in1 != kNone) {
-                                read8(in1, box_in1, lane, g, scale1, p);
+                                numbers8<KEPT>(raw1, g, scale1, p);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) v[g][e] = mul2(v[g][e], slope(t, p[e], q[e]));
                                 if (form1 != kNone) write8(kBf16, box1, lane, g, 1.f, q);
                             }
                         } else {
-                            read8(in0, box_in0, lane, g, scale0, p);
-                            read8(in1, box_in1, lane, g, scale1, q);
+                            numbers8<KEPT>(raw0, g, scale0, p);
+                            numbers8<KEPT>(raw1, g, scale1, q);
                             F2 up[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
@@ -695,7 +726,11 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                         }
                         if constexpr (KIND == LINEAR || KIND == LINEAR_BACK) {
                             if (in0 != kNone) {
-                                read8(F32 ? kF32 : kBf16, box_in0, lane, g, 1.f, p);
+                                if constexpr (FORM0 == kF32) {
+                                    raw0.w[2 * g] = lds16(piece_at<8>(box_in0, lane, 2 * g));
+                                    raw0.w[2 * g + 1] = lds16(piece_at<8>(box_in0, lane, 2 * g + 1));
+                                }
+                                numbers8<FORM0>(raw0, g, 1.f, p);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) v[g][e] = add2(v[g][e], p[e]);
                             }
@@ -712,6 +747,10 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 }
                 for (int k = OUT0; k <= OUT2; ++k)
                     if (a.side[k].form != kNone && !a.side[k].tma) box_out(a.side[k], mine + a.side[k].box[b], lane, row0, col, a.M, a.N);
+                if (by_hand && i + 2 < valid) {
+                    stored();
+                    box_in(a.side[IN0], mine + a.side[IN0].box[b], lane, row0, col + 64, a.M, a.N);
+                }
                 ++chunk;
                 return true;
             };
@@ -875,7 +914,7 @@ struct Product {
     Side side[SIDES];
 };
 
-template <int KIND, bool PAIR, int BN, bool F32>
+template <int KIND, bool PAIR, int BN, bool F32, bool IN8>
 int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK;
     constexpr int COLS = TWO ? BN / 2 : BN, TM = PAIR ? 256 : 128, STAGE = dg_stage_bytes<PAIR, BN>();
@@ -888,7 +927,10 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     a.status = ctx->gemm_status; a.wait_ns = ctx->wait_limit_ns;
     a.in_bytes = 0;
     Maps maps;
-    int rc = make_map(ctx, &maps.a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.a, p.M, p.K, p.a_stride, 64, 128);
+    // (what lies in the rest of A's 128 rows only reaches rows of the result that do not exist)
+    const uint32_t a_rows = p.M < 128 ? (uint32_t)(p.M + 7) / 8 * 8 : 128;
+    a.a_bytes = (int)a_rows * 128;
+    int rc = make_map(ctx, &maps.a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.a, p.M, p.K, p.a_stride, 64, a_rows);
     for (int i = 0; i < (TWO ? 2 : 1) && rc == ADLOCO_OK; ++i)
         rc = BACK ? make_map(ctx, &maps.b[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.b[i], p.K, p.N, p.b_stride[i], 64, 64)
                   : make_map(ctx, &maps.b[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.b[i], p.N, p.K, p.b_stride[i], 64, TWO ? COLS : PAIR ? BN / 2 : BN);
@@ -933,7 +975,7 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     const int64_t left = DG_SMEM - 1024 - DG_BAR_BYTES - (int64_t)DG_EPI * a.warp_bytes;
     a.stages = (int)(left / STAGE < DG_MAX_STAGES ? left / STAGE : DG_MAX_STAGES);
     if (a.stages < 2) return ADLOCO_ERR_UNSUPPORTED;
-    auto* kernel = dense_tile_kernel<KIND, PAIR, BN, F32>;
+    auto* kernel = dense_tile_kernel<KIND, PAIR, BN, F32, IN8>;
     static std::atomic<bool> attr_set[64];            // the attribute is per device
     if (!attr_set[ctx->device & 63].load()) {
         ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DG_SMEM));
@@ -946,25 +988,38 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     return ADLOCO_OK;
 }
 
-template <int KIND, bool F32>
+// Which tiles: those that take the least time in rounds of all SMs.  A stage of 64 of K takes a CTA as long as L2 needs to
+// deliver its operands, 64 bytes a clock: 512 clocks for a pair's 256 x 256 (as long as its MMAs) and for one CTA's 128 x 128,
+// 384 for a pair's 256 x 128 and one CTA's 128 x 64, less where A has fewer rows; a tile's epilogue as much as four (two, one) stages
+// that nothing hides when there is one round.
+template <int KIND, bool F32, bool IN8 = false>
 int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
-    constexpr int COLS = KIND == GATED ? 128 : 256;
-    const int64_t pairs = ((p.M + 255) / 256) * ((p.N + COLS - 1) / COLS);
-    if (pairs >= ctx->sm_count / 2 && cta_pairs_possible(ctx)) return launch_tiles<KIND, true, 256, F32>(ctx, p, st);
+    constexpr int SHARE = KIND == GATED ? 2 : 1;      // of a tile's columns a projection's are
     bool bytes = false;                               // 8-bit outputs: a block of 128 columns in one tile (F32: in one warp)
     for (int i = OUT0; i < SIDES; ++i) bytes = bytes || p.side[i].form == kBytes;
-    const int64_t rows = (p.M + 127) / 128;
-    [[maybe_unused]] const bool wide = bytes || rows * ((p.N + 127) / 128) >= ctx->sm_count;
+    const bool pairs = cta_pairs_possible(ctx);
+    const int64_t kb = (p.K + 63) / 64, a_rows = p.M < 128 ? p.M : 128;
+    auto clocks = [&](int64_t tile_m, int64_t tile_n, int64_t workers, int64_t bytes_a_stage, int64_t epilogue) {
+        const int64_t tiles = ((p.M + tile_m - 1) / tile_m) * ((p.N + tile_n / SHARE - 1) / (tile_n / SHARE)), rounds = (tiles + workers - 1) / workers;
+        return rounds * kb * (bytes_a_stage / 64) + epilogue * 512 * (rounds > 1 ? 1 : 2);
+    };
+    const int64_t never = int64_t(1) << 62, sms = ctx->sm_count;
+    const int64_t pair256 = pairs ? clocks(256, 256, sms / 2, a_rows * 128 + 16384, 4) : never;
+    const int64_t pair128 = pairs && !(bytes && (SHARE == 2 || F32)) ? clocks(256, 128, sms / 2, a_rows * 128 + 8192, 2) : never;
+    const int64_t solo128 = bytes && SHARE == 2 ? never : clocks(128, 128, sms, a_rows * 128 + 16384, 2);
+    const int64_t least = std::min(std::min(pair256, pair128), solo128);
     if constexpr (KIND == GATED) {
-        if (wide) return launch_tiles<KIND, false, 256, F32>(ctx, p, st);
-        return launch_tiles<KIND, false, 128, F32>(ctx, p, st);
+        if (bytes && clocks(128, 256, sms, a_rows * 128 + 32768, 4) < pair256) return launch_tiles<KIND, false, 256, F32, IN8>(ctx, p, st);
     } else {
+        if (!bytes && clocks(128, 64, sms, a_rows * 128 + 8192, 1) < least) return launch_tiles<KIND, false, 64, F32, IN8>(ctx, p, st);
         if constexpr (KIND == LINEAR && F32) {
-            if (bytes) return launch_tiles<KIND, false, 256, F32>(ctx, p, st);
+            if (bytes) return pair256 < clocks(128, 256, sms, a_rows * 128 + 32768, 4) ? launch_tiles<KIND, true, 256, F32, IN8>(ctx, p, st)
+                                                                                      : launch_tiles<KIND, false, 256, F32, IN8>(ctx, p, st);
         }
-        if (wide) return launch_tiles<KIND, false, 128, F32>(ctx, p, st);
-        return launch_tiles<KIND, false, 64, F32>(ctx, p, st);
     }
+    if (least == pair256) return launch_tiles<KIND, true, 256, F32, IN8>(ctx, p, st);
+    if (least == pair128) return launch_tiles<KIND, true, 128, F32, IN8>(ctx, p, st);
+    return launch_tiles<KIND, false, 128, F32, IN8>(ctx, p, st);
 }
 
 template <bool TWO>
@@ -1005,6 +1060,7 @@ int launch_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args& c
     p.side[IN1] = kept_side(c.z);
     p.side[OUT0] = side_of(c.dx, c.dx_stride, form);
     p.side[OUT1] = side_of(c.a, c.a_stride, kBf16);
+    if (c.z.scale) return form == kF32 ? choose_tiles<LINEAR_BACK, true, true>(ctx, p, st) : choose_tiles<LINEAR_BACK, false, true>(ctx, p, st);
     return form == kF32 ? choose_tiles<LINEAR_BACK, true>(ctx, p, st) : choose_tiles<LINEAR_BACK, false>(ctx, p, st);
 }
 
@@ -1024,7 +1080,7 @@ int launch_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_back
     p.side[OUT0] = side_of(c.a, c.a_stride, kBf16);
     p.side[OUT1] = side_of(c.d_gate, c.d_gate_stride, kBf16);
     p.side[OUT2] = side_of(c.d_up, c.d_up_stride, kBf16);
-    return choose_tiles<GATED_BACK, false>(ctx, p, st);
+    return c.gate.scale ? choose_tiles<GATED_BACK, false, true>(ctx, p, st) : choose_tiles<GATED_BACK, false>(ctx, p, st);
 }
 
 }  // namespace adloco
