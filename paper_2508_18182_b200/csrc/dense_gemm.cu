@@ -38,10 +38,11 @@ struct Side {
 
 struct GemmArgs {
     int M, N, K;                      // output rows, output columns (of each projection), contraction
-    int kb;                           // blocks of 64 along K
+    int kb;                           // stages along K
     int tiles_n, tiles;
     int act;
     int stages;
+    int split;                        // CTAs that share a tile's K, one cluster (1: none do)
     int a_bytes;                      // of A in a stage: of all its 128 rows, or of those that exist
     uint32_t warp_bytes;              // boxes of one epilogue warp
     uint32_t in_bytes;                // that arrive by TMA for one chunk
@@ -284,6 +285,8 @@ __device__ __forceinline__ float larger(float m, float v) {
 // has both numbers of an output.
 // F32 (outputs): the tensor cores cut off each sum's low bits (relative error 1e-6 after 1000 terms, growing with their number); the
 // sum of every 512 of K is added up in registers instead, rounded to nearest.
+// SPLIT K: where few tiles leave most SMs idle, up to four CTAs of a cluster take a part of K each.  All but the first write
+// their sums into the first one's shared memory, which adds them up in their order and goes on alone.
 // The epilogue's eight warps each own 32 rows and half the columns, in chunks of 32: the operands of the next chunk arrive by
 // TMA while this one is computed, the results leave by TMA.
 constexpr int DG_THREADS = 320, DG_EPI = 8;
@@ -293,7 +296,13 @@ constexpr int DG_SEGMENT = 8;                              // blocks of K in one
 constexpr int DG_BAR_BYTES = 512 + DG_EPI * 512;            // and 128 columns of the bias for each warp of the epilogue
 constexpr int DG_SMEM = 232448 - 256;                      // what a block can have, less the kernel's own few words
 template <bool PAIR, int BN>
-__host__ __device__ constexpr int dg_stage_bytes() { return DG_A_BYTES + (PAIR ? BN / 2 : BN) * 128; }
+__host__ __device__ constexpr int dg_block_bytes() { return DG_A_BYTES + (PAIR ? BN / 2 : BN) * 128; }      // of 64 of K
+// Blocks of K in a stage: waits, signals and issue take a thread about 370 clocks a stage, more than a small tile's operands and
+// MMAs (256 x 4096 x 4096, operands in L2: 16.7 us with one block a stage, 12.9 with two).
+template <bool PAIR, int BN>
+__host__ __device__ constexpr int dg_stage_blocks() { return BN == 64 || (PAIR && BN == 128) ? 2 : 1; }
+template <bool PAIR, int BN>
+__host__ __device__ constexpr int dg_stage_bytes() { return dg_block_bytes<PAIR, BN>() * dg_stage_blocks<PAIR, BN>(); }
 
 // The tiles of one worker: dealt round, the tiles along N fastest, so that all workers sit on the same rows of A at a time.
 struct Walk {
@@ -320,7 +329,8 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     constexpr int COLS = TWO ? BN / 2 : BN;                // output columns of a tile
     constexpr int TM = PAIR ? 256 : 128;
     constexpr int CHUNKS = COLS / 64;                      // of an epilogue warp
-    constexpr int STAGE = dg_stage_bytes<PAIR, BN>();
+    constexpr int STAGE = dg_stage_bytes<PAIR, BN>(), BLOCK = dg_block_bytes<PAIR, BN>(), BLOCKS = dg_stage_blocks<PAIR, BN>();
+    constexpr int SEGMENT = DG_SEGMENT / BLOCKS;           // stages in one sum of an F32 tile
     constexpr int B_ROWS = PAIR ? BN / 2 : BN;             // of the weight (or of its columns, backward) in a CTA's stage
     static_assert(CHUNKS >= 1 && (!BACK || B_ROWS % 64 == 0), "a chunk is 32 columns, a box of the weight's columns 64");
 
@@ -333,14 +343,17 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     auto acc_full = [&](uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + s); };
     auto acc_empty = [&](uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 2 + s); };
     auto in_bar = [&](uint32_t w, uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * w + s); };
-    const uint32_t drain_bar = bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * DG_EPI);
-    static_assert(8 * (2 * DG_MAX_STAGES + 5 + 2 * DG_EPI) <= 512, "barriers");
+    const uint32_t drain_bar = bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * DG_EPI), join_bar = drain_bar + 8u;
+    const uint32_t join = bars + DG_BAR_BYTES;                 // the other parts' sums
+    static_assert(8 * (2 * DG_MAX_STAGES + 6 + 2 * DG_EPI) <= 512, "barriers");
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // warp: known to be uniform
     const uint32_t rank = PAIR ? cluster_cta_rank() : 0;       // 0: the CTA that issues the MMAs
-    Walk walk(a, PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x);
+    const uint32_t split = PAIR ? 1u : (uint32_t)a.split, part = PAIR || split == 1 ? 0u : cluster_cta_rank();
+    Walk walk(a, PAIR ? (int)(blockIdx.x >> 1) : (int)(blockIdx.x / split), PAIR ? (int)(gridDim.x >> 1) : (int)(gridDim.x / split));
+    const int k_first = (int)(a.kb * part / split), k_end = (int)(a.kb * (part + 1) / split);      // this CTA's blocks of K
     const uint32_t stages = (uint32_t)a.stages;
     if (threadIdx.x == 0) {
         abort_flag = 0;
@@ -349,6 +362,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
         for (uint32_t w = 0; w < DG_EPI; ++w)
             for (uint32_t s = 0; s < 2; ++s) mbar_init(in_bar(w, s), 1);
         mbar_init(drain_bar, 1);
+        mbar_init(join_bar, (split - 1) * DG_EPI + 1);
         fence_barrier_init();
         prefetch_tmap(&maps.a);
         prefetch_tmap(&maps.b[0]);
@@ -362,49 +376,57 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     }
     tc_fence_before();
     __syncthreads();
-    if (PAIR) cluster_sync_all();                              // the peer's barriers exist before anything is signalled on them
+    if (PAIR || split > 1) cluster_sync_all();                 // the peers' barriers exist before anything is signalled on them
     tc_fence_after();
     after_predecessor();
     const uint32_t tmem = tmem_slot;
     volatile int* abortp = &abort_flag;
-    const int segments = F32 ? (a.kb + DG_SEGMENT - 1) / DG_SEGMENT : 1;
+    const int segments = F32 ? (k_end - k_first + SEGMENT - 1) / SEGMENT : 1;
 
     if (warp == 0) {
         // ---------------- TMA producer, one per CTA ----------------
-        if (lane == 0) {
+        {
+            const bool leader = elect_one();
             Ring ps;
             uint32_t issued = 0;
             bool ok = true;
             for (; ok && walk.more(); walk.next()) {
                 const int m0 = walk.m * TM + (int)rank * 128, n0 = walk.n * COLS;
-                for (int k = 0; k < a.kb; ++k) {
-                    if (!mbar_wait(empty_bar(ps.stage), ps.phase ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
-                    const uint32_t sA = smem_base + ps.stage * STAGE, sB = sA + DG_A_BYTES;
-                    const uint32_t bar = PAIR ? map_to_cta(full_bar(ps.stage), 0) : full_bar(ps.stage);
-                    if (rank == 0) mbar_arrive_expect_tx(full_bar(ps.stage), (PAIR ? 2 : 1) * (STAGE - DG_A_BYTES + a.a_bytes));
-                    auto load = [&](uint32_t dst, const CUtensorMap* m, int c0, int c1) {
-                        if (PAIR) tma_load_2d_pair(dst, m, bar, c0, c1);
-                        else tma_load_2d(dst, m, bar, c0, c1);
-                    };
-                    load(sA, &maps.a, k * 64, m0);
-                    if (TWO) {
-                        if (PAIR) {
-                            load(sB, &maps.b[rank], k * 64, n0);
-                        } else {
-                            load(sB, &maps.b[0], k * 64, n0);
-                            load(sB + COLS * 128, &maps.b[1], k * 64, n0);
-                        }
-                    } else if (!BACK) {
-                        load(sB, &maps.b[0], k * 64, n0 + (int)rank * B_ROWS);
-                    } else {
+                for (int k = k_first; k < k_end; ++k) {
+                    if (!wait_warp<false>(empty_bar(ps.stage), ps.phase ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
+                    if (leader) {
+                        const uint32_t bar = PAIR ? map_to_cta(full_bar(ps.stage), 0) : full_bar(ps.stage);
+                        if (rank == 0) mbar_arrive_expect_tx(full_bar(ps.stage), (PAIR ? 2 : 1) * BLOCKS * (BLOCK - DG_A_BYTES + a.a_bytes));
+                        auto load = [&](uint32_t dst, const CUtensorMap* m, int c0, int c1) {
+                            if (PAIR) tma_load_2d_pair(dst, m, bar, c0, c1);
+                            else tma_load_2d(dst, m, bar, c0, c1);
+                        };
 #pragma unroll
-                        for (int c = 0; c < B_ROWS; c += 64) load(sB + c * 128, &maps.b[0], n0 + (int)rank * B_ROWS + c, k * 64);
+                        for (int s = 0; s < BLOCKS; ++s) {
+                            const uint32_t sA = smem_base + ps.stage * STAGE + s * BLOCK, sB = sA + DG_A_BYTES;
+                            const int at = (k * BLOCKS + s) * 64;      // beyond K: zeros
+                            load(sA, &maps.a, at, m0);
+                            if (TWO) {
+                                if (PAIR) {
+                                    load(sB, &maps.b[rank], at, n0);
+                                } else {
+                                    load(sB, &maps.b[0], at, n0);
+                                    load(sB + COLS * 128, &maps.b[1], at, n0);
+                                }
+                            } else if (!BACK) {
+                                load(sB, &maps.b[0], at, n0 + (int)rank * B_ROWS);
+                            } else {
+#pragma unroll
+                                for (int c = 0; c < B_ROWS; c += 64) load(sB + c * 128, &maps.b[0], n0 + (int)rank * B_ROWS + c, at);
+                            }
+                        }
                     }
+                    __syncwarp();
                     ++issued;
                     ps.advance(stages);
                 }
             }
-            if (!ok) {
+            if (!ok && leader) {
                 if (PAIR) {
                     // leaving after a time-out: the byte counts of copies in flight complete on the even CTA's barriers, which
                     // the odd CTA cannot wait on: both sit out a grace period far beyond the flight time of a copy
@@ -421,6 +443,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     }
                 }
             }
+            __syncwarp();
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer (of a pair the even CTA's; the whole warp keeps step, one lane issues) ----------------
@@ -433,9 +456,9 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
             uint32_t n = 0;
             bool ok = true;
             for (; ok && walk.more(); walk.next()) {
-                for (int k0 = 0; ok && k0 < a.kb; ++n) {
+                for (int k0 = k_first; ok && k0 < k_end; ++n) {
                     const uint32_t buf = n & 1u;
-                    const int k1 = F32 ? min(a.kb, k0 + DG_SEGMENT) : a.kb;
+                    const int k1 = F32 ? min(k_end, k0 + SEGMENT) : k_end;
                     if (!wait_warp<PAIR>(acc_empty(buf), ((n >> 1) & 1u) ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
                     for (int k = k0; k < k1; ++k) {
                         if (!wait_warp<false>(full_bar(ps.stage), ps.phase, abortp, a.wait_ns)) { ok = false; break; }
@@ -444,11 +467,11 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                             const uint32_t at = smem_base + ps.stage * STAGE;
                             const uint64_t dA = descA + (at >> 4), dB = descB + ((at + DG_A_BYTES) >> 4);
 #pragma unroll
-                            for (int kk = 0; kk < 4; ++kk) {
+                            for (int kk = 0; kk < 4 * BLOCKS; ++kk) {
                                 // 16 of K further: 32 bytes along a row, or 16 rows of 128 bytes
-                                const uint64_t db = dB + (BACK ? 128 : 2) * kk;
-                                if (PAIR) mma_bf16_pair(tmem + buf * BN, dA + 2 * kk, db, idesc, (k == k0 && kk == 0) ? 0u : 1u);
-                                else mma_bf16(tmem + buf * BN, dA + 2 * kk, db, idesc, (k == k0 && kk == 0) ? 0u : 1u);
+                                const uint64_t da = dA + (BLOCK >> 4) * (kk / 4) + 2 * (kk % 4), db = dB + (BLOCK >> 4) * (kk / 4) + (BACK ? 128 : 2) * (kk % 4);
+                                if (PAIR) mma_bf16_pair(tmem + buf * BN, da, db, idesc, (k == k0 && kk == 0) ? 0u : 1u);
+                                else mma_bf16(tmem + buf * BN, da, db, idesc, (k == k0 && kk == 0) ? 0u : 1u);
                             }
                             if (PAIR) mma_commit_pair(empty_bar(ps.stage), 3);
                             else mma_commit(empty_bar(ps.stage));
@@ -483,7 +506,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
         const uint32_t mine = boxes + w * a.warp_bytes;
         const uint32_t lane_tmem = tmem + ((q * 32u) << 16);
         const int first = (int)half * (COLS / 2);              // of the tile's columns
-        const bool fetches = a.in_bytes != 0;
+        const bool fetches = a.in_bytes != 0 && part == 0;
         uint32_t n = 0, chunk = 0;                             // accumulators and chunks so far
         uint32_t fetched = 0;                                  // chunks whose operands have been asked for
         auto row_of = [&](const Walk& t) { return t.m * TM + (int)rank * 128 + (int)q * 32; };
@@ -510,7 +533,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
         };
         const uint32_t bias_at = bars + 512 + w * 512;
         const bool twice = a.twice != 0;
-        const bool by_hand = KIND != GATED && KIND != GATED_BACK && a.side[IN0].form != kNone && !a.side[IN0].tma;
+        const bool by_hand = KIND != GATED && KIND != GATED_BACK && a.side[IN0].form != kNone && !a.side[IN0].tma && part == 0;
         constexpr int OUT = F32 ? kF32 : kBf16, KEPT = IN8 ? kBytes : kBf16, FORM0 = KIND == GATED_BACK ? KEPT : OUT;
         const int form0 = a.side[OUT0].form, form1 = a.side[OUT1].form;
         const int in0 = a.side[IN0].form, in1 = a.side[IN1].form;
@@ -583,16 +606,64 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     release(buf);
                 }
                 if (!ok) break;
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) add_bias(first - block + 32 * i + 8 * g, sum[i][g]);
             } else {
                 if (!wait_warp<false>(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
                 tc_fence_after();
                 ++n;
             }
             const uint32_t acc = lane_tmem + buf * BN;
+            // a part's number of this lane's row: 16-byte pieces of a row swapped so that neighbouring rows fall on all banks
+            auto joint = [&](uint32_t base, uint32_t of, int c) {
+                return base + ((of - 1) * 128 + q * 32 + lane) * (BN * 4u) + (uint32_t)(((c >> 2) ^ (lane & 7)) << 4);
+            };
+            if (!PAIR && part > 0) {                           // the launch has one tile a cluster: this is all that it does
+                const uint32_t there = map_to_cta(join, 0);
+#pragma unroll
+                for (int i = 0; i < (TWO ? 2 : 1) * CHUNKS; ++i) {
+                    const int c = (TWO && i >= CHUNKS ? COLS - 32 * CHUNKS : 0) + first + 32 * i;
+                    uint32_t r[32];
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            r[2 * e] = __float_as_uint(sum[i][e >> 2][e & 3].x);
+                            r[2 * e + 1] = __float_as_uint(sum[i][e >> 2][e & 3].y);
+                        }
+                    } else {
+                        tmem_ld32(acc + c, r);
+                        tmem_ld_wait();
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) st_cluster_v4(joint(there, part, c + e), r[e], r[e + 1], r[e + 2], r[e + 3]);
+                }
+                if (!F32) release(buf);
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to_cta(join_bar, 0));
+                continue;
+            }
+            if (!PAIR && split > 1) {
+                if (w == 0 && lane == 0) mbar_arrive(join_bar);
+                if (!wait_warp<true>(join_bar, 0, abortp, a.wait_ns)) { ok = false; break; }
+            }
+            auto add_parts = [&](int c, F2 (&v)[4]) {          // to the eight columns from c on of the accumulator
+                if (PAIR) return;
+                for (uint32_t of = 1; of < split; ++of) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 o = lds16(joint(join, of, c + 4 * h));
+                        v[2 * h] = add2(v[2 * h], F2{__uint_as_float(o.x), __uint_as_float(o.y)});
+                        v[2 * h + 1] = add2(v[2 * h + 1], F2{__uint_as_float(o.z), __uint_as_float(o.w)});
+                    }
+                }
+            };
+            if constexpr (F32) {
+#pragma unroll
+                for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        add_parts(first + 32 * i + 8 * g, sum[i][g]);
+                        add_bias(first - block + 32 * i + 8 * g, sum[i][g]);
+                    }
+            }
             // the scales of what is kept in 8 bits: both warps of these rows look at all 128 columns of the block (F32: one
             // has them all, in its sums)
             float inv1 = 0.f, inv2 = 0.f;
@@ -677,7 +748,11 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     }
                     if (i == CHUNKS - 1) release(buf);
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) add_bias(first - block + 32 * i + 8 * g, v[g]);
+                    for (int g = 0; g < 4; ++g) {
+                        add_parts(first + 32 * i + 8 * g, v[g]);
+                        if constexpr (TWO) add_parts(COLS + first + 32 * i + 8 * g, x[g]);
+                        add_bias(first - block + 32 * i + 8 * g, v[g]);
+                    }
                 }
                 const uint32_t box_in0 = mine + a.side[IN0].box[b], box_in1 = mine + a.side[IN1].box[b];
                 const uint32_t box0 = mine + a.side[OUT0].box[b], box1 = mine + a.side[OUT1].box[b], box2 = mine + a.side[OUT2].box[b];
@@ -775,7 +850,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     // ---------------- teardown ----------------
     tc_fence_before();
     __syncthreads();
-    if (PAIR) cluster_sync_all();                              // neither CTA frees tensor memory or leaves while its peer still works
+    if (PAIR || split > 1) cluster_sync_all();                 // no CTA frees tensor memory or leaves while a peer still works
     if (warp == 1) {
         tc_fence_after();
         if (PAIR) tmem_dealloc_pair(tmem, 512);
@@ -786,10 +861,12 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
 
 // ---- few rows ---------------------------------------------------------------------------------------
 // Up to 16 tokens forward: the time is the weight's bytes from memory.  A block takes 16 rows of the weight (or eight of
-// either projection), its warps the blocks of 128 of K in turn; a lane loads 16 bytes of two of those rows and of a row of
+// either projection), its warps the blocks of 64 of K in turn; a lane loads 16 bytes of two of those rows and of a row of
 // each eight of x straight into the fragments of the warp's own matrix instruction (m16n8k16, the weight's rows as its M):
 // the order of K within 32 is the same for both and does not matter.  The warps' sums meet in shared memory, in a fixed order.
-constexpr int FEW_ROWS = 16, FEW_MAX_WARPS = 16, FEW_MAX_M = 16;
+// Blocks are small enough for four an SM, so that one wave of them covers the usual widths (with 16 warps and 74 registers a
+// thread one block fitted: 13.1 us against 7.8 for one token through 2048 -> 8192).
+constexpr int FEW_ROWS = 16, FEW_MAX_WARPS = 8, FEW_MAX_M = 16;
 struct FewArgs {
     int M, N, K, act;
     const __nv_bfloat16 *x, *w[2];
@@ -797,13 +874,12 @@ struct FewArgs {
     const float* bias;
     Side residual, out0, out1, out2;
 };
-__device__ __forceinline__ uint4 eight_of(const __nv_bfloat16* row, int k, int K) {      // zeros beyond K
-    if (k + 8 <= K) return *reinterpret_cast<const uint4*>(row + k);
+__device__ __noinline__ uint4 last_of(const __nv_bfloat16* row, int n) {                // fewer than eight, zeros behind
     uint32_t w[4] = {0u, 0u, 0u, 0u};
     const unsigned short* h = reinterpret_cast<const unsigned short*>(row);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (k + i < K) w[i >> 1] |= (uint32_t)h[k + i] << (16 * (i & 1));
+        if (i < n) w[i >> 1] |= (uint32_t)h[i] << (16 * (i & 1));
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -818,7 +894,7 @@ __device__ __forceinline__ void store_one(const Side& s, int64_t at, float v) {
     else static_cast<__nv_bfloat16*>(s.p)[at] = __float2bfloat16_rn(v);
 }
 template <int TILES, bool TWO>                                                      // TILES: of eight rows of x
-__global__ void __launch_bounds__(32 * FEW_MAX_WARPS) dense_few_kernel(const __grid_constant__ FewArgs a) {
+__global__ void __launch_bounds__(32 * FEW_MAX_WARPS, TILES == 1 ? 4 : 3) dense_few_kernel(const __grid_constant__ FewArgs a) {
     extern __shared__ float sums[];                                                 // [warps][TILES * 8][FEW_ROWS + 1]
     after_predecessor();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, g = lane >> 2, t = lane & 3;
@@ -832,31 +908,45 @@ __global__ void __launch_bounds__(32 * FEW_MAX_WARPS) dense_few_kernel(const __g
     for (int j = 0; j < TILES; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
-    const int blocks = (a.K + 127) / 128;
-    for (int kb = warp; kb < blocks; kb += warps) {
-        uint4 p[4], q[4], x[TILES][4];
+    const int whole = a.K / 64;                                                     // blocks that no row ends in
+#pragma unroll 2
+    for (int kb = warp; kb < whole; kb += warps) {
+        uint4 p[2], q[2], x[TILES][2];
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const int k = kb * 128 + h * 32 + t * 8;
-            p[h] = r0 && k < a.K ? eight_of(w0, k, a.K) : none;
-            q[h] = r1 && k < a.K ? eight_of(w1, k, a.K) : none;
-        }
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const int k = kb * 128 + h * 32 + t * 8;
+        for (int h = 0; h < 2; ++h) {
+            const int k = kb * 64 + h * 32 + t * 8;
+            p[h] = r0 ? *reinterpret_cast<const uint4*>(w0 + k) : none;
+            q[h] = r1 ? *reinterpret_cast<const uint4*>(w1 + k) : none;
 #pragma unroll
             for (int j = 0; j < TILES; ++j) {
                 const int m = j * 8 + g;
-                x[j][h] = m < a.M && k < a.K ? eight_of(a.x + (int64_t)m * a.x_stride, k, a.K) : none;
+                x[j][h] = m < a.M ? *reinterpret_cast<const uint4*>(a.x + (int64_t)m * a.x_stride + k) : none;
             }
         }
 #pragma unroll
-        for (int h = 0; h < 4; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < TILES; ++j) {
                 mma_16816(acc[j], p[h].x, q[h].x, p[h].y, q[h].y, x[j][h].x, x[j][h].y);
                 mma_16816(acc[j], p[h].z, q[h].z, p[h].w, q[h].w, x[j][h].z, x[j][h].w);
             }
+    }
+    if (whole * 64 < a.K && whole % warps == warp) {                                // the last one, by the warp whose turn it is
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+            const int k = whole * 64 + h * 32 + t * 8, n = a.K - k;
+            auto some = [&](const __nv_bfloat16* row, bool there) {
+                return !there || n <= 0 ? none : n >= 8 ? *reinterpret_cast<const uint4*>(row + k) : last_of(row + k, n);
+            };
+            const uint4 p = some(w0, r0), q = some(w1, r1);
+#pragma unroll
+            for (int j = 0; j < TILES; ++j) {
+                const int m = j * 8 + g;
+                const uint4 x = some(a.x + (int64_t)m * a.x_stride, m < a.M);
+                mma_16816(acc[j], p.x, q.x, p.y, q.y, x.x, x.y);
+                mma_16816(acc[j], p.z, q.z, p.w, q.w, x.z, x.w);
+            }
+        }
     }
     float* mine = sums + warp * (TILES * 8) * (FEW_ROWS + 1);
 #pragma unroll
@@ -915,11 +1005,13 @@ struct Product {
 };
 
 template <int KIND, bool PAIR, int BN, bool F32, bool IN8>
-int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
+int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st, int split = 1) {
     constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK;
     constexpr int COLS = TWO ? BN / 2 : BN, TM = PAIR ? 256 : 128, STAGE = dg_stage_bytes<PAIR, BN>();
     GemmArgs a;
-    a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K; a.kb = (int)((p.K + 63) / 64);
+    a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K;
+    constexpr int BLOCKS = dg_stage_blocks<PAIR, BN>();
+    a.kb = (int)((p.K + 64 * BLOCKS - 1) / (64 * BLOCKS));
     const int64_t tm = (p.M + TM - 1) / TM, tn = (p.N + COLS - 1) / COLS;
     if (tm * tn > 0x7fffffff) return ADLOCO_ERR_UNSUPPORTED;
     a.tiles_n = (int)tn; a.tiles = (int)(tm * tn);
@@ -972,8 +1064,14 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
         if (over[i] >= 0 && a.side[i].form != kNone && a.side[over[i]].form == a.side[i].form)
             for (int b = 0; b < 2; ++b) a.side[i].box[b] = a.side[over[i]].box[b];
     a.warp_bytes = (used + 1023u) & ~1023u;
-    const int64_t left = DG_SMEM - 1024 - DG_BAR_BYTES - (int64_t)DG_EPI * a.warp_bytes;
-    a.stages = (int)(left / STAGE < DG_MAX_STAGES ? left / STAGE : DG_MAX_STAGES);
+    int64_t extra = 0;
+    for (;; split /= 2) {                             // parts whose sums leave room for four stages
+        extra = DG_BAR_BYTES + (split - 1) * 128 * BN * 4;
+        const int64_t left = DG_SMEM - 1024 - extra - (int64_t)DG_EPI * a.warp_bytes;
+        a.stages = (int)(left / STAGE < DG_MAX_STAGES ? left / STAGE : DG_MAX_STAGES);
+        if (split == 1 || a.stages * BLOCKS >= 4) break;
+    }
+    a.split = split;
     if (a.stages < 2) return ADLOCO_ERR_UNSUPPORTED;
     auto* kernel = dense_tile_kernel<KIND, PAIR, BN, F32, IN8>;
     static std::atomic<bool> attr_set[64];            // the attribute is per device
@@ -981,9 +1079,9 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
         ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DG_SMEM));
         attr_set[ctx->device & 63].store(true);
     }
-    const size_t smem = (size_t)a.stages * STAGE + DG_EPI * (size_t)a.warp_bytes + DG_BAR_BYTES + 1024;
+    const size_t smem = (size_t)a.stages * STAGE + DG_EPI * (size_t)a.warp_bytes + (size_t)extra + 1024;
     const int most = PAIR ? ctx->sm_count / 2 : ctx->sm_count, workers = a.tiles < most ? a.tiles : most;
-    ADLOCO_CUDA_TRY(ctx, launch_early(kernel, dim3((PAIR ? 2 : 1) * workers), DG_THREADS, smem, st, PAIR ? 2 : 1, maps, a));
+    ADLOCO_CUDA_TRY(ctx, launch_early(kernel, dim3((PAIR ? 2 : split) * workers), DG_THREADS, smem, st, PAIR ? 2 : split, maps, a));
     ctx->launches++;
     return ADLOCO_OK;
 }
@@ -1010,8 +1108,29 @@ int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     const int64_t least = std::min(std::min(pair256, pair128), solo128);
     if constexpr (KIND == GATED) {
         if (bytes && clocks(128, 256, sms, a_rows * 128 + 32768, 4) < pair256) return launch_tiles<KIND, false, 256, F32, IN8>(ctx, p, st);
+        if (!bytes) {                                 // as below, with 64 columns of each projection
+            int64_t best = least;
+            int split = 1;
+            const int64_t tiles = ((p.M + 127) / 128) * ((p.N + 63) / 64);
+            for (int s = 2; pairs && s <= 2 && tiles * s <= sms && kb >= 4 * s; s *= 2) {
+                const int64_t t = (kb + s - 1) / s * ((a_rows * 128 + 16384) / 64) + 2048 + s * 512;
+                if (t < best) { best = t; split = s; }
+            }
+            if (split > 1) return launch_tiles<KIND, false, 128, F32, IN8>(ctx, p, st, split);
+        }
     } else {
-        if (!bytes && clocks(128, 64, sms, a_rows * 128 + 8192, 1) < least) return launch_tiles<KIND, false, 64, F32, IN8>(ctx, p, st);
+        if (!bytes) {
+            // tiles of 64 columns, and a part of K for each of two or four CTAs where a cluster of them finds room: the join
+            // takes as long as two stages a part
+            int64_t best = clocks(128, 64, sms, a_rows * 128 + 8192, 1);
+            int split = 1;
+            const int64_t tiles = ((p.M + 127) / 128) * ((p.N + 63) / 64);
+            for (int s = 2; pairs && s <= 4 && tiles * s <= sms && kb >= 8 * s; s *= 2) {
+                const int64_t t = (kb + s - 1) / s * ((a_rows * 128 + 8192) / 64) + 1024 + s * 1024;
+                if (t < best) { best = t; split = s; }
+            }
+            if (best < least) return launch_tiles<KIND, false, 64, F32, IN8>(ctx, p, st, split);
+        }
         if constexpr (KIND == LINEAR && F32) {
             if (bytes) return pair256 < clocks(128, 256, sms, a_rows * 128 + 32768, 4) ? launch_tiles<KIND, true, 256, F32, IN8>(ctx, p, st)
                                                                                       : launch_tiles<KIND, false, 256, F32, IN8>(ctx, p, st);
@@ -1030,9 +1149,12 @@ int launch_few(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     for (int i = 0; i < 2; ++i) { a.w[i] = static_cast<const __nv_bfloat16*>(p.b[i]); a.w_stride[i] = p.b_stride[i]; }
     a.bias = p.bias;
     a.residual = p.side[IN0]; a.out0 = p.side[OUT0]; a.out1 = p.side[OUT1]; a.out2 = p.side[OUT2];
-    const int each = TWO ? FEW_ROWS / 2 : FEW_ROWS, blocks = (int)((p.K + 127) / 128);
-    const int warps = blocks < FEW_MAX_WARPS ? blocks : FEW_MAX_WARPS, tiles = p.M <= 8 ? 1 : 2;
+    const int each = TWO ? FEW_ROWS / 2 : FEW_ROWS, blocks = (int)((p.K + 63) / 64);
+    const int tiles = p.M <= 8 ? 1 : 2;
     const dim3 grid((unsigned)((p.N + each - 1) / each));
+    // as many warps a block as leave room for all blocks at once (64 registers a thread: 32 warps an SM), where that is no fewer than two
+    const int an_sm = (int)((grid.x + ctx->sm_count - 1) / ctx->sm_count), fit = an_sm <= 16 ? 32 / an_sm : FEW_MAX_WARPS;
+    const int warps = std::min(std::min(blocks, fit), FEW_MAX_WARPS);
     const size_t smem = (size_t)warps * tiles * 8 * (FEW_ROWS + 1) * sizeof(float);
     const cudaError_t e = tiles == 1 ? launch_early(dense_few_kernel<1, TWO>, grid, 32 * warps, smem, st, 1, a)
                                      : launch_early(dense_few_kernel<2, TWO>, grid, 32 * warps, smem, st, 1, a);
