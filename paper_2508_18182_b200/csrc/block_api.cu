@@ -417,6 +417,10 @@ int adloco_token_logprobs(adloco_ctx* ctx, const adloco_token_logprobs_args* a, 
     if (a->top < 0 || a->top > a->V || (a->top > 0) != (a->top_values != nullptr) || (a->top > 0) != (a->top_ids != nullptr)) return ADLOCO_ERR_INVALID_ARG;
     if (a->logp && !a->targets) return ADLOCO_ERR_INVALID_ARG;
     if (!a->logp && !a->entropy && !a->lse && a->top == 0) return ADLOCO_ERR_INVALID_ARG;
+    const void* outs[] = {a->logp, a->entropy, a->lse, a->top_values, a->top_ids};
+    for (int i = 0; i < 5; ++i)
+        for (int j = 0; j < i; ++j)
+            if (outs[i] && (outs[i] == outs[j] || outs[i] == a->logits)) return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(a->logits, a->dtype) || !elem_aligned(a->targets, ADLOCO_F32) || !elem_aligned(a->logp, ADLOCO_F32) ||
         !elem_aligned(a->entropy, ADLOCO_F32) || !elem_aligned(a->lse, ADLOCO_F32) || !elem_aligned(a->top_values, ADLOCO_F32) ||
         !elem_aligned(a->top_ids, ADLOCO_F32))

@@ -87,7 +87,8 @@ __device__ __forceinline__ F2 value(Act<ADLOCO_ACT_RELU>, F2 z) { return F2{relu
 __device__ __forceinline__ F2 value(Act<ADLOCO_ACT_GELU>, F2 z) {
     F2 e;
     const F2 q = tail_of(z, e);
-    return F2{fmaf(-fabsf(z.x), q.x, fmaxf(z.x, 0.f)), fmaf(-fabsf(z.y), q.y, fmaxf(z.y, 0.f))};
+    // z where the tail is below all numbers; an infinity times its 0 would be none
+    return F2{fmaf(-fminf(fabsf(z.x), 1e30f), q.x, fmaxf(z.x, 0.f)), fmaf(-fminf(fabsf(z.y), 1e30f), q.y, fmaxf(z.y, 0.f))};
 }
 __device__ __forceinline__ F2 value(Act<ADLOCO_ACT_GELU_TANH>, F2 z) { return mul2(z, tanh_gate(z)); }
 __device__ __forceinline__ F2 value(Act<ADLOCO_ACT_SILU>, F2 z) { return mul2(z, logistic(z)); }

@@ -115,6 +115,8 @@ def test_logprobs(ctx):
     refused(ctx, bad, ctx.token_logprobs, l, t, v(), top_values=z(4, 3, dtype=F32), top_ids=z(4, 3, dtype=torch.int64))
     refused(ctx, bad, ctx.token_logprobs, l, t, v(), top_values=z(4, 11, dtype=F32), top_ids=z(4, 11, dtype=torch.int32))
     refused(ctx, types, ctx.token_logprobs, z(4, 100), t, v(), top_values=z(4, 65, dtype=F32), top_ids=z(4, 65, dtype=torch.int32))
+    one = v()
+    refused(ctx, bad, ctx.token_logprobs, l, t, one, lse=one)                 # two outputs in one place
     refused(ctx, bad, ctx.token_logprobs_backward, l, t, v(), v(), z(4, 10, dtype=F32))
     refused(ctx, bad, ctx.token_logprobs_backward, l, t, v(), v(), z(4, 9))
     refused(ctx, bad, ctx.token_logprobs_backward, l, t, v(), v(), z(4, 10), entropy=v())
