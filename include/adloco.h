@@ -27,7 +27,8 @@
  *     several streams at once -- the layers of one micro-batch only add into
  *     n and into their own S, and alternating them on two streams overlaps
  *     one kernel's tail with the next one's start.  So may the operators between the
- *     linear layers (adloco_add_rmsnorm to adloco_blockscale_matmul).
+ *     linear layers (adloco_add_rmsnorm to adloco_blockscale_dequantize), of the linear layers in bf16
+ *     and the loss (adloco_linear to adloco_token_logprobs_backward).
  *   - Sizes are int64_t element counts; all byte offsets are 64-bit inside.
  *   - There is no CPU fallback: without a usable CUDA device the calls fail
  *     with ADLOCO_ERR_CUDA.
