@@ -128,35 +128,56 @@ struct LogprobArgs {
     int32_t* top_ids;
 };
 
+template <bool V> struct Is { static constexpr bool value = V; };
 template <int TPR>
 __device__ __forceinline__ void row_sync() {
     if (TPR == 32) __syncwarp();
     else __syncthreads();
 }
 
+// The extremes of U pieces.  A NaN counts as neither; bf16 takes two numbers an instruction.
+template <int U>
+__device__ __forceinline__ void extremes(const uint4 (&w)[U], float& low, float& high, float) {
+    high = -INFINITY;
+    low = -INFINITY;                                            // not looked for: as dear as what knowing it saves
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        high = fmaxf(high, fmaxf(fmaxf(__uint_as_float(w[u].x), __uint_as_float(w[u].y)), fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w))));
+}
+template <int U>
+__device__ __forceinline__ void extremes(const uint4 (&w)[U], float& low, float& high, __nv_bfloat16) {
+    const __nv_bfloat162* v = reinterpret_cast<const __nv_bfloat162*>(&w[0]);
+    __nv_bfloat162 h = v[0], l = v[0];
+#pragma unroll
+    for (int i = 1; i < 4 * U; ++i) { h = __hmax2(h, v[i]); l = __hmin2(l, v[i]); }
+    high = fmaxf(__low2float(h), __high2float(h));
+    low = fminf(__low2float(l), __high2float(l));
+}
 template <typename T, bool ENTROPY, int U>
 __device__ __forceinline__ void add_pieces(const uint4 (&w)[U], Sums& a, float& top) {
     constexpr int N = Piece<T>::N;
-    float v[U][N];
-    float m = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        unpack(w[u], v[u]);
-#pragma unroll
-        for (int i = 0; i < N; i += 2) m = fmaxf(m, fmaxf(v[u][i], v[u][i + 1]));
-    }
+    float low, m;
+    extremes(w, low, m, T());
     top = fmaxf(top, m);
     if (m > a.m) a = brought_to(a, m);
     const F2 minus = both(-a.m);
     F2 s = both(0.f), e = both(0.f);
+    auto add = [&](auto some_infinite) {                        // a logit of -Inf adds 0, which its distance would make a NaN of
+        constexpr bool CLAMP = decltype(some_infinite)::value;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            float v[N];
+            unpack(w[u], v);
 #pragma unroll
-        for (int i = 0; i < N; i += 2) {
-            const F2 d = add2(F2{v[u][i], v[u][i + 1]}, minus), x = exp2_fast(mul2(d, both(kLog2e)));
-            s = add2(s, x);
-            if (ENTROPY) e = fma2(x, F2{max_or_nan(d.x, -1e4f), max_or_nan(d.y, -1e4f)}, e);
+            for (int i = 0; i < N; i += 2) {
+                const F2 d = add2(F2{v[i], v[i + 1]}, minus), x = exp2_fast(mul2(d, both(kLog2e)));
+                s = add2(s, x);
+                if (ENTROPY) e = fma2(x, CLAMP ? F2{max_or_nan(d.x, -1e4f), max_or_nan(d.y, -1e4f)} : d, e);
+            }
         }
+    };
+    if (sizeof(T) == 2 && ENTROPY && low > -INFINITY && m - low < 1e30f) add(Is<false>{});
+    else add(Is<true>{});
     a.s += s.x + s.y;
     if (ENTROPY) a.e += e.x + e.y;
 }
