@@ -658,7 +658,8 @@ int adloco_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_back
  *            contiguous, both or neither, 0 <= top <= 64, top <= V
  * A row whose target is outside [0, V) has logp 0.  Logits of -Inf (tokens ruled out) have probability 0 and log-probability
  * -Inf; a row of nothing else has lse, logp and top_values -Inf and entropy 0.  A row with a NaN or +Inf has NaN in all of them,
- * and ids of some tokens of the vocabulary.  fp32 throughout, one pass over the logits (the choice of the top tokens reads them again, from L2). */
+ * and ids of some tokens of the vocabulary.  fp32 throughout, one pass over the logits (choosing the best tokens reads a few parts of a row again, a row of many equal logits once for
+ * each of them). */
 typedef struct {
     int64_t rows, V;
     const void* logits;

@@ -279,7 +279,7 @@ __device__ __forceinline__ float larger(float m, float v) {
 // ---- the tile kernel ------------------------------------------------------------------------------
 // Persistent, 320 threads: warp 0 brings tiles by TMA, warp 1 issues the MMAs, warps 2-9 are the epilogue.  PAIR: 256 x BN
 // tiles shared by the two CTAs of a cluster (cta_group::2): CTA r holds rows 128 r .. + 127 of the tile in its tensor memory
-// and loads those rows of A and half of B's; otherwise 128 x BN tiles of one CTA.  A stage is 64 of K.  Two accumulators
+// and loads those rows of A and half of B's; otherwise 128 x BN tiles of one CTA.  A stage is 64 of K, 128 in small tiles.  Two accumulators
 // take turns, so that a tile's epilogue runs beside the next tile's MMAs.  B is a weight [N, K] forward, its rows along the
 // tensor cores' K; backward the same weight is read as it lies, its rows along the contraction (MN-major).
 // GATED: the tile's columns are BN / 2 of each projection (in a pair, CTA r brings projection r), so a thread of the epilogue
@@ -289,7 +289,11 @@ __device__ __forceinline__ float larger(float m, float v) {
 // SPLIT K: where few tiles leave most SMs idle, up to four CTAs of a cluster take a part of K each.  All but the first write
 // their sums into the first one's shared memory, which adds them up in their order and goes on alone.
 // The epilogue's eight warps each own 32 rows and half the columns, in chunks of 32: the operands of the next chunk arrive by
-// TMA while this one is computed, the results leave by TMA.
+// TMA while this one is computed, the results leave by TMA.  IN8: what the forward pass kept is in 8 bits.
+// What bounds it: at long K the tensor pipe and the power cap (8192 x 4096 -> 4096: 169 us, 1.63 PFLOP/s); at K = 768 a tile's MMAs take
+// 6.1 thousand clocks and its operands as many of L2's, and the epilogue's matrices go through the same L2 and copy engine
+// beside them: 32768 x 768 -> 2048 takes 75 us with one bf16 output, 103 with gelu and z kept, 143 on the way back through the gate with
+// five matrices (4.7 TB/s).  Sixteen epilogue warps, operands and results without TMA, and prefetches into L2 gained nothing or lost.
 constexpr int DG_THREADS = 320, DG_EPI = 8;
 constexpr int DG_A_BYTES = 128 * 128;
 constexpr int DG_MAX_STAGES = 8;

@@ -82,7 +82,7 @@ struct Run {
 constexpr int kMaxTop = 64;
 constexpr int kTopThreads = 256, kClusterThreads = 512;
 constexpr int kCluster = 8;
-// 64 registers a thread: more blocks with fewer spill (8192 x 50257 bf16: 170 us; with 5 and 6 blocks an SM 235 and 312)
+// 64 registers a thread: more blocks with fewer spill (8192 x 50257 bf16: 170 us, with 5 and 6 blocks an SM 235 and 312)
 template <int TPR, bool CLUSTER> constexpr int kBlocks = TPR == 32 ? 8 : CLUSTER ? 2 : 4;
 template <int TPR> __host__ __device__ constexpr int groups_of() { return TPR < 128 ? TPR : 128; }
 constexpr int kCandidates = 512;                                // of a row
