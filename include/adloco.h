@@ -540,8 +540,8 @@ int adloco_blockscale_dequantize(adloco_ctx* ctx, adloco_dtype dtype, int64_t ro
  * return.  Operands of a product (x, w, dy) are bf16 with 16-byte aligned rows (base, and a pitch that is a multiple of 8);
  * other tensors may have any pitch, 16-byte aligned rows being the fast ones.  Products are exact, sums fp32: the tensor
  * cores' own in bf16 outputs (they cut off low bits: a relative error of 1e-6 after 1000 terms), with every 512 terms added
- * up to nearest where an output is F32; every output is rounded once.  An output may be the same memory as an elementwise operand
- * (residual, z, gate, up) of the same type and pitch; no other overlap is allowed.
+ * up to nearest where an output is F32 or what is kept goes to 8 bits; every output is rounded once.  An output may be the same
+ * memory as an elementwise operand (residual, z, gate, up) of the same type and pitch; no other overlap is allowed.
  * None of them uses the ctx workspace. */
 typedef enum {
     ADLOCO_ACT_NONE = 0,

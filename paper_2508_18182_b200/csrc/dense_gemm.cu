@@ -21,6 +21,9 @@ namespace {
 
 enum Kind { LINEAR, LINEAR_BACK, GATED, GATED_BACK };
 enum Form { kNone, kBf16, kF32, kBytes };
+// What the epilogue takes for a product: the tensor cores' sum as it is, or the parts of K added up in registers, for outputs
+// in fp32 or ones whose sums go to 8 bits.
+enum Sum { kPlain, kSummed, kSummedF32 };
 enum { IN0, IN1, OUT0, OUT1, OUT2, SIDES };
 
 // An elementwise operand or output of the epilogue.  Its box: 32 rows x 32 columns in shared memory, one for the even
@@ -284,8 +287,11 @@ __device__ __forceinline__ float larger(float m, float v) {
 // tensor cores' K; backward the same weight is read as it lies, its rows along the contraction (MN-major).
 // GATED: the tile's columns are BN / 2 of each projection (in a pair, CTA r brings projection r), so a thread of the epilogue
 // has both numbers of an output.
-// F32 (outputs): the tensor cores cut off each sum's low bits (relative error 1e-6 after 1000 terms, growing with their number); the
-// sum of every 512 of K is added up in registers instead, rounded to nearest.
+// SUMMED: the tensor cores cut off each sum's low bits (relative error 1e-6 after 1000 terms, growing with their number); the
+// sum of every 512 of K is added up in registers instead, rounded to nearest: for fp32 outputs (F32), and where sums go to 8 bits,
+// whose steps are so wide (2^-4) that each number on the other side of a border shows (4096 x 2048 -> 2 x 5632, both kept, and the way
+// back: 7.0e-4 of the norm away from the fp32 form with the accumulator as it is, 3.4e-4 so, 2.4e-4 with a sum of every 256; 131, 132
+// and 139 us forward).
 // SPLIT K: where few tiles leave most SMs idle, up to four CTAs of a cluster take a part of K each.  All but the first write
 // their sums into the first one's shared memory, which adds them up in their order and goes on alone.
 // The epilogue's eight warps each own 32 rows and half the columns, in chunks of 32: the operands of the next chunk arrive by
@@ -297,7 +303,7 @@ __device__ __forceinline__ float larger(float m, float v) {
 constexpr int DG_THREADS = 320, DG_EPI = 8;
 constexpr int DG_A_BYTES = 128 * 128;
 constexpr int DG_MAX_STAGES = 8;
-constexpr int DG_SEGMENT = 8;                              // blocks of K in one sum of an F32 tile
+constexpr int DG_SEGMENT = 8;                              // blocks of K in one sum of a SUMMED tile
 constexpr int DG_BAR_BYTES = 512 + DG_EPI * 512;            // and 128 columns of the bias for each warp of the epilogue
 constexpr int DG_SMEM = 232448 - 256;                      // what a block can have, less the kernel's own few words
 template <bool PAIR, int BN>
@@ -328,14 +334,15 @@ struct Walk {
     }
 };
 
-template <int KIND, bool PAIR, int BN, bool F32, bool IN8>
+template <int KIND, bool PAIR, int BN, int SUM, bool IN8>
 __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmArgs a) {
     constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK, FORWARD = !BACK;
+    constexpr bool SUMMED = SUM != kPlain, F32 = SUM == kSummedF32;
     constexpr int COLS = TWO ? BN / 2 : BN;                // output columns of a tile
     constexpr int TM = PAIR ? 256 : 128;
     constexpr int CHUNKS = COLS / 64;                      // of an epilogue warp
     constexpr int STAGE = dg_stage_bytes<PAIR, BN>(), BLOCK = dg_block_bytes<PAIR, BN>(), BLOCKS = dg_stage_blocks<PAIR, BN>();
-    constexpr int SEGMENT = DG_SEGMENT / BLOCKS;           // stages in one sum of an F32 tile
+    constexpr int SEGMENT = DG_SEGMENT / BLOCKS;           // stages in one sum of a SUMMED tile
     constexpr int B_ROWS = PAIR ? BN / 2 : BN;             // of the weight (or of its columns, backward) in a CTA's stage
     static_assert(CHUNKS >= 1 && (!BACK || B_ROWS % 64 == 0), "a chunk is 32 columns, a box of the weight's columns 64");
 
@@ -349,8 +356,9 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     auto acc_empty = [&](uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 2 + s); };
     auto in_bar = [&](uint32_t w, uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * w + s); };
     const uint32_t drain_bar = bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * DG_EPI), join_bar = drain_bar + 8u;
-    const uint32_t join = bars + DG_BAR_BYTES;                 // the other parts' sums
-    static_assert(8 * (2 * DG_MAX_STAGES + 6 + 2 * DG_EPI) <= 512, "barriers");
+    auto swap_bar = [&](uint32_t w) { return bars + 8u * (2 * DG_MAX_STAGES + 6 + 2 * DG_EPI + w); };
+    const uint32_t join = bars + DG_BAR_BYTES;                 // the other parts' sums, or the maxima that warps tell one another
+    static_assert(8 * (2 * DG_MAX_STAGES + 6 + 3 * DG_EPI) <= 512, "barriers");
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
@@ -364,8 +372,10 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
         abort_flag = 0;
         for (uint32_t s = 0; s < stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
         for (uint32_t s = 0; s < 2; ++s) { mbar_init(acc_full(s), 1); mbar_init(acc_empty(s), (PAIR ? 2 : 1) * DG_EPI); }
-        for (uint32_t w = 0; w < DG_EPI; ++w)
+        for (uint32_t w = 0; w < DG_EPI; ++w) {
             for (uint32_t s = 0; s < 2; ++s) mbar_init(in_bar(w, s), 1);
+            mbar_init(swap_bar(w), 1);
+        }
         mbar_init(drain_bar, 1);
         mbar_init(join_bar, (split - 1) * DG_EPI + 1);
         fence_barrier_init();
@@ -386,7 +396,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     after_predecessor();
     const uint32_t tmem = tmem_slot;
     volatile int* abortp = &abort_flag;
-    const int segments = F32 ? (k_end - k_first + SEGMENT - 1) / SEGMENT : 1;
+    const int segments = SUMMED ? (k_end - k_first + SEGMENT - 1) / SEGMENT : 1;
 
     if (warp == 0) {
         // ---------------- TMA producer, one per CTA ----------------
@@ -463,7 +473,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
             for (; ok && walk.more(); walk.next()) {
                 for (int k0 = k_first; ok && k0 < k_end; ++n) {
                     const uint32_t buf = n & 1u;
-                    const int k1 = F32 ? min(k_end, k0 + SEGMENT) : k_end;
+                    const int k1 = SUMMED ? min(k_end, k0 + SEGMENT) : k_end;
                     if (!wait_warp<PAIR>(acc_empty(buf), ((n >> 1) & 1u) ^ 1u, abortp, a.wait_ns)) { ok = false; break; }
                     for (int k = k0; k < k1; ++k) {
                         if (!wait_warp<false>(full_bar(ps.stage), ps.phase, abortp, a.wait_ns)) { ok = false; break; }
@@ -514,6 +524,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
         const bool fetches = a.in_bytes != 0 && part == 0;
         uint32_t n = 0, chunk = 0;                             // accumulators and chunks so far
         uint32_t fetched = 0;                                  // chunks whose operands have been asked for
+        uint32_t swaps = 0;                                    // maxima told to the other warp of these rows
         auto row_of = [&](const Walk& t) { return t.m * TM + (int)rank * 128 + (int)q * 32; };
         auto col_of = [&](const Walk& t, int i) { return t.n * COLS + first + 32 * i; };
         auto stored = [&]() {                                  // this warp's stores so far have read their boxes
@@ -588,13 +599,16 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     v[2 * h + 1] = add2(v[2 * h + 1], F2{__uint_as_float(w.z), __uint_as_float(w.w)});
                 }
             };
-            F2 sum[F32 ? CHUNKS : 1][4][4];
+            F2 sum[SUMMED ? CHUNKS : 1][4][4], sum2[SUMMED ? CHUNKS : 1][TWO ? 4 : 1][4];      // TWO: sum2 of the other projection
             uint32_t buf = n & 1u;
-            if (F32) {
+            if constexpr (SUMMED) {
 #pragma unroll
                 for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sum[i][e >> 2][e & 3] = both(0.f);
+                    for (int e = 0; e < 16; ++e) {
+                        sum[i][e >> 2][e & 3] = both(0.f);
+                        if constexpr (TWO) sum2[i][e >> 2][e & 3] = both(0.f);
+                    }
                 for (int s = 0; s < segments; ++s, ++n) {
                     buf = n & 1u;
                     if (!wait_warp<false>(acc_full(buf), (n >> 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
@@ -607,6 +621,13 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
 #pragma unroll
                         for (int e = 0; e < 16; ++e)
                             sum[i][e >> 2][e & 3] = add2(sum[i][e >> 2][e & 3], F2{__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])});
+                        if constexpr (TWO) {
+                            tmem_ld32(lane_tmem + buf * BN + COLS + first + 32 * i, r);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                sum2[i][e >> 2][e & 3] = add2(sum2[i][e >> 2][e & 3], F2{__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])});
+                        }
                     }
                     release(buf);
                 }
@@ -627,7 +648,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 for (int i = 0; i < (TWO ? 2 : 1) * CHUNKS; ++i) {
                     const int c = (TWO && i >= CHUNKS ? COLS - 32 * CHUNKS : 0) + first + 32 * i;
                     uint32_t r[32];
-                    if constexpr (F32) {
+                    if constexpr (SUMMED) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             r[2 * e] = __float_as_uint(sum[i][e >> 2][e & 3].x);
@@ -640,7 +661,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) st_cluster_v4(joint(there, part, c + e), r[e], r[e + 1], r[e + 2], r[e + 3]);
                 }
-                if (!F32) release(buf);
+                if (!SUMMED) release(buf);
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(join_bar, 0));
                 continue;
@@ -660,7 +681,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     }
                 }
             };
-            if constexpr (F32) {
+            if constexpr (SUMMED) {
 #pragma unroll
                 for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
@@ -669,37 +690,31 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                         add_bias(first - block + 32 * i + 8 * g, sum[i][g]);
                     }
             }
-            // the scales of what is kept in 8 bits: both warps of these rows look at all 128 columns of the block (F32: one
-            // has them all, in its sums)
+            // the scales of what is kept in 8 bits.  A warp whose sums are half of the block's 128 columns tells the other warp of
+            // these rows their maxima: in one of two places in turn, since neither goes on to the next tile but one before the
+            // other has read this one's.
             float inv1 = 0.f, inv2 = 0.f;
-            if (FORWARD && form1 == kBytes && valid > 0) {
+            if (FORWARD && form1 == kBytes && row0 < a.M) {
                 float m1 = 0.f, m2 = 0.f;
-                if (F32) {
+                if constexpr (SUMMED) {
 #pragma unroll
                     for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) m1 = larger(larger(m1, sum[i][e >> 2][e & 3].x), sum[i][e >> 2][e & 3].y);
-                } else {
-#pragma unroll 1
-                    for (int c = 0; c < AROUND; c += 32) {
-                        uint32_t r[32];
-                        tmem_ld32(acc + block + c, r);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            F2 v[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) v[e] = F2{__uint_as_float(r[8 * g + 2 * e]), __uint_as_float(r[8 * g + 2 * e + 1])};
-                            add_bias(c + 8 * g, v);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) m1 = larger(larger(m1, v[e].x), v[e].y);
+                        for (int e = 0; e < 16; ++e) {
+                            m1 = larger(larger(m1, sum[i][e >> 2][e & 3].x), sum[i][e >> 2][e & 3].y);
+                            if constexpr (TWO) m2 = larger(larger(m2, sum2[i][e >> 2][e & 3].x), sum2[i][e >> 2][e & 3].y);
                         }
-                        if (TWO) {
-                            tmem_ld32(acc + COLS + block + c, r);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) m2 = larger(m2, __uint_as_float(r[e]));
-                        }
+                    if constexpr (CHUNKS < 4) {
+                        const uint32_t place = (swaps & 1u) * 256u + (uint32_t)lane * 8u;
+                        asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(join + w * 512u + place), "f"(m1), "f"(m2) : "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(swap_bar(w ^ 4u));
+                        if (!wait_warp<false>(swap_bar(w), swaps & 1u, abortp, a.wait_ns)) { ok = false; break; }
+                        ++swaps;
+                        float o1, o2;
+                        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(o1), "=f"(o2) : "r"(join + (w ^ 4u) * 512u + place) : "memory");
+                        m1 = larger(m1, o1);
+                        m2 = larger(m2, o2);
                     }
                 }
                 const uint32_t s1 = scale_byte(__float_as_uint(m1)), s2 = scale_byte(__float_as_uint(m2));
@@ -718,13 +733,12 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 scale1 = scale_of(a.side[IN1].scale[(int64_t)row * a.side[IN1].scale_pitch + at]);
             }
 
-            auto one_chunk = [&](int i, F2 (&v)[4][4]) -> bool {
+            auto one_chunk = [&](int i, F2 (&v)[4][4], F2 (&x)[TWO ? 4 : 1][4]) -> bool {
                 const int col = col_of(walk, i);
                 const uint32_t b = chunk & 1u;
-                F2 x[TWO ? 4 : 1][4];
-                uint32_t r[F32 ? 1 : 32], u[TWO ? 32 : 1];
-                if constexpr (!F32) tmem_ld32(acc + first + 32 * i, r);
-                if constexpr (TWO) tmem_ld32(acc + COLS + first + 32 * i, u);
+                uint32_t r[SUMMED ? 1 : 32], u[TWO && !SUMMED ? 32 : 1];
+                if constexpr (!SUMMED) tmem_ld32(acc + first + 32 * i, r);
+                if constexpr (TWO && !SUMMED) tmem_ld32(acc + COLS + first + 32 * i, u);
                 if (fetches) {
                     stored();                                  // the next chunk's boxes are free
                     const uint32_t now = chunk;
@@ -743,7 +757,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     }
                     __syncwarp();
                 }
-                if constexpr (!F32) {
+                if constexpr (!SUMMED) {
                     tmem_ld_wait();
 #pragma unroll
                     for (int e = 0; e < 16; ++e) v[e >> 2][e & 3] = F2{__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])};
@@ -834,13 +848,13 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 ++chunk;
                 return true;
             };
-            if constexpr (F32) {
+            if constexpr (SUMMED) {
 #pragma unroll
                 for (int i = 0; i < CHUNKS; ++i)
-                    if (ok && i < valid) ok = one_chunk(i, sum[i]);
+                    if (ok && i < valid) ok = one_chunk(i, sum[i], sum2[i]);
             } else {
 #pragma unroll 1
-                for (int i = 0; ok && i < valid; ++i) ok = one_chunk(i, sum[0]);
+                for (int i = 0; ok && i < valid; ++i) ok = one_chunk(i, sum[0], sum2[0]);
                 if (ok && valid < CHUNKS) release(buf);
             }
         }
@@ -1009,7 +1023,7 @@ struct Product {
     Side side[SIDES];
 };
 
-template <int KIND, bool PAIR, int BN, bool F32, bool IN8>
+template <int KIND, bool PAIR, int BN, int SUM, bool IN8>
 int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st, int split = 1) {
     constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK;
     constexpr int COLS = TWO ? BN / 2 : BN, TM = PAIR ? 256 : 128, STAGE = dg_stage_bytes<PAIR, BN>();
@@ -1071,14 +1085,14 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st, int split =
     a.warp_bytes = (used + 1023u) & ~1023u;
     int64_t extra = 0;
     for (;; split /= 2) {                             // parts whose sums leave room for four stages
-        extra = DG_BAR_BYTES + (split - 1) * 128 * BN * 4;
+        extra = DG_BAR_BYTES + (a.side[OUT1].form == kBytes ? DG_EPI * 512 : (split - 1) * 128 * BN * 4);
         const int64_t left = DG_SMEM - 1024 - extra - (int64_t)DG_EPI * a.warp_bytes;
         a.stages = (int)(left / STAGE < DG_MAX_STAGES ? left / STAGE : DG_MAX_STAGES);
         if (split == 1 || a.stages * BLOCKS >= 4) break;
     }
     a.split = split;
     if (a.stages < 2) return ADLOCO_ERR_UNSUPPORTED;
-    auto* kernel = dense_tile_kernel<KIND, PAIR, BN, F32, IN8>;
+    auto* kernel = dense_tile_kernel<KIND, PAIR, BN, SUM, IN8>;
     static std::atomic<bool> attr_set[64];            // the attribute is per device
     if (!attr_set[ctx->device & 63].load()) {
         ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DG_SMEM));
@@ -1095,11 +1109,10 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st, int split =
 // deliver its operands, 64 bytes a clock: 512 clocks for a pair's 256 x 256 (as long as its MMAs) and for one CTA's 128 x 128,
 // 384 for a pair's 256 x 128 and one CTA's 128 x 64, less where A has fewer rows; a tile's epilogue as much as four (two, one) stages
 // that nothing hides when there is one round.
-template <int KIND, bool F32, bool IN8 = false>
+template <int KIND, int SUM, bool IN8 = false>
 int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     constexpr int SHARE = KIND == GATED ? 2 : 1;      // of a tile's columns a projection's are
-    bool bytes = false;                               // 8-bit outputs: a block of 128 columns in one tile (F32: in one warp)
-    for (int i = OUT0; i < SIDES; ++i) bytes = bytes || p.side[i].form == kBytes;
+    const bool bytes = p.side[OUT1].form == kBytes;   // 8-bit outputs: a block of 128 columns in one tile
     const bool pairs = cta_pairs_possible(ctx);
     const int64_t kb = (p.K + 63) / 64, a_rows = p.M < 128 ? p.M : 128;
     auto clocks = [&](int64_t tile_m, int64_t tile_n, int64_t workers, int64_t bytes_a_stage, int64_t epilogue) {
@@ -1107,13 +1120,17 @@ int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
         return rounds * kb * (bytes_a_stage / 64) + epilogue * 512 * (rounds > 1 ? 1 : 2);
     };
     const int64_t never = int64_t(1) << 62, sms = ctx->sm_count;
-    const int64_t pair256 = pairs ? clocks(256, 256, sms / 2, a_rows * 128 + 16384, 4) : never;
-    const int64_t pair128 = pairs && !(bytes && (SHARE == 2 || F32)) ? clocks(256, 128, sms / 2, a_rows * 128 + 8192, 2) : never;
+    // (z in 8 bits beside a bf16 output: the sums of 128 columns spill beside all else in registers: 32768 x 768 -> 2048 131 us,
+    // 117 with tiles of 128 columns, whose warps have 64 each)
+    const int64_t pair256 = pairs && !(KIND == LINEAR && SUM == kSummed) ? clocks(256, 256, sms / 2, a_rows * 128 + 16384, 4) : never;
+    const int64_t pair128 = pairs && !(bytes && SHARE == 2) ? clocks(256, 128, sms / 2, a_rows * 128 + 8192, 2) : never;
     const int64_t solo128 = bytes && SHARE == 2 ? never : clocks(128, 128, sms, a_rows * 128 + 16384, 2);
     const int64_t least = std::min(std::min(pair256, pair128), solo128);
-    if constexpr (KIND == GATED) {
-        if (bytes && clocks(128, 256, sms, a_rows * 128 + 32768, 4) < pair256) return launch_tiles<KIND, false, 256, F32, IN8>(ctx, p, st);
-        if (!bytes) {                                 // as below, with 64 columns of each projection
+    if constexpr (KIND == GATED && SUM == kSummed) {  // 128 columns of each projection in any case
+        return clocks(128, 256, sms, a_rows * 128 + 32768, 4) < pair256 ? launch_tiles<KIND, false, 256, SUM, IN8>(ctx, p, st)
+                                                                        : launch_tiles<KIND, true, 256, SUM, IN8>(ctx, p, st);
+    } else {
+        if constexpr (KIND == GATED) {                // as below, with 64 columns of each projection
             int64_t best = least;
             int split = 1;
             const int64_t tiles = ((p.M + 127) / 128) * ((p.N + 63) / 64);
@@ -1121,29 +1138,26 @@ int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
                 const int64_t t = (kb + s - 1) / s * ((a_rows * 128 + 16384) / 64) + 2048 + s * 512;
                 if (t < best) { best = t; split = s; }
             }
-            if (split > 1) return launch_tiles<KIND, false, 128, F32, IN8>(ctx, p, st, split);
-        }
-    } else {
-        if (!bytes) {
-            // tiles of 64 columns, and a part of K for each of two or four CTAs where a cluster of them finds room: the join
-            // takes as long as two stages a part
-            int64_t best = clocks(128, 64, sms, a_rows * 128 + 8192, 1);
-            int split = 1;
-            const int64_t tiles = ((p.M + 127) / 128) * ((p.N + 63) / 64);
-            for (int s = 2; pairs && s <= 4 && tiles * s <= sms && kb >= 8 * s; s *= 2) {
-                const int64_t t = (kb + s - 1) / s * ((a_rows * 128 + 8192) / 64) + 1024 + s * 1024;
-                if (t < best) { best = t; split = s; }
+            if (split > 1) return launch_tiles<KIND, false, 128, SUM, IN8>(ctx, p, st, split);
+        } else if constexpr (SUM != kSummed) {
+            if (!bytes) {
+                // tiles of 64 columns, and a part of K for each of two or four CTAs where a cluster of them finds room: the join
+                // takes as long as two stages a part
+                int64_t best = clocks(128, 64, sms, a_rows * 128 + 8192, 1);
+                int split = 1;
+                const int64_t tiles = ((p.M + 127) / 128) * ((p.N + 63) / 64);
+                for (int s = 2; pairs && s <= 4 && tiles * s <= sms && kb >= 8 * s; s *= 2) {
+                    const int64_t t = (kb + s - 1) / s * ((a_rows * 128 + 8192) / 64) + 1024 + s * 1024;
+                    if (t < best) { best = t; split = s; }
+                }
+                if (best < least) return launch_tiles<KIND, false, 64, SUM, IN8>(ctx, p, st, split);
             }
-            if (best < least) return launch_tiles<KIND, false, 64, F32, IN8>(ctx, p, st, split);
         }
-        if constexpr (KIND == LINEAR && F32) {
-            if (bytes) return pair256 < clocks(128, 256, sms, a_rows * 128 + 32768, 4) ? launch_tiles<KIND, true, 256, F32, IN8>(ctx, p, st)
-                                                                                      : launch_tiles<KIND, false, 256, F32, IN8>(ctx, p, st);
-        }
+        if constexpr (SUM != kSummed)
+            if (least == pair256) return launch_tiles<KIND, true, 256, SUM, IN8>(ctx, p, st);
+        if (least == pair128) return launch_tiles<KIND, true, 128, SUM, IN8>(ctx, p, st);
+        return launch_tiles<KIND, false, 128, SUM, IN8>(ctx, p, st);
     }
-    if (least == pair256) return launch_tiles<KIND, true, 256, F32, IN8>(ctx, p, st);
-    if (least == pair128) return launch_tiles<KIND, true, 128, F32, IN8>(ctx, p, st);
-    return launch_tiles<KIND, false, 128, F32, IN8>(ctx, p, st);
 }
 
 template <bool TWO>
@@ -1177,7 +1191,8 @@ int launch_linear(adloco_ctx* ctx, const adloco_linear_args& c, cudaStream_t st)
     p.side[OUT0] = side_of(c.y, c.y_stride, form);
     p.side[OUT1] = kept_side(c.z);
     if (c.M <= FEW_MAX_M && p.side[OUT1].form != kBytes) return launch_few<false>(ctx, p, st);
-    return form == kF32 ? choose_tiles<LINEAR, true>(ctx, p, st) : choose_tiles<LINEAR, false>(ctx, p, st);
+    if (form == kF32) return choose_tiles<LINEAR, kSummedF32>(ctx, p, st);
+    return p.side[OUT1].form == kBytes ? choose_tiles<LINEAR, kSummed>(ctx, p, st) : choose_tiles<LINEAR, kPlain>(ctx, p, st);
 }
 
 int launch_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args& c, cudaStream_t st) {
@@ -1187,8 +1202,8 @@ int launch_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args& c
     p.side[IN1] = kept_side(c.z);
     p.side[OUT0] = side_of(c.dx, c.dx_stride, form);
     p.side[OUT1] = side_of(c.a, c.a_stride, kBf16);
-    if (c.z.scale) return form == kF32 ? choose_tiles<LINEAR_BACK, true, true>(ctx, p, st) : choose_tiles<LINEAR_BACK, false, true>(ctx, p, st);
-    return form == kF32 ? choose_tiles<LINEAR_BACK, true>(ctx, p, st) : choose_tiles<LINEAR_BACK, false>(ctx, p, st);
+    if (c.z.scale) return form == kF32 ? choose_tiles<LINEAR_BACK, kSummedF32, true>(ctx, p, st) : choose_tiles<LINEAR_BACK, kPlain, true>(ctx, p, st);
+    return form == kF32 ? choose_tiles<LINEAR_BACK, kSummedF32>(ctx, p, st) : choose_tiles<LINEAR_BACK, kPlain>(ctx, p, st);
 }
 
 int launch_gated_linear(adloco_ctx* ctx, const adloco_gated_linear_args& c, cudaStream_t st) {
@@ -1197,7 +1212,7 @@ int launch_gated_linear(adloco_ctx* ctx, const adloco_gated_linear_args& c, cuda
     p.side[OUT1] = kept_side(c.gate);
     p.side[OUT2] = kept_side(c.up);
     if (c.M <= FEW_MAX_M && p.side[OUT1].form != kBytes) return launch_few<true>(ctx, p, st);
-    return choose_tiles<GATED, false>(ctx, p, st);
+    return p.side[OUT1].form == kBytes ? choose_tiles<GATED, kSummed>(ctx, p, st) : choose_tiles<GATED, kPlain>(ctx, p, st);
 }
 
 int launch_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_backward_args& c, cudaStream_t st) {
@@ -1207,7 +1222,7 @@ int launch_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_back
     p.side[OUT0] = side_of(c.a, c.a_stride, kBf16);
     p.side[OUT1] = side_of(c.d_gate, c.d_gate_stride, kBf16);
     p.side[OUT2] = side_of(c.d_up, c.d_up_stride, kBf16);
-    return c.gate.scale ? choose_tiles<GATED_BACK, false, true>(ctx, p, st) : choose_tiles<GATED_BACK, false>(ctx, p, st);
+    return c.gate.scale ? choose_tiles<GATED_BACK, kPlain, true>(ctx, p, st) : choose_tiles<GATED_BACK, kPlain>(ctx, p, st);
 }
 
 }  // namespace adloco
