@@ -176,7 +176,8 @@ __device__ __forceinline__ void add_pieces(const uint4 (&w)[U], Sums& a, float& 
             }
         }
     };
-    if (sizeof(T) == 2 && ENTROPY && low > -INFINITY && m - low < 1e30f) add(Is<false>{});
+    // (of the distances to the running maximum, which may be far above these pieces' own)
+    if (sizeof(T) == 2 && ENTROPY && low > -INFINITY && a.m - low < 1e30f) add(Is<false>{});
     else add(Is<true>{});
     a.s += s.x + s.y;
     if (ENTROPY) a.e += e.x + e.y;
