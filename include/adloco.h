@@ -675,7 +675,8 @@ int adloco_token_logprobs(adloco_ctx* ctx, const adloco_token_logprobs_args* arg
 
 /* The logits' gradient of sum_r d_logp_r logp_r + d_entropy_r entropy_r:
  *   d_logits_j = d_logp (delta_jt - p_j) - d_entropy p_j (log p_j + entropy),    p_j = exp(l_j - lse)
- *   logits, targets, lse, entropy  as given to and by the call above (entropy and d_entropy: both or neither)
+ *   logits, targets, lse, entropy  as given to and by the call above (entropy and d_entropy: both or neither); lse is a float: the
+ *            probabilities are right to 2^-24 |lse|
  *   d_logits  dev [rows, V] in dtype, pitch d_logits_stride; may be logits itself, with the same pitch
  * A row whose target is outside [0, V) takes no part in logp.  A row that takes part in nothing (and whose d_entropy is 0 or
  * not given), or with lse -Inf, gets zeros whatever its logits hold. */

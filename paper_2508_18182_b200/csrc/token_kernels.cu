@@ -414,14 +414,16 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, kBlocks<TPR, CLUSTER>) 
     const bool none = all.s == 0.f;                             // every logit is -Inf
     const float log_s = logf(all.s);
     const float lse = none ? -INFINITY : all.m + log_s;
+    // log-probabilities from the distance to the maximum: lse is rounded to its own size, which says nothing about theirs
+    auto logp_of = [&](float l) { return none ? -INFINITY : (l - all.m) - log_s; };
     if (t == 0) {
-        if (a.logp) a.logp[row] = !given ? 0.f : none ? -INFINITY : at_target - lse;
+        if (a.logp) a.logp[row] = given ? logp_of(at_target) : 0.f;
         if (ENTROPY) a.entropy[row] = none ? 0.f : log_s - __fdiv_rn(all.e, all.s);
         if (a.lse) a.lse[row] = lse;
     }
     for (int i = t; i < a.top; i += TPR) {
         const uint64_t key = sh.best[i];
-        a.top_values[row * a.top + i] = none ? -INFINITY : value_of(key) - lse;
+        a.top_values[row * a.top + i] = logp_of(value_of(key));
         a.top_ids[row * a.top + i] = (int32_t)~(uint32_t)key;
     }
 }

@@ -56,3 +56,17 @@ def test_groups_of_the_lowest_number_behind_usual_ones(ctx, n, V):
     l[:, V // 3:] = -INF
     for a, b in zip(got, run(ctx, l, t, 5)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n,V", [(3, 500), (40, 6000), (2, 50257), (1200, 3000)])
+def test_a_number_added_to_all_logits_changes_no_log_probability(ctx, n, V):
+    """Multiples of 2^-6 below 2^15 are fp32 numbers and so are their differences: all but lse is the same to the last bit."""
+    g = torch.Generator().manual_seed(V)
+    l = torch.randint(-300, 300, (n, V), generator=g).float().div(64).to(DEV)
+    t = torch.randint(0, V, (n,), generator=g, dtype=torch.int32).to(DEV)
+    first = run(ctx, l, t, 5)
+    for shift in (2.0 ** 14, -(2.0 ** 14)):
+        other = run(ctx, l + shift, t, 5)
+        for i in (0, 1, 3, 4):
+            assert torch.equal(first[i], other[i]), i
+        assert bool(((other[2].double() - shift - first[2].double()).abs() <= 2.0 ** -9).all())
