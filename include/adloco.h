@@ -542,6 +542,7 @@ int adloco_blockscale_dequantize(adloco_ctx* ctx, adloco_dtype dtype, int64_t ro
  * cores' own in bf16 outputs (they cut off low bits: a relative error of 1e-6 after 1000 terms), with every 512 terms added
  * up to nearest where an output is F32 or what is kept goes to 8 bits; every output is rounded once.  An output may be the same
  * memory as an elementwise operand (residual, z, gate, up) of the same type and pitch; no other overlap is allowed.
+ * Activations and their derivatives have their limits at the infinities, and a NaN at a NaN.
  * None of them uses the ctx workspace. */
 typedef enum {
     ADLOCO_ACT_NONE = 0,

@@ -78,6 +78,21 @@ __device__ __forceinline__ F2 tail_of(F2 z, F2& e) {
     q = fma2(q, t, both(0.127414796f));
     return mul2(mul2(q, t), e);
 }
+// Of an infinity the limits: factors that meet one that is 0 there are kept finite, by a bound beyond which value and slope
+// are z or 0 and 1 or 0 to the last bit.  A NaN stays one.
+__device__ __forceinline__ float no_less(float z, float low) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(low));
+    return r;
+}
+__device__ __forceinline__ float no_more(float z, float high) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(high));
+    return r;
+}
+__device__ __forceinline__ F2 no_less(F2 z, float low) { return F2{no_less(z.x, low), no_less(z.y, low)}; }
+__device__ __forceinline__ F2 no_more(F2 z, float high) { return F2{no_more(z.x, high), no_more(z.y, high)}; }
+constexpr float kFar = 200.f;
 __device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }                 // a NaN stays one
 // (1 + tanh(v)) / 2 is the logistic function of 2 v, v = sqrt(2 / pi) (z + 0.044715 z^3)
 constexpr float kTanhSlope = 1.5957691216f;
@@ -93,8 +108,8 @@ __device__ __forceinline__ F2 value(Act<ADLOCO_ACT_GELU>, F2 z) {
     // z where the tail is below all numbers; an infinity times its 0 would be none
     return F2{fmaf(-fminf(fabsf(z.x), 1e30f), q.x, fmaxf(z.x, 0.f)), fmaf(-fminf(fabsf(z.y), 1e30f), q.y, fmaxf(z.y, 0.f))};
 }
-__device__ __forceinline__ F2 value(Act<ADLOCO_ACT_GELU_TANH>, F2 z) { return mul2(z, tanh_gate(z)); }
-__device__ __forceinline__ F2 value(Act<ADLOCO_ACT_SILU>, F2 z) { return mul2(z, logistic(z)); }
+__device__ __forceinline__ F2 value(Act<ADLOCO_ACT_GELU_TANH>, F2 z) { return mul2(no_less(z, -kFar), tanh_gate(z)); }
+__device__ __forceinline__ F2 value(Act<ADLOCO_ACT_SILU>, F2 z) { return mul2(no_less(z, -kFar), logistic(z)); }
 
 __device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_NONE>, F2 z, F2& a) { a = z; return both(1.f); }
 __device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_RELU>, F2 z, F2& a) {
@@ -103,20 +118,20 @@ __device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_RELU>, F2 z, F2& a) {
 }
 __device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_GELU>, F2 z, F2& a) {
     F2 e;
-    const F2 q = tail_of(z, e), p = fma2(q, both(-1.f), both(1.f));
-    const F2 h = {z.x < 0.f ? q.x : p.x, z.y < 0.f ? q.y : p.y};
-    a = mul2(z, h);
-    return fma2(mul2(z, e), both(0.39894228f), h);
+    const F2 q = tail_of(z, e), low = no_less(z, -kFar);
+    const F2 h = {z.x < 0.f ? q.x : 1.f - q.x, z.y < 0.f ? q.y : 1.f - q.y};
+    a = mul2(low, h);
+    return fma2(mul2(no_more(low, kFar), e), both(0.39894228f), h);
 }
 __device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_GELU_TANH>, F2 z, F2& a) {
-    const F2 h = tanh_gate(z);
-    a = mul2(z, h);
-    return fma2(mul2(a, fma2(h, both(-1.f), both(1.f))), fma2(mul2(z, z), both(kTanhSlope * 0.134145f), both(kTanhSlope)), h);
+    const F2 low = no_less(z, -kFar), near = no_more(low, kFar), h = tanh_gate(near);
+    a = mul2(low, h);
+    return fma2(mul2(mul2(near, h), fma2(h, both(-1.f), both(1.f))), fma2(mul2(near, near), both(kTanhSlope * 0.134145f), both(kTanhSlope)), h);
 }
 __device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_SILU>, F2 z, F2& a) {
-    const F2 h = logistic(z);
-    a = mul2(z, h);
-    return fma2(a, fma2(h, both(-1.f), both(1.f)), h);
+    const F2 low = no_less(z, -kFar), near = no_more(low, kFar), h = logistic(near);
+    a = mul2(low, h);
+    return fma2(mul2(near, h), fma2(h, both(-1.f), both(1.f)), h);
 }
 // f with the activation as a type: one branch for all that it does
 template <typename F>
