@@ -927,7 +927,8 @@ __device__ __forceinline__ void store_one(const Side& s, int64_t at, float v) {
     if (s.form == kF32) static_cast<float*>(s.p)[at] = v;
     else static_cast<__nv_bfloat16*>(s.p)[at] = __float2bfloat16_rn(v);
 }
-template <int TILES, bool TWO>                                                      // TILES: of eight rows of x
+// F32 outputs take a warp's sums out of the tensor cores every 512 terms, as the tile kernel's do.
+template <int TILES, bool TWO, bool F32>                                            // TILES: of eight rows of x
 __global__ void __launch_bounds__(32 * FEW_MAX_WARPS, TILES == 1 ? 4 : 3) dense_few_kernel(const __grid_constant__ FewArgs a) {
     extern __shared__ float sums[];                                                 // [warps][TILES * 8][FEW_ROWS + 1]
     after_predecessor();
@@ -937,14 +938,25 @@ __global__ void __launch_bounds__(32 * FEW_MAX_WARPS, TILES == 1 ? 4 : 3) dense_
     const __nv_bfloat16* w0 = a.w[0] + (int64_t)(n0 + g) * a.w_stride[0];
     const __nv_bfloat16* w1 = TWO ? a.w[1] + (int64_t)(n0 + g) * a.w_stride[1] : w0 + 8 * a.w_stride[0];
     const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-    float acc[TILES][4];
+    float acc[TILES][4], total[F32 ? TILES : 1][4];
 #pragma unroll
     for (int j = 0; j < TILES; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+        for (int i = 0; i < 4; ++i) {
+            acc[j][i] = 0.f;
+            if (F32) total[j][i] = 0.f;
+        }
+    auto add_up = [&]() {
+#pragma unroll
+        for (int j = 0; j < (F32 ? TILES : 0); ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { total[j][i] += acc[j][i]; acc[j][i] = 0.f; }
+    };
     const int whole = a.K / 64;                                                     // blocks that no row ends in
+    int terms = 0;                                                                  // blocks in the sums
 #pragma unroll 2
     for (int kb = warp; kb < whole; kb += warps) {
+        if (F32 && terms++ == DG_SEGMENT) { add_up(); terms = 1; }
         uint4 p[2], q[2], x[TILES][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -982,11 +994,12 @@ __global__ void __launch_bounds__(32 * FEW_MAX_WARPS, TILES == 1 ? 4 : 3) dense_
             }
         }
     }
+    add_up();
     float* mine = sums + warp * (TILES * 8) * (FEW_ROWS + 1);
 #pragma unroll
     for (int j = 0; j < TILES; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mine[(j * 8 + 2 * t + (i & 1)) * (FEW_ROWS + 1) + g + 8 * (i >> 1)] = acc[j][i];
+        for (int i = 0; i < 4; ++i) mine[(j * 8 + 2 * t + (i & 1)) * (FEW_ROWS + 1) + g + 8 * (i >> 1)] = F32 ? total[F32 ? j : 0][i] : acc[j][i];
     __syncthreads();
     constexpr int OUT = TWO ? FEW_ROWS / 2 : FEW_ROWS;
     for (int i = threadIdx.x; i < TILES * 8 * OUT; i += blockDim.x) {
@@ -1175,7 +1188,7 @@ int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     }
 }
 
-template <bool TWO>
+template <bool TWO, bool F32>
 int launch_few(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     FewArgs a;
     a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K; a.act = p.act;
@@ -1190,8 +1203,8 @@ int launch_few(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
     const int an_sm = (int)((grid.x + ctx->sm_count - 1) / ctx->sm_count), fit = an_sm <= 16 ? 32 / an_sm : FEW_MAX_WARPS;
     const int warps = std::min(std::min(blocks, fit), FEW_MAX_WARPS);
     const size_t smem = (size_t)warps * tiles * 8 * (FEW_ROWS + 1) * sizeof(float);
-    const cudaError_t e = tiles == 1 ? launch_early(dense_few_kernel<1, TWO>, grid, 32 * warps, smem, st, 1, a)
-                                     : launch_early(dense_few_kernel<2, TWO>, grid, 32 * warps, smem, st, 1, a);
+    const cudaError_t e = tiles == 1 ? launch_early(dense_few_kernel<1, TWO, F32>, grid, 32 * warps, smem, st, 1, a)
+                                     : launch_early(dense_few_kernel<2, TWO, F32>, grid, 32 * warps, smem, st, 1, a);
     ADLOCO_CUDA_TRY(ctx, e);
     ctx->launches++;
     return ADLOCO_OK;
@@ -1205,7 +1218,7 @@ int launch_linear(adloco_ctx* ctx, const adloco_linear_args& c, cudaStream_t st)
     p.side[IN0] = side_of(c.residual, c.residual_stride, form);
     p.side[OUT0] = side_of(c.y, c.y_stride, form);
     p.side[OUT1] = kept_side(c.z);
-    if (c.M <= FEW_MAX_M && p.side[OUT1].form != kBytes) return launch_few<false>(ctx, p, st);
+    if (c.M <= FEW_MAX_M && p.side[OUT1].form != kBytes) return form == kF32 ? launch_few<false, true>(ctx, p, st) : launch_few<false, false>(ctx, p, st);
     if (form == kF32) return choose_tiles<LINEAR, kSummedF32>(ctx, p, st);
     return p.side[OUT1].form == kBytes ? choose_tiles<LINEAR, kSummed>(ctx, p, st) : choose_tiles<LINEAR, kPlain>(ctx, p, st);
 }
@@ -1226,7 +1239,7 @@ int launch_gated_linear(adloco_ctx* ctx, const adloco_gated_linear_args& c, cuda
     p.side[OUT0] = side_of(c.a, c.a_stride, kBf16);
     p.side[OUT1] = kept_side(c.gate);
     p.side[OUT2] = kept_side(c.up);
-    if (c.M <= FEW_MAX_M && p.side[OUT1].form != kBytes) return launch_few<true>(ctx, p, st);
+    if (c.M <= FEW_MAX_M && p.side[OUT1].form != kBytes) return launch_few<true, false>(ctx, p, st);
     return p.side[OUT1].form == kBytes ? choose_tiles<GATED, kSummed>(ctx, p, st) : choose_tiles<GATED, kPlain>(ctx, p, st);
 }
 
