@@ -541,7 +541,8 @@ int adloco_blockscale_dequantize(adloco_ctx* ctx, adloco_dtype dtype, int64_t ro
  * other tensors may have any pitch, 16-byte aligned rows being the fast ones.  Products are exact, sums fp32: the tensor
  * cores' own in bf16 outputs (they cut off low bits: a relative error of 1e-6 after 1000 terms), with every 512 terms added
  * up to nearest where an output is F32 or what is kept goes to 8 bits; every output is rounded once.  An output may be the same
- * memory as an elementwise operand (residual, z, gate, up) of the same type and pitch; no other overlap is allowed.
+ * memory as an elementwise operand (residual, z, gate, up) of the same type and pitch; any other overlap of an output, scales
+ * among them, is refused.
  * Activations and their derivatives have their limits at the infinities, and a NaN at a NaN.
  * None of them uses the ctx workspace. */
 typedef enum {
@@ -656,7 +657,7 @@ int adloco_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_back
  * largest first, equal ones by the lower id.
  *   logits   dev [rows, V] in dtype, pitch logits_stride;  targets dev int32 [rows], may be NULL when logp is
  *   logp, entropy, lse   dev [rows] float, each may be NULL;  top_values float, top_ids int32 dev [rows, top]
- *            contiguous, both or neither, 0 <= top <= 64, top <= V
+ *            contiguous, both or neither, 0 <= top <= 64, top <= V.  No output may overlap anything else.
  * A row whose target is outside [0, V) has logp 0.  Logits of -Inf (tokens ruled out) have probability 0 and log-probability
  * -Inf; a row of nothing else has lse, logp and top_values -Inf and entropy 0.  A row with a NaN or +Inf has NaN in all of them,
  * and ids of some tokens of the vocabulary.  fp32 throughout, one pass over the logits (choosing the best tokens reads a few parts of a row again, a row of many equal logits once for
@@ -678,7 +679,7 @@ int adloco_token_logprobs(adloco_ctx* ctx, const adloco_token_logprobs_args* arg
  *   d_logits_j = d_logp (delta_jt - p_j) - d_entropy p_j (log p_j + entropy),    p_j = exp(l_j - lse)
  *   logits, targets, lse, entropy  as given to and by the call above (entropy and d_entropy: both or neither); lse is a float: the
  *            probabilities are right to 2^-24 |lse|
- *   d_logits  dev [rows, V] in dtype, pitch d_logits_stride; may be logits itself, with the same pitch
+ *   d_logits  dev [rows, V] in dtype, pitch d_logits_stride; may be logits itself, with the same pitch, and overlap nothing else
  * A row whose target is outside [0, V) takes no part in logp.  A row that takes part in nothing (and whose d_entropy is 0 or
  * not given), or with lse -Inf, gets zeros whatever its logits hold. */
 typedef struct {

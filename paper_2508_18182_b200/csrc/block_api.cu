@@ -121,25 +121,47 @@ int check_kept(const adloco_kept& k, int64_t cols) {
     const int rc = check_bytes(k.p, k.stride, cols);
     return rc != ADLOCO_OK ? rc : check_row_scales(k.scale, k.scale_stride, cols);
 }
-// What a product's epilogue reads and writes element by element: an output may be one of those operands, in its type and
-// pitch, but no other output and no operand of the product.
-struct Matrix {
+// Where a matrix lies: rows of `width` bytes, `pitch` bytes apart.
+struct Area {
     const void* p;
-    int64_t stride, bytes;              // an element's
+    int64_t pitch, width, rows;
 };
-bool apart(std::initializer_list<Matrix> outs, std::initializer_list<Matrix> elementwise, std::initializer_list<const void*> operands, int64_t rows) {
-    for (const Matrix* o = outs.begin(); o != outs.end(); ++o) {
-        if (!o->p) continue;
-        for (const Matrix* other = outs.begin(); other != o; ++other)
-            if (other->p == o->p) return false;
-        for (const Matrix& e : elementwise)
-            if (e.p == o->p && (e.bytes != o->bytes || !in_step(o->p, o->stride, e.p, e.stride, rows))) return false;
-        for (const void* x : operands)
-            if (x == o->p) return false;
+Area area(const void* p, int64_t stride, int64_t cols, int64_t rows, int64_t bytes) { return Area{p, stride * bytes, cols * bytes, rows}; }
+Area line(const void* p, int64_t n, int64_t bytes = 4) { return Area{p, n * bytes, n * bytes, 1}; }
+Area values_of(const adloco_kept& k, int64_t rows, int64_t cols) { return area(k.p, k.stride, cols, rows, k.scale ? 1 : 2); }
+Area scales_of(const adloco_kept& k, int64_t rows, int64_t cols) { return area(k.scale, k.scale_stride, (cols + 127) / 128, rows, 1); }
+bool same_place(const Area& a, const Area& b) {
+    return a.p == b.p && a.width == b.width && a.rows == b.rows && (a.rows == 1 || a.pitch == b.pitch);
+}
+// Do two matrices share a byte?  Exact where the pitches are alike (columns of one matrix) or one of them is a single row no
+// longer than the other's pitch; what else lies within one another's span counts as sharing.
+bool touch(const Area& a, const Area& b) {
+    typedef __int128 wide;
+    if (!a.p || !b.p) return false;
+    const wide at = (wide)reinterpret_cast<uintptr_t>(a.p), bt = (wide)reinterpret_cast<uintptr_t>(b.p);
+    if (at + (wide)(a.rows - 1) * a.pitch + a.width <= bt || bt + (wide)(b.rows - 1) * b.pitch + b.width <= at) return false;
+    if (a.rows == 1 && b.rows == 1) return true;
+    const int64_t pitch = a.rows > 1 ? a.pitch : b.pitch;
+    if ((b.rows > 1 && b.pitch != pitch) || a.width > pitch || b.width > pitch) return true;
+    // row j of b begins d bytes behind the beginning of a's row j + k, and reaches into its next one where it passes the pitch
+    wide k = (bt - at) / pitch, d = (bt - at) % pitch;
+    if (d < 0) { d += pitch; --k; }
+    const auto some = [&](wide shift) { return shift < a.rows && -shift < b.rows; };
+    return (d < a.width && some(k)) || (d + b.width > pitch && some(k + 1));
+}
+// An output may be one of the operands that are read at the place that is written (the same elements, row for row), but may
+// share nothing else with them, nor anything with another output or with what is read elsewhere.
+bool apart(std::initializer_list<Area> outs, std::initializer_list<Area> elementwise, std::initializer_list<Area> others) {
+    for (const Area* o = outs.begin(); o != outs.end(); ++o) {
+        for (const Area* other = outs.begin(); other != o; ++other)
+            if (touch(*o, *other)) return false;
+        for (const Area& e : elementwise)
+            if (touch(*o, e) && !same_place(*o, e)) return false;
+        for (const Area& x : others)
+            if (touch(*o, x)) return false;
     }
     return true;
 }
-Matrix matrix_of(const adloco_kept& k) { return Matrix{k.p, k.stride, k.scale ? 1 : 2}; }
 bool known_act(int32_t a) { return a >= ADLOCO_ACT_NONE && a <= ADLOCO_ACT_SILU; }
 bool too_large(std::initializer_list<int64_t> extents) {
     for (int64_t e : extents)
@@ -334,12 +356,15 @@ int adloco_blockscale_matmul(adloco_ctx* ctx, const adloco_blockscale_matmul_arg
 int adloco_blockscale_dequantize(adloco_ctx* ctx, adloco_dtype dtype, int64_t rows, int64_t cols, const void* q,
                                  int64_t q_stride, const uint8_t* scale, int64_t scale_stride, void* x, int64_t x_stride,
                                  void* stream) {
-    if (!ctx || !q || !scale || !x || rows < 1 || cols < 1 || x_stride < cols || x == q) return ADLOCO_ERR_INVALID_ARG;
+    if (!ctx || !q || !scale || !x || rows < 1 || cols < 1 || x_stride < cols) return ADLOCO_ERR_INVALID_ARG;
     if (!known(dtype) || too_large({rows, cols})) return ADLOCO_ERR_UNSUPPORTED;
     if (!elem_aligned(x, dtype)) return ADLOCO_ERR_ALIGNMENT;
     int rc = check_bytes(q, q_stride, cols);
     if (rc == ADLOCO_OK) rc = check_row_scales(scale, scale_stride, cols);
     if (rc != ADLOCO_OK) return rc;
+    if (!apart({area(x, x_stride, cols, rows, (int64_t)elem_bytes(dtype))}, {},
+               {area(q, q_stride, cols, rows, 1), area(scale, scale_stride, (cols + 127) / 128, rows, 1)}))
+        return ADLOCO_ERR_INVALID_ARG;
     DeviceGuard g(ctx->device);
     return launch_blockscale_dequantize(ctx, dtype == ADLOCO_BF16, rows, cols, q, q_stride, scale, scale_stride, x, x_stride,
                                         static_cast<cudaStream_t>(stream));
@@ -354,7 +379,10 @@ int adloco_linear(adloco_ctx* ctx, const adloco_linear_args* a, void* stream) {
     if (rc == ADLOCO_OK) rc = check_kept(a->z, a->N);
     if (rc != ADLOCO_OK) return rc;
     const int64_t es = (int64_t)elem_bytes(a->out_dtype);
-    if (!apart({{a->y, a->y_stride, es}, matrix_of(a->z)}, {{a->residual, a->residual_stride, es}}, {a->x, a->w, a->bias}, a->M)) return ADLOCO_ERR_INVALID_ARG;
+    if (!apart({area(a->y, a->y_stride, a->N, a->M, es), values_of(a->z, a->M, a->N), scales_of(a->z, a->M, a->N)},
+               {area(a->residual, a->residual_stride, a->N, a->M, es)},
+               {area(a->x, a->x_stride, a->K, a->M, 2), area(a->w, a->w_stride, a->K, a->N, 2), line(a->bias, a->N)}))
+        return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(a->y, a->out_dtype) || !elem_aligned(a->residual, a->out_dtype) || !elem_aligned(a->bias, ADLOCO_F32)) return ADLOCO_ERR_ALIGNMENT;
     DeviceGuard g(ctx->device);
     return launch_linear(ctx, *a, static_cast<cudaStream_t>(stream));
@@ -370,7 +398,9 @@ int adloco_linear_backward(adloco_ctx* ctx, const adloco_linear_backward_args* a
     if (rc == ADLOCO_OK) rc = check_kept(a->z, a->K);
     if (rc != ADLOCO_OK) return rc;
     const int64_t es = (int64_t)elem_bytes(a->out_dtype);
-    if (!apart({{a->dx, a->dx_stride, es}, {a->a, a->a_stride, 2}}, {{a->residual, a->residual_stride, es}, matrix_of(a->z)}, {a->dy, a->w}, a->M))
+    if (!apart({area(a->dx, a->dx_stride, a->K, a->M, es), area(a->a, a->a_stride, a->K, a->M, 2)},
+               {area(a->residual, a->residual_stride, a->K, a->M, es), values_of(a->z, a->M, a->K)},
+               {area(a->dy, a->dy_stride, a->N, a->M, 2), area(a->w, a->w_stride, a->K, a->N, 2), scales_of(a->z, a->M, a->K)}))
         return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(a->dx, a->out_dtype) || !elem_aligned(a->residual, a->out_dtype) || !elem_aligned(a->a, ADLOCO_BF16)) return ADLOCO_ERR_ALIGNMENT;
     DeviceGuard g(ctx->device);
@@ -387,7 +417,10 @@ int adloco_gated_linear(adloco_ctx* ctx, const adloco_gated_linear_args* a, void
     if (rc == ADLOCO_OK) rc = check_kept(a->gate, a->f);
     if (rc == ADLOCO_OK) rc = check_kept(a->up, a->f);
     if (rc != ADLOCO_OK) return rc;
-    if (!apart({{a->a, a->a_stride, 2}, matrix_of(a->gate), matrix_of(a->up)}, {}, {a->x, a->w_gate, a->w_up}, a->M)) return ADLOCO_ERR_INVALID_ARG;
+    if (!apart({area(a->a, a->a_stride, a->f, a->M, 2), values_of(a->gate, a->M, a->f), values_of(a->up, a->M, a->f), scales_of(a->gate, a->M, a->f),
+                scales_of(a->up, a->M, a->f)},
+               {}, {area(a->x, a->x_stride, a->d, a->M, 2), area(a->w_gate, a->w_gate_stride, a->d, a->f, 2), area(a->w_up, a->w_up_stride, a->d, a->f, 2)}))
+        return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(a->a, ADLOCO_BF16)) return ADLOCO_ERR_ALIGNMENT;
     DeviceGuard g(ctx->device);
     return launch_gated_linear(ctx, *a, static_cast<cudaStream_t>(stream));
@@ -403,8 +436,10 @@ int adloco_gated_linear_backward(adloco_ctx* ctx, const adloco_gated_linear_back
     if (rc == ADLOCO_OK) rc = check_kept(a->gate, a->f);
     if (rc == ADLOCO_OK) rc = check_kept(a->up, a->f);
     if (rc != ADLOCO_OK) return rc;
-    if (!apart({{a->d_gate, a->d_gate_stride, 2}, {a->d_up, a->d_up_stride, 2}, {a->a, a->a_stride, 2}}, {matrix_of(a->gate), matrix_of(a->up)},
-               {a->dy, a->w_down}, a->M))
+    if (!apart({area(a->d_gate, a->d_gate_stride, a->f, a->M, 2), area(a->d_up, a->d_up_stride, a->f, a->M, 2), area(a->a, a->a_stride, a->f, a->M, 2)},
+               {values_of(a->gate, a->M, a->f), values_of(a->up, a->M, a->f)},
+               {area(a->dy, a->dy_stride, a->d, a->M, 2), area(a->w_down, a->w_down_stride, a->f, a->d, 2), scales_of(a->gate, a->M, a->f),
+                scales_of(a->up, a->M, a->f)}))
         return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(a->d_gate, ADLOCO_BF16) || !elem_aligned(a->d_up, ADLOCO_BF16) || !elem_aligned(a->a, ADLOCO_BF16)) return ADLOCO_ERR_ALIGNMENT;
     DeviceGuard g(ctx->device);
@@ -417,10 +452,10 @@ int adloco_token_logprobs(adloco_ctx* ctx, const adloco_token_logprobs_args* a, 
     if (a->top < 0 || a->top > a->V || (a->top > 0) != (a->top_values != nullptr) || (a->top > 0) != (a->top_ids != nullptr)) return ADLOCO_ERR_INVALID_ARG;
     if (a->logp && !a->targets) return ADLOCO_ERR_INVALID_ARG;
     if (!a->logp && !a->entropy && !a->lse && a->top == 0) return ADLOCO_ERR_INVALID_ARG;
-    const void* outs[] = {a->logp, a->entropy, a->lse, a->top_values, a->top_ids};
-    for (int i = 0; i < 5; ++i)
-        for (int j = 0; j < i; ++j)
-            if (outs[i] && (outs[i] == outs[j] || outs[i] == a->logits)) return ADLOCO_ERR_INVALID_ARG;
+    if (!apart({line(a->logp, a->rows), line(a->entropy, a->rows), line(a->lse, a->rows), line(a->top_values, a->rows * a->top),
+                line(a->top_ids, a->rows * a->top)},
+               {}, {area(a->logits, a->logits_stride, a->V, a->rows, (int64_t)elem_bytes(a->dtype)), line(a->targets, a->rows)}))
+        return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(a->logits, a->dtype) || !elem_aligned(a->targets, ADLOCO_F32) || !elem_aligned(a->logp, ADLOCO_F32) ||
         !elem_aligned(a->entropy, ADLOCO_F32) || !elem_aligned(a->lse, ADLOCO_F32) || !elem_aligned(a->top_values, ADLOCO_F32) ||
         !elem_aligned(a->top_ids, ADLOCO_F32))
@@ -432,8 +467,10 @@ int adloco_token_logprobs(adloco_ctx* ctx, const adloco_token_logprobs_args* a, 
 int adloco_token_logprobs_backward(adloco_ctx* ctx, const adloco_token_logprobs_backward_args* a, void* stream) {
     if (!ctx || !a || !a->logits || !a->targets || !a->lse || !a->d_logp || !a->d_logits || a->rows < 1 || a->V < 1) return ADLOCO_ERR_INVALID_ARG;
     if (!known(a->dtype) || too_large({a->rows, a->V})) return ADLOCO_ERR_UNSUPPORTED;
-    if (a->logits_stride < a->V || a->d_logits_stride < a->V || !a->entropy != !a->d_entropy ||
-        !in_step(a->d_logits, a->d_logits_stride, a->logits, a->logits_stride, a->rows))
+    if (a->logits_stride < a->V || a->d_logits_stride < a->V || !a->entropy != !a->d_entropy) return ADLOCO_ERR_INVALID_ARG;
+    const int64_t es = (int64_t)elem_bytes(a->dtype);
+    if (!apart({area(a->d_logits, a->d_logits_stride, a->V, a->rows, es)}, {area(a->logits, a->logits_stride, a->V, a->rows, es)},
+               {line(a->targets, a->rows), line(a->lse, a->rows), line(a->d_logp, a->rows), line(a->entropy, a->rows), line(a->d_entropy, a->rows)}))
         return ADLOCO_ERR_INVALID_ARG;
     if (!elem_aligned(a->logits, a->dtype) || !elem_aligned(a->d_logits, a->dtype) || !elem_aligned(a->targets, ADLOCO_F32) ||
         !elem_aligned(a->lse, ADLOCO_F32) || !elem_aligned(a->d_logp, ADLOCO_F32) || !elem_aligned(a->entropy, ADLOCO_F32) ||
