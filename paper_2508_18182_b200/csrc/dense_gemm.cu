@@ -45,7 +45,7 @@ struct GemmArgs {
     int tiles_n, tiles;
     int act;
     int stages;
-    int split;                        // CTAs that share a tile's K, one cluster (1: none do)
+    int split;                        // 2: two CTAs of a cluster share a tile's K; 1: none do
     int a_bytes;                      // of A in a stage: of all its 128 rows, or of those that exist
     uint32_t warp_bytes;              // boxes of one epilogue warp
     uint32_t in_bytes;                // that arrive by TMA for one chunk
@@ -307,8 +307,8 @@ __device__ __forceinline__ float larger(float m, float v) {
 // whose steps are so wide (2^-4) that each number on the other side of a border shows (4096 x 2048 -> 2 x 5632, both kept, and the way
 // back: 7.0e-4 of the norm away from the fp32 form with the accumulator as it is, 3.4e-4 so, 2.4e-4 with a sum of every 256; 131, 132
 // and 139 us forward).
-// SPLIT K: where few tiles leave most SMs idle, up to four CTAs of a cluster take a part of K each.  All but the first write
-// their sums into the first one's shared memory, which adds them up in their order and goes on alone.
+// SPLIT K: where few tiles of 64 columns leave most SMs idle, two CTAs of a cluster take half of K each.  The second one writes its
+// sums into the first one's shared memory, which adds them to its own and goes on alone.
 // The epilogue's eight warps each own 32 rows and half the columns, in chunks of 32: the operands of the next chunk arrive by
 // TMA while this one is computed, the results leave by TMA.  IN8: what the forward pass kept is in 8 bits.
 // What bounds it: at long K the tensor pipe and the power cap (8192 x 4096 -> 4096: 169 us, 1.63 PFLOP/s); at K = 768 a tile's MMAs take
@@ -349,10 +349,13 @@ struct Walk {
     }
 };
 
+template <int KIND, bool PAIR, int BN>
+__host__ __device__ constexpr bool dg_can_split() { return !PAIR && KIND != GATED && BN == 64; }
+
 template <int KIND, bool PAIR, int BN, int SUM, bool IN8>
 __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmArgs a) {
     constexpr bool TWO = KIND == GATED, BACK = KIND == LINEAR_BACK || KIND == GATED_BACK, FORWARD = !BACK;
-    constexpr bool SUMMED = SUM != kPlain, F32 = SUM == kSummedF32;
+    constexpr bool SUMMED = SUM != kPlain, F32 = SUM == kSummedF32, SPLIT = dg_can_split<KIND, PAIR, BN>();
     constexpr int COLS = TWO ? BN / 2 : BN;                // output columns of a tile
     constexpr int TM = PAIR ? 256 : 128;
     constexpr int CHUNKS = COLS / 64;                      // of an epilogue warp
@@ -372,14 +375,14 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     auto in_bar = [&](uint32_t w, uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * w + s); };
     const uint32_t drain_bar = bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * DG_EPI), join_bar = drain_bar + 8u;
     auto swap_bar = [&](uint32_t w) { return bars + 8u * (2 * DG_MAX_STAGES + 6 + 2 * DG_EPI + w); };
-    const uint32_t join = bars + DG_BAR_BYTES;                 // the other parts' sums, or the maxima that warps tell one another
+    const uint32_t join = bars + DG_BAR_BYTES;                 // the other half's sums, or the maxima that warps tell one another
     static_assert(8 * (2 * DG_MAX_STAGES + 6 + 3 * DG_EPI) <= 512, "barriers");
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // warp: known to be uniform
     const uint32_t rank = PAIR ? cluster_cta_rank() : 0;       // 0: the CTA that issues the MMAs
-    const uint32_t split = PAIR ? 1u : (uint32_t)a.split, part = PAIR || split == 1 ? 0u : cluster_cta_rank();
+    const uint32_t split = SPLIT ? (uint32_t)a.split : 1u, part = split == 1 ? 0u : cluster_cta_rank();
     Walk walk(a, PAIR ? (int)(blockIdx.x >> 1) : (int)(blockIdx.x / split), PAIR ? (int)(gridDim.x >> 1) : (int)(gridDim.x / split));
     const int k_first = (int)(a.kb * part / split), k_end = (int)(a.kb * (part + 1) / split);      // this CTA's blocks of K
     const uint32_t stages = (uint32_t)a.stages;
@@ -392,7 +395,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
             mbar_init(swap_bar(w), 1);
         }
         mbar_init(drain_bar, 1);
-        mbar_init(join_bar, (split - 1) * DG_EPI + 1);
+        if (SPLIT) mbar_init(join_bar, DG_EPI + 1);
         fence_barrier_init();
         prefetch_tmap(&maps.a);
         prefetch_tmap(&maps.b[0]);
@@ -653,15 +656,13 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 ++n;
             }
             const uint32_t acc = lane_tmem + buf * BN;
-            // a part's number of this lane's row: 16-byte pieces of a row swapped so that neighbouring rows fall on all banks
-            auto joint = [&](uint32_t base, uint32_t of, int c) {
-                return base + ((of - 1) * 128 + q * 32 + lane) * (BN * 4u) + (uint32_t)(((c >> 2) ^ (lane & 7)) << 4);
-            };
-            if (!PAIR && part > 0) {                           // the launch has one tile a cluster: this is all that it does
+            // the second half's number of this lane's row: 16-byte pieces of a row swapped so that neighbouring rows fall on all banks
+            auto joint = [&](uint32_t base, int c) { return base + (q * 32 + lane) * (BN * 4u) + (uint32_t)(((c >> 2) ^ (lane & 7)) << 4); };
+            if (SPLIT && part > 0) {                           // the launch has one tile a cluster: this is all that it does
                 const uint32_t there = map_to_cta(join, 0);
 #pragma unroll
-                for (int i = 0; i < (TWO ? 2 : 1) * CHUNKS; ++i) {
-                    const int c = (TWO && i >= CHUNKS ? COLS - 32 * CHUNKS : 0) + first + 32 * i;
+                for (int i = 0; i < CHUNKS; ++i) {
+                    const int c = first + 32 * i;
                     uint32_t r[32];
                     if constexpr (SUMMED) {
 #pragma unroll
@@ -674,26 +675,24 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                         tmem_ld_wait();
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) st_cluster_v4(joint(there, part, c + e), r[e], r[e + 1], r[e + 2], r[e + 3]);
+                    for (int e = 0; e < 32; e += 4) st_cluster_v4(joint(there, c + e), r[e], r[e + 1], r[e + 2], r[e + 3]);
                 }
                 if (!SUMMED) release(buf);
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(join_bar, 0));
                 continue;
             }
-            if (!PAIR && split > 1) {
+            if (SPLIT && split > 1) {
                 if (w == 0 && lane == 0) mbar_arrive(join_bar);
                 if (!wait_warp<true>(join_bar, 0, abortp, a.wait_ns)) { ok = false; break; }
             }
-            auto add_parts = [&](int c, F2 (&v)[4]) {          // to the eight columns from c on of the accumulator
-                if (PAIR) return;
-                for (uint32_t of = 1; of < split; ++of) {
+            auto add_half = [&](int c, F2 (&v)[4]) {           // to the eight columns from c on of the accumulator
+                if (!SPLIT || split == 1) return;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint4 o = lds16(joint(join, of, c + 4 * h));
-                        v[2 * h] = add2(v[2 * h], F2{__uint_as_float(o.x), __uint_as_float(o.y)});
-                        v[2 * h + 1] = add2(v[2 * h + 1], F2{__uint_as_float(o.z), __uint_as_float(o.w)});
-                    }
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 o = lds16(joint(join, c + 4 * h));
+                    v[2 * h] = add2(v[2 * h], F2{__uint_as_float(o.x), __uint_as_float(o.y)});
+                    v[2 * h + 1] = add2(v[2 * h + 1], F2{__uint_as_float(o.z), __uint_as_float(o.w)});
                 }
             };
             if constexpr (SUMMED) {
@@ -701,7 +700,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        add_parts(first + 32 * i + 8 * g, sum[i][g]);
+                        add_half(first + 32 * i + 8 * g, sum[i][g]);
                         add_bias(first - block + 32 * i + 8 * g, sum[i][g]);
                     }
             }
@@ -783,8 +782,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     if (i == CHUNKS - 1) release(buf);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        add_parts(first + 32 * i + 8 * g, v[g]);
-                        if constexpr (TWO) add_parts(COLS + first + 32 * i + 8 * g, x[g]);
+                        add_half(first + 32 * i + 8 * g, v[g]);
                         add_bias(first - block + 32 * i + 8 * g, v[g]);
                     }
                 }
@@ -1049,7 +1047,53 @@ struct Product {
     int64_t b_stride[2];
     const float* bias;
     Side side[SIDES];
+    uint32_t warp_bytes, in_bytes;    // what lay_out makes of the sides
+    int twice;
 };
+
+// How the sides reach their boxes, and where these lie in an epilogue warp's memory: largest first so that each starts on a
+// multiple of its swizzle's span; operands twice (they are fetched a chunk ahead), outputs twice where nothing is fetched and
+// that takes no more than 8 KB, an output over the operand of its form that is read at the same place.
+template <int KIND>
+void lay_out(Product& p) {
+    p.in_bytes = 0;
+    int64_t outputs = 0;
+    for (int i = 0; i < SIDES; ++i) {
+        Side& s = p.side[i];
+        if (s.form == kNone) continue;
+        const int64_t es = elem(s.form);
+        s.pieces = aligned16(s.p) && s.pitch * es % 16 == 0;
+        // a store writes a row's last 16 bytes in full, beyond the matrix too
+        s.tma = s.pieces && (i <= IN1 || p.N * es % 16 == 0);
+        if (s.tma && i <= IN1) p.in_bytes += (uint32_t)(1024 * es);
+        if (i >= OUT0) outputs += 1024 * es;
+    }
+    p.twice = p.in_bytes == 0 && 2 * outputs <= 8192;
+    constexpr int over[SIDES] = {-1, -1, KIND == GATED_BACK ? -1 : IN0, KIND == GATED_BACK ? IN0 : KIND == LINEAR_BACK ? IN1 : -1,
+                                 KIND == GATED_BACK ? IN1 : -1};
+    uint32_t used = 0;
+    for (int form : {(int)kF32, (int)kBf16, (int)kBytes})
+        for (int i = 0; i < SIDES; ++i) {
+            Side& s = p.side[i];
+            if (s.form != form || (over[i] >= 0 && p.side[over[i]].form == form)) continue;
+            const uint32_t bytes = (uint32_t)(1024 * elem(form));
+            s.box[0] = used;
+            s.box[1] = i <= IN1 || p.twice ? used + bytes : used;
+            used = s.box[1] + bytes;
+        }
+    for (int i = OUT0; i < SIDES; ++i)
+        if (over[i] >= 0 && p.side[i].form != kNone && p.side[over[i]].form == p.side[i].form)
+            for (int b = 0; b < 2; ++b) p.side[i].box[b] = p.side[over[i]].box[b];
+    p.warp_bytes = (used + 1023u) & ~1023u;
+}
+
+// Shared memory beside the ring and the boxes: barriers, the bias, and the sums of K's other half or the maxima of what goes to 8 bits.
+int64_t words_of(const Product& p, int split) { return DG_BAR_BYTES + (split > 1 ? 128 * 64 * 4 : p.side[OUT1].form == kBytes ? DG_EPI * 512 : 0); }
+template <bool PAIR, int BN>
+int stages_of(const Product& p, int split) {
+    const int64_t n = (DG_SMEM - 1024 - words_of(p, split) - (int64_t)DG_EPI * p.warp_bytes) / dg_stage_bytes<PAIR, BN>();
+    return (int)(n < DG_MAX_STAGES ? n : DG_MAX_STAGES);
+}
 
 template <int KIND, bool PAIR, int BN, int SUM, bool IN8>
 int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st, int split = 1) {
@@ -1064,7 +1108,10 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st, int split =
     a.tiles_n = (int)tn; a.tiles = (int)(tm * tn);
     a.act = p.act; a.bias = p.bias;
     a.status = ctx->gemm_status; a.wait_ns = ctx->wait_limit_ns;
-    a.in_bytes = 0;
+    a.in_bytes = p.in_bytes; a.twice = p.twice; a.warp_bytes = p.warp_bytes;
+    a.split = split;
+    a.stages = stages_of<PAIR, BN>(p, split);
+    if (a.stages < 2) return ADLOCO_ERR_UNSUPPORTED;
     Maps maps;
     // (what lies in the rest of A's 128 rows only reaches rows of the result that do not exist)
     const uint32_t a_rows = p.M < 128 ? (uint32_t)(p.M + 7) / 8 * 8 : 128;
@@ -1075,58 +1122,21 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st, int split =
                   : make_map(ctx, &maps.b[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.b[i], p.N, p.K, p.b_stride[i], 64, TWO ? COLS : PAIR ? BN / 2 : BN);
     if (!TWO) maps.b[1] = maps.b[0];
     for (int i = 0; i < SIDES && rc == ADLOCO_OK; ++i) {
-        Side& s = a.side[i] = p.side[i];
+        const Side& s = a.side[i] = p.side[i];
         maps.side[i] = maps.a;                        // not looked at where no box goes by TMA
-        if (s.form == kNone) continue;
-        const int64_t es = elem(s.form);
-        s.pieces = aligned16(s.p) && s.pitch * es % 16 == 0;
-        // a store writes a row's last 16 bytes in full, beyond the matrix too
-        s.tma = s.pieces && (i <= IN1 || p.N * es % 16 == 0);
         if (!s.tma) continue;
         rc = s.form == kBf16 ? make_map(ctx, &maps.side[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, s.p, p.M, p.N, s.pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)
            : s.form == kF32 ? make_map(ctx, &maps.side[i], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, s.p, p.M, p.N, s.pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B)
                             : make_map(ctx, &maps.side[i], CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, s.p, p.M, p.N, s.pitch, 32, 32, CU_TENSOR_MAP_SWIZZLE_32B);
-        if (i <= IN1) a.in_bytes += (uint32_t)(1024 * es);
     }
     if (rc != ADLOCO_OK) return rc;
-    // the boxes of an epilogue warp, largest first so that each starts on a multiple of its swizzle's span: operands twice
-    // (they are fetched a chunk ahead), outputs twice where nothing is fetched and that takes no more than 8 KB, an output over
-    // the operand of its form that is read at the same place
-    constexpr int over[SIDES] = {-1, -1, KIND == GATED_BACK ? -1 : IN0, KIND == GATED_BACK ? IN0 : KIND == LINEAR_BACK ? IN1 : -1,
-                                 KIND == GATED_BACK ? IN1 : -1};
-    int64_t outputs = 0;
-    for (int i = OUT0; i < SIDES; ++i) outputs += a.side[i].form == kNone ? 0 : 1024 * elem(a.side[i].form);
-    a.twice = a.in_bytes == 0 && 2 * outputs <= 8192;
-    uint32_t used = 0;
-    for (int form : {(int)kF32, (int)kBf16, (int)kBytes})
-        for (int i = 0; i < SIDES; ++i) {
-            Side& s = a.side[i];
-            if (s.form != form || (over[i] >= 0 && a.side[over[i]].form == form)) continue;
-            const uint32_t bytes = (uint32_t)(1024 * elem(form));
-            s.box[0] = used;
-            s.box[1] = i <= IN1 || a.twice ? used + bytes : used;
-            used = s.box[1] + bytes;
-        }
-    for (int i = OUT0; i < SIDES; ++i)
-        if (over[i] >= 0 && a.side[i].form != kNone && a.side[over[i]].form == a.side[i].form)
-            for (int b = 0; b < 2; ++b) a.side[i].box[b] = a.side[over[i]].box[b];
-    a.warp_bytes = (used + 1023u) & ~1023u;
-    int64_t extra = 0;
-    for (;; split /= 2) {                             // parts whose sums leave room for four stages
-        extra = DG_BAR_BYTES + (a.side[OUT1].form == kBytes ? DG_EPI * 512 : (split - 1) * 128 * BN * 4);
-        const int64_t left = DG_SMEM - 1024 - extra - (int64_t)DG_EPI * a.warp_bytes;
-        a.stages = (int)(left / STAGE < DG_MAX_STAGES ? left / STAGE : DG_MAX_STAGES);
-        if (split == 1 || a.stages * BLOCKS >= 4) break;
-    }
-    a.split = split;
-    if (a.stages < 2) return ADLOCO_ERR_UNSUPPORTED;
     auto* kernel = dense_tile_kernel<KIND, PAIR, BN, SUM, IN8>;
     static std::atomic<bool> attr_set[64];            // the attribute is per device
     if (!attr_set[ctx->device & 63].load()) {
         ADLOCO_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DG_SMEM));
         attr_set[ctx->device & 63].store(true);
     }
-    const size_t smem = (size_t)a.stages * STAGE + DG_EPI * (size_t)a.warp_bytes + (size_t)extra + 1024;
+    const size_t smem = (size_t)a.stages * STAGE + DG_EPI * (size_t)a.warp_bytes + (size_t)words_of(p, split) + 1024;
     const int most = PAIR ? ctx->sm_count / 2 : ctx->sm_count, workers = a.tiles < most ? a.tiles : most;
     ADLOCO_CUDA_TRY(ctx, launch_early(kernel, dim3((PAIR ? 2 : split) * workers), DG_THREADS, smem, st, PAIR ? 2 : split, maps, a));
     ctx->launches++;
@@ -1138,7 +1148,8 @@ int launch_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st, int split =
 // 384 for a pair's 256 x 128 and one CTA's 128 x 64, less where A has fewer rows; a tile's epilogue as much as four (two, one) stages
 // that nothing hides when there is one round.
 template <int KIND, int SUM, bool IN8 = false>
-int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
+int choose_tiles(adloco_ctx* ctx, Product& p, cudaStream_t st) {
+    lay_out<KIND>(p);
     constexpr int SHARE = KIND == GATED ? 2 : 1;      // of a tile's columns a projection's are
     const bool bytes = p.side[OUT1].form == kBytes;   // 8-bit outputs: a block of 128 columns in one tile
     const bool pairs = cta_pairs_possible(ctx);
@@ -1158,27 +1169,14 @@ int choose_tiles(adloco_ctx* ctx, const Product& p, cudaStream_t st) {
         return clocks(128, 256, sms, a_rows * 128 + 32768, 4) < pair256 ? launch_tiles<KIND, false, 256, SUM, IN8>(ctx, p, st)
                                                                         : launch_tiles<KIND, true, 256, SUM, IN8>(ctx, p, st);
     } else {
-        if constexpr (KIND == GATED) {                // as below, with 64 columns of each projection
-            int64_t best = least;
-            int split = 1;
-            const int64_t tiles = ((p.M + 127) / 128) * ((p.N + 63) / 64);
-            for (int s = 2; pairs && s <= 2 && tiles * s <= sms && kb >= 4 * s; s *= 2) {
-                const int64_t t = (kb + s - 1) / s * ((a_rows * 128 + 16384) / 64) + 2048 + s * 512;
-                if (t < best) { best = t; split = s; }
-            }
-            if (split > 1) return launch_tiles<KIND, false, 128, SUM, IN8>(ctx, p, st, split);
-        } else if constexpr (SUM != kSummed) {
+        if constexpr (KIND != GATED && SUM != kSummed) {
             if (!bytes) {
-                // tiles of 64 columns, and a part of K for each of two or four CTAs where a cluster of them finds room: the join
-                // takes as long as two stages a part
-                int64_t best = clocks(128, 64, sms, a_rows * 128 + 8192, 1);
-                int split = 1;
-                const int64_t tiles = ((p.M + 127) / 128) * ((p.N + 63) / 64);
-                for (int s = 2; pairs && s <= 4 && tiles * s <= sms && kb >= 8 * s; s *= 2) {
-                    const int64_t t = (kb + s - 1) / s * ((a_rows * 128 + 8192) / 64) + 1024 + s * 1024;
-                    if (t < best) { best = t; split = s; }
-                }
-                if (best < least) return launch_tiles<KIND, false, 64, SUM, IN8>(ctx, p, st, split);
+                // tiles of 64 columns, and half of K for each of two CTAs where all clusters run at once, there is work for both, and their
+                // join leaves the ring two stages beside the boxes: the join takes as long as four stages
+                const int64_t alone = clocks(128, 64, sms, a_rows * 128 + 8192, 1), tiles = ((p.M + 127) / 128) * ((p.N + 63) / 64);
+                const bool split = pairs && tiles * 2 <= sms && kb >= 16 && stages_of<false, 64>(p, 2) >= 2;
+                const int64_t both = split ? (kb + 1) / 2 * ((a_rows * 128 + 8192) / 64) + 3 * 1024 : never;
+                if (std::min(alone, both) < least) return launch_tiles<KIND, false, 64, SUM, IN8>(ctx, p, st, both < alone ? 2 : 1);
             }
         }
         if constexpr (SUM != kSummed)
