@@ -144,8 +144,8 @@ def test_gated_linear(ctx, shape, pair, columns, act, keep):
 
 @pytest.mark.parametrize("act,form,again", [("silu", "bf16", True), ("silu", "bytes", True), ("gelu", "bytes", True), ("gelu_tanh", "bf16", False), ("gelu", "bf16", True),
                                             ("none", "bytes", False), ("relu", "bf16", True)])
-@pytest.mark.parametrize("shape", [GATED_PAIRS, GATED_HALVES])
-def test_gated_linear_backward(ctx, shape, act, form, again):
+@pytest.mark.parametrize("shape,pair,columns", [(GATED_PAIRS, True, 256), (GATED_HALVES, False, 64), (GATED_SINGLE, False, 128)])
+def test_gated_linear_backward(ctx, shape, pair, columns, act, form, again):
     M, d, f = shape
     dy, w = rows(1, M, d, std=0.1), rows(2, d, f, std=f ** -0.5)
     err = (d + 2) * 2.0 ** -23 * (np.abs(np64(dy)) @ np.abs(np64(w)))
@@ -162,7 +162,7 @@ def test_gated_linear_backward(ctx, shape, act, form, again):
         gate, up = (widened(q, s, M, f) for q, s in both)
     outs = [hole(M, f, pad=k) for k in range(3)]
     ran(lambda: ctx.gated_linear_backward(dy, w, *src, outs[0][:M, :f], outs[1][:M, :f], activation=act, a=outs[2][:M, :f] if again else None, **given),
-        "gated_backward", *((True, 256) if shape == GATED_PAIRS else (False, 64)), PLAIN, form == "bytes")
+        "gated_backward", pair, columns, PLAIN, form == "bytes")
     dg_ref, du_ref, a_ref = L.gated_linear_backward(np64(dy), np64(w), gate, up, act)
     h, fine = np.abs(L.act(gate, act)[0]), 2.0 ** -19 * (1 + np.abs(gate))
     close(outs[0][:M, :f], dg_ref, rounding(BF) * np.abs(dg_ref) + np.abs(up) * (1.2 * err + fine * np.abs(da)), "d_gate")

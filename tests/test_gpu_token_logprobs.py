@@ -73,6 +73,8 @@ def check(o, l, t, top):
 
 
 # a warp a row (to 512), 128 threads (to 4096), a block, and a cluster (few rows from 16384 on)
+# (as an earlier rule had it: now a warp a row to 512, a block of 256 threads, and a cluster; test_gpu_token_logprobs_forms.py names the
+# kernel of each case and has the many rows that take a warp each up to 12288)
 @pytest.mark.parametrize("V", [1, 2, 7, 8, 31, 100, 257, 512, 513, 1000, 4095, 4096, 4097, 9999, 16383, 16384, 50257, 131072])
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_logprobs(ctx, V, dtype):
