@@ -734,7 +734,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                 const uint32_t s1 = scale_byte(__float_as_uint(m1)), s2 = scale_byte(__float_as_uint(m2));
                 inv1 = inv_scale(s1);
                 inv2 = inv_scale(s2);
-                if (first == block && row < a.M) {
+                if (first == block && row < a.M && valid > 0) {        // (a tile's second block may lie beyond the matrix)
                     a.side[OUT1].scale[(int64_t)row * a.side[OUT1].scale_pitch + (col0 >> 7)] = (uint8_t)s1;
                     if (TWO) a.side[OUT2].scale[(int64_t)row * a.side[OUT2].scale_pitch + (col0 >> 7)] = (uint8_t)s2;
                 }

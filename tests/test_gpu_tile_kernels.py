@@ -36,20 +36,21 @@ def ran(call, kind, pair, columns, sums, in8, blocks=None):
 
 
 # Of M x N outputs and K terms: pairs of CTAs with 256 x 256 (ragged in every direction), pairs with 256 x 128, single CTAs with 128 x 128,
-# with 128 x 64 and K shared by two of them, and with 128 x 64 alone
-PAIRS, HALVES, SOLO, SHARED, SINGLE = (2300, 2001, 1100), (1665, 777, 1001), (100, 9601, 1000), (300, 401, 2100), (300, 401, 200)
+# with 128 x 64 and K shared by two of them, and with 128 x 64 alone; NARROW ends in the first half of a tile
+PAIRS, NARROW, HALVES, SOLO, SHARED, SINGLE = (2300, 2001, 1100), (2300, 1900, 1100), (1665, 777, 1001), (100, 9601, 1000), (300, 401, 2100), (300, 401, 200)
 BLOCKS = {SHARED: 42, SINGLE: 21}
 
 
 def expected(shape, dtype, to8):
     """(pair, columns) of a linear call; 256 columns are not for sums that go to 8 bits beside a bf16 output."""
-    if shape == PAIRS:
+    if shape in (PAIRS, NARROW):
         return (True, 128) if to8 and dtype == BF else (True, 256)
     return {HALVES: (True, 128), SOLO: (False, 128), SHARED: (False, 64), SINGLE: (False, 64)}[shape]
 
 
 LINEAR = [(PAIRS, BF, "gelu", True, 0, "bf16"), (PAIRS, BF, "silu", False, 1, None), (PAIRS, F32, "gelu_tanh", True, 3, "bf16"), (PAIRS, F32, "relu", True, 0, "bytes"),
           (PAIRS, BF, "gelu", True, 0, "bytes"), (PAIRS, BF, "none", True, 8, None), (PAIRS, F32, "none", False, 1, None),
+          (NARROW, F32, "gelu", True, 0, "bytes"), (NARROW, BF, "gelu", True, 0, "bytes"),
           (SHARED, BF, "gelu", True, 0, "bf16"), (SHARED, BF, "silu", True, 1, None), (SHARED, F32, "gelu_tanh", True, 0, None), (SHARED, F32, "none", False, 3, "bf16"),
           (SINGLE, BF, "gelu", True, 0, "bf16"), (SINGLE, F32, "none", True, 0, None), (HALVES, BF, "gelu", True, 1, "bf16"), (HALVES, F32, "silu", True, 0, None),
           (HALVES, F32, "silu", False, 0, "bytes"), (HALVES, BF, "none", False, 0, "bytes"), (SOLO, BF, "relu", True, 0, "bf16"), (SOLO, F32, "gelu_tanh", True, 0, "bytes"),
@@ -111,13 +112,13 @@ def test_linear_backward(ctx, shape, dtype, act, kept, again, res_pad):
         untouched(a, M, K)
 
 
-GATED_PAIRS = (2300, 1100, 2001)                             # M, d, f
+GATED_PAIRS, GATED_NARROW = (2300, 1100, 2001), (2300, 1100, 1940)      # M, d, f
 GATED_HALVES, GATED_SINGLE = (300, 2100, 401), (100, 1280, 9601)      # the latter: more tiles than pairs of SMs
 
 
 @pytest.mark.parametrize("shape,pair,columns,act,keep", [(GATED_PAIRS, True, 256, "silu", "bf16"), (GATED_PAIRS, True, 256, "gelu", None), (GATED_PAIRS, True, 256, "gelu_tanh", "bytes"),
                                                          (GATED_PAIRS, True, 256, "silu", "bytes"), (GATED_HALVES, True, 128, "silu", "bf16"), (GATED_HALVES, True, 128, "gelu", None),
-                                                         (GATED_HALVES, True, 256, "silu", "bytes"), (GATED_SINGLE, False, 256, "gelu", "bytes"), (GATED_SINGLE, False, 128, "silu", "bf16")])
+                                                         (GATED_HALVES, True, 256, "silu", "bytes"), (GATED_NARROW, True, 256, "gelu", "bytes"), (GATED_SINGLE, False, 256, "gelu", "bytes"), (GATED_SINGLE, False, 128, "silu", "bf16")])
 def test_gated_linear(ctx, shape, pair, columns, act, keep):
     M, d, f = shape
     x, wg, wu = rows(1, M, d), rows(2, f, d, std=d ** -0.5), rows(3, f, d, std=d ** -0.5, pad=16)
