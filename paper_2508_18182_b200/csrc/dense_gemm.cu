@@ -129,9 +129,9 @@ __device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_GELU_TANH>, F2 z, F2& a) {
     return fma2(mul2(mul2(near, h), fma2(h, both(-1.f), both(1.f))), fma2(mul2(near, near), both(kTanhSlope * 0.134145f), both(kTanhSlope)), h);
 }
 __device__ __forceinline__ F2 slope(Act<ADLOCO_ACT_SILU>, F2 z, F2& a) {
-    const F2 low = no_less(z, -kFar), near = no_more(low, kFar), h = logistic(near);
-    a = mul2(low, h);
-    return fma2(mul2(near, h), fma2(h, both(-1.f), both(1.f)), h);
+    const F2 h = logistic(z);
+    a = mul2(no_less(z, -kFar), h);
+    return fma2(no_more(a, kFar), fma2(h, both(-1.f), both(1.f)), h);
 }
 // f with the activation as a type: one branch for all that it does
 template <typename F>
