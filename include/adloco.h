@@ -548,7 +548,7 @@ int adloco_blockscale_dequantize(adloco_ctx* ctx, adloco_dtype dtype, int64_t ro
 typedef enum {
     ADLOCO_ACT_NONE = 0,
     ADLOCO_ACT_RELU = 1,
-    ADLOCO_ACT_GELU = 2,        /* z (1 + erf(z / sqrt 2)) / 2 */
+    ADLOCO_ACT_GELU = 2,        /* z (1 + erf(z / sqrt 2)) / 2, to 2e-7 */
     ADLOCO_ACT_GELU_TANH = 3,   /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
     ADLOCO_ACT_SILU = 4         /* z / (1 + exp(-z)) */
 } adloco_activation;
@@ -566,7 +566,8 @@ typedef struct {
 /* z = x w^T + bias;  y = residual + act(z)
  *   x [M, K], w [N, K] dev bf16;  bias dev [N] float, may be NULL
  *   residual, y  dev [M, N] in out_dtype;  residual may be NULL
- *   z            kept for adloco_linear_backward of the next layer, [M, N]; optional */
+ *   z            kept for adloco_linear_backward of the next layer, [M, N]; optional.  (With an activation and a residual together the
+ *                next layer's input is their sum, whose way back these calls do not have.) */
 typedef struct {
     int64_t M, N, K;
     const void* x;

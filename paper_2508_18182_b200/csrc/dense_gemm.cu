@@ -311,10 +311,10 @@ __device__ __forceinline__ float larger(float m, float v) {
 // sums into the first one's shared memory, which adds them to its own and goes on alone.
 // The epilogue's eight warps each own 32 rows and half the columns, in chunks of 32: the operands of the next chunk arrive by
 // TMA while this one is computed, the results leave by TMA.  IN8: what the forward pass kept is in 8 bits.
-// What bounds it: at long K the tensor pipe and the power cap (8192 x 4096 -> 4096: 169 us, 1.63 PFLOP/s); at K = 768 a tile's MMAs take
+// What bounds it: at long K the tensor pipe and the power cap (8192 x 4096 -> 4096: 176 us, 1.56 PFLOP/s); at K = 768 a tile's MMAs take
 // 6.1 thousand clocks and its operands as many of L2's, and the epilogue's matrices go through the same L2 and copy engine
-// beside them: 32768 x 768 -> 2048 takes 75 us with one bf16 output, 103 with gelu and z kept, 143 on the way back through the gate with
-// five matrices (4.7 TB/s).  Sixteen epilogue warps, operands and results without TMA, and prefetches into L2 gained nothing or lost.
+// beside them: 32768 x 768 -> 2048 takes 75 us with one bf16 output, 105 with gelu and z kept, 151 on the way back through the gate with
+// five matrices (4.8 TB/s), as graph replays of some ms; in a long row of calls, at the power cap, 120 with gelu and z and 172 back through the gate.  Sixteen epilogue warps, operands and results without TMA, and prefetches into L2 gained nothing or lost.
 constexpr int DG_THREADS = 320, DG_EPI = 8;
 constexpr int DG_A_BYTES = 128 * 128;
 constexpr int DG_MAX_STAGES = 8;
