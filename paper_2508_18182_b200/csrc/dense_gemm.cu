@@ -374,9 +374,9 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
     auto acc_empty = [&](uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 2 + s); };
     auto in_bar = [&](uint32_t w, uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * w + s); };
     const uint32_t drain_bar = bars + 8u * (2 * DG_MAX_STAGES + 4 + 2 * DG_EPI), join_bar = drain_bar + 8u;
-    auto swap_bar = [&](uint32_t w) { return bars + 8u * (2 * DG_MAX_STAGES + 6 + 2 * DG_EPI + w); };
+    auto swap_bar = [&](uint32_t w, uint32_t s) { return bars + 8u * (2 * DG_MAX_STAGES + 6 + 2 * DG_EPI + 2 * w + s); };
     const uint32_t join = bars + DG_BAR_BYTES;                 // the other half's sums, or the maxima that warps tell one another
-    static_assert(8 * (2 * DG_MAX_STAGES + 6 + 3 * DG_EPI) <= 512, "barriers");
+    static_assert(8 * (2 * DG_MAX_STAGES + 6 + 4 * DG_EPI) <= 512, "barriers");
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
@@ -391,8 +391,7 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
         for (uint32_t s = 0; s < stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
         for (uint32_t s = 0; s < 2; ++s) { mbar_init(acc_full(s), 1); mbar_init(acc_empty(s), (PAIR ? 2 : 1) * DG_EPI); }
         for (uint32_t w = 0; w < DG_EPI; ++w) {
-            for (uint32_t s = 0; s < 2; ++s) mbar_init(in_bar(w, s), 1);
-            mbar_init(swap_bar(w), 1);
+            for (uint32_t s = 0; s < 2; ++s) { mbar_init(in_bar(w, s), 1); mbar_init(swap_bar(w, s), 1); }
         }
         mbar_init(drain_bar, 1);
         if (SPLIT) mbar_init(join_bar, DG_EPI + 1);
@@ -705,8 +704,8 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                     }
             }
             // the scales of what is kept in 8 bits.  A warp whose sums are half of the block's 128 columns tells the other warp of
-            // these rows their maxima: in one of two places in turn, since neither goes on to the next tile but one before the
-            // other has read this one's.
+            // these rows their maxima: through one of two places and barriers in turn, since a warp may be a tile ahead, but is not
+            // two before the other has been told of this one and has read it.
             float inv1 = 0.f, inv2 = 0.f;
             if (FORWARD && form1 == kBytes && row0 < a.M) {
                 float m1 = 0.f, m2 = 0.f;
@@ -719,11 +718,11 @@ __global__ void __launch_bounds__(DG_THREADS, 1) dense_tile_kernel(const __grid_
                             if constexpr (TWO) m2 = larger(larger(m2, sum2[i][e >> 2][e & 3].x), sum2[i][e >> 2][e & 3].y);
                         }
                     if constexpr (CHUNKS < 4) {
-                        const uint32_t place = (swaps & 1u) * 256u + (uint32_t)lane * 8u;
+                        const uint32_t turn = swaps & 1u, place = turn * 256u + (uint32_t)lane * 8u;
                         asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(join + w * 512u + place), "f"(m1), "f"(m2) : "memory");
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(swap_bar(w ^ 4u));
-                        if (!wait_warp<false>(swap_bar(w), swaps & 1u, abortp, a.wait_ns)) { ok = false; break; }
+                        if (lane == 0) mbar_arrive(swap_bar(w ^ 4u, turn));
+                        if (!wait_warp<false>(swap_bar(w, turn), (swaps >> 1) & 1u, abortp, a.wait_ns)) { ok = false; break; }
                         ++swaps;
                         float o1, o2;
                         asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(o1), "=f"(o2) : "r"(join + (w ^ 4u) * 512u + place) : "memory");
